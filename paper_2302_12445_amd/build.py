@@ -1,4 +1,4 @@
-"""Builds libdear.so (host planner + gfx950 kernels) in-tree with hipcc."""
+"""Builds libdear.so (host planner + gfx950 kernels) and libdear_ops.so (training operators) in-tree with hipcc."""
 from __future__ import annotations
 
 import os
@@ -14,6 +14,10 @@ HEADERS = [os.path.join(CSRC, "dear_internal.h"), os.path.join(ROOT, "include", 
 PROBE_LIB = os.path.join(PKG, "libdear_probe.so")
 PROBE_SOURCES = [os.path.join(CSRC, "hbm_probe.hip")]
 PROBE_HEADERS = [os.path.join(ROOT, "include", "dear_probe.h")]
+# training operators, a library of their own (include/dear_ops.h)
+OPS_LIB = os.path.join(PKG, "libdear_ops.so")
+OPS_SOURCES = [os.path.join(CSRC, f) for f in ("attention.hip", "norm.hip", "weight_grad.hip")]
+OPS_HEADERS = [os.path.join(CSRC, "ops_common.h"), os.path.join(ROOT, "include", "dear_ops.h"), os.path.join(ROOT, "include", "dear.h")]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",
@@ -59,6 +63,14 @@ def build_probe(force: bool = True) -> str:
     return _compile(PROBE_LIB, PROBE_SOURCES)
 
 
+def build_ops(force: bool = True) -> str:
+    """Compile libdear_ops.so (attention, norm, checkpoints)."""
+    if not force and not _stale(OPS_LIB, OPS_SOURCES + OPS_HEADERS):
+        return OPS_LIB
+    return _compile(OPS_LIB, OPS_SOURCES)
+
+
 if __name__ == "__main__":
     print(build())
     print(build_probe())
+    print(build_ops())

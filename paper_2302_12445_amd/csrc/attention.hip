@@ -1,0 +1,486 @@
+// Attention and its backward pass (formulas: dear_ops.h).
+#include <cmath>
+
+#include "ops_common.h"
+
+#pragma clang fp contract(fast)
+
+namespace {
+
+using namespace dear_ops;
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int THREADS = 256, WAVES = THREADS / 64;
+constexpr int BLOCK = 32 * WAVES;  // rows that a workgroup owns: 32 for each wave
+constexpr int STEP = 64;           // rows of the other sequence that it takes at a time
+
+struct heads {
+    char *data;
+    int64_t batch, token, head;  // strides in bytes
+};
+
+struct params {
+    int32_t q_heads, kv_heads, head_dim, causal;
+    int32_t q_len, kv_len, tiles;
+    float scale;
+    const int32_t *q_lens, *kv_lens;
+    heads q, k, v, out, dout, dq, dk, dv;
+    float *lse, *delta;
+};
+
+__device__ __forceinline__ char *at(const heads &t, int b, int h) {
+    return t.data + b * t.batch + h * t.head;
+}
+
+__device__ __forceinline__ int length(const int32_t *lens, int b, int most) {
+    return lens ? min(max(lens[b], 0), most) : most;
+}
+
+// STEP rows of W values, row by row in pieces of sixteen bytes, on their way from memory to LDS: rows at or beyond
+// `valid` and values at or beyond head_dim are zeros, whatever stands there.
+template <typename T, int W> struct stage {
+    static constexpr int PER_ROW = W * sizeof(T) / 16, N = STEP * PER_ROW / THREADS;
+    u32x4 piece[N];
+
+    __device__ __forceinline__ void load(const char *p, int64_t token, int row0, int valid, int head_dim) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = threadIdx.x + i * THREADS, row = row0 + c / PER_ROW, byte = c % PER_ROW * 16;
+            piece[i] = u32x4{0, 0, 0, 0};
+            if (row < valid && byte < head_dim * (int)sizeof(T)) piece[i] = *(const u32x4 *)(p + row * token + byte);
+        }
+    }
+    __device__ __forceinline__ void store(DEAR_LDS T *s) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int c = threadIdx.x + i * THREADS;
+            *(DEAR_LDS u32x4 *)(s + c / PER_ROW * tile<T, W>::stride + c % PER_ROW * (16 / sizeof(T))) = piece[i];
+        }
+    }
+};
+
+// The 32 rows of one wave as fragments, from memory.
+template <typename T, int W>
+__device__ __forceinline__ void load_rows(frag<T> *f, const char *p, int64_t token, int row, int valid, int head_dim, int half) {
+#pragma unroll
+    for (int kk = 0; kk < W / 16; ++kk) {
+        const int d = 16 * kk + 8 * half;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) f[kk][t] = (T)0.f;
+        if (row < valid && d < head_dim) f[kk] = *(const frag<T> *)(p + row * token + d * sizeof(T));
+    }
+}
+
+// Rows 32 db + row_of(r, half) of column `token` of a transposed result, as rows of memory.
+template <typename T, int W>
+__device__ __forceinline__ void store_row(char *p, const f32x16 *x, float factor, int head_dim, int half) {
+#pragma unroll
+    for (int db = 0; db < W / 32; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int d = 32 * db + 8 * g + 4 * half;
+            if (d < head_dim) {
+                typedef T vec __attribute__((ext_vector_type(4)));
+                vec o;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) o[t] = (T)(x[db][4 * g + t] * factor);
+                *(vec *)(p + d * sizeof(T)) = o;
+            }
+        }
+}
+
+// Workgroup -> (batch, head, tile).
+__device__ __forceinline__ void place(const params &a, int heads, int &b, int &h, int &t) {
+    const unsigned id = blockIdx.x, pair = id / (unsigned)a.tiles;
+    t = id % (unsigned)a.tiles;
+    b = pair / (unsigned)heads;
+    h = pair % (unsigned)heads;
+}
+
+// ------------------------------------------------------------------------------------ forward
+template <typename T, int W> __global__ __launch_bounds__(THREADS) void attention_kernel(params a) {
+    __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
+    DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
+    int b, h, t;
+    place(a, a.q_heads, b, h, t);
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
+    const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
+    const int kvh = h / (a.q_heads / a.kv_heads);
+    const char *qp = at(a.q, b, h), *kp = at(a.k, b, kvh), *vp = at(a.v, b, kvh);
+    const int i = t * BLOCK + wave * 32 + (lane & 31);  // this lane's query
+    // keys 0 .. last are visible to it
+    const int last = i < nq ? (a.causal ? min(nk - 1, i + nk - nq) : nk - 1) : -1;
+    const int block_end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    // the same of the whole wave: the fewest keys of a query, and the most
+    const int wave_first = t * BLOCK + wave * 32;
+    const int wave_least = wave_first + 31 < nq ? (a.causal ? min(nk - 1, wave_first + nk - nq) : nk - 1) : -1;
+
+    frag<T> q[W / 16];
+    load_rows<T, W>(q, qp, a.q.token, i, nq, a.head_dim, half);
+    f32x16 o[W / 32] = {};
+    float top = -INFINITY, sum = 0.f;
+    const float c = a.scale * LOG2E;
+
+    stage<T, W> kst, vst;
+    if (block_end > 0) {
+        kst.load(kp, a.k.token, 0, nk, a.head_dim);
+        vst.load(vp, a.v.token, 0, nk, a.head_dim);
+    }
+    for (int j0 = 0; j0 < block_end; j0 += STEP) {
+        __syncthreads();
+        kst.store(ks);
+        vst.store(vs);
+        __syncthreads();
+        if (j0 + STEP < block_end) {
+            kst.load(kp, a.k.token, j0 + STEP, nk, a.head_dim);
+            vst.load(vp, a.v.token, j0 + STEP, nk, a.head_dim);
+        }
+        f32x16 s[STEP / 32] = {};
+#pragma unroll
+        for (int kb = 0; kb < STEP / 32; ++kb)
+#pragma unroll
+            for (int kk = 0; kk < W / 16; ++kk) s[kb] = mma(straight<W>(ks, 32 * kb, kk, lane), q[kk], s[kb]);
+        if (j0 + STEP - 1 > wave_least) {
+#pragma unroll
+            for (int kb = 0; kb < STEP / 32; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kb][r] = j0 + 32 * kb + row_of(r, half) <= last ? s[kb][r] : -INFINITY;
+        }
+        float most = top;
+#pragma unroll
+        for (int kb = 0; kb < STEP / 32; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) most = fmaxf(most, s[kb][r]);
+        most = halves_max(most);
+        const float base = most == -INFINITY ? 0.f : most * c;
+        const float keep = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top * c - base);
+        top = most;
+        sum *= keep;
+#pragma unroll
+        for (int kb = 0; kb < STEP / 32; ++kb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[kb][r] = __builtin_amdgcn_exp2f(s[kb][r] * c - base);
+                sum += s[kb][r];
+            }
+#pragma unroll
+        for (int db = 0; db < W / 32; ++db) o[db] *= keep;
+#pragma unroll
+        for (int kb = 0; kb < STEP / 32; ++kb)
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                float x[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x[u] = s[kb][8 * st + u];
+                const frag<T> p = to_frag<T>(x);
+#pragma unroll
+                for (int db = 0; db < W / 32; ++db)
+                    o[db] = mma(transposed<W>(vs, 32 * kb + 16 * st, 32 * db, lane), p, o[db]);
+            }
+    }
+    if (i >= a.q_len) return;
+    sum = halves_sum(sum);
+    const bool none = top == -INFINITY && sum == 0.f;
+    store_row<T, W>(at(a.out, b, h) + i * a.out.token, o, none ? 0.f : 1.f / sum, a.head_dim, half);
+    if (half == 0)
+        a.lse[((int64_t)b * a.q_heads + h) * a.q_len + i] = none ? -INFINITY : (top * c + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
+// ------------------------------------------------------------------------------------ backward: queries
+// dq of 32 queries a wave, over all keys.  As in the forward pass the results of the first products are taken
+// transposed, a query to a lane, so that lse and delta are one value a lane.  It also writes delta for the other kernel.
+template <typename T, int W> __global__ __launch_bounds__(THREADS) void attention_dq_kernel(params a) {
+    __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
+    DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
+    int b, h, t;
+    place(a, a.q_heads, b, h, t);
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
+    const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
+    const int kvh = h / (a.q_heads / a.kv_heads);
+    const char *kp = at(a.k, b, kvh), *vp = at(a.v, b, kvh);
+    const int i = t * BLOCK + wave * 32 + (lane & 31);
+    const int last = i < nq ? (a.causal ? min(nk - 1, i + nk - nq) : nk - 1) : -1;
+    const int block_end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    const int wave_first = t * BLOCK + wave * 32;
+    const int wave_least = wave_first + 31 < nq ? (a.causal ? min(nk - 1, wave_first + nk - nq) : nk - 1) : -1;
+
+    frag<T> q[W / 16], g[W / 16];
+    load_rows<T, W>(q, at(a.q, b, h), a.q.token, i, nq, a.head_dim, half);
+    load_rows<T, W>(g, at(a.dout, b, h), a.dout.token, i, nq, a.head_dim, half);
+    const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_len + i;
+    float delta = 0.f;
+    {
+        frag<T> out[W / 16];
+        load_rows<T, W>(out, at(a.out, b, h), a.out.token, i, nq, a.head_dim, half);
+#pragma unroll
+        for (int kk = 0; kk < W / 16; ++kk)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) delta += (float)g[kk][u] * (float)out[kk][u];
+    }
+    delta = halves_sum(delta);
+    if (half == 0 && i < a.q_len) a.delta[row] = delta;
+    const float z = i < nq ? a.lse[row] : -INFINITY;
+    const float base = z == -INFINITY ? 0.f : z * LOG2E, c = a.scale * LOG2E;
+
+    f32x16 dq[W / 32] = {};
+    stage<T, W> kst, vst;
+    if (block_end > 0) {
+        kst.load(kp, a.k.token, 0, nk, a.head_dim);
+        vst.load(vp, a.v.token, 0, nk, a.head_dim);
+    }
+    for (int j0 = 0; j0 < block_end; j0 += STEP) {
+        __syncthreads();
+        kst.store(ks);
+        vst.store(vs);
+        __syncthreads();
+        if (j0 + STEP < block_end) {
+            kst.load(kp, a.k.token, j0 + STEP, nk, a.head_dim);
+            vst.load(vp, a.v.token, j0 + STEP, nk, a.head_dim);
+        }
+#pragma unroll
+        for (int kb = 0; kb < STEP / 32; ++kb) {
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int kk = 0; kk < W / 16; ++kk) {
+                s = mma(straight<W>(ks, 32 * kb, kk, lane), q[kk], s);
+                dp = mma(straight<W>(vs, 32 * kb, kk, lane), g[kk], dp);
+            }
+            const bool whole = j0 + 32 * kb + 31 <= wave_least;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const float p = __builtin_amdgcn_exp2f(s[r] * c - base);
+                s[r] = whole || j0 + 32 * kb + row_of(r, half) <= last ? p * (dp[r] - delta) : 0.f;
+            }
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                float x[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x[u] = s[8 * st + u];
+                const frag<T> ds = to_frag<T>(x);
+#pragma unroll
+                for (int db = 0; db < W / 32; ++db)
+                    dq[db] = mma(transposed<W>(ks, 32 * kb + 16 * st, 32 * db, lane), ds, dq[db]);
+            }
+        }
+    }
+    if (i < a.q_len) store_row<T, W>(at(a.dq, b, h) + i * a.dq.token, dq, a.scale, a.head_dim, half);
+}
+
+// ------------------------------------------------------------------------------------ backward: keys and values
+// dk and dv of 32 keys a wave, over the queries of all heads that share them: one workgroup adds them all up, in order.
+template <typename T, int W> __global__ __launch_bounds__(THREADS) void attention_dkv_kernel(params a) {
+    __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
+    __shared__ __attribute__((aligned(16))) float rows[2][STEP];  // lse * log2(e) and delta of the queries
+    DEAR_LDS T *qs = (DEAR_LDS T *)lds, *gs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
+    int b, kvh, t;
+    place(a, a.kv_heads, b, kvh, t);
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
+    const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
+    const int group = a.q_heads / a.kv_heads;
+    const int wave_first = t * BLOCK + wave * 32, j = wave_first + (lane & 31);  // this lane's key
+    // queries first .. nq - 1 see it
+    const int first = j < nk ? (a.causal ? max(0, j - nk + nq) : 0) : nq;
+    const int wave_last = wave_first + 31 < nk ? (a.causal ? max(0, wave_first + 31 - nk + nq) : 0) : nq;
+    const int begin = t * BLOCK >= nk ? nq : a.causal ? max(0, t * BLOCK - nk + nq) / STEP * STEP : 0;
+
+    frag<T> k[W / 16], v[W / 16];
+    load_rows<T, W>(k, at(a.k, b, kvh), a.k.token, j, nk, a.head_dim, half);
+    load_rows<T, W>(v, at(a.v, b, kvh), a.v.token, j, nk, a.head_dim, half);
+    f32x16 dk[W / 32] = {}, dv[W / 32] = {};
+    const float c = a.scale * LOG2E;
+
+    for (int h = kvh * group; h < (kvh + 1) * group; ++h) {
+        const char *qp = at(a.q, b, h), *gp = at(a.dout, b, h);
+        const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_len;
+        stage<T, W> qst, gst;
+        float z = 0.f;
+        // one value a thread: the first STEP threads take lse, the next ones delta
+        auto load_z = [&](int i0) {
+            const int i = i0 + threadIdx.x % STEP;
+            if (threadIdx.x < STEP) {
+                z = i < nq ? a.lse[row + i] * LOG2E : INFINITY;
+                if (z == -INFINITY) z = INFINITY;  // no key is seen: all probabilities are 0
+            } else if (threadIdx.x < 2 * STEP) {
+                z = i < nq ? a.delta[row + i] : 0.f;
+            }
+        };
+        if (begin < nq) {
+            qst.load(qp, a.q.token, begin, nq, a.head_dim);
+            gst.load(gp, a.dout.token, begin, nq, a.head_dim);
+            load_z(begin);
+        }
+        for (int i0 = begin; i0 < nq; i0 += STEP) {
+            __syncthreads();
+            qst.store(qs);
+            gst.store(gs);
+            if (threadIdx.x < 2 * STEP) rows[threadIdx.x / STEP][threadIdx.x % STEP] = z;
+            __syncthreads();
+            if (i0 + STEP < nq) {
+                qst.load(qp, a.q.token, i0 + STEP, nq, a.head_dim);
+                gst.load(gp, a.dout.token, i0 + STEP, nq, a.head_dim);
+                load_z(i0 + STEP);
+            }
+#pragma unroll
+            for (int qb = 0; qb < STEP / 32; ++qb) {
+                f32x16 s = {}, dp = {};
+#pragma unroll
+                for (int kk = 0; kk < W / 16; ++kk) {
+                    s = mma(straight<W>(qs, 32 * qb, kk, lane), k[kk], s);
+                    dp = mma(straight<W>(gs, 32 * qb, kk, lane), v[kk], dp);
+                }
+                const bool whole = i0 + 32 * qb >= wave_last && i0 + 32 * qb + 31 < nq;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int n = 32 * qb + row_of(r, half);
+                    const float p = __builtin_amdgcn_exp2f(s[r] * c - rows[0][n]);
+                    s[r] = whole || (i0 + n >= first && i0 + n < nq) ? p : 0.f;
+                    dp[r] = s[r] * (dp[r] - rows[1][n]);
+                }
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    float x[8], y[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) x[u] = s[8 * st + u], y[u] = dp[8 * st + u];
+                    const frag<T> p = to_frag<T>(x), ds = to_frag<T>(y);
+#pragma unroll
+                    for (int db = 0; db < W / 32; ++db) {
+                        dv[db] = mma(transposed<W>(gs, 32 * qb + 16 * st, 32 * db, lane), p, dv[db]);
+                        dk[db] = mma(transposed<W>(qs, 32 * qb + 16 * st, 32 * db, lane), ds, dk[db]);
+                    }
+                }
+            }
+        }
+    }
+    if (j >= a.kv_len) return;
+    store_row<T, W>(at(a.dk, b, kvh) + j * a.dk.token, dk, a.scale, a.head_dim, half);
+    store_row<T, W>(at(a.dv, b, kvh) + j * a.dv.token, dv, 1.f, a.head_dim, half);
+}
+
+// ------------------------------------------------------------------------------------ host
+constexpr int64_t MAX_LEN = 1 << 30;
+
+int check_sizes(const dear_attention_t *p) {
+    if (!p) return DEAR_EINVAL;
+    if (p->batch < 0 || p->q_heads < 1 || p->kv_heads < 1 || p->q_heads % p->kv_heads) return DEAR_EINVAL;
+    if (p->head_dim < 8 || p->head_dim > 128 || p->head_dim % 8) return DEAR_EINVAL;
+    if (p->q_len < 0 || p->q_len > MAX_LEN || p->kv_len < 0 || p->kv_len > MAX_LEN) return DEAR_EINVAL;
+    if (p->dtype != DEAR_F32 && p->dtype != DEAR_BF16) return DEAR_EINVAL;
+    if (p->causal != 0 && p->causal != 1) return DEAR_EINVAL;
+    if (!(p->scale > 0.f) || !std::isfinite(p->scale)) return DEAR_EINVAL;
+    return DEAR_OK;
+}
+
+// Whether a tensor of n tokens is there, and aligned; what is written has a place of its own for every element.
+int check_heads(const dear_heads_t &t, const dear_attention_t *p, int64_t n, bool written) {
+    if (p->batch == 0 || n == 0) return DEAR_OK;
+    if (!t.data) return DEAR_EINVAL;
+    const int64_t g = p->dtype == DEAR_BF16 ? 2 : 4;
+    if (!aligned(t.data, 16) || t.batch_stride * g % 16 || t.token_stride * g % 16 || t.head_stride * g % 16) return DEAR_EALIGN;
+    if (t.batch_stride < 0 || t.token_stride < 0 || t.head_stride < 0) return DEAR_EINVAL;
+    if (written) {
+        const int64_t heads = &t == &p->dk || &t == &p->dv ? p->kv_heads : p->q_heads;
+        if ((n > 1 && t.token_stride < p->head_dim) || (heads > 1 && t.head_stride < p->head_dim) ||
+            (p->batch > 1 && t.batch_stride < p->head_dim))
+            return DEAR_EINVAL;
+    }
+    return DEAR_OK;
+}
+
+params make(const dear_attention_t *p) {
+    const int64_t g = p->dtype == DEAR_BF16 ? 2 : 4;
+    auto t = [g](const dear_heads_t &x) {
+        return heads{(char *)x.data, x.batch_stride * g, x.token_stride * g, x.head_stride * g};
+    };
+    params a = {};
+    a.q_heads = p->q_heads, a.kv_heads = p->kv_heads, a.head_dim = p->head_dim, a.causal = p->causal;
+    a.q_len = (int32_t)p->q_len, a.kv_len = (int32_t)p->kv_len, a.scale = p->scale;
+    a.q_lens = p->q_lens, a.kv_lens = p->kv_lens;
+    a.q = t(p->q), a.k = t(p->k), a.v = t(p->v), a.out = t(p->out);
+    a.dout = t(p->dout), a.dq = t(p->dq), a.dk = t(p->dk), a.dv = t(p->dv);
+    a.lse = p->lse, a.delta = (float *)p->workspace;
+    return a;
+}
+
+bool too_big(int64_t heads, int64_t batch, int64_t tiles) {
+    return heads * batch > INT32_MAX || heads * batch * tiles > INT32_MAX;
+}
+
+#define DEAR_BY_TYPE(p, kernel, grid, a, stream)                                                          \
+    do {                                                                                                  \
+        if ((p)->dtype == DEAR_BF16 && (p)->head_dim <= 64) kernel<bf16, 64><<<grid, THREADS, 0, stream>>>(a); \
+        else if ((p)->dtype == DEAR_BF16) kernel<bf16, 128><<<grid, THREADS, 0, stream>>>(a);             \
+        else if ((p)->head_dim <= 64) kernel<float, 64><<<grid, THREADS, 0, stream>>>(a);                 \
+        else kernel<float, 128><<<grid, THREADS, 0, stream>>>(a);                                         \
+    } while (0)
+
+}  // namespace
+
+extern "C" {
+
+int dear_attention_workspace(const dear_attention_t *p, int64_t *bytes) {
+    if (!bytes) return DEAR_EINVAL;
+    if (int rc = check_sizes(p)) return rc;
+    *bytes = 0;
+    return DEAR_OK;
+}
+
+int dear_attention_backward_workspace(const dear_attention_t *p, int64_t *bytes) {
+    if (!bytes) return DEAR_EINVAL;
+    if (int rc = check_sizes(p)) return rc;
+    *bytes = p->q_len * p->batch * p->q_heads * 4;
+    return DEAR_OK;
+}
+
+int dear_attention(const dear_attention_t *p, void *hip_stream) {
+    if (int rc = check_sizes(p)) return rc;
+    if (int rc = check_heads(p->q, p, p->q_len, false)) return rc;
+    if (int rc = check_heads(p->k, p, p->kv_len, false)) return rc;
+    if (int rc = check_heads(p->v, p, p->kv_len, false)) return rc;
+    if (int rc = check_heads(p->out, p, p->q_len, true)) return rc;
+    if (p->batch == 0 || p->q_len == 0) return DEAR_OK;
+    if (!p->lse) return DEAR_EINVAL;
+    if (!aligned(p->lse, 4)) return DEAR_EALIGN;
+    params a = make(p);
+    a.tiles = (int32_t)ceil_div(p->q_len, BLOCK);
+    if (too_big(p->q_heads, p->batch, a.tiles)) return DEAR_ETOOBIG;
+    const unsigned grid = (unsigned)a.tiles * p->q_heads * p->batch;
+    DEAR_BY_TYPE(p, attention_kernel, grid, a, (hipStream_t)hip_stream);
+    return launch_status();
+}
+
+int dear_attention_backward(const dear_attention_t *p, void *hip_stream) {
+    if (int rc = check_sizes(p)) return rc;
+    for (const dear_heads_t *t : {&p->q, &p->out, &p->dout})
+        if (int rc = check_heads(*t, p, p->q_len, false)) return rc;
+    for (const dear_heads_t *t : {&p->k, &p->v})
+        if (int rc = check_heads(*t, p, p->kv_len, false)) return rc;
+    if (int rc = check_heads(p->dq, p, p->q_len, true)) return rc;
+    for (const dear_heads_t *t : {&p->dk, &p->dv})
+        if (int rc = check_heads(*t, p, p->kv_len, true)) return rc;
+    if (p->batch == 0 || (p->q_len == 0 && p->kv_len == 0)) return DEAR_OK;
+    int64_t need = 0;
+    (void)dear_attention_backward_workspace(p, &need);
+    if (need) {
+        if (!p->lse || !p->workspace) return DEAR_EINVAL;
+        if (!aligned(p->lse, 4) || !aligned(p->workspace, 256)) return DEAR_EALIGN;
+        if (p->workspace_bytes < need) return DEAR_ETOOBIG;
+    }
+    params a = make(p);
+    const int64_t q_tiles = ceil_div(p->q_len, BLOCK), kv_tiles = ceil_div(p->kv_len, BLOCK);
+    if (too_big(p->q_heads, p->batch, q_tiles) || too_big(p->kv_heads, p->batch, kv_tiles)) return DEAR_ETOOBIG;
+    if (q_tiles) {
+        a.tiles = (int32_t)q_tiles;
+        const unsigned grid = (unsigned)q_tiles * p->q_heads * p->batch;
+        DEAR_BY_TYPE(p, attention_dq_kernel, grid, a, (hipStream_t)hip_stream);
+        if (int rc = launch_status()) return rc;
+    }
+    if (kv_tiles) {
+        a.tiles = (int32_t)kv_tiles;
+        const unsigned grid = (unsigned)kv_tiles * p->kv_heads * p->batch;
+        DEAR_BY_TYPE(p, attention_dkv_kernel, grid, a, (hipStream_t)hip_stream);
+        if (int rc = launch_status()) return rc;
+    }
+    return DEAR_OK;
+}
+
+}  // extern "C"
