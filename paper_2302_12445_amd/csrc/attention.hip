@@ -14,6 +14,12 @@ constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int BLOCK = 32 * WAVES;  // rows that a workgroup owns: 32 for each wave
 constexpr int STEP = 64;           // rows of the other sequence that it takes at a time
 
+// Waves of a SIMD that the kernels are compiled for.  With two, one's products run beside the other's softmax; wide rows
+// of fp32, and wide dk and dv with their operands, take the registers of both.
+template <typename T, int W> constexpr int resident(bool dkv) {
+    return sizeof(T) == 2 ? (dkv && W == 128 ? 1 : 2) : (W == 128 || dkv ? 1 : 2);
+}
+
 struct heads {
     char *data;
     int64_t batch, token, head;  // strides in bytes
@@ -98,7 +104,7 @@ __device__ __forceinline__ void place(const params &a, int heads, int &b, int &h
 }
 
 // ------------------------------------------------------------------------------------ forward
-template <typename T, int W> __global__ __launch_bounds__(THREADS) void attention_kernel(params a) {
+template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(false))) void attention_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
     int b, h, t;
@@ -189,7 +195,7 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS) void attentio
 // ------------------------------------------------------------------------------------ backward: queries
 // dq of 32 queries a wave, over all keys.  As in the forward pass the results of the first products are taken
 // transposed, a query to a lane, so that lse and delta are one value a lane.  It also writes delta for the other kernel.
-template <typename T, int W> __global__ __launch_bounds__(THREADS) void attention_dq_kernel(params a) {
+template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(false))) void attention_dq_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
     int b, h, t;
@@ -268,7 +274,7 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS) void attentio
 
 // ------------------------------------------------------------------------------------ backward: keys and values
 // dk and dv of 32 keys a wave, over the queries of all heads that share them: one workgroup adds them all up, in order.
-template <typename T, int W> __global__ __launch_bounds__(THREADS) void attention_dkv_kernel(params a) {
+template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(true))) void attention_dkv_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     __shared__ __attribute__((aligned(16))) float rows[2][STEP];  // lse * log2(e) and delta of the queries
     DEAR_LDS T *qs = (DEAR_LDS T *)lds, *gs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));

@@ -109,8 +109,7 @@ __global__ __launch_bounds__(256) void decode_kernel(const int8_t *codes, const 
 // ------------------------------------------------------------------------------------ norm
 // Sum over the threads of a row: 64, or all of the workgroup's.
 template <int TPR> __device__ __forceinline__ float row_sum(float x) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
+    x = wave_sum(x);
     if (TPR > 64) {
         __shared__ float part[TPR / 64];
         __syncthreads();  // the sums of the call before have been read
@@ -234,16 +233,33 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_backward_kernel(const T *d
     }
 }
 
-// Sum of n rows of `part`, 64 columns a workgroup, a quarter of the rows a wave.
-__global__ __launch_bounds__(256) void column_sum_kernel(const float *part, int32_t n, int32_t cols, float *out) {
-    __shared__ float sums[4][64];
+// Sum of n rows of `part`, 64 columns a workgroup: each of 16 waves adds every sixteenth row, and the waves' sums are
+// added in order.
+constexpr int SUM_WAVES = 16;
+__global__ __launch_bounds__(64 * SUM_WAVES) void column_sum_kernel(const float *part, int32_t n, int32_t cols, float *out) {
+    __shared__ float sums[SUM_WAVES][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
     float s = 0.f;
-    if (col < cols)
-        for (int k = wave; k < n; k += 4) s += part[(int64_t)k * cols + col];
+    if (col < cols) {
+        constexpr int U = 8;  // loads in flight
+        int k = wave;
+        for (; k + (U - 1) * SUM_WAVES < n; k += U * SUM_WAVES) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = part[(int64_t)(k + u * SUM_WAVES) * cols + col];
+#pragma unroll
+            for (int u = 0; u < U; ++u) s += x[u];
+        }
+        for (; k < n; k += SUM_WAVES) s += part[(int64_t)k * cols + col];
+    }
     sums[wave][lane] = s;
     __syncthreads();
-    if (wave == 0 && col < cols) out[col] = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    if (wave == 0 && col < cols) {
+        s = 0.f;
+#pragma unroll
+        for (int w = 0; w < SUM_WAVES; ++w) s += sums[w][lane];
+        out[col] = s;
+    }
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -438,7 +454,7 @@ int dear_add_rms_norm_backward(const void *dy, int64_t dy_stride, const void *h,
                                                  (float *)workspace, groups, stream});
         if (int rc = launch_status()) return rc;
     }
-    column_sum_kernel<<<(unsigned)ceil_div(cols, 64), 256, 0, stream>>>((const float *)workspace, groups, (int32_t)cols, dweight);
+    column_sum_kernel<<<(unsigned)ceil_div(cols, 64), 64 * SUM_WAVES, 0, stream>>>((const float *)workspace, groups, (int32_t)cols, dweight);
     return launch_status();
 }
 

@@ -66,6 +66,21 @@ __device__ __forceinline__ float halves_sum(float x) {
     return __uint_as_float(w[0]) + __uint_as_float(w[1]);
 }
 
+
+// Sum over the wave, the same in all lanes: quads, eights and sixteens by moves within a row of sixteen lanes, then
+// across the rows.
+template <int CTRL> __device__ __forceinline__ float plus_moved(float x) {
+    return x + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float wave_sum(float x) {
+    x = plus_moved<0xB1>(x);   // quad_perm 1, 0, 3, 2
+    x = plus_moved<0x4E>(x);   // quad_perm 2, 3, 0, 1
+    x = plus_moved<0x141>(x);  // row_half_mirror
+    x = plus_moved<0x140>(x);  // row_mirror
+    auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return halves_sum(__uint_as_float(w[0]) + __uint_as_float(w[1]));
+}
+
 __device__ __forceinline__ int row_of(int r, int half) { return 8 * (r / 4) + 4 * half + r % 4; }
 
 // A tile of rows of W values in LDS.  Rows are padded so that the sixteen-byte pieces of eight rows, and the

@@ -103,6 +103,157 @@ template <typename T, bool VEC> __global__ __launch_bounds__(THREADS) void weigh
         }
 }
 
+// ------------------------------------------------------------------------------------ bf16, whole vectors
+// A workgroup owns 128 x 128 outputs and each of its four waves sums all of them over rows of its own, 32 of every 128:
+// a wave reads eight fragments for sixteen products, and the waves meet only at the end, to add their sums.
+constexpr int WROWS = 32;                            // rows of a wave's step
+constexpr int WSTEP = WROWS * (THREADS / 64);        // rows of a workgroup's step
+constexpr int WTILE = WROWS * tile<bf16, 128>::stride;  // elements of one operand's tile
+
+struct wave_step {
+    u32x4 y[8], x[4];
+    uint32_t e[4];
+};
+
+template <bool WHOLE>
+__device__ __forceinline__ void load_step(wave_step &w, const char *y, const int8_t *x, const uint8_t *e, uint32_t y_off, uint32_t x_off,
+                                          uint32_t e_off, uint32_t y_stride, uint32_t x_stride, uint32_t e_stride, int lane, int left) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = 4 * i + lane / 16;
+        w.y[i] = *(const u32x4 *)(y + (y_off + (uint32_t)(WHOLE ? row : min(row, left - 1)) * y_stride));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = 8 * i + lane / 8, r = WHOLE ? row : min(row, left - 1);
+        w.x[i] = *(const u32x4 *)(x + (x_off + (uint32_t)r * x_stride));
+        w.e[i] = e[e_off + (uint32_t)r * e_stride];
+        // rows beyond the last repeat it, times 0
+        if (!WHOLE && row >= left) w.e[i] = 0;
+    }
+}
+
+__device__ __forceinline__ void store_step(const wave_step &w, DEAR_LDS bf16 *ys, DEAR_LDS bf16 *xs, int lane) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        *(DEAR_LDS u32x4 *)(ys + (4 * i + lane / 16) * tile<bf16, 128>::stride + lane % 16 * 8) = w.y[i];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float step = __uint_as_float(w.e[i] << 23);
+        u32x4 q[2];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t c = w.x[i][k / 2];
+            const float lo = (float)((int)(c << (24 - 16 * (k % 2))) >> 24) * step;
+            const float hi = (float)((int)(c << (16 - 16 * (k % 2))) >> 24) * step;
+            // both are bf16 values: their upper halves
+            q[k / 4][k % 4] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+        }
+        DEAR_LDS bf16 *p = xs + (8 * i + lane / 8) * tile<bf16, 128>::stride + lane % 8 * 16;
+        *(DEAR_LDS u32x4 *)p = q[0];
+        *(DEAR_LDS u32x4 *)(p + 8) = q[1];
+    }
+}
+
+__device__ __forceinline__ void multiply_step(f32x16 (&acc)[4][4], const DEAR_LDS bf16 *ys, const DEAR_LDS bf16 *xs, int lane) {
+#pragma unroll
+    for (int s = 0; s < WROWS / 16; ++s) {
+        bf16x8 y[4], x[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            y[u] = transposed<128>(ys, 16 * s, 32 * u, lane);
+            x[u] = transposed<128>(xs, 16 * s, 32 * u, lane);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) acc[u][v] = mma(y[u], x[v], acc[u][v]);
+    }
+}
+
+__global__ __launch_bounds__(THREADS, 1) void weight_grad_wide_kernel(params a) {
+    // first two buffers of two tiles for each wave, then the waves' sums, two quarters at a time
+    __shared__ __attribute__((aligned(16))) char lds[4 * 4 * WTILE * sizeof(bf16)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned per_split = (unsigned)a.n_tiles * a.k_tiles, split = blockIdx.x / per_split, id = blockIdx.x % per_split;
+    const int n0 = (int)(id % a.n_tiles) * 128, k0 = (int)(id / a.n_tiles) * 128;
+    const int64_t begin = (int64_t)split * a.chunk + wave * WROWS, end = min(a.rows, (int64_t)(split + 1) * a.chunk);
+    DEAR_LDS bf16 *const buf = (DEAR_LDS bf16 *)lds + wave * 4 * WTILE;
+
+    f32x16 acc[4][4] = {};
+    // outputs beyond the last repeat the first: they are not stored
+    const uint32_t y_stride = (uint32_t)a.dy_stride * 2, x_stride = (uint32_t)a.padded, e_stride = (uint32_t)a.groups;
+    const int yc = n0 + lane % 16 * 8, xc = k0 + lane % 8 * 16;
+    const uint32_t y_off = (uint32_t)(yc < a.outs ? yc : 0) * 2, x_off = xc < a.padded ? xc : 0, e_off = x_off / GROUP;
+    const char *y = (const char *)a.dy + begin * a.dy_stride * 2;
+    const int8_t *x = a.codes + begin * a.padded;
+    const uint8_t *e = a.exponents + begin * a.groups;
+    const int64_t rows = end - begin, steps = rows > 0 ? (rows + WSTEP - 1) / WSTEP : 0;  // of this wave
+    const int last = (int)(rows - (steps - 1) * WSTEP);  // rows from the last step on
+    wave_step w;
+    // step t: its operands go to LDS while the products of the step before run, and come from memory one step earlier
+    auto load = [&](bool whole) {
+        if (whole) load_step<true>(w, y, x, e, y_off, x_off, e_off, y_stride, x_stride, e_stride, lane, 0);
+        else load_step<false>(w, y, x, e, y_off, x_off, e_off, y_stride, x_stride, e_stride, lane, last);
+        y += (int64_t)WSTEP * y_stride, x += (int64_t)WSTEP * x_stride, e += (int64_t)WSTEP * e_stride;
+    };
+    if (steps > 0) {
+        load(steps > 1);
+        store_step(w, buf, buf + WTILE, lane);
+        if (steps > 1) load(steps > 2);
+        int64_t t = 0;
+        DEAR_LDS bf16 *now = buf, *next = buf + 2 * WTILE;
+        for (; t + 3 < steps; ++t) {
+            multiply_step(acc, now, now + WTILE, lane);
+            store_step(w, next, next + WTILE, lane);
+            load(true);
+            DEAR_LDS bf16 *const other = now;
+            now = next, next = other;
+        }
+        for (; t < steps; ++t) {
+            multiply_step(acc, now, now + WTILE, lane);
+            if (t + 1 < steps) store_step(w, next, next + WTILE, lane);
+            if (t + 2 < steps) load(false);
+            DEAR_LDS bf16 *const other = now;
+            now = next, next = other;
+        }
+    }
+
+    float *out = a.out + (int64_t)split * a.outs * a.ins;
+    DEAR_LDS float *sums = (DEAR_LDS float *)lds;  // [wave][64 rows][128]
+    const bool vec = a.ins % 4 == 0;
+#pragma unroll
+    for (int pair = 0; pair < 2; ++pair) {
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    sums[(wave * 64 + 32 * u + row_of(r, lane >> 5)) * 128 + 32 * v + (lane & 31)] = acc[2 * pair + u][v][r];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int row = 8 * i + threadIdx.x / 32, col = threadIdx.x % 32 * 4;
+            f32x4 t = *(DEAR_LDS f32x4 *)(sums + row * 128 + col);
+#pragma unroll
+            for (int k = 1; k < 4; ++k) t += *(DEAR_LDS f32x4 *)(sums + (k * 64 + row) * 128 + col);
+            const int n = n0 + 64 * pair + row, k = k0 + col;
+            if (n < a.outs) {
+                float *p = out + (int64_t)n * a.ins + k;
+                if (vec) {
+                    if (k < a.ins) *(f32x4 *)p = t;
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (k + q < a.ins) p[q] = t[q];
+                }
+            }
+        }
+    }
+}
+
 __global__ __launch_bounds__(256) void split_sum_kernel(const float *part, int splits, int64_t n, float *out) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= n) return;
@@ -114,10 +265,16 @@ __global__ __launch_bounds__(256) void split_sum_kernel(const float *part, int s
 // ------------------------------------------------------------------------------------ host
 constexpr int64_t MAX_WIDTH = 1 << 24, MAX_ROWS = (int64_t)1 << 40;
 
-// Splits of the rows: as many as it takes for 512 workgroups, with no fewer than 256 rows each.
+// Whether the wide kernel takes it: bf16 in whole vectors, with rows that 32-bit offsets reach.
+bool wide(int32_t dtype, int64_t dy_stride, int64_t outs) {
+    return dtype == DEAR_BF16 && outs % 8 == 0 && dy_stride < (1 << 24);
+}
+
+// Splits of the rows, each a sum of its own in the workspace: as many as it takes for 512 workgroups, with no fewer than
+// 256 rows each.
 int splits_of(int64_t rows, int64_t outs, int64_t ins) {
     const int64_t tiles = ceil_div(outs, BN) * ceil_div(ins, BK);
-    int64_t n = 512 / tiles;
+    int64_t n = 256 / tiles;
     if (n > rows / 256) n = rows / 256;
     return n < 1 ? 1 : (int)n;
 }
@@ -154,7 +311,7 @@ int dear_checkpoint_weight_grad(const void *dy, int32_t dtype, int64_t dy_stride
     const int splits = splits_of(rows, outs, ins);
     params a = {};
     a.dy = dy, a.codes = codes, a.exponents = exponents, a.dy_stride = dy_stride, a.rows = rows;
-    a.chunk = ceil_div(ceil_div(rows, splits), BM) * BM;
+    a.chunk = ceil_div(ceil_div(rows, splits), WSTEP) * WSTEP;
     a.outs = (int32_t)outs, a.ins = (int32_t)ins, a.groups = (int32_t)ceil_div(ins, GROUP), a.padded = a.groups * GROUP;
     a.n_tiles = (int32_t)ceil_div(outs, BN), a.k_tiles = (int32_t)ceil_div(ins, BK);
     a.out = splits > 1 ? (float *)workspace : dw;
@@ -162,7 +319,8 @@ int dear_checkpoint_weight_grad(const void *dy, int32_t dtype, int64_t dy_stride
     if (groups > INT32_MAX || ceil_div(outs * ins, 256) > INT32_MAX) return DEAR_ETOOBIG;
     const unsigned grid = (unsigned)groups;
     const bool vec = aligned(dy, 16) && dy_stride * size % 16 == 0 && outs * size % 16 == 0;
-    if (dtype == DEAR_BF16 && vec) weight_grad_kernel<bf16, true><<<grid, THREADS, 0, stream>>>(a);
+    if (vec && wide(dtype, dy_stride, outs)) weight_grad_wide_kernel<<<grid, THREADS, 0, stream>>>(a);
+    else if (dtype == DEAR_BF16 && vec) weight_grad_kernel<bf16, true><<<grid, THREADS, 0, stream>>>(a);
     else if (dtype == DEAR_BF16) weight_grad_kernel<bf16, false><<<grid, THREADS, 0, stream>>>(a);
     else if (vec) weight_grad_kernel<float, true><<<grid, THREADS, 0, stream>>>(a);
     else weight_grad_kernel<float, false><<<grid, THREADS, 0, stream>>>(a);
