@@ -17,6 +17,9 @@ PROBE_HEADERS = [os.path.join(ROOT, "include", "dear_probe.h")]
 # training operators, a library of their own (include/dear_ops.h)
 OPS_LIB = os.path.join(PKG, "libdear_ops.so")
 OPS_SOURCES = [os.path.join(CSRC, f) for f in ("attention.hip", "norm.hip", "weight_grad.hip")]
+# accumulators of 16 values stay whole where control flow meets: taken apart into single values, as the compiler would
+# by its own measure, they are copied one by one in every step (attention's dk and dv: 48 spilled registers, and none so)
+OPS_FLAGS = ["-mllvm", "-amdgpu-codegenprepare-break-large-phis=false"]
 OPS_HEADERS = [os.path.join(CSRC, "ops_common.h"), os.path.join(ROOT, "include", "dear_ops.h"), os.path.join(ROOT, "include", "dear.h")]
 
 HIPCC_FLAGS = [
@@ -67,7 +70,7 @@ def build_ops(force: bool = True) -> str:
     """Compile libdear_ops.so (attention, norm, checkpoints)."""
     if not force and not _stale(OPS_LIB, OPS_SOURCES + OPS_HEADERS):
         return OPS_LIB
-    return _compile(OPS_LIB, OPS_SOURCES)
+    return _compile(OPS_LIB, OPS_SOURCES, OPS_FLAGS)
 
 
 if __name__ == "__main__":

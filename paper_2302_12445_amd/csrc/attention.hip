@@ -1,5 +1,6 @@
 // Attention and its backward pass (formulas: dear_ops.h).
 #include <cmath>
+#include <type_traits>
 
 #include "ops_common.h"
 
@@ -13,6 +14,7 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int THREADS = 256, WAVES = THREADS / 64;
 constexpr int BLOCK = 32 * WAVES;  // rows that a workgroup owns: 32 for each wave
 constexpr int STEP = 64;           // rows of the other sequence that it takes at a time
+constexpr int KEYS = 64;           // keys of a workgroup that computes dk and dv
 
 // Waves of a SIMD that the kernels are compiled for.  With two, one's products run beside the other's softmax; wide rows
 // of fp32, and wide dk and dv with their operands, take the registers of both.
@@ -27,7 +29,7 @@ struct heads {
 
 struct params {
     int32_t q_heads, kv_heads, head_dim, causal;
-    int32_t q_len, kv_len, tiles;
+    int32_t q_len, kv_len, batch, tiles;
     float scale;
     const int32_t *q_lens, *kv_lens;
     heads q, k, v, out, dout, dq, dk, dv;
@@ -95,12 +97,21 @@ __device__ __forceinline__ void store_row(char *p, const f32x16 *x, float factor
         }
 }
 
-// Workgroup -> (batch, head, tile).
-__device__ __forceinline__ void place(const params &a, int heads, int &b, int &h, int &t) {
-    const unsigned id = blockIdx.x, pair = id / (unsigned)a.tiles;
-    t = id % (unsigned)a.tiles;
-    b = pair / (unsigned)heads;
-    h = pair % (unsigned)heads;
+// Workgroup -> (batch, head, tile), for `heads` heads of which `shared` neighbours read the same keys.  Workgroups go to
+// the eight XCDs in turn.  Where it divides evenly an XCD gets whole groups of heads (every eighth, so that sequences of
+// different lengths are spread), or at least whole heads; it takes them one after another with all their tiles, which find
+// the other sequence in its L2 cache, or, in a causal call, whose tiles are numbered from the longest on, the same tile of
+// all its heads and then the next, so that the shortest come last.
+__device__ __forceinline__ void place(const params &a, unsigned heads, unsigned shared, int &b, int &h, int &t) {
+    const unsigned pairs = heads * a.batch, tiles = a.tiles;
+    unsigned pair, id = blockIdx.x, xcd = 0, own = pairs;
+    if (pairs % 8 == 0) xcd = id % 8, id /= 8, own = pairs / 8;
+    t = a.causal ? id / own : id % tiles;
+    pair = a.causal ? id % own : id / tiles;
+    if (pairs / shared % 8 == 0) pair = (pair / shared * 8 + xcd) * shared + pair % shared;
+    else pair += xcd * own;
+    b = pair / heads;
+    h = pair % heads;
 }
 
 // ------------------------------------------------------------------------------------ forward
@@ -108,7 +119,8 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
     int b, h, t;
-    place(a, a.q_heads, b, h, t);
+    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t);
+    if (a.causal) t = a.tiles - 1 - t;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
     const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
     const int kvh = h / (a.q_heads / a.kv_heads);
@@ -192,6 +204,161 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
         a.lse[((int64_t)b * a.q_heads + h) * a.q_len + i] = none ? -INFINITY : (top * c + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
+// ------------------------------------------------------------------------------------ bf16, tiles filled directly
+// Loads of STEP rows of W values that write LDS themselves.  A lane brings the same piece of every row that it has a part
+// in; its offsets from the tile's first row are 32 bits (the host sees to it that they fit).  Rows at or beyond `valid`
+// repeat the last one: what they stand for is masked, and their values are no others than those already read.  Values at
+// or beyond head_dim are not loaded; `clear` has put zeros there.
+template <int W> struct direct_loads {
+    static constexpr int N = STEP / direct<W>::ROWS / WAVES;  // loads of a wave
+    uint32_t piece, token, row;  // byte of the piece, bytes from row to row, first row of this lane
+    bool some;
+
+    __device__ __forceinline__ direct_loads(int64_t token_stride, int head_dim, int lane, int wave) {
+        row = wave * direct<W>::ROWS + lane / direct<W>::PIECES;
+        const int c = lane % direct<W>::PIECES ^ direct<W>::turn(row);  // `turn` is the same for all loads of the lane
+        piece = c * 16, token = (uint32_t)token_stride, some = c * 8 < head_dim;
+    }
+    // p: the tile's first row; left >= 1: valid rows from there on
+    __device__ __forceinline__ void load(const char *p, int left, DEAR_LDS bf16 *s, int wave) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t r = row + i * WAVES * direct<W>::ROWS;
+            if (left < STEP) r = min(r, (uint32_t)left - 1);
+            if (W % 64 != 0 || some) load_to_lds(p + (r * token + piece), s + (i * WAVES + wave) * 512);
+        }
+    }
+};
+
+template <int W> __device__ __forceinline__ void clear(DEAR_LDS bf16 *s) {
+    for (int i = threadIdx.x; i < STEP * W / 8; i += THREADS) *(DEAR_LDS u32x4 *)(s + i * 8) = u32x4{0, 0, 0, 0};
+}
+
+// Scores of a step's keys to a running softmax.  `base` is what the powers are taken against: the running maximum, times
+// scale * log2(e), of some step before.  It follows the maximum only when that has grown by more than GROWTH = 2^8, so
+// that the sums are seldom rescaled; out = o / sum and lse do not depend on it.
+constexpr float GROWTH = 8.f;
+
+// Order of a block of N products with a fragment read for each: AHEAD reads first, then a product and a read in turn.
+template <int N, int AHEAD> __device__ __forceinline__ void read_ahead() {
+    __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+    for (int n = 0; n < N - AHEAD; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
+
+template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_direct_kernel(params a) {
+    __shared__ __attribute__((aligned(16))) bf16 ks0[STEP * W], ks1[STEP * W], vs0[STEP * W], vs1[STEP * W];
+    int b, h, t;
+    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t);
+    if (a.causal) t = a.tiles - 1 - t;
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
+    const int kvh = h / (a.q_heads / a.kv_heads);
+    const int i = t * BLOCK + wave * 32 + (lane & 31);  // this lane's query
+    // keys 0 .. last are visible to it
+    const int last = i < nq ? (a.causal ? min(nk - 1, i + nk - nq) : nk - 1) : -1;
+    const int block_end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    const int wave_first = t * BLOCK + wave * 32;
+    const int wave_least = wave_first + 31 < nq ? (a.causal ? min(nk - 1, wave_first + nk - nq) : nk - 1) : -1;
+    const float c = a.scale * LOG2E;
+
+    f32x16 o[W / 32] = {};
+    float top = -INFINITY, base = 0.f, limit = -INFINITY, sum = 0.f;
+    if (block_end > 0) {
+        if (a.head_dim < W) {
+            for (DEAR_LDS bf16 *s : {(DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs0, (DEAR_LDS bf16 *)vs1}) clear<W>(s);
+            __syncthreads();
+        }
+        const direct_loads<W> kl(a.k.token, a.head_dim, lane, wave), vl(a.v.token, a.head_dim, lane, wave);
+        const char *kp = at(a.k, b, kvh), *vp = at(a.v, b, kvh);
+        int j0 = 0;
+        auto load = [&](DEAR_LDS bf16 *ks, DEAR_LDS bf16 *vs, int j) {
+            if (j < block_end) {
+                kl.load(kp, nk - j, ks, wave);
+                vl.load(vp, nk - j, vs, wave);
+                kp += STEP * a.k.token, vp += STEP * a.v.token;
+            }
+        };
+        load((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0, 0);
+        frag<bf16> q[W / 16];
+        load_rows<bf16, W>(q, at(a.q, b, h), a.q.token, i, nq, a.head_dim, half);
+        direct<W> rd(lane);
+        auto step = [&](const DEAR_LDS bf16 *ks, const DEAR_LDS bf16 *vs) {
+            rd.renew();
+            f32x16 s[STEP / 32] = {};
+#pragma unroll
+            for (int kk = 0; kk < W / 16; ++kk)
+#pragma unroll
+                for (int kb = 0; kb < STEP / 32; ++kb) s[kb] = mma(rd.straight(ks, 32 * kb, kk), q[kk], s[kb]);
+            read_ahead<W / 16 * (STEP / 32), W == 128 ? 8 : 4>();
+            if (j0 + STEP - 1 > wave_least) {
+                __builtin_amdgcn_sched_barrier(0);  // keeps this a branch: as selects it would cost every step
+#pragma unroll
+                for (int kb = 0; kb < STEP / 32; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[kb][r] = j0 + 32 * kb + row_of(r, half) <= last ? s[kb][r] : -INFINITY;
+            }
+            float most = s[0][0];
+#pragma unroll
+            for (int kb = 0; kb < STEP / 32; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) most = fmaxf(most, s[kb][r]);
+            most = halves_max(most);
+            if (__builtin_amdgcn_ballot_w64(most > limit)) {
+                const float old = base;
+                top = fmaxf(top, most);
+                base = top == -INFINITY ? 0.f : top * c;
+                limit = top + GROWTH / c;
+                const float keep = __builtin_amdgcn_exp2f(old - base);  // of nothing yet, whatever it is
+                sum *= keep;
+#pragma unroll
+                for (int db = 0; db < W / 32; ++db) o[db] *= keep;
+            }
+#pragma unroll
+            for (int kb = 0; kb < STEP / 32; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[kb][r] = __builtin_amdgcn_exp2f(s[kb][r] * c - base);
+                    sum += s[kb][r];
+                }
+#pragma unroll
+            for (int kb = 0; kb < STEP / 32; ++kb)
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    float x[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) x[u] = s[kb][8 * st + u];
+                    const frag<bf16> p = to_frag<bf16>(x);
+#pragma unroll
+                    for (int db = 0; db < W / 32; ++db)
+                        o[db] = mma(rd.transposed(vs, 32 * kb + 16 * st, db), p, o[db]);
+                }
+            j0 += STEP;
+        };
+        // one barrier a step: behind it this step's tiles are whole, and the other buffers are no longer read
+        while (true) {
+            loads_barrier();
+            load((DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs1, j0 + STEP);
+            step((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0);
+            if (j0 >= block_end) break;
+            loads_barrier();
+            load((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0, j0 + STEP);
+            step((DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs1);
+            if (j0 >= block_end) break;
+        }
+    }
+    if (i >= a.q_len) return;
+    sum = halves_sum(sum);
+    const bool none = top == -INFINITY && sum == 0.f;
+    store_row<bf16, W>(at(a.out, b, h) + i * a.out.token, o, none ? 0.f : 1.f / sum, a.head_dim, half);
+    if (half == 0)
+        a.lse[((int64_t)b * a.q_heads + h) * a.q_len + i] = none ? -INFINITY : (base + __builtin_amdgcn_logf(sum)) * LN2;
+}
+
 // ------------------------------------------------------------------------------------ backward: queries
 // dq of 32 queries a wave, over all keys.  As in the forward pass the results of the first products are taken
 // transposed, a query to a lane, so that lse and delta are one value a lane.  It also writes delta for the other kernel.
@@ -199,7 +366,8 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
     int b, h, t;
-    place(a, a.q_heads, b, h, t);
+    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t);
+    if (a.causal) t = a.tiles - 1 - t;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
     const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
     const int kvh = h / (a.q_heads / a.kv_heads);
@@ -274,20 +442,21 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
 
 // ------------------------------------------------------------------------------------ backward: keys and values
 // dk and dv of 32 keys a wave, over the queries of all heads that share them: one workgroup adds them all up, in order.
+// Two waves have the same keys and take every other 32 queries; their sums are added at the end.
 template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(true))) void attention_dkv_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     __shared__ __attribute__((aligned(16))) float rows[2][STEP];  // lse * log2(e) and delta of the queries
     DEAR_LDS T *qs = (DEAR_LDS T *)lds, *gs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
     int b, kvh, t;
-    place(a, a.kv_heads, b, kvh, t);
+    place(a, a.kv_heads, 1, b, kvh, t);
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
     const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
     const int group = a.q_heads / a.kv_heads;
-    const int wave_first = t * BLOCK + wave * 32, j = wave_first + (lane & 31);  // this lane's key
+    const int turn = wave % 2, wave_first = t * KEYS + wave / 2 * 32, j = wave_first + (lane & 31);  // this lane's key
     // queries first .. nq - 1 see it
     const int first = j < nk ? (a.causal ? max(0, j - nk + nq) : 0) : nq;
     const int wave_last = wave_first + 31 < nk ? (a.causal ? max(0, wave_first + 31 - nk + nq) : 0) : nq;
-    const int begin = t * BLOCK >= nk ? nq : a.causal ? max(0, t * BLOCK - nk + nq) / STEP * STEP : 0;
+    const int begin = t * KEYS >= nk ? nq : a.causal ? max(0, t * KEYS - nk + nq) / STEP * STEP : 0;
 
     frag<T> k[W / 16], v[W / 16];
     load_rows<T, W>(k, at(a.k, b, kvh), a.k.token, j, nk, a.head_dim, half);
@@ -326,8 +495,8 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
                 gst.load(gp, a.dout.token, i0 + STEP, nq, a.head_dim);
                 load_z(i0 + STEP);
             }
-#pragma unroll
-            for (int qb = 0; qb < STEP / 32; ++qb) {
+            {
+                const int qb = turn;
                 f32x16 s = {}, dp = {};
 #pragma unroll
                 for (int kk = 0; kk < W / 16; ++kk) {
@@ -357,9 +526,303 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
             }
         }
     }
+    DEAR_LDS float *sums = (DEAR_LDS float *)lds + wave / 2 * (W / 32 * 16 * 64);
+    for (f32x16 *x : {dk, dv}) {
+        __syncthreads();
+#pragma unroll
+        for (int db = 0; db < W / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (turn == 1) sums[(db * 16 + r) * 64 + lane] = x[db][r];
+        __syncthreads();
+#pragma unroll
+        for (int db = 0; db < W / 32; ++db)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (turn == 0) x[db][r] += sums[(db * 16 + r) * 64 + lane];
+    }
+    if (turn == 1) return;
     if (j >= a.kv_len) return;
     store_row<T, W>(at(a.dk, b, kvh) + j * a.dk.token, dk, a.scale, a.head_dim, half);
     store_row<T, W>(at(a.dv, b, kvh) + j * a.dv.token, dv, 1.f, a.head_dim, half);
+}
+
+// ------------------------------------------------------------------------------------ bf16 backward, tiles filled directly
+template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_direct_kernel(params a) {
+    __shared__ __attribute__((aligned(16))) bf16 ks0[STEP * W], ks1[STEP * W], vs0[STEP * W], vs1[STEP * W];
+    int b, h, t;
+    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t);
+    if (a.causal) t = a.tiles - 1 - t;
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
+    const int kvh = h / (a.q_heads / a.kv_heads);
+    const int i = t * BLOCK + wave * 32 + (lane & 31);
+    const int last = i < nq ? (a.causal ? min(nk - 1, i + nk - nq) : nk - 1) : -1;
+    const int block_end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    const int wave_first = t * BLOCK + wave * 32;
+    const int wave_least = wave_first + 31 < nq ? (a.causal ? min(nk - 1, wave_first + nk - nq) : nk - 1) : -1;
+    const float c = a.scale * LOG2E;
+    const bool any = block_end > 0;
+
+    const direct_loads<W> kl(a.k.token, a.head_dim, lane, wave), vl(a.v.token, a.head_dim, lane, wave);
+    const char *kp = at(a.k, b, kvh), *vp = at(a.v, b, kvh);
+    auto load = [&](DEAR_LDS bf16 *ks, DEAR_LDS bf16 *vs, int j) {
+        if (j < block_end) {
+            kl.load(kp, nk - j, ks, wave);
+            vl.load(vp, nk - j, vs, wave);
+            kp += STEP * a.k.token, vp += STEP * a.v.token;
+        }
+    };
+    if (any && a.head_dim < W) {
+        for (DEAR_LDS bf16 *s : {(DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs0, (DEAR_LDS bf16 *)vs1}) clear<W>(s);
+        __syncthreads();
+    }
+    load((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0, 0);
+
+    frag<bf16> q[W / 16], g[W / 16];
+    load_rows<bf16, W>(q, at(a.q, b, h), a.q.token, i, nq, a.head_dim, half);
+    load_rows<bf16, W>(g, at(a.dout, b, h), a.dout.token, i, nq, a.head_dim, half);
+    const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_len + i;
+    float delta = 0.f;
+    {
+        frag<bf16> out[W / 16];
+        load_rows<bf16, W>(out, at(a.out, b, h), a.out.token, i, nq, a.head_dim, half);
+#pragma unroll
+        for (int kk = 0; kk < W / 16; ++kk)
+#pragma unroll
+            for (int u = 0; u < 8; ++u) delta += (float)g[kk][u] * (float)out[kk][u];
+    }
+    delta = halves_sum(delta);
+    if (half == 0 && i < a.q_len) a.delta[row] = delta;
+    const float z = i < nq ? a.lse[row] : -INFINITY, base = z == -INFINITY ? 0.f : z * LOG2E;
+
+    f32x16 dq[W / 32] = {};
+    int j0 = 0;
+    direct<W> rd(lane);
+    auto step = [&](const DEAR_LDS bf16 *ks, const DEAR_LDS bf16 *vs) {
+        rd.renew();
+#pragma unroll
+        for (int kb = 0; kb < STEP / 32; ++kb) {
+            f32x16 s = {}, dp;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dp[r] = -delta;
+#pragma unroll
+            for (int kk = 0; kk < W / 16; ++kk) {
+                s = mma(rd.straight(ks, 32 * kb, kk), q[kk], s);
+                dp = mma(rd.straight(vs, 32 * kb, kk), g[kk], dp);
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(s[r] * c - base) * dp[r];
+            if (j0 + 32 * kb + 31 > wave_least) {
+                __builtin_amdgcn_sched_barrier(0);  // keeps this a branch: as selects it would cost every step
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = j0 + 32 * kb + row_of(r, half) <= last ? s[r] : 0.f;
+            }
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                float x[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) x[u] = s[8 * st + u];
+                const frag<bf16> ds = to_frag<bf16>(x);
+#pragma unroll
+                for (int db = 0; db < W / 32; ++db)
+                    dq[db] = mma(rd.transposed(ks, 32 * kb + 16 * st, db), ds, dq[db]);
+            }
+        }
+        j0 += STEP;
+    };
+    while (any) {
+        loads_barrier();
+        load((DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs1, j0 + STEP);
+        step((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0);
+        if (j0 >= block_end) break;
+        loads_barrier();
+        load((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0, j0 + STEP);
+        step((DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs1);
+        if (j0 >= block_end) break;
+    }
+    if (i < a.q_len) store_row<bf16, W>(at(a.dq, b, h) + i * a.dq.token, dq, a.scale, a.head_dim, half);
+}
+
+// dk and dv of 64 keys a workgroup: two waves have the same 32 keys and take every other 32 queries; their sums are added
+// at the end.  The accumulators and both operands of 32 keys take the registers of a SIMD, so that a wave has to
+// overlap its own products: the scores of the next queries are computed beside the softmax of these.
+template <int W> __global__ __launch_bounds__(THREADS, W == 128 ? 1 : 2) void attention_dkv_direct_kernel(params a) {
+    // tiles of even steps and of odd ones, two of each in turn: arrays of their own, so that the compiler sees that the loads
+    // under way are not what a step reads
+    __shared__ __attribute__((aligned(16))) bf16 qs0[2 * STEP * W], qs1[2 * STEP * W], gs0[2 * STEP * W], gs1[2 * STEP * W];
+    __shared__ __attribute__((aligned(16))) float rows[4][2][STEP];  // lse * log2(e) and -delta of the queries
+    int b, kvh, t;
+    place(a, a.kv_heads, 1, b, kvh, t);
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
+    const int group = a.q_heads / a.kv_heads, turn = wave & 1;
+    const int wave_first = t * KEYS + wave / 2 * 32, j = wave_first + (lane & 31);  // this lane's key
+    // queries first .. nq - 1 see it; those beyond nq have probabilities of 0 by their lse
+    const int first = j < nk ? (a.causal ? max(0, j - nk + nq) : 0) : nq;
+    const int wave_last = wave_first + 31 < nk ? (a.causal ? max(0, wave_first + 31 - nk + nq) : 0) : nq;
+    const int begin = t * KEYS >= nk ? nq : a.causal ? max(0, t * KEYS - nk + nq) / STEP * STEP : 0;
+    const int steps = begin < nq ? (nq - begin + STEP - 1) / STEP * group : 0;
+    const float c = a.scale * LOG2E;
+
+    f32x16 dk[W / 32] = {}, dv[W / 32] = {};
+    if (steps > 0) {
+        if (a.head_dim < W) {
+            for (DEAR_LDS bf16 *s : {(DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs0, (DEAR_LDS bf16 *)gs1}) {
+                clear<W>(s);
+                clear<W>(s + STEP * W);
+            }
+            __syncthreads();
+        }
+        const direct_loads<W> ql(a.q.token, a.head_dim, lane, wave), gl(a.dout.token, a.head_dim, lane, wave);
+        // the next step to be loaded: its queries, and its head's tensors
+        int h = kvh * group, next = begin;
+        const char *qp = at(a.q, b, h) + begin * a.q.token, *gp = at(a.dout, b, h) + begin * a.dout.token;
+        float z = 0.f;
+        auto load = [&](DEAR_LDS bf16 *qs, DEAR_LDS bf16 *gs) {
+            if (h < (kvh + 1) * group) {
+                ql.load(qp, nq - next, qs, wave);
+                gl.load(gp, nq - next, gs, wave);
+                // one value a thread: the first STEP threads take lse, the next ones delta
+                if (wave < 2) {
+                    const int i = next + lane;
+                    const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_len + i;
+                    if (wave == 0) {
+                        z = i < nq ? a.lse[row] * LOG2E : INFINITY;
+                        if (z == -INFINITY) z = INFINITY;  // no key is seen: all probabilities are 0
+                    } else {
+                        z = i < nq ? -a.delta[row] : 0.f;
+                    }
+                }
+                qp += STEP * a.q.token, gp += STEP * a.dout.token, next += STEP;
+                if (next >= nq) {
+                    h += 1, next = begin;
+                    qp = at(a.q, b, h) + begin * a.q.token, gp = at(a.dout, b, h) + begin * a.dout.token;
+                }
+            }
+        };
+        auto load_done = [&](int step) {
+            if (wave < 2) rows[step & 3][wave][lane] = z;
+        };
+        load((DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)gs0);
+        load_done(0);
+        load((DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs1);
+        load_done(1);
+        frag<bf16> k[W / 16], v[W / 16];
+        load_rows<bf16, W>(k, at(a.k, b, kvh), a.k.token, j, nk, a.head_dim, half);
+        load_rows<bf16, W>(v, at(a.v, b, kvh), a.v.token, j, nk, a.head_dim, half);
+        loads_barrier();
+
+        // scores and dp - delta of a step's queries; masked scores start, and stay, at -infinity
+        int i0 = begin;  // the queries of the next scores
+        // with the place of the 32 queries that are this wave's turn
+        direct<W> rd(lane);
+#pragma unroll
+        for (int kk = 0; kk < W / 16; ++kk) rd.row_at[kk] += 64 * W * turn;
+#pragma unroll
+        for (int db = 0; db < W / 32; ++db) rd.column_at[db][0] += 64 * W * turn, rd.column_at[db][1] += 64 * W * turn;
+        f32x16 s, dp;
+        auto scores = [&](const DEAR_LDS bf16 *qs, const DEAR_LDS bf16 *gs, int step) {
+            const float (*r)[STEP] = rows[step & 3];
+#pragma unroll
+            for (int u = 0; u < 16; u += 4) {
+                const f32x4 d = *(const f32x4 *)&r[1][32 * turn + row_of(u, half)];
+                dp[u] = d[0], dp[u + 1] = d[1], dp[u + 2] = d[2], dp[u + 3] = d[3];
+            }
+            s = f32x16{};
+            if (i0 + 32 * turn < wave_last) {
+                __builtin_amdgcn_sched_barrier(0);  // keeps this a branch
+#pragma unroll
+                for (int u = 0; u < 16; ++u) s[u] = i0 + 32 * turn + row_of(u, half) >= first ? 0.f : -INFINITY;
+            }
+            i0 += STEP;
+            if (i0 >= nq) i0 = begin;
+#pragma unroll
+            for (int kk = 0; kk < W / 16; ++kk) {
+                s = mma(rd.straight(qs, 0, kk), k[kk], s);
+                dp = mma(rd.straight(gs, 0, kk), v[kk], dp);
+            }
+        };
+        frag<bf16> p[2], ds[2];
+        auto soften = [&](frag<bf16> (&pn)[2], frag<bf16> (&dsn)[2], int step) {
+            const float (*r)[STEP] = rows[step & 3];
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                float x[8], y[8];
+#pragma unroll
+                for (int u = 0; u < 8; u += 4) {
+                    const f32x4 e = *(const f32x4 *)&r[0][32 * turn + row_of(8 * st + u, half)];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        x[u + w] = __builtin_amdgcn_exp2f(s[8 * st + u + w] * c - e[w]);
+                        y[u + w] = x[u + w] * dp[8 * st + u + w];
+                    }
+                }
+                pn[st] = to_frag<bf16>(x), dsn[st] = to_frag<bf16>(y);
+            }
+        };
+        auto accumulate = [&](const DEAR_LDS bf16 *qs, const DEAR_LDS bf16 *gs) {
+#pragma unroll
+            for (int st = 0; st < 2; ++st)
+#pragma unroll
+                for (int db = 0; db < W / 32; ++db) {
+                    dv[db] = mma(rd.transposed(gs, 16 * st, db), p[st], dv[db]);
+                    dk[db] = mma(rd.transposed(qs, 16 * st, db), ds[st], dk[db]);
+                }
+        };
+        // Step n: behind its barrier the tiles of step n + 1 are whole and those of step n - 2 no longer read, into whose place
+        // those of step n + 2 go.  The softmax of step n runs beside the products of step n - 1; the scores of step n + 1
+        // follow (behind the last step: of whatever stands there, not used).
+        auto step = [&](int n, const DEAR_LDS bf16 *qs, const DEAR_LDS bf16 *gs, DEAR_LDS bf16 *qs_load, DEAR_LDS bf16 *gs_load) {
+            loads_barrier();
+            load(qs_load + (n / 2 + 1) % 2 * (STEP * W), gs_load + (n / 2 + 1) % 2 * (STEP * W));
+            frag<bf16> pn[2], dsn[2];
+            soften(pn, dsn, n);
+            accumulate(qs, gs);
+            p[0] = pn[0], p[1] = pn[1], ds[0] = dsn[0], ds[1] = dsn[1];
+            scores(qs, gs, n + 1);
+            load_done(n + 2);
+        };
+        // Step 0 has no products behind it.  Reads of scores begin with tile 0, those of products too; each goes on to the
+        // other place of its arrays every second step.
+        int n = 0;
+        scores((DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)gs0, 0);
+        load((DEAR_LDS bf16 *)qs0 + STEP * W, (DEAR_LDS bf16 *)gs0 + STEP * W);
+        soften(p, ds, 0);
+        scores((DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs1, 1);
+        load_done(2);
+        rd.turn_rows();
+        while (true) {
+            if (++n >= steps) break;
+            step(n, (DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)gs0, (DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs1);
+            if (++n >= steps) break;
+            step(n, (DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs1, (DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)gs0);
+            rd.turn_rows();
+            rd.turn_columns();
+        }
+        if (n % 2) accumulate((DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)gs0);
+        else accumulate((DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs1);
+        // the other wave's sums, dk's and then dv's, where the tiles were
+        DEAR_LDS float *sums = wave / 2 ? (DEAR_LDS float *)qs1 : (DEAR_LDS float *)qs0;
+        static_assert(W / 32 * 16 * 64 * 4 <= STEP * W * 2, "the sums of 32 keys fit a tile");
+        for (f32x16 *x : {dk, dv}) {
+            __syncthreads();
+#pragma unroll
+            for (int db = 0; db < W / 32; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (turn == 1) sums[(db * 16 + r) * 64 + lane] = x[db][r];
+            __syncthreads();
+#pragma unroll
+            for (int db = 0; db < W / 32; ++db)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (turn == 0) x[db][r] += sums[(db * 16 + r) * 64 + lane];
+        }
+    }
+    if (turn == 1 || j >= a.kv_len) return;
+    store_row<bf16, W>(at(a.dk, b, kvh) + j * a.dk.token, dk, a.scale, a.head_dim, half);
+    store_row<bf16, W>(at(a.dv, b, kvh) + j * a.dv.token, dv, 1.f, a.head_dim, half);
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -399,13 +862,16 @@ params make(const dear_attention_t *p) {
     };
     params a = {};
     a.q_heads = p->q_heads, a.kv_heads = p->kv_heads, a.head_dim = p->head_dim, a.causal = p->causal;
-    a.q_len = (int32_t)p->q_len, a.kv_len = (int32_t)p->kv_len, a.scale = p->scale;
+    a.q_len = (int32_t)p->q_len, a.kv_len = (int32_t)p->kv_len, a.scale = p->scale, a.batch = p->batch;
     a.q_lens = p->q_lens, a.kv_lens = p->kv_lens;
     a.q = t(p->q), a.k = t(p->k), a.v = t(p->v), a.out = t(p->out);
     a.dout = t(p->dout), a.dq = t(p->dq), a.dk = t(p->dk), a.dv = t(p->dv);
     a.lse = p->lse, a.delta = (float *)p->workspace;
     return a;
 }
+
+// Whether the rows of a step lie within 2^31 bytes, so that tiles can be filled directly.
+bool near(const dear_attention_t *p, const dear_heads_t &t) { return p->dtype == DEAR_BF16 && t.token_stride < (1 << 30) / STEP; }
 
 bool too_big(int64_t heads, int64_t batch, int64_t tiles) {
     return heads * batch > INT32_MAX || heads * batch * tiles > INT32_MAX;
@@ -450,7 +916,11 @@ int dear_attention(const dear_attention_t *p, void *hip_stream) {
     a.tiles = (int32_t)ceil_div(p->q_len, BLOCK);
     if (too_big(p->q_heads, p->batch, a.tiles)) return DEAR_ETOOBIG;
     const unsigned grid = (unsigned)a.tiles * p->q_heads * p->batch;
-    DEAR_BY_TYPE(p, attention_kernel, grid, a, (hipStream_t)hip_stream);
+    hipStream_t stream = (hipStream_t)hip_stream;
+    const bool direct = near(p, p->k) && near(p, p->v);
+    if (direct && p->head_dim <= 64) attention_direct_kernel<64><<<grid, THREADS, 0, stream>>>(a);
+    else if (direct) attention_direct_kernel<128><<<grid, THREADS, 0, stream>>>(a);
+    else DEAR_BY_TYPE(p, attention_kernel, grid, a, stream);
     return launch_status();
 }
 
@@ -472,18 +942,24 @@ int dear_attention_backward(const dear_attention_t *p, void *hip_stream) {
         if (p->workspace_bytes < need) return DEAR_ETOOBIG;
     }
     params a = make(p);
-    const int64_t q_tiles = ceil_div(p->q_len, BLOCK), kv_tiles = ceil_div(p->kv_len, BLOCK);
+    const bool direct = near(p, p->q) && near(p, p->dout) && near(p, p->k) && near(p, p->v);
+    hipStream_t stream = (hipStream_t)hip_stream;
+    const int64_t q_tiles = ceil_div(p->q_len, BLOCK), kv_tiles = ceil_div(p->kv_len, KEYS);
     if (too_big(p->q_heads, p->batch, q_tiles) || too_big(p->kv_heads, p->batch, kv_tiles)) return DEAR_ETOOBIG;
     if (q_tiles) {
         a.tiles = (int32_t)q_tiles;
         const unsigned grid = (unsigned)q_tiles * p->q_heads * p->batch;
-        DEAR_BY_TYPE(p, attention_dq_kernel, grid, a, (hipStream_t)hip_stream);
+        if (direct && p->head_dim <= 64) attention_dq_direct_kernel<64><<<grid, THREADS, 0, stream>>>(a);
+        else if (direct) attention_dq_direct_kernel<128><<<grid, THREADS, 0, stream>>>(a);
+        else DEAR_BY_TYPE(p, attention_dq_kernel, grid, a, stream);
         if (int rc = launch_status()) return rc;
     }
     if (kv_tiles) {
         a.tiles = (int32_t)kv_tiles;
         const unsigned grid = (unsigned)kv_tiles * p->kv_heads * p->batch;
-        DEAR_BY_TYPE(p, attention_dkv_kernel, grid, a, (hipStream_t)hip_stream);
+        if (direct && p->head_dim <= 64) attention_dkv_direct_kernel<64><<<grid, THREADS, 0, stream>>>(a);
+        else if (direct) attention_dkv_direct_kernel<128><<<grid, THREADS, 0, stream>>>(a);
+        else DEAR_BY_TYPE(p, attention_dkv_kernel, grid, a, stream);
         if (int rc = launch_status()) return rc;
     }
     return DEAR_OK;

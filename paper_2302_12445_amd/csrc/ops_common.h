@@ -117,6 +117,73 @@ template <int W> __device__ __forceinline__ f32x8 transposed(const DEAR_LDS floa
     return f;
 }
 
+// ------------------------------------------------------------------------------------ tiles that memory fills directly
+// Rows of W bf16 values without padding, brought by loads that write LDS themselves: a wave's load puts 64 pieces of 16
+// bytes in a row, so that the order of the pieces is what keeps reads apart in the banks.  Piece c of a row stands at
+// c ^ turn(row): for 128 values (256 bytes, one line of all banks) the eight rows that a quarter of a straight read
+// touches, and the four rows of a transposing one, differ; for 64 values two rows share a line, and pairs of rows differ.
+template <int W> struct direct {
+    static constexpr int PIECES = W / 8;                     // of a row
+    static constexpr int ROWS = 64 / PIECES;                 // of a wave's load
+    __device__ static __forceinline__ int turn(int row) {
+        return W == 128 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
+    }
+    // Offset in bytes of piece c of a row.
+    __device__ static __forceinline__ uint32_t at(int row, int c) { return row * (2 * W) + (c ^ turn(row)) * 16; }
+
+    // A lane's offsets from a tile's start, of straight reads by step and of transposing ones by columns and rows.  `renew`
+    // tells the compiler once a step that they may have changed: otherwise it keeps the sum of each with the place of
+    // each tile, which is a constant of the instruction, in a register of its own.
+    uint32_t row_at[W / 16], column_at[W / 32][2];
+    __device__ __forceinline__ direct(int lane) {
+#pragma unroll
+        for (int kk = 0; kk < W / 16; ++kk) row_at[kk] = at(lane & 31, 2 * kk + (lane >> 5));
+        const int row = 4 * (lane >> 5) + (lane & 15) / 4, c = 2 * (lane >> 4 & 1) + (lane & 3) / 2;
+#pragma unroll
+        for (int db = 0; db < W / 32; ++db)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) column_at[db][u] = at(row + 8 * u, 4 * db + c) + 8 * (lane & 1);
+    }
+    __device__ __forceinline__ void renew() {
+#pragma unroll
+        for (int kk = 0; kk < W / 16; ++kk) asm("" : "+v"(row_at[kk]));
+#pragma unroll
+        for (int db = 0; db < W / 32; ++db) asm("" : "+v"(column_at[db][0]), "+v"(column_at[db][1]));
+    }
+    // To the other one of two tiles of 64 rows, one behind the other.
+    __device__ __forceinline__ void turn_rows() {
+#pragma unroll
+        for (int kk = 0; kk < W / 16; ++kk) row_at[kk] ^= 64 * W * 2;
+    }
+    __device__ __forceinline__ void turn_columns() {
+#pragma unroll
+        for (int db = 0; db < W / 32; ++db) column_at[db][0] ^= 64 * W * 2, column_at[db][1] ^= 64 * W * 2;
+    }
+
+    // Rows row0 .. +31 (a multiple of 32), slots of step kk, as `straight`.
+    __device__ __forceinline__ bf16x8 straight(const DEAR_LDS bf16 *s, int row0, int kk) const {
+        return *(const DEAR_LDS bf16x8 *)((const DEAR_LDS char *)(s + row0 * W) + row_at[kk]);
+    }
+    // Columns 32 db .. +31, slots of rows row0 .. +15 (a multiple of 16), as `transposed`.
+    __device__ __forceinline__ bf16x8 transposed(const DEAR_LDS bf16 *s, int row0, int db) const {
+        const DEAR_LDS char *p = (const DEAR_LDS char *)(s + row0 * W);
+        const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((DEAR_LDS bf16x4 *)(p + column_at[db][0]));
+        const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((DEAR_LDS bf16x4 *)(p + column_at[db][1]));
+        return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+};
+
+__device__ __forceinline__ void load_to_lds(const char *p, DEAR_LDS void *s) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)p, s, 16, 0, 0);
+}
+
+// Barrier behind which the tiles that this workgroup's waves have loaded to LDS are whole: each wave first waits for its
+// own loads (vmcnt 0), which a barrier by itself does not.
+__device__ __forceinline__ void loads_barrier() {
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();
+}
+
 inline bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int launch_status() { return hipGetLastError() == hipSuccess ? DEAR_OK : DEAR_EHIP; }
