@@ -29,11 +29,13 @@ struct heads {
 
 struct params {
     int32_t q_heads, kv_heads, head_dim, causal;
-    int32_t q_len, kv_len, batch, tiles;
+    int32_t q_len, kv_len, batch, tiles, q_tiles;  // tiles: of this launch; q_tiles: BLOCKs of queries
     float scale;
     const int32_t *q_lens, *kv_lens;
     heads q, k, v, out, dout, dq, dk, dv;
-    float *lse, *delta;
+    float *lse;
+    // backward, of the queries of all tiles: lse * log2(e), or infinity where no key is seen, and -delta
+    float *powers, *deltas;
 };
 
 __device__ __forceinline__ char *at(const heads &t, int b, int h) {
@@ -209,7 +211,7 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
 // in; its offsets from the tile's first row are 32 bits (the host sees to it that they fit).  Rows at or beyond `valid`
 // repeat the last one: what they stand for is masked, and their values are no others than those already read.  Values at
 // or beyond head_dim are not loaded; `clear` has put zeros there.
-template <int W> struct direct_loads {
+template <int W, int WAVES> struct direct_loads {
     static constexpr int N = STEP / direct<W>::ROWS / WAVES;  // loads of a wave
     uint32_t piece, token, row;  // byte of the piece, bytes from row to row, first row of this lane
     bool some;
@@ -231,7 +233,7 @@ template <int W> struct direct_loads {
 };
 
 template <int W> __device__ __forceinline__ void clear(DEAR_LDS bf16 *s) {
-    for (int i = threadIdx.x; i < STEP * W / 8; i += THREADS) *(DEAR_LDS u32x4 *)(s + i * 8) = u32x4{0, 0, 0, 0};
+    for (unsigned i = threadIdx.x; i < STEP * W / 8; i += blockDim.x) *(DEAR_LDS u32x4 *)(s + i * 8) = u32x4{0, 0, 0, 0};
 }
 
 // Scores of a step's keys to a running softmax.  `base` is what the powers are taken against: the running maximum, times
@@ -273,7 +275,7 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_direct_
             for (DEAR_LDS bf16 *s : {(DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs0, (DEAR_LDS bf16 *)vs1}) clear<W>(s);
             __syncthreads();
         }
-        const direct_loads<W> kl(a.k.token, a.head_dim, lane, wave), vl(a.v.token, a.head_dim, lane, wave);
+        const direct_loads<W, WAVES> kl(a.k.token, a.head_dim, lane, wave), vl(a.v.token, a.head_dim, lane, wave);
         const char *kp = at(a.k, b, kvh), *vp = at(a.v, b, kvh);
         int j0 = 0;
         auto load = [&](DEAR_LDS bf16 *ks, DEAR_LDS bf16 *vs, int j) {
@@ -360,6 +362,19 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_direct_
 }
 
 // ------------------------------------------------------------------------------------ backward: queries
+// lse * log2(e) of query i, as what its powers are taken against: infinity where it sees no key, so that its probabilities
+// are 0.  Kept, with -delta, for the kernel that computes dk and dv; there is a place for every query of every tile.
+__device__ __forceinline__ float row_values(const params &a, int b, int h, int i, int nq, int half, float delta) {
+    const float z = i < nq ? a.lse[((int64_t)b * a.q_heads + h) * a.q_len + i] : -INFINITY;
+    const float base = z == -INFINITY ? INFINITY : z * LOG2E;
+    if (half == 0) {
+        const int64_t row = ((int64_t)b * a.q_heads + h) * a.tiles * BLOCK + i;
+        a.powers[row] = base;
+        a.deltas[row] = -delta;
+    }
+    return base;
+}
+
 // dq of 32 queries a wave, over all keys.  As in the forward pass the results of the first products are taken
 // transposed, a query to a lane, so that lse and delta are one value a lane.  It also writes delta for the other kernel.
 template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(false))) void attention_dq_kernel(params a) {
@@ -381,7 +396,6 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
     frag<T> q[W / 16], g[W / 16];
     load_rows<T, W>(q, at(a.q, b, h), a.q.token, i, nq, a.head_dim, half);
     load_rows<T, W>(g, at(a.dout, b, h), a.dout.token, i, nq, a.head_dim, half);
-    const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_len + i;
     float delta = 0.f;
     {
         frag<T> out[W / 16];
@@ -392,9 +406,7 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
             for (int u = 0; u < 8; ++u) delta += (float)g[kk][u] * (float)out[kk][u];
     }
     delta = halves_sum(delta);
-    if (half == 0 && i < a.q_len) a.delta[row] = delta;
-    const float z = i < nq ? a.lse[row] : -INFINITY;
-    const float base = z == -INFINITY ? 0.f : z * LOG2E, c = a.scale * LOG2E;
+    const float base = row_values(a, b, h, i, nq, half, delta), c = a.scale * LOG2E;
 
     f32x16 dq[W / 32] = {};
     stage<T, W> kst, vst;
@@ -445,7 +457,7 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
 // Two waves have the same keys and take every other 32 queries; their sums are added at the end.
 template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(true))) void attention_dkv_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
-    __shared__ __attribute__((aligned(16))) float rows[2][STEP];  // lse * log2(e) and delta of the queries
+    __shared__ __attribute__((aligned(16))) float rows[2][STEP];  // what the queries' powers are taken against, and -delta
     DEAR_LDS T *qs = (DEAR_LDS T *)lds, *gs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
     int b, kvh, t;
     place(a, a.kv_heads, 1, b, kvh, t);
@@ -466,18 +478,13 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
 
     for (int h = kvh * group; h < (kvh + 1) * group; ++h) {
         const char *qp = at(a.q, b, h), *gp = at(a.dout, b, h);
-        const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_len;
+        const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_tiles * BLOCK;
         stage<T, W> qst, gst;
         float z = 0.f;
-        // one value a thread: the first STEP threads take lse, the next ones delta
+        // one value a thread: the first STEP threads take what powers are taken against, the next ones -delta
         auto load_z = [&](int i0) {
-            const int i = i0 + threadIdx.x % STEP;
-            if (threadIdx.x < STEP) {
-                z = i < nq ? a.lse[row + i] * LOG2E : INFINITY;
-                if (z == -INFINITY) z = INFINITY;  // no key is seen: all probabilities are 0
-            } else if (threadIdx.x < 2 * STEP) {
-                z = i < nq ? a.delta[row + i] : 0.f;
-            }
+            const int64_t i = row + i0 + threadIdx.x % STEP;
+            if (threadIdx.x < 2 * STEP) z = threadIdx.x < STEP ? a.powers[i] : a.deltas[i];
         };
         if (begin < nq) {
             qst.load(qp, a.q.token, begin, nq, a.head_dim);
@@ -509,7 +516,7 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
                     const int n = 32 * qb + row_of(r, half);
                     const float p = __builtin_amdgcn_exp2f(s[r] * c - rows[0][n]);
                     s[r] = whole || (i0 + n >= first && i0 + n < nq) ? p : 0.f;
-                    dp[r] = s[r] * (dp[r] - rows[1][n]);
+                    dp[r] = s[r] * (dp[r] + rows[1][n]);
                 }
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
@@ -564,7 +571,7 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_dire
     const float c = a.scale * LOG2E;
     const bool any = block_end > 0;
 
-    const direct_loads<W> kl(a.k.token, a.head_dim, lane, wave), vl(a.v.token, a.head_dim, lane, wave);
+    const direct_loads<W, WAVES> kl(a.k.token, a.head_dim, lane, wave), vl(a.v.token, a.head_dim, lane, wave);
     const char *kp = at(a.k, b, kvh), *vp = at(a.v, b, kvh);
     auto load = [&](DEAR_LDS bf16 *ks, DEAR_LDS bf16 *vs, int j) {
         if (j < block_end) {
@@ -582,7 +589,6 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_dire
     frag<bf16> q[W / 16], g[W / 16];
     load_rows<bf16, W>(q, at(a.q, b, h), a.q.token, i, nq, a.head_dim, half);
     load_rows<bf16, W>(g, at(a.dout, b, h), a.dout.token, i, nq, a.head_dim, half);
-    const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_len + i;
     float delta = 0.f;
     {
         frag<bf16> out[W / 16];
@@ -593,8 +599,7 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_dire
             for (int u = 0; u < 8; ++u) delta += (float)g[kk][u] * (float)out[kk][u];
     }
     delta = halves_sum(delta);
-    if (half == 0 && i < a.q_len) a.delta[row] = delta;
-    const float z = i < nq ? a.lse[row] : -INFINITY, base = z == -INFINITY ? 0.f : z * LOG2E;
+    const float base = row_values(a, b, h, i, nq, half, delta);
 
     f32x16 dq[W / 32] = {};
     int j0 = 0;
@@ -644,56 +649,42 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_dire
     if (i < a.q_len) store_row<bf16, W>(at(a.dq, b, h) + i * a.dq.token, dq, a.scale, a.head_dim, half);
 }
 
-// dk and dv of 64 keys a workgroup: two waves have the same 32 keys and take every other 32 queries; their sums are added
-// at the end.  The accumulators and both operands of 32 keys take the registers of a SIMD, so that a wave has to
-// overlap its own products: the scores of the next queries are computed beside the softmax of these.
-template <int W> __global__ __launch_bounds__(THREADS, W == 128 ? 1 : 2) void attention_dkv_direct_kernel(params a) {
-    // tiles of even steps and of odd ones, two of each in turn: arrays of their own, so that the compiler sees that the loads
-    // under way are not what a step reads
-    __shared__ __attribute__((aligned(16))) bf16 qs0[2 * STEP * W], qs1[2 * STEP * W], gs0[2 * STEP * W], gs1[2 * STEP * W];
-    __shared__ __attribute__((aligned(16))) float rows[4][2][STEP];  // lse * log2(e) and -delta of the queries
+// dk and dv of 128 keys a workgroup, 32 a wave, for rows of 64 values: the operands and sums of both fit a wave beside a
+// second one.
+__global__ __launch_bounds__(THREADS, 2) void attention_dkv_direct_kernel(params a) {
+    constexpr int W = 64;
+    __shared__ __attribute__((aligned(16))) bf16 qs0[STEP * W], qs1[STEP * W], gs0[STEP * W], gs1[STEP * W];
+    __shared__ __attribute__((aligned(16))) float powers0[STEP], powers1[STEP], deltas0[STEP], deltas1[STEP];
     int b, kvh, t;
     place(a, a.kv_heads, 1, b, kvh, t);
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
-    const int group = a.q_heads / a.kv_heads, turn = wave & 1;
-    const int wave_first = t * KEYS + wave / 2 * 32, j = wave_first + (lane & 31);  // this lane's key
-    // queries first .. nq - 1 see it; those beyond nq have probabilities of 0 by their lse
+    const int group = a.q_heads / a.kv_heads;
+    const int wave_first = t * BLOCK + wave * 32, j = wave_first + (lane & 31);  // this lane's key
+    // queries first .. nq - 1 see it; those beyond nq have probabilities of 0 by their powers
     const int first = j < nk ? (a.causal ? max(0, j - nk + nq) : 0) : nq;
     const int wave_last = wave_first + 31 < nk ? (a.causal ? max(0, wave_first + 31 - nk + nq) : 0) : nq;
-    const int begin = t * KEYS >= nk ? nq : a.causal ? max(0, t * KEYS - nk + nq) / STEP * STEP : 0;
+    const int begin = t * BLOCK >= nk ? nq : a.causal ? max(0, t * BLOCK - nk + nq) / STEP * STEP : 0;
     const int steps = begin < nq ? (nq - begin + STEP - 1) / STEP * group : 0;
     const float c = a.scale * LOG2E;
 
     f32x16 dk[W / 32] = {}, dv[W / 32] = {};
     if (steps > 0) {
         if (a.head_dim < W) {
-            for (DEAR_LDS bf16 *s : {(DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs0, (DEAR_LDS bf16 *)gs1}) {
-                clear<W>(s);
-                clear<W>(s + STEP * W);
-            }
+            for (DEAR_LDS bf16 *s : {(DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs0, (DEAR_LDS bf16 *)gs1}) clear<W>(s);
             __syncthreads();
         }
-        const direct_loads<W> ql(a.q.token, a.head_dim, lane, wave), gl(a.dout.token, a.head_dim, lane, wave);
+        const direct_loads<W, WAVES> ql(a.q.token, a.head_dim, lane, wave), gl(a.dout.token, a.head_dim, lane, wave);
         // the next step to be loaded: its queries, and its head's tensors
-        int h = kvh * group, next = begin;
+        int h = kvh * group, next = begin, loaded = 0;
         const char *qp = at(a.q, b, h) + begin * a.q.token, *gp = at(a.dout, b, h) + begin * a.dout.token;
-        float z = 0.f;
-        auto load = [&](DEAR_LDS bf16 *qs, DEAR_LDS bf16 *gs) {
-            if (h < (kvh + 1) * group) {
+        auto load = [&](DEAR_LDS bf16 *qs, DEAR_LDS bf16 *gs, DEAR_LDS float *powers, DEAR_LDS float *deltas) {
+            if (loaded++ < steps) {
                 ql.load(qp, nq - next, qs, wave);
                 gl.load(gp, nq - next, gs, wave);
-                // one value a thread: the first STEP threads take lse, the next ones delta
-                if (wave < 2) {
-                    const int i = next + lane;
-                    const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_len + i;
-                    if (wave == 0) {
-                        z = i < nq ? a.lse[row] * LOG2E : INFINITY;
-                        if (z == -INFINITY) z = INFINITY;  // no key is seen: all probabilities are 0
-                    } else {
-                        z = i < nq ? -a.delta[row] : 0.f;
-                    }
-                }
+                const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_tiles * BLOCK + next + lane;
+                if (wave == 0) load_value_to_lds(a.powers + row, powers);
+                if (wave == 1) load_value_to_lds(a.deltas + row, deltas);
                 qp += STEP * a.q.token, gp += STEP * a.dout.token, next += STEP;
                 if (next >= nq) {
                     h += 1, next = begin;
@@ -701,128 +692,256 @@ template <int W> __global__ __launch_bounds__(THREADS, W == 128 ? 1 : 2) void at
                 }
             }
         };
-        auto load_done = [&](int step) {
-            if (wave < 2) rows[step & 3][wave][lane] = z;
-        };
-        load((DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)gs0);
-        load_done(0);
-        load((DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs1);
-        load_done(1);
+#define DEAR_LOAD(n) load((DEAR_LDS bf16 *)qs##n, (DEAR_LDS bf16 *)gs##n, (DEAR_LDS float *)powers##n, (DEAR_LDS float *)deltas##n)
+        DEAR_LOAD(0);
         frag<bf16> k[W / 16], v[W / 16];
         load_rows<bf16, W>(k, at(a.k, b, kvh), a.k.token, j, nk, a.head_dim, half);
         load_rows<bf16, W>(v, at(a.v, b, kvh), a.v.token, j, nk, a.head_dim, half);
-        loads_barrier();
-
-        // scores and dp - delta of a step's queries; masked scores start, and stay, at -infinity
-        int i0 = begin;  // the queries of the next scores
-        // with the place of the 32 queries that are this wave's turn
         direct<W> rd(lane);
+        int n = 0, i0 = begin;
+        auto step = [&](const DEAR_LDS bf16 *qs, const DEAR_LDS bf16 *gs, const DEAR_LDS float *powers, const DEAR_LDS float *deltas) {
+            rd.renew();
 #pragma unroll
-        for (int kk = 0; kk < W / 16; ++kk) rd.row_at[kk] += 64 * W * turn;
+            for (int qb = 0; qb < STEP / 32; ++qb) {
+                f32x16 s = {}, dp;
+                if (i0 + 32 * qb < wave_last) {  // masked scores start, and stay, at -infinity
+                    __builtin_amdgcn_sched_barrier(0);  // keeps this a branch
 #pragma unroll
-        for (int db = 0; db < W / 32; ++db) rd.column_at[db][0] += 64 * W * turn, rd.column_at[db][1] += 64 * W * turn;
-        f32x16 s, dp;
-        auto scores = [&](const DEAR_LDS bf16 *qs, const DEAR_LDS bf16 *gs, int step) {
-            const float (*r)[STEP] = rows[step & 3];
+                    for (int r = 0; r < 16; ++r) s[r] = i0 + 32 * qb + row_of(r, half) >= first ? 0.f : -INFINITY;
+                }
 #pragma unroll
-            for (int u = 0; u < 16; u += 4) {
-                const f32x4 d = *(const f32x4 *)&r[1][32 * turn + row_of(u, half)];
-                dp[u] = d[0], dp[u + 1] = d[1], dp[u + 2] = d[2], dp[u + 3] = d[3];
-            }
-            s = f32x16{};
-            if (i0 + 32 * turn < wave_last) {
-                __builtin_amdgcn_sched_barrier(0);  // keeps this a branch
+                for (int r = 0; r < 16; r += 4) {
+                    const f32x4 d = *(const DEAR_LDS f32x4 *)(deltas + 32 * qb + row_of(r, half));
+                    dp[r] = d[0], dp[r + 1] = d[1], dp[r + 2] = d[2], dp[r + 3] = d[3];
+                }
 #pragma unroll
-                for (int u = 0; u < 16; ++u) s[u] = i0 + 32 * turn + row_of(u, half) >= first ? 0.f : -INFINITY;
+                for (int kk = 0; kk < W / 16; ++kk) {
+                    s = mma(rd.straight(qs, 32 * qb, kk), k[kk], s);
+                    dp = mma(rd.straight(gs, 32 * qb, kk), v[kk], dp);
+                }
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    float x[8], y[8];
+#pragma unroll
+                    for (int u = 0; u < 8; u += 4) {
+                        const f32x4 e = *(const DEAR_LDS f32x4 *)(powers + 32 * qb + row_of(8 * st + u, half));
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            x[u + w] = __builtin_amdgcn_exp2f(s[8 * st + u + w] * c - e[w]);
+                            y[u + w] = x[u + w] * dp[8 * st + u + w];
+                        }
+                    }
+                    const frag<bf16> p = to_frag<bf16>(x), ds = to_frag<bf16>(y);
+#pragma unroll
+                    for (int db = 0; db < W / 32; ++db) {
+                        dv[db] = mma(rd.transposed(gs, 32 * qb + 16 * st, db), p, dv[db]);
+                        dk[db] = mma(rd.transposed(qs, 32 * qb + 16 * st, db), ds, dk[db]);
+                    }
+                }
             }
             i0 += STEP;
             if (i0 >= nq) i0 = begin;
-#pragma unroll
-            for (int kk = 0; kk < W / 16; ++kk) {
-                s = mma(rd.straight(qs, 0, kk), k[kk], s);
-                dp = mma(rd.straight(gs, 0, kk), v[kk], dp);
-            }
+            return ++n < steps;
         };
-        frag<bf16> p[2], ds[2];
-        auto soften = [&](frag<bf16> (&pn)[2], frag<bf16> (&dsn)[2], int step) {
-            const float (*r)[STEP] = rows[step & 3];
-#pragma unroll
-            for (int st = 0; st < 2; ++st) {
-                float x[8], y[8];
-#pragma unroll
-                for (int u = 0; u < 8; u += 4) {
-                    const f32x4 e = *(const f32x4 *)&r[0][32 * turn + row_of(8 * st + u, half)];
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        x[u + w] = __builtin_amdgcn_exp2f(s[8 * st + u + w] * c - e[w]);
-                        y[u + w] = x[u + w] * dp[8 * st + u + w];
-                    }
-                }
-                pn[st] = to_frag<bf16>(x), dsn[st] = to_frag<bf16>(y);
-            }
-        };
-        auto accumulate = [&](const DEAR_LDS bf16 *qs, const DEAR_LDS bf16 *gs) {
-#pragma unroll
-            for (int st = 0; st < 2; ++st)
-#pragma unroll
-                for (int db = 0; db < W / 32; ++db) {
-                    dv[db] = mma(rd.transposed(gs, 16 * st, db), p[st], dv[db]);
-                    dk[db] = mma(rd.transposed(qs, 16 * st, db), ds[st], dk[db]);
-                }
-        };
-        // Step n: behind its barrier the tiles of step n + 1 are whole and those of step n - 2 no longer read, into whose place
-        // those of step n + 2 go.  The softmax of step n runs beside the products of step n - 1; the scores of step n + 1
-        // follow (behind the last step: of whatever stands there, not used).
-        auto step = [&](int n, const DEAR_LDS bf16 *qs, const DEAR_LDS bf16 *gs, DEAR_LDS bf16 *qs_load, DEAR_LDS bf16 *gs_load) {
-            loads_barrier();
-            load(qs_load + (n / 2 + 1) % 2 * (STEP * W), gs_load + (n / 2 + 1) % 2 * (STEP * W));
-            frag<bf16> pn[2], dsn[2];
-            soften(pn, dsn, n);
-            accumulate(qs, gs);
-            p[0] = pn[0], p[1] = pn[1], ds[0] = dsn[0], ds[1] = dsn[1];
-            scores(qs, gs, n + 1);
-            load_done(n + 2);
-        };
-        // Step 0 has no products behind it.  Reads of scores begin with tile 0, those of products too; each goes on to the
-        // other place of its arrays every second step.
-        int n = 0;
-        scores((DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)gs0, 0);
-        load((DEAR_LDS bf16 *)qs0 + STEP * W, (DEAR_LDS bf16 *)gs0 + STEP * W);
-        soften(p, ds, 0);
-        scores((DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs1, 1);
-        load_done(2);
-        rd.turn_rows();
+#define DEAR_STEP(n, other)  \
+    loads_barrier();         \
+    DEAR_LOAD(other);        \
+    if (!step((DEAR_LDS bf16 *)qs##n, (DEAR_LDS bf16 *)gs##n, (DEAR_LDS float *)powers##n, (DEAR_LDS float *)deltas##n)) break;
         while (true) {
-            if (++n >= steps) break;
-            step(n, (DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)gs0, (DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs1);
-            if (++n >= steps) break;
-            step(n, (DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs1, (DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)gs0);
-            rd.turn_rows();
-            rd.turn_columns();
+            DEAR_STEP(0, 1)
+            DEAR_STEP(1, 0)
         }
-        if (n % 2) accumulate((DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)gs0);
-        else accumulate((DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)gs1);
-        // the other wave's sums, dk's and then dv's, where the tiles were
-        DEAR_LDS float *sums = wave / 2 ? (DEAR_LDS float *)qs1 : (DEAR_LDS float *)qs0;
+#undef DEAR_STEP
+#undef DEAR_LOAD
+    }
+    if (j >= a.kv_len) return;
+    store_row<bf16, W>(at(a.dk, b, kvh) + j * a.dk.token, dk, a.scale, a.head_dim, half);
+    store_row<bf16, W>(at(a.dv, b, kvh) + j * a.dv.token, dv, 1.f, a.head_dim, half);
+}
+
+// dk and dv of 64 keys a workgroup of eight waves, for rows of 128 values.  Four compute probabilities and dv, four the gradients of the scores
+// and dk: so each half needs the operands and sums of one of the two, two waves fit a SIMD, and there (waves w and w + 4)
+// one of either kind runs beside the other.  Two waves of a kind have the same 32 keys and take every other 32 queries;
+// their sums are added at the end.  Step n: the first kind computes s, p and dv of tile n and leaves p in LDS; the second
+// takes p of tile n - 1, its dp from the step before, and computes dk of tile n - 1, then dp of tile n.
+constexpr int KV_WAVES = 8;
+
+__global__ __launch_bounds__(64 * KV_WAVES, 2) void attention_dkv_halves_kernel(params a) {
+    constexpr int W = 128;
+    // Tiles in turn, three of the queries, as the one before is still read, and two of all else: arrays of their own, so that
+    // the compiler sees that the loads under way are not what a step reads.
+    __shared__ __attribute__((aligned(16))) bf16 qs0[STEP * W], qs1[STEP * W], qs2[STEP * W], gs0[STEP * W], gs1[STEP * W];
+    __shared__ __attribute__((aligned(16))) float powers0[STEP], powers1[STEP], deltas0[STEP], deltas1[STEP];
+    __shared__ __attribute__((aligned(16))) float ps[2][4][4][64 * 4];  // step, wave, quarter of its values: four a lane
+    int b, kvh, t;
+    place(a, a.kv_heads, 1, b, kvh, t);
+    const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
+    const int group = a.q_heads / a.kv_heads, part = wave & 3, turn = part & 1;
+    const bool second = wave >= 4;
+    const int wave_first = t * KEYS + part / 2 * 32, j = wave_first + (lane & 31);  // this lane's key
+    // queries first .. nq - 1 see it; those beyond nq have probabilities of 0 by their powers
+    const int first = j < nk ? (a.causal ? max(0, j - nk + nq) : 0) : nq;
+    const int wave_last = wave_first + 31 < nk ? (a.causal ? max(0, wave_first + 31 - nk + nq) : 0) : nq;
+    const int begin = t * KEYS >= nk ? nq : a.causal ? max(0, t * KEYS - nk + nq) / STEP * STEP : 0;
+    const int steps = begin < nq ? (nq - begin + STEP - 1) / STEP * group : 0;
+    const float c = a.scale * LOG2E;
+
+    f32x16 sum[W / 32] = {};  // dv, or dk
+    if (steps > 0) {
+        if (a.head_dim < W) {
+            for (DEAR_LDS bf16 *s : {(DEAR_LDS bf16 *)qs0, (DEAR_LDS bf16 *)qs1, (DEAR_LDS bf16 *)qs2, (DEAR_LDS bf16 *)gs0,
+                                     (DEAR_LDS bf16 *)gs1})
+                clear<W>(s);
+            __syncthreads();
+        }
+        const direct_loads<W, KV_WAVES> ql(a.q.token, a.head_dim, lane, wave), gl(a.dout.token, a.head_dim, lane, wave);
+        // the next step to be loaded: its queries, and its head's tensors
+        int h = kvh * group, next = begin, loaded = 0;
+        const char *qp = at(a.q, b, h) + begin * a.q.token, *gp = at(a.dout, b, h) + begin * a.dout.token;
+        auto load = [&](DEAR_LDS bf16 *qs, DEAR_LDS bf16 *gs, DEAR_LDS float *powers, DEAR_LDS float *deltas) {
+            if (loaded < steps) {
+                ql.load(qp, nq - next, qs, wave);
+                gl.load(gp, nq - next, gs, wave);
+                const int64_t row = ((int64_t)b * a.q_heads + h) * a.q_tiles * BLOCK + next + lane;
+                if (wave == 0) load_value_to_lds(a.powers + row, powers);
+                if (wave == 4) load_value_to_lds(a.deltas + row, deltas);
+                qp += STEP * a.q.token, gp += STEP * a.dout.token, next += STEP;
+                if (next >= nq) {
+                    h += 1, next = begin;
+                    qp = at(a.q, b, h) + begin * a.q.token, gp = at(a.dout, b, h) + begin * a.dout.token;
+                }
+            }
+            ++loaded;
+        };
+#define DEAR_LOAD(q, g) load((DEAR_LDS bf16 *)qs##q, (DEAR_LDS bf16 *)gs##g, (DEAR_LDS float *)powers##g, (DEAR_LDS float *)deltas##g)
+        DEAR_LOAD(0, 0);
+        frag<bf16> kv[W / 16];  // the keys, or the values
+        load_rows<bf16, W>(kv, second ? at(a.v, b, kvh) : at(a.k, b, kvh), second ? a.v.token : a.k.token, j, nk, a.head_dim, half);
+
+        // with the place of the 32 queries that are this wave's turn
+        direct<W> rd(lane);
+        rd.move(64 * W * turn);
+        if (!second) {
+            int i0 = begin;
+            auto step = [&](int n, const DEAR_LDS bf16 *qs, const DEAR_LDS bf16 *gs, const DEAR_LDS float *powers) {
+                f32x16 s = {};
+                if (i0 + 32 * turn < wave_last) {  // masked scores start, and stay, at -infinity
+                    __builtin_amdgcn_sched_barrier(0);  // keeps this a branch
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = i0 + 32 * turn + row_of(r, half) >= first ? 0.f : -INFINITY;
+                }
+                i0 += STEP;
+                if (i0 >= nq) i0 = begin;
+#pragma unroll
+                for (int kk = 0; kk < W / 16; ++kk) s = mma(rd.straight(qs, 0, kk), kv[kk], s);
+                frag<bf16> p[2];
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    float x[8];
+#pragma unroll
+                    for (int u = 0; u < 8; u += 4) {
+                        const f32x4 e = *(const DEAR_LDS f32x4 *)(powers + 32 * turn + row_of(8 * st + u, half));
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) x[u + w] = __builtin_amdgcn_exp2f(s[8 * st + u + w] * c - e[w]);
+                        *(DEAR_LDS f32x4 *)(&ps[n & 1][part][2 * st + u / 4][lane * 4]) = f32x4{x[u], x[u + 1], x[u + 2], x[u + 3]};
+                    }
+                    p[st] = to_frag<bf16>(x);
+                }
+#pragma unroll
+                for (int st = 0; st < 2; ++st)
+#pragma unroll
+                    for (int db = 0; db < W / 32; ++db) sum[db] = mma(rd.transposed(gs, 16 * st, db), p[st], sum[db]);
+            };
+            int n = 0;
+#define DEAR_STEP(q, g, q_load, g_load)                                                      \
+    loads_barrier();                                                                         \
+    if (n == steps) break;                                                                   \
+    DEAR_LOAD(q_load, g_load);                                                               \
+    step(n, (DEAR_LDS bf16 *)qs##q, (DEAR_LDS bf16 *)gs##g, (DEAR_LDS float *)powers##g);     \
+    ++n;
+            while (true) {
+                rd.renew();
+                DEAR_STEP(0, 0, 1, 1)
+                DEAR_STEP(1, 1, 2, 0)
+                DEAR_STEP(2, 0, 0, 1)
+                rd.renew();
+                DEAR_STEP(0, 1, 1, 0)
+                DEAR_STEP(1, 0, 2, 1)
+                DEAR_STEP(2, 1, 0, 0)
+            }
+#undef DEAR_STEP
+        } else {
+            f32x16 dp;
+            auto before = [&](int n, const DEAR_LDS bf16 *qs) {  // dk of tile n
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    float x[8];
+#pragma unroll
+                    for (int u = 0; u < 8; u += 4) {
+                        const f32x4 p = *(const DEAR_LDS f32x4 *)(&ps[n & 1][part][2 * st + u / 4][lane * 4]);
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) x[u + w] = p[w] * dp[8 * st + u + w];
+                    }
+                    const frag<bf16> ds = to_frag<bf16>(x);
+#pragma unroll
+                    for (int db = 0; db < W / 32; ++db) sum[db] = mma(rd.transposed(qs, 16 * st, db), ds, sum[db]);
+                }
+            };
+            auto step = [&](const DEAR_LDS bf16 *gs, const DEAR_LDS float *deltas) {
+#pragma unroll
+                for (int u = 0; u < 16; u += 4) {
+                    const f32x4 d = *(const DEAR_LDS f32x4 *)(deltas + 32 * turn + row_of(u, half));
+                    dp[u] = d[0], dp[u + 1] = d[1], dp[u + 2] = d[2], dp[u + 3] = d[3];
+                }
+#pragma unroll
+                for (int kk = 0; kk < W / 16; ++kk) dp = mma(rd.straight(gs, 0, kk), kv[kk], dp);
+            };
+            int n = 0;
+            loads_barrier();
+            DEAR_LOAD(1, 1);
+            step((DEAR_LDS bf16 *)gs0, (DEAR_LDS float *)deltas0);
+#define DEAR_STEP(q, g, q_load, g_load)                                     \
+    loads_barrier();                                                        \
+    before(n, (DEAR_LDS bf16 *)qs##q);                                      \
+    if (++n == steps) break;                                                \
+    DEAR_LOAD(q_load, g_load);                                              \
+    step((DEAR_LDS bf16 *)gs##g, (DEAR_LDS float *)deltas##g);
+            while (true) {
+                rd.renew();
+                DEAR_STEP(0, 1, 2, 0)
+                DEAR_STEP(1, 0, 0, 1)
+                DEAR_STEP(2, 1, 1, 0)
+                rd.renew();
+                DEAR_STEP(0, 0, 2, 1)
+                DEAR_STEP(1, 1, 0, 0)
+                DEAR_STEP(2, 0, 1, 1)
+            }
+#undef DEAR_STEP
+#undef DEAR_LOAD
+        }
+        // the sums of the wave with the other turn, where the tiles were
+        __syncthreads();
         static_assert(W / 32 * 16 * 64 * 4 <= STEP * W * 2, "the sums of 32 keys fit a tile");
-        for (f32x16 *x : {dk, dv}) {
-            __syncthreads();
+        DEAR_LDS float *sums = second ? (part / 2 ? (DEAR_LDS float *)gs1 : (DEAR_LDS float *)gs0)
+                                      : (part / 2 ? (DEAR_LDS float *)qs1 : (DEAR_LDS float *)qs0);
+        if (turn == 1) {
 #pragma unroll
             for (int db = 0; db < W / 32; ++db)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (turn == 1) sums[(db * 16 + r) * 64 + lane] = x[db][r];
-            __syncthreads();
+                for (int r = 0; r < 16; ++r) sums[(db * 16 + r) * 64 + lane] = sum[db][r];
+        }
+        __syncthreads();
+        if (turn == 0) {
 #pragma unroll
             for (int db = 0; db < W / 32; ++db)
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (turn == 0) x[db][r] += sums[(db * 16 + r) * 64 + lane];
+                for (int r = 0; r < 16; ++r) sum[db][r] += sums[(db * 16 + r) * 64 + lane];
         }
     }
     if (turn == 1 || j >= a.kv_len) return;
-    store_row<bf16, W>(at(a.dk, b, kvh) + j * a.dk.token, dk, a.scale, a.head_dim, half);
-    store_row<bf16, W>(at(a.dv, b, kvh) + j * a.dv.token, dv, 1.f, a.head_dim, half);
+    const heads &out = second ? a.dk : a.dv;
+    store_row<bf16, W>(at(out, b, kvh) + j * out.token, sum, second ? a.scale : 1.f, a.head_dim, half);
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -866,7 +985,7 @@ params make(const dear_attention_t *p) {
     a.q_lens = p->q_lens, a.kv_lens = p->kv_lens;
     a.q = t(p->q), a.k = t(p->k), a.v = t(p->v), a.out = t(p->out);
     a.dout = t(p->dout), a.dq = t(p->dq), a.dk = t(p->dk), a.dv = t(p->dv);
-    a.lse = p->lse, a.delta = (float *)p->workspace;
+    a.lse = p->lse;
     return a;
 }
 
@@ -899,7 +1018,7 @@ int dear_attention_workspace(const dear_attention_t *p, int64_t *bytes) {
 int dear_attention_backward_workspace(const dear_attention_t *p, int64_t *bytes) {
     if (!bytes) return DEAR_EINVAL;
     if (int rc = check_sizes(p)) return rc;
-    *bytes = p->q_len * p->batch * p->q_heads * 4;
+    *bytes = ceil_div(p->q_len, BLOCK) * BLOCK * p->batch * p->q_heads * 8;  // of every query of every tile two values
     return DEAR_OK;
 }
 
@@ -944,8 +1063,10 @@ int dear_attention_backward(const dear_attention_t *p, void *hip_stream) {
     params a = make(p);
     const bool direct = near(p, p->q) && near(p, p->dout) && near(p, p->k) && near(p, p->v);
     hipStream_t stream = (hipStream_t)hip_stream;
-    const int64_t q_tiles = ceil_div(p->q_len, BLOCK), kv_tiles = ceil_div(p->kv_len, KEYS);
+    const int64_t q_tiles = ceil_div(p->q_len, BLOCK), kv_tiles = ceil_div(p->kv_len, direct && p->head_dim <= 64 ? BLOCK : KEYS);
     if (too_big(p->q_heads, p->batch, q_tiles) || too_big(p->kv_heads, p->batch, kv_tiles)) return DEAR_ETOOBIG;
+    a.q_tiles = (int32_t)q_tiles;
+    a.powers = (float *)p->workspace, a.deltas = a.powers + q_tiles * BLOCK * p->batch * p->q_heads;
     if (q_tiles) {
         a.tiles = (int32_t)q_tiles;
         const unsigned grid = (unsigned)q_tiles * p->q_heads * p->batch;
@@ -957,8 +1078,8 @@ int dear_attention_backward(const dear_attention_t *p, void *hip_stream) {
     if (kv_tiles) {
         a.tiles = (int32_t)kv_tiles;
         const unsigned grid = (unsigned)kv_tiles * p->kv_heads * p->batch;
-        if (direct && p->head_dim <= 64) attention_dkv_direct_kernel<64><<<grid, THREADS, 0, stream>>>(a);
-        else if (direct) attention_dkv_direct_kernel<128><<<grid, THREADS, 0, stream>>>(a);
+        if (direct && p->head_dim <= 64) attention_dkv_direct_kernel<<<grid, THREADS, 0, stream>>>(a);
+        else if (direct) attention_dkv_halves_kernel<<<grid, 64 * KV_WAVES, 0, stream>>>(a);
         else DEAR_BY_TYPE(p, attention_dkv_kernel, grid, a, stream);
         if (int rc = launch_status()) return rc;
     }

@@ -150,14 +150,12 @@ template <int W> struct direct {
 #pragma unroll
         for (int db = 0; db < W / 32; ++db) asm("" : "+v"(column_at[db][0]), "+v"(column_at[db][1]));
     }
-    // To the other one of two tiles of 64 rows, one behind the other.
-    __device__ __forceinline__ void turn_rows() {
+    // By n bytes: a multiple of 32 rows.
+    __device__ __forceinline__ void move(int n) {
 #pragma unroll
-        for (int kk = 0; kk < W / 16; ++kk) row_at[kk] ^= 64 * W * 2;
-    }
-    __device__ __forceinline__ void turn_columns() {
+        for (int kk = 0; kk < W / 16; ++kk) row_at[kk] += n;
 #pragma unroll
-        for (int db = 0; db < W / 32; ++db) column_at[db][0] ^= 64 * W * 2, column_at[db][1] ^= 64 * W * 2;
+        for (int db = 0; db < W / 32; ++db) column_at[db][0] += n, column_at[db][1] += n;
     }
 
     // Rows row0 .. +31 (a multiple of 32), slots of step kk, as `straight`.
@@ -175,6 +173,11 @@ template <int W> struct direct {
 
 __device__ __forceinline__ void load_to_lds(const char *p, DEAR_LDS void *s) {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)p, s, 16, 0, 0);
+}
+
+// One value a lane.
+__device__ __forceinline__ void load_value_to_lds(const float *p, DEAR_LDS float *s) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)p, s, 4, 0, 0);
 }
 
 // Barrier behind which the tiles that this workgroup's waves have loaded to LDS are whole: each wave first waits for its
