@@ -1,6 +1,7 @@
 // Residual addition + root-mean-square norm with its backward pass, and checkpoints in 8 bits
 // (definitions: dear_ops.h).  All of it is bound by HBM.
 #include <cmath>
+#include <type_traits>
 
 #include "ops_common.h"
 
@@ -14,27 +15,28 @@ constexpr int GROUP = DEAR_CHECKPOINT_GROUP;
 constexpr int LANE = 8;  // neighbours that a lane holds: four lanes share a group
 
 // ------------------------------------------------------------------------------------ eight neighbours of a row
-// Whole vectors where rows start on multiples of 16 bytes and hold a multiple of 8 values, single values otherwise.
-// Values beyond the row are zeros.
+// Whole vectors, aligned where rows start on multiples of 16 bytes and hold a multiple of 8 values (VEC); otherwise from any
+// element on, which global memory allows, and single values at the row's end.  Values beyond the row are zeros.
+template <typename T> struct anywhere { typedef frag<T> type __attribute__((aligned(sizeof(T)))); };
+
 template <typename T, bool VEC> __device__ __forceinline__ void load8(float *x, const T *row, int col, int cols) {
-    if (VEC) {
-        if (col < cols) {
-            const frag<T> f = *(const frag<T> *)(row + col);
+    if (VEC ? col < cols : col + LANE <= cols) {
+        frag<T> f;
+        if (VEC) f = *(const frag<T> *)(row + col);
+        else f = *(const typename anywhere<T>::type *)(row + col);
 #pragma unroll
-            for (int t = 0; t < LANE; ++t) x[t] = (float)f[t];
-        } else {
-#pragma unroll
-            for (int t = 0; t < LANE; ++t) x[t] = 0.f;
-        }
+        for (int t = 0; t < LANE; ++t) x[t] = (float)f[t];
     } else {
 #pragma unroll
-        for (int t = 0; t < LANE; ++t) x[t] = col + t < cols ? (float)row[col + t] : 0.f;
+        for (int t = 0; t < LANE; ++t) x[t] = !VEC && col + t < cols ? (float)row[col + t] : 0.f;
     }
 }
 
 template <typename T, bool VEC> __device__ __forceinline__ void store8(T *row, const float *x, int col, int cols) {
     if (VEC) {
         if (col < cols) *(frag<T> *)(row + col) = to_frag<T>(x);
+    } else if (col + LANE <= cols) {
+        *(typename anywhere<T>::type *)(row + col) = to_frag<T>(x);
     } else {
 #pragma unroll
         for (int t = 0; t < LANE; ++t)
@@ -81,29 +83,42 @@ __device__ __forceinline__ void decode8(float *x, u32x2 codes, uint32_t exponent
     for (int t = 0; t < LANE; ++t) x[t] = (float)((int)(codes[t / 4] << (24 - 8 * (t % 4))) >> 24) * step;
 }
 
-template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void encode_kernel(const T *x, int64_t row_stride, int64_t rows, int32_t cols, uint32_t per_row,
+// Piece n of the rows: per_row pieces each, or, where per_row is 0, rows of whole groups that follow one another without gaps.
+template <typename INDEX> struct piece {
+    INDEX row;
+    int col, cols;
+    __device__ __forceinline__ piece(INDEX n, INDEX per_row, int32_t all) {
+        if (per_row == 0) {
+            row = n, col = 0, cols = LANE;
+        } else {
+            row = n / per_row, col = (int)(n - row * per_row) * LANE, cols = all;
+        }
+    }
+};
+
+template <typename T, bool VEC, typename INDEX>
+__global__ __launch_bounds__(256) void encode_kernel(const T *x, int64_t row_stride, INDEX total, int32_t cols, INDEX per_row,
                                                      int8_t *codes, uint8_t *exponents) {
-    const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = n / per_row;
-    if (row >= (uint64_t)rows) return;  // whole quads: per_row is a multiple of four
-    const int col = (int)(n - row * per_row) * LANE;
+    const INDEX n = (INDEX)blockIdx.x * 256 + threadIdx.x;
+    if (n >= total) return;  // whole quads: per_row is a multiple of four
+    const piece<INDEX> p(n, per_row, cols);
     float v[LANE];
-    load8<T, VEC>(v, x + row * row_stride, col, cols);
+    load8<T, VEC>(v, x + (int64_t)p.row * row_stride, p.col, p.cols);
     uint32_t e;
     const u32x2 c = encode8(v, e);
-    *(u32x2 *)(codes + n * LANE) = c;
+    *(u32x2 *)(codes + (int64_t)n * LANE) = c;
     if ((threadIdx.x & 3) == 0) exponents[n / 4] = (uint8_t)e;
 }
 
-template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void decode_kernel(const int8_t *codes, const uint8_t *exponents, int64_t rows, int32_t cols,
-                                                     uint32_t per_row, T *out) {
-    const uint64_t n = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = n / per_row;
-    if (row >= (uint64_t)rows) return;
-    const int col = (int)(n - row * per_row) * LANE;
+template <typename T, bool VEC, typename INDEX>
+__global__ __launch_bounds__(256) void decode_kernel(const int8_t *codes, const uint8_t *exponents, INDEX total, int32_t cols,
+                                                     INDEX per_row, T *out, int64_t row_stride) {
+    const INDEX n = (INDEX)blockIdx.x * 256 + threadIdx.x;
+    if (n >= total) return;
+    const piece<INDEX> p(n, per_row, cols);
     float v[LANE];
-    decode8(v, *(const u32x2 *)(codes + n * LANE), exponents[n / 4]);
-    store8<T, VEC>(out + row * cols, v, col, cols);
+    decode8(v, *(const u32x2 *)(codes + (int64_t)n * LANE), exponents[n / 4]);
+    store8<T, VEC>(out + (int64_t)p.row * row_stride, v, p.col, p.cols);
 }
 
 // ------------------------------------------------------------------------------------ norm
@@ -179,38 +194,53 @@ __global__ __launch_bounds__(block_of(TPR)) void norm_backward_kernel(const T *d
                                                                       const float *rstd, int64_t rows, int32_t cols, T *dx, float *part) {
     constexpr int RPB = block_of(TPR) / TPR;
     const int tid = threadIdx.x % TPR;
-    float w[V][LANE], dw[V][LANE];
+    // A row and the weights stay in registers, or, of the widest rows, come again for the second pass, from the L2 cache.
+    constexpr bool HOLD = V <= 2 || TPR == 64;
+    constexpr int H = HOLD ? V : 1;
+    float w[H][LANE], g[H][LANE], n[H][LANE], dw[V][LANE];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        load8<float, VEC>(w[i], weight, (i * TPR + tid) * LANE, cols);
+        if (HOLD) load8<float, VEC>(w[i % H], weight, (i * TPR + tid) * LANE, cols);
 #pragma unroll
         for (int t = 0; t < LANE; ++t) dw[i][t] = 0.f;
     }
     for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR; row < rows; row += (int64_t)gridDim.x * RPB) {
         const float r = rstd[row];
-        float g[V][LANE], n[V][LANE], sum = 0.f;
+        auto load = [&](int i) {  // n: the normed row, g: dy * weight
+            const int col = (i * TPR + tid) * LANE, k = i % H;
+            load8<T, VEC>(g[k], dy + row * dy_stride, col, cols);
+            load8<T, VEC>(n[k], h + row * h_stride, col, cols);
+            if (!HOLD) load8<float, VEC>(w[k], weight, col, cols);
+        };
+        float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int col = (i * TPR + tid) * LANE;
-            load8<T, VEC>(g[i], dy + row * dy_stride, col, cols);
-            load8<T, VEC>(n[i], h + row * h_stride, col, cols);
+            const int k = i % H;
+            load(i);
 #pragma unroll
             for (int t = 0; t < LANE; ++t) {
-                n[i][t] *= r;
-                dw[i][t] += g[i][t] * n[i][t];
-                g[i][t] *= w[i][t];
-                sum += g[i][t] * n[i][t];
+                n[k][t] *= r;
+                dw[i][t] += g[k][t] * n[k][t];
+                g[k][t] *= w[k][t];
+                sum += g[k][t] * n[k][t];
             }
+            if (!HOLD) __builtin_amdgcn_sched_barrier(0);  // one vector after another: their loads together do not fit
         }
         const float mean = row_sum<TPR>(sum) / (float)cols;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int col = (i * TPR + tid) * LANE;
+            const int col = (i * TPR + tid) * LANE, k = i % H;
+            if (!HOLD) {
+                load(i);
+#pragma unroll
+                for (int t = 0; t < LANE; ++t) n[k][t] *= r, g[k][t] *= w[k][t];
+            }
             float d[LANE];
             if (dh) load8<T, VEC>(d, dh + row * dh_stride, col, cols);
 #pragma unroll
-            for (int t = 0; t < LANE; ++t) g[i][t] = (g[i][t] - n[i][t] * mean) * r + (dh ? d[t] : 0.f);
-            store8<T, VEC>(dx + row * cols, g[i], col, cols);
+            for (int t = 0; t < LANE; ++t) g[k][t] = (g[k][t] - n[k][t] * mean) * r + (dh ? d[t] : 0.f);
+            store8<T, VEC>(dx + row * cols, g[k], col, cols);
+            if (!HOLD) __builtin_amdgcn_sched_barrier(0);
         }
     }
     float *out = part + (int64_t)blockIdx.x * cols;
@@ -263,8 +293,6 @@ __global__ __launch_bounds__(64 * SUM_WAVES) void column_sum_kernel(const float 
 }
 
 // ------------------------------------------------------------------------------------ host
-constexpr int BACKWARD_GROUPS = 512;  // workgroups of the backward pass, and rows of its workspace, at most
-
 int size_of(int32_t dtype) { return dtype == DEAR_BF16 ? 2 : 4; }
 bool known(int32_t dtype) { return dtype == DEAR_BF16 || dtype == DEAR_F32; }
 
@@ -273,39 +301,31 @@ bool vectors(const void *p, int64_t stride, int64_t cols, int n) {
     return !p || (aligned(p, 16) && stride * n % 16 == 0 && cols % LANE == 0);
 }
 
-int threads_of_row(int64_t cols) { return cols <= 2048 ? 64 : cols <= 8192 ? 256 : 1024; }
+// Threads of a row: a wave up to 2048 columns, then as many as it takes for two vectors each, or for four of the widest.
+int threads_of_row(int64_t cols) { return cols <= 2048 ? 64 : cols <= 4096 ? 256 : cols <= 8192 ? 512 : 1024; }
 
+// Workgroups of the backward pass, and rows of its workspace: as many as fill the chip with rows under way.  8192 rows of
+// 1024 and 4096 columns: 512 / 1024 / 2048 workgroups 18.0 / 18.0 / 22.2 and 67 / 52 / 62 us.
 int backward_groups(int64_t rows, int64_t cols) {
-    const int64_t per = cols <= 2048 ? 4 : 1;
-    const int64_t n = ceil_div(rows, per);
-    return (int)(n < BACKWARD_GROUPS ? n : BACKWARD_GROUPS);
+    const int64_t n = ceil_div(rows, cols <= 2048 ? 4 : 1), most = cols <= 4096 ? 1024 : 512;
+    return (int)(n < most ? n : most);
 }
 
 template <typename T, int TPR, int V, bool VEC, typename F> void call(F f) { f.template operator()<T, TPR, V, VEC>(); }
 
-// Calls f for the type, the threads of a row and its vectors; rows that are read value by value take the most vectors.
+// Calls f for the type, the threads of a row and its vectors.
 template <typename T, bool VEC, typename F> void by_cols(int64_t cols, F f) {
-    const int tpr = threads_of_row(cols);
-    const int v = VEC ? (int)ceil_div(cols, tpr * LANE) : 4;
+    const int tpr = threads_of_row(cols), v = (int)ceil_div(cols, tpr * LANE);
     if (tpr == 64) {
-        if constexpr (VEC) {
-            if (v == 1) return call<T, 64, 1, VEC>(f);
-            if (v == 2) return call<T, 64, 2, VEC>(f);
-            if (v == 3) return call<T, 64, 3, VEC>(f);
-        }
+        if (v == 1) return call<T, 64, 1, VEC>(f);
+        if (v == 2) return call<T, 64, 2, VEC>(f);
+        if (v == 3) return call<T, 64, 3, VEC>(f);
         return call<T, 64, 4, VEC>(f);
     }
-    if (tpr == 256) {
-        if constexpr (VEC) {
-            if (v == 2) return call<T, 256, 2, VEC>(f);
-            if (v == 3) return call<T, 256, 3, VEC>(f);
-        }
-        return call<T, 256, 4, VEC>(f);
-    }
-    if constexpr (VEC) {
-        if (v == 2) return call<T, 1024, 2, VEC>(f);
-        if (v == 3) return call<T, 1024, 3, VEC>(f);
-    }
+    if (tpr == 256) return call<T, 256, 2, VEC>(f);
+    if (tpr == 512) return call<T, 512, 2, VEC>(f);
+    if (v <= 2) return call<T, 1024, 2, VEC>(f);
+    if (v == 3) return call<T, 1024, 3, VEC>(f);
     return call<T, 1024, 4, VEC>(f);
 }
 
@@ -353,6 +373,35 @@ struct backward_call {
     }
 };
 
+// Pieces of the rows of a checkpoint, and of one row, or 0 where rows without gaps (`dense`) are of whole groups.
+struct pieces {
+    int64_t total, per_row;
+    unsigned grid;
+};
+
+int count(int64_t rows, int64_t cols, bool dense, pieces &n) {
+    n.per_row = ceil_div(cols, GROUP) * (GROUP / LANE);
+    if (rows > INT64_MAX / 4 / n.per_row || ceil_div(rows * n.per_row, 256) > INT32_MAX) return DEAR_ETOOBIG;
+    n.total = rows * n.per_row;
+    n.grid = (unsigned)ceil_div(n.total, 256);
+    if (dense && cols % GROUP == 0) n.per_row = 0;
+    return DEAR_OK;
+}
+
+// Calls f with values of the type, of whether there are whole vectors, and of the pieces' index: 64 bits where 32 do not do.
+template <typename F> void by_types(int32_t dtype, bool vec, int64_t total, F f) {
+    auto by_index = [&](auto t, auto v) {
+        if (total <= INT32_MAX) f(t, v, uint32_t());
+        else f(t, v, uint64_t());
+    };
+    auto by_vec = [&](auto t) {
+        if (vec) by_index(t, std::true_type());
+        else by_index(t, std::false_type());
+    };
+    if (dtype == DEAR_BF16) by_vec(bf16());
+    else by_vec(float());
+}
+
 // A tensor that is read row by row.
 int check_rows(const void *p, int64_t stride, int32_t dtype, int64_t rows, int64_t cols) {
     if (!p || (rows > 1 && stride < cols)) return DEAR_EINVAL;
@@ -370,18 +419,17 @@ int dear_checkpoint_encode(const void *x, int32_t dtype, int64_t rows, int64_t c
     if (int rc = check_rows(x, row_stride, dtype, rows, cols)) return rc;
     if (!codes || !exponents) return DEAR_EINVAL;
     if (!aligned(codes, 16)) return DEAR_EALIGN;
-    const int64_t per_row = ceil_div(cols, GROUP) * (GROUP / LANE);
-    if (rows > INT64_MAX / 4 / per_row || ceil_div(rows * per_row, 256) > INT32_MAX) return DEAR_ETOOBIG;
-    const unsigned grid = (unsigned)ceil_div(rows * per_row, 256);
-    const bool vec = vectors(x, row_stride, cols, size_of(dtype));
+    pieces n;
+    if (int rc = count(rows, cols, vectors(x, row_stride, cols, size_of(dtype)) && (row_stride == cols || rows == 1), n)) return rc;
     hipStream_t s = (hipStream_t)hip_stream;
-#define DEAR_ENCODE(T, VEC) \
-    encode_kernel<T, VEC><<<grid, 256, 0, s>>>((const T *)x, row_stride, rows, (int32_t)cols, (uint32_t)per_row, codes, exponents)
-    if (dtype == DEAR_BF16 && vec) DEAR_ENCODE(bf16, true);
-    else if (dtype == DEAR_BF16) DEAR_ENCODE(bf16, false);
-    else if (vec) DEAR_ENCODE(float, true);
-    else DEAR_ENCODE(float, false);
-#undef DEAR_ENCODE
+    const bool vec = vectors(x, row_stride, cols, size_of(dtype));
+    const int64_t stride = n.per_row ? row_stride : LANE;
+    by_types(dtype, vec, n.total, [&](auto t, auto v, auto index) {
+        typedef decltype(t) T;
+        typedef decltype(index) INDEX;
+        encode_kernel<T, decltype(v)::value, INDEX>
+            <<<n.grid, 256, 0, s>>>((const T *)x, stride, (INDEX)n.total, (int32_t)cols, (INDEX)n.per_row, codes, exponents);
+    });
     return launch_status();
 }
 
@@ -391,18 +439,17 @@ int dear_checkpoint_decode(const int8_t *codes, const uint8_t *exponents, int64_
     if (rows == 0) return DEAR_OK;
     if (!codes || !exponents || !out) return DEAR_EINVAL;
     if (!aligned(codes, 16) || !aligned(out, size_of(dtype))) return DEAR_EALIGN;
-    const int64_t per_row = ceil_div(cols, GROUP) * (GROUP / LANE);
-    if (rows > INT64_MAX / 4 / per_row || ceil_div(rows * per_row, 256) > INT32_MAX) return DEAR_ETOOBIG;
-    const unsigned grid = (unsigned)ceil_div(rows * per_row, 256);
-    const bool vec = vectors(out, cols, cols, size_of(dtype));
+    pieces n;
+    if (int rc = count(rows, cols, vectors(out, cols, cols, size_of(dtype)), n)) return rc;
     hipStream_t s = (hipStream_t)hip_stream;
-#define DEAR_DECODE(T, VEC) \
-    decode_kernel<T, VEC><<<grid, 256, 0, s>>>(codes, exponents, rows, (int32_t)cols, (uint32_t)per_row, (T *)out)
-    if (dtype == DEAR_BF16 && vec) DEAR_DECODE(bf16, true);
-    else if (dtype == DEAR_BF16) DEAR_DECODE(bf16, false);
-    else if (vec) DEAR_DECODE(float, true);
-    else DEAR_DECODE(float, false);
-#undef DEAR_DECODE
+    const bool vec = vectors(out, cols, cols, size_of(dtype));
+    const int64_t stride = n.per_row ? cols : LANE;
+    by_types(dtype, vec, n.total, [&](auto t, auto v, auto index) {
+        typedef decltype(t) T;
+        typedef decltype(index) INDEX;
+        decode_kernel<T, decltype(v)::value, INDEX>
+            <<<n.grid, 256, 0, s>>>(codes, exponents, (INDEX)n.total, (int32_t)cols, (INDEX)n.per_row, (T *)out, stride);
+    });
     return launch_status();
 }
 

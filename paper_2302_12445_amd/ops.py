@@ -15,6 +15,7 @@ loading raises.  layers.py has the autograd functions over these calls.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 import os
 import struct
@@ -86,21 +87,21 @@ def _like(t: torch.Tensor, ref: torch.Tensor, what: str) -> None:
         raise ValueError("%s is %s on %s, expected %s on %s" % (what, t.dtype, t.device, ref.dtype, ref.device))
 
 
-class _on:
-    """Makes a tensor's device the current one, where it is not, and gives its current stream."""
+# neither is a name that torch promises to keep
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
-    def __init__(self, t: torch.Tensor):
-        self.index = t.device.index
-        self.guard = None if self.index == torch.cuda.current_device() else torch.cuda.device(self.index)
 
-    def __enter__(self) -> int:
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch.cuda.current_stream(self.index).cuda_stream
-
-    def __exit__(self, *exc) -> None:
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _on_its_device(f):
+    """Makes the device of the call's first tensor the current one, where it is not."""
+    @functools.wraps(f)
+    def call(t, *args, **kwargs):
+        first = t.codes if type(t) is Checkpoint else t
+        if not first.is_cuda or first.get_device() == _current_device():
+            return f(t, *args, **kwargs)
+        with torch.cuda.device(first.device):
+            return f(t, *args, **kwargs)
+    return call
 
 
 # ------------------------------------------------------------------------------------ attention
@@ -109,45 +110,54 @@ _ATTENTION = struct.Struct("@4i2q2ifi2Q" + "Q3q" * 4 + "Q" + "Q3q" * 4 + "Qq")
 _NONE = (0, 0, 0, 0)
 
 
-def _readable(t: torch.Tensor, what: str) -> torch.Tensor:
-    """The tensor, or a copy of it that the library can read: head_dim contiguous, pieces of 16 bytes."""
-    if t.dim() != 4:
-        raise ValueError("%s has shape %s, expected [batch, tokens, heads, head_dim]" % (what, tuple(t.shape)))
-    unit = 16 // t.element_size()
-    s = t.stride()
-    # a stride along an axis of one element says nothing, and may be anything
-    fine = (s[3] == 1 or t.shape[3] == 1) and t.data_ptr() % 16 == 0 and all(s[i] % unit == 0 for i in range(3) if t.shape[i] > 1)
-    return t if fine else t.contiguous().clone() if t.data_ptr() % 16 else t.contiguous()
+def _readable(t: torch.Tensor, what: str):
+    """The tensor, or a copy of it that the library can read (head_dim contiguous, pieces of 16 bytes), and its address and
+    strides, those along axes of one element, which say nothing, as 0."""
+    n = t.shape
+    if len(n) != 4:
+        raise ValueError("%s has shape %s, expected [batch, tokens, heads, head_dim]" % (what, tuple(n)))
+    at, unit = t.data_ptr(), 16 // t.element_size()
+    if not t.is_contiguous() or at % 16:
+        s = t.stride()
+        batch, token, head = s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0, s[2] if n[2] > 1 else 0
+        if (s[3] == 1 or n[3] == 1) and at % 16 == 0 and batch % unit == 0 and token % unit == 0 and head % unit == 0:
+            return t, (at, batch, token, head)
+        t = t.clone(memory_format=torch.contiguous_format)
+        at = t.data_ptr()
+    return t, (at, n[1] * n[2] * n[3], n[2] * n[3], n[3])
 
 
-def _strided(t: torch.Tensor) -> Tuple[int, int, int, int]:
-    """Address and strides; strides along axes of one element as 0."""
-    s, n = t.stride(), t.shape
-    return t.data_ptr(), s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0, s[2] if n[2] > 1 else 0
+def _empty_as(t: torch.Tensor) -> torch.Tensor:
+    """A contiguous output of a tensor's shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
-def _attention_sizes(q, k, v, scale, q_lens, kv_lens):
+def _new(like: torch.Tensor, shape):
+    """A contiguous output of the shape, and its address and strides."""
+    t = _empty_as(like) if like.shape == shape else torch.empty(shape, dtype=like.dtype, device=like.device)
+    return t, (t.data_ptr(), shape[1] * shape[2] * shape[3], shape[2] * shape[3], shape[3])
+
+
+def _attention_sizes(q, k, v, causal, scale, q_lens, kv_lens):
+    """(q, k, v) as the library reads them, their places, and the leading members of dear_attention_t."""
     d = _dtype(q, "q")
     _like(k, q, "k")
     _like(v, q, "v")
-    q, k, v = _readable(q, "q"), _readable(k, "k"), _readable(v, "v")
+    (q, pq), (k, pk), (v, pv) = _readable(q, "q"), _readable(k, "k"), _readable(v, "v")
     B, Sq, H, D = q.shape
-    if k.shape != v.shape or k.shape[0] != B or k.shape[3] != D:
+    Bk, Sk, Hkv, Dk = k.shape
+    if k.shape != v.shape or Bk != B or Dk != D:
         raise ValueError("shapes do not agree: q %s, k %s, v %s" % (tuple(q.shape), tuple(k.shape), tuple(v.shape)))
     for lens, what in ((q_lens, "q_lens"), (kv_lens, "kv_lens")):
         if lens is not None and (lens.dtype != torch.int32 or lens.device != q.device or lens.shape != (B,) or not lens.is_contiguous()):
             raise ValueError("%s: expected a contiguous int32 tensor of %d on %s" % (what, B, q.device))
-    scale = 1.0 / math.sqrt(D) if scale is None else float(scale)
-    return q, k, v, (B, H, k.shape[2], D, Sq, k.shape[1], d), scale
+    # (head_dim 0 is refused by the library)
+    scale = 1.0 / math.sqrt(D or 1) if scale is None else float(scale)
+    return (q, k, v), (*pq, *pk, *pv), (B, H, Hkv, D, Sq, Sk, d, 1 if causal else 0, scale, 0,
+                                        0 if q_lens is None else q_lens.data_ptr(), 0 if kv_lens is None else kv_lens.data_ptr())
 
 
-def _attention_bytes(sizes, scale, causal, q_lens, kv_lens, q, k, v, out, lse, dout=_NONE, dq=_NONE, dk=_NONE, dv=_NONE,
-                     workspace=0, workspace_bytes=0) -> bytes:
-    return _ATTENTION.pack(*sizes, 1 if causal else 0, scale, 0, 0 if q_lens is None else q_lens.data_ptr(),
-                           0 if kv_lens is None else kv_lens.data_ptr(), *q, *k, *v, *out, lse, *dout, *dq, *dk, *dv,
-                           workspace, workspace_bytes)
-
-
+@_on_its_device
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
               q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None
               ) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -156,49 +166,45 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
     Gives (out [B, Sq, H, D], lse [B, H, Sq] fp32).  scale: 1 / sqrt(D) by default.  q_lens, kv_lens: int32 [B], the
     valid tokens of each sequence.  causal: the last valid query sees all valid keys, the one before it one less.
     """
-    q, k, v, sizes, scale = _attention_sizes(q, k, v, scale, q_lens, kv_lens)
-    B, H, _, D, Sq = sizes[:5]
+    kept, places, head = _attention_sizes(q, k, v, causal, scale, q_lens, kv_lens)  # kept: until the work is enqueued
+    B, H, _, D, Sq = head[:5]
     lib = load_library()
-    with _on(q) as stream:
-        out = torch.empty((B, Sq, H, D), dtype=q.dtype, device=q.device)
-        lse = torch.empty((B, H, Sq), dtype=torch.float32, device=q.device)
-        need = C.c_int64()
-        args = (sizes, scale, causal, q_lens, kv_lens, _strided(q), _strided(k), _strided(v), _strided(out), lse.data_ptr())
-        packed = _attention_bytes(*args)
-        _check(lib.dear_attention_workspace(packed, C.byref(need)), "dear_attention_workspace")
-        if need.value:
-            space = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-            packed = _attention_bytes(*args, workspace=space.data_ptr(), workspace_bytes=need.value)
-        _check(lib.dear_attention(packed, stream), "dear_attention")
+    out, po = _new(q, (B, Sq, H, D))
+    lse = torch.empty((B, H, Sq), dtype=torch.float32, device=q.device)
+    args = (*head, *places, *po, lse.data_ptr(), *_NONE, *_NONE, *_NONE, *_NONE)
+    packed = _ATTENTION.pack(*args, 0, 0)
+    need = C.c_int64()
+    _check(lib.dear_attention_workspace(packed, C.byref(need)), "dear_attention_workspace")
+    if need.value:
+        space = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+        packed = _ATTENTION.pack(*args, space.data_ptr(), need.value)
+    _check(lib.dear_attention(packed, _raw_stream(q.get_device())), "dear_attention")
     return out, lse
 
 
+@_on_its_device
 def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
                        lse: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
                        q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None
                        ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Gradients (dq, dk, dv) from the gradient of out and what attention() gave, with the same arguments."""
-    q, k, v, sizes, scale = _attention_sizes(q, k, v, scale, q_lens, kv_lens)
-    B, H, Hkv, D, Sq, Sk = sizes[:6]
+    kept, places, head = _attention_sizes(q, k, v, causal, scale, q_lens, kv_lens)
+    B, H, Hkv, D, Sq, Sk = head[:6]
     _like(out, q, "out")
     _like(dout, q, "dout")
     if out.shape != q.shape or dout.shape != q.shape:
         raise ValueError("out %s and dout %s: expected %s" % (tuple(out.shape), tuple(dout.shape), tuple(q.shape)))
     if lse.dtype != torch.float32 or lse.device != q.device or lse.shape != (B, H, Sq) or not lse.is_contiguous():
         raise ValueError("lse: expected a contiguous float32 tensor of shape %s on %s" % ((B, H, Sq), q.device))
-    out, dout = _readable(out, "out"), _readable(dout, "dout")
+    (out, po), (dout, pd) = _readable(out, "out"), _readable(dout, "dout")
     lib = load_library()
-    with _on(q) as stream:
-        dq = torch.empty((B, Sq, H, D), dtype=q.dtype, device=q.device)
-        dk = torch.empty((B, Sk, Hkv, D), dtype=q.dtype, device=q.device)
-        dv = torch.empty((B, Sk, Hkv, D), dtype=q.dtype, device=q.device)
-        need = C.c_int64()
-        args = (sizes, scale, causal, q_lens, kv_lens, _strided(q), _strided(k), _strided(v), _strided(out), lse.data_ptr(),
-                _strided(dout), _strided(dq), _strided(dk), _strided(dv))
-        _check(lib.dear_attention_backward_workspace(_attention_bytes(*args), C.byref(need)), "dear_attention_backward_workspace")
-        space = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-        packed = _attention_bytes(*args, workspace=space.data_ptr(), workspace_bytes=need.value)
-        _check(lib.dear_attention_backward(packed, stream), "dear_attention_backward")
+    (dq, gq), (dk, gk), (dv, gv) = _new(q, (B, Sq, H, D)), _new(k, (B, Sk, Hkv, D)), _new(v, (B, Sk, Hkv, D))
+    args = (*head, *places, *po, lse.data_ptr(), *pd, *gq, *gk, *gv)
+    need = C.c_int64()
+    _check(lib.dear_attention_backward_workspace(_ATTENTION.pack(*args, 0, 0), C.byref(need)), "dear_attention_backward_workspace")
+    space = torch.empty(need.value, dtype=torch.uint8, device=q.device)
+    _check(lib.dear_attention_backward(_ATTENTION.pack(*args, space.data_ptr(), need.value), _raw_stream(q.get_device())),
+           "dear_attention_backward")
     return dq, dk, dv
 
 
@@ -211,16 +217,19 @@ class Checkpoint(NamedTuple):
     cols: int
 
 
-def _as_rows(t: torch.Tensor, what: str) -> torch.Tensor:
-    """[..., cols] as [rows, cols] with contiguous columns, copied only if its rows lie at no one distance."""
-    if t.dim() < 1 or t.shape[-1] < 1:
-        raise ValueError("%s has shape %s, expected [..., cols]" % (what, tuple(t.shape)))
-    r = t.reshape(-1, t.shape[-1]) if t.dim() != 2 else t
-    return r if (r.stride(1) == 1 or r.shape[1] == 1) and (r.shape[0] <= 1 or r.stride(0) >= r.shape[1]) else r.contiguous()
-
-
-def _stride(r: torch.Tensor) -> int:
-    return r.stride(0) if r.shape[0] > 1 else r.shape[1]
+def _as_rows(t: torch.Tensor, what: str) -> Tuple[torch.Tensor, int, int, int]:
+    """[..., cols] as rows of contiguous columns, copied only if the rows lie at no one distance: the tensor, rows, cols,
+    elements from row to row."""
+    n = t.shape
+    if not n or n[-1] < 1:
+        raise ValueError("%s has shape %s, expected [..., cols]" % (what, tuple(n)))
+    cols = n[-1]
+    if t.is_contiguous():
+        return t, t.numel() // cols, cols, cols
+    r = t if len(n) == 2 else t.reshape(-1, cols)
+    if (r.stride(1) != 1 and cols > 1) or (r.shape[0] > 1 and r.stride(0) < cols):
+        r = r.contiguous()
+    return r, r.shape[0], cols, r.stride(0) if r.shape[0] > 1 else cols
 
 
 def _empty_checkpoint(rows: int, cols: int, device) -> Checkpoint:
@@ -241,49 +250,49 @@ def _checkpoint(kept: Checkpoint) -> int:
     return rows
 
 
+@_on_its_device
 def checkpoint_encode(x: torch.Tensor) -> Checkpoint:
     """x [..., cols] in 8 bits: 32 neighbours of a row share the smallest power of two with which they fit 127."""
     d = _dtype(x, "x")
-    r = _as_rows(x, "x")
-    lib = load_library()
-    with _on(x) as stream:
-        kept = _empty_checkpoint(r.shape[0], r.shape[1], x.device)
-        _check(lib.dear_checkpoint_encode(r.data_ptr(), d, r.shape[0], r.shape[1], _stride(r), kept.codes.data_ptr(),
-                                          kept.exponents.data_ptr(), stream), "dear_checkpoint_encode")
+    r, rows, cols, stride = _as_rows(x, "x")
+    kept = _empty_checkpoint(rows, cols, x.device)
+    _check(load_library().dear_checkpoint_encode(r.data_ptr(), d, rows, cols, stride, kept.codes.data_ptr(), kept.exponents.data_ptr(),
+                                                 _raw_stream(x.get_device())), "dear_checkpoint_encode")
     return kept
 
 
+@_on_its_device
 def checkpoint_decode(kept: Checkpoint, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """What a checkpoint holds, [rows, cols]; exact in either type."""
     rows = _checkpoint(kept)
     if dtype not in _DTYPE:
         raise ValueError("%s: bfloat16 and float32 are supported" % dtype)
-    lib = load_library()
-    with _on(kept.codes) as stream:
-        out = torch.empty((rows, kept.cols), dtype=dtype, device=kept.codes.device)
-        _check(lib.dear_checkpoint_decode(kept.codes.data_ptr(), kept.exponents.data_ptr(), rows, kept.cols, _DTYPE[dtype],
-                                          out.data_ptr(), stream), "dear_checkpoint_decode")
+    codes, exponents, cols = kept
+    out = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+    _check(load_library().dear_checkpoint_decode(codes.data_ptr(), exponents.data_ptr(), rows, cols, _DTYPE[dtype], out.data_ptr(),
+                                                 _raw_stream(codes.get_device())), "dear_checkpoint_decode")
     return out
 
 
+@_on_its_device
 def checkpoint_weight_grad(dy: torch.Tensor, kept: Checkpoint) -> torch.Tensor:
     """Gradient [outs, ins] in fp32 of a linear layer's weight, from its output's gradient dy [..., outs] and the
     checkpoint of its input [rows, ins]."""
     rows = _checkpoint(kept)
     d = _dtype(dy, "dy")
-    r = _as_rows(dy, "dy")
-    if r.shape[0] != rows or dy.device != kept.codes.device:
-        raise ValueError("dy has %d rows on %s, the checkpoint %d on %s" % (r.shape[0], dy.device, rows, kept.codes.device))
-    outs, ins = r.shape[1], kept.cols
+    r, dy_rows, outs, stride = _as_rows(dy, "dy")
+    codes, exponents, ins = kept
+    if dy_rows != rows or dy.device != codes.device:
+        raise ValueError("dy has %d rows on %s, the checkpoint %d on %s" % (dy_rows, dy.device, rows, codes.device))
     lib = load_library()
-    with _on(dy) as stream:
-        dw = torch.empty((outs, ins), dtype=torch.float32, device=dy.device)
-        need = C.c_int64()
-        _check(lib.dear_checkpoint_weight_grad_workspace(d, rows, outs, ins, C.byref(need)), "dear_checkpoint_weight_grad_workspace")
+    dw = torch.empty((outs, ins), dtype=torch.float32, device=dy.device)
+    need, space = C.c_int64(), None
+    _check(lib.dear_checkpoint_weight_grad_workspace(d, rows, outs, ins, C.byref(need)), "dear_checkpoint_weight_grad_workspace")
+    if need.value:
         space = torch.empty(need.value, dtype=torch.uint8, device=dy.device)
-        _check(lib.dear_checkpoint_weight_grad(r.data_ptr(), d, _stride(r), kept.codes.data_ptr(), kept.exponents.data_ptr(), rows,
-                                               outs, ins, dw.data_ptr(), space.data_ptr(), need.value, stream),
-               "dear_checkpoint_weight_grad")
+    _check(lib.dear_checkpoint_weight_grad(r.data_ptr(), d, stride, codes.data_ptr(), exponents.data_ptr(), rows, outs, ins, dw.data_ptr(),
+                                           None if space is None else space.data_ptr(), need.value, _raw_stream(dy.get_device())),
+           "dear_checkpoint_weight_grad")
     return dw
 
 
@@ -293,6 +302,7 @@ def _weight(weight: torch.Tensor, cols: int, device) -> None:
         raise ValueError("weight: expected a contiguous float32 tensor of %d on %s" % (cols, device))
 
 
+@_on_its_device
 def add_rms_norm(x: torch.Tensor, residual: Optional[torch.Tensor], weight: torch.Tensor, eps: float = 1e-5,
                  keep: bool = True) -> Tuple[torch.Tensor, torch.Tensor, Optional[Checkpoint], torch.Tensor]:
     """h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight over the last axis.
@@ -301,54 +311,53 @@ def add_rms_norm(x: torch.Tensor, residual: Optional[torch.Tensor], weight: torc
     rstd fp32 [rows].  residual None: h is x itself.  weight: fp32.
     """
     d = _dtype(x, "x")
-    r = _as_rows(x, "x")
-    rows, cols = r.shape
-    _weight(weight, cols, x.device)
-    add = None
+    r, rows, cols, stride = _as_rows(x, "x")
+    device, shape = x.device, x.shape
+    _weight(weight, cols, device)
+    h, h_at, add, add_at, add_stride = x, None, None, None, 0
     if residual is not None:
         _like(residual, x, "residual")
-        if residual.shape != x.shape:
-            raise ValueError("residual has shape %s, x %s" % (tuple(residual.shape), tuple(x.shape)))
-        add = _as_rows(residual, "residual")
-    lib = load_library()
-    with _on(x) as stream:
-        h = x if add is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        rstd = torch.empty(rows, dtype=torch.float32, device=x.device)
-        kept = _empty_checkpoint(rows, cols, x.device) if keep else None
-        _check(lib.dear_add_rms_norm(
-            r.data_ptr(), _stride(r), None if add is None else add.data_ptr(), 0 if add is None else _stride(add),
-            weight.data_ptr(), d, rows, cols, eps, None if add is None else h.data_ptr(), y.data_ptr(),
-            kept.codes.data_ptr() if keep else None, kept.exponents.data_ptr() if keep else None, rstd.data_ptr(), stream),
-            "dear_add_rms_norm")
+        if residual.shape != shape:
+            raise ValueError("residual has shape %s, x %s" % (tuple(residual.shape), tuple(shape)))
+        add, _, _, add_stride = _as_rows(residual, "residual")
+        h = _empty_as(x)
+        h_at, add_at = h.data_ptr(), add.data_ptr()
+    y = _empty_as(x)
+    rstd = torch.empty(rows, dtype=torch.float32, device=device)
+    kept = _empty_checkpoint(rows, cols, device) if keep else None
+    _check(load_library().dear_add_rms_norm(
+        r.data_ptr(), stride, add_at, add_stride, weight.data_ptr(), d, rows, cols, eps, h_at, y.data_ptr(),
+        kept.codes.data_ptr() if keep else None, kept.exponents.data_ptr() if keep else None, rstd.data_ptr(),
+        _raw_stream(x.get_device())), "dear_add_rms_norm")
     return h, y, kept, rstd
 
 
+@_on_its_device
 def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor,
                           dh: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Gradients (dx, dweight): dx of x and of residual alike, dweight fp32.  dh: the gradient that reaches h by other
     ways than the norm."""
     d = _dtype(dy, "dy")
-    given = [(dy, "dy"), (h, "h")] + ([(dh, "dh")] if dh is not None else [])
-    for t, what in given[1:]:
-        _like(t, dy, what)
-        if t.shape != dy.shape:
-            raise ValueError("%s has shape %s, dy %s" % (what, tuple(t.shape), tuple(dy.shape)))
-    ry, rh = _as_rows(dy, "dy"), _as_rows(h, "h")
-    rd = None if dh is None else _as_rows(dh, "dh")
-    rows, cols = ry.shape
-    _weight(weight, cols, dy.device)
-    if rstd.dtype != torch.float32 or rstd.device != dy.device or rstd.shape != (rows,) or not rstd.is_contiguous():
-        raise ValueError("rstd: expected a contiguous float32 tensor of %d on %s" % (rows, dy.device))
+    device, shape = dy.device, dy.shape
+    for t, what in ((h, "h"), (dh, "dh")):
+        if t is not None:
+            _like(t, dy, what)
+            if t.shape != shape:
+                raise ValueError("%s has shape %s, dy %s" % (what, tuple(t.shape), tuple(shape)))
+    ry, rows, cols, dy_stride = _as_rows(dy, "dy")
+    rh, _, _, h_stride = _as_rows(h, "h")
+    rd, _, _, dh_stride = (None, 0, 0, 0) if dh is None else _as_rows(dh, "dh")
+    _weight(weight, cols, device)
+    if rstd.dtype != torch.float32 or rstd.device != device or rstd.shape != (rows,) or not rstd.is_contiguous():
+        raise ValueError("rstd: expected a contiguous float32 tensor of %d on %s" % (rows, device))
     lib = load_library()
-    with _on(dy) as stream:
-        dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
-        dweight = torch.empty(cols, dtype=torch.float32, device=dy.device)
-        need = C.c_int64()
-        _check(lib.dear_add_rms_norm_backward_workspace(d, rows, cols, C.byref(need)), "dear_add_rms_norm_backward_workspace")
-        space = torch.empty(need.value, dtype=torch.uint8, device=dy.device)
-        _check(lib.dear_add_rms_norm_backward(
-            ry.data_ptr(), _stride(ry), rh.data_ptr(), _stride(rh), None if rd is None else rd.data_ptr(),
-            0 if rd is None else _stride(rd), weight.data_ptr(), rstd.data_ptr(), d, rows, cols, dx.data_ptr(),
-            dweight.data_ptr(), space.data_ptr(), need.value, stream), "dear_add_rms_norm_backward")
+    dx = _empty_as(dy)
+    dweight = torch.empty(cols, dtype=torch.float32, device=device)
+    need = C.c_int64()
+    _check(lib.dear_add_rms_norm_backward_workspace(d, rows, cols, C.byref(need)), "dear_add_rms_norm_backward_workspace")
+    space = torch.empty(need.value, dtype=torch.uint8, device=device)
+    _check(lib.dear_add_rms_norm_backward(
+        ry.data_ptr(), dy_stride, rh.data_ptr(), h_stride, None if rd is None else rd.data_ptr(), dh_stride, weight.data_ptr(),
+        rstd.data_ptr(), d, rows, cols, dx.data_ptr(), dweight.data_ptr(), space.data_ptr(), need.value, _raw_stream(dy.get_device())),
+        "dear_add_rms_norm_backward")
     return dx, dweight
