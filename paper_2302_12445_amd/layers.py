@@ -1,0 +1,158 @@
+"""Autograd functions and modules over the training operators (ops.py), for models that DistOptim trains: parameters and
+their gradients are fp32, activations bf16 or fp32, and what a layer keeps for its backward pass is in 8 bits where the
+operator allows it.
+
+    h, y, kept = AddRMSNorm(width)(x, residual)   # kept: y in 8 bits, from the norm's own kernel
+    z = CheckpointLinear(width, outs)(y, kept)    # weight gradient from the checkpoint; makes one itself where none is given
+    out = attend(q, k, v, causal=True)            # keeps q, k, v, out and the log-sum-exp; recomputes the probabilities
+"""
+from __future__ import annotations
+
+import math
+from typing import Optional, Tuple
+
+import torch
+
+from . import ops
+
+
+class _Attention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, causal, scale, q_lens, kv_lens):
+        out, lse = ops.attention(q, k, v, causal=causal, scale=scale, q_lens=q_lens, kv_lens=kv_lens)
+        ctx.save_for_backward(q, k, v, out, lse, q_lens, kv_lens)
+        ctx.causal, ctx.scale = causal, scale
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        q, k, v, out, lse, q_lens, kv_lens = ctx.saved_tensors
+        grads = ops.attention_backward(dout, q, k, v, out, lse, causal=ctx.causal, scale=ctx.scale, q_lens=q_lens, kv_lens=kv_lens)
+        return (*grads, None, None, None, None)
+
+
+def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
+           q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """ops.attention's out, with gradients of q, k and v."""
+    return _Attention.apply(q, k, v, causal, scale, q_lens, kv_lens)
+
+
+class _AddRMSNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps):
+        h, y, kept, rstd = ops.add_rms_norm(x, residual, weight, eps)
+        ctx.save_for_backward(h, weight, rstd)
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(kept.codes, kept.exponents)
+        # without a residual h is x, which an output of its own has to stand for
+        return h if residual is not None else x.view_as(x), y, kept.codes, kept.exponents
+
+    @staticmethod
+    def backward(ctx, dh, dy, _codes, _exponents):
+        h, weight, rstd = ctx.saved_tensors
+        if dy is None:  # nobody used y
+            dx, dweight = dh, None
+        else:
+            dx, dweight = ops.add_rms_norm_backward(dy, h, weight, rstd, dh=dh)
+        return dx, dx if ctx.needs_input_grad[1] else None, dweight, None
+
+
+class AddRMSNorm(torch.nn.Module):
+    """h = x + residual; y = h / sqrt(mean(h^2) + eps) * weight.  Gives (h, y, the checkpoint of y)."""
+
+    def __init__(self, width: int, eps: float = 1e-5):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.ones(width))
+        self.eps = eps
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, ops.Checkpoint]:
+        h, y, codes, exponents = _AddRMSNorm.apply(x, residual, self.weight, self.eps)
+        return h, y, ops.Checkpoint(codes, exponents, self.weight.numel())
+
+
+class _CheckpointLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, kept):
+        rows = x.reshape(-1, x.shape[-1])
+        w = weight.to(x.dtype)
+        out = rows @ w.t() if bias is None else torch.addmm(bias.to(x.dtype), rows, w.t())
+        if kept is None:
+            kept = ops.checkpoint_encode(rows)
+        ctx.save_for_backward(kept.codes, kept.exponents, weight)
+        ctx.cols, ctx.has_bias, ctx.shape = kept.cols, bias is not None, x.shape
+        return out.view(*x.shape[:-1], weight.shape[0])
+
+    @staticmethod
+    def backward(ctx, dout):
+        codes, exponents, weight = ctx.saved_tensors
+        rows = dout.reshape(-1, dout.shape[-1])
+        dx = (rows @ weight.to(rows.dtype)).view(ctx.shape) if ctx.needs_input_grad[0] else None
+        dw = ops.checkpoint_weight_grad(rows, ops.Checkpoint(codes, exponents, ctx.cols)) if ctx.needs_input_grad[1] else None
+        db = rows.sum(0, dtype=torch.float32) if ctx.has_bias and ctx.needs_input_grad[2] else None
+        return dx, dw, db, None
+
+
+class CheckpointLinear(torch.nn.Module):
+    """A linear layer that keeps its input in 8 bits for the backward pass: a quarter (fp32) or half (bf16) of the memory.
+    Products with the weight are torch's, in the input's type; the weight's gradient is fp32, from the checkpoint."""
+
+    def __init__(self, ins: int, outs: int, bias: bool = True):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.empty(outs, ins))
+        self.bias = torch.nn.Parameter(torch.zeros(outs)) if bias else None
+        torch.nn.init.uniform_(self.weight, -1 / math.sqrt(ins), 1 / math.sqrt(ins))
+
+    def forward(self, x: torch.Tensor, kept: Optional[ops.Checkpoint] = None) -> torch.Tensor:
+        """kept: the checkpoint of x, where it is there already."""
+        return _CheckpointLinear.apply(x, self.weight, self.bias, kept)
+
+
+class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
+    """Within it, what torch's own operations keep for their backward passes is kept as checkpoints: floating tensors on
+    the GPU of at least `least` elements that are no parameters (as a GELU's input; not for what has to come back exactly,
+    such as a mask in floating point).
+
+        with saved_in_8_bits():
+            z = torch.nn.functional.gelu(u)
+    """
+
+    def __init__(self, least: int = 1 << 16):
+        def pack(t):
+            if not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or t.numel() < least or isinstance(t, torch.nn.Parameter):
+                return t
+            return ops.checkpoint_encode(t.detach()), t.shape, t.dtype
+
+        def unpack(kept):
+            if isinstance(kept, torch.Tensor):
+                return kept
+            checkpoint, shape, dtype = kept
+            return ops.checkpoint_decode(checkpoint, dtype).view(shape)
+        super().__init__(pack, unpack)
+
+
+class TransformerBlock(torch.nn.Module):
+    """Pre-norm transformer block over (x, residual), as one layer of a stack: attention and a feed-forward network, each
+    behind a norm that adds the residual on the way.  Gives the block's (output, residual) for the next one's norm."""
+
+    def __init__(self, width: int, heads: int, kv_heads: Optional[int] = None, ffn: Optional[int] = None, causal: bool = True):
+        super().__init__()
+        self.heads, self.kv_heads, self.causal = heads, kv_heads or heads, causal
+        self.head_dim = width // heads
+        self.norm1 = AddRMSNorm(width)
+        self.qkv = CheckpointLinear(width, (self.heads + 2 * self.kv_heads) * self.head_dim)
+        self.proj = CheckpointLinear(width, width)
+        self.norm2 = AddRMSNorm(width)
+        self.up = CheckpointLinear(width, ffn or 4 * width)
+        self.down = CheckpointLinear(ffn or 4 * width, width)
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                lens: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        batch, tokens, width = x.shape
+        h, y, kept = self.norm1(x, residual)
+        q, k, v = self.qkv(y, kept).view(batch, tokens, -1, self.head_dim).split([self.heads, self.kv_heads, self.kv_heads], 2)
+        out = attend(q, k, v, causal=self.causal, q_lens=lens, kv_lens=lens)
+        h, y, kept = self.norm2(self.proj(out.reshape(batch, tokens, width)), h)
+        u = self.up(y, kept)
+        with saved_in_8_bits():
+            z = torch.nn.functional.gelu(u)
+        return self.down(z), h
