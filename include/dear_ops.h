@@ -81,8 +81,9 @@ typedef struct {
 int dear_attention(const dear_attention_t *args, void *hip_stream);
 int dear_attention_backward(const dear_attention_t *args, void *hip_stream);
 
-/* Bytes of workspace that a call with these sizes needs (pointers and strides are not looked at).
- * Errors: DEAR_EINVAL. */
+/* Bytes of workspace that a call with these sizes needs (pointers and strides are not looked at): where
+ * there are few rows, the sequence that they attend to is split, and the splits' results are joined.
+ * Errors: DEAR_EINVAL, DEAR_ETOOBIG. */
 int dear_attention_workspace(const dear_attention_t *args, int64_t *bytes);
 int dear_attention_backward_workspace(const dear_attention_t *args, int64_t *bytes);
 

@@ -30,12 +30,16 @@ struct heads {
 struct params {
     int32_t q_heads, kv_heads, head_dim, causal;
     int32_t q_len, kv_len, batch, tiles, q_tiles;  // tiles: of this launch; q_tiles: BLOCKs of queries
+    int32_t splits;      // of the sequence that a workgroup goes through
     float scale;
     const int32_t *q_lens, *kv_lens;
     heads q, k, v, out, dout, dq, dk, dv;
     float *lse;
     // backward, of the queries of all tiles: lse * log2(e), or infinity where no key is seen, and -delta
     float *powers, *deltas;
+    // with several splits, of each: outputs that are not yet joined, fp32 [split, batch, head, token, head_dim], and, forward,
+    // what the powers are taken against and their sums [split, batch, head, token]
+    float *part, *part_base, *part_sum;
 };
 
 __device__ __forceinline__ char *at(const heads &t, int b, int h) {
@@ -99,14 +103,15 @@ __device__ __forceinline__ void store_row(char *p, const f32x16 *x, float factor
         }
 }
 
-// Workgroup -> (batch, head, tile), for `heads` heads of which `shared` neighbours read the same keys.  Workgroups go to
+// Workgroup -> (batch, head, tile, split), for `heads` heads of which `shared` neighbours read the same keys.  Workgroups go to
 // the eight XCDs in turn.  Where it divides evenly an XCD gets whole groups of heads (every eighth, so that sequences of
 // different lengths are spread), or at least whole heads; it takes them one after another with all their tiles, which find
 // the other sequence in its L2 cache, or, in a causal call, whose tiles are numbered from the longest on, the same tile of
 // all its heads and then the next, so that the shortest come last.
-__device__ __forceinline__ void place(const params &a, unsigned heads, unsigned shared, int &b, int &h, int &t) {
+__device__ __forceinline__ void place(const params &a, unsigned heads, unsigned shared, int &b, int &h, int &t, int &split) {
     const unsigned pairs = heads * a.batch, tiles = a.tiles;
-    unsigned pair, id = blockIdx.x, xcd = 0, own = pairs;
+    unsigned pair, id = blockIdx.x % (pairs * tiles), xcd = 0, own = pairs;
+    split = blockIdx.x / (pairs * tiles);
     if (pairs % 8 == 0) xcd = id % 8, id /= 8, own = pairs / 8;
     t = a.causal ? id / own : id % tiles;
     pair = a.causal ? id % own : id / tiles;
@@ -116,12 +121,24 @@ __device__ __forceinline__ void place(const params &a, unsigned heads, unsigned 
     h = pair % heads;
 }
 
+// The split's share of begin .. end: whole steps.
+__device__ __forceinline__ void share(const params &a, int split, int &begin, int &end) {
+    const int steps = (end - begin + STEP - 1) / STEP, each = (steps + a.splits - 1) / a.splits * STEP;
+    begin += split * each;
+    end = min(end, begin + each);
+}
+
+// Where the split's output of a row stands until all are joined.
+__device__ __forceinline__ char *part_row(const params &a, int heads, int len, int split, int b, int h, int i) {
+    return (char *)(a.part + ((((int64_t)split * a.batch + b) * heads + h) * len + i) * a.head_dim);
+}
+
 // ------------------------------------------------------------------------------------ forward
 template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(false))) void attention_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
-    int b, h, t;
-    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t);
+    int b, h, t, split;
+    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t, split);
     if (a.causal) t = a.tiles - 1 - t;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
     const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
@@ -130,7 +147,8 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
     const int i = t * BLOCK + wave * 32 + (lane & 31);  // this lane's query
     // keys 0 .. last are visible to it
     const int last = i < nq ? (a.causal ? min(nk - 1, i + nk - nq) : nk - 1) : -1;
-    const int block_end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    int begin = 0, end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    share(a, split, begin, end);
     // the same of the whole wave: the fewest keys of a query, and the most
     const int wave_first = t * BLOCK + wave * 32;
     const int wave_least = wave_first + 31 < nq ? (a.causal ? min(nk - 1, wave_first + nk - nq) : nk - 1) : -1;
@@ -142,16 +160,16 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
     const float c = a.scale * LOG2E;
 
     stage<T, W> kst, vst;
-    if (block_end > 0) {
-        kst.load(kp, a.k.token, 0, nk, a.head_dim);
-        vst.load(vp, a.v.token, 0, nk, a.head_dim);
+    if (begin < end) {
+        kst.load(kp, a.k.token, begin, nk, a.head_dim);
+        vst.load(vp, a.v.token, begin, nk, a.head_dim);
     }
-    for (int j0 = 0; j0 < block_end; j0 += STEP) {
+    for (int j0 = begin; j0 < end; j0 += STEP) {
         __syncthreads();
         kst.store(ks);
         vst.store(vs);
         __syncthreads();
-        if (j0 + STEP < block_end) {
+        if (j0 + STEP < end) {
             kst.load(kp, a.k.token, j0 + STEP, nk, a.head_dim);
             vst.load(vp, a.v.token, j0 + STEP, nk, a.head_dim);
         }
@@ -201,6 +219,12 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
     if (i >= a.q_len) return;
     sum = halves_sum(sum);
     const bool none = top == -INFINITY && sum == 0.f;
+    if (a.splits > 1) {
+        store_row<float, W>(part_row(a, a.q_heads, a.q_len, split, b, h, i), o, 1.f, a.head_dim, half);
+        const int64_t row = (((int64_t)split * a.batch + b) * a.q_heads + h) * a.q_len + i;
+        if (half == 0) a.part_base[row] = top == -INFINITY ? 0.f : top * c, a.part_sum[row] = sum;
+        return;
+    }
     store_row<T, W>(at(a.out, b, h) + i * a.out.token, o, none ? 0.f : 1.f / sum, a.head_dim, half);
     if (half == 0)
         a.lse[((int64_t)b * a.q_heads + h) * a.q_len + i] = none ? -INFINITY : (top * c + __builtin_amdgcn_logf(sum)) * LN2;
@@ -254,8 +278,8 @@ template <int N, int AHEAD> __device__ __forceinline__ void read_ahead() {
 
 template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_direct_kernel(params a) {
     __shared__ __attribute__((aligned(16))) bf16 ks0[STEP * W], ks1[STEP * W], vs0[STEP * W], vs1[STEP * W];
-    int b, h, t;
-    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t);
+    int b, h, t, split;
+    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t, split);
     if (a.causal) t = a.tiles - 1 - t;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
@@ -263,29 +287,30 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_direct_
     const int i = t * BLOCK + wave * 32 + (lane & 31);  // this lane's query
     // keys 0 .. last are visible to it
     const int last = i < nq ? (a.causal ? min(nk - 1, i + nk - nq) : nk - 1) : -1;
-    const int block_end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    int begin = 0, end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    share(a, split, begin, end);
     const int wave_first = t * BLOCK + wave * 32;
     const int wave_least = wave_first + 31 < nq ? (a.causal ? min(nk - 1, wave_first + nk - nq) : nk - 1) : -1;
     const float c = a.scale * LOG2E;
 
     f32x16 o[W / 32] = {};
     float top = -INFINITY, base = 0.f, limit = -INFINITY, sum = 0.f;
-    if (block_end > 0) {
+    if (begin < end) {
         if (a.head_dim < W) {
             for (DEAR_LDS bf16 *s : {(DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs0, (DEAR_LDS bf16 *)vs1}) clear<W>(s);
             __syncthreads();
         }
         const direct_loads<W, WAVES> kl(a.k.token, a.head_dim, lane, wave), vl(a.v.token, a.head_dim, lane, wave);
-        const char *kp = at(a.k, b, kvh), *vp = at(a.v, b, kvh);
-        int j0 = 0;
+        const char *kp = at(a.k, b, kvh) + begin * a.k.token, *vp = at(a.v, b, kvh) + begin * a.v.token;
+        int j0 = begin;
         auto load = [&](DEAR_LDS bf16 *ks, DEAR_LDS bf16 *vs, int j) {
-            if (j < block_end) {
+            if (j < end) {
                 kl.load(kp, nk - j, ks, wave);
                 vl.load(vp, nk - j, vs, wave);
                 kp += STEP * a.k.token, vp += STEP * a.v.token;
             }
         };
-        load((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0, 0);
+        load((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0, begin);
         frag<bf16> q[W / 16];
         load_rows<bf16, W>(q, at(a.q, b, h), a.q.token, i, nq, a.head_dim, half);
         direct<W> rd(lane);
@@ -346,16 +371,22 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_direct_
             loads_barrier();
             load((DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs1, j0 + STEP);
             step((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0);
-            if (j0 >= block_end) break;
+            if (j0 >= end) break;
             loads_barrier();
             load((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0, j0 + STEP);
             step((DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs1);
-            if (j0 >= block_end) break;
+            if (j0 >= end) break;
         }
     }
     if (i >= a.q_len) return;
     sum = halves_sum(sum);
     const bool none = top == -INFINITY && sum == 0.f;
+    if (a.splits > 1) {
+        store_row<float, W>(part_row(a, a.q_heads, a.q_len, split, b, h, i), o, 1.f, a.head_dim, half);
+        const int64_t row = (((int64_t)split * a.batch + b) * a.q_heads + h) * a.q_len + i;
+        if (half == 0) a.part_base[row] = base, a.part_sum[row] = sum;
+        return;
+    }
     store_row<bf16, W>(at(a.out, b, h) + i * a.out.token, o, none ? 0.f : 1.f / sum, a.head_dim, half);
     if (half == 0)
         a.lse[((int64_t)b * a.q_heads + h) * a.q_len + i] = none ? -INFINITY : (base + __builtin_amdgcn_logf(sum)) * LN2;
@@ -364,10 +395,10 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_direct_
 // ------------------------------------------------------------------------------------ backward: queries
 // lse * log2(e) of query i, as what its powers are taken against: infinity where it sees no key, so that its probabilities
 // are 0.  Kept, with -delta, for the kernel that computes dk and dv; there is a place for every query of every tile.
-__device__ __forceinline__ float row_values(const params &a, int b, int h, int i, int nq, int half, float delta) {
+__device__ __forceinline__ float row_values(const params &a, int b, int h, int i, int split, int nq, int half, float delta) {
     const float z = i < nq ? a.lse[((int64_t)b * a.q_heads + h) * a.q_len + i] : -INFINITY;
     const float base = z == -INFINITY ? INFINITY : z * LOG2E;
-    if (half == 0) {
+    if (half == 0 && split == 0) {
         const int64_t row = ((int64_t)b * a.q_heads + h) * a.tiles * BLOCK + i;
         a.powers[row] = base;
         a.deltas[row] = -delta;
@@ -380,8 +411,8 @@ __device__ __forceinline__ float row_values(const params &a, int b, int h, int i
 template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(false))) void attention_dq_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
-    int b, h, t;
-    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t);
+    int b, h, t, split;
+    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t, split);
     if (a.causal) t = a.tiles - 1 - t;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
     const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
@@ -389,7 +420,8 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
     const char *kp = at(a.k, b, kvh), *vp = at(a.v, b, kvh);
     const int i = t * BLOCK + wave * 32 + (lane & 31);
     const int last = i < nq ? (a.causal ? min(nk - 1, i + nk - nq) : nk - 1) : -1;
-    const int block_end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    int begin = 0, end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    share(a, split, begin, end);
     const int wave_first = t * BLOCK + wave * 32;
     const int wave_least = wave_first + 31 < nq ? (a.causal ? min(nk - 1, wave_first + nk - nq) : nk - 1) : -1;
 
@@ -406,20 +438,20 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
             for (int u = 0; u < 8; ++u) delta += (float)g[kk][u] * (float)out[kk][u];
     }
     delta = halves_sum(delta);
-    const float base = row_values(a, b, h, i, nq, half, delta), c = a.scale * LOG2E;
+    const float base = row_values(a, b, h, i, split, nq, half, delta), c = a.scale * LOG2E;
 
     f32x16 dq[W / 32] = {};
     stage<T, W> kst, vst;
-    if (block_end > 0) {
-        kst.load(kp, a.k.token, 0, nk, a.head_dim);
-        vst.load(vp, a.v.token, 0, nk, a.head_dim);
+    if (begin < end) {
+        kst.load(kp, a.k.token, begin, nk, a.head_dim);
+        vst.load(vp, a.v.token, begin, nk, a.head_dim);
     }
-    for (int j0 = 0; j0 < block_end; j0 += STEP) {
+    for (int j0 = begin; j0 < end; j0 += STEP) {
         __syncthreads();
         kst.store(ks);
         vst.store(vs);
         __syncthreads();
-        if (j0 + STEP < block_end) {
+        if (j0 + STEP < end) {
             kst.load(kp, a.k.token, j0 + STEP, nk, a.head_dim);
             vst.load(vp, a.v.token, j0 + STEP, nk, a.head_dim);
         }
@@ -449,7 +481,9 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
             }
         }
     }
-    if (i < a.q_len) store_row<T, W>(at(a.dq, b, h) + i * a.dq.token, dq, a.scale, a.head_dim, half);
+    if (i >= a.q_len) return;
+    if (a.splits > 1) store_row<float, W>(part_row(a, a.q_heads, a.q_len, split, b, h, i), dq, 1.f, a.head_dim, half);
+    else store_row<T, W>(at(a.dq, b, h) + i * a.dq.token, dq, a.scale, a.head_dim, half);
 }
 
 // ------------------------------------------------------------------------------------ backward: keys and values
@@ -459,8 +493,8 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     __shared__ __attribute__((aligned(16))) float rows[2][STEP];  // what the queries' powers are taken against, and -delta
     DEAR_LDS T *qs = (DEAR_LDS T *)lds, *gs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
-    int b, kvh, t;
-    place(a, a.kv_heads, 1, b, kvh, t);
+    int b, kvh, t, split;
+    place(a, a.kv_heads, 1, b, kvh, t, split);
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
     const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
     const int group = a.q_heads / a.kv_heads;
@@ -468,7 +502,8 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
     // queries first .. nq - 1 see it
     const int first = j < nk ? (a.causal ? max(0, j - nk + nq) : 0) : nq;
     const int wave_last = wave_first + 31 < nk ? (a.causal ? max(0, wave_first + 31 - nk + nq) : 0) : nq;
-    const int begin = t * KEYS >= nk ? nq : a.causal ? max(0, t * KEYS - nk + nq) / STEP * STEP : 0;
+    int begin = t * KEYS >= nk ? nq : a.causal ? max(0, t * KEYS - nk + nq) / STEP * STEP : 0, end = nq;
+    share(a, split, begin, end);
 
     frag<T> k[W / 16], v[W / 16];
     load_rows<T, W>(k, at(a.k, b, kvh), a.k.token, j, nk, a.head_dim, half);
@@ -486,18 +521,18 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
             const int64_t i = row + i0 + threadIdx.x % STEP;
             if (threadIdx.x < 2 * STEP) z = threadIdx.x < STEP ? a.powers[i] : a.deltas[i];
         };
-        if (begin < nq) {
+        if (begin < end) {
             qst.load(qp, a.q.token, begin, nq, a.head_dim);
             gst.load(gp, a.dout.token, begin, nq, a.head_dim);
             load_z(begin);
         }
-        for (int i0 = begin; i0 < nq; i0 += STEP) {
+        for (int i0 = begin; i0 < end; i0 += STEP) {
             __syncthreads();
             qst.store(qs);
             gst.store(gs);
             if (threadIdx.x < 2 * STEP) rows[threadIdx.x / STEP][threadIdx.x % STEP] = z;
             __syncthreads();
-            if (i0 + STEP < nq) {
+            if (i0 + STEP < end) {
                 qst.load(qp, a.q.token, i0 + STEP, nq, a.head_dim);
                 gst.load(gp, a.dout.token, i0 + STEP, nq, a.head_dim);
                 load_z(i0 + STEP);
@@ -550,6 +585,11 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
     }
     if (turn == 1) return;
     if (j >= a.kv_len) return;
+    if (a.splits > 1) {  // dk's come first, then dv's
+        store_row<float, W>(part_row(a, a.kv_heads, a.kv_len, split, b, kvh, j), dk, 1.f, a.head_dim, half);
+        store_row<float, W>(part_row(a, a.kv_heads, a.kv_len, a.splits + split, b, kvh, j), dv, 1.f, a.head_dim, half);
+        return;
+    }
     store_row<T, W>(at(a.dk, b, kvh) + j * a.dk.token, dk, a.scale, a.head_dim, half);
     store_row<T, W>(at(a.dv, b, kvh) + j * a.dv.token, dv, 1.f, a.head_dim, half);
 }
@@ -557,24 +597,25 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
 // ------------------------------------------------------------------------------------ bf16 backward, tiles filled directly
 template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_direct_kernel(params a) {
     __shared__ __attribute__((aligned(16))) bf16 ks0[STEP * W], ks1[STEP * W], vs0[STEP * W], vs1[STEP * W];
-    int b, h, t;
-    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t);
+    int b, h, t, split;
+    place(a, a.q_heads, a.q_heads / a.kv_heads, b, h, t, split);
     if (a.causal) t = a.tiles - 1 - t;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
     const int kvh = h / (a.q_heads / a.kv_heads);
     const int i = t * BLOCK + wave * 32 + (lane & 31);
     const int last = i < nq ? (a.causal ? min(nk - 1, i + nk - nq) : nk - 1) : -1;
-    const int block_end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    int begin = 0, end = t * BLOCK >= nq ? 0 : a.causal ? min(nk, min(t * BLOCK + BLOCK, nq) + nk - nq) : nk;
+    share(a, split, begin, end);
     const int wave_first = t * BLOCK + wave * 32;
     const int wave_least = wave_first + 31 < nq ? (a.causal ? min(nk - 1, wave_first + nk - nq) : nk - 1) : -1;
     const float c = a.scale * LOG2E;
-    const bool any = block_end > 0;
+    const bool any = begin < end;
 
     const direct_loads<W, WAVES> kl(a.k.token, a.head_dim, lane, wave), vl(a.v.token, a.head_dim, lane, wave);
-    const char *kp = at(a.k, b, kvh), *vp = at(a.v, b, kvh);
+    const char *kp = at(a.k, b, kvh) + begin * a.k.token, *vp = at(a.v, b, kvh) + begin * a.v.token;
     auto load = [&](DEAR_LDS bf16 *ks, DEAR_LDS bf16 *vs, int j) {
-        if (j < block_end) {
+        if (j < end) {
             kl.load(kp, nk - j, ks, wave);
             vl.load(vp, nk - j, vs, wave);
             kp += STEP * a.k.token, vp += STEP * a.v.token;
@@ -584,7 +625,7 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_dire
         for (DEAR_LDS bf16 *s : {(DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs0, (DEAR_LDS bf16 *)vs1}) clear<W>(s);
         __syncthreads();
     }
-    load((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0, 0);
+    load((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0, begin);
 
     frag<bf16> q[W / 16], g[W / 16];
     load_rows<bf16, W>(q, at(a.q, b, h), a.q.token, i, nq, a.head_dim, half);
@@ -599,10 +640,10 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_dire
             for (int u = 0; u < 8; ++u) delta += (float)g[kk][u] * (float)out[kk][u];
     }
     delta = halves_sum(delta);
-    const float base = row_values(a, b, h, i, nq, half, delta);
+    const float base = row_values(a, b, h, i, split, nq, half, delta);
 
     f32x16 dq[W / 32] = {};
-    int j0 = 0;
+    int j0 = begin;
     direct<W> rd(lane);
     auto step = [&](const DEAR_LDS bf16 *ks, const DEAR_LDS bf16 *vs) {
         rd.renew();
@@ -640,13 +681,15 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_dire
         loads_barrier();
         load((DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs1, j0 + STEP);
         step((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0);
-        if (j0 >= block_end) break;
+        if (j0 >= end) break;
         loads_barrier();
         load((DEAR_LDS bf16 *)ks0, (DEAR_LDS bf16 *)vs0, j0 + STEP);
         step((DEAR_LDS bf16 *)ks1, (DEAR_LDS bf16 *)vs1);
-        if (j0 >= block_end) break;
+        if (j0 >= end) break;
     }
-    if (i < a.q_len) store_row<bf16, W>(at(a.dq, b, h) + i * a.dq.token, dq, a.scale, a.head_dim, half);
+    if (i >= a.q_len) return;
+    if (a.splits > 1) store_row<float, W>(part_row(a, a.q_heads, a.q_len, split, b, h, i), dq, 1.f, a.head_dim, half);
+    else store_row<bf16, W>(at(a.dq, b, h) + i * a.dq.token, dq, a.scale, a.head_dim, half);
 }
 
 // dk and dv of 128 keys a workgroup, 32 a wave, for rows of 64 values: the operands and sums of both fit a wave beside a
@@ -655,8 +698,8 @@ __global__ __launch_bounds__(THREADS, 2) void attention_dkv_direct_kernel(params
     constexpr int W = 64;
     __shared__ __attribute__((aligned(16))) bf16 qs0[STEP * W], qs1[STEP * W], gs0[STEP * W], gs1[STEP * W];
     __shared__ __attribute__((aligned(16))) float powers0[STEP], powers1[STEP], deltas0[STEP], deltas1[STEP];
-    int b, kvh, t;
-    place(a, a.kv_heads, 1, b, kvh, t);
+    int b, kvh, t, split;
+    place(a, a.kv_heads, 1, b, kvh, t, split);
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
     const int group = a.q_heads / a.kv_heads;
@@ -664,8 +707,9 @@ __global__ __launch_bounds__(THREADS, 2) void attention_dkv_direct_kernel(params
     // queries first .. nq - 1 see it; those beyond nq have probabilities of 0 by their powers
     const int first = j < nk ? (a.causal ? max(0, j - nk + nq) : 0) : nq;
     const int wave_last = wave_first + 31 < nk ? (a.causal ? max(0, wave_first + 31 - nk + nq) : 0) : nq;
-    const int begin = t * BLOCK >= nk ? nq : a.causal ? max(0, t * BLOCK - nk + nq) / STEP * STEP : 0;
-    const int steps = begin < nq ? (nq - begin + STEP - 1) / STEP * group : 0;
+    int begin = t * BLOCK >= nk ? nq : a.causal ? max(0, t * BLOCK - nk + nq) / STEP * STEP : 0, end = nq;
+    share(a, split, begin, end);
+    const int steps = begin < end ? (end - begin + STEP - 1) / STEP * group : 0;
     const float c = a.scale * LOG2E;
 
     f32x16 dk[W / 32] = {}, dv[W / 32] = {};
@@ -686,7 +730,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_dkv_direct_kernel(params
                 if (wave == 0) load_value_to_lds(a.powers + row, powers);
                 if (wave == 1) load_value_to_lds(a.deltas + row, deltas);
                 qp += STEP * a.q.token, gp += STEP * a.dout.token, next += STEP;
-                if (next >= nq) {
+                if (next >= end) {
                     h += 1, next = begin;
                     qp = at(a.q, b, h) + begin * a.q.token, gp = at(a.dout, b, h) + begin * a.dout.token;
                 }
@@ -740,7 +784,7 @@ __global__ __launch_bounds__(THREADS, 2) void attention_dkv_direct_kernel(params
                 }
             }
             i0 += STEP;
-            if (i0 >= nq) i0 = begin;
+            if (i0 >= end) i0 = begin;
             return ++n < steps;
         };
 #define DEAR_STEP(n, other)  \
@@ -755,6 +799,11 @@ __global__ __launch_bounds__(THREADS, 2) void attention_dkv_direct_kernel(params
 #undef DEAR_LOAD
     }
     if (j >= a.kv_len) return;
+    if (a.splits > 1) {  // dk's come first, then dv's
+        store_row<float, W>(part_row(a, a.kv_heads, a.kv_len, split, b, kvh, j), dk, 1.f, a.head_dim, half);
+        store_row<float, W>(part_row(a, a.kv_heads, a.kv_len, a.splits + split, b, kvh, j), dv, 1.f, a.head_dim, half);
+        return;
+    }
     store_row<bf16, W>(at(a.dk, b, kvh) + j * a.dk.token, dk, a.scale, a.head_dim, half);
     store_row<bf16, W>(at(a.dv, b, kvh) + j * a.dv.token, dv, 1.f, a.head_dim, half);
 }
@@ -773,8 +822,8 @@ __global__ __launch_bounds__(64 * KV_WAVES, 2) void attention_dkv_halves_kernel(
     __shared__ __attribute__((aligned(16))) bf16 qs0[STEP * W], qs1[STEP * W], qs2[STEP * W], gs0[STEP * W], gs1[STEP * W];
     __shared__ __attribute__((aligned(16))) float powers0[STEP], powers1[STEP], deltas0[STEP], deltas1[STEP];
     __shared__ __attribute__((aligned(16))) float ps[2][4][4][64 * 4];  // step, wave, quarter of its values: four a lane
-    int b, kvh, t;
-    place(a, a.kv_heads, 1, b, kvh, t);
+    int b, kvh, t, split;
+    place(a, a.kv_heads, 1, b, kvh, t, split);
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int nq = length(a.q_lens, b, a.q_len), nk = length(a.kv_lens, b, a.kv_len);
     const int group = a.q_heads / a.kv_heads, part = wave & 3, turn = part & 1;
@@ -783,8 +832,9 @@ __global__ __launch_bounds__(64 * KV_WAVES, 2) void attention_dkv_halves_kernel(
     // queries first .. nq - 1 see it; those beyond nq have probabilities of 0 by their powers
     const int first = j < nk ? (a.causal ? max(0, j - nk + nq) : 0) : nq;
     const int wave_last = wave_first + 31 < nk ? (a.causal ? max(0, wave_first + 31 - nk + nq) : 0) : nq;
-    const int begin = t * KEYS >= nk ? nq : a.causal ? max(0, t * KEYS - nk + nq) / STEP * STEP : 0;
-    const int steps = begin < nq ? (nq - begin + STEP - 1) / STEP * group : 0;
+    int begin = t * KEYS >= nk ? nq : a.causal ? max(0, t * KEYS - nk + nq) / STEP * STEP : 0, end = nq;
+    share(a, split, begin, end);
+    const int steps = begin < end ? (end - begin + STEP - 1) / STEP * group : 0;
     const float c = a.scale * LOG2E;
 
     f32x16 sum[W / 32] = {};  // dv, or dk
@@ -807,7 +857,7 @@ __global__ __launch_bounds__(64 * KV_WAVES, 2) void attention_dkv_halves_kernel(
                 if (wave == 0) load_value_to_lds(a.powers + row, powers);
                 if (wave == 4) load_value_to_lds(a.deltas + row, deltas);
                 qp += STEP * a.q.token, gp += STEP * a.dout.token, next += STEP;
-                if (next >= nq) {
+                if (next >= end) {
                     h += 1, next = begin;
                     qp = at(a.q, b, h) + begin * a.q.token, gp = at(a.dout, b, h) + begin * a.dout.token;
                 }
@@ -832,7 +882,7 @@ __global__ __launch_bounds__(64 * KV_WAVES, 2) void attention_dkv_halves_kernel(
                     for (int r = 0; r < 16; ++r) s[r] = i0 + 32 * turn + row_of(r, half) >= first ? 0.f : -INFINITY;
                 }
                 i0 += STEP;
-                if (i0 >= nq) i0 = begin;
+                if (i0 >= end) i0 = begin;
 #pragma unroll
                 for (int kk = 0; kk < W / 16; ++kk) s = mma(rd.straight(qs, 0, kk), kv[kk], s);
                 frag<bf16> p[2];
@@ -940,12 +990,80 @@ __global__ __launch_bounds__(64 * KV_WAVES, 2) void attention_dkv_halves_kernel(
         }
     }
     if (turn == 1 || j >= a.kv_len) return;
+    if (a.splits > 1) {  // dk's come first, then dv's
+        store_row<float, W>(part_row(a, a.kv_heads, a.kv_len, second ? split : a.splits + split, b, kvh, j), sum, 1.f, a.head_dim, half);
+        return;
+    }
     const heads &out = second ? a.dk : a.dv;
     store_row<bf16, W>(at(out, b, kvh) + j * out.token, sum, second ? a.scale : 1.f, a.head_dim, half);
 }
 
+// ------------------------------------------------------------------------------------ splits joined
+// Eight values of a row a thread; a row of the splits' outputs is [batch, head, token].
+struct joined {
+    int64_t row;
+    int b, h, i, d;
+    bool some;
+    __device__ __forceinline__ joined(int batch, int heads, int len, int head_dim) {
+        const int pieces = head_dim / 8;
+        const int64_t n = (int64_t)blockIdx.x * THREADS + threadIdx.x, rows = (int64_t)batch * heads * len;
+        row = n / pieces, d = (int)(n % pieces) * 8;
+        some = row < rows;
+        i = (int)(row % len), h = (int)(row / len % heads), b = (int)(row / len / heads);
+    }
+};
+
+template <typename T> __device__ __forceinline__ void store_eight(char *p, int d, const float *x) { *(frag<T> *)(p + d * sizeof(T)) = to_frag<T>(x); }
+
+template <typename T> __global__ __launch_bounds__(THREADS) void join_attention_kernel(params a) {
+    const joined at_row(a.batch, a.q_heads, a.q_len, a.head_dim);
+    if (!at_row.some) return;
+    const int64_t rows = (int64_t)a.batch * a.q_heads * a.q_len, row = at_row.row;
+    float most = -INFINITY;
+    for (int s = 0; s < a.splits; ++s)
+        if (a.part_sum[s * rows + row] != 0.f) most = fmaxf(most, a.part_base[s * rows + row]);
+    float x[8] = {}, total = 0.f;
+    for (int s = 0; s < a.splits; ++s) {
+        const float sum = a.part_sum[s * rows + row];
+        const float keep = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(a.part_base[s * rows + row] - most);
+        const f32x8 o = *(const f32x8 *)(a.part + (s * rows + row) * a.head_dim + at_row.d);
+        if (sum != 0.f) {
+            total += sum * keep;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) x[u] += o[u] * keep;
+        }
+    }
+    const bool none = total == 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] *= none ? 0.f : 1.f / total;
+    store_eight<T>(at(a.out, at_row.b, at_row.h) + at_row.i * a.out.token, at_row.d, x);
+    if (at_row.d == 0) a.lse[row] = none ? -INFINITY : (most + __builtin_amdgcn_logf(total)) * LN2;
+}
+
+// out = factor * the sum of the splits' rows.
+template <typename T>
+__global__ __launch_bounds__(THREADS) void join_sums_kernel(const float *part, int splits, heads out, int batch, int n_heads, int len, int head_dim,
+                                                            float factor) {
+    const joined at_row(batch, n_heads, len, head_dim);
+    if (!at_row.some) return;
+    const int64_t rows = (int64_t)batch * n_heads * len;
+    float x[8] = {};
+    for (int s = 0; s < splits; ++s) {
+        const f32x8 o = *(const f32x8 *)(part + (s * rows + at_row.row) * head_dim + at_row.d);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] += o[u];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) x[u] *= factor;
+    store_eight<T>(at(out, at_row.b, at_row.h) + at_row.i * out.token, at_row.d, x);
+}
+
 // ------------------------------------------------------------------------------------ host
 constexpr int64_t MAX_LEN = 1 << 30;
+
+bool too_big(int64_t heads, int64_t batch, int64_t tiles) {
+    return heads * batch > INT32_MAX || heads * batch * tiles > INT32_MAX;
+}
 
 int check_sizes(const dear_attention_t *p) {
     if (!p) return DEAR_EINVAL;
@@ -955,6 +1073,8 @@ int check_sizes(const dear_attention_t *p) {
     if (p->dtype != DEAR_F32 && p->dtype != DEAR_BF16) return DEAR_EINVAL;
     if (p->causal != 0 && p->causal != 1) return DEAR_EINVAL;
     if (!(p->scale > 0.f) || !std::isfinite(p->scale)) return DEAR_EINVAL;
+    if (too_big(p->q_heads, p->batch, ceil_div(p->q_len, BLOCK)) || too_big(p->kv_heads, p->batch, ceil_div(p->kv_len, KEYS)))
+        return DEAR_ETOOBIG;
     return DEAR_OK;
 }
 
@@ -992,10 +1112,6 @@ params make(const dear_attention_t *p) {
 // Whether the rows of a step lie within 2^31 bytes, so that tiles can be filled directly.
 bool near(const dear_attention_t *p, const dear_heads_t &t) { return p->dtype == DEAR_BF16 && t.token_stride < (1 << 30) / STEP; }
 
-bool too_big(int64_t heads, int64_t batch, int64_t tiles) {
-    return heads * batch > INT32_MAX || heads * batch * tiles > INT32_MAX;
-}
-
 #define DEAR_BY_TYPE(p, kernel, grid, a, stream)                                                          \
     do {                                                                                                  \
         if ((p)->dtype == DEAR_BF16 && (p)->head_dim <= 64) kernel<bf16, 64><<<grid, THREADS, 0, stream>>>(a); \
@@ -1004,6 +1120,66 @@ bool too_big(int64_t heads, int64_t batch, int64_t tiles) {
         else kernel<float, 128><<<grid, THREADS, 0, stream>>>(a);                                         \
     } while (0)
 
+// Splits of the sequence that workgroups go through, where there are too few of them for the chip: the number with the least
+// time by this estimate, in microseconds.  The chip takes 256 * `resident` workgroups at a time; one goes through its share of
+// the steps in `step` each; joining the splits costs `join`, and 3 TB/s for `bytes` of output each.  Measured with and without:
+// one query, 8 heads, 8192 keys of 128 values 29 and 164 us; 4 sequences of 656 with 2 key heads for 8, backward 45 and 88.
+int splits_for(int64_t groups, int64_t steps, double step, double resident, double join, double bytes) {
+    int best = 1;
+    double least = 0;
+    for (int64_t s = 1; s <= 16 && (s == 1 || s <= steps); ++s) {
+        const double t = std::ceil((double)(groups * s) / (256 * resident)) * (double)ceil_div(steps, s) * step +
+                         (s == 1 ? 0 : join + (double)s * bytes / 3e6);
+        if (s == 1 || t < least) best = (int)s, least = t;
+    }
+    return best;
+}
+
+// A step of 64 keys or queries: bf16, waiting for its loads, 0.6 to 1.5 us; fp32, by its matrix instructions, 4.2 and, with the
+// backward pass's products, 7.5 for each 64 values of a row.  Causal calls do half of the steps.
+int64_t steps_of(const dear_attention_t *p, int64_t length) { return ceil_div(ceil_div(length, STEP), p->causal ? 2 : 1); }
+
+int q_splits(const dear_attention_t *p, bool backward) {
+    const bool wide = p->head_dim > 64, f32 = p->dtype == DEAR_F32;
+    const double step = f32 ? (backward ? 7.5 : 4.2) * (wide ? 2 : 1) : (backward ? 0.8 : 0.6) * (wide ? 1.5 : 1);
+    const int64_t rows = p->q_len * p->batch * p->q_heads;
+    return splits_for(ceil_div(p->q_len, BLOCK) * p->batch * p->q_heads, steps_of(p, p->kv_len), step, f32 ? 1 : wide || backward ? 2 : 4, 8,
+                      (double)(rows * p->head_dim * 4));
+}
+int kv_splits(const dear_attention_t *p, int keys) {
+    const bool wide = p->head_dim > 64, f32 = p->dtype == DEAR_F32;
+    const double step = (f32 ? 7.5 * (wide ? 2 : 1) : wide ? 1.2 : 1) * (p->q_heads / p->kv_heads);
+    const int64_t rows = p->kv_len * p->batch * p->kv_heads;
+    return splits_for(ceil_div(p->kv_len, keys) * p->batch * p->kv_heads, steps_of(p, p->q_len), step, f32 || wide ? 1 : 2, 16,
+                      (double)(2 * rows * p->head_dim * 4));
+}
+
+// What the splits' outputs take until they are joined.
+int64_t forward_bytes(const dear_attention_t *p) {
+    const int n = q_splits(p, false);
+    return n > 1 ? ceil_div(n * p->q_len * p->batch * p->q_heads * (p->head_dim + 2) * 4, 256) * 256 : 0;
+}
+int64_t dq_bytes(const dear_attention_t *p) {
+    const int n = q_splits(p, true);
+    return n > 1 ? n * p->q_len * p->batch * p->q_heads * p->head_dim * 4 : 0;
+}
+int64_t dkv_bytes(const dear_attention_t *p, int keys) {
+    const int n = kv_splits(p, keys);
+    return n > 1 ? 2 * n * p->kv_len * p->batch * p->kv_heads * p->head_dim * 4 : 0;
+}
+int64_t rows_bytes(const dear_attention_t *p) { return ceil_div(p->q_len, BLOCK) * BLOCK * p->batch * p->q_heads * 8; }
+
+int check_workspace(const dear_attention_t *p, int64_t need) {
+    if (need == 0) return DEAR_OK;
+    if (!p->workspace) return DEAR_EINVAL;
+    if (!aligned(p->workspace, 256)) return DEAR_EALIGN;
+    return p->workspace_bytes < need ? DEAR_ETOOBIG : DEAR_OK;
+}
+
+unsigned join_grid(const dear_attention_t *p, int64_t heads, int64_t len) {
+    return (unsigned)ceil_div(p->batch * heads * len * (p->head_dim / 8), THREADS);
+}
+
 }  // namespace
 
 extern "C" {
@@ -1011,14 +1187,19 @@ extern "C" {
 int dear_attention_workspace(const dear_attention_t *p, int64_t *bytes) {
     if (!bytes) return DEAR_EINVAL;
     if (int rc = check_sizes(p)) return rc;
-    *bytes = 0;
+    *bytes = forward_bytes(p);
     return DEAR_OK;
 }
 
 int dear_attention_backward_workspace(const dear_attention_t *p, int64_t *bytes) {
     if (!bytes) return DEAR_EINVAL;
     if (int rc = check_sizes(p)) return rc;
-    *bytes = ceil_div(p->q_len, BLOCK) * BLOCK * p->batch * p->q_heads * 8;  // of every query of every tile two values
+    // of every query of every tile two values, and the splits' outputs, dq's and then dk's and dv's; strides may call for
+    // either width of tiles
+    int64_t parts = dq_bytes(p);
+    for (int keys : {KEYS, BLOCK})
+        if (dkv_bytes(p, keys) > parts) parts = dkv_bytes(p, keys);
+    *bytes = rows_bytes(p) + parts;
     return DEAR_OK;
 }
 
@@ -1031,16 +1212,25 @@ int dear_attention(const dear_attention_t *p, void *hip_stream) {
     if (p->batch == 0 || p->q_len == 0) return DEAR_OK;
     if (!p->lse) return DEAR_EINVAL;
     if (!aligned(p->lse, 4)) return DEAR_EALIGN;
+    if (int rc = check_workspace(p, forward_bytes(p))) return rc;
     params a = make(p);
-    a.tiles = (int32_t)ceil_div(p->q_len, BLOCK);
-    if (too_big(p->q_heads, p->batch, a.tiles)) return DEAR_ETOOBIG;
-    const unsigned grid = (unsigned)a.tiles * p->q_heads * p->batch;
+    a.tiles = (int32_t)ceil_div(p->q_len, BLOCK), a.splits = q_splits(p, false);
+    const int64_t rows = p->q_len * p->batch * p->q_heads;
+    a.part = (float *)p->workspace, a.part_base = a.part + a.splits * rows * p->head_dim, a.part_sum = a.part_base + a.splits * rows;
+    const unsigned grid = (unsigned)a.tiles * p->q_heads * p->batch * a.splits;
     hipStream_t stream = (hipStream_t)hip_stream;
     const bool direct = near(p, p->k) && near(p, p->v);
     if (direct && p->head_dim <= 64) attention_direct_kernel<64><<<grid, THREADS, 0, stream>>>(a);
     else if (direct) attention_direct_kernel<128><<<grid, THREADS, 0, stream>>>(a);
     else DEAR_BY_TYPE(p, attention_kernel, grid, a, stream);
-    return launch_status();
+    if (int rc = launch_status()) return rc;
+    if (a.splits > 1) {
+        const unsigned join = join_grid(p, p->q_heads, p->q_len);
+        if (p->dtype == DEAR_BF16) join_attention_kernel<bf16><<<join, THREADS, 0, stream>>>(a);
+        else join_attention_kernel<float><<<join, THREADS, 0, stream>>>(a);
+        return launch_status();
+    }
+    return DEAR_OK;
 }
 
 int dear_attention_backward(const dear_attention_t *p, void *hip_stream) {
@@ -1053,35 +1243,51 @@ int dear_attention_backward(const dear_attention_t *p, void *hip_stream) {
     for (const dear_heads_t *t : {&p->dk, &p->dv})
         if (int rc = check_heads(*t, p, p->kv_len, true)) return rc;
     if (p->batch == 0 || (p->q_len == 0 && p->kv_len == 0)) return DEAR_OK;
+    if (p->q_len > 0) {
+        if (!p->lse) return DEAR_EINVAL;
+        if (!aligned(p->lse, 4)) return DEAR_EALIGN;
+    }
     int64_t need = 0;
     (void)dear_attention_backward_workspace(p, &need);
-    if (need) {
-        if (!p->lse || !p->workspace) return DEAR_EINVAL;
-        if (!aligned(p->lse, 4) || !aligned(p->workspace, 256)) return DEAR_EALIGN;
-        if (p->workspace_bytes < need) return DEAR_ETOOBIG;
-    }
+    if (int rc = check_workspace(p, need)) return rc;
     params a = make(p);
     const bool direct = near(p, p->q) && near(p, p->dout) && near(p, p->k) && near(p, p->v);
     hipStream_t stream = (hipStream_t)hip_stream;
-    const int64_t q_tiles = ceil_div(p->q_len, BLOCK), kv_tiles = ceil_div(p->kv_len, direct && p->head_dim <= 64 ? BLOCK : KEYS);
-    if (too_big(p->q_heads, p->batch, q_tiles) || too_big(p->kv_heads, p->batch, kv_tiles)) return DEAR_ETOOBIG;
+    const int keys = direct && p->head_dim <= 64 ? BLOCK : KEYS;
+    const int64_t q_tiles = ceil_div(p->q_len, BLOCK), kv_tiles = ceil_div(p->kv_len, keys);
     a.q_tiles = (int32_t)q_tiles;
     a.powers = (float *)p->workspace, a.deltas = a.powers + q_tiles * BLOCK * p->batch * p->q_heads;
+    a.part = (float *)((char *)p->workspace + rows_bytes(p));
+    auto join = [&](const float *part, const heads &out, int n_heads, int64_t len, float factor) {
+        const unsigned grid = join_grid(p, n_heads, len);
+        if (p->dtype == DEAR_BF16)
+            join_sums_kernel<bf16><<<grid, THREADS, 0, stream>>>(part, a.splits, out, p->batch, n_heads, (int)len, p->head_dim, factor);
+        else
+            join_sums_kernel<float><<<grid, THREADS, 0, stream>>>(part, a.splits, out, p->batch, n_heads, (int)len, p->head_dim, factor);
+        return launch_status();
+    };
     if (q_tiles) {
-        a.tiles = (int32_t)q_tiles;
-        const unsigned grid = (unsigned)q_tiles * p->q_heads * p->batch;
+        a.tiles = (int32_t)q_tiles, a.splits = q_splits(p, true);
+        const unsigned grid = (unsigned)q_tiles * p->q_heads * p->batch * a.splits;
         if (direct && p->head_dim <= 64) attention_dq_direct_kernel<64><<<grid, THREADS, 0, stream>>>(a);
         else if (direct) attention_dq_direct_kernel<128><<<grid, THREADS, 0, stream>>>(a);
         else DEAR_BY_TYPE(p, attention_dq_kernel, grid, a, stream);
         if (int rc = launch_status()) return rc;
+        if (a.splits > 1)
+            if (int rc = join(a.part, a.dq, p->q_heads, p->q_len, p->scale)) return rc;
     }
     if (kv_tiles) {
-        a.tiles = (int32_t)kv_tiles;
-        const unsigned grid = (unsigned)kv_tiles * p->kv_heads * p->batch;
+        a.tiles = (int32_t)kv_tiles, a.splits = kv_splits(p, keys);
+        const unsigned grid = (unsigned)kv_tiles * p->kv_heads * p->batch * a.splits;
         if (direct && p->head_dim <= 64) attention_dkv_direct_kernel<<<grid, THREADS, 0, stream>>>(a);
         else if (direct) attention_dkv_halves_kernel<<<grid, 64 * KV_WAVES, 0, stream>>>(a);
         else DEAR_BY_TYPE(p, attention_dkv_kernel, grid, a, stream);
         if (int rc = launch_status()) return rc;
+        if (a.splits > 1) {
+            const int64_t all = a.splits * p->kv_len * p->batch * p->kv_heads * p->head_dim;
+            if (int rc = join(a.part, a.dk, p->kv_heads, p->kv_len, p->scale)) return rc;
+            if (int rc = join(a.part + all, a.dv, p->kv_heads, p->kv_len, 1.f)) return rc;
+        }
     }
     return DEAR_OK;
 }

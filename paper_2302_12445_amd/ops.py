@@ -92,16 +92,24 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda in
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _on_its_device(f):
-    """Makes the device of the call's first tensor the current one, where it is not."""
-    @functools.wraps(f)
-    def call(t, *args, **kwargs):
-        first = t.codes if type(t) is Checkpoint else t
-        if not first.is_cuda or first.get_device() == _current_device():
-            return f(t, *args, **kwargs)
-        with torch.cuda.device(first.device):
-            return f(t, *args, **kwargs)
-    return call
+def _elsewhere(t: torch.Tensor) -> bool:
+    """Whether the call has to be made again with the tensor's device as the current one."""
+    return t.is_cuda and t.get_device() != _current_device()
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention_workspace(name: str, *head) -> int:
+    need = C.c_int64()
+    _check(getattr(load_library(), name)(_ATTENTION.pack(*head, *([0] * 37)), C.byref(need)), name)
+    return need.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _workspace(name: str, *sizes) -> int:
+    """Bytes that a call of these sizes needs."""
+    need = C.c_int64()
+    _check(getattr(load_library(), name)(*sizes, C.byref(need)), name)
+    return need.value
 
 
 # ------------------------------------------------------------------------------------ attention
@@ -157,7 +165,6 @@ def _attention_sizes(q, k, v, causal, scale, q_lens, kv_lens):
                                         0 if q_lens is None else q_lens.data_ptr(), 0 if kv_lens is None else kv_lens.data_ptr())
 
 
-@_on_its_device
 def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
               q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None
               ) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -166,28 +173,30 @@ def attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = 
     Gives (out [B, Sq, H, D], lse [B, H, Sq] fp32).  scale: 1 / sqrt(D) by default.  q_lens, kv_lens: int32 [B], the
     valid tokens of each sequence.  causal: the last valid query sees all valid keys, the one before it one less.
     """
+    if _elsewhere(q):
+        with torch.cuda.device(q.device):
+            return attention(q, k, v, causal, scale, q_lens, kv_lens)
     kept, places, head = _attention_sizes(q, k, v, causal, scale, q_lens, kv_lens)  # kept: until the work is enqueued
     B, H, _, D, Sq = head[:5]
     lib = load_library()
     out, po = _new(q, (B, Sq, H, D))
     lse = torch.empty((B, H, Sq), dtype=torch.float32, device=q.device)
-    args = (*head, *places, *po, lse.data_ptr(), *_NONE, *_NONE, *_NONE, *_NONE)
-    packed = _ATTENTION.pack(*args, 0, 0)
-    need = C.c_int64()
-    _check(lib.dear_attention_workspace(packed, C.byref(need)), "dear_attention_workspace")
-    if need.value:
-        space = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-        packed = _ATTENTION.pack(*args, space.data_ptr(), need.value)
-    _check(lib.dear_attention(packed, _raw_stream(q.get_device())), "dear_attention")
+    need, space = _attention_workspace("dear_attention_workspace", *head[:10]), None
+    if need:
+        space = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(lib.dear_attention(_ATTENTION.pack(*head, *places, *po, lse.data_ptr(), *_NONE, *_NONE, *_NONE, *_NONE,
+                                              space.data_ptr() if need else 0, need), _raw_stream(q.get_device())), "dear_attention")
     return out, lse
 
 
-@_on_its_device
 def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
                        lse: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
                        q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None
                        ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Gradients (dq, dk, dv) from the gradient of out and what attention() gave, with the same arguments."""
+    if _elsewhere(dout):
+        with torch.cuda.device(dout.device):
+            return attention_backward(dout, q, k, v, out, lse, causal, scale, q_lens, kv_lens)
     kept, places, head = _attention_sizes(q, k, v, causal, scale, q_lens, kv_lens)
     B, H, Hkv, D, Sq, Sk = head[:6]
     _like(out, q, "out")
@@ -199,12 +208,10 @@ def attention_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: 
     (out, po), (dout, pd) = _readable(out, "out"), _readable(dout, "dout")
     lib = load_library()
     (dq, gq), (dk, gk), (dv, gv) = _new(q, (B, Sq, H, D)), _new(k, (B, Sk, Hkv, D)), _new(v, (B, Sk, Hkv, D))
-    args = (*head, *places, *po, lse.data_ptr(), *pd, *gq, *gk, *gv)
-    need = C.c_int64()
-    _check(lib.dear_attention_backward_workspace(_ATTENTION.pack(*args, 0, 0), C.byref(need)), "dear_attention_backward_workspace")
-    space = torch.empty(need.value, dtype=torch.uint8, device=q.device)
-    _check(lib.dear_attention_backward(_ATTENTION.pack(*args, space.data_ptr(), need.value), _raw_stream(q.get_device())),
-           "dear_attention_backward")
+    need = _attention_workspace("dear_attention_backward_workspace", *head[:10])
+    space = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(lib.dear_attention_backward(_ATTENTION.pack(*head, *places, *po, lse.data_ptr(), *pd, *gq, *gk, *gv, space.data_ptr(), need),
+                                       _raw_stream(q.get_device())), "dear_attention_backward")
     return dq, dk, dv
 
 
@@ -250,9 +257,11 @@ def _checkpoint(kept: Checkpoint) -> int:
     return rows
 
 
-@_on_its_device
 def checkpoint_encode(x: torch.Tensor) -> Checkpoint:
     """x [..., cols] in 8 bits: 32 neighbours of a row share the smallest power of two with which they fit 127."""
+    if _elsewhere(x):
+        with torch.cuda.device(x.device):
+            return checkpoint_encode(x)
     d = _dtype(x, "x")
     r, rows, cols, stride = _as_rows(x, "x")
     kept = _empty_checkpoint(rows, cols, x.device)
@@ -261,9 +270,11 @@ def checkpoint_encode(x: torch.Tensor) -> Checkpoint:
     return kept
 
 
-@_on_its_device
 def checkpoint_decode(kept: Checkpoint, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """What a checkpoint holds, [rows, cols]; exact in either type."""
+    if _elsewhere(kept.codes):
+        with torch.cuda.device(kept.codes.device):
+            return checkpoint_decode(kept, dtype)
     rows = _checkpoint(kept)
     if dtype not in _DTYPE:
         raise ValueError("%s: bfloat16 and float32 are supported" % dtype)
@@ -274,10 +285,12 @@ def checkpoint_decode(kept: Checkpoint, dtype: torch.dtype = torch.bfloat16) -> 
     return out
 
 
-@_on_its_device
 def checkpoint_weight_grad(dy: torch.Tensor, kept: Checkpoint) -> torch.Tensor:
     """Gradient [outs, ins] in fp32 of a linear layer's weight, from its output's gradient dy [..., outs] and the
     checkpoint of its input [rows, ins]."""
+    if _elsewhere(dy):
+        with torch.cuda.device(dy.device):
+            return checkpoint_weight_grad(dy, kept)
     rows = _checkpoint(kept)
     d = _dtype(dy, "dy")
     r, dy_rows, outs, stride = _as_rows(dy, "dy")
@@ -286,12 +299,11 @@ def checkpoint_weight_grad(dy: torch.Tensor, kept: Checkpoint) -> torch.Tensor:
         raise ValueError("dy has %d rows on %s, the checkpoint %d on %s" % (dy_rows, dy.device, rows, codes.device))
     lib = load_library()
     dw = torch.empty((outs, ins), dtype=torch.float32, device=dy.device)
-    need, space = C.c_int64(), None
-    _check(lib.dear_checkpoint_weight_grad_workspace(d, rows, outs, ins, C.byref(need)), "dear_checkpoint_weight_grad_workspace")
-    if need.value:
-        space = torch.empty(need.value, dtype=torch.uint8, device=dy.device)
+    need, space = _workspace("dear_checkpoint_weight_grad_workspace", d, rows, outs, ins), None
+    if need:
+        space = torch.empty(need, dtype=torch.uint8, device=dy.device)
     _check(lib.dear_checkpoint_weight_grad(r.data_ptr(), d, stride, codes.data_ptr(), exponents.data_ptr(), rows, outs, ins, dw.data_ptr(),
-                                           None if space is None else space.data_ptr(), need.value, _raw_stream(dy.get_device())),
+                                           space.data_ptr() if need else None, need, _raw_stream(dy.get_device())),
            "dear_checkpoint_weight_grad")
     return dw
 
@@ -302,7 +314,6 @@ def _weight(weight: torch.Tensor, cols: int, device) -> None:
         raise ValueError("weight: expected a contiguous float32 tensor of %d on %s" % (cols, device))
 
 
-@_on_its_device
 def add_rms_norm(x: torch.Tensor, residual: Optional[torch.Tensor], weight: torch.Tensor, eps: float = 1e-5,
                  keep: bool = True) -> Tuple[torch.Tensor, torch.Tensor, Optional[Checkpoint], torch.Tensor]:
     """h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight over the last axis.
@@ -310,6 +321,9 @@ def add_rms_norm(x: torch.Tensor, residual: Optional[torch.Tensor], weight: torc
     Gives (h, y, kept, rstd): h and y of x's type and shape, kept the checkpoint of y in 8 bits (None without `keep`),
     rstd fp32 [rows].  residual None: h is x itself.  weight: fp32.
     """
+    if _elsewhere(x):
+        with torch.cuda.device(x.device):
+            return add_rms_norm(x, residual, weight, eps, keep)
     d = _dtype(x, "x")
     r, rows, cols, stride = _as_rows(x, "x")
     device, shape = x.device, x.shape
@@ -332,11 +346,13 @@ def add_rms_norm(x: torch.Tensor, residual: Optional[torch.Tensor], weight: torc
     return h, y, kept, rstd
 
 
-@_on_its_device
 def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor, rstd: torch.Tensor,
                           dh: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Gradients (dx, dweight): dx of x and of residual alike, dweight fp32.  dh: the gradient that reaches h by other
     ways than the norm."""
+    if _elsewhere(dy):
+        with torch.cuda.device(dy.device):
+            return add_rms_norm_backward(dy, h, weight, rstd, dh)
     d = _dtype(dy, "dy")
     device, shape = dy.device, dy.shape
     for t, what in ((h, "h"), (dh, "dh")):
@@ -353,11 +369,10 @@ def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tenso
     lib = load_library()
     dx = _empty_as(dy)
     dweight = torch.empty(cols, dtype=torch.float32, device=device)
-    need = C.c_int64()
-    _check(lib.dear_add_rms_norm_backward_workspace(d, rows, cols, C.byref(need)), "dear_add_rms_norm_backward_workspace")
-    space = torch.empty(need.value, dtype=torch.uint8, device=device)
+    need = _workspace("dear_add_rms_norm_backward_workspace", d, rows, cols)
+    space = torch.empty(need, dtype=torch.uint8, device=device)
     _check(lib.dear_add_rms_norm_backward(
         ry.data_ptr(), dy_stride, rh.data_ptr(), h_stride, None if rd is None else rd.data_ptr(), dh_stride, weight.data_ptr(),
-        rstd.data_ptr(), d, rows, cols, dx.data_ptr(), dweight.data_ptr(), space.data_ptr(), need.value, _raw_stream(dy.get_device())),
+        rstd.data_ptr(), d, rows, cols, dx.data_ptr(), dweight.data_ptr(), space.data_ptr(), need, _raw_stream(dy.get_device())),
         "dear_add_rms_norm_backward")
     return dx, dweight

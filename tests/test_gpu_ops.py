@@ -92,6 +92,23 @@ def test_attention_lengths(ops, dim, causal, dtype):
         assert not out[2, :50].any() and (lse[2, :, :50] == -math.inf).all() and not dq[2, :50].any()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", [(1, 3, 2000, 2, 1, 64), (2, 200, 900, 1, 1, 128), (1, 1500, 130, 2, 2, 40), (2, 640, 640, 4, 1, 64),
+                                   (1, 900, 1100, 3, 1, 104)])
+def test_attention_few_rows(ops, shape, causal, dtype):
+    """Calls of few workgroups, which split the sequences; lengths that leave splits, or all of them, without a token."""
+    B, Sq, Sk, H, Hkv, D = shape
+    print("case few rows", shape, causal, dtype, flush=True)
+    gen = torch.Generator().manual_seed(sum(shape))
+    q, k, v = normal(gen, (B, Sq, H, D), dtype), normal(gen, (B, Sk, Hkv, D), dtype), normal(gen, (B, Sk, Hkv, D), dtype)
+    check_attention(ops, q, k, v, causal, label="whole")
+    check_attention(ops, q, k, v, causal, q_lens=[Sq] + [Sq // 3] * (B - 1), kv_lens=[Sk // 5] + [Sk] * (B - 1), label="short")
+    check_attention(ops, q, k, v, causal, q_lens=[Sq] * B, kv_lens=[0] + [1] * (B - 1), label="none")
+    k[:, Sk // 2] *= 30  # one split has the maximum of most rows
+    check_attention(ops, q, k, v, causal, label="maximum")
+
+
 def test_attention_of_nothing(ops):
     for B, Sq, Sk in ((0, 4, 4), (2, 0, 4), (2, 4, 0), (2, 0, 0)):
         q, k = torch.zeros(B, Sq, 2, 64, dtype=BF16, device=DEV), torch.zeros(B, Sk, 2, 64, dtype=BF16, device=DEV)
