@@ -50,7 +50,8 @@ typedef struct {
  * (the last query sees the last key), with nq = q_lens[b], nk = kv_lens[b] clamped to
  * 0 .. q_len, 0 .. kv_len.  A query that sees no key gets out = 0, lse = -inf and gradients of 0; a
  * key that no query sees gets gradients of 0.  What stands in tokens beyond the lengths is never
- * used.  Query head h reads key head h / (q_heads / kv_heads).
+ * used.  Within them values are taken to be finite: a NaN or an infinity there may also reach rows of
+ * its sequence that it is not visible to (0 * infinity).  Query head h reads key head h / (q_heads / kv_heads).
  * Products are taken of the inputs' type (fp32: fp32 matrix instructions); sums, the softmax and lse
  * are fp32.  In bf16 the probabilities and, in the backward pass, the gradients of s are rounded to
  * bf16 as operands of the second products.  */

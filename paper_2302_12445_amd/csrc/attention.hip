@@ -1,4 +1,19 @@
 // Attention and its backward pass (formulas: dear_ops.h).
+//
+// Forward: one pass over the keys with the running maximum m and sum l of a row; a step's scores s give p = exp(s - m), and what
+// was summed before is multiplied by exp(m_before - m).  Backward: p = exp(s - lse) again from q, k and lse, so that no matrix of
+// queries by keys is ever in memory; with delta = dout . out (its row sum), ds = p * (dout v' - delta):
+//     dq = scale * ds k      dk = scale * ds' q      dv = p' dout
+// dq sums over keys and dk, dv over queries: a kernel for each, that computes s and dout v' for itself (7 products for the 5 that
+// one pass needs), as sums over workgroups would take atomics, whose order changes results, or fp32 copies in memory.
+//
+// Layout of products.  A wave owns 32 rows of one sequence, and a step's first products are taken with these as columns: a lane
+// then holds values of one of its rows (with lane + 32 all of them), so that maxima, sums, lse and delta need one value a lane and
+// the result, rounded to the type, is the next product's operand as it stands.  Operands that are summed over their rows are read
+// from LDS with the transposing reads.
+//
+// Roundings.  Scores, p, ds, maxima and all sums are fp32.  In bf16 p and ds are rounded to bf16, as the matrix instructions take
+// both operands in one type: 2^-9 of each, no more than the inputs' own rounding.  The sum l is of the p before their rounding.
 #include <cmath>
 #include <type_traits>
 
@@ -16,8 +31,8 @@ constexpr int BLOCK = 32 * WAVES;  // rows that a workgroup owns: 32 for each wa
 constexpr int STEP = 64;           // rows of the other sequence that it takes at a time
 constexpr int KEYS = 64;           // keys of a workgroup that computes dk and dv
 
-// Waves of a SIMD that the kernels are compiled for.  With two, one's products run beside the other's softmax; wide rows
-// of fp32, and wide dk and dv with their operands, take the registers of both.
+// Waves of a SIMD that the kernels of this part are compiled for.  With two, one's products run beside the other's softmax; wide
+// rows of fp32, and wide dk and dv with their operands, take the registers of both.
 template <typename T, int W> constexpr int resident(bool dkv) {
     return sizeof(T) == 2 ? (dkv && W == 128 ? 1 : 2) : (W == 128 || dkv ? 1 : 2);
 }
@@ -134,6 +149,9 @@ __device__ __forceinline__ char *part_row(const params &a, int heads, int len, i
 }
 
 // ------------------------------------------------------------------------------------ forward
+// fp32, and bf16 whose rows lie too far apart for the kernels below.  Tiles go through registers to LDS, a step's loads beside the
+// products of the step before.  In fp32 the matrix instructions bound it (154 TFLOP/s reached by large products): 3 x 385 queries
+// and keys, 12 heads of 64, 38 us a call.
 template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(false))) void attention_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
@@ -251,7 +269,7 @@ template <int W, int WAVES> struct direct_loads {
         for (int i = 0; i < N; ++i) {
             uint32_t r = row + i * WAVES * direct<W>::ROWS;
             if (left < STEP) r = min(r, (uint32_t)left - 1);
-            if (W % 64 != 0 || some) load_to_lds(p + (r * token + piece), s + (i * WAVES + wave) * 512);
+            if (some) load_to_lds(p + (r * token + piece), s + (i * WAVES + wave) * 512);
         }
     }
 };
@@ -276,6 +294,10 @@ template <int N, int AHEAD> __device__ __forceinline__ void read_ahead() {
     __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
 }
 
+// Forward in bf16: 128 queries a workgroup, 32 a wave, two workgroups' waves a SIMD, steps of 64 keys in two buffers that are
+// filled beside the products of the step before.  Long sequences are bound by the matrix instructions, beside which the powers run;
+// short ones by the latency of a step's loads and barrier.  Measured: 8192 queries and keys, causal, 16 heads of 128 for 4, 285 us
+// = 963 TFLOP/s; 16 sequences of 512 with ragged lengths, 16 heads of 64, 24 us = 2.3 TB/s; 128 queries and keys, 16 heads, 6 us.
 template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_direct_kernel(params a) {
     __shared__ __attribute__((aligned(16))) bf16 ks0[STEP * W], ks1[STEP * W], vs0[STEP * W], vs1[STEP * W];
     int b, h, t, split;
@@ -408,6 +430,7 @@ __device__ __forceinline__ float row_values(const params &a, int b, int h, int i
 
 // dq of 32 queries a wave, over all keys.  As in the forward pass the results of the first products are taken
 // transposed, a query to a lane, so that lse and delta are one value a lane.  It also writes delta for the other kernel.
+// fp32, 3 x 385 with ragged lengths, 12 heads of 64, in two splits: 44 us, by its matrix instructions.
 template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(false))) void attention_dq_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
@@ -488,7 +511,8 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
 
 // ------------------------------------------------------------------------------------ backward: keys and values
 // dk and dv of 32 keys a wave, over the queries of all heads that share them: one workgroup adds them all up, in order.
-// Two waves have the same keys and take every other 32 queries; their sums are added at the end.
+// Two waves have the same keys and take every other 32 queries; their sums are added at the end.  fp32, 3 x 385 with ragged
+// lengths, 12 heads of 64: 51 us, by its matrix instructions.
 template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(true))) void attention_dkv_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     __shared__ __attribute__((aligned(16))) float rows[2][STEP];  // what the queries' powers are taken against, and -delta
@@ -537,33 +561,30 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
                 gst.load(gp, a.dout.token, i0 + STEP, nq, a.head_dim);
                 load_z(i0 + STEP);
             }
-            {
-                const int qb = turn;
-                f32x16 s = {}, dp = {};
+            f32x16 s = {}, dp = {};
 #pragma unroll
-                for (int kk = 0; kk < W / 16; ++kk) {
-                    s = mma(straight<W>(qs, 32 * qb, kk, lane), k[kk], s);
-                    dp = mma(straight<W>(gs, 32 * qb, kk, lane), v[kk], dp);
-                }
-                const bool whole = i0 + 32 * qb >= wave_last && i0 + 32 * qb + 31 < nq;
+            for (int kk = 0; kk < W / 16; ++kk) {
+                s = mma(straight<W>(qs, 32 * turn, kk, lane), k[kk], s);
+                dp = mma(straight<W>(gs, 32 * turn, kk, lane), v[kk], dp);
+            }
+            const bool whole = i0 + 32 * turn >= wave_last && i0 + 32 * turn + 31 < nq;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int n = 32 * qb + row_of(r, half);
-                    const float p = __builtin_amdgcn_exp2f(s[r] * c - rows[0][n]);
-                    s[r] = whole || (i0 + n >= first && i0 + n < nq) ? p : 0.f;
-                    dp[r] = s[r] * (dp[r] + rows[1][n]);
-                }
+            for (int r = 0; r < 16; ++r) {
+                const int n = 32 * turn + row_of(r, half);
+                const float p = __builtin_amdgcn_exp2f(s[r] * c - rows[0][n]);
+                s[r] = whole || (i0 + n >= first && i0 + n < nq) ? p : 0.f;
+                dp[r] = s[r] * (dp[r] + rows[1][n]);
+            }
 #pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    float x[8], y[8];
+            for (int st = 0; st < 2; ++st) {
+                float x[8], y[8];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) x[u] = s[8 * st + u], y[u] = dp[8 * st + u];
-                    const frag<T> p = to_frag<T>(x), ds = to_frag<T>(y);
+                for (int u = 0; u < 8; ++u) x[u] = s[8 * st + u], y[u] = dp[8 * st + u];
+                const frag<T> p = to_frag<T>(x), ds = to_frag<T>(y);
 #pragma unroll
-                    for (int db = 0; db < W / 32; ++db) {
-                        dv[db] = mma(transposed<W>(gs, 32 * qb + 16 * st, 32 * db, lane), p, dv[db]);
-                        dk[db] = mma(transposed<W>(qs, 32 * qb + 16 * st, 32 * db, lane), ds, dk[db]);
-                    }
+                for (int db = 0; db < W / 32; ++db) {
+                    dv[db] = mma(transposed<W>(gs, 32 * turn + 16 * st, 32 * db, lane), p, dv[db]);
+                    dk[db] = mma(transposed<W>(qs, 32 * turn + 16 * st, 32 * db, lane), ds, dk[db]);
                 }
             }
         }
@@ -595,6 +616,9 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
 }
 
 // ------------------------------------------------------------------------------------ bf16 backward, tiles filled directly
+// dq as above, its tiles as in the forward pass.  Bound by the matrix instructions where sequences are long: 2 x 4096, causal, 16
+// heads of 128 for 4, 201 us = 1026 TFLOP/s of its three products; by the latency of steps where they are short: 16 x 512, ragged,
+// 16 heads of 64, 35 us.  Three waves a SIMD have too few registers (1 x 2048, causal, with dk and dv: 91 us for 84).
 template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_direct_kernel(params a) {
     __shared__ __attribute__((aligned(16))) bf16 ks0[STEP * W], ks1[STEP * W], vs0[STEP * W], vs1[STEP * W];
     int b, h, t, split;
@@ -693,7 +717,7 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_dire
 }
 
 // dk and dv of 128 keys a workgroup, 32 a wave, for rows of 64 values: the operands and sums of both fit a wave beside a
-// second one.
+// second one.  16 x 512, ragged, 16 heads: 44 us, by the latency of steps; in two kinds of waves as below 68 us.
 __global__ __launch_bounds__(THREADS, 2) void attention_dkv_direct_kernel(params a) {
     constexpr int W = 64;
     __shared__ __attribute__((aligned(16))) bf16 qs0[STEP * W], qs1[STEP * W], gs0[STEP * W], gs1[STEP * W];
@@ -808,11 +832,13 @@ __global__ __launch_bounds__(THREADS, 2) void attention_dkv_direct_kernel(params
     store_row<bf16, W>(at(a.dv, b, kvh) + j * a.dv.token, dv, 1.f, a.head_dim, half);
 }
 
-// dk and dv of 64 keys a workgroup of eight waves, for rows of 128 values.  Four compute probabilities and dv, four the gradients of the scores
-// and dk: so each half needs the operands and sums of one of the two, two waves fit a SIMD, and there (waves w and w + 4)
-// one of either kind runs beside the other.  Two waves of a kind have the same 32 keys and take every other 32 queries;
-// their sums are added at the end.  Step n: the first kind computes s, p and dv of tile n and leaves p in LDS; the second
-// takes p of tile n - 1, its dp from the step before, and computes dk of tile n - 1, then dp of tile n.
+// dk and dv of 64 keys a workgroup of eight waves, for rows of 128 values.  Four compute probabilities and dv, four the
+// gradients of the scores and dk: so each half needs the operands and sums of one of the two, two waves fit a SIMD, and there
+// (waves w and w + 4) one of either kind runs beside the other.  Two waves of a kind have the same 32 keys and take every other
+// 32 queries; their sums are added at the end.  Step n: the first kind computes s, p and dv of tile n and leaves p, in fp32, in
+// LDS; the second takes p of tile n - 1, its dp from the step before, and computes dk of tile n - 1, then dp of tile n.
+// Bound by the matrix instructions: 2 x 4096, causal, 16 heads of 128 for 4, 291 us = 945 TFLOP/s of its four products; all in
+// one kind of waves, one a SIMD, 434 us.
 constexpr int KV_WAVES = 8;
 
 __global__ __launch_bounds__(64 * KV_WAVES, 2) void attention_dkv_halves_kernel(params a) {
@@ -1109,7 +1135,8 @@ params make(const dear_attention_t *p) {
     return a;
 }
 
-// Whether the rows of a step lie within 2^31 bytes, so that tiles can be filled directly.
+// Whether the rows of a step lie within 2^31 bytes, so that tiles can be filled directly.  With and without: 2 x 4096, causal, 16
+// heads of 128 for 4, forward 160 and 185 us, backward 492 and 812; 16 x 512, 16 heads of 64, 30 and 33, 91 and 126.
 bool near(const dear_attention_t *p, const dear_heads_t &t) { return p->dtype == DEAR_BF16 && t.token_stride < (1 << 30) / STEP; }
 
 #define DEAR_BY_TYPE(p, kernel, grid, a, stream)                                                          \
