@@ -14,6 +14,7 @@
 //
 // Roundings.  Scores, p, ds, maxima and all sums are fp32.  In bf16 p and ds are rounded to bf16, as the matrix instructions take
 // both operands in one type: 2^-9 of each, no more than the inputs' own rounding.  The sum l is of the p before their rounding.
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -1149,35 +1150,33 @@ bool near(const dear_attention_t *p, const dear_heads_t &t) { return p->dtype ==
 
 // Splits of the sequence that workgroups go through, where there are too few of them for the chip: the number with the least
 // time by this estimate, in microseconds.  The chip takes 256 * `resident` workgroups at a time; one goes through its share of
-// the steps in `step` each; joining the splits costs `join`, and 3 TB/s for `bytes` of output each.  Measured with and without:
+// the steps in `step` each (in a causal call the longest does, and all together half of them); joining the splits costs `join`, and 3 TB/s for `bytes` of output each.  Measured with and without:
 // one query, 8 heads, 8192 keys of 128 values 29 and 164 us; 4 sequences of 656 with 2 key heads for 8, backward 45 and 88.
-int splits_for(int64_t groups, int64_t steps, double step, double resident, double join, double bytes) {
+int splits_for(const dear_attention_t *p, int64_t groups, int64_t steps, double step, double resident, double join, double bytes) {
     int best = 1;
     double least = 0;
     for (int64_t s = 1; s <= 16 && (s == 1 || s <= steps); ++s) {
-        const double t = std::ceil((double)(groups * s) / (256 * resident)) * (double)ceil_div(steps, s) * step +
-                         (s == 1 ? 0 : join + (double)s * bytes / 3e6);
+        const double turns = (double)(groups * s) / (256 * resident), share = (double)ceil_div(steps, s) * step;
+        const double t = (p->causal ? std::fmax(1, turns / 2) : std::ceil(turns)) * share + (s == 1 ? 0 : join + (double)s * bytes / 3e6);
         if (s == 1 || t < least) best = (int)s, least = t;
     }
     return best;
 }
 
 // A step of 64 keys or queries: bf16, waiting for its loads, 0.6 to 1.5 us; fp32, by its matrix instructions, 4.2 and, with the
-// backward pass's products, 7.5 for each 64 values of a row.  Causal calls do half of the steps.
-int64_t steps_of(const dear_attention_t *p, int64_t length) { return ceil_div(ceil_div(length, STEP), p->causal ? 2 : 1); }
-
+// backward pass's products, 7.5 for each 64 values of a row.
 int q_splits(const dear_attention_t *p, bool backward) {
     const bool wide = p->head_dim > 64, f32 = p->dtype == DEAR_F32;
     const double step = f32 ? (backward ? 7.5 : 4.2) * (wide ? 2 : 1) : (backward ? 0.8 : 0.6) * (wide ? 1.5 : 1);
     const int64_t rows = p->q_len * p->batch * p->q_heads;
-    return splits_for(ceil_div(p->q_len, BLOCK) * p->batch * p->q_heads, steps_of(p, p->kv_len), step, f32 ? 1 : wide || backward ? 2 : 4, 8,
+    return splits_for(p, ceil_div(p->q_len, BLOCK) * p->batch * p->q_heads, ceil_div(p->kv_len, STEP), step, f32 ? 1 : wide || backward ? 2 : 4, 8,
                       (double)(rows * p->head_dim * 4));
 }
 int kv_splits(const dear_attention_t *p, int keys) {
     const bool wide = p->head_dim > 64, f32 = p->dtype == DEAR_F32;
     const double step = (f32 ? 7.5 * (wide ? 2 : 1) : wide ? 1.2 : 1) * (p->q_heads / p->kv_heads);
     const int64_t rows = p->kv_len * p->batch * p->kv_heads;
-    return splits_for(ceil_div(p->kv_len, keys) * p->batch * p->kv_heads, steps_of(p, p->q_len), step, f32 || wide ? 1 : 2, 16,
+    return splits_for(p, ceil_div(p->kv_len, keys) * p->batch * p->kv_heads, ceil_div(p->causal ? std::min(p->q_len, p->kv_len) : p->q_len, STEP), step, f32 || wide ? 1 : 2, 16,
                       (double)(2 * rows * p->head_dim * 4));
 }
 
