@@ -1150,8 +1150,9 @@ bool near(const dear_attention_t *p, const dear_heads_t &t) { return p->dtype ==
 
 // Splits of the sequence that workgroups go through, where there are too few of them for the chip: the number with the least
 // time by this estimate, in microseconds.  The chip takes 256 * `resident` workgroups at a time; one goes through its share of
-// the steps in `step` each (in a causal call the longest does, and all together half of them); joining the splits costs `join`, and 3 TB/s for `bytes` of output each.  Measured with and without:
-// one query, 8 heads, 8192 keys of 128 values 29 and 164 us; 4 sequences of 656 with 2 key heads for 8, backward 45 and 88.
+// the steps in `step` each (in a causal call the longest does, and all together half of them); joining the splits costs `join`,
+// and 3 TB/s for `bytes` of output each.  Measured with and without: one query, 8 heads, 8192 keys of 128 values 29 and 164 us;
+// 4 sequences of 656 with 2 key heads for 8, backward 45 and 88.
 int splits_for(const dear_attention_t *p, int64_t groups, int64_t steps, double step, double resident, double join, double bytes) {
     int best = 1;
     double least = 0;
@@ -1169,14 +1170,15 @@ int q_splits(const dear_attention_t *p, bool backward) {
     const bool wide = p->head_dim > 64, f32 = p->dtype == DEAR_F32;
     const double step = f32 ? (backward ? 7.5 : 4.2) * (wide ? 2 : 1) : (backward ? 0.8 : 0.6) * (wide ? 1.5 : 1);
     const int64_t rows = p->q_len * p->batch * p->q_heads;
-    return splits_for(p, ceil_div(p->q_len, BLOCK) * p->batch * p->q_heads, ceil_div(p->kv_len, STEP), step, f32 ? 1 : wide || backward ? 2 : 4, 8,
-                      (double)(rows * p->head_dim * 4));
+    return splits_for(p, ceil_div(p->q_len, BLOCK) * p->batch * p->q_heads, ceil_div(p->kv_len, STEP), step,
+                      f32 ? 1 : wide || backward ? 2 : 4, 8, (double)(rows * p->head_dim * 4));
 }
 int kv_splits(const dear_attention_t *p, int keys) {
     const bool wide = p->head_dim > 64, f32 = p->dtype == DEAR_F32;
     const double step = (f32 ? 7.5 * (wide ? 2 : 1) : wide ? 1.2 : 1) * (p->q_heads / p->kv_heads);
     const int64_t rows = p->kv_len * p->batch * p->kv_heads;
-    return splits_for(p, ceil_div(p->kv_len, keys) * p->batch * p->kv_heads, ceil_div(p->causal ? std::min(p->q_len, p->kv_len) : p->q_len, STEP), step, f32 || wide ? 1 : 2, 16,
+    const int64_t seen = p->causal ? std::min(p->q_len, p->kv_len) : p->q_len;  // queries that a key is visible to, at most
+    return splits_for(p, ceil_div(p->kv_len, keys) * p->batch * p->kv_heads, ceil_div(seen, STEP), step, f32 || wide ? 1 : 2, 16,
                       (double)(2 * rows * p->head_dim * 4));
 }
 
