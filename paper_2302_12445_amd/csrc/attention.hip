@@ -359,11 +359,11 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_direct_
                 for (int r = 0; r < 16; ++r) most = fmaxf(most, s[kb][r]);
             most = halves_max(most);
             if (__builtin_amdgcn_ballot_w64(most > limit)) {
-                const float old = base;
+                const float old = top == -INFINITY ? -INFINITY : base;  // nothing yet: what is kept is 0, far below 0 too
                 top = fmaxf(top, most);
                 base = top == -INFINITY ? 0.f : top * c;
                 limit = top + GROWTH / c;
-                const float keep = __builtin_amdgcn_exp2f(old - base);  // of nothing yet, whatever it is
+                const float keep = __builtin_amdgcn_exp2f(old - base);
                 sum *= keep;
 #pragma unroll
                 for (int db = 0; db < W / 32; ++db) o[db] *= keep;

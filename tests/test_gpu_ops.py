@@ -160,6 +160,19 @@ def test_attention_large_scores(ops, dtype):
     check_attention(ops, q, k, v, scale=1e-3, label="scale")
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("shape", [(2, 130, 2, 64), (1, 200, 2, 128), (1, 900, 1, 96)])
+def test_attention_scores_far_below_zero(ops, shape, causal, dtype):
+    """Scores of minus hundreds alone: powers taken against 0 would all be 0, and those of the first maximum overflow."""
+    gen = torch.Generator().manual_seed(5)
+    q, k = normal(gen, shape, dtype, 3.0).abs() + 5, -normal(gen, shape, dtype, 3.0).abs() - 5
+    v = normal(gen, shape, dtype)
+    check_attention(ops, q, k, v, causal, label="low")
+    k[:, 100:] /= 4  # the maximum rises late
+    check_attention(ops, q, k, v, causal, label="rising")
+
+
 def test_attention_nan_and_infinity_reach_the_result(ops):
     gen = torch.Generator().manual_seed(2)
     q, k, v = (normal(gen, (2, 40, 2, 64), BF16) for _ in range(3))
