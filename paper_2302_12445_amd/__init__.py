@@ -3,6 +3,9 @@
 The product is libdear.so (C ABI in include/dear.h, HIP kernels for gfx950); this package
 is its thin ctypes binding.  Importing the package does not load the library; the first
 call does, and raises if the library has not been built.
+
+ops.py and layers.py are the training operators of libdear_ops.so (include/dear_ops.h): attention, RMS
+norm and 8-bit checkpoints for the transformer blocks whose gradients are aggregated.
 """
 from .binding import (  # noqa: F401
     DEAR_BF16, DEAR_F32, DEAR_NO_LIMIT, DEAR_SHARD_ALIGN, Context, DearError, Plan,
