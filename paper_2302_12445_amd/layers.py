@@ -5,6 +5,8 @@ operator allows it.
     h, y, kept = AddRMSNorm(width)(x, residual)   # kept: y in 8 bits, from the norm's own kernel
     z = CheckpointLinear(width, outs)(y, kept)    # weight gradient from the checkpoint; makes one itself where none is given
     out = attend(q, k, v, causal=True)            # keeps q, k, v, out and the log-sum-exp; recomputes the probabilities
+
+The operators' gradients cannot be differentiated again: second derivatives that need it raise RuntimeError.
 """
 from __future__ import annotations
 
@@ -14,6 +16,25 @@ from typing import Optional, Tuple
 import torch
 
 from . import ops
+
+
+class _FirstOrder(torch.autograd.Function):
+    """Gradients as they are, as results of the tensors that they depend on: differentiating them raises."""
+
+    @staticmethod
+    def forward(ctx, gradients, *tensors):
+        return gradients
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("attention, RMS norm and the weight gradient from a checkpoint have no second derivatives")
+
+
+def _first_order(gradients, *tensors):
+    """What the operators give has no graph, so that under create_graph second derivatives would lack it without a word:
+    there it is tied to the tensors that it comes from (some may be None)."""
+    tensors = [t for t in tensors if t is not None and t.requires_grad]
+    return _FirstOrder.apply(gradients, *tensors) if torch.is_grad_enabled() and tensors else gradients
 
 
 class _Attention(torch.autograd.Function):
@@ -28,7 +49,7 @@ class _Attention(torch.autograd.Function):
     def backward(ctx, dout):
         q, k, v, out, lse, q_lens, kv_lens = ctx.saved_tensors
         grads = ops.attention_backward(dout, q, k, v, out, lse, causal=ctx.causal, scale=ctx.scale, q_lens=q_lens, kv_lens=kv_lens)
-        return (*grads, None, None, None, None)
+        return (*_first_order(grads, dout, q, k, v), None, None, None, None)
 
 
 def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
@@ -53,7 +74,7 @@ class _AddRMSNorm(torch.autograd.Function):
         if dy is None:  # nobody used y
             dx, dweight = dh, None
         else:
-            dx, dweight = ops.add_rms_norm_backward(dy, h, weight, rstd, dh=dh)
+            dx, dweight = _first_order(ops.add_rms_norm_backward(dy, h, weight, rstd, dh=dh), dy, dh, h, weight)
         return dx, dx if ctx.needs_input_grad[1] else None, dweight, None
 
 
@@ -78,16 +99,20 @@ class _CheckpointLinear(torch.autograd.Function):
         out = rows @ w.t() if bias is None else torch.addmm(bias.to(x.dtype), rows, w.t())
         if kept is None:
             kept = ops.checkpoint_encode(rows)
-        ctx.save_for_backward(kept.codes, kept.exponents, weight)
+        source = x.new_empty(0)  # of the same inputs as out: what the weight's gradient is tied to, in the place of x
+        ctx.save_for_backward(kept.codes, kept.exponents, weight, source)
+        ctx.set_materialize_grads(False)
         ctx.cols, ctx.has_bias, ctx.shape = kept.cols, bias is not None, x.shape
-        return out.view(*x.shape[:-1], weight.shape[0])
+        return out.view(*x.shape[:-1], weight.shape[0]), source
 
     @staticmethod
-    def backward(ctx, dout):
-        codes, exponents, weight = ctx.saved_tensors
+    def backward(ctx, dout, _source):
+        codes, exponents, weight, source = ctx.saved_tensors
         rows = dout.reshape(-1, dout.shape[-1])
         dx = (rows @ weight.to(rows.dtype)).view(ctx.shape) if ctx.needs_input_grad[0] else None
-        dw = ops.checkpoint_weight_grad(rows, ops.Checkpoint(codes, exponents, ctx.cols)) if ctx.needs_input_grad[1] else None
+        dw = None
+        if ctx.needs_input_grad[1]:
+            dw, = _first_order((ops.checkpoint_weight_grad(rows, ops.Checkpoint(codes, exponents, ctx.cols)),), rows, source)
         db = rows.sum(0, dtype=torch.float32) if ctx.has_bias and ctx.needs_input_grad[2] else None
         return dx, dw, db, None
 
@@ -104,7 +129,7 @@ class CheckpointLinear(torch.nn.Module):
 
     def forward(self, x: torch.Tensor, kept: Optional[ops.Checkpoint] = None) -> torch.Tensor:
         """kept: the checkpoint of x, where it is there already."""
-        return _CheckpointLinear.apply(x, self.weight, self.bias, kept)
+        return _CheckpointLinear.apply(x, self.weight, self.bias, kept)[0]
 
 
 class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
