@@ -144,7 +144,7 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     def __init__(self, least: int = 1 << 16):
         def pack(t):
             if not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or t.numel() < least or isinstance(t, torch.nn.Parameter):
-                return t
+                return t.detach()  # not t: an operation that keeps its own output would be held by what it keeps, for ever
             return ops.checkpoint_encode(t.detach()), t.shape, t.dtype
 
         def unpack(kept):

@@ -2,7 +2,9 @@
 carry no graph of their own."""
 from __future__ import annotations
 
+import gc
 import math
+import weakref
 
 import pytest
 import torch
@@ -123,3 +125,32 @@ def test_first_derivatives_with_a_graph_are_the_same(plain):
         return (linear(y, kept) + h).square().sum()
     for a, b in zip(torch.autograd.grad(loss(), params), torch.autograd.grad(loss(), params, create_graph=True)):
         assert torch.equal(a, b) and b.requires_grad and not a.requires_grad
+
+
+# ------------------------------------------------------------------------------------ what saved_in_8_bits leaves as it is
+@pytest.mark.parametrize("function", [torch.sigmoid, torch.tanh, torch.exp, lambda x: torch.softmax(x, -1)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float64])
+def test_graphs_of_what_is_left_alone_are_freed(function, dtype):
+    """Operations that keep their own output: were that held by the graph itself, a graph that is dropped without a backward
+    pass would never be freed."""
+    x = torch.randn(8, 8, dtype=dtype, requires_grad=True)
+    with layers.saved_in_8_bits():
+        source = x * 1.0
+        out = function(source)
+    alive = [weakref.ref(source.grad_fn), weakref.ref(out.grad_fn)]
+    del source, out
+    gc.collect()
+    assert [r() for r in alive] == [None, None]
+
+
+def test_what_is_left_alone_is_the_same_tensor_s_values():
+    x = torch.randn(8, 8, dtype=torch.float64, requires_grad=True)
+
+    def gradients():
+        first, = torch.autograd.grad((torch.sigmoid(x) * torch.tanh(x * 2)).sum(), x, create_graph=True)
+        return first, torch.autograd.grad(first.square().sum(), x)[0]
+    want = gradients()
+    with layers.saved_in_8_bits():
+        got = gradients()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
