@@ -144,12 +144,16 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     def __init__(self, least: int = 1 << 16):
         def pack(t):
             if not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or t.numel() < least or isinstance(t, torch.nn.Parameter):
-                return t.detach()  # not t: an operation that keeps its own output would be held by what it keeps, for ever
+                # not t: an operation that keeps its own output would be held by what it keeps, for ever
+                return t.detach(), t._version
             return ops.checkpoint_encode(t.detach()), t.shape, t.dtype
 
         def unpack(kept):
-            if isinstance(kept, torch.Tensor):
-                return kept
+            if len(kept) == 2:
+                t, version = kept
+                if t._version != version:  # torch looks no more, once there are hooks
+                    raise RuntimeError("a tensor of shape %s that the backward pass needs was changed in place" % (tuple(t.shape),))
+                return t
             checkpoint, shape, dtype = kept
             return ops.checkpoint_decode(checkpoint, dtype).view(shape)
         super().__init__(pack, unpack)

@@ -154,3 +154,13 @@ def test_what_is_left_alone_is_the_same_tensor_s_values():
         got = gradients()
     for a, b in zip(got, want):
         assert torch.equal(a, b)
+
+
+def test_what_is_left_alone_and_changed_in_place_is_noticed():
+    x = torch.randn(8, 8, requires_grad=True)
+    with layers.saved_in_8_bits():
+        source = x * 1.0
+        out = source.square()
+    source.add_(1)
+    with pytest.raises(RuntimeError, match="in place"):
+        out.sum().backward()
