@@ -137,8 +137,8 @@ def test_graphs_of_what_is_left_alone_are_freed(function, dtype):
     with layers.saved_in_8_bits():
         source = x * 1.0
         out = function(source)
-    alive = [weakref.ref(source.grad_fn), weakref.ref(out.grad_fn)]
-    del source, out
+    alive = [weakref.ref(x), weakref.ref(out)]  # x is held by the graph that leads to it
+    del x, source, out
     gc.collect()
     assert [r() for r in alive] == [None, None]
 
