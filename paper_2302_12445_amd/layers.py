@@ -132,10 +132,26 @@ class CheckpointLinear(torch.nn.Module):
         return _CheckpointLinear.apply(x, self.weight, self.bias, kept)[0]
 
 
+# Nodes of operations whose result holds its inputs' values: views, copies, casts, parts and what joins them.
+_SAME_VALUES = {name + "Backward" for name in (
+    "T", "Transpose", "Permute", "View", "UnsafeView", "ReshapeAlias", "Unsqueeze", "Squeeze", "Expand", "Repeat", "AsStrided", "Slice", "Select",
+    "Index", "IndexSelect", "Split", "SplitWithSizes", "Unbind", "Unfold", "Diagonal", "Alias", "Clone", "ToCopy", "Cat", "Stack")}
+
+
+def _of_parameters(node) -> bool:
+    """Whether a node of the graph gives values of parameters alone."""
+    if hasattr(node, "variable"):
+        return isinstance(node.variable, torch.nn.Parameter)
+    sources = [n for n, _ in node.next_functions if n is not None]
+    return node.name().rstrip("0123456789") in _SAME_VALUES and bool(sources) and all(map(_of_parameters, sources))
+
+
 class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
-    """Within it, what torch's own operations keep for their backward passes is kept as checkpoints: floating tensors on
-    the GPU of at least `least` elements that are no parameters (as a GELU's input; not for what has to come back exactly,
-    such as a mask in floating point).
+    """Within it, what torch's own operations keep for their backward passes is kept as checkpoints: activations (as a GELU's
+    input), which are floating tensors on the GPU of at least `least` elements that were computed on the way of a gradient.
+    What is left as it is: parameters and other leaves, what holds values of parameters alone (views, casts, parts, joined ones),
+    and whatever takes no part in the gradient, as statistics.  Not for what has to come back exactly, such as a mask in floating
+    point, nor for infinities: a group of 32 neighbours that holds one comes back as NaN.
 
         with saved_in_8_bits():
             z = torch.nn.functional.gelu(u)
@@ -143,7 +159,8 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
     def __init__(self, least: int = 1 << 16):
         def pack(t):
-            if not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or t.numel() < least or isinstance(t, torch.nn.Parameter):
+            if (not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or t.numel() < least
+                    or t.grad_fn is None or _of_parameters(t.grad_fn)):
                 # not t: an operation that keeps its own output would be held by what it keeps, for ever
                 return t.detach(), t._version
             return ops.checkpoint_encode(t.detach()), t.shape, t.dtype
