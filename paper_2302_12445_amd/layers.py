@@ -11,11 +11,25 @@ The operators' gradients cannot be differentiated again: second derivatives that
 from __future__ import annotations
 
 import math
+import threading
 from typing import Optional, Tuple
 
 import torch
 
 from . import ops
+
+
+_applied = threading.local()
+
+
+def _apply(function, *args):
+    """The function's apply.  What it keeps is what its backward pass computes with (a log-sum-exp, a norm's factors), and not
+    for saved_in_8_bits."""
+    outer, _applied.here = getattr(_applied, "here", False), True
+    try:
+        return function.apply(*args)
+    finally:
+        _applied.here = outer
 
 
 class _FirstOrder(torch.autograd.Function):
@@ -55,7 +69,7 @@ class _Attention(torch.autograd.Function):
 def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = False, scale: Optional[float] = None,
            q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
     """ops.attention's out, with gradients of q, k and v."""
-    return _Attention.apply(q, k, v, causal, scale, q_lens, kv_lens)
+    return _apply(_Attention, q, k, v, causal, scale, q_lens, kv_lens)
 
 
 class _AddRMSNorm(torch.autograd.Function):
@@ -87,7 +101,7 @@ class AddRMSNorm(torch.nn.Module):
         self.eps = eps
 
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, ops.Checkpoint]:
-        h, y, codes, exponents = _AddRMSNorm.apply(x, residual, self.weight, self.eps)
+        h, y, codes, exponents = _apply(_AddRMSNorm, x, residual, self.weight, self.eps)
         return h, y, ops.Checkpoint(codes, exponents, self.weight.numel())
 
 
@@ -129,7 +143,7 @@ class CheckpointLinear(torch.nn.Module):
 
     def forward(self, x: torch.Tensor, kept: Optional[ops.Checkpoint] = None) -> torch.Tensor:
         """kept: the checkpoint of x, where it is there already."""
-        return _CheckpointLinear.apply(x, self.weight, self.bias, kept)[0]
+        return _apply(_CheckpointLinear, x, self.weight, self.bias, kept)[0]
 
 
 # Nodes of operations whose result holds its inputs' values: views, copies, casts, parts and what joins them.
@@ -150,7 +164,7 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     """Within it, what torch's own operations keep for their backward passes is kept as checkpoints: activations (as a GELU's
     input), which are floating tensors on the GPU of at least `least` elements that were computed on the way of a gradient.
     What is left as it is: parameters and other leaves, what holds values of parameters alone (views, casts, parts, joined ones),
-    and whatever takes no part in the gradient, as statistics.  Not for what has to come back exactly, such as a mask in floating
+    and whatever takes no part in the gradient, as statistics; also what the layers of this file keep.  Not for what has to come back exactly, such as a mask in floating
     point, nor for infinities: a group of 32 neighbours that holds one comes back as NaN.
 
         with saved_in_8_bits():
@@ -160,7 +174,7 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     def __init__(self, least: int = 1 << 16):
         def pack(t):
             if (not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or t.numel() < least
-                    or t.grad_fn is None or _of_parameters(t.grad_fn)):
+                    or t.grad_fn is None or _of_parameters(t.grad_fn) or getattr(_applied, "here", False)):
                 # not t: an operation that keeps its own output would be held by what it keeps, for ever
                 return t.detach(), t._version
             return ops.checkpoint_encode(t.detach()), t.shape, t.dtype

@@ -54,6 +54,49 @@ def test_weights_are_left_as_they_are(layers, form, trained):
         assert not torch.equal(got, want) and (got - want).norm() < 0.02 * want.norm()
 
 
+# ------------------------------------------------------------------------------------ the framework's own functions
+@pytest.mark.parametrize("ragged", [False, True])
+def test_attend_keeps_what_it_keeps(layers, ragged):
+    """Its log-sum-exp in 8 bits would be up to 3 % off in every probability, and NaN beside a padded row's infinity."""
+    q, k, v = (normal(16, 512, 16, 64, seed=n, dtype=BF16).requires_grad_() for n in range(3))
+    lens = torch.arange(512, 256, -16, dtype=torch.int32, device=DEV) if ragged else None
+    scale = normal(16, 512, 16, 64, seed=4, dtype=BF16)
+    def loss():
+        return (layers.attend(q * 1.0, k * 1.0, v * 1.0, q_lens=lens, kv_lens=lens) * scale).sum()
+    want = gradients(layers.saved_in_8_bits(least=1 << 40), loss, q, k, v)
+    got = gradients(layers.saved_in_8_bits(), loss, q, k, v)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b) and torch.isfinite(a).all()
+
+
+def test_norm_keeps_what_it_keeps(layers):
+    norm = layers.AddRMSNorm(64).to(DEV)
+    x, residual = (normal(1 << 16, 64, seed=n).requires_grad_() for n in range(2))
+    scale = normal(1 << 16, 64, seed=2)
+    def loss():
+        h, y, _ = norm(x * 1.0, residual * 1.0)
+        return (y * scale + h).sum()
+    want = gradients(layers.saved_in_8_bits(least=1 << 40), loss, x, residual, norm.weight)
+    for a, b in zip(gradients(layers.saved_in_8_bits(), loss, x, residual, norm.weight), want):
+        assert torch.equal(a, b)
+
+
+def test_a_whole_block_in_8_bits(layers):
+    """What is not the block's own functions is the GELU, which it keeps in 8 bits itself."""
+    torch.manual_seed(3)
+    block = layers.TransformerBlock(256, 4, 2).to(DEV)
+    x, residual = (normal(8, 100, 256, seed=n, dtype=BF16).requires_grad_() for n in range(2))
+    lens = torch.tensor([100, 71, 1, 50, 99, 100, 3, 64], dtype=torch.int32, device=DEV)
+    scale = normal(8, 100, 256, seed=2, dtype=BF16)
+    def loss():
+        out, h = block(x, residual, lens)
+        return (out * scale + h).sum()
+    wanted = (x, residual, *block.parameters())
+    want = gradients(torch.enable_grad(), loss, *wanted)
+    for a, b in zip(gradients(layers.saved_in_8_bits(), loss, *wanted), want):
+        assert torch.equal(a, b) and torch.isfinite(a).all()
+
+
 # ------------------------------------------------------------------------------------ what takes no part in the gradient
 def test_statistics_are_left_as_they_are(layers):
     """A layer norm of torch's keeps its rows' means and factors, no activations: with as many rows as are worth keeping in 8
