@@ -173,11 +173,15 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
     def __init__(self, least: int = 1 << 16):
         def pack(t):
-            if (not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or t.numel() < least
+            if (not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or t.numel() < max(least, 1)
                     or t.grad_fn is None or _of_parameters(t.grad_fn) or getattr(_applied, "here", False)):
                 # not t: an operation that keeps its own output would be held by what it keeps, for ever
                 return t.detach(), t._version
-            return ops.checkpoint_encode(t.detach()), t.shape, t.dtype
+            rows, n = t.detach(), t.numel()
+            if not t.dim() or t.shape[-1] % ops.GROUP:
+                # rows that fill no whole groups would each be filled up with zeros: the values as they follow one another instead
+                rows = rows.reshape(-1, ops.GROUP) if n % ops.GROUP == 0 else rows.reshape(1, -1) if n <= ops.MAX_COLS else rows
+            return ops.checkpoint_encode(rows), t.shape, t.dtype
 
         def unpack(kept):
             if len(kept) == 2:
