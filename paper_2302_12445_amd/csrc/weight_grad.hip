@@ -169,12 +169,13 @@ struct wave_loader {
     uint32_t y_stride, x_stride, e_stride;  // bytes
     uint32_t y_off, x_off, e_off;           // of the lane's piece
 
-    // left: rows from the step's first on; those beyond repeat the last one, times 0
+    // left: rows from the step's first on; those beyond are zeros (of the codes: the last row again, times 0)
     template <bool WHOLE> __device__ __forceinline__ void load_y(DEAR_LDS bf16 *s, int lane, int left) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int row = 4 * i + lane / 16;
-            load_to_lds(y + (y_off + (uint32_t)(WHOLE ? row : min(row, left - 1)) * y_stride), s + i * 512);
+            if (WHOLE || row < left) load_to_lds(y + (y_off + (uint32_t)row * y_stride), s + i * 512);
+            else *(DEAR_LDS u32x4 *)(s + i * 512 + lane * 8) = u32x4{0, 0, 0, 0};
         }
         y += (int64_t)WSTEP * y_stride;
     }
