@@ -276,13 +276,13 @@ __global__ __launch_bounds__(THREADS, 1) void weight_grad_wide_kernel(params a) 
         load_x(w0, 0);
         store_x(w0, xa, lane);
         load_x(w1, 1);
-        // Step t, in buffer t % 2: waits for its dy and for the codes of step t + 1, which are the wave's own loads (vmcnt 0),
-        // reads its first fragments beside the products of the second ones of the step before, and its second ones beside
+        // Step t, in buffer t % 2: waits for its dy and for the codes of step t + 1, which are the wave's own loads, and for its
+        // own reads of the buffer that is filled next (vmcnt 0 and lgkmcnt 0), reads its first fragments beside the products of the second ones of the step before, and its second ones beside
         // the products of the first.  MORE: steps to t + 2 are there and whole.
         auto step = [&](auto more, int64_t t, const wave_codes &w, wave_codes &w_next, const DEAR_LDS bf16 *y, const DEAR_LDS bf16 *x,
                         DEAR_LDS bf16 *y_next, DEAR_LDS bf16 *x_next) {
             constexpr bool MORE = decltype(more)::value;
-            __builtin_amdgcn_s_waitcnt(0x0f70);
+            __builtin_amdgcn_s_waitcnt(0x0070);
 #pragma unroll
             for (int u = 0; u < 4; ++u) asm("" : "+v"(column_at[u]));
             if (MORE) in.load_y<true>(y_next, lane, 0), in.load_x<true>(w_next, lane, 0);
