@@ -277,8 +277,9 @@ __global__ __launch_bounds__(THREADS, 1) void weight_grad_wide_kernel(params a) 
         store_x(w0, xa, lane);
         load_x(w1, 1);
         // Step t, in buffer t % 2: waits for its dy and for the codes of step t + 1, which are the wave's own loads, and for its
-        // own reads of the buffer that is filled next (vmcnt 0 and lgkmcnt 0), reads its first fragments beside the products of the second ones of the step before, and its second ones beside
-        // the products of the first.  MORE: steps to t + 2 are there and whole.
+        // own reads of the buffer that is filled next (vmcnt 0 and lgkmcnt 0), reads its first fragments beside the products of the
+        // second ones of the step before, and its second ones beside the products of the first.  MORE: steps to t + 2 are there
+        // and whole.
         auto step = [&](auto more, int64_t t, const wave_codes &w, wave_codes &w_next, const DEAR_LDS bf16 *y, const DEAR_LDS bf16 *x,
                         DEAR_LDS bf16 *y_next, DEAR_LDS bf16 *x_next) {
             constexpr bool MORE = decltype(more)::value;
