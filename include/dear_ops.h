@@ -141,7 +141,7 @@ int dear_checkpoint_weight_grad_workspace(int32_t dtype, int64_t rows, int64_t o
  *   rstd         fp32, [rows], written
  * h may be x or residual itself (same address and strides).  rows >= 0, 1 <= cols <= DEAR_NORM_MAX_COLS.
  * Tensors are aligned to their element types, codes to 16 bytes.
- * Errors: DEAR_EINVAL, DEAR_EALIGN, DEAR_EHIP.
+ * Errors: DEAR_EINVAL, DEAR_EALIGN, DEAR_EHIP; DEAR_ETOOBIG for 2^31 rows or more (forward).
  */
 #define DEAR_NORM_MAX_COLS 32768
 int dear_add_rms_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride,

@@ -362,9 +362,16 @@ struct forward_call {
     float *rstd;
     hipStream_t stream;
     template <typename T, int TPR, int V, bool VEC> void operator()() {
-        const unsigned grid = (unsigned)ceil_div(rows, block_of(TPR) / TPR);
-        norm_kernel<T, TPR, V, VEC><<<grid, block_of(TPR), 0, stream>>>((const T *)x, x_stride, (const T *)residual, residual_stride,
-                                                                        weight, rows, cols, eps, (T *)h, (T *)y, codes, exponents, rstd);
+        constexpr int RPB = block_of(TPR) / TPR;
+        const int64_t groups = ceil_div(cols, GROUP), most = MAX_THREADS / block_of(TPR) * RPB;  // rows of a launch
+        for (int64_t first = 0; first < rows; first += most) {
+            const int64_t n = rows - first < most ? rows - first : most;
+            auto from = [&](const void *p, int64_t stride) { return p ? (T *)p + first * stride : nullptr; };
+            norm_kernel<T, TPR, V, VEC><<<(unsigned)ceil_div(n, RPB), block_of(TPR), 0, stream>>>(
+                from(x, x_stride), x_stride, from(residual, residual_stride), residual_stride, weight, n, cols, eps, from(h, cols),
+                from(y, cols), codes ? codes + first * groups * GROUP : nullptr, exponents ? exponents + first * groups : nullptr,
+                rstd + first);
+        }
     }
 };
 

@@ -187,6 +187,9 @@ __device__ __forceinline__ void loads_barrier() {
     __syncthreads();
 }
 
+// HIP takes fewer than 2^32 threads along a dimension of a launch.
+constexpr int64_t MAX_THREADS = 0xffffffff;
+
 inline bool aligned(const void *p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int launch_status() { return hipGetLastError() == hipSuccess ? DEAR_OK : DEAR_EHIP; }
