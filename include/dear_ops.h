@@ -100,7 +100,7 @@ int dear_attention_backward_workspace(const dear_attention_t *args, int64_t *byt
  *
  *   codes      int8, [rows, round_up(cols, DEAR_CHECKPOINT_GROUP)] contiguous, 16-byte aligned
  *   exponents  uint8, [rows, ceil(cols / DEAR_CHECKPOINT_GROUP)] contiguous
- *   rows >= 0, 1 <= cols < 2^31
+ *   rows >= 0, 1 <= cols <= 2^31 - 33; DEAR_ETOOBIG from 2^42 codes on
  */
 #define DEAR_CHECKPOINT_GROUP 32
 

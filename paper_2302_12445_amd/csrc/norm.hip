@@ -86,10 +86,10 @@ __device__ __forceinline__ void decode8(float *x, u32x2 codes, uint32_t exponent
 }
 
 // Piece n of the rows: per_row pieces each, or, where per_row is 0, rows of whole groups that follow one another without gaps.
-template <typename INDEX> struct piece {
-    INDEX row;
+struct piece {
+    uint32_t row;
     int col, cols;
-    __device__ __forceinline__ piece(INDEX n, INDEX per_row, int32_t all) {
+    __device__ __forceinline__ piece(uint32_t n, uint32_t per_row, int32_t all) {
         if (per_row == 0) {
             row = n, col = 0, cols = LANE;
         } else {
@@ -100,12 +100,12 @@ template <typename INDEX> struct piece {
 
 // A vector of eight a thread, its group's magnitude by two exchanges within the quad.  8192 x 4096 in bf16: 16 us = 6.3 TB/s, the
 // rate of a copy.
-template <typename T, bool VEC, typename INDEX>
-__global__ __launch_bounds__(256) void encode_kernel(const T *x, int64_t row_stride, INDEX total, int32_t cols, INDEX per_row,
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void encode_kernel(const T *x, int64_t row_stride, uint32_t total, int32_t cols, uint32_t per_row,
                                                      int8_t *codes, uint8_t *exponents) {
-    const INDEX n = (INDEX)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t n = blockIdx.x * 256 + threadIdx.x;
     if (n >= total) return;  // whole quads: per_row is a multiple of four
-    const piece<INDEX> p(n, per_row, cols);
+    const piece p(n, per_row, cols);
     float v[LANE];
     load8<T, VEC>(v, x + (int64_t)p.row * row_stride, p.col, p.cols);
     uint32_t e;
@@ -115,12 +115,12 @@ __global__ __launch_bounds__(256) void encode_kernel(const T *x, int64_t row_str
 }
 
 // 8192 x 4096 to bf16: 15 us = 6.8 TB/s, the rate of a copy.
-template <typename T, bool VEC, typename INDEX>
-__global__ __launch_bounds__(256) void decode_kernel(const int8_t *codes, const uint8_t *exponents, INDEX total, int32_t cols,
-                                                     INDEX per_row, T *out, int64_t row_stride) {
-    const INDEX n = (INDEX)blockIdx.x * 256 + threadIdx.x;
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void decode_kernel(const int8_t *codes, const uint8_t *exponents, uint32_t total, int32_t cols,
+                                                     uint32_t per_row, T *out, int64_t row_stride) {
+    const uint32_t n = blockIdx.x * 256 + threadIdx.x;
     if (n >= total) return;
-    const piece<INDEX> p(n, per_row, cols);
+    const piece p(n, per_row, cols);
     float v[LANE];
     decode8(v, *(const u32x2 *)(codes + (int64_t)n * LANE), exponents[n / 4]);
     store8<T, VEC>(out + (int64_t)p.row * row_stride, v, p.col, p.cols);
@@ -391,30 +391,23 @@ struct backward_call {
     }
 };
 
-// Pieces of the rows of a checkpoint, and of one row, or 0 where rows without gaps (`dense`) are of whole groups.
-struct pieces {
-    int64_t total, per_row;
-    unsigned grid;
-};
-
-int count(int64_t rows, int64_t cols, bool dense, pieces &n) {
-    n.per_row = ceil_div(cols, GROUP) * (GROUP / LANE);
-    if (rows > INT64_MAX / 4 / n.per_row || ceil_div(rows * n.per_row, 256) > INT32_MAX) return DEAR_ETOOBIG;
-    n.total = rows * n.per_row;
-    n.grid = (unsigned)ceil_div(n.total, 256);
-    if (dense && cols % GROUP == 0) n.per_row = 0;
-    return DEAR_OK;
+// The launches of a call on a checkpoint: as many rows at a time as 31 bits count the pieces of.  Calls
+// f(first row, pieces, pieces of a row) for each; pieces of a row: 0 where rows without gaps (`dense`) are of whole groups.
+template <typename F> int launches(int64_t rows, int64_t cols, bool dense, F f) {
+    const int64_t per_row = ceil_div(cols, GROUP) * (GROUP / LANE), most = INT32_MAX / per_row;
+    if (rows > INT64_MAX / 4 / per_row || ceil_div(rows * per_row, 256) > INT32_MAX) return DEAR_ETOOBIG;
+    for (int64_t first = 0; first < rows; first += most) {
+        const int64_t n = rows - first < most ? rows - first : most;
+        f(first, (uint32_t)(n * per_row), dense && cols % GROUP == 0 ? 0u : (uint32_t)per_row);
+    }
+    return launch_status();
 }
 
-// Calls f with values of the type, of whether there are whole vectors, and of the pieces' index: 64 bits where 32 do not do.
-template <typename F> void by_types(int32_t dtype, bool vec, int64_t total, F f) {
-    auto by_index = [&](auto t, auto v) {
-        if (total <= INT32_MAX) f(t, v, uint32_t());
-        else f(t, v, uint64_t());
-    };
+// Calls f with values of the type and of whether there are whole vectors.
+template <typename F> void by_types(int32_t dtype, bool vec, F f) {
     auto by_vec = [&](auto t) {
-        if (vec) by_index(t, std::true_type());
-        else by_index(t, std::false_type());
+        if (vec) f(t, std::true_type());
+        else f(t, std::false_type());
     };
     if (dtype == DEAR_BF16) by_vec(bf16());
     else by_vec(float());
@@ -437,18 +430,17 @@ int dear_checkpoint_encode(const void *x, int32_t dtype, int64_t rows, int64_t c
     if (int rc = check_rows(x, row_stride, dtype, rows, cols)) return rc;
     if (!codes || !exponents) return DEAR_EINVAL;
     if (!aligned(codes, 16)) return DEAR_EALIGN;
-    pieces n;
-    if (int rc = count(rows, cols, vectors(x, row_stride, cols, size_of(dtype)) && (row_stride == cols || rows == 1), n)) return rc;
     hipStream_t s = (hipStream_t)hip_stream;
     const bool vec = vectors(x, row_stride, cols, size_of(dtype));
-    const int64_t stride = n.per_row ? row_stride : LANE;
-    by_types(dtype, vec, n.total, [&](auto t, auto v, auto index) {
-        typedef decltype(t) T;
-        typedef decltype(index) INDEX;
-        encode_kernel<T, decltype(v)::value, INDEX>
-            <<<n.grid, 256, 0, s>>>((const T *)x, stride, (INDEX)n.total, (int32_t)cols, (INDEX)n.per_row, codes, exponents);
+    const int64_t groups = ceil_div(cols, GROUP);
+    return launches(rows, cols, vec && (row_stride == cols || rows == 1), [&](int64_t first, uint32_t total, uint32_t per_row) {
+        by_types(dtype, vec, [&](auto t, auto v) {
+            typedef decltype(t) T;
+            encode_kernel<T, decltype(v)::value><<<(total + 255) / 256, 256, 0, s>>>(
+                (const T *)x + first * row_stride, per_row ? row_stride : LANE, total, (int32_t)cols, per_row,
+                codes + first * groups * GROUP, exponents + first * groups);
+        });
     });
-    return launch_status();
 }
 
 int dear_checkpoint_decode(const int8_t *codes, const uint8_t *exponents, int64_t rows, int64_t cols, int32_t dtype, void *out,
@@ -457,18 +449,17 @@ int dear_checkpoint_decode(const int8_t *codes, const uint8_t *exponents, int64_
     if (rows == 0) return DEAR_OK;
     if (!codes || !exponents || !out) return DEAR_EINVAL;
     if (!aligned(codes, 16) || !aligned(out, size_of(dtype))) return DEAR_EALIGN;
-    pieces n;
-    if (int rc = count(rows, cols, vectors(out, cols, cols, size_of(dtype)), n)) return rc;
     hipStream_t s = (hipStream_t)hip_stream;
     const bool vec = vectors(out, cols, cols, size_of(dtype));
-    const int64_t stride = n.per_row ? cols : LANE;
-    by_types(dtype, vec, n.total, [&](auto t, auto v, auto index) {
-        typedef decltype(t) T;
-        typedef decltype(index) INDEX;
-        decode_kernel<T, decltype(v)::value, INDEX>
-            <<<n.grid, 256, 0, s>>>(codes, exponents, (INDEX)n.total, (int32_t)cols, (INDEX)n.per_row, (T *)out, stride);
+    const int64_t groups = ceil_div(cols, GROUP);
+    return launches(rows, cols, vec, [&](int64_t first, uint32_t total, uint32_t per_row) {
+        by_types(dtype, vec, [&](auto t, auto v) {
+            typedef decltype(t) T;
+            decode_kernel<T, decltype(v)::value><<<(total + 255) / 256, 256, 0, s>>>(
+                codes + first * groups * GROUP, exponents + first * groups, total, (int32_t)cols, per_row, (T *)out + first * cols,
+                per_row ? cols : LANE);
+        });
     });
-    return launch_status();
 }
 
 int dear_add_rms_norm(const void *x, int64_t x_stride, const void *residual, int64_t residual_stride, const float *weight,

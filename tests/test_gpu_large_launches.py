@@ -17,6 +17,12 @@ def ops():
     return m
 
 
+@pytest.fixture(autouse=True)
+def memory_given_back():
+    yield
+    torch.cuda.empty_cache()
+
+
 def random(rows, cols, dtype, seed):
     return torch.randn(rows, cols, generator=torch.Generator(DEV).manual_seed(seed), device=DEV, dtype=dtype)
 
@@ -39,3 +45,24 @@ def test_norm_of_2_to_the_26_rows(ops, residual):
         got = h[a:b], y[a:b], ops.Checkpoint(kept.codes[a:b], kept.exponents[a:b], cols), rstd[a:b]
         for p, q in zip((*got[:2], *got[2][:2], got[3]), (*want[:2], *want[2][:2], want[3])):
             assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("cols", [1, 32])
+def test_checkpoint_of_2_to_the_32_pieces(ops, cols):
+    """Rows of one value, each filled up to a group, and rows of whole groups: 2^32 pieces of eight codes."""
+    rows, edge = (1 << 30) + 1003, 1 << 29
+    print("case", rows, cols, flush=True)
+    x = random(rows, cols, BF16, 1) if cols == 1 else torch.empty(rows, cols, dtype=BF16, device=DEV)
+    near = parts(rows, edge) + parts(rows, 2 * edge)[1:2]
+    if cols > 1:  # values where they are looked at
+        for n, (a, b) in enumerate(near):
+            x[a:b] = random(b - a, cols, BF16, n)
+    kept = ops.checkpoint_encode(x)
+    for a, b in near:
+        want = ops.checkpoint_encode(x[a:b])
+        assert torch.equal(kept.codes[a:b], want.codes) and torch.equal(kept.exponents[a:b], want.exponents)
+    del x
+    got = ops.checkpoint_decode(kept)
+    for a, b in near:
+        want = ops.checkpoint_decode(ops.Checkpoint(kept.codes[a:b], kept.exponents[a:b], cols))
+        assert torch.equal(got[a:b], want)
