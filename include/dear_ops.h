@@ -77,8 +77,9 @@ typedef struct {
 } dear_attention_t;
 
 /* Base pointers must be 16-byte aligned and strides multiples of 16 bytes (DEAR_EALIGN otherwise).
- * Errors: DEAR_EINVAL, DEAR_EALIGN, DEAR_EHIP; DEAR_ETOOBIG for 2^31 workgroups or more, or where
- * workspace_bytes is less than the call needs. */
+ * Errors: DEAR_EINVAL, DEAR_EALIGN, DEAR_EHIP; DEAR_ETOOBIG where workspace_bytes is less than the call
+ * needs, or where a launch would have 2^32 threads or more: 256 for every 128 queries of a head and, backward,
+ * 256 (bf16 of more than 64 values 512) for every 64 keys of a key head. */
 int dear_attention(const dear_attention_t *args, void *hip_stream);
 int dear_attention_backward(const dear_attention_t *args, void *hip_stream);
 

@@ -1148,15 +1148,21 @@ bool near(const dear_attention_t *p, const dear_heads_t &t) { return p->dtype ==
         else kernel<float, 128><<<grid, THREADS, 0, stream>>>(a);                                         \
     } while (0)
 
+// Workgroups of a launch without splits, and the most threads that one has.
+int64_t q_groups(const dear_attention_t *p) { return ceil_div(p->q_len, BLOCK) * p->batch * p->q_heads; }
+int64_t kv_groups(const dear_attention_t *p, int keys) { return ceil_div(p->kv_len, keys) * p->batch * p->kv_heads; }
+int kv_threads(const dear_attention_t *p) { return p->dtype == DEAR_BF16 && p->head_dim > 64 ? 64 * KV_WAVES : THREADS; }
+
 // Splits of the sequence that workgroups go through, where there are too few of them for the chip: the number with the least
 // time by this estimate, in microseconds.  The chip takes 256 * `resident` workgroups at a time; one goes through its share of
 // the steps in `step` each (in a causal call the longest does, and all together half of them); joining the splits costs `join`,
 // and 3 TB/s for `bytes` of output each.  Measured with and without: one query, 8 heads, 8192 keys of 128 values 29 and 164 us;
 // 4 sequences of 656 with 2 key heads for 8, backward 45 and 88.
-int splits_for(const dear_attention_t *p, int64_t groups, int64_t steps, double step, double resident, double join, double bytes) {
+int splits_for(const dear_attention_t *p, int64_t groups, int threads, int64_t steps, double step, double resident, double join, double bytes) {
     int best = 1;
     double least = 0;
-    for (int64_t s = 1; s <= 16 && (s == 1 || s <= steps); ++s) {
+    // (joining takes a thread for eight values of 4 bytes)
+    for (int64_t s = 1; s <= 16 && (s == 1 || (s <= steps && groups * s * threads <= MAX_THREADS && bytes <= 32. * MAX_THREADS)); ++s) {
         const double turns = (double)(groups * s) / (256 * resident), share = (double)ceil_div(steps, s) * step;
         const double t = (p->causal ? std::fmax(1, turns / 2) : std::ceil(turns)) * share + (s == 1 ? 0 : join + (double)s * bytes / 3e6);
         if (s == 1 || t < least) best = (int)s, least = t;
@@ -1170,7 +1176,7 @@ int q_splits(const dear_attention_t *p, bool backward) {
     const bool wide = p->head_dim > 64, f32 = p->dtype == DEAR_F32;
     const double step = f32 ? (backward ? 7.5 : 4.2) * (wide ? 2 : 1) : (backward ? 0.8 : 0.6) * (wide ? 1.5 : 1);
     const int64_t rows = p->q_len * p->batch * p->q_heads;
-    return splits_for(p, ceil_div(p->q_len, BLOCK) * p->batch * p->q_heads, ceil_div(p->kv_len, STEP), step,
+    return splits_for(p, q_groups(p), THREADS, ceil_div(p->kv_len, STEP), step,
                       f32 ? 1 : wide || backward ? 2 : 4, 8, (double)(rows * p->head_dim * 4));
 }
 int kv_splits(const dear_attention_t *p, int keys) {
@@ -1178,7 +1184,7 @@ int kv_splits(const dear_attention_t *p, int keys) {
     const double step = (f32 ? 7.5 * (wide ? 2 : 1) : wide ? 1.2 : 1) * (p->q_heads / p->kv_heads);
     const int64_t rows = p->kv_len * p->batch * p->kv_heads;
     const int64_t seen = p->causal ? std::min(p->q_len, p->kv_len) : p->q_len;  // queries that a key is visible to, at most
-    return splits_for(p, ceil_div(p->kv_len, keys) * p->batch * p->kv_heads, ceil_div(seen, STEP), step, f32 || wide ? 1 : 2, 16,
+    return splits_for(p, kv_groups(p, keys), kv_threads(p), ceil_div(seen, STEP), step, f32 || wide ? 1 : 2, 16,
                       (double)(2 * rows * p->head_dim * 4));
 }
 
@@ -1240,6 +1246,7 @@ int dear_attention(const dear_attention_t *p, void *hip_stream) {
     if (p->batch == 0 || p->q_len == 0) return DEAR_OK;
     if (!p->lse) return DEAR_EINVAL;
     if (!aligned(p->lse, 4)) return DEAR_EALIGN;
+    if (q_groups(p) * THREADS > MAX_THREADS) return DEAR_ETOOBIG;
     if (int rc = check_workspace(p, forward_bytes(p))) return rc;
     params a = make(p);
     a.tiles = (int32_t)ceil_div(p->q_len, BLOCK), a.splits = q_splits(p, false);
@@ -1275,13 +1282,14 @@ int dear_attention_backward(const dear_attention_t *p, void *hip_stream) {
         if (!p->lse) return DEAR_EINVAL;
         if (!aligned(p->lse, 4)) return DEAR_EALIGN;
     }
+    const bool direct = near(p, p->q) && near(p, p->dout) && near(p, p->k) && near(p, p->v);
+    const int keys = direct && p->head_dim <= 64 ? BLOCK : KEYS;
+    if (q_groups(p) * THREADS > MAX_THREADS || kv_groups(p, keys) * kv_threads(p) > MAX_THREADS) return DEAR_ETOOBIG;
     int64_t need = 0;
     (void)dear_attention_backward_workspace(p, &need);
     if (int rc = check_workspace(p, need)) return rc;
     params a = make(p);
-    const bool direct = near(p, p->q) && near(p, p->dout) && near(p, p->k) && near(p, p->v);
     hipStream_t stream = (hipStream_t)hip_stream;
-    const int keys = direct && p->head_dim <= 64 ? BLOCK : KEYS;
     const int64_t q_tiles = ceil_div(p->q_len, BLOCK), kv_tiles = ceil_div(p->kv_len, keys);
     a.q_tiles = (int32_t)q_tiles;
     a.powers = (float *)p->workspace, a.deltas = a.powers + q_tiles * BLOCK * p->batch * p->q_heads;

@@ -190,3 +190,14 @@ def test_tensors_off_the_gpu_are_refused():
 
 def test_errors_are_described():
     assert "align" in dear.strerror(EALIGN)
+
+
+def test_attention_of_more_threads_than_a_launch_takes():
+    """2^24 workgroups of 256 threads, or 2^23 of 512, are refused before anything is launched."""
+    lib, room = ops.load_library(), 1 << 60
+    many = dict(batch=1 << 20, q_heads=16, kv_heads=16, q_len=16, kv_len=24, workspace_bytes=room)
+    assert lib.dear_attention(attention_bytes(**many), None) == ETOOBIG
+    assert lib.dear_attention_backward(attention_bytes(**many), None) == ETOOBIG
+    keys = dict(batch=1 << 16, q_heads=16, kv_heads=16, q_len=16, kv_len=512, workspace_bytes=room)
+    assert lib.dear_attention_backward(attention_bytes(**dict(keys, head_dim=128)), None) == ETOOBIG
+    assert lib.dear_attention_backward(attention_bytes(**dict(keys, kv_len=1024, dtype=0)), None) == ETOOBIG
