@@ -122,7 +122,8 @@ int dear_checkpoint_decode(const int8_t *codes, const uint8_t *exponents, int64_
  *   workspace  256-byte aligned, as many bytes as dear_checkpoint_weight_grad_workspace says; NULL
  *              where that is 0
  * outs, ins: 1 .. 2^24; rows: 0 .. 2^40.
- * Errors of the calls on checkpoints: DEAR_EINVAL, DEAR_EALIGN, DEAR_EHIP; DEAR_ETOOBIG as above. */
+ * Errors of the calls on checkpoints: DEAR_EINVAL, DEAR_EALIGN, DEAR_EHIP; DEAR_ETOOBIG as above, the weight
+ * gradient's for 2^24 tiles of 128 x 128 outputs or more. */
 int dear_checkpoint_weight_grad(const void *dy, int32_t dtype, int64_t dy_stride, const int8_t *codes,
                                 const uint8_t *exponents, int64_t rows, int64_t outs, int64_t ins, float *dw,
                                 void *workspace, int64_t workspace_bytes, void *hip_stream);

@@ -400,7 +400,7 @@ choice choose(int32_t dtype, bool can_wide, int64_t rows, int64_t outs, int64_t 
     const int64_t tiles = ceil_div(outs, BN) * ceil_div(ins, BK), most = ceil_div(rows, 128) < 64 ? ceil_div(rows, 128) : 64;
     const double resident = dtype == DEAR_F32 ? 3 : 4, alone = dtype == DEAR_F32 ? 11 : 2.9, share = dtype == DEAR_F32 ? 8 : 1.5;
     choice best = {can_wide, 1, 0};
-    for (int64_t s = 1; s == 1 || s <= most; ++s) {
+    for (int64_t s = 1; s == 1 || (s <= most && tiles * s * THREADS <= MAX_THREADS && outs * ins <= MAX_THREADS); ++s) {
         const double chunk = (double)ceil_div(ceil_div(rows, s), 128), a_cu = (double)ceil_div(tiles * s, 256);
         const double sums = s == 1 ? 0 : 4 + (double)(s + 1) * (double)outs * (double)ins * 4 / 5e6;
         const double wait = std::ceil(a_cu / resident) * chunk * alone, work = a_cu * chunk * share;
@@ -455,7 +455,7 @@ int dear_checkpoint_weight_grad(const void *dy, int32_t dtype, int64_t dy_stride
     a.n_tiles = (int32_t)ceil_div(outs, BN), a.k_tiles = (int32_t)ceil_div(ins, BK);
     a.out = splits > 1 ? (float *)workspace : dw;
     const int64_t groups = (int64_t)a.n_tiles * a.k_tiles * splits;
-    if (groups > INT32_MAX || ceil_div(outs * ins, 256) > INT32_MAX) return DEAR_ETOOBIG;
+    if (groups * THREADS > MAX_THREADS) return DEAR_ETOOBIG;
     const unsigned grid = (unsigned)groups;
     if (c.wide) weight_grad_wide_kernel<<<grid, THREADS, 0, stream>>>(a);
     else if (dtype == DEAR_BF16 && vec) weight_grad_kernel<bf16, true><<<grid, THREADS, 0, stream>>>(a);

@@ -201,3 +201,10 @@ def test_attention_of_more_threads_than_a_launch_takes():
     keys = dict(batch=1 << 16, q_heads=16, kv_heads=16, q_len=16, kv_len=512, workspace_bytes=room)
     assert lib.dear_attention_backward(attention_bytes(**dict(keys, head_dim=128)), None) == ETOOBIG
     assert lib.dear_attention_backward(attention_bytes(**dict(keys, kv_len=1024, dtype=0)), None) == ETOOBIG
+
+
+def test_weight_grad_of_more_threads_than_a_launch_takes():
+    """2^24 tiles of 256 threads are refused before anything is launched."""
+    f, p, big = ops.load_library().dear_checkpoint_weight_grad, SPACE, 1 << 60
+    assert f(p, 1, 1 << 19, p, p, 4, 1 << 19, 1 << 19, p, p, big, None) == ETOOBIG
+    assert f(p, 0, 1 << 24, p, p, 4, 1 << 24, 1 << 14, p, p, big, None) == ETOOBIG
