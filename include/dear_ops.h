@@ -35,7 +35,8 @@ extern "C" {
 
 /* A [batch, token, head, head_dim] tensor: head_dim is contiguous, the other strides are in
  * elements.  A tensor that is read may have strides of 0 (broadcast); one that is written must
- * not map two elements to one place. */
+ * not map two elements to one place: in the order of their strides, each axis of several elements
+ * has a stride of at least what head_dim and the axes before it span. */
 typedef struct {
     void *data;
     int64_t batch_stride, token_stride, head_stride;

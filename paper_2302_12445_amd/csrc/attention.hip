@@ -1105,7 +1105,8 @@ int check_sizes(const dear_attention_t *p) {
     return DEAR_OK;
 }
 
-// Whether a tensor of n tokens is there, and aligned; what is written has a place of its own for every element.
+// Whether a tensor of n tokens is there, and aligned; what is written has a place of its own for every element: from the shortest
+// stride on each one is at least as long as what the axes before it span.
 int check_heads(const dear_heads_t &t, const dear_attention_t *p, int64_t n, bool written) {
     if (p->batch == 0 || n == 0) return DEAR_OK;
     if (!t.data) return DEAR_EINVAL;
@@ -1113,10 +1114,16 @@ int check_heads(const dear_heads_t &t, const dear_attention_t *p, int64_t n, boo
     if (!aligned(t.data, 16) || t.batch_stride * g % 16 || t.token_stride * g % 16 || t.head_stride * g % 16) return DEAR_EALIGN;
     if (t.batch_stride < 0 || t.token_stride < 0 || t.head_stride < 0) return DEAR_EINVAL;
     if (written) {
-        const int64_t heads = &t == &p->dk || &t == &p->dv ? p->kv_heads : p->q_heads;
-        if ((n > 1 && t.token_stride < p->head_dim) || (heads > 1 && t.head_stride < p->head_dim) ||
-            (p->batch > 1 && t.batch_stride < p->head_dim))
-            return DEAR_EINVAL;
+        struct axis {
+            int64_t stride, count;
+        } axes[3] = {{t.batch_stride, p->batch}, {t.token_stride, n}, {t.head_stride, &t == &p->dk || &t == &p->dv ? p->kv_heads : p->q_heads}};
+        std::sort(axes, axes + 3, [](const axis &a, const axis &b) { return a.stride < b.stride; });
+        int64_t span = p->head_dim;
+        for (const axis &a : axes) {
+            if (a.count == 1) continue;
+            if (a.stride < span || a.stride > (INT64_MAX - span) / a.count) return DEAR_EINVAL;
+            span += (a.count - 1) * a.stride;
+        }
     }
     return DEAR_OK;
 }

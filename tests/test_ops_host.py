@@ -208,3 +208,30 @@ def test_weight_grad_of_more_threads_than_a_launch_takes():
     f, p, big = ops.load_library().dear_checkpoint_weight_grad, SPACE, 1 << 60
     assert f(p, 1, 1 << 19, p, p, 4, 1 << 19, 1 << 19, p, p, big, None) == ETOOBIG
     assert f(p, 0, 1 << 24, p, p, 4, 1 << 24, 1 << 14, p, p, big, None) == ETOOBIG
+
+
+# batch 2, 4 query and 2 key heads of 64 values, 16 queries and 24 keys; (data, batch, token, head) strides
+OVERLAPPING = [(64, 64), (64, 128), (128, 64), (256, 128), (64, 512), (192, 64)]  # token, head
+APART = [(4096, 64, 1024), (8192, 256, 64), (64 * 16 * 4, 64, 64 * 16), (1 << 20, 1 << 10, 64), (64, 512, 128), (256, 512, 64), (8192, 264, 64)]
+
+
+@pytest.mark.parametrize("token,head", OVERLAPPING)
+@pytest.mark.parametrize("name", ["out", "dq"])
+def test_attention_refuses_outputs_whose_elements_share_a_place(name, token, head):
+    """Strides that are each long enough by themselves, and still lead two elements to one place."""
+    call = ops.load_library().dear_attention if name == "out" else ops.load_library().dear_attention_backward
+    few = dict(kv_len=8192, workspace_bytes=0)  # a call that needs a workspace, which is looked at last
+    assert call(attention_bytes(**{name: (SPACE, 1 << 20, token, head)}, **few), None) == EINVAL
+    assert call(attention_bytes(**{name: (SPACE, 512, 256, 64)}, **few), None) == EINVAL  # batches
+    assert call(attention_bytes(**{name: (SPACE, 64, 1 << 10, 1 << 20)}, **few), None) == ETOOBIG
+
+
+def test_attention_takes_outputs_of_any_order():
+    """Refused for their workspace alone."""
+    lib = ops.load_library()
+    for batch, token, head in APART:
+        change = dict(dq=(SPACE, batch, token, head), workspace_bytes=0)
+        assert lib.dear_attention_backward(attention_bytes(**change), None) == ETOOBIG, (batch, token, head)
+    # axes of one element: their strides say nothing
+    one = dict(batch=1, q_heads=1, kv_heads=1, q_len=1, workspace_bytes=0)
+    assert lib.dear_attention_backward(attention_bytes(dq=(SPACE, 0, 0, 0), **one), None) == ETOOBIG
