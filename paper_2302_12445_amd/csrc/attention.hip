@@ -1098,7 +1098,7 @@ int check_sizes(const dear_attention_t *p) {
     if (p->head_dim < 8 || p->head_dim > 128 || p->head_dim % 8) return DEAR_EINVAL;
     if (p->q_len < 0 || p->q_len > MAX_LEN || p->kv_len < 0 || p->kv_len > MAX_LEN) return DEAR_EINVAL;
     if (p->dtype != DEAR_F32 && p->dtype != DEAR_BF16) return DEAR_EINVAL;
-    if (p->causal != 0 && p->causal != 1) return DEAR_EINVAL;
+    if ((p->causal != 0 && p->causal != 1) || p->reserved != 0) return DEAR_EINVAL;
     if (!(p->scale > 0.f) || !std::isfinite(p->scale)) return DEAR_EINVAL;
     if (too_big(p->q_heads, p->batch, ceil_div(p->q_len, BLOCK)) || too_big(p->kv_heads, p->batch, ceil_div(p->kv_len, KEYS)))
         return DEAR_ETOOBIG;

@@ -235,3 +235,15 @@ def test_attention_takes_outputs_of_any_order():
     # axes of one element: their strides say nothing
     one = dict(batch=1, q_heads=1, kv_heads=1, q_len=1, workspace_bytes=0)
     assert lib.dear_attention_backward(attention_bytes(dq=(SPACE, 0, 0, 0), **one), None) == ETOOBIG
+
+
+def test_attention_refuses_what_is_reserved():
+    lib, at = ops.load_library(), 4 * 4 + 2 * 8 + 2 * 4 + 4  # behind scale
+    packed = bytearray(attention_bytes(kv_len=8192, workspace_bytes=0))
+    n = C.c_int64()
+    assert lib.dear_attention_workspace(bytes(packed), C.byref(n)) == OK and n.value > 0
+    packed[at] = 1
+    for f in (lib.dear_attention, lib.dear_attention_backward):
+        assert f(bytes(packed), None) == EINVAL
+    for f in (lib.dear_attention_workspace, lib.dear_attention_backward_workspace):
+        assert f(bytes(packed), C.byref(n)) == EINVAL
