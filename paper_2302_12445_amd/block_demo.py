@@ -35,7 +35,7 @@ class TinyTransformer(torch.nn.Module):
         x, residual = (self.embed(tokens) + self.position(at)).to(self.dtype), None
         for block in self.blocks:
             x, residual = block(x, residual, lens)
-        _, y, _ = self.norm(x, residual)
+        _, y, _ = self.norm(x, residual, keep=False)
         return self.head(y.float())
 
 

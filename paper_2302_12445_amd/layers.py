@@ -74,13 +74,14 @@ def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = Fal
 
 class _AddRMSNorm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, residual, weight, eps):
-        h, y, kept, rstd = ops.add_rms_norm(x, residual, weight, eps)
+    def forward(ctx, x, residual, weight, eps, keep):
+        h, y, kept, rstd = ops.add_rms_norm(x, residual, weight, eps, keep=keep)
         ctx.save_for_backward(h, weight, rstd)
         ctx.set_materialize_grads(False)
-        ctx.mark_non_differentiable(kept.codes, kept.exponents)
+        if keep:
+            ctx.mark_non_differentiable(kept.codes, kept.exponents)
         # without a residual h is x, which an output of its own has to stand for
-        return h if residual is not None else x.view_as(x), y, kept.codes, kept.exponents
+        return (h if residual is not None else x.view_as(x), y, *(kept[:2] if keep else (None, None)))
 
     @staticmethod
     def backward(ctx, dh, dy, _codes, _exponents):
@@ -89,29 +90,33 @@ class _AddRMSNorm(torch.autograd.Function):
             dx, dweight = dh, None
         else:
             dx, dweight = _first_order(ops.add_rms_norm_backward(dy, h, weight, rstd, dh=dh), dy, dh, h, weight)
-        return dx, dx if ctx.needs_input_grad[1] else None, dweight, None
+        return dx, dx if ctx.needs_input_grad[1] else None, dweight, None, None
 
 
 class AddRMSNorm(torch.nn.Module):
-    """h = x + residual; y = h / sqrt(mean(h^2) + eps) * weight.  Gives (h, y, the checkpoint of y)."""
+    """h = x + residual; y = h / sqrt(mean(h^2) + eps) * weight.  Gives (h, y, the checkpoint of y), or None in the
+    checkpoint's place where the call says that nothing will read it."""
 
     def __init__(self, width: int, eps: float = 1e-5):
         super().__init__()
         self.weight = torch.nn.Parameter(torch.ones(width))
         self.eps = eps
 
-    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, ops.Checkpoint]:
-        h, y, codes, exponents = _apply(_AddRMSNorm, x, residual, self.weight, self.eps)
-        return h, y, ops.Checkpoint(codes, exponents, self.weight.numel())
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, keep: bool = True
+                ) -> Tuple[torch.Tensor, torch.Tensor, Optional[ops.Checkpoint]]:
+        h, y, codes, exponents = _apply(_AddRMSNorm, x, residual, self.weight, self.eps, keep)
+        return h, y, ops.Checkpoint(codes, exponents, self.weight.numel()) if keep else None
 
 
 class _CheckpointLinear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, kept):
+    def forward(ctx, x, weight, bias, kept, keep):
         rows = x.reshape(-1, x.shape[-1])
         w = weight.to(x.dtype)
         out = rows @ w.t() if bias is None else torch.addmm(bias.to(x.dtype), rows, w.t())
-        if kept is None:
+        if not keep:
+            kept = ops.Checkpoint(None, None, x.shape[-1])
+        elif kept is None:
             kept = ops.checkpoint_encode(rows)
         source = x.new_empty(0)  # of the same inputs as out: what the weight's gradient is tied to, in the place of x
         ctx.save_for_backward(kept.codes, kept.exponents, weight, source)
@@ -128,7 +133,7 @@ class _CheckpointLinear(torch.autograd.Function):
         if ctx.needs_input_grad[1]:
             dw, = _first_order((ops.checkpoint_weight_grad(rows, ops.Checkpoint(codes, exponents, ctx.cols)),), rows, source)
         db = rows.sum(0, dtype=torch.float32) if ctx.has_bias and ctx.needs_input_grad[2] else None
-        return dx, dw, db, None
+        return dx, dw, db, None, None
 
 
 class CheckpointLinear(torch.nn.Module):
@@ -143,7 +148,8 @@ class CheckpointLinear(torch.nn.Module):
 
     def forward(self, x: torch.Tensor, kept: Optional[ops.Checkpoint] = None) -> torch.Tensor:
         """kept: the checkpoint of x, where it is there already."""
-        return _apply(_CheckpointLinear, x, self.weight, self.bias, kept)[0]
+        # a checkpoint is for the weight's gradient alone
+        return _apply(_CheckpointLinear, x, self.weight, self.bias, kept, torch.is_grad_enabled() and self.weight.requires_grad)[0]
 
 
 # Nodes of operations whose result holds its inputs' values: views, copies, casts, parts and what joins them.
@@ -212,10 +218,11 @@ class TransformerBlock(torch.nn.Module):
     def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None,
                 lens: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
         batch, tokens, width = x.shape
-        h, y, kept = self.norm1(x, residual)
+        trained = torch.is_grad_enabled()
+        h, y, kept = self.norm1(x, residual, trained and self.qkv.weight.requires_grad)
         q, k, v = self.qkv(y, kept).view(batch, tokens, -1, self.head_dim).split([self.heads, self.kv_heads, self.kv_heads], 2)
         out = attend(q, k, v, causal=self.causal, q_lens=lens, kv_lens=lens)
-        h, y, kept = self.norm2(self.proj(out.reshape(batch, tokens, width)), h)
+        h, y, kept = self.norm2(self.proj(out.reshape(batch, tokens, width)), h, trained and self.up.weight.requires_grad)
         u = self.up(y, kept)
         with saved_in_8_bits():
             z = torch.nn.functional.gelu(u)

@@ -127,6 +127,52 @@ def test_first_derivatives_with_a_graph_are_the_same(plain):
         assert torch.equal(a, b) and b.requires_grad and not a.requires_grad
 
 
+# ------------------------------------------------------------------------------------ work that nobody asks for
+def test_linear_makes_no_checkpoint_that_nothing_reads(plain):
+    linear, x = layers.CheckpointLinear(8, 3).double(), leaf(6, 8)
+    with torch.no_grad():
+        want = linear(x)
+    assert plain == []
+    assert torch.equal(linear(x), want) and plain == ["checkpoint_encode"]
+    plain.clear()
+    linear.weight.requires_grad_(False)  # a weight that is not trained
+    linear(x).sum().backward()
+    assert plain == [] and torch.allclose(x.grad, linear.weight.sum(0).expand(6, 8))
+    assert linear.bias.grad is not None and linear.weight.grad is None
+    with torch.no_grad():
+        linear(x, ops.Checkpoint(x, torch.zeros(1, dtype=torch.uint8), 8))
+    assert plain == []
+
+
+def test_norm_without_a_checkpoint(plain, monkeypatch):
+    norm, x = layers.AddRMSNorm(8).double(), leaf(6, 8)
+    asked = []
+    call = ops.add_rms_norm
+    monkeypatch.setattr(ops, "add_rms_norm", lambda *args, **kwargs: asked.append(kwargs.get("keep", True)) or call(*args, **kwargs))
+    h, y, kept = norm(x, x, keep=False)
+    assert kept is None and asked == [False]
+    (h + y).sum().backward()
+    assert torch.isfinite(x.grad).all() and torch.isfinite(norm.weight.grad).all()
+    assert norm(x, x)[2] is not None and norm(x, x, keep=True)[2] is not None and asked == [False, True, True]
+
+
+def test_block_makes_no_checkpoints_without_gradients(plain, monkeypatch):
+    """Nor does the demo's model for its last norm, which no linear layer on a checkpoint follows."""
+    from paper_2302_12445_amd.block_demo import TinyTransformer
+    asked = []
+    call = ops.add_rms_norm
+    monkeypatch.setattr(ops, "add_rms_norm", lambda *args, **kwargs: asked.append(kwargs.get("keep", True)) or call(*args, **kwargs))
+    torch.manual_seed(0)
+    model = TinyTransformer(16, 32, 4, 2, 2, 5, torch.float32)
+    tokens, lens = torch.randint(0, 16, (2, 5)), torch.tensor([5, 5], dtype=torch.int32)
+    monkeypatch.setattr(layers, "attend", lambda q, k, v, **_: q + k.repeat_interleave(2, 2) + v.repeat_interleave(2, 2))
+    with torch.no_grad():
+        want = model(tokens, lens)
+    assert asked == [False] * 5 and "checkpoint_encode" not in plain
+    asked.clear()
+    assert torch.equal(model(tokens, lens), want) and asked == [True] * 4 + [False]
+
+
 # ------------------------------------------------------------------------------------ what saved_in_8_bits leaves as it is
 @pytest.mark.parametrize("function", [torch.sigmoid, torch.tanh, torch.exp, lambda x: torch.softmax(x, -1)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float64])
