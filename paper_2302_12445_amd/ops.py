@@ -117,6 +117,7 @@ def _workspace(name: str, *sizes) -> int:
 # dear_attention_t
 _ATTENTION = struct.Struct("@4i2q2ifi2Q" + "Q3q" * 4 + "Q" + "Q3q" * 4 + "Qq")
 _NONE = (0, 0, 0, 0)
+_F32_MAX = (2 - 2 ** -23) * 2.0 ** 127
 
 
 def _readable(t: torch.Tensor, what: str):
@@ -162,6 +163,8 @@ def _attention_sizes(q, k, v, causal, scale, q_lens, kv_lens):
             raise ValueError("%s: expected a contiguous int32 tensor of %d on %s" % (what, B, q.device))
     # (head_dim 0 is refused by the library)
     scale = 1.0 / math.sqrt(D or 1) if scale is None else float(scale)
+    if _F32_MAX < abs(scale) < math.inf:  # (others are the library's to refuse)
+        raise ValueError("scale %g: fp32 does not hold it" % scale)
     return (q, k, v), (*pq, *pk, *pv), (B, H, Hkv, D, Sq, Sk, d, 1 if causal else 0, scale, 0,
                                         0 if q_lens is None else q_lens.data_ptr(), 0 if kv_lens is None else kv_lens.data_ptr())
 

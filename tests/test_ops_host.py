@@ -247,3 +247,12 @@ def test_attention_refuses_what_is_reserved():
         assert f(bytes(packed), None) == EINVAL
     for f in (lib.dear_attention_workspace, lib.dear_attention_backward_workspace):
         assert f(bytes(packed), C.byref(n)) == EINVAL
+
+
+@pytest.mark.parametrize("scale", [1e39, -1e39, 3.5e38])
+def test_a_scale_that_fp32_does_not_hold_is_a_value_error(monkeypatch, scale):
+    monkeypatch.setattr(ops, "_dtype", lambda t, what: 0)  # (tensors here are on the CPU)
+    q = torch.zeros(1, 4, 2, 64)
+    ops._ATTENTION.pack(*ops._attention_sizes(q, q, q, False, 3.4e38, None, None)[2], *([0] * 35))
+    with pytest.raises(ValueError):
+        ops._attention_sizes(q, q, q, False, scale, None, None)
