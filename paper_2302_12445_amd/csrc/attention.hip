@@ -13,7 +13,9 @@
 // from LDS with the transposing reads.
 //
 // Roundings.  Scores, p, ds, maxima and all sums are fp32.  In bf16 p and ds are rounded to bf16, as the matrix instructions take
-// both operands in one type: 2^-9 of each, no more than the inputs' own rounding.  The sum l is of the p before their rounding.
+// both operands in one type: at most 2^-8 of each, as the inputs' and the output's own roundings; two parts of each would take as
+// many products again.  Outputs' error against 64 bits is 1.3 to 1.4 times that of all fp32 rounded once.  The sum l is of the p
+// before their rounding.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -151,8 +153,8 @@ __device__ __forceinline__ char *part_row(const params &a, int heads, int len, i
 
 // ------------------------------------------------------------------------------------ forward
 // fp32, and bf16 whose rows lie too far apart for the kernels below.  Tiles go through registers to LDS, a step's loads beside the
-// products of the step before.  In fp32 the matrix instructions bound it (154 TFLOP/s reached by large products): 3 x 385 queries
-// and keys, 12 heads of 64, 38 us a call.
+// products of the step before, two barriers a step.  3 x 385 queries and keys in fp32, 12 heads of 64, 38 us a call, four times what
+// its products take at the rate of large ones (154 TFLOP/s).
 template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(false))) void attention_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
@@ -296,9 +298,10 @@ template <int N, int AHEAD> __device__ __forceinline__ void read_ahead() {
 }
 
 // Forward in bf16: 128 queries a workgroup, 32 a wave, two workgroups' waves a SIMD, steps of 64 keys in two buffers that are
-// filled beside the products of the step before.  Long sequences are bound by the matrix instructions, beside which the powers run;
-// short ones by the latency of a step's loads and barrier.  Measured: 8192 queries and keys, causal, 16 heads of 128 for 4, 285 us
-// = 963 TFLOP/s; 16 sequences of 512 with ragged lengths, 16 heads of 64, 24 us = 2.3 TB/s; 128 queries and keys, 16 heads, 6 us.
+// filled beside the products of the step before.  Rows of 128 are bound by the matrix instructions (busy 59 % of the time) and the
+// softmax's instructions beside them (53 %); rows of 64, with half the products for as many scores, by the softmax's (61 and 28 %;
+// waves wait 30 % of theirs).  Measured: 8192 queries and keys, causal, 16 heads of 128 for 4, 276 to 285 us = 963 TFLOP/s and more; 16
+// sequences of 512 with ragged lengths, 16 heads of 64, 24 us = 2.3 TB/s; 128 queries and keys, 16 heads, 6 us.
 template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_direct_kernel(params a) {
     __shared__ __attribute__((aligned(16))) bf16 ks0[STEP * W], ks1[STEP * W], vs0[STEP * W], vs1[STEP * W];
     int b, h, t, split;
@@ -431,7 +434,8 @@ __device__ __forceinline__ float row_values(const params &a, int b, int h, int i
 
 // dq of 32 queries a wave, over all keys.  As in the forward pass the results of the first products are taken
 // transposed, a query to a lane, so that lse and delta are one value a lane.  It also writes delta for the other kernel.
-// fp32, 3 x 385 with ragged lengths, 12 heads of 64, in two splits: 44 us, by its matrix instructions.
+// fp32, 3 x 385 with ragged lengths, 12 heads of 64, in seven splits: 44 us, and 6 to join them; its matrix instructions are busy
+// 49 % of the time.
 template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(false))) void attention_dq_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     DEAR_LDS T *ks = (DEAR_LDS T *)lds, *vs = (DEAR_LDS T *)(lds + tile<T, W>::bytes(STEP));
@@ -513,7 +517,7 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
 // ------------------------------------------------------------------------------------ backward: keys and values
 // dk and dv of 32 keys a wave, over the queries of all heads that share them: one workgroup adds them all up, in order.
 // Two waves have the same keys and take every other 32 queries; their sums are added at the end.  fp32, 3 x 385 with ragged
-// lengths, 12 heads of 64: 51 us, by its matrix instructions.
+// lengths, 12 heads of 64: 51 us, one wave a SIMD, whose matrix instructions are busy 46 % of the time.
 template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, W>(true))) void attention_dkv_kernel(params a) {
     __shared__ __attribute__((aligned(16))) char lds[2 * tile<T, W>::bytes(STEP)];
     __shared__ __attribute__((aligned(16))) float rows[2][STEP];  // what the queries' powers are taken against, and -delta
@@ -617,9 +621,10 @@ template <typename T, int W> __global__ __launch_bounds__(THREADS, (resident<T, 
 }
 
 // ------------------------------------------------------------------------------------ bf16 backward, tiles filled directly
-// dq as above, its tiles as in the forward pass.  Bound by the matrix instructions where sequences are long: 2 x 4096, causal, 16
-// heads of 128 for 4, 201 us = 1026 TFLOP/s of its three products; by the latency of steps where they are short: 16 x 512, ragged,
-// 16 heads of 64, 35 us.  Three waves a SIMD have too few registers (1 x 2048, causal, with dk and dv: 91 us for 84).
+// dq as above, its tiles as in the forward pass.  Bound by the matrix instructions where sequences are long: 2 x 4096,
+// causal, 16 heads of 128 for 4, 201 us = 1026 TFLOP/s of its three products.  16 x 512, ragged, 16 heads of 64, 35 us:
+// matrix instructions busy 28 %, vector instructions 40 %, and waves wait 42 % of their time.  Three waves a SIMD have too
+// few registers (1 x 2048, causal, with dk and dv: 91 us for 84).
 template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_direct_kernel(params a) {
     __shared__ __attribute__((aligned(16))) bf16 ks0[STEP * W], ks1[STEP * W], vs0[STEP * W], vs1[STEP * W];
     int b, h, t, split;
@@ -718,7 +723,8 @@ template <int W> __global__ __launch_bounds__(THREADS, 2) void attention_dq_dire
 }
 
 // dk and dv of 128 keys a workgroup, 32 a wave, for rows of 64 values: the operands and sums of both fit a wave beside a
-// second one.  16 x 512, ragged, 16 heads: 44 us, by the latency of steps; in two kinds of waves as below 68 us.
+// second one.  16 x 512, ragged, 16 heads: 44 us, matrix instructions busy 31 %, vector instructions 38 %, waves waiting 39 % of
+// their time; in two kinds of waves as below 68 us.
 __global__ __launch_bounds__(THREADS, 2) void attention_dkv_direct_kernel(params a) {
     constexpr int W = 64;
     __shared__ __attribute__((aligned(16))) bf16 qs0[STEP * W], qs1[STEP * W], gs0[STEP * W], gs1[STEP * W];

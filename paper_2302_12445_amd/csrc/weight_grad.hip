@@ -142,18 +142,20 @@ template <typename T, bool VEC> __global__ __launch_bounds__(THREADS, 2) void we
 }
 
 // ------------------------------------------------------------------------------------ bf16, whole vectors
-// A workgroup owns 128 x 128 outputs and each of its four waves sums all of them over rows of its own, 32 of every 128:
-// a wave reads eight fragments for sixteen products, and the waves meet only at the end, to add their sums.  dy goes from
+// A workgroup owns 128 x 128 outputs and each of its four waves sums all of them over rows of its own, 32 of every 128: a
+// wave reads eight fragments for sixteen products, and the waves meet only at the end, to add their sums.  dy goes from
 // memory to LDS by itself; codes come to registers, and as values to LDS, beside the products of the step before.  8192 rows,
-// 1024 x 4096: 83 us = 830 TFLOP/s; it is bound by what stands beside the products: the reads of fragments and the values made of
-// codes.  The same outputs cut among the waves, 64 x 64 each, read twice as much from LDS and need a barrier a step: 186 us, and
-// eight waves of 128 x 64 with a barrier a step 116.
+// 1024 x 4096: 81 us a call = 850 TFLOP/s; with one wave a SIMD matrix instructions are busy 39 % of the time, the vector
+// instructions that make values of codes 36 %, and 31 % of the LDS's cycles are bank conflicts.  The same outputs cut among
+// the waves, 64 x 64 each, read twice as much from LDS and need a barrier a step: 186 us, and eight waves of 128 x 64 with a
+// barrier a step 116.
 constexpr int WROWS = 32;                      // rows of a wave's step
 constexpr int WSTEP = WROWS * (THREADS / 64);  // rows of a workgroup's step
 constexpr int WTILE = WROWS * 128;             // elements of one operand's tile
 
 // Tiles have rows of 128 values without padding; piece c (16 bytes) of a row stands at c ^ turn(row), so that the four rows
-// of a transposing read, and two rows that are written, lie in different banks.
+// of a transposing read lie in different banks.  Values are written 32 bytes apart from lane to lane, which is what conflicts
+// there are (attention's tiles, read alike and written in neighbouring pieces, have none).
 __device__ __forceinline__ int turn(int row) { return (row & 3) << 2 | (row & 1); }
 
 struct wave_codes {
