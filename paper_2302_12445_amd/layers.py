@@ -170,7 +170,8 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     """Within it, what torch's own operations keep for their backward passes is kept as checkpoints: activations (as a GELU's
     input), which are floating tensors on the GPU of at least `least` elements that were computed on the way of a gradient.
     What is left as it is: parameters and other leaves, what holds values of parameters alone (views, casts, parts, joined ones),
-    and whatever takes no part in the gradient, as statistics; also what the layers of this file keep.  Not for what has to come back exactly, such as a mask in floating
+    whatever takes no part in the gradient, as statistics, and rows so short that a checkpoint would be no smaller; also what the
+    layers of this file keep.  Not for what has to come back exactly, such as a mask in floating
     point, nor for infinities: a group of 32 neighbours that holds one comes back as NaN.
 
         with saved_in_8_bits():
@@ -178,16 +179,16 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     """
 
     def __init__(self, least: int = 1 << 16):
+        def smaller(t):  # a row's last group is filled up, so that narrow rows are not, and columns (norms' factors) 33 bytes a value
+            cols = t.shape[-1] if t.dim() else 1
+            return -(-cols // ops.GROUP) * (ops.GROUP + 1) < cols * t.element_size()
+
         def pack(t):
-            if (not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or t.numel() < max(least, 1)
+            if (not t.is_cuda or t.dtype not in (torch.bfloat16, torch.float32) or t.numel() < max(least, 1) or not smaller(t)
                     or t.grad_fn is None or _of_parameters(t.grad_fn) or getattr(_applied, "here", False)):
                 # not t: an operation that keeps its own output would be held by what it keeps, for ever
                 return t.detach(), t._version
-            rows, n = t.detach(), t.numel()
-            if not t.dim() or t.shape[-1] % ops.GROUP:
-                # rows that fill no whole groups would each be filled up with zeros: the values as they follow one another instead
-                rows = rows.reshape(-1, ops.GROUP) if n % ops.GROUP == 0 else rows.reshape(1, -1) if n <= ops.MAX_COLS else rows
-            return ops.checkpoint_encode(rows), t.shape, t.dtype
+            return ops.checkpoint_encode(t.detach()), t.shape, t.dtype
 
         def unpack(kept):
             if len(kept) == 2:

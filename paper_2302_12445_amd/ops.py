@@ -28,7 +28,6 @@ from .binding import DEAR_BF16, DEAR_F32, DearError
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdear_ops.so")
 GROUP = 32  # DEAR_CHECKPOINT_GROUP
-MAX_COLS = (1 << 31) - 1 - GROUP  # of a checkpoint
 NORM_MAX_COLS = 32768
 
 EXPORTS = [

@@ -118,33 +118,44 @@ def test_statistics_are_left_as_they_are(layers):
 
 # ------------------------------------------------------------------------------------ memory
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("shape", [(512, 1024), (70001, 1), (30000, 33), (200000, 3), (7, 11, 13, 129)])
-def test_what_is_kept_takes_a_byte_a_value(layers, shape, dtype):
-    """Codes, and a byte for every 32 values and what fills up a row, whatever the last axis is; and the gradient is the GELU's at the values kept."""
+@pytest.mark.parametrize("shape", [(512, 1024), (70001, 1), (30000, 33), (200000, 3), (7, 11, 13, 129), (5000, 14)])
+def test_what_is_kept_is_never_larger(layers, shape, dtype):
+    """33 bytes for every 32 values of a row, the last of which are filled up; where that is no less than the values themselves
+    (short rows), these.  The gradient is the GELU's at the values kept."""
     from paper_2302_12445_amd import ops
-    n = torch.Size(shape).numel()
+    n, size = torch.Size(shape).numel(), dtype.itemsize
+    codes = n // shape[-1] * -(-shape[-1] // 32) * 33
     u = normal(*shape, dtype=dtype).requires_grad_()
     gelu(u * 1.0).sum().backward()  # (libraries' workspaces)
-    exact, u.grad = u.grad, None
+    u.grad = None
     torch.cuda.synchronize()
-    with layers.saved_in_8_bits():
-        v = u * 1.0
-        z = gelu(v)
-    value = v.detach().clone()
     before = torch.cuda.memory_allocated()
-    z.sum().backward()
-    torch.cuda.synchronize()
-    gradient = u.grad.numel() * u.element_size()
-    del v  # its last use: after it the node is gone, whose checkpoint the backward pass has freed
-    freed = before - (torch.cuda.memory_allocated() - gradient)
-    assert freed < n * u.element_size() + n * 1.1 + 4096
-    assert freed > n * u.element_size()  # v itself is among it
-    near = u.grad.float() - exact.float()
-    assert near.abs().max() > 0 and near.abs().max() <= 2 * value.float().abs().max() / 127 + 2 ** -7
-    if shape[-1] % 32 == 0:
-        kept = ops.checkpoint_decode(ops.checkpoint_encode(value), dtype).view(shape).requires_grad_()
-        gelu(kept).sum().backward()
-        assert torch.equal(u.grad, kept.grad)
+    with layers.saved_in_8_bits(least=1000):
+        z = gelu(u * 1.0).sum()
+    kept = torch.cuda.memory_allocated() - before
+    assert kept <= min(codes, n * size) + 4096
+    z.backward()
+    value = u.detach()
+    if codes < n * size:
+        value = ops.checkpoint_decode(ops.checkpoint_encode(value), dtype).view(shape)
+    value = value.requires_grad_()
+    gelu(value).sum().backward()
+    assert torch.equal(u.grad, value.grad)
+
+
+def test_a_norm_s_factors_by_hand(layers):
+    """A column of factors, one of them huge as a padded row's is: its neighbours' gradients are those of their own factors."""
+    x = normal(1 << 16, 64)
+    x[100] = 0
+    x.requires_grad_()
+    scale = normal(1 << 16, 64, seed=1)
+    def loss():
+        y = x * 1.0
+        return (y * torch.rsqrt(y.square().mean(1, keepdim=True) + 1e-12) * scale).sum()
+    want, = gradients(layers.saved_in_8_bits(least=1 << 40), loss, x)
+    got, = gradients(layers.saved_in_8_bits(), loss, x)
+    rest = torch.arange(1 << 16, device=DEV) != 100
+    assert (got - want)[rest].norm() < 0.02 * want[rest].norm()
 
 
 def test_single_values_and_nothing(layers):
