@@ -160,10 +160,19 @@ _SAME_VALUES = {name + "Backward" for name in (
 
 def _of_parameters(node) -> bool:
     """Whether a node of the graph gives values of parameters alone."""
-    if hasattr(node, "variable"):
-        return isinstance(node.variable, torch.nn.Parameter)
-    sources = [n for n, _ in node.next_functions if n is not None]
-    return node.name().rstrip("0123456789") in _SAME_VALUES and bool(sources) and all(map(_of_parameters, sources))
+    seen, left = {node}, [node]
+    while left:
+        node = left.pop()
+        if hasattr(node, "variable"):
+            if not isinstance(node.variable, torch.nn.Parameter):
+                return False
+            continue
+        sources = {n for n, _ in node.next_functions if n is not None}
+        if node.name().rstrip("0123456789") not in _SAME_VALUES or not sources:
+            return False
+        left += sources - seen
+        seen |= sources
+    return True
 
 
 class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):

@@ -210,3 +210,20 @@ def test_what_is_left_alone_and_changed_in_place_is_noticed():
     source.add_(1)
     with pytest.raises(RuntimeError, match="in place"):
         out.sum().backward()
+
+
+def test_whose_values_a_tensor_holds():
+    weight, x = torch.nn.Parameter(torch.randn(8, 4)), torch.randn(8, 4, requires_grad=True)
+    for f in (lambda t: t.t(), lambda t: t.bfloat16(), lambda t: t.chunk(2)[1], lambda t: torch.stack([t[:4], t[4:]]), lambda t: t.squeeze(0),
+              lambda t: t[torch.tensor([1, 3])], lambda t: t.flatten().view(2, 16), lambda t: t.expand(3, 8, 4), lambda t: t.mT.contiguous()):
+        assert layers._of_parameters(f(weight).grad_fn) and not layers._of_parameters(f(x * 1).grad_fn)
+    for t in (weight * 1, x @ weight.t(), torch.cat([weight, x * 1]), torch.cat([weight * 1, weight])):
+        assert not layers._of_parameters(t.grad_fn)
+    # long chains, as of what grows piece by piece, and what is joined with itself over and over
+    for source in (weight, x * 1):
+        chain = doubled = source
+        for _ in range(3000):
+            chain = chain.view(8, 4)
+        for _ in range(64):
+            doubled = torch.stack([doubled, doubled])[0]
+        assert layers._of_parameters(chain.grad_fn) == layers._of_parameters(doubled.grad_fn) == (source is weight)
