@@ -7,6 +7,9 @@
  *                 8 bits; backward pass
  *   checkpoints   activations kept in 8 bits for the backward pass, and the weight gradient of a
  *                 linear layer computed from the checkpoint of its input
+ *   recurrence    gated linear recurrence along the steps of sequences; backward pass
+ *   experts       products of rows with the weights of their experts, and both gradients
+ *   gradients     the norm over a model's gradients, and clipping
  *
  * The library is libdear_ops.so.  Status codes and element types are those of dear.h
  * (dear_strerror describes a status).
@@ -164,6 +167,118 @@ int dear_add_rms_norm_backward(const void *dy, int64_t dy_stride, const void *h,
                                int64_t rows, int64_t cols, void *dx, float *dweight, void *workspace,
                                int64_t workspace_bytes, void *hip_stream);
 int dear_add_rms_norm_backward_workspace(int32_t dtype, int64_t rows, int64_t cols, int64_t *bytes);
+
+/* ---------------------------------------------------------------------------------
+ * Gated linear recurrence along the steps of a batch of sequences, each channel by itself:
+ *     a[t] = 1 / (1 + exp(-gate[t]));  s[t] = a[t] * s[t-1] + (1 - a[t]) * x[t];  h[t] = s[t] (rounded to dtype)
+ * from s[-1] = state, over the first lens[b] steps of sequence b (clamped to 0 .. steps); behind them
+ * the state stays, h is 0 and what x and gate hold is never used.  Backward, with G the gradient of s:
+ *     G[t] = dh[t] + a[t+1] * G[t+1]  (G = dlast behind the last step, as if through a = 1)
+ *     dx[t] = (1 - a[t]) * G[t];  dgate[t] = G[t] * (s[t-1] - x[t]) * a[t] * (1 - a[t]);  dstate = a[0] * G[0]
+ * and 0 behind the last step.  States and sums are fp32 throughout: the backward pass computes the
+ * states again from those that the forward pass kept.  A NaN or an infinity stays within its sequence and channel.
+ */
+#define DEAR_RECURRENCE_KEPT 256 /* steps from one kept state to the next */
+
+/* A [batch, step, channel] tensor: channels are contiguous, the other strides are in elements, step_stride
+ * below 2^22 (DEAR_ETOOBIG otherwise).  Strides of 0 and tensors that are written: as for dear_heads_t. */
+typedef struct {
+    void *data;
+    int64_t batch_stride, step_stride;
+} dear_steps_t;
+
+typedef struct {
+    int32_t batch;           /* >= 0                                                             */
+    int32_t width;           /* channels: 1 .. 2^24                                              */
+    int64_t steps;           /* 0 .. 2^30: steps that the tensors hold for each sequence         */
+    int32_t dtype;           /* DEAR_F32 or DEAR_BF16, of all tensors but states                 */
+    int32_t reserved;        /* 0                                                                */
+    const int32_t *lens;     /* [batch] valid steps, or NULL: all                                */
+    dear_steps_t x, gate;    /* read                                                             */
+    const float *state;      /* [batch, width] contiguous, read by the forward pass; NULL: zeros */
+    float *kept;             /* [batch, ceil(steps / DEAR_RECURRENCE_KEPT), width]: the state before every
+                                256th step; forward: written, or NULL; backward: read            */
+    dear_steps_t h;          /* forward: written                                                 */
+    float *last;             /* [batch, width] forward: the state behind the last step, written; or NULL.
+                                May be state itself                                              */
+    /* backward only */
+    dear_steps_t dh;         /* read: gradient of h                                              */
+    const float *dlast;      /* [batch, width] gradient of last, or NULL: zeros                  */
+    dear_steps_t dx, dgate;  /* written                                                          */
+    float *dstate;           /* [batch, width] written, or NULL.  May be dlast itself            */
+    void *workspace;         /* 256-byte aligned; NULL where its size is 0                       */
+    int64_t workspace_bytes;
+} dear_recurrence_t;
+
+/* Tensors are aligned to their element types (16 bytes, with strides and widths to match, are faster).
+ * Errors: DEAR_EINVAL, DEAR_EALIGN, DEAR_EHIP; DEAR_ETOOBIG where workspace_bytes is less than the call needs, or where a
+ * launch would have 2^32 threads or more: 512 for every 64 channels (fp32: 32) of a sequence or, where there are less than
+ * 512 such groups, of every 256 steps. */
+int dear_recurrence(const dear_recurrence_t *args, void *hip_stream);
+int dear_recurrence_backward(const dear_recurrence_t *args, void *hip_stream);
+/* Bytes of workspace that either call with these sizes needs (pointers and strides are not looked at). */
+int dear_recurrence_workspace(const dear_recurrence_t *args, int64_t *bytes);
+
+/* ---------------------------------------------------------------------------------
+ * Products grouped by expert.  Rows are sorted by expert: expert e has rows ends[e-1] .. ends[e] - 1 (expert 0 from row 0
+ * on), with each end taken to be at least the one before it and at most `rows`; an expert may have none.
+ *     linear        y[m, n]  = sum over k of x[m, k] * weight[e(m), n, k]
+ *     input_grad    dx[m, k] = sum over n of dy[m, n] * weight[e(m), n, k]
+ *     weight_grad   dweight[e, n, k] = sum over the rows m of expert e of dy[m, n] * x[m, k]
+ * Rows behind the last expert's get 0, what they hold is not used, and an expert without rows gets a weight gradient of 0.
+ * Products are taken of the inputs' type (fp32: fp32 matrix instructions), sums are fp32, y and dx are rounded once.
+ * A NaN or an infinity reaches the results that it is a factor of, and no others.
+ */
+typedef struct {
+    int64_t rows;            /* 0 .. 2^31 - 1                                                    */
+    int32_t experts;         /* 1 .. 2^16                                                        */
+    int32_t outs, ins;       /* 1 .. 2^20                                                        */
+    int32_t dtype;           /* DEAR_F32 or DEAR_BF16, of x, weight, dy, y and dx                */
+    const int32_t *ends;     /* [experts]                                                        */
+    const void *x;           /* [rows, ins], rows x_stride elements apart                        */
+    int64_t x_stride;
+    const void *weight;      /* [experts, outs, ins] contiguous                                  */
+    const void *dy;          /* [rows, outs], rows dy_stride elements apart                      */
+    int64_t dy_stride;
+    void *out;               /* written, contiguous: y [rows, outs], dx [rows, ins] or dweight fp32 [experts, outs, ins] */
+    void *workspace;         /* 256-byte aligned; NULL where its size is 0                       */
+    int64_t workspace_bytes;
+} dear_experts_t;
+
+/* A call looks only at the members that its product has.  Strides are at least the rows' widths, where there are several rows.
+ * Tensors are aligned to their element types (16 bytes, with strides and widths to match, are faster).
+ * Errors: DEAR_EINVAL, DEAR_EALIGN, DEAR_EHIP; DEAR_ETOOBIG where workspace_bytes is less than the call needs, or where a launch
+ * would have 2^32 threads or more: 256 for every 128 x 128 outputs of an expert. */
+int dear_expert_linear(const dear_experts_t *args, void *hip_stream);
+int dear_expert_input_grad(const dear_experts_t *args, void *hip_stream);
+int dear_expert_weight_grad(const dear_experts_t *args, void *hip_stream);
+/* Bytes of workspace that a call with these sizes needs (pointers and strides are not looked at). */
+int dear_expert_linear_workspace(const dear_experts_t *args, int64_t *bytes);
+int dear_expert_input_grad_workspace(const dear_experts_t *args, int64_t *bytes);
+int dear_expert_weight_grad_workspace(const dear_experts_t *args, int64_t *bytes);
+
+/* ---------------------------------------------------------------------------------
+ * The norm over the gradients of all tensors of a list, and the gradients scaled down to a largest norm:
+ *     norm = sqrt(sum of g^2 over all elements of all tensors)
+ *     out = g * min(1, max_norm / norm), rounded to out_dtype
+ * Squares are added in 64 bits, norm is rounded to fp32 once.  A NaN or an infinity among the gradients makes the norm one;
+ * with a norm of NaN every out is NaN, with an infinite one finite gradients become 0 and infinite ones NaN.
+ */
+typedef struct {
+    const void *data;        /* elements in a row, without gaps; aligned to their type           */
+    void *out;               /* clip: written; data itself (with its type) or a place of its own */
+    int64_t elements;        /* 0 .. 2^56                                                        */
+    int32_t dtype, out_dtype;/* DEAR_F32 or DEAR_BF16 each                                       */
+} dear_grad_t;
+
+/* grads: host memory, count (0 .. 2^20) tensors.  norm: device, one fp32, written.  workspace: 256-byte aligned, as many bytes
+ * as dear_grad_norm_workspace says.  max_norm > 0 (an infinity clips nothing).  A gradient that need not change is not written
+ * where out is data.  Outputs that overlap one another, or other tensors' inputs, are refused.
+ * Errors: DEAR_EINVAL, DEAR_EALIGN, DEAR_ENOMEM (host), DEAR_EHIP; DEAR_ETOOBIG where the workspace is too small. */
+int dear_grad_norm(const dear_grad_t *grads, int64_t count, float *norm, void *workspace, int64_t workspace_bytes, void *hip_stream);
+int dear_clip_grads(const dear_grad_t *grads, int64_t count, float max_norm, float *norm, void *workspace, int64_t workspace_bytes,
+                    void *hip_stream);
+int dear_grad_norm_workspace(int64_t count, int64_t *bytes);
 
 #ifdef __cplusplus
 }

@@ -16,7 +16,7 @@ PROBE_SOURCES = [os.path.join(CSRC, "hbm_probe.hip")]
 PROBE_HEADERS = [os.path.join(ROOT, "include", "dear_probe.h")]
 # training operators, a library of their own (include/dear_ops.h)
 OPS_LIB = os.path.join(PKG, "libdear_ops.so")
-OPS_SOURCES = [os.path.join(CSRC, f) for f in ("attention.hip", "norm.hip", "weight_grad.hip")]
+OPS_SOURCES = [os.path.join(CSRC, f) for f in ("attention.hip", "norm.hip", "weight_grad.hip", "recurrence.hip", "experts.hip", "grad_norm.hip")]
 # accumulators of 16 values stay whole where control flow meets: taken apart into single values, as the compiler would
 # by its own measure, they are copied one by one in every step (attention's dk and dv: 48 spilled registers, and none so)
 OPS_FLAGS = ["-mllvm", "-amdgpu-codegenprepare-break-large-phis=false"]

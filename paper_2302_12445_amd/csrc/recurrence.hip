@@ -1,0 +1,576 @@
+// Gated linear recurrence along the steps of each sequence, forward and backward (definitions: dear_ops.h).
+//
+//     a = sigmoid(gate);  s[t] = a[t] s[t-1] + (1 - a[t]) x[t]
+//     G[t] = dh[t] + e[t+1],  e[t] = a[t] G[t];  dx = (1 - a) G;  dgate = G (s[t-1] - x) a (1 - a)
+//
+// A stretch of steps is a map s -> A s + H with A the product of its a; two stretches in a row are again one:
+// (A2 A1, A2 H1 + H2).  Backward the map is e -> A e + E with the same A, from the last step to the first.  So a tile of
+// 256 steps is cut into strips of eight: a lane joins its own steps, lanes and waves join theirs, and a second
+// walk over the strip, from the state before it, gives the outputs; every tensor is read once.  The backward pass needs the
+// states before each step as well: it computes them again, in fp32, from the states that the forward pass kept at each tile's
+// first step, which takes less traffic than to read h, and no rounding.
+//
+// HBM bounds it: 6 bytes of bf16 an element forward and 10 backward.
+#include <type_traits>
+
+#include "ops_common.h"
+
+#pragma clang fp contract(fast)
+
+namespace {
+
+using namespace dear_ops;
+
+constexpr int KEPT = DEAR_RECURRENCE_KEPT;  // steps from one kept state to the next: a whole tile
+constexpr int R = 8;                        // steps of a lane's strip
+constexpr int N = 4;                        // channels of a lane
+constexpr int ROW_LANES = 16;               // lanes across the channels; the wave's other axis is time, four strips
+constexpr int STRIPS = 64 / ROW_LANES;
+constexpr int WAVE_STEPS = STRIPS * R;
+constexpr int CG = N * ROW_LANES;           // channels of a workgroup: in bf16 128 bytes of a row, a line of the cache
+constexpr int WAVES = KEPT / WAVE_STEPS;    // that a tile fills
+static_assert(KEPT % WAVE_STEPS == 0, "a tile is made of whole waves");
+
+struct rows_t {
+    const void *data;
+    int64_t batch_stride, step_stride;
+};
+
+struct params {
+    rows_t x, gate, h, dh, dx, dgate;
+    const float *state, *dlast;
+    float *last, *dstate, *kept;
+    const int32_t *lens;
+    float *maps;  // of tiles that workgroups share a sequence's steps by: [batch, tiles + 1, 2, width]
+    int64_t steps;
+    int32_t width, groups, tiles;
+};
+
+// a = sigmoid(g) and b = 1 - a, each to full relative precision: from exp(-|g|), which neither overflows nor cancels.
+__device__ __forceinline__ void gates(float g, float &a, float &b) {
+    const float t = __builtin_amdgcn_exp2f(__builtin_fabsf(g) * -1.44269504088896f);
+    const float big = __builtin_amdgcn_rcpf(1.f + t), small = t * big;
+    a = g >= 0.f ? big : small;
+    b = g >= 0.f ? small : big;
+}
+
+// Of a lane and the one at distance 16 or 32: the value of the earlier and of the later.
+template <int D> __device__ __forceinline__ void neighbours(float x, float &earlier, float &later) {
+    const uint32_t u = __float_as_uint(x);
+    auto w = D == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false) : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    earlier = __uint_as_float(w[0]), later = __uint_as_float(w[1]);
+}
+
+// One level of joining the strips of a wave.  A, H, E: the map of the lane's block of strips, which becomes that of the block twice
+// as long.  before: the map from the block's first step to the lane's, behind: backward from the block's last step to the lane's.
+template <int D, bool FORWARD, bool BACKWARD>
+__device__ __forceinline__ void join(float &A, float &H, float &E, float &before_A, float &before_H, float &behind_A, float &behind_E, int lane) {
+    float A0, A1;
+    neighbours<D>(A, A0, A1);
+    const bool later = lane & D;
+    if (FORWARD) {
+        float H0, H1;
+        neighbours<D>(H, H0, H1);
+        before_H = later ? before_A * H0 + before_H : before_H;
+        before_A = later ? before_A * A0 : before_A;
+        H = A1 * H0 + H1;
+    }
+    if (BACKWARD) {
+        float E0, E1;
+        neighbours<D>(E, E0, E1);
+        behind_E = later ? behind_E : behind_A * E1 + behind_E;
+        behind_A = later ? behind_A : behind_A * A1;
+        E = A0 * E1 + E0;
+    }
+    A = A0 * A1;
+}
+
+// How a lane's N channels lie in memory.
+enum { SINGLE, ANYWHERE, ALIGNED };
+
+// Where a lane stands: its channels, its strip and, of a tile, its first step.  Lanes behind the last channel take the last ones over
+// again, with the same results, so that no lane needs a branch.
+struct place {
+    int64_t b;
+    int lane, wave, col, step;
+    __device__ __forceinline__ place(const params &a, uint32_t sequence_group, int mode) {
+        lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        b = sequence_group / a.groups;
+        col = (int)(sequence_group % a.groups) * CG + lane % ROW_LANES * N;
+        if (mode != SINGLE) col = min(col, a.width - N);
+        step = wave * WAVE_STEPS + lane / ROW_LANES * R;
+    }
+};
+
+__device__ __forceinline__ int64_t length(const params &a, int64_t b) {
+    return a.lens ? min(max((int64_t)a.lens[b], (int64_t)0), a.steps) : a.steps;
+}
+
+template <typename T> struct four { typedef T type __attribute__((ext_vector_type(N))); };
+template <typename T> using values = typename four<T>::type;
+template <typename T> struct four_anywhere { typedef values<T> type __attribute__((aligned(sizeof(T)))); };  // global memory takes it
+
+template <typename T, int MODE> __device__ __forceinline__ values<T> load(const T *row, int col, int cols) {
+    if (MODE == ALIGNED) return *(const values<T> *)(row + col);
+    if (MODE == ANYWHERE) return *(const typename four_anywhere<T>::type *)(row + col);
+    values<T> v;
+#pragma unroll
+    for (int c = 0; c < N; ++c) v[c] = row[min(col + c, cols - 1)];
+    return v;
+}
+template <typename T, int MODE> __device__ __forceinline__ void store(T *row, values<T> v, int col, int cols) {
+    if (MODE == ALIGNED) *(values<T> *)(row + col) = v;
+    else if (MODE == ANYWHERE) *(typename four_anywhere<T>::type *)(row + col) = v;
+    else
+#pragma unroll
+        for (int c = 0; c < N; ++c) row[min(col + c, cols - 1)] = v[c];
+}
+
+// Of a tensor the R rows of a lane's strip in a tile that starts at `at` (the same for the whole workgroup, so that a lane's address is
+// 32 bits beside it).  Only `valid` rows of the tile, one at least, are read: behind them the last one again.
+template <typename T> __device__ __forceinline__ char *tile_at(const rows_t &t, int64_t b, int tile) {
+    return (char *)t.data + (b * t.batch_stride + (int64_t)tile * KEPT * t.step_stride) * (int64_t)sizeof(T);
+}
+template <typename T, int MODE>
+__device__ __forceinline__ void load_strip(values<T> (&v)[R], const rows_t &from, int tile, const place &p, int valid, int cols) {
+    const char *at = tile_at<T>(from, p.b, tile);
+    const uint32_t stride = (uint32_t)from.step_stride * (uint32_t)sizeof(T);
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = load<T, MODE>((const T *)(at + (uint32_t)min(p.step + r, valid - 1) * stride), p.col, cols);
+}
+template <typename T, int MODE>
+__device__ __forceinline__ void store_strip(const values<T> (&v)[R], const rows_t &to, int tile, const place &p, int there, int cols) {
+    char *at = tile_at<T>(to, p.b, tile);
+    const uint32_t stride = (uint32_t)to.step_stride * (uint32_t)sizeof(T);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (p.step + r < there) store<T, MODE>((T *)(at + (uint32_t)(p.step + r) * stride), v[r], p.col, cols);
+}
+// Of the steps left from a tile's first on, those within it.
+__device__ __forceinline__ int within(int64_t steps, int tile) {
+    return (int)min(max(steps - (int64_t)tile * KEPT, (int64_t)0), (int64_t)KEPT);
+}
+
+// A row of states.
+template <int MODE> __device__ __forceinline__ void load_state(float *s, const float *row, int col, int cols) {
+    const values<float> v = load<float, MODE>(row, col, cols);
+#pragma unroll
+    for (int c = 0; c < N; ++c) s[c] = v[c];
+}
+template <int MODE> __device__ __forceinline__ void store_state(float *row, const float *s, int col, int cols) {
+    store<float, MODE>(row, values<float>{s[0], s[1], s[2], s[3]}, col, cols);
+}
+
+// The map of a tile's steps before the last wave has been joined: each wave's in LDS, [wave][A, H or E][channel].
+template <int W> using wave_maps = float[W][3][CG];
+
+// State behind the tiles before `tile`, from the maps in memory: the first is that of the state before the first step.
+template <int MODE> __device__ __forceinline__ void fold_before(float *s, const params &a, int64_t b, int tile, int col) {
+    const float *m = a.maps + b * (a.tiles + 1) * 2 * a.width;
+    load_state<MODE>(s, m + a.width, col, a.width);
+    for (int i = 1; i <= tile; ++i) {
+        float A[N], H[N];
+        load_state<MODE>(A, m + (int64_t)i * 2 * a.width, col, a.width);
+        load_state<MODE>(H, m + ((int64_t)i * 2 + 1) * a.width, col, a.width);
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] = A[c] * s[c] + H[c];
+    }
+}
+// Backward: from the tiles behind `tile`; the last map is that of the gradient of the last state.
+template <int MODE> __device__ __forceinline__ void fold_behind(float *e, const params &a, int64_t b, int tile, int col) {
+    const float *m = a.maps + b * (a.tiles + 1) * 2 * a.width;
+    load_state<MODE>(e, m + ((int64_t)a.tiles * 2 + 1) * a.width, col, a.width);
+    for (int i = a.tiles - 1; i > tile; --i) {
+        float A[N], E[N];
+        load_state<MODE>(A, m + (int64_t)i * 2 * a.width, col, a.width);
+        load_state<MODE>(E, m + ((int64_t)i * 2 + 1) * a.width, col, a.width);
+#pragma unroll
+        for (int c = 0; c < N; ++c) e[c] = A[c] * e[c] + E[c];
+    }
+}
+
+// Maps of single tiles, for sequences whose tiles go to workgroups of their own; the state before the first step, or the gradient
+// behind the last, becomes a map that forgets what was before it.
+template <typename T, int W, int MODE, bool BACKWARD> __global__ __launch_bounds__(64 * W) void maps_kernel(params a) {
+    __shared__ wave_maps<W> lds;
+    const int tile = (int)(blockIdx.x % a.tiles);
+    const place p(a, blockIdx.x / a.tiles, MODE);
+    const int valid = within(length(a, p.b), tile);
+    const rows_t &in = BACKWARD ? a.dh : a.x;
+    values<T> g[R] = {}, v[R] = {};
+    if (valid > 0) {
+        load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
+        load_strip<T, MODE>(v, in, tile, p, valid, a.width);
+    }
+    float A[N], H[N];
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        A[c] = 1.f, H[c] = 0.f;
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+            const int r = BACKWARD ? R - 1 - k : k;
+            if (p.step + r < valid) {
+                float ga, gb;
+                gates((float)g[r][c], ga, gb);
+                A[c] *= ga;
+                H[c] = BACKWARD ? ga * ((float)v[r][c] + H[c]) : ga * H[c] + gb * (float)v[r][c];
+            }
+        }
+        float x = 0.f, y = 0.f, z = 0.f;
+        join<16, !BACKWARD, BACKWARD>(A[c], H[c], H[c], x, y, z, x, p.lane);
+        join<32, !BACKWARD, BACKWARD>(A[c], H[c], H[c], x, y, z, x, p.lane);
+        if (p.lane < ROW_LANES) {
+            lds[p.wave][0][p.lane * N + c] = A[c];
+            lds[p.wave][1][p.lane * N + c] = H[c];
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x >= ROW_LANES) return;
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        float sum_A = 1.f, sum_H = 0.f;
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            const int w = BACKWARD ? W - 1 - k : k;
+            const float wa = lds[w][0][p.lane * N + c];
+            sum_H = wa * sum_H + lds[w][1][p.lane * N + c];
+            sum_A *= wa;
+        }
+        A[c] = sum_A, H[c] = sum_H;
+    }
+    float *m = a.maps + p.b * (a.tiles + 1) * 2 * a.width;
+    const int at = BACKWARD ? tile : tile + 1;
+    store_state<MODE>(m + (int64_t)at * 2 * a.width, A, p.col, a.width);
+    store_state<MODE>(m + ((int64_t)at * 2 + 1) * a.width, H, p.col, a.width);
+    if (tile == (BACKWARD ? a.tiles - 1 : 0)) {
+        const float *first = BACKWARD ? a.dlast : a.state;
+        float s[N] = {};
+        if (first) load_state<MODE>(s, first + p.b * a.width, p.col, a.width);
+        store_state<MODE>(m + ((int64_t)(BACKWARD ? a.tiles : 0) * 2 + 1) * a.width, s, p.col, a.width);
+    }
+}
+
+// A workgroup of W waves takes the tiles of a sequence's CG channels one after another or, where maps of tiles are there (SHARED),
+// one tile.
+template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W) void recurrence_kernel(params a) {
+    __shared__ wave_maps<W> lds[SHARED ? 1 : 2];
+    const place p(a, SHARED ? blockIdx.x / a.tiles : blockIdx.x, MODE);
+    const int first = SHARED ? (int)(blockIdx.x % a.tiles) : 0, behind = SHARED ? first + 1 : a.tiles;
+    const int64_t end = length(a, p.b);
+    const bool speaks = threadIdx.x < ROW_LANES;  // stores states
+    float carry[N] = {};
+    if (SHARED) fold_before<MODE>(carry, a, p.b, first, p.col);
+    else if (a.state) load_state<MODE>(carry, a.state + p.b * a.width, p.col, a.width);
+#pragma clang loop unroll(disable)
+    for (int tile = first; tile < behind; ++tile) {
+        const int valid = within(end, tile), there = within(a.steps, tile);
+        if (speaks && a.kept) store_state<MODE>(a.kept + (p.b * a.tiles + tile) * a.width, carry, p.col, a.width);
+        values<T> g[R], x[R];
+        if (valid == 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) x[r] = values<T>{};
+            store_strip<T, MODE>(x, a.h, tile, p, there, a.width);
+            continue;
+        }
+        load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
+        load_strip<T, MODE>(x, a.x, tile, p, valid, a.width);
+        auto &maps = lds[SHARED ? 0 : tile & 1];
+        float ga[R][N], gx[R][N], before_A[N], before_H[N];
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            float A = 1.f, H = 0.f, none = 0.f;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float gb;
+                gates((float)g[r][c], ga[r][c], gb);
+                gx[r][c] = gb * (float)x[r][c];
+                if (p.step + r >= valid) ga[r][c] = 1.f, gx[r][c] = 0.f;  // the state stays
+                A *= ga[r][c];
+                H = ga[r][c] * H + gx[r][c];
+            }
+            before_A[c] = 1.f, before_H[c] = 0.f;
+            join<16, true, false>(A, H, none, before_A[c], before_H[c], none, none, p.lane);
+            join<32, true, false>(A, H, none, before_A[c], before_H[c], none, none, p.lane);
+            if (p.lane < ROW_LANES) {
+                maps[p.wave][0][p.lane * N + c] = A;
+                maps[p.wave][1][p.lane * N + c] = H;
+            }
+            __builtin_amdgcn_sched_barrier(0);  // one channel after another: together they take registers that waves could have
+        }
+        // two buffers: a wave that writes the next tile's maps has read these of the tile before
+        __syncthreads();
+        float s[N];
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                if (w == p.wave) s[c] = carry[c];
+                carry[c] = maps[w][0][p.lane % ROW_LANES * N + c] * carry[c] + maps[w][1][p.lane % ROW_LANES * N + c];
+            }
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] = before_A[c] * s[c] + before_H[c];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                s[c] = ga[r][c] * s[c] + gx[r][c];
+                x[r][c] = p.step + r < valid ? (T)s[c] : (T)0.f;
+            }
+        }
+        store_strip<T, MODE>(x, a.h, tile, p, there, a.width);
+    }
+    if (speaks && a.last && behind == a.tiles) store_state<MODE>(a.last + p.b * a.width, carry, p.col, a.width);
+}
+
+// As above, from the last tile to the first; the states before the tile's steps come from the kept one.
+template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W) void recurrence_backward_kernel(params a) {
+    __shared__ wave_maps<W> lds[SHARED ? 1 : 2];
+    const place p(a, SHARED ? blockIdx.x / a.tiles : blockIdx.x, MODE);
+    const int first = SHARED ? (int)(blockIdx.x % a.tiles) : 0, last = SHARED ? first : a.tiles - 1;
+    const int64_t end = length(a, p.b);
+    const bool speaks = threadIdx.x < ROW_LANES;
+    float carry[N] = {};
+    if (SHARED) fold_behind<MODE>(carry, a, p.b, last, p.col);
+    else if (a.dlast) load_state<MODE>(carry, a.dlast + p.b * a.width, p.col, a.width);
+#pragma clang loop unroll(disable)
+    for (int tile = last; tile >= first; --tile) {
+        const int valid = within(end, tile), there = within(a.steps, tile);
+        values<T> g[R], x[R], dh[R];
+        if (valid == 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) x[r] = values<T>{};
+            store_strip<T, MODE>(x, a.dx, tile, p, there, a.width);
+            store_strip<T, MODE>(x, a.dgate, tile, p, there, a.width);
+            continue;
+        }
+        load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
+        load_strip<T, MODE>(x, a.x, tile, p, valid, a.width);
+        load_strip<T, MODE>(dh, a.dh, tile, p, valid, a.width);
+        float s[N];
+        load_state<MODE>(s, a.kept + (p.b * a.tiles + tile) * a.width, p.col, a.width);
+        auto &maps = lds[SHARED ? 0 : tile & 1];
+        float before_A[N], before_H[N], behind_A[N], behind_E[N];
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            float A = 1.f, H = 0.f, E = 0.f, ga[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float gb;
+                gates((float)g[r][c], ga[r], gb);
+                float gx = gb * (float)x[r][c];
+                if (p.step + r >= valid) ga[r] = 1.f, gx = 0.f;
+                A *= ga[r];
+                H = ga[r] * H + gx;
+            }
+#pragma unroll
+            for (int r = R - 1; r >= 0; --r) E = ga[r] * ((p.step + r < valid ? (float)dh[r][c] : 0.f) + E);
+            before_A[c] = behind_A[c] = 1.f, before_H[c] = behind_E[c] = 0.f;
+            join<16, true, true>(A, H, E, before_A[c], before_H[c], behind_A[c], behind_E[c], p.lane);
+            join<32, true, true>(A, H, E, before_A[c], before_H[c], behind_A[c], behind_E[c], p.lane);
+            if (p.lane < ROW_LANES) {
+                maps[p.wave][0][p.lane * N + c] = A;
+                maps[p.wave][1][p.lane * N + c] = H;
+                maps[p.wave][2][p.lane * N + c] = E;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __syncthreads();
+        float e[N];
+#pragma unroll
+        for (int w = W - 1; w >= 0; --w)
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                if (w == p.wave) e[c] = carry[c];
+                carry[c] = maps[w][0][p.lane % ROW_LANES * N + c] * carry[c] + maps[w][2][p.lane % ROW_LANES * N + c];
+            }
+#pragma unroll
+        for (int w = 0; w < W - 1; ++w)
+            if (w < p.wave)
+#pragma unroll
+                for (int c = 0; c < N; ++c) s[c] = maps[w][0][p.lane % ROW_LANES * N + c] * s[c] + maps[w][1][p.lane % ROW_LANES * N + c];
+        // the gates are computed again, channel by channel: kept from above they would take 64 registers
+        values<T> dx[R], dg[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) asm("" : "+v"(g[r]), "+v"(x[r]), "+v"(dh[r]));
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            s[c] = before_A[c] * s[c] + before_H[c];
+            e[c] = behind_A[c] * e[c] + behind_E[c];
+            float ga[R], gb[R], q[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                gates((float)g[r][c], ga[r], gb[r]);
+                q[r] = (s[c] - (float)x[r][c]) * ga[r] * gb[r];
+                s[c] = ga[r] * s[c] + gb[r] * (float)x[r][c];  // (behind the last step not used)
+            }
+#pragma unroll
+            for (int r = R - 1; r >= 0; --r) {
+                const bool in = p.step + r < valid;
+                const float G = (float)dh[r][c] + e[c];
+                dx[r][c] = in ? (T)(gb[r] * G) : (T)0.f;
+                dg[r][c] = in ? (T)(q[r] * G) : (T)0.f;
+                e[c] = in ? ga[r] * G : e[c];
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        store_strip<T, MODE>(dx, a.dx, tile, p, there, a.width);
+        store_strip<T, MODE>(dg, a.dgate, tile, p, there, a.width);
+    }
+    if (speaks && a.dstate && first == 0) store_state<MODE>(a.dstate + p.b * a.width, carry, p.col, a.width);
+}
+
+// ------------------------------------------------------------------------------------ host
+constexpr int64_t MAX_STEPS = (int64_t)1 << 30;
+constexpr int32_t MAX_WIDTH = 1 << 24;
+constexpr int64_t MAX_STEP_STRIDE = 1 << 22;  // so that 32 bits reach the rows of a tile
+
+int size_of(int32_t dtype) { return dtype == DEAR_BF16 ? 2 : 4; }
+
+// Channels of a workgroup.
+int64_t groups_of(const dear_recurrence_t &r) { return ceil_div(r.width, CG); }
+
+// Whether the tiles of a sequence go to workgroups of their own, which takes a launch more and reads the inputs twice (backward two of
+// three): where there are several tiles and the sequences' channels alone do not fill the chip.
+bool shares(const dear_recurrence_t &r) { return r.steps > KEPT && r.batch * groups_of(r) < 512; }
+
+int check(const dear_recurrence_t *r) {
+    if (!r || (r->dtype != DEAR_F32 && r->dtype != DEAR_BF16) || r->batch < 0 || r->steps < 0 || r->steps > MAX_STEPS) return DEAR_EINVAL;
+    if (r->width < 1 || r->width > MAX_WIDTH || r->reserved != 0) return DEAR_EINVAL;
+    return DEAR_OK;
+}
+
+// A tensor of the structure, which is read or, where it is written, has a place of its own for each element.
+int check_tensor(const dear_recurrence_t &r, const dear_steps_t &t, bool written) {
+    if (!t.data || t.batch_stride < 0 || t.step_stride < 0) return DEAR_EINVAL;
+    if (r.steps > 1 && t.step_stride >= MAX_STEP_STRIDE) return DEAR_ETOOBIG;
+    if (written) {
+        const int64_t batch = r.batch, steps = r.steps;
+        const bool by_batch = t.batch_stride >= t.step_stride;  // which of the axes lies further apart
+        const int64_t inner = by_batch ? t.step_stride : t.batch_stride, outer = by_batch ? t.batch_stride : t.step_stride;
+        const int64_t inner_n = by_batch ? steps : batch, outer_n = by_batch ? batch : steps;
+        int64_t span = r.width;
+        if (inner_n > 1) {
+            if (inner < span) return DEAR_EINVAL;
+            if (inner > (INT64_MAX - span) / inner_n) return DEAR_EINVAL;
+            span += (inner_n - 1) * inner;
+        }
+        if (outer_n > 1 && outer < span) return DEAR_EINVAL;
+    }
+    return aligned(t.data, size_of(r.dtype)) ? DEAR_OK : DEAR_EALIGN;
+}
+
+int64_t workspace_of(const dear_recurrence_t &r) {
+    return r.batch && shares(r) ? (int64_t)r.batch * (ceil_div(r.steps, KEPT) + 1) * 2 * r.width * 4 : 0;
+}
+
+bool vectors(const dear_recurrence_t &r, const dear_steps_t &t) {
+    const int n = size_of(r.dtype);
+    return aligned(t.data, N * n) && t.batch_stride % N == 0 && t.step_stride % N == 0;
+}
+
+int check_call(const dear_recurrence_t *r, bool backward) {
+    if (int rc = check(r)) return rc;
+    if (r->batch == 0) return DEAR_OK;
+    if (!aligned(r->lens, 4) || !aligned(r->state, 4) || !aligned(r->last, 4) || !aligned(r->kept, 4) || !aligned(r->dlast, 4) ||
+        !aligned(r->dstate, 4))
+        return DEAR_EALIGN;
+    if (r->steps > 0) {
+        if (backward && !r->kept) return DEAR_EINVAL;
+        if (int rc = check_tensor(*r, r->x, false)) return rc;
+        if (int rc = check_tensor(*r, r->gate, false)) return rc;
+        if (!backward)
+            if (int rc = check_tensor(*r, r->h, true)) return rc;
+        if (backward) {
+            if (int rc = check_tensor(*r, r->dh, false)) return rc;
+            if (int rc = check_tensor(*r, r->dx, true)) return rc;
+            if (int rc = check_tensor(*r, r->dgate, true)) return rc;
+        }
+        const int64_t need = workspace_of(*r);
+        if (need && !r->workspace) return DEAR_EINVAL;
+        if (need && !aligned(r->workspace, 256)) return DEAR_EALIGN;
+        if (need > r->workspace_bytes) return DEAR_ETOOBIG;
+        if (r->batch * groups_of(*r) * (shares(*r) ? ceil_div(r->steps, KEPT) : 1) * 64 * WAVES > MAX_THREADS) return DEAR_ETOOBIG;
+    }
+    return DEAR_OK;
+}
+
+// The state of sequences without steps.
+__global__ __launch_bounds__(256) void copy_state_kernel(const float *from, float *to, int64_t n) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) to[i] = from ? from[i] : 0.f;
+}
+
+template <typename T, int MODE, bool BACKWARD> void launch(const params &a, int64_t groups, bool shared, hipStream_t stream) {
+    auto by_waves = [&](auto waves) {
+        constexpr int W = decltype(waves)::value;
+        if (BACKWARD) recurrence_backward_kernel<T, W, MODE, false><<<(unsigned)groups, 64 * W, 0, stream>>>(a);
+        else recurrence_kernel<T, W, MODE, false><<<(unsigned)groups, 64 * W, 0, stream>>>(a);
+    };
+    if (shared) {
+        constexpr int W = WAVES;
+        const unsigned n = (unsigned)(groups * a.tiles);
+        maps_kernel<T, W, MODE, BACKWARD><<<n, 64 * W, 0, stream>>>(a);
+        if (BACKWARD) recurrence_backward_kernel<T, W, MODE, true><<<n, 64 * W, 0, stream>>>(a);
+        else recurrence_kernel<T, W, MODE, true><<<n, 64 * W, 0, stream>>>(a);
+    } else if (a.steps <= WAVE_STEPS) {
+        by_waves(std::integral_constant<int, 1>());
+    } else if (a.steps <= 3 * WAVE_STEPS) {
+        by_waves(std::integral_constant<int, 3>());
+    } else {
+        by_waves(std::integral_constant<int, WAVES>());
+    }
+}
+
+int call(const dear_recurrence_t *r, bool backward, hipStream_t stream) {
+    if (int rc = check_call(r, backward)) return rc;
+    if (r->batch == 0) return DEAR_OK;
+    if (r->steps == 0) {
+        const float *from = backward ? r->dlast : r->state;
+        float *to = backward ? r->dstate : r->last;
+        const int64_t n = (int64_t)r->batch * r->width;
+        if (!to || to == from) return DEAR_OK;
+        if (n > MAX_THREADS) return DEAR_ETOOBIG;
+        copy_state_kernel<<<(unsigned)ceil_div(n, 256), 256, 0, stream>>>(from, to, n);
+        return launch_status();
+    }
+    auto rows = [](const dear_steps_t &t) { return rows_t{t.data, t.batch_stride, t.step_stride}; };
+    params a = {};
+    a.x = rows(r->x), a.gate = rows(r->gate), a.h = rows(r->h), a.dh = rows(r->dh), a.dx = rows(r->dx), a.dgate = rows(r->dgate);
+    a.state = r->state, a.dlast = r->dlast, a.last = r->last, a.dstate = r->dstate, a.kept = r->kept, a.lens = r->lens;
+    a.maps = (float *)r->workspace, a.steps = r->steps, a.width = r->width;
+    const int64_t groups = groups_of(*r) * r->batch;
+    a.groups = (int32_t)groups_of(*r), a.tiles = (int32_t)ceil_div(r->steps, KEPT);
+    bool vec = r->width % N == 0 && vectors(*r, r->x) && vectors(*r, r->gate);
+    vec = vec && (backward ? vectors(*r, r->dh) && vectors(*r, r->dx) && vectors(*r, r->dgate) : vectors(*r, r->h));
+    vec = vec && aligned(r->state, 16) && aligned(r->last, 16) && aligned(r->kept, 16) && aligned(r->dlast, 16) && aligned(r->dstate, 16);
+    auto by_mode = [&](auto t, auto mode) {
+        typedef decltype(t) T;
+        if (backward) launch<T, decltype(mode)::value, true>(a, groups, shares(*r), stream);
+        else launch<T, decltype(mode)::value, false>(a, groups, shares(*r), stream);
+    };
+    auto by_type = [&](auto t) {
+        if (vec) by_mode(t, std::integral_constant<int, ALIGNED>());
+        else if (r->width >= N) by_mode(t, std::integral_constant<int, ANYWHERE>());
+        else by_mode(t, std::integral_constant<int, SINGLE>());
+    };
+    if (r->dtype == DEAR_BF16) by_type(bf16());
+    else by_type(float());
+    return launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+int dear_recurrence(const dear_recurrence_t *args, void *hip_stream) { return call(args, false, (hipStream_t)hip_stream); }
+
+int dear_recurrence_backward(const dear_recurrence_t *args, void *hip_stream) { return call(args, true, (hipStream_t)hip_stream); }
+
+int dear_recurrence_workspace(const dear_recurrence_t *args, int64_t *bytes) {
+    if (!bytes) return DEAR_EINVAL;
+    if (int rc = check(args)) return rc;
+    *bytes = workspace_of(*args);
+    return DEAR_OK;
+}
+
+}  // extern "C"

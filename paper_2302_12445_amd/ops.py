@@ -6,6 +6,11 @@
     dx, dweight = add_rms_norm_backward(dy, h, weight, rstd, dh=dh)
     kept = checkpoint_encode(x); x = checkpoint_decode(kept, dtype)
     dw = checkpoint_weight_grad(dy, kept)                            # fp32 [outs, ins]
+    h, last, kept = recurrence(x, gate, state)                       # [B, T, C]; last: fp32 [B, C]
+    dx, dgate, dstate = recurrence_backward(dh, x, gate, kept)
+    y = expert_linear(x, weight, ends)                               # rows sorted by expert; weight [E, outs, ins]
+    dx, dw = expert_input_grad(dy, weight, ends), expert_weight_grad(dy, x, ends)
+    norm = clip_grads(grads, max_norm)                               # of all tensors of a list, in place; grad_norm(grads)
 
 Tensors are on a GPU, bf16 or fp32.  Work is enqueued on the current torch stream of the tensors'
 device; outputs and workspaces come from torch's allocator.  Wrong arguments raise ValueError or
@@ -19,7 +24,7 @@ import functools
 import math
 import os
 import struct
-from typing import NamedTuple, Optional, Tuple
+from typing import NamedTuple, Optional, Sequence, Tuple
 
 import torch
 
@@ -29,11 +34,16 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdear_ops.so")
 GROUP = 32  # DEAR_CHECKPOINT_GROUP
 NORM_MAX_COLS = 32768
+KEPT = 256  # DEAR_RECURRENCE_KEPT
 
 EXPORTS = [
     "dear_attention", "dear_attention_workspace", "dear_attention_backward", "dear_attention_backward_workspace",
     "dear_checkpoint_encode", "dear_checkpoint_decode", "dear_checkpoint_weight_grad", "dear_checkpoint_weight_grad_workspace",
     "dear_add_rms_norm", "dear_add_rms_norm_backward", "dear_add_rms_norm_backward_workspace",
+    "dear_recurrence", "dear_recurrence_backward", "dear_recurrence_workspace",
+    "dear_expert_linear", "dear_expert_input_grad", "dear_expert_weight_grad", "dear_expert_linear_workspace",
+    "dear_expert_input_grad_workspace", "dear_expert_weight_grad_workspace",
+    "dear_grad_norm", "dear_clip_grads", "dear_grad_norm_workspace",
 ]
 
 _DTYPE = {torch.bfloat16: DEAR_BF16, torch.float32: DEAR_F32}
@@ -50,11 +60,16 @@ def load_library() -> C.CDLL:
     lib = C.CDLL(LIB_PATH)
     vp, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
     out64 = C.POINTER(i64)
-    # dear_attention_t is passed as the bytes that struct packs
-    lib.dear_attention.argtypes = [C.c_char_p, vp]
-    lib.dear_attention_backward.argtypes = [C.c_char_p, vp]
-    lib.dear_attention_workspace.argtypes = [C.c_char_p, out64]
-    lib.dear_attention_backward_workspace.argtypes = [C.c_char_p, out64]
+    # structures are passed as the bytes that struct packs
+    for name in ("dear_attention", "dear_attention_backward", "dear_recurrence", "dear_recurrence_backward", "dear_expert_linear",
+                 "dear_expert_input_grad", "dear_expert_weight_grad"):
+        getattr(lib, name).argtypes = [C.c_char_p, vp]
+    for name in ("dear_attention_workspace", "dear_attention_backward_workspace", "dear_recurrence_workspace",
+                 "dear_expert_linear_workspace", "dear_expert_input_grad_workspace", "dear_expert_weight_grad_workspace"):
+        getattr(lib, name).argtypes = [C.c_char_p, out64]
+    lib.dear_grad_norm.argtypes = [C.c_char_p, i64, vp, vp, i64, vp]
+    lib.dear_clip_grads.argtypes = [C.c_char_p, i64, f32, vp, vp, i64, vp]
+    lib.dear_grad_norm_workspace.argtypes = [i64, out64]
     lib.dear_checkpoint_encode.argtypes = [vp, i32, i64, i64, i64, vp, vp, vp]
     lib.dear_checkpoint_decode.argtypes = [vp, vp, i64, i64, i32, vp, vp]
     lib.dear_checkpoint_weight_grad.argtypes = [vp, i32, i64, vp, vp, i64, i64, i64, vp, vp, i64, vp]
@@ -101,6 +116,14 @@ def _elsewhere(t: torch.Tensor) -> bool:
 def _attention_workspace(name: str, *head) -> int:
     need = C.c_int64()
     _check(getattr(load_library(), name)(_ATTENTION.pack(*head, *([0] * 37)), C.byref(need)), name)
+    return need.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _packed_workspace(name: str, layout: struct.Struct, members: int, *head) -> int:
+    """Bytes that a call with a structure of these leading members needs."""
+    need = C.c_int64()
+    _check(getattr(load_library(), name)(layout.pack(*head, *([0] * (members - len(head)))), C.byref(need)), name)
     return need.value
 
 
@@ -379,3 +402,266 @@ def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tenso
         rstd.data_ptr(), d, rows, cols, dx.data_ptr(), dweight.data_ptr(), space.data_ptr(), need, _raw_stream(dy.get_device())),
         "dear_add_rms_norm_backward")
     return dx, dweight
+
+
+# ------------------------------------------------------------------------------------ recurrence
+# dear_recurrence_t
+_RECURRENCE = struct.Struct("@2iq2iQ" + "Q2q" * 2 + "2Q" + "Q2q" + "Q" + "Q2q" + "Q" + "Q2q" * 2 + "2Qq")
+_RECURRENCE_MEMBERS = 6 + 6 + 2 + 3 + 1 + 3 + 1 + 6 + 3
+_MAX_STEP_STRIDE = 1 << 22
+_NO_STEPS = (0, 0, 0)
+
+
+def _steps(t: torch.Tensor, what: str):
+    """The tensor, or a copy of it that the library can read (channels contiguous), and its address and strides, those along axes
+    of one element, which say nothing, as 0."""
+    n = t.shape
+    if len(n) != 3 or n[2] < 1:
+        raise ValueError("%s has shape %s, expected [batch, steps, channels]" % (what, tuple(n)))
+    s = t.stride()
+    batch, step = s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0
+    if (s[2] != 1 and n[2] > 1) or step >= _MAX_STEP_STRIDE:
+        t = t.clone(memory_format=torch.contiguous_format)
+        batch, step = n[1] * n[2] if n[0] > 1 else 0, n[2] if n[1] > 1 else 0
+    return t, (t.data_ptr(), batch, step)
+
+
+def _new_steps(like: torch.Tensor):
+    t = _empty_as(like)
+    n = t.shape
+    return t, (t.data_ptr(), n[1] * n[2], n[2])
+
+
+def _state(t: Optional[torch.Tensor], shape, device, what: str) -> int:
+    """The address of fp32 values of the shape, 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype != torch.float32 or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s: expected a contiguous float32 tensor of shape %s on %s" % (what, tuple(shape), device))
+    return t.data_ptr()
+
+
+def _recurrence_sizes(x, gate, lens):
+    """(x, gate) as the library reads them, their places, and the leading members of dear_recurrence_t."""
+    d = _dtype(x, "x")
+    _like(gate, x, "gate")
+    if gate.shape != x.shape:
+        raise ValueError("gate has shape %s, x %s" % (tuple(gate.shape), tuple(x.shape)))
+    (x, px), (gate, pg) = _steps(x, "x"), _steps(gate, "gate")
+    B, T, channels = x.shape
+    if lens is not None and (lens.dtype != torch.int32 or lens.device != x.device or lens.shape != (B,) or not lens.is_contiguous()):
+        raise ValueError("lens: expected a contiguous int32 tensor of %d on %s" % (B, x.device))
+    return (x, gate), (*px, *pg), (B, channels, T, d, 0, 0 if lens is None else lens.data_ptr())
+
+
+def _recurrence_space(head, device):
+    need = _packed_workspace("dear_recurrence_workspace", _RECURRENCE, _RECURRENCE_MEMBERS, *head[:5])
+    space = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    return space, space.data_ptr() if need else 0, need
+
+
+def recurrence(x: torch.Tensor, gate: torch.Tensor, state: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None,
+               keep: bool = True) -> Tuple[torch.Tensor, torch.Tensor, Optional[torch.Tensor]]:
+    """Gated linear recurrence s[t] = a * s[t-1] + (1 - a) * x[t] with a = sigmoid(gate[t]), channel by channel, of x and gate [B, T, C].
+
+    Gives (h, last, kept): h[t] = s[t], of x's type; last fp32 [B, C], the state behind the last step, which a call on the next steps
+    (one token, or many) takes as `state`; kept fp32 [B, ceil(T / 256), C] for recurrence_backward (None without `keep`).
+    state: fp32 [B, C] before the first step, zeros by default.  lens: int32 [B], the valid steps of each sequence; behind them h is 0.
+    """
+    if _elsewhere(x):
+        with torch.cuda.device(x.device):
+            return recurrence(x, gate, state, lens, keep)
+    held, places, head = _recurrence_sizes(x, gate, lens)  # held: until the work is enqueued
+    B, channels, T = head[:3]
+    at = _state(state, (B, channels), x.device, "state")
+    h, ph = _new_steps(x)
+    last = torch.empty((B, channels), dtype=torch.float32, device=x.device)
+    kept = torch.empty((B, -(-T // KEPT), channels), dtype=torch.float32, device=x.device) if keep else None
+    space, space_at, need = _recurrence_space(head, x.device)
+    packed = _RECURRENCE.pack(*head, *places, at, kept.data_ptr() if keep else 0, *ph, last.data_ptr(), *_NO_STEPS, 0, *_NO_STEPS, *_NO_STEPS, 0,
+                              space_at, need)
+    _check(load_library().dear_recurrence(packed, _raw_stream(x.get_device())), "dear_recurrence")
+    return h, last, kept
+
+
+def recurrence_backward(dh: torch.Tensor, x: torch.Tensor, gate: torch.Tensor, kept: torch.Tensor, lens: Optional[torch.Tensor] = None,
+                        dlast: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Gradients (dx, dgate, dstate) from the gradient of h, what recurrence() kept, and its arguments; dstate is fp32 [B, C], of the state
+    before the first step.  dlast: fp32 [B, C], the gradient of last."""
+    if _elsewhere(dh):
+        with torch.cuda.device(dh.device):
+            return recurrence_backward(dh, x, gate, kept, lens, dlast)
+    held, places, head = _recurrence_sizes(x, gate, lens)
+    B, channels, T = head[:3]
+    _like(dh, x, "dh")
+    if dh.shape != x.shape:
+        raise ValueError("dh has shape %s, x %s" % (tuple(dh.shape), tuple(x.shape)))
+    dh, pd = _steps(dh, "dh")
+    kept_at = _state(kept, (B, -(-T // KEPT), channels), x.device, "kept")
+    dlast_at = _state(dlast, (B, channels), x.device, "dlast")
+    (dx, px), (dgate, pg) = _new_steps(x), _new_steps(gate)
+    dstate = torch.empty((B, channels), dtype=torch.float32, device=x.device)
+    space, space_at, need = _recurrence_space(head, x.device)
+    packed = _RECURRENCE.pack(*head, *places, 0, kept_at, *_NO_STEPS, 0, *pd, dlast_at, *px, *pg, dstate.data_ptr(), space_at, need)
+    _check(load_library().dear_recurrence_backward(packed, _raw_stream(x.get_device())), "dear_recurrence_backward")
+    return dx, dgate, dstate
+
+
+# ------------------------------------------------------------------------------------ experts
+# dear_experts_t
+_EXPERTS = struct.Struct("@q4i2Qq2Qq2Qq")
+_EXPERTS_MEMBERS = 14
+
+
+def _expert_rows(t: torch.Tensor, what: str):
+    if t.dim() != 2:
+        raise ValueError("%s has shape %s, expected [rows, width]" % (what, tuple(t.shape)))
+    return _as_rows(t, what)
+
+
+def _expert_ends(ends: torch.Tensor, experts: int, device) -> None:
+    if ends.dtype != torch.int32 or ends.device != device or ends.shape != (experts,) or not ends.is_contiguous():
+        raise ValueError("ends: expected a contiguous int32 tensor of %d on %s" % (experts, device))
+
+
+def _expert_weight(weight: torch.Tensor, rows: torch.Tensor, axis: int, what: str) -> torch.Tensor:
+    """A weight [experts, outs, ins] that rows are multiplied with along one of its axes."""
+    _like(weight, rows, "weight")
+    if weight.dim() != 3 or weight.shape[axis] != rows.shape[1]:
+        raise ValueError("weight has shape %s, %s %s" % (tuple(weight.shape), what, tuple(rows.shape)))
+    return weight.contiguous()
+
+
+def _expert_call(name: str, head, ends, x, x_stride, weight, dy, dy_stride, out) -> None:
+    need, space = _packed_workspace(name + "_workspace", _EXPERTS, _EXPERTS_MEMBERS, *head), None
+    if need:
+        space = torch.empty(need, dtype=torch.uint8, device=out.device)
+    packed = _EXPERTS.pack(*head, ends.data_ptr(), x, x_stride, weight, dy, dy_stride, out.data_ptr(), space.data_ptr() if need else 0, need)
+    _check(getattr(load_library(), name)(packed, _raw_stream(out.get_device())), name)
+
+
+def expert_linear(x: torch.Tensor, weight: torch.Tensor, ends: torch.Tensor) -> torch.Tensor:
+    """y [rows, outs] of x [rows, ins], sorted by expert, and weight [experts, outs, ins]: expert e has the rows ends[e-1] .. ends[e] - 1.
+
+    ends: int32 [experts], on the GPU; an expert may have no rows, and rows behind the last one's are 0 in y.
+    """
+    if _elsewhere(x):
+        with torch.cuda.device(x.device):
+            return expert_linear(x, weight, ends)
+    d = _dtype(x, "x")
+    r, rows, ins, stride = _expert_rows(x, "x")
+    w = _expert_weight(weight, x, 2, "x")
+    experts, outs = w.shape[:2]
+    _expert_ends(ends, experts, x.device)
+    y = torch.empty((rows, outs), dtype=x.dtype, device=x.device)
+    _expert_call("dear_expert_linear", (rows, experts, outs, ins, d), ends, r.data_ptr(), stride, w.data_ptr(), 0, 0, y)
+    return y
+
+
+def expert_input_grad(dy: torch.Tensor, weight: torch.Tensor, ends: torch.Tensor) -> torch.Tensor:
+    """Gradient [rows, ins] of expert_linear's x from that of its y."""
+    if _elsewhere(dy):
+        with torch.cuda.device(dy.device):
+            return expert_input_grad(dy, weight, ends)
+    d = _dtype(dy, "dy")
+    r, rows, outs, stride = _expert_rows(dy, "dy")
+    w = _expert_weight(weight, dy, 1, "dy")
+    experts, _, ins = w.shape
+    _expert_ends(ends, experts, dy.device)
+    dx = torch.empty((rows, ins), dtype=dy.dtype, device=dy.device)
+    _expert_call("dear_expert_input_grad", (rows, experts, outs, ins, d), ends, 0, 0, w.data_ptr(), r.data_ptr(), stride, dx)
+    return dx
+
+
+def expert_weight_grad(dy: torch.Tensor, x: torch.Tensor, ends: torch.Tensor) -> torch.Tensor:
+    """Gradient [experts, outs, ins] in fp32 of expert_linear's weight from x and the gradient of y."""
+    if _elsewhere(dy):
+        with torch.cuda.device(dy.device):
+            return expert_weight_grad(dy, x, ends)
+    d = _dtype(dy, "dy")
+    _like(x, dy, "x")
+    ry, rows, outs, dy_stride = _expert_rows(dy, "dy")
+    rx, x_rows, ins, x_stride = _expert_rows(x, "x")
+    if x_rows != rows:
+        raise ValueError("dy has %d rows, x %d" % (rows, x_rows))
+    experts = ends.numel()
+    _expert_ends(ends, experts, dy.device)
+    dw = torch.empty((experts, outs, ins), dtype=torch.float32, device=dy.device)
+    _expert_call("dear_expert_weight_grad", (rows, experts, outs, ins, d), ends, rx.data_ptr(), x_stride, 0, ry.data_ptr(), dy_stride, dw)
+    return dw
+
+
+# ------------------------------------------------------------------------------------ gradients
+_GRAD_MEMBERS = "2Qq2i"  # dear_grad_t
+
+
+@functools.lru_cache(maxsize=256)
+def _grad_layout(count: int) -> struct.Struct:
+    return struct.Struct("@" + _GRAD_MEMBERS * count)
+
+
+def _dense(t: torch.Tensor) -> bool:
+    """Whether the elements fill one stretch of memory, in whatever order of axes."""
+    if t.is_contiguous():
+        return True
+    span = 1
+    for stride, n in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != span:
+            return False
+        span *= n
+    return True
+
+
+def _grad_norm(tensors: Sequence[torch.Tensor], out: Optional[Sequence[torch.Tensor]], max_norm: Optional[float]) -> torch.Tensor:
+    tensors = list(tensors)
+    if not tensors:
+        raise ValueError("no tensors")
+    clip = max_norm is not None
+    outs = tensors if out is None else list(out)
+    if len(outs) != len(tensors):
+        raise ValueError("%d tensors and %d outputs" % (len(tensors), len(outs)))
+    device, members, held = tensors[0].device, [], []
+    if tensors[0].is_cuda and tensors[0].get_device() != _current_device():
+        with torch.cuda.device(device):
+            return _grad_norm(tensors, out, max_norm)
+    for g, o in zip(tensors, outs):
+        d, od = _dtype(g, "a gradient"), _dtype(o, "an output")
+        if g.device != device or o.device != device:
+            raise ValueError("tensors are on %s, %s and %s" % (device, g.device, o.device))
+        if o.shape != g.shape:
+            raise ValueError("an output has shape %s, its gradient %s" % (tuple(o.shape), tuple(g.shape)))
+        if clip and not _dense(o):
+            raise ValueError("an output of shape %s and strides %s has gaps" % (tuple(o.shape), o.stride()))
+        if (o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous())) or not _dense(g):
+            g = torch.empty_strided(o.shape, o.stride(), dtype=g.dtype, device=device).copy_(g) if clip else g.contiguous()
+            held.append(g)
+        members += (g.data_ptr(), o.data_ptr(), g.numel(), d, od)
+    lib, count = load_library(), len(tensors)
+    norm = torch.empty((), dtype=torch.float32, device=device)
+    need = _workspace("dear_grad_norm_workspace", count)
+    space = torch.empty(need, dtype=torch.uint8, device=device)
+    packed, stream = _grad_layout(count).pack(*members), _raw_stream(norm.get_device())
+    if clip:
+        _check(lib.dear_clip_grads(packed, count, max_norm, norm.data_ptr(), space.data_ptr(), need, stream), "dear_clip_grads")
+        for o in outs:
+            torch.autograd.graph.increment_version(o)
+    else:
+        _check(lib.dear_grad_norm(packed, count, norm.data_ptr(), space.data_ptr(), need, stream), "dear_grad_norm")
+    return norm
+
+
+def grad_norm(tensors: Sequence[torch.Tensor]) -> torch.Tensor:
+    """The norm over all elements of the tensors (bf16 or fp32, also both), fp32, on their GPU."""
+    return _grad_norm(tensors, None, None)
+
+
+def clip_grads(tensors: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
+    """Scales the tensors by min(1, max_norm / norm), with norm that over all of them, and gives norm.
+
+    In place, or into `out`: tensors of the same shapes, bf16 or fp32 each, so that fp32 gradients can be had of bf16 ones.  Nothing is
+    written that need not change.  The norm stays on the GPU: nothing waits for it.
+    """
+    max_norm = float(max_norm)
+    if not max_norm > 0:
+        raise ValueError("max_norm %g: expected a number above 0" % max_norm)
+    return _grad_norm(tensors, out, max_norm)

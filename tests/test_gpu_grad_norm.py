@@ -1,0 +1,171 @@
+"""GPU: the norm over many gradients and clipping against their definitions in 64 bits; bounds as derived in
+recurrent_reference.py."""
+from __future__ import annotations
+
+import math
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import ops_reference as ref  # noqa: E402
+import recurrent_reference as rec  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def ops():
+    from paper_2302_12445_amd import ops as m
+    m.load_library()
+    return m
+
+
+def normal(gen, shape, dtype=F32, scale=1.0):
+    return (torch.randn(shape, generator=gen) * scale).to(dtype).to(DEV)
+
+
+def check(ops, grads, max_norm, out=None):
+    want, wants, off, offs = rec.clip(grads, max_norm, [t.dtype for t in (out or grads)])
+    ref.within(ops.grad_norm(grads), want, off, "norm")
+    before = [g.clone() for g in grads]
+    norm = ops.clip_grads(grads, max_norm, out)
+    assert norm.shape == () and norm.dtype == F32
+    ref.within(norm, want, off, "norm of clip")
+    for n, (g, w, o) in enumerate(zip(out or grads, wants, offs)):
+        ref.within(g, w, o, "tensor %d" % n)
+    if out is not None or not norm > max_norm:
+        assert all(torch.equal(a, b) for a, b in zip(grads, before))
+    return norm
+
+
+LISTS = [[1], [5], [0, 3, 0], [2048], [2049, 1, 7], [4096, 4095, 3], [1023, 1, 1025] * 20, list(range(1, 330)), [1 << 20, 17, 300001], [7] * 700]
+
+
+@pytest.mark.parametrize("max_norm", [0.5, 1e9])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("sizes", range(len(LISTS)))
+def test_lists(ops, sizes, dtype, max_norm):
+    print("case", sizes, dtype, max_norm, flush=True)
+    gen = torch.Generator().manual_seed(sizes)
+    check(ops, [normal(gen, (n,), dtype) for n in LISTS[sizes]], max_norm)
+
+
+@pytest.mark.parametrize("max_norm", [0.5, 1e9])
+def test_types_and_outputs(ops, max_norm):
+    """Both types in one list, each into either, tensors that start anywhere, what lies between them left as it is."""
+    gen = torch.Generator().manual_seed(3)
+    grads, outs, guards = [], [], []
+    for n in (1, 3, 8, 9, 1000, 4099, 70000):
+        for t in (BF16, F32):
+            for o in (BF16, F32):
+                buffer = torch.full((n + 9,), 7.0, dtype=o, device=DEV)
+                grads.append(normal(gen, (n + 3,), t)[3:])
+                outs.append(buffer[5:5 + n])
+                guards.append(buffer)
+    check(ops, grads, max_norm, outs)
+    for b in guards:
+        assert (b[:5] == 7).all() and (b[-4:] == 7).all()
+
+
+def test_shapes_and_orders(ops):
+    """Tensors in other orders of their axes in place; slices with gaps as inputs, refused as outputs."""
+    gen = torch.Generator().manual_seed(4)
+    turned, last = normal(gen, (30, 50)).t(), normal(gen, (2, 3, 8, 8)).to(memory_format=torch.channels_last)
+    check(ops, [turned, last, normal(gen, ())], 0.5)
+    gaps = normal(gen, (40, 64))[:, :50]
+    check(ops, [gaps, turned], 0.5, [torch.empty(40, 50, device=DEV), torch.empty_like(turned)])
+    check(ops, [gaps, turned], 0.5, [torch.empty(50, 40, device=DEV).t(), torch.empty(50, 30, device=DEV)])
+    check(ops, [torch.ones((), device=DEV).expand(7, 5)], 0.5, [torch.empty(7, 5, device=DEV)])
+    with pytest.raises(ValueError):
+        ops.clip_grads([gaps], 0.5)
+
+
+def test_places_that_are_shared_are_refused(ops):
+    from paper_2302_12445_amd import DearError
+    t = normal(torch.Generator().manual_seed(5), (100,))
+    before = t.clone()
+    for grads, out in (([t, t], None), ([t[:60], t[50:]], None), ([t[:50], t[50:]], [t[50:], t[:50]]), ([t[:50]], [t[1:51]]),
+                       ([t[:50]], [t.view(BF16)[:50]])):
+        with pytest.raises(DearError):
+            ops.clip_grads(grads, 0.5, out)
+    assert torch.equal(t, before)
+    ref.within(ops.grad_norm([t, t]), torch.sqrt(2 * (ref.f64(t) ** 2).sum()), torch.tensor(1e-5), "a tensor twice")
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-22, 1e18, 1e30, 3e38])
+def test_magnitudes(ops, scale):
+    """Squares that fp32 does not hold."""
+    g = torch.tensor([1.0, -0.5, 0.25, 0.0] * 500, device=DEV) * scale
+    check(ops, [g], scale / 8)
+
+
+def test_not_finite(ops):
+    gen = torch.Generator().manual_seed(6)
+    a, b = normal(gen, (5000,)), normal(gen, (300,), BF16)
+    b[7] = math.nan
+    assert torch.isnan(ops.grad_norm([a, b])) and torch.isnan(ops.clip_grads([a, b], 1.0))
+    assert torch.isnan(a).all() and torch.isnan(b.float()).all()
+    a, b = normal(gen, (5000,)), normal(gen, (300,), BF16)
+    b[7] = -math.inf
+    assert ops.clip_grads([a, b], 1.0) == math.inf
+    assert not a.any() and torch.isnan(b[7]) and not b[:7].any() and not b[8:].any()
+    c = normal(gen, (5000,))
+    before = c.clone()
+    ops.clip_grads([c], math.inf)
+    assert torch.equal(c, before)
+
+
+def test_clipped_twice(ops):
+    """What is clipped has the largest norm, but for rounding, and a second time changes by no more than a rounding."""
+    g = [normal(torch.Generator().manual_seed(7), (n,)) for n in (10000, 30)]
+    ops.clip_grads(g, 2.0)
+    norm = ops.grad_norm(g)
+    assert abs(norm.item() - 2.0) < 2.0 * 2 ** -22
+    before = [t.clone() for t in g]
+    ops.clip_grads(g, 2.0)
+    for t, b in zip(g, before):
+        assert torch.allclose(t, b, rtol=2 ** -22, atol=0)
+
+
+def test_noticed_by_autograd(ops):
+    """A tensor that a backward pass needs and that was clipped in place."""
+    x = torch.ones(10, device=DEV, requires_grad=True)
+    y = x * 2
+    z = y * y
+    ops.clip_grads([y.detach()], 0.5)
+    with pytest.raises(RuntimeError):
+        z.sum().backward()
+
+
+def test_same_bits_again_and_in_a_graph(ops):
+    gen = torch.Generator().manual_seed(8)
+    grads = [normal(gen, (n,)) for n in (300001, 5, 70000)] + [normal(gen, (9999,), BF16)]
+    out = [torch.empty(g.shape, device=DEV) for g in grads]
+    norm = ops.clip_grads(grads, 1.0, out)
+    first = [o.clone() for o in out]
+    assert torch.equal(ops.clip_grads(grads, 1.0, out), norm) and all(torch.equal(a, b) for a, b in zip(out, first))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        n = ops.clip_grads(grads, 1.0, out)
+    for scale in (0.5, 1e-4, 3.0):
+        for g in grads:
+            g.copy_(normal(gen, g.shape, g.dtype, scale))
+        graph.replay()
+        eager = [torch.empty_like(o) for o in out]
+        want = ops.clip_grads(grads, 1.0, eager)
+        torch.cuda.synchronize()
+        assert torch.equal(n, want) and all(torch.equal(a, b) for a, b in zip(out, eager))
+
+
+def test_far_elements(ops):
+    """More elements in one tensor than 32 bits count."""
+    n = (1 << 32) + 5
+    g = torch.zeros(n, dtype=BF16, device=DEV)
+    g[-1], g[n // 2], g[0] = 3.0, 4.0, 12.0
+    assert ops.clip_grads([g], 6.5) == 13.0
+    assert g[-1] == 1.5 and g[n // 2] == 2.0 and g[0] == 6.0 and g.count_nonzero() == 3
