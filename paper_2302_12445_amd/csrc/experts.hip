@@ -227,6 +227,363 @@ template <typename T, bool VEC, int KIND> __global__ __launch_bounds__(THREADS, 
         }
 }
 
+// ------------------------------------------------------------------------------------ bf16, whole vectors, many rows
+// 256 x 256 outputs a workgroup, 128 x 128 a wave, 64 of the summed index a step.  A wave's sums fill half of a SIMD's registers, so that
+// it reads 16 KB from LDS for 64 matrix instructions, two thirds of what waves of half the size would; it is then alone on its SIMD, and all
+// that is not a matrix instruction has to be issued beside them: fragments of a quarter step are read while those of the one before are
+// multiplied, across the barrier of a step too, and memory fills one half of LDS by itself while the other is read.  Workgroups stay
+// for several tiles: the first step of the next tile is loaded beside the last one of this, and sums are stored beside the loads of the
+// second.
+constexpr int WT = 256, WS = 64;                 // outputs' rows and columns of a tile; summed index of a step
+constexpr int HALF = WT * WS * 2;                // bytes of an operand's step
+constexpr int WORKGROUPS = 256;                  // one a CU
+constexpr int TABLE = 1024;                      // experts, and the rows behind the last, that the table in LDS has places for
+
+// An operand's step in LDS, 32 KB.  Along the summed index: 256 rows of 64 values, which the first form of `direct` reads in rows.  Across it:
+// two halves of 64 rows of 128 columns, read with transposing reads so that slots 0 .. 7 of half h are rows 8 h .. 8 h + 7 of sixteen, as in
+// rows.  Pieces of 16 bytes are turned within their row, as memory fills it, so that reads of several rows lie in different banks.
+template <bool ACROSS> struct side {
+    __device__ static __forceinline__ int turn(int row) {
+        return ACROSS ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
+    }
+    uint32_t read_at[ACROSS ? 8 : 4];  // bytes, of this lane's reads: by columns and rows, or by quarter steps
+    uint32_t load_at[8];               // bytes from the step's place in memory, of this lane's pieces
+    int lane, wave;
+
+    // which: the wave's 128 outputs of the tile's 256
+    __device__ __forceinline__ side(int which, int lane_, int wave_) : lane(lane_), wave(wave_) {
+        if (ACROSS) {
+            const int row = 8 * (lane >> 5) + (lane & 15) / 4, c = 2 * (lane >> 4 & 1) + (lane & 3) / 2;
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    read_at[2 * u + k] = which * (HALF / 2) + (row + 4 * k) * 256 + ((4 * u + c) ^ turn(row + 4 * k)) * 16 + 8 * (lane & 1);
+        } else {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+                read_at[kk] = which * (HALF / 2) + (lane & 31) * 128 + ((2 * kk + (lane >> 5)) ^ turn(lane & 31)) * 16;
+        }
+    }
+    // Fragment u (32 outputs) of quarter step kk.
+    __device__ __forceinline__ bf16x8 read(const DEAR_LDS char *s, int u, int kk) const {
+        if (ACROSS) {
+            const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((DEAR_LDS bf16x4 *)(s + read_at[2 * u] + 4096 * kk));
+            const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((DEAR_LDS bf16x4 *)(s + read_at[2 * u + 1] + 4096 * kk));
+            return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        return *(const DEAR_LDS bf16x8 *)(s + read_at[kk] + 4096 * u);
+    }
+    // Row of the operand's tile, and first value of the row, of this lane's load i.
+    __device__ __forceinline__ int row(int i) const { return ACROSS ? (wave % 2) * 32 + 4 * i + lane / 16 : wave * 64 + 8 * i + lane / 8; }
+    __device__ __forceinline__ int value(int i) const {
+        return ACROSS ? (wave / 2) * 128 + (lane % 16 ^ turn(row(i))) * 8 : (lane % 8 ^ turn(row(i))) * 8;
+    }
+    // rows, values: how many of the tile's outputs there are, one at least; beyond them the last row, or the first values, again.  left: of
+    // the summed index in the step, one at least; beyond it what is there already is read again, to be made zeros.
+    __device__ __forceinline__ void aim(uint32_t stride, int outputs, int left) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = min(row(i), (ACROSS ? left : outputs) - 1), v = value(i);
+            load_at[i] = (uint32_t)r * stride + (v < (ACROSS ? outputs : left) ? v : 0) * 2;
+        }
+    }
+    // Where load i puts this wave's pieces.
+    __device__ __forceinline__ DEAR_LDS char *place(DEAR_LDS char *to, int i) const {
+        return to + (ACROSS ? (wave / 2) * (HALF / 2) + ((wave % 2) * 32 + 4 * i) * 256 : (wave * 64 + 8 * i) * 128);
+    }
+    __device__ __forceinline__ void load(const char *from, DEAR_LDS char *to, int i) const { load_to_lds(from + load_at[i], place(to, i)); }
+    // Zeros behind the first `left` of the summed index, in the pieces that this lane has loaded.
+    __device__ __forceinline__ void clear(DEAR_LDS char *to, int left) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((ACROSS ? row(i) : value(i)) >= left) *(DEAR_LDS u32x4 *)(place(to, i) + lane * 16) = u32x4{0, 0, 0, 0};
+    }
+};
+
+// A tile: its operands' first step in memory and its place among the outputs.
+struct wide_tile {
+    const char *a, *b;
+    int64_t sum;           // of the summed index
+    int64_t out, row_end;  // first row of the outputs, behind the last (of a weight gradient in all experts' rows)
+    int32_t col, a_rows, b_rows;
+    bool none;
+};
+
+template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_kernel(params p) {
+    constexpr bool A_ACROSS = KIND == WEIGHT_GRAD, B_ACROSS = KIND != LINEAR;
+    // steps in turn, in arrays of their own: a read from one need not wait for what memory brings to another
+    __shared__ __attribute__((aligned(16))) char a0[HALF], a1[HALF], b0[HALF], b1[HALF];
+    __shared__ int32_t ends[TABLE], upto[TABLE];  // rows up to and with an expert's, and its tiles (of a weight gradient: experts by their rows)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rows = (int)p.rows;
+
+    // the table, each wave for itself, with the same values
+    {
+        int32_t before = 0, tiles = 0;
+        for (int e0 = 0; e0 <= p.experts; e0 += 64) {
+            const int e = e0 + lane;
+            int32_t end = e < p.experts ? min(max(p.ends[e], 0), rows) : rows;
+            end = max(max_before(end, lane), before);
+            int32_t begin = __shfl_up(end, 1);
+            if (lane == 0) begin = before;
+            const int32_t all = tiles + sum_before(e <= p.experts ? (int32_t)(((uint32_t)(end - begin) + WT - 1) / WT) : 0, lane);
+            if (e <= p.experts && wave == 0) {
+                ends[e] = end;
+                if (KIND != WEIGHT_GRAD) upto[e] = all;
+            }
+            before = __builtin_amdgcn_readfirstlane(__shfl(end, 63));
+            tiles = __builtin_amdgcn_readfirstlane(__shfl(all, 63));
+        }
+        __syncthreads();
+        if (KIND == WEIGHT_GRAD) {
+            // experts with most rows first, so that what is left in the end is short; for more of them than there are threads as they come
+            if (p.experts <= THREADS) {
+                const int e = threadIdx.x;
+                if (e < p.experts) {
+                    const int mine = ends[e] - (e ? ends[e - 1] : 0);
+                    int rank = 0, begin = 0;
+                    for (int i = 0; i < p.experts; ++i) {
+                        const int end = ends[i], n = end - begin;
+                        rank += n > mine || (n == mine && i < e);
+                        begin = end;
+                    }
+                    upto[rank] = e;
+                }
+            } else {
+                for (int e = threadIdx.x; e < p.experts; e += THREADS) upto[e] = e;
+            }
+            __syncthreads();
+        }
+    }
+
+    // Items go to the eight XCDs in runs of 32, one for each of its CUs: neighbours of a strip of four columns, which share rows and columns.
+    const unsigned per = (unsigned)p.a_tiles * p.b_tiles, items = KIND == WEIGHT_GRAD ? per * p.experts : per;
+    unsigned round = 0;
+    auto next = [&]() {
+        wide_tile t;
+        for (;; ++round) {
+            const unsigned item = (round * 8 + blockIdx.x % 8) * 32 + blockIdx.x / 8;
+            t.none = round * WORKGROUPS >= items;
+            if (t.none) return t;
+            if (item >= items) continue;
+            const unsigned id = item % per, strip = id / (4u * p.a_tiles), wide = min(4u, p.b_tiles - 4 * strip), in_strip = id - strip * 4 * p.a_tiles;
+            const int a_tile = (int)(in_strip / wide), b_tile = (int)(4 * strip + in_strip % wide);
+            t.col = b_tile * WT;
+            t.b_rows = p.n_b - t.col;
+            int expert;
+            if (KIND == WEIGHT_GRAD) {
+                expert = __builtin_amdgcn_readfirstlane(upto[item / per]);
+                const int begin = expert ? __builtin_amdgcn_readfirstlane(ends[expert - 1]) : 0;
+                t.sum = __builtin_amdgcn_readfirstlane(ends[expert]) - begin;
+                t.a_rows = p.n_a - a_tile * WT;
+                t.a = (const char *)p.a + ((int64_t)begin * p.a_stride + (int64_t)a_tile * WT) * 2;
+                t.b = (const char *)p.b + ((int64_t)begin * p.b_stride + t.col) * 2;
+                t.out = (int64_t)expert * p.n_a + a_tile * WT, t.row_end = (int64_t)(expert + 1) * p.n_a;
+            } else {
+                int first = 0;
+                expert = -1;
+                for (int e0 = 0; e0 <= p.experts; e0 += 64) {
+                    const int e = min(e0 + lane, p.experts);
+                    const uint64_t found = __ballot(upto[e] > a_tile);
+                    if (found) {
+                        expert = min(e0 + (int)__builtin_ctzll(found), p.experts);
+                        break;
+                    }
+                }
+                if (expert < 0) continue;  // there are fewer tiles
+                const int begin = expert ? __builtin_amdgcn_readfirstlane(ends[expert - 1]) : 0, end = __builtin_amdgcn_readfirstlane(ends[expert]);
+                first = begin + (a_tile - (expert ? __builtin_amdgcn_readfirstlane(upto[expert - 1]) : 0)) * WT;
+                t.sum = expert < p.experts ? p.sum : 0;
+                t.a_rows = end - first;
+                t.a = (const char *)p.a + (int64_t)first * p.a_stride * 2;
+                t.b = (const char *)p.b + ((int64_t)expert * p.sum * p.n_b + (KIND == LINEAR ? (int64_t)t.col * p.sum : t.col)) * 2;
+                t.out = first, t.row_end = end;
+            }
+            if (t.sum > 0) {
+                ++round;
+                return t;
+            }
+            // nothing to add: zeros
+            typedef typename std::conditional<KIND == WEIGHT_GRAD, float, bf16>::type O;
+            constexpr int E = 16 / sizeof(O);
+            for (int i = threadIdx.x; i < WT * WT / E; i += THREADS) {
+                const int64_t row = t.out + i / (WT / E);
+                const int col = t.col + i % (WT / E) * E;
+                if (row < t.row_end && col < p.n_b) *(u32x4 *)((O *)p.out + row * p.n_b + col) = u32x4{0, 0, 0, 0};
+            }
+        }
+    };
+
+    side<A_ACROSS> a(wave / 2, lane, wave);
+    side<B_ACROSS> b(wave % 2, lane, wave);
+    const uint32_t a_stride = (uint32_t)p.a_stride * 2, b_stride = (uint32_t)p.b_stride * 2;
+    const char *from_a = nullptr, *from_b = nullptr;
+    int64_t left = 0;  // of the summed index, from the step that is loaded next on
+    wide_tile now = next(), then = now, done = now;
+    if (now.none) return;
+    auto aim = [&](const wide_tile &t, int rows) {
+        a.aim(a_stride, t.a_rows, rows);
+        b.aim(b_stride, t.b_rows, rows);
+    };
+    auto begin = [&](const wide_tile &t) {
+        from_a = t.a, from_b = t.b, left = t.sum;
+        aim(t, (int)min(left, (int64_t)WS));
+    };
+    auto loaded = [&] {
+        from_a += A_ACROSS ? (int64_t)WS * a_stride : WS * 2;
+        from_b += B_ACROSS ? (int64_t)WS * b_stride : WS * 2;
+        left -= WS;
+    };
+
+    begin(now);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) a.load(from_a, (DEAR_LDS char *)a0, i), b.load(from_b, (DEAR_LDS char *)b0, i);
+    loaded();
+    f32x16 acc[4][4];
+    struct {
+        bf16x8 a[4], b[4];
+    } f, g;
+    auto read = [&](auto &x, const DEAR_LDS char *from_a, const DEAR_LDS char *from_b, int kk) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x.a[u] = a.read(from_a, u, kk), x.b[u] = b.read(from_b, u, kk);
+    };
+    auto multiply = [&](auto &x, auto first) {  // first: of a tile's sums
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int v = 0; v < 4; ++v)  // a lane has one row of the outputs
+                acc[u][v] = mma(x.b[v], x.a[u], decltype(first)::value ? f32x16{} : acc[u][v]);
+    };
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
+    auto store = [&](const wide_tile &t) {
+        const int64_t row0 = t.out + (wave / 2) * 128 + (lane & 31);
+        const int col0 = t.col + (wave % 2) * 128;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t row = row0 + 32 * u;
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                if (KIND == WEIGHT_GRAD) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int col = col0 + 32 * v + 8 * q + 4 * (lane >> 5);
+                        f32x4 x;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[k] = acc[u][v][4 * q + k];
+                        if (row < t.row_end && col < p.n_b) *(f32x4 *)((float *)p.out + row * p.n_b + col) = x;
+                    }
+                } else {
+                    // the halves of the wave exchange fours of columns, and have eight in a row each
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t x[2][2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const bf16x2 y = {(bf16)acc[u][v][8 * q + 4 * h + 2 * k], (bf16)acc[u][v][8 * q + 4 * h + 2 * k + 1]};
+                                x[h][k] = __builtin_bit_cast(uint32_t, y);
+                            }
+                        const auto w0 = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
+                        const auto w1 = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+                        const int col = col0 + 32 * v + 16 * q + 8 * (lane >> 5);
+                        if (row < t.row_end && col < p.n_b)
+                            *(u32x4 *)((bf16 *)p.out + row * p.n_b + col) = u32x4{(uint32_t)w0[0], (uint32_t)w1[0], (uint32_t)w0[1], (uint32_t)w1[1]};
+                    }
+                }
+            }
+        }
+    };
+    // Beside 16 matrix instructions the reads of a quarter step, and loads where there are some.
+    auto beside = [](auto loads) {
+        constexpr int READS = (A_ACROSS ? 8 : 4) + (B_ACROSS ? 8 : 4);
+#pragma unroll
+        for (int u = 0; u < 16; ++u) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (u * READS / 16 != (u + 1) * READS / 16) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if (decltype(loads)::value) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+    };
+    // The step in x and y is there, and all waves have read the one that is loaded over.  valid: of its part of the sum.
+    auto ready = [&](DEAR_LDS char *x, DEAR_LDS char *y, int64_t valid) {
+        __builtin_amdgcn_s_waitcnt(0x0070);
+        if (valid < WS) {
+            a.clear(x, (int)max(valid, (int64_t)0)), b.clear(y, (int)max(valid, (int64_t)0));
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+        }
+        __syncthreads();
+    };
+    // What comes behind this tile's whole steps: a part of one, or (sums are made of pairs of steps) nothing, for which its first again.
+    auto rest = [&](const wide_tile &t) {
+        if (left >= WS) return;
+        if (left <= 0) from_a = t.a, from_b = t.b;
+        aim(t, (int)(left > 0 ? left : 1));
+    };
+    auto load = [&](DEAR_LDS char *to_a, DEAR_LDS char *to_b) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a.load(from_a, to_a, i), b.load(from_b, to_b, i);
+    };
+    // A step of a tile but its first: with the products that are left over from the step before.
+    auto step = [&](DEAR_LDS char *x, DEAR_LDS char *y, DEAR_LDS char *to_a, DEAR_LDS char *to_b) {
+        read(f, x, y, 0);
+        load(to_a, to_b);
+        multiply(g, no);
+        beside(yes);
+        read(g, x, y, 1);
+        multiply(f, no);
+        beside(no);
+        read(f, x, y, 2);
+        multiply(g, no);
+        beside(no);
+        read(g, x, y, 3);
+        multiply(f, no);
+        beside(no);
+        loaded();
+    };
+    DEAR_LDS char *const xa = (DEAR_LDS char *)a0, *const ya = (DEAR_LDS char *)b0, *const xb = (DEAR_LDS char *)a1, *const yb = (DEAR_LDS char *)b1;
+    bool any = false;  // sums of a tile to store
+    for (;;) {
+        if (!now.none) rest(now);
+        ready(xa, ya, left + WS);
+        if (!now.none) {
+            load(xb, yb);
+            loaded();
+        }
+        if (any) {
+            multiply(g, no);
+            store(done);
+        }
+        if (now.none) break;
+        read(f, xa, ya, 0);
+        read(g, xa, ya, 1);
+        multiply(f, yes);
+        read(f, xa, ya, 2);
+        multiply(g, no);
+        read(g, xa, ya, 3);
+        multiply(f, no);
+        for (;;) {
+            const int64_t valid = left + WS;
+            const bool last = left <= 0;
+            if (last) {
+                then = next();
+                begin(then.none ? now : then);  // (behind the last tile its first step again, which nothing reads)
+            } else {
+                rest(now);
+            }
+            ready(xb, yb, valid);
+            step(xb, yb, xa, ya);
+            if (last) break;
+            const int64_t more = left + WS;
+            rest(now);
+            ready(xa, ya, more);
+            step(xa, ya, xb, yb);
+        }
+        done = now, now = then, any = true;
+    }
+}
+
 // ------------------------------------------------------------------------------------ host
 constexpr int64_t MAX_ROWS = INT32_MAX;
 constexpr int32_t MAX_EXPERTS = 1 << 16, MAX_WIDTH = 1 << 20;
@@ -248,6 +605,15 @@ int check_rows(const dear_experts_t &x, const void *p, int64_t stride, int64_t w
 bool vectors(const dear_experts_t &x, const void *p, int64_t stride, int64_t width) {
     const int n = size_of(x.dtype);
     return aligned(p, 16) && stride * n % 16 == 0 && width * n % 16 == 0;
+}
+
+// Whether the wide kernel takes a call: bf16 in whole vectors, with rows that 32-bit offsets reach, and enough of it.
+template <int KIND> bool wide(const dear_experts_t &x, bool vec, const params &p) {
+    const int64_t most = 1 << 22;
+    if (x.dtype != DEAR_BF16 || !vec || !aligned(p.out, 16) || x.experts >= TABLE || p.n_b % 8 || p.a_stride >= most || p.b_stride >= most) return false;
+    const int64_t a_tiles = KIND == WEIGHT_GRAD ? ceil_div(x.outs, WT) * x.experts : x.rows / WT + x.experts + 1;
+    if (a_tiles * ceil_div(p.n_b, WT) > INT32_MAX / 2) return false;
+    return x.rows / x.experts >= WT / 2;
 }
 
 template <int KIND> int64_t workspace_of(const dear_experts_t &) { return 0; }
@@ -280,6 +646,12 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
     } else {
         p.a = x->dy, p.a_stride = x->dy_stride, p.b = x->x, p.b_stride = x->x_stride, p.n_a = x->outs, p.n_b = x->ins;
         vec = vectors(*x, p.a, p.a_stride, x->outs) && vectors(*x, p.b, p.b_stride, x->ins);
+    }
+    if (wide<KIND>(*x, vec, p)) {
+        p.a_tiles = (int32_t)(KIND == WEIGHT_GRAD ? ceil_div(x->outs, WT) : x->rows / WT + x->experts + 1);
+        p.b_tiles = (int32_t)ceil_div(p.n_b, WT);
+        experts_wide_kernel<KIND><<<WORKGROUPS, THREADS, 0, stream>>>(p);
+        return launch_status();
     }
     // tiles of rows: each expert, and the rows behind the last, may have one that is not whole
     p.a_tiles = (int32_t)(KIND == WEIGHT_GRAD ? ceil_div(x->outs, BA) : x->rows / BA + x->experts + 1);
