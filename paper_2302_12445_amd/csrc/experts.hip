@@ -227,42 +227,41 @@ template <typename T, bool VEC, int KIND> __global__ __launch_bounds__(THREADS, 
         }
 }
 
-// ------------------------------------------------------------------------------------ bf16, whole vectors, many rows
-// 256 x 256 outputs a workgroup, 128 x 128 a wave, 64 of the summed index a step.  A wave's sums fill half of a SIMD's registers, so that
-// it reads 16 KB from LDS for 64 matrix instructions, two thirds of what waves of half the size would; it is then alone on its SIMD, and all
-// that is not a matrix instruction has to be issued beside them: fragments of a quarter step are read while those of the one before are
-// multiplied, across the barrier of a step too, and memory fills one half of LDS by itself while the other is read.  Workgroups stay
-// for several tiles: the first step of the next tile is loaded beside the last one of this, and sums are stored beside the loads of the
-// second.
-constexpr int WT = 256, WS = 64;                 // outputs' rows and columns of a tile; summed index of a step
-constexpr int HALF = WT * WS * 2;                // bytes of an operand's step
-constexpr int WORKGROUPS = 256;                  // one a CU
-constexpr int TABLE = 1024;                      // experts, and the rows behind the last, that the table in LDS has places for
+// ------------------------------------------------------------------------------------ bf16, whole vectors
+// SIZE x SIZE outputs a workgroup, a quarter of them a wave, 64 of the summed index a step.  In tiles of 256 a wave's sums fill half of a
+// SIMD's registers, so that it reads 16 KB from LDS for 64 matrix instructions; it is then alone on its SIMD, and all that is not a matrix
+// instruction has to be issued beside them: fragments of a quarter step are read while those of the one before are multiplied, across the
+// barrier of a step too, and memory fills one half of LDS by itself while the other is read.  Workgroups stay for several tiles: the first
+// step of the next tile is loaded beside the last one of this, and sums are stored beside the loads of the second.
+constexpr int WS = 64;          // summed index of a step
+constexpr int CUS = 256;
+constexpr int TABLE = 1024;     // experts that the table in LDS has places for
 
-// An operand's step in LDS, 32 KB.  Along the summed index: 256 rows of 64 values, which the first form of `direct` reads in rows.  Across it:
-// two halves of 64 rows of 128 columns, read with transposing reads so that slots 0 .. 7 of half h are rows 8 h .. 8 h + 7 of sixteen, as in
-// rows.  Pieces of 16 bytes are turned within their row, as memory fills it, so that reads of several rows lie in different banks.
-template <bool ACROSS> struct side {
+// An operand's step in LDS.  Along the summed index: SIZE rows of 64 values, read in rows.  Across it: 64 rows of 128 columns, twice in tiles
+// of 256, read with transposing reads so that slots 0 .. 7 of half h are rows 8 h .. 8 h + 7 of sixteen, as in rows.  Pieces of 16 bytes are
+// turned within their row, as memory fills it, so that reads of several rows lie in different banks.
+template <bool ACROSS, int SIZE> struct side {
+    static constexpr int F = SIZE / 64, LOADS = SIZE / 32;  // fragments of a wave; its loads for a step, 1 KB each
     __device__ static __forceinline__ int turn(int row) {
         return ACROSS ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
     }
-    uint32_t read_at[ACROSS ? 8 : 4];  // bytes, of this lane's reads: by columns and rows, or by quarter steps
-    uint32_t load_at[8];               // bytes from the step's place in memory, of this lane's pieces
+    uint32_t read_at[ACROSS ? 2 * F : 4];  // bytes, of this lane's reads: by columns and rows, or by quarter steps
+    uint32_t load_at[LOADS];               // bytes from the step's place in memory, of this lane's pieces
     int lane, wave;
 
-    // which: the wave's 128 outputs of the tile's 256
+    // which: the wave's half of the tile's outputs
     __device__ __forceinline__ side(int which, int lane_, int wave_) : lane(lane_), wave(wave_) {
         if (ACROSS) {
-            const int row = 8 * (lane >> 5) + (lane & 15) / 4, c = 2 * (lane >> 4 & 1) + (lane & 3) / 2;
+            const int row = 8 * (lane >> 5) + (lane & 15) / 4, c = 2 * (lane >> 4 & 1) + (lane & 3) / 2 + (SIZE == 128 ? 8 * which : 0);
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
+            for (int u = 0; u < F; ++u)
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
-                    read_at[2 * u + k] = which * (HALF / 2) + (row + 4 * k) * 256 + ((4 * u + c) ^ turn(row + 4 * k)) * 16 + 8 * (lane & 1);
+                    read_at[2 * u + k] = (SIZE == 256 ? which * 16384 : 0) + (row + 4 * k) * 256 + ((4 * u + c) ^ turn(row + 4 * k)) * 16 + 8 * (lane & 1);
         } else {
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-                read_at[kk] = which * (HALF / 2) + (lane & 31) * 128 + ((2 * kk + (lane >> 5)) ^ turn(lane & 31)) * 16;
+                read_at[kk] = which * (SIZE / 2 * 128) + (lane & 31) * 128 + ((2 * kk + (lane >> 5)) ^ turn(lane & 31)) * 16;
         }
     }
     // Fragment u (32 outputs) of quarter step kk.
@@ -274,29 +273,31 @@ template <bool ACROSS> struct side {
         }
         return *(const DEAR_LDS bf16x8 *)(s + read_at[kk] + 4096 * u);
     }
-    // Row of the operand's tile, and first value of the row, of this lane's load i.
-    __device__ __forceinline__ int row(int i) const { return ACROSS ? (wave % 2) * 32 + 4 * i + lane / 16 : wave * 64 + 8 * i + lane / 8; }
-    __device__ __forceinline__ int value(int i) const {
-        return ACROSS ? (wave / 2) * 128 + (lane % 16 ^ turn(row(i))) * 8 : (lane % 8 ^ turn(row(i))) * 8;
+    // Row of the operand's tile, and first value of the row, of this lane's load i; where the load puts this wave's pieces.
+    __device__ __forceinline__ int first(int i) const {
+        return ACROSS ? (SIZE == 256 ? wave % 2 * 32 : wave * 16) + 4 * i : wave * (SIZE / 4) + 8 * i;
     }
-    // rows, values: how many of the tile's outputs there are, one at least; beyond them the last row, or the first values, again.  left: of
-    // the summed index in the step, one at least; beyond it what is there already is read again, to be made zeros.
+    __device__ __forceinline__ int row(int i) const { return first(i) + (ACROSS ? lane / 16 : lane / 8); }
+    __device__ __forceinline__ int value(int i) const {
+        return ACROSS ? (SIZE == 256 ? wave / 2 * 128 : 0) + (lane % 16 ^ turn(row(i))) * 8 : (lane % 8 ^ turn(row(i))) * 8;
+    }
+    __device__ __forceinline__ DEAR_LDS char *place(DEAR_LDS char *to, int i) const {
+        return to + (ACROSS ? (SIZE == 256 ? wave / 2 * 16384 : 0) + first(i) * 256 : first(i) * 128);
+    }
+    // outputs: how many of the tile's there are, one at least; beyond them the last row, or the first values, again.  left: of the summed
+    // index in the step, one at least; beyond it what is there already is read again, to be made zeros.
     __device__ __forceinline__ void aim(uint32_t stride, int outputs, int left) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < LOADS; ++i) {
             const int r = min(row(i), (ACROSS ? left : outputs) - 1), v = value(i);
             load_at[i] = (uint32_t)r * stride + (v < (ACROSS ? outputs : left) ? v : 0) * 2;
         }
-    }
-    // Where load i puts this wave's pieces.
-    __device__ __forceinline__ DEAR_LDS char *place(DEAR_LDS char *to, int i) const {
-        return to + (ACROSS ? (wave / 2) * (HALF / 2) + ((wave % 2) * 32 + 4 * i) * 256 : (wave * 64 + 8 * i) * 128);
     }
     __device__ __forceinline__ void load(const char *from, DEAR_LDS char *to, int i) const { load_to_lds(from + load_at[i], place(to, i)); }
     // Zeros behind the first `left` of the summed index, in the pieces that this lane has loaded.
     __device__ __forceinline__ void clear(DEAR_LDS char *to, int left) const {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < LOADS; ++i)
             if ((ACROSS ? row(i) : value(i)) >= left) *(DEAR_LDS u32x4 *)(place(to, i) + lane * 16) = u32x4{0, 0, 0, 0};
     }
 };
@@ -310,113 +311,16 @@ struct wide_tile {
     bool none;
 };
 
-template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_kernel(params p) {
+// The tiles that next() gives, one after another.  xa, ya and xb, yb: the operands' places for steps in turn, arrays of their own, so that a
+// read from one need not wait for what memory brings to another; lines: 4 KB a wave.
+template <int KIND, int SIZE, typename NEXT>
+__device__ __forceinline__ void run(const params &p, DEAR_LDS char *xa, DEAR_LDS char *ya, DEAR_LDS char *xb, DEAR_LDS char *yb,
+                                    DEAR_LDS char *lines, NEXT next) {
     constexpr bool A_ACROSS = KIND == WEIGHT_GRAD, B_ACROSS = KIND != LINEAR;
-    // steps in turn, in arrays of their own: a read from one need not wait for what memory brings to another
-    __shared__ __attribute__((aligned(16))) char a0[HALF], a1[HALF], b0[HALF], b1[HALF];
-    __shared__ int32_t ends[TABLE], upto[TABLE];  // rows up to and with an expert's, and its tiles (of a weight gradient: experts by their rows)
+    constexpr int F = SIZE / 64, LOADS = SIZE / 32, WAVE = SIZE / 2;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int rows = (int)p.rows;
-
-    // the table, each wave for itself, with the same values
-    {
-        int32_t before = 0, tiles = 0;
-        for (int e0 = 0; e0 <= p.experts; e0 += 64) {
-            const int e = e0 + lane;
-            int32_t end = e < p.experts ? min(max(p.ends[e], 0), rows) : rows;
-            end = max(max_before(end, lane), before);
-            int32_t begin = __shfl_up(end, 1);
-            if (lane == 0) begin = before;
-            const int32_t all = tiles + sum_before(e <= p.experts ? (int32_t)(((uint32_t)(end - begin) + WT - 1) / WT) : 0, lane);
-            if (e <= p.experts && wave == 0) {
-                ends[e] = end;
-                if (KIND != WEIGHT_GRAD) upto[e] = all;
-            }
-            before = __builtin_amdgcn_readfirstlane(__shfl(end, 63));
-            tiles = __builtin_amdgcn_readfirstlane(__shfl(all, 63));
-        }
-        __syncthreads();
-        if (KIND == WEIGHT_GRAD) {
-            // experts with most rows first, so that what is left in the end is short; for more of them than there are threads as they come
-            if (p.experts <= THREADS) {
-                const int e = threadIdx.x;
-                if (e < p.experts) {
-                    const int mine = ends[e] - (e ? ends[e - 1] : 0);
-                    int rank = 0, begin = 0;
-                    for (int i = 0; i < p.experts; ++i) {
-                        const int end = ends[i], n = end - begin;
-                        rank += n > mine || (n == mine && i < e);
-                        begin = end;
-                    }
-                    upto[rank] = e;
-                }
-            } else {
-                for (int e = threadIdx.x; e < p.experts; e += THREADS) upto[e] = e;
-            }
-            __syncthreads();
-        }
-    }
-
-    // Items go to the eight XCDs in runs of 32, one for each of its CUs: neighbours of a strip of four columns, which share rows and columns.
-    const unsigned per = (unsigned)p.a_tiles * p.b_tiles, items = KIND == WEIGHT_GRAD ? per * p.experts : per;
-    unsigned round = 0;
-    auto next = [&]() {
-        wide_tile t;
-        for (;; ++round) {
-            const unsigned item = (round * 8 + blockIdx.x % 8) * 32 + blockIdx.x / 8;
-            t.none = round * WORKGROUPS >= items;
-            if (t.none) return t;
-            if (item >= items) continue;
-            const unsigned id = item % per, strip = id / (4u * p.a_tiles), wide = min(4u, p.b_tiles - 4 * strip), in_strip = id - strip * 4 * p.a_tiles;
-            const int a_tile = (int)(in_strip / wide), b_tile = (int)(4 * strip + in_strip % wide);
-            t.col = b_tile * WT;
-            t.b_rows = p.n_b - t.col;
-            int expert;
-            if (KIND == WEIGHT_GRAD) {
-                expert = __builtin_amdgcn_readfirstlane(upto[item / per]);
-                const int begin = expert ? __builtin_amdgcn_readfirstlane(ends[expert - 1]) : 0;
-                t.sum = __builtin_amdgcn_readfirstlane(ends[expert]) - begin;
-                t.a_rows = p.n_a - a_tile * WT;
-                t.a = (const char *)p.a + ((int64_t)begin * p.a_stride + (int64_t)a_tile * WT) * 2;
-                t.b = (const char *)p.b + ((int64_t)begin * p.b_stride + t.col) * 2;
-                t.out = (int64_t)expert * p.n_a + a_tile * WT, t.row_end = (int64_t)(expert + 1) * p.n_a;
-            } else {
-                int first = 0;
-                expert = -1;
-                for (int e0 = 0; e0 <= p.experts; e0 += 64) {
-                    const int e = min(e0 + lane, p.experts);
-                    const uint64_t found = __ballot(upto[e] > a_tile);
-                    if (found) {
-                        expert = min(e0 + (int)__builtin_ctzll(found), p.experts);
-                        break;
-                    }
-                }
-                if (expert < 0) continue;  // there are fewer tiles
-                const int begin = expert ? __builtin_amdgcn_readfirstlane(ends[expert - 1]) : 0, end = __builtin_amdgcn_readfirstlane(ends[expert]);
-                first = begin + (a_tile - (expert ? __builtin_amdgcn_readfirstlane(upto[expert - 1]) : 0)) * WT;
-                t.sum = expert < p.experts ? p.sum : 0;
-                t.a_rows = end - first;
-                t.a = (const char *)p.a + (int64_t)first * p.a_stride * 2;
-                t.b = (const char *)p.b + ((int64_t)expert * p.sum * p.n_b + (KIND == LINEAR ? (int64_t)t.col * p.sum : t.col)) * 2;
-                t.out = first, t.row_end = end;
-            }
-            if (t.sum > 0) {
-                ++round;
-                return t;
-            }
-            // nothing to add: zeros
-            typedef typename std::conditional<KIND == WEIGHT_GRAD, float, bf16>::type O;
-            constexpr int E = 16 / sizeof(O);
-            for (int i = threadIdx.x; i < WT * WT / E; i += THREADS) {
-                const int64_t row = t.out + i / (WT / E);
-                const int col = t.col + i % (WT / E) * E;
-                if (row < t.row_end && col < p.n_b) *(u32x4 *)((O *)p.out + row * p.n_b + col) = u32x4{0, 0, 0, 0};
-            }
-        }
-    };
-
-    side<A_ACROSS> a(wave / 2, lane, wave);
-    side<B_ACROSS> b(wave % 2, lane, wave);
+    side<A_ACROSS, SIZE> a(wave / 2, lane, wave);
+    side<B_ACROSS, SIZE> b(wave % 2, lane, wave);
     const uint32_t a_stride = (uint32_t)p.a_stride * 2, b_stride = (uint32_t)p.b_stride * 2;
     const char *from_a = nullptr, *from_b = nullptr;
     int64_t left = 0;  // of the summed index, from the step that is loaded next on
@@ -435,75 +339,94 @@ template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_k
         from_b += B_ACROSS ? (int64_t)WS * b_stride : WS * 2;
         left -= WS;
     };
-
-    begin(now);
+    auto load = [&](DEAR_LDS char *to_a, DEAR_LDS char *to_b, int from, int to) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) a.load(from_a, (DEAR_LDS char *)a0, i), b.load(from_b, (DEAR_LDS char *)b0, i);
-    loaded();
-    f32x16 acc[4][4];
+        for (int i = from; i < to; ++i) a.load(from_a, to_a, i), b.load(from_b, to_b, i);
+    };
+
+    f32x16 acc[F][F];
     struct {
-        bf16x8 a[4], b[4];
+        bf16x8 a[F], b[F];
     } f, g;
+    constexpr std::true_type yes;
+    constexpr std::false_type no;
     auto read = [&](auto &x, const DEAR_LDS char *from_a, const DEAR_LDS char *from_b, int kk) {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) x.a[u] = a.read(from_a, u, kk), x.b[u] = b.read(from_b, u, kk);
+        for (int u = 0; u < F; ++u) x.a[u] = a.read(from_a, u, kk), x.b[u] = b.read(from_b, u, kk);
     };
     auto multiply = [&](auto &x, auto first) {  // first: of a tile's sums
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int u = 0; u < F; ++u)
 #pragma unroll
-            for (int v = 0; v < 4; ++v)  // a lane has one row of the outputs
+            for (int v = 0; v < F; ++v)  // a lane has one row of the outputs
                 acc[u][v] = mma(x.b[v], x.a[u], decltype(first)::value ? f32x16{} : acc[u][v]);
     };
-    constexpr std::true_type yes;
-    constexpr std::false_type no;
+    // A lane has, of a row, columns apart: through 4 KB of LDS a wave, 32 rows of 128 bytes at a time, eight lanes get a whole line each.  Stored
+    // from the lanes they come as quarters of lines (16384 x 4096 x 1024 145 us, so 132); and past the caches, which the operands want (8192
+    // x 8192 x 8192 weight gradient 830 us, so 798).
     auto store = [&](const wide_tile &t) {
-        const int64_t row0 = t.out + (wave / 2) * 128 + (lane & 31);
-        const int col0 = t.col + (wave % 2) * 128;
+        typedef typename std::conditional<KIND == WEIGHT_GRAD, float, bf16>::type O;
+        constexpr int BLOCKS = KIND == WEIGHT_GRAD ? 1 : 2;  // of 32 columns in a line
+        DEAR_LDS char *s = lines + wave * 4096;
+        const int l = lane & 31, line_at = lane / 8 * 128 + (lane % 8 ^ lane / 8) * 16;
+        const int rows = (int)min(t.row_end - t.out, (int64_t)SIZE), cols = min(p.n_b - t.col, SIZE), pitch = p.n_b * (int)sizeof(O);
+        const int row0 = (wave / 2) * WAVE + lane / 8, col0 = (wave % 2) * WAVE + lane % 8 * (int)(16 / sizeof(O));
+        const uint32_t off = (uint32_t)row0 * (uint32_t)pitch + col0 * (uint32_t)sizeof(O);
+        char *const at = (char *)((O *)p.out + t.out * p.n_b + t.col);
+        const bool whole = rows == SIZE && cols == SIZE;
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int64_t row = row0 + 32 * u;
+        for (int u = 0; u < F; ++u)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
+            for (int v = 0; v < F; v += BLOCKS) {
+                auto put = [&](int piece, u32x4 x) { *(DEAR_LDS u32x4 *)(s + l * 128 + (piece ^ (l & 7)) * 16) = x; };
                 if (KIND == WEIGHT_GRAD) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const int col = col0 + 32 * v + 8 * q + 4 * (lane >> 5);
                         f32x4 x;
 #pragma unroll
                         for (int k = 0; k < 4; ++k) x[k] = acc[u][v][4 * q + k];
-                        if (row < t.row_end && col < p.n_b) *(f32x4 *)((float *)p.out + row * p.n_b + col) = x;
+                        put(2 * q + (lane >> 5), __builtin_bit_cast(u32x4, x));
                     }
                 } else {
                     // the halves of the wave exchange fours of columns, and have eight in a row each
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        uint32_t x[2][2];
+                    for (int w = 0; w < 2; ++w)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t x[2][2];
 #pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                const bf16x2 y = {(bf16)acc[u][v][8 * q + 4 * h + 2 * k], (bf16)acc[u][v][8 * q + 4 * h + 2 * k + 1]};
-                                x[h][k] = __builtin_bit_cast(uint32_t, y);
-                            }
-                        const auto w0 = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
-                        const auto w1 = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
-                        const int col = col0 + 32 * v + 16 * q + 8 * (lane >> 5);
-                        if (row < t.row_end && col < p.n_b)
-                            *(u32x4 *)((bf16 *)p.out + row * p.n_b + col) = u32x4{(uint32_t)w0[0], (uint32_t)w1[0], (uint32_t)w0[1], (uint32_t)w1[1]};
-                    }
+                            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                                for (int k = 0; k < 2; ++k) {
+                                    const f32x16 &c = acc[u][v + w];
+                                    const bf16x2 y = {(bf16)c[8 * q + 4 * h + 2 * k], (bf16)c[8 * q + 4 * h + 2 * k + 1]};
+                                    x[h][k] = __builtin_bit_cast(uint32_t, y);
+                                }
+                            const auto w0 = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
+                            const auto w1 = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+                            put(4 * w + 2 * q + (lane >> 5), u32x4{(uint32_t)w0[0], (uint32_t)w1[0], (uint32_t)w0[1], (uint32_t)w1[1]});
+                        }
                 }
-            }
-        }
-    };
-    // Beside 16 matrix instructions the reads of a quarter step, and loads where there are some.
-    auto beside = [](auto loads) {
-        constexpr int READS = (A_ACROSS ? 8 : 4) + (B_ACROSS ? 8 : 4);
+                __builtin_amdgcn_wave_barrier();
 #pragma unroll
-        for (int u = 0; u < 16; ++u) {
+                for (int i = 0; i < 4; ++i) {
+                    const u32x4 x = *(DEAR_LDS u32x4 *)(s + i * 1024 + line_at);
+                    if (whole || (row0 + 32 * u + 8 * i < rows && col0 + 32 * v < cols))
+                        __builtin_nontemporal_store(x, (u32x4 *)(at + (int64_t)(32 * u + 8 * i) * pitch + 32 * v * (int)sizeof(O) + off));
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+    };
+    // Beside the matrix instructions of a quarter step its reads, and `loads` loads.
+    auto beside = [](auto loads) {
+        constexpr int N = F * F, READS = F * ((A_ACROSS ? 2 : 1) + (B_ACROSS ? 2 : 1)), LOADS = decltype(loads)::value;
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            if (u * READS / 16 != (u + 1) * READS / 16) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            if (decltype(loads)::value) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+#pragma unroll
+            for (int k = u * READS / N; k < (u + 1) * READS / N; ++k) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+            for (int k = u * LOADS / N; k < (u + 1) * LOADS / N; ++k) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
         }
     };
     // The step in x and y is there, and all waves have read the one that is loaded over.  valid: of its part of the sum.
@@ -521,34 +444,40 @@ template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_k
         if (left <= 0) from_a = t.a, from_b = t.b;
         aim(t, (int)(left > 0 ? left : 1));
     };
-    auto load = [&](DEAR_LDS char *to_a, DEAR_LDS char *to_b) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) a.load(from_a, to_a, i), b.load(from_b, to_b, i);
-    };
     // A step of a tile but its first: with the products that are left over from the step before.
     auto step = [&](DEAR_LDS char *x, DEAR_LDS char *y, DEAR_LDS char *to_a, DEAR_LDS char *to_b) {
+        // half of the loads in the first quarter, and none in the last: all in the first one wait for one another's way (8192 x 8192 x 8192
+        // 1013 us, so 947), and spread over all they come too late (988)
+        typedef std::integral_constant<int, LOADS> half;
+        typedef std::integral_constant<int, LOADS / 2> fourth;
+        typedef std::integral_constant<int, 0> none;
         read(f, x, y, 0);
-        load(to_a, to_b);
+        load(to_a, to_b, 0, LOADS / 2);
         multiply(g, no);
-        beside(yes);
+        beside(half());
         read(g, x, y, 1);
+        load(to_a, to_b, LOADS / 2, LOADS * 3 / 4);
         multiply(f, no);
-        beside(no);
+        beside(fourth());
         read(f, x, y, 2);
+        load(to_a, to_b, LOADS * 3 / 4, LOADS);
         multiply(g, no);
-        beside(no);
+        beside(fourth());
         read(g, x, y, 3);
         multiply(f, no);
-        beside(no);
+        beside(none());
         loaded();
     };
-    DEAR_LDS char *const xa = (DEAR_LDS char *)a0, *const ya = (DEAR_LDS char *)b0, *const xb = (DEAR_LDS char *)a1, *const yb = (DEAR_LDS char *)b1;
+
+    begin(now);
+    load(xa, ya, 0, LOADS);
+    loaded();
     bool any = false;  // sums of a tile to store
     for (;;) {
         if (!now.none) rest(now);
         ready(xa, ya, left + WS);
         if (!now.none) {
-            load(xb, yb);
+            load(xb, yb, 0, LOADS);
             loaded();
         }
         if (any) {
@@ -584,6 +513,162 @@ template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_k
     }
 }
 
+// What a workgroup knows of the experts: rows up to and with each one's, and its tiles or, of a weight gradient, experts by their rows.
+struct experts_table {
+    int32_t ends[TABLE], upto[TABLE];
+};
+
+template <int KIND, int SIZE> __device__ __forceinline__ void fill(experts_table &x, const params &p) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, rows = (int)p.rows;
+    int32_t before = 0, tiles = 0;
+    for (int e0 = 0; e0 < p.experts; e0 += 64) {  // each wave for itself, with the same values
+        const int e = e0 + lane;
+        int32_t end = e < p.experts ? min(max(p.ends[e], 0), rows) : 0;
+        end = max(max_before(end, lane), before);
+        int32_t begin = __shfl_up(end, 1);
+        if (lane == 0) begin = before;
+        const int32_t all = tiles + sum_before((int32_t)(((uint32_t)(end - begin) + SIZE - 1) / SIZE), lane);
+        if (e < p.experts && wave == 0) {
+            x.ends[e] = end;
+            if (KIND != WEIGHT_GRAD) x.upto[e] = all;
+        }
+        before = __builtin_amdgcn_readfirstlane(__shfl(end, 63));
+        tiles = __builtin_amdgcn_readfirstlane(__shfl(all, 63));
+    }
+    __syncthreads();
+    if (KIND != WEIGHT_GRAD) return;
+    // experts with most rows first, so that what is left in the end is short; of more than there are threads as they come
+    for (int e = threadIdx.x; e < p.experts; e += THREADS) {
+        int rank = e;
+        if (p.experts <= THREADS) {
+            const int mine = x.ends[e] - (e ? x.ends[e - 1] : 0);
+            rank = 0;
+            int begin = 0;
+            for (int i = 0; i < p.experts; ++i) {
+                const int end = x.ends[i], n = end - begin;
+                rank += n > mine || (n == mine && i < e);
+                begin = end;
+            }
+        }
+        x.upto[rank] = e;
+    }
+    __syncthreads();
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Rows of no expert: zeros.
+template <typename O> __device__ __forceinline__ void zero_rows(const params &p, int64_t first, int64_t behind) {
+    constexpr int E = 16 / sizeof(O);
+    const int64_t n = (behind - first) * (p.n_b / E);
+    u32x4 *out = (u32x4 *)((O *)p.out + first * p.n_b);
+    for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < n; i += (int64_t)gridDim.x * THREADS) out[i] = u32x4{0, 0, 0, 0};
+}
+
+// Tile (a_tile, b_tile) of the experts' tiles of SIZE, or a part of it: rows and columns from `down` and `across` on.  Its sum is 0 where
+// there are no outputs.
+template <int KIND, int SIZE>
+__device__ __forceinline__ wide_tile tile_of(const experts_table &x, const params &p, int rank, int a_tile, int b_tile, int down, int across) {
+    wide_tile t;
+    t.none = false;
+    t.col = b_tile * SIZE + across;
+    t.b_rows = p.n_b - t.col;
+    int expert = 0;
+    if (KIND == WEIGHT_GRAD) {
+        expert = uniform(x.upto[rank]);
+        const int begin = expert ? uniform(x.ends[expert - 1]) : 0, row = a_tile * SIZE + down;
+        t.sum = uniform(x.ends[expert]) - begin;
+        t.a_rows = p.n_a - row;
+        t.a = (const char *)p.a + ((int64_t)begin * p.a_stride + row) * 2;
+        t.b = (const char *)p.b + ((int64_t)begin * p.b_stride + t.col) * 2;
+        t.out = (int64_t)expert * p.n_a + row, t.row_end = (int64_t)(expert + 1) * p.n_a;
+    } else {
+        const int lane = threadIdx.x & 63;
+        for (int e0 = 0; e0 < p.experts; e0 += 64) {
+            const uint64_t found = __ballot(x.upto[min(e0 + lane, p.experts - 1)] > a_tile);
+            if (found) {
+                expert = e0 + (int)__builtin_ctzll(found);
+                break;
+            }
+        }
+        const int begin = expert ? uniform(x.ends[expert - 1]) : 0, end = uniform(x.ends[expert]);
+        const int64_t first = begin + (int64_t)(a_tile - (expert ? uniform(x.upto[expert - 1]) : 0)) * SIZE + down;
+        t.sum = p.sum;
+        t.a_rows = (int)(end - first);
+        t.a = (const char *)p.a + first * p.a_stride * 2;
+        t.b = (const char *)p.b + ((int64_t)expert * p.sum * p.n_b + (KIND == LINEAR ? (int64_t)t.col * p.sum : t.col)) * 2;
+        t.out = first, t.row_end = end;
+    }
+    if (t.a_rows <= 0 || t.b_rows <= 0) t.sum = 0;
+    return t;
+}
+
+// A weight gradient's tile of an expert without rows.
+template <int SIZE> __device__ __forceinline__ void zero_tile(const params &p, const wide_tile &t) {
+    for (int i = threadIdx.x; i < SIZE * SIZE / 4; i += THREADS) {
+        const int64_t row = t.out + i / (SIZE / 4);
+        const int col = t.col + i % (SIZE / 4) * 4;
+        if (row < t.row_end && col < p.n_b) *(u32x4 *)((float *)p.out + row * p.n_b + col) = u32x4{0, 0, 0, 0};
+    }
+}
+
+// Item i of a column strip's order: strips four tiles wide, so that neighbours share rows and columns.
+struct in_strips {
+    int a, b;
+    __device__ __forceinline__ in_strips(unsigned i, unsigned a_tiles, unsigned b_tiles) {
+        const unsigned strip = i / (4u * a_tiles), wide = min(4u, b_tiles - 4 * strip), in = i - strip * 4 * a_tiles;
+        a = (int)(in / wide), b = (int)(4 * strip + in % wide);
+    }
+};
+
+// Tiles of 256.  Items go to the eight XCDs in runs of 32, one for each of its CUs; of a weight gradient, whose tiles differ, every other round
+// backwards.  What fills a last round by half at most goes in quarters, tiles of 128: 256 of them take 0.38 of a round of tiles (sums of 4096:
+// 40 of 106 us), so that one or two rounds of quarters are ahead of a round, and three are not (12288 x 1024 x 4096 126 against 106 us).
+template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_kernel(params p) {
+    constexpr int BYTES = 256 * WS * 2;
+    __shared__ __attribute__((aligned(16))) char a0[BYTES], a1[BYTES], b0[BYTES], b1[BYTES], lines[THREADS / 64 * 4096];
+    __shared__ experts_table table;
+    fill<KIND, 256>(table, p);
+    const unsigned b_tiles = (unsigned)p.b_tiles, a_tiles = KIND == WEIGHT_GRAD ? (unsigned)p.a_tiles : (unsigned)uniform(table.upto[p.experts - 1]);
+    const unsigned per = a_tiles * b_tiles, items = KIND == WEIGHT_GRAD ? per * p.experts : per, over = items % CUS;
+    const unsigned whole = over <= CUS / 2 ? items - over : items;
+    if (KIND != WEIGHT_GRAD) zero_rows<bf16>(p, uniform(table.ends[p.experts - 1]), p.rows);
+    auto xa = (DEAR_LDS char *)a0, ya = (DEAR_LDS char *)b0, xb = (DEAR_LDS char *)a1, yb = (DEAR_LDS char *)b1;
+    unsigned round = 0;
+    run<KIND, 256>(p, xa, ya, xb, yb, (DEAR_LDS char *)lines, [&] {
+        wide_tile t;
+        for (;;) {
+            const unsigned in_round = blockIdx.x % 8 * 32 + blockIdx.x / 8;
+            const unsigned item = round * CUS + (KIND == WEIGHT_GRAD && round % 2 ? CUS - 1 - in_round : in_round);
+            t.none = round * CUS >= whole;
+            if (t.none) return t;
+            ++round;
+            if (item >= whole) continue;
+            const in_strips at(item % per, a_tiles, b_tiles);
+            t = tile_of<KIND, 256>(table, p, (int)(item / per), at.a, at.b, 0, 0);
+            if (t.sum > 0) return t;
+            zero_tile<256>(p, t);
+        }
+    });
+    if (whole == items) return;
+    __syncthreads();
+    round = 0;
+    run<KIND, 128>(p, xa, ya, xb, yb, (DEAR_LDS char *)lines, [&] {
+        wide_tile t;
+        for (;;) {
+            const unsigned item = round * CUS + blockIdx.x;
+            t.none = round * CUS >= 4 * over;
+            if (t.none) return t;
+            ++round;
+            if (item >= 4 * over) continue;
+            const in_strips at((whole + item / 4) % per, a_tiles, b_tiles);
+            t = tile_of<KIND, 256>(table, p, (int)((whole + item / 4) / per), at.a, at.b, (int)(item / 2 % 2) * 128, (int)(item % 2) * 128);
+            if (t.sum > 0) return t;
+            if (KIND == WEIGHT_GRAD && t.a_rows > 0 && t.b_rows > 0) zero_tile<128>(p, t);
+        }
+    });
+}
+
 // ------------------------------------------------------------------------------------ host
 constexpr int64_t MAX_ROWS = INT32_MAX;
 constexpr int32_t MAX_EXPERTS = 1 << 16, MAX_WIDTH = 1 << 20;
@@ -610,10 +695,10 @@ bool vectors(const dear_experts_t &x, const void *p, int64_t stride, int64_t wid
 // Whether the wide kernel takes a call: bf16 in whole vectors, with rows that 32-bit offsets reach, and enough of it.
 template <int KIND> bool wide(const dear_experts_t &x, bool vec, const params &p) {
     const int64_t most = 1 << 22;
-    if (x.dtype != DEAR_BF16 || !vec || !aligned(p.out, 16) || x.experts >= TABLE || p.n_b % 8 || p.a_stride >= most || p.b_stride >= most) return false;
-    const int64_t a_tiles = KIND == WEIGHT_GRAD ? ceil_div(x.outs, WT) * x.experts : x.rows / WT + x.experts + 1;
-    if (a_tiles * ceil_div(p.n_b, WT) > INT32_MAX / 2) return false;
-    return x.rows / x.experts >= WT / 2;
+    if (x.dtype != DEAR_BF16 || !vec || !aligned(p.out, 16) || x.experts > TABLE || p.n_b % 8 || p.a_stride >= most || p.b_stride >= most) return false;
+    const int64_t a_tiles = KIND == WEIGHT_GRAD ? ceil_div(x.outs, 256) * x.experts : x.rows / 256 + x.experts;
+    if (a_tiles * ceil_div(p.n_b, 256) > INT32_MAX / 8) return false;
+    return x.rows / x.experts >= 128;
 }
 
 template <int KIND> int64_t workspace_of(const dear_experts_t &) { return 0; }
@@ -648,9 +733,8 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
         vec = vectors(*x, p.a, p.a_stride, x->outs) && vectors(*x, p.b, p.b_stride, x->ins);
     }
     if (wide<KIND>(*x, vec, p)) {
-        p.a_tiles = (int32_t)(KIND == WEIGHT_GRAD ? ceil_div(x->outs, WT) : x->rows / WT + x->experts + 1);
-        p.b_tiles = (int32_t)ceil_div(p.n_b, WT);
-        experts_wide_kernel<KIND><<<WORKGROUPS, THREADS, 0, stream>>>(p);
+        p.a_tiles = (int32_t)ceil_div(p.n_a, 256), p.b_tiles = (int32_t)ceil_div(p.n_b, 256);
+        experts_wide_kernel<KIND><<<CUS, THREADS, 0, stream>>>(p);
         return launch_status();
     }
     // tiles of rows: each expert, and the rows behind the last, may have one that is not whole
