@@ -6,11 +6,12 @@
 // A stretch of steps is a map s -> A s + H with A the product of its a; two stretches in a row are again one:
 // (A2 A1, A2 H1 + H2).  Backward the map is e -> A e + E with the same A, from the last step to the first.  So a tile of
 // 256 steps is cut into strips of eight: a lane joins its own steps, lanes and waves join theirs, and a second
-// walk over the strip, from the state before it, gives the outputs; every tensor is read once.  The backward pass needs the
-// states before each step as well: it computes them again, in fp32, from the states that the forward pass kept at each tile's
-// first step, which takes less traffic than to read h, and no rounding.
+// walk over the strip, from the state before it, gives the outputs; every tensor is read once.  Where sequences and channels
+// alone do not fill the chip, each tile has a workgroup of its own, which tells the others its map and joins those of the tiles before
+// it.  The backward pass needs the states before each step as well: it computes them again, in fp32, from the states that the
+// forward pass kept at each tile's first step, which takes less traffic than to read h, and no rounding.
 //
-// HBM bounds it: 6 bytes of bf16 an element forward and 10 backward.
+// HBM bounds it, 6 bytes of bf16 an element forward and 10 backward, and the vector instructions come close to that.
 #include <type_traits>
 
 #include "ops_common.h"
@@ -41,17 +42,18 @@ struct params {
     const float *state, *dlast;
     float *last, *dstate, *kept;
     const int32_t *lens;
-    float *maps;  // of tiles that workgroups share a sequence's steps by: [batch, tiles + 1, 2, width]
+    uint32_t *ticket;   // workgroups that have begun, where they share a sequence's steps
+    uint64_t *maps;     // of their tiles, [batch, tiles, width]: A and H, or E, of the tiles in their order; at first all ones
     int64_t steps;
     int32_t width, groups, tiles;
 };
 
-// a = sigmoid(g) and b = 1 - a, each to full relative precision: from exp(-|g|), which neither overflows nor cancels.
+// a = sigmoid(g) and b = 1 - a, each to full relative precision: with t = exp(-g) they are 1 / (1 + t) and t / (1 + t), and t stops where
+// fp32 has no reciprocal of it.  A NaN stays one.
 __device__ __forceinline__ void gates(float g, float &a, float &b) {
-    const float t = __builtin_amdgcn_exp2f(__builtin_fabsf(g) * -1.44269504088896f);
-    const float big = __builtin_amdgcn_rcpf(1.f + t), small = t * big;
-    a = g >= 0.f ? big : small;
-    b = g >= 0.f ? small : big;
+    const float t = __builtin_amdgcn_exp2f(__builtin_elementwise_minimum(g * -1.44269504088896f, 126.f));
+    a = __builtin_amdgcn_rcpf(1.f + t);
+    b = t * a;
 }
 
 // Of a lane and the one at distance 16 or 32: the value of the earlier and of the later.
@@ -162,118 +164,123 @@ template <int MODE> __device__ __forceinline__ void store_state(float *row, cons
 }
 
 // The map of a tile's steps before the last wave has been joined: each wave's in LDS, [wave][A, H or E][channel].
-template <int W> using wave_maps = float[W][3][CG];
+template <int W> struct wave_maps_of { typedef float type[W][3][CG] __attribute__((aligned(16))); };
+template <int W> using wave_maps = typename wave_maps_of<W>::type;
 
-// State behind the tiles before `tile`, from the maps in memory: the first is that of the state before the first step.
-template <int MODE> __device__ __forceinline__ void fold_before(float *s, const params &a, int64_t b, int tile, int col) {
-    const float *m = a.maps + b * (a.tiles + 1) * 2 * a.width;
-    load_state<MODE>(s, m + a.width, col, a.width);
-    for (int i = 1; i <= tile; ++i) {
-        float A[N], H[N];
-        load_state<MODE>(A, m + (int64_t)i * 2 * a.width, col, a.width);
-        load_state<MODE>(H, m + ((int64_t)i * 2 + 1) * a.width, col, a.width);
+// s through a wave's map, of A and H (1) or E (2); one wave's after another, as all of them at once take registers.
+template <int WHICH, int W> __device__ __forceinline__ void pass(float *s, const wave_maps<W> &maps, int w, const place &p) {
+    const values<float> A = *(const values<float> *)&maps[w][0][p.lane % ROW_LANES * N], H = *(const values<float> *)&maps[w][WHICH][p.lane % ROW_LANES * N];
 #pragma unroll
-        for (int c = 0; c < N; ++c) s[c] = A[c] * s[c] + H[c];
-    }
-}
-// Backward: from the tiles behind `tile`; the last map is that of the gradient of the last state.
-template <int MODE> __device__ __forceinline__ void fold_behind(float *e, const params &a, int64_t b, int tile, int col) {
-    const float *m = a.maps + b * (a.tiles + 1) * 2 * a.width;
-    load_state<MODE>(e, m + ((int64_t)a.tiles * 2 + 1) * a.width, col, a.width);
-    for (int i = a.tiles - 1; i > tile; --i) {
-        float A[N], E[N];
-        load_state<MODE>(A, m + (int64_t)i * 2 * a.width, col, a.width);
-        load_state<MODE>(E, m + ((int64_t)i * 2 + 1) * a.width, col, a.width);
-#pragma unroll
-        for (int c = 0; c < N; ++c) e[c] = A[c] * e[c] + E[c];
-    }
+    for (int c = 0; c < N; ++c) s[c] = A[c] * s[c] + H[c];
+    __builtin_amdgcn_sched_barrier(0);
 }
 
-// Maps of single tiles, for sequences whose tiles go to workgroups of their own; the state before the first step, or the gradient
-// behind the last, becomes a map that forgets what was before it.
-template <typename T, int W, int MODE, bool BACKWARD> __global__ __launch_bounds__(64 * W) void maps_kernel(params a) {
-    __shared__ wave_maps<W> lds;
-    const int tile = (int)(blockIdx.x % a.tiles);
-    const place p(a, blockIdx.x / a.tiles, MODE);
-    const int valid = within(length(a, p.b), tile);
-    const rows_t &in = BACKWARD ? a.dh : a.x;
-    values<T> g[R] = {}, v[R] = {};
-    if (valid > 0) {
-        load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
-        load_strip<T, MODE>(v, in, tile, p, valid, a.width);
+constexpr uint64_t UNTOLD = ~(uint64_t)0;
+
+// What workgroups share, before they begin: maps, and a copy of the state that they start from, as its place may be the last one's too.
+__global__ __launch_bounds__(256) void untold_kernel(uint64_t *maps, int64_t n, uint32_t *ticket, const float *from, float *state, int64_t states) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) maps[i] = UNTOLD;
+    if (i < states) state[i] = from ? from[i] : 0.f;
+    if (i == 0) *ticket = 0;
+}
+
+// The workgroup's place among those that have begun: whoever has a smaller number has begun before, and tells its map without waiting for
+// anyone, so that every wait for a smaller number ends, in whatever order workgroups are started.
+__device__ __forceinline__ uint32_t take_ticket(uint32_t *ticket) {
+    __shared__ uint32_t mine;
+    if (threadIdx.x == 0) mine = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(mine);
+}
+
+// A map as one word, so that who reads it reads all of it, and needs no fence.
+__device__ __forceinline__ uint64_t *map_at(const params &a, int64_t b, int order, int col, int c) {
+    return a.maps + (b * a.tiles + order) * a.width + min(col + c, a.width - 1);
+}
+__device__ __forceinline__ void tell(const params &a, const place &p, int order, const float *A, const float *H) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        const uint32_t x = A[c] != A[c] ? 0x7fc00000u : __float_as_uint(A[c]);  // (some NaN is all ones)
+        __hip_atomic_store(map_at(a, p.b, order, p.col, c), (uint64_t)__float_as_uint(H[c]) << 32 | x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
+}
+
+// s through the maps of the tiles before `order`: strips take a run of tiles each, and are joined as a tile's are.  The order in which maps
+// are joined does not depend on when they are told.
+template <int W> __device__ __forceinline__ void through_earlier(float *s, const params &a, const place &p, int order, wave_maps<W> &maps) {
+    const int each = (order + W * STRIPS - 1) / (W * STRIPS), first = (p.wave * STRIPS + p.lane / ROW_LANES) * each;
     float A[N], H[N];
 #pragma unroll
-    for (int c = 0; c < N; ++c) {
-        A[c] = 1.f, H[c] = 0.f;
+    for (int c = 0; c < N; ++c) A[c] = 1.f, H[c] = 0.f;
+    for (int i = first; i < min(first + each, order); ++i) {
+        uint64_t x[N];
+        for (;;) {
+            bool told = true;
 #pragma unroll
-        for (int k = 0; k < R; ++k) {
-            const int r = BACKWARD ? R - 1 - k : k;
-            if (p.step + r < valid) {
-                float ga, gb;
-                gates((float)g[r][c], ga, gb);
-                A[c] *= ga;
-                H[c] = BACKWARD ? ga * ((float)v[r][c] + H[c]) : ga * H[c] + gb * (float)v[r][c];
+            for (int c = 0; c < N; ++c) {
+                x[c] = __hip_atomic_load(map_at(a, p.b, i, p.col, c), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                told = told && x[c] != UNTOLD;
             }
+            if (told) break;
+            __builtin_amdgcn_s_sleep(1);
         }
-        float x = 0.f, y = 0.f, z = 0.f;
-        join<16, !BACKWARD, BACKWARD>(A[c], H[c], H[c], x, y, z, x, p.lane);
-        join<32, !BACKWARD, BACKWARD>(A[c], H[c], H[c], x, y, z, x, p.lane);
-        if (p.lane < ROW_LANES) {
-            lds[p.wave][0][p.lane * N + c] = A[c];
-            lds[p.wave][1][p.lane * N + c] = H[c];
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            const float mine = __uint_as_float((uint32_t)x[c]);
+            H[c] = mine * H[c] + __uint_as_float((uint32_t)(x[c] >> 32));
+            A[c] *= mine;
         }
+    }
+    float none = 0.f;
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        join<16, true, false>(A[c], H[c], none, none, none, none, none, p.lane);
+        join<32, true, false>(A[c], H[c], none, none, none, none, none, p.lane);
+        if (p.lane < ROW_LANES) maps[p.wave][0][p.lane * N + c] = A[c], maps[p.wave][1][p.lane * N + c] = H[c];
     }
     __syncthreads();
-    if (threadIdx.x >= ROW_LANES) return;
-#pragma unroll
-    for (int c = 0; c < N; ++c) {
-        float sum_A = 1.f, sum_H = 0.f;
-#pragma unroll
-        for (int k = 0; k < W; ++k) {
-            const int w = BACKWARD ? W - 1 - k : k;
-            const float wa = lds[w][0][p.lane * N + c];
-            sum_H = wa * sum_H + lds[w][1][p.lane * N + c];
-            sum_A *= wa;
-        }
-        A[c] = sum_A, H[c] = sum_H;
-    }
-    float *m = a.maps + p.b * (a.tiles + 1) * 2 * a.width;
-    const int at = BACKWARD ? tile : tile + 1;
-    store_state<MODE>(m + (int64_t)at * 2 * a.width, A, p.col, a.width);
-    store_state<MODE>(m + ((int64_t)at * 2 + 1) * a.width, H, p.col, a.width);
-    if (tile == (BACKWARD ? a.tiles - 1 : 0)) {
-        const float *first = BACKWARD ? a.dlast : a.state;
-        float s[N] = {};
-        if (first) load_state<MODE>(s, first + p.b * a.width, p.col, a.width);
-        store_state<MODE>(m + ((int64_t)(BACKWARD ? a.tiles : 0) * 2 + 1) * a.width, s, p.col, a.width);
-    }
+    for (int w = 0; w < W; ++w) pass<1, W>(s, maps, w, p);
 }
 
-// A workgroup of W waves takes the tiles of a sequence's CG channels one after another or, where maps of tiles are there (SHARED),
-// one tile.
-template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W) void recurrence_kernel(params a) {
-    __shared__ wave_maps<W> lds[SHARED ? 1 : 2];
-    const place p(a, SHARED ? blockIdx.x / a.tiles : blockIdx.x, MODE);
-    const int first = SHARED ? (int)(blockIdx.x % a.tiles) : 0, behind = SHARED ? first + 1 : a.tiles;
+// Steps behind the last one: a = 1 and nothing added, by gates of infinity and values of 0.
+template <typename T> __device__ __forceinline__ void still(values<T> (&g)[R], values<T> (&x)[R], const place &p, int valid) {
+    const T open = (T)__builtin_inff();
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const bool in = p.step + r < valid;
+        g[r] = in ? g[r] : values<T>{open, open, open, open};
+        x[r] = in ? x[r] : values<T>{};
+    }
+}
+template <typename T> __device__ __forceinline__ void zero_behind(values<T> (&x)[R], const place &p, int valid) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) x[r] = p.step + r < valid ? x[r] : values<T>{};
+}
+
+// Workgroups that take a sequence's tiles one after another have two sets of maps: a wave that writes the next tile's has read those of the
+// tile before.  Those that share a sequence (SHARED) take one tile, and have the earlier tiles' maps in the second set.
+template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W, SHARED && sizeof(T) == 2 ? 4 : 2) void recurrence_kernel(params a) {
+    __shared__ wave_maps<W> lds[2];
+    const uint32_t id = SHARED ? take_ticket(a.ticket) : blockIdx.x, all = SHARED ? gridDim.x / a.tiles : 1;
+    const place p(a, SHARED ? id % all : id, MODE);
+    const int first = SHARED ? (int)(id / all) : 0, behind = SHARED ? first + 1 : a.tiles;
     const int64_t end = length(a, p.b);
     const bool speaks = threadIdx.x < ROW_LANES;  // stores states
     float carry[N] = {};
-    if (SHARED) fold_before<MODE>(carry, a, p.b, first, p.col);
-    else if (a.state) load_state<MODE>(carry, a.state + p.b * a.width, p.col, a.width);
+    if (a.state) load_state<MODE>(carry, a.state + p.b * a.width, p.col, a.width);
 #pragma clang loop unroll(disable)
     for (int tile = first; tile < behind; ++tile) {
         const int valid = within(end, tile), there = within(a.steps, tile);
-        if (speaks && a.kept) store_state<MODE>(a.kept + (p.b * a.tiles + tile) * a.width, carry, p.col, a.width);
         values<T> g[R], x[R];
-        if (valid == 0) {
+        if (valid > 0) {
+            load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
+            load_strip<T, MODE>(x, a.x, tile, p, valid, a.width);
+        } else {
 #pragma unroll
-            for (int r = 0; r < R; ++r) x[r] = values<T>{};
-            store_strip<T, MODE>(x, a.h, tile, p, there, a.width);
-            continue;
+            for (int r = 0; r < R; ++r) g[r] = x[r] = values<T>{};
         }
-        load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
-        load_strip<T, MODE>(x, a.x, tile, p, valid, a.width);
+        if (valid < WAVE_STEPS * W) still<T>(g, x, p, valid);
         auto &maps = lds[SHARED ? 0 : tile & 1];
         float ga[R][N], gx[R][N], before_A[N], before_H[N];
 #pragma unroll
@@ -284,68 +291,81 @@ template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__
                 float gb;
                 gates((float)g[r][c], ga[r][c], gb);
                 gx[r][c] = gb * (float)x[r][c];
-                if (p.step + r >= valid) ga[r][c] = 1.f, gx[r][c] = 0.f;  // the state stays
                 A *= ga[r][c];
                 H = ga[r][c] * H + gx[r][c];
             }
             before_A[c] = 1.f, before_H[c] = 0.f;
             join<16, true, false>(A, H, none, before_A[c], before_H[c], none, none, p.lane);
             join<32, true, false>(A, H, none, before_A[c], before_H[c], none, none, p.lane);
-            if (p.lane < ROW_LANES) {
-                maps[p.wave][0][p.lane * N + c] = A;
-                maps[p.wave][1][p.lane * N + c] = H;
-            }
+            if (p.lane < ROW_LANES) maps[p.wave][0][p.lane * N + c] = A, maps[p.wave][1][p.lane * N + c] = H;
             __builtin_amdgcn_sched_barrier(0);  // one channel after another: together they take registers that waves could have
         }
-        // two buffers: a wave that writes the next tile's maps has read these of the tile before
         __syncthreads();
+        if (SHARED) {
+            if (speaks && first + 1 < a.tiles) {
+                float A[N], H[N];
+#pragma unroll
+                for (int c = 0; c < N; ++c) {
+                    A[c] = 1.f, H[c] = 0.f;
+#pragma unroll
+                    for (int w = 0; w < W; ++w) {
+                        const float m = maps[w][0][p.lane * N + c];
+                        H[c] = m * H[c] + maps[w][1][p.lane * N + c];
+                        A[c] *= m;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                tell(a, p, tile, A, H);
+            }
+            if (tile > 0) through_earlier<W>(carry, a, p, tile, lds[1]);
+        }
+        if (speaks && a.kept) store_state<MODE>(a.kept + (p.b * a.tiles + tile) * a.width, carry, p.col, a.width);
         float s[N];
 #pragma unroll
-        for (int w = 0; w < W; ++w)
+        for (int w = 0; w < W; ++w) {
+            if (w == p.wave)
 #pragma unroll
-            for (int c = 0; c < N; ++c) {
-                if (w == p.wave) s[c] = carry[c];
-                carry[c] = maps[w][0][p.lane % ROW_LANES * N + c] * carry[c] + maps[w][1][p.lane % ROW_LANES * N + c];
-            }
+                for (int c = 0; c < N; ++c) s[c] = carry[c];
+            if (!SHARED || w < p.wave || (p.wave == 0 && tile == a.tiles - 1)) pass<1, W>(carry, maps, w, p);
+        }
 #pragma unroll
         for (int c = 0; c < N; ++c) s[c] = before_A[c] * s[c] + before_H[c];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
+        for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int c = 0; c < N; ++c) {
                 s[c] = ga[r][c] * s[c] + gx[r][c];
-                x[r][c] = p.step + r < valid ? (T)s[c] : (T)0.f;
+                x[r][c] = (T)s[c];
             }
-        }
+        if (valid < there) zero_behind<T>(x, p, valid);
         store_strip<T, MODE>(x, a.h, tile, p, there, a.width);
     }
     if (speaks && a.last && behind == a.tiles) store_state<MODE>(a.last + p.b * a.width, carry, p.col, a.width);
 }
 
 // As above, from the last tile to the first; the states before the tile's steps come from the kept one.
-template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W) void recurrence_backward_kernel(params a) {
-    __shared__ wave_maps<W> lds[SHARED ? 1 : 2];
-    const place p(a, SHARED ? blockIdx.x / a.tiles : blockIdx.x, MODE);
-    const int first = SHARED ? (int)(blockIdx.x % a.tiles) : 0, last = SHARED ? first : a.tiles - 1;
+template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W, SHARED && sizeof(T) == 2 ? 4 : 2) void recurrence_backward_kernel(params a) {
+    __shared__ wave_maps<W> lds[2];
+    const uint32_t id = SHARED ? take_ticket(a.ticket) : blockIdx.x, all = SHARED ? gridDim.x / a.tiles : 1;
+    const place p(a, SHARED ? id % all : id, MODE);
+    const int order = SHARED ? (int)(id / all) : 0, last = a.tiles - 1 - order, first = SHARED ? last : 0;
     const int64_t end = length(a, p.b);
     const bool speaks = threadIdx.x < ROW_LANES;
     float carry[N] = {};
-    if (SHARED) fold_behind<MODE>(carry, a, p.b, last, p.col);
-    else if (a.dlast) load_state<MODE>(carry, a.dlast + p.b * a.width, p.col, a.width);
+    if (a.dlast) load_state<MODE>(carry, a.dlast + p.b * a.width, p.col, a.width);
 #pragma clang loop unroll(disable)
     for (int tile = last; tile >= first; --tile) {
         const int valid = within(end, tile), there = within(a.steps, tile);
         values<T> g[R], x[R], dh[R];
-        if (valid == 0) {
+        if (valid > 0) {
+            load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
+            load_strip<T, MODE>(x, a.x, tile, p, valid, a.width);
+            load_strip<T, MODE>(dh, a.dh, tile, p, valid, a.width);
+        } else {
 #pragma unroll
-            for (int r = 0; r < R; ++r) x[r] = values<T>{};
-            store_strip<T, MODE>(x, a.dx, tile, p, there, a.width);
-            store_strip<T, MODE>(x, a.dgate, tile, p, there, a.width);
-            continue;
+            for (int r = 0; r < R; ++r) g[r] = x[r] = dh[r] = values<T>{};
         }
-        load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
-        load_strip<T, MODE>(x, a.x, tile, p, valid, a.width);
-        load_strip<T, MODE>(dh, a.dh, tile, p, valid, a.width);
+        if (valid < WAVE_STEPS * W) still<T>(g, x, p, valid), zero_behind<T>(dh, p, valid);
         float s[N];
         load_state<MODE>(s, a.kept + (p.b * a.tiles + tile) * a.width, p.col, a.width);
         auto &maps = lds[SHARED ? 0 : tile & 1];
@@ -357,13 +377,11 @@ template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__
             for (int r = 0; r < R; ++r) {
                 float gb;
                 gates((float)g[r][c], ga[r], gb);
-                float gx = gb * (float)x[r][c];
-                if (p.step + r >= valid) ga[r] = 1.f, gx = 0.f;
                 A *= ga[r];
-                H = ga[r] * H + gx;
+                H = ga[r] * H + gb * (float)x[r][c];
             }
 #pragma unroll
-            for (int r = R - 1; r >= 0; --r) E = ga[r] * ((p.step + r < valid ? (float)dh[r][c] : 0.f) + E);
+            for (int r = R - 1; r >= 0; --r) E = ga[r] * E + ga[r] * (float)dh[r][c];
             before_A[c] = behind_A[c] = 1.f, before_H[c] = behind_E[c] = 0.f;
             join<16, true, true>(A, H, E, before_A[c], before_H[c], behind_A[c], behind_E[c], p.lane);
             join<32, true, true>(A, H, E, before_A[c], before_H[c], behind_A[c], behind_E[c], p.lane);
@@ -375,46 +393,72 @@ template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__
             __builtin_amdgcn_sched_barrier(0);
         }
         __syncthreads();
+        if (SHARED) {
+            if (speaks && first > 0) {
+                float A[N], E[N];
+#pragma unroll
+                for (int c = 0; c < N; ++c) {
+                    A[c] = 1.f, E[c] = 0.f;
+#pragma unroll
+                    for (int w = W - 1; w >= 0; --w) {
+                        const float m = maps[w][0][p.lane * N + c];
+                        E[c] = m * E[c] + maps[w][2][p.lane * N + c];
+                        A[c] *= m;
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                tell(a, p, order, A, E);
+            }
+            if (order > 0) through_earlier<W>(carry, a, p, order, lds[1]);
+        }
         float e[N];
 #pragma unroll
-        for (int w = W - 1; w >= 0; --w)
+        for (int w = W - 1; w >= 0; --w) {
+            if (w == p.wave)
 #pragma unroll
-            for (int c = 0; c < N; ++c) {
-                if (w == p.wave) e[c] = carry[c];
-                carry[c] = maps[w][0][p.lane % ROW_LANES * N + c] * carry[c] + maps[w][2][p.lane % ROW_LANES * N + c];
-            }
+                for (int c = 0; c < N; ++c) e[c] = carry[c];
+            if (!SHARED || w > p.wave || (p.wave == 0 && tile == 0)) pass<2, W>(carry, maps, w, p);
+        }
 #pragma unroll
         for (int w = 0; w < W - 1; ++w)
-            if (w < p.wave)
-#pragma unroll
-                for (int c = 0; c < N; ++c) s[c] = maps[w][0][p.lane % ROW_LANES * N + c] * s[c] + maps[w][1][p.lane % ROW_LANES * N + c];
-        // the gates are computed again, channel by channel: kept from above they would take 64 registers
-        values<T> dx[R], dg[R];
+            if (w < p.wave) pass<1, W>(s, maps, w, p);
+        // the gates are computed again, channel by channel, and the gradients take the inputs' places: kept from above they would take 64 registers
 #pragma unroll
         for (int r = 0; r < R; ++r) asm("" : "+v"(g[r]), "+v"(x[r]), "+v"(dh[r]));
 #pragma unroll
-        for (int c = 0; c < N; ++c) {
-            s[c] = before_A[c] * s[c] + before_H[c];
-            e[c] = behind_A[c] * e[c] + behind_E[c];
-            float ga[R], gb[R], q[R];
+        for (int c0 = 0; c0 < N; c0 += 2) {
+            float dx[2][R], dg[2][R];
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                gates((float)g[r][c], ga[r], gb[r]);
-                q[r] = (s[c] - (float)x[r][c]) * ga[r] * gb[r];
-                s[c] = ga[r] * s[c] + gb[r] * (float)x[r][c];  // (behind the last step not used)
+            for (int k = 0; k < 2; ++k) {
+                const int c = c0 + k;
+                s[c] = before_A[c] * s[c] + before_H[c];
+                e[c] = behind_A[c] * e[c] + behind_E[c];
+                float ga[R], gb[R], q[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    gates((float)g[r][c], ga[r], gb[r]);
+                    q[r] = (s[c] - (float)x[r][c]) * ga[r];
+                    s[c] = ga[r] * s[c] + gb[r] * (float)x[r][c];
+                }
+#pragma unroll
+                for (int r = R - 1; r >= 0; --r) {
+                    const float G = (float)dh[r][c] + e[c];
+                    dx[k][r] = gb[r] * G;
+                    dg[k][r] = q[r] * dx[k][r];
+                    e[c] = ga[r] * G;
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-            for (int r = R - 1; r >= 0; --r) {
-                const bool in = p.step + r < valid;
-                const float G = (float)dh[r][c] + e[c];
-                dx[r][c] = in ? (T)(gb[r] * G) : (T)0.f;
-                dg[r][c] = in ? (T)(q[r] * G) : (T)0.f;
-                e[c] = in ? ga[r] * G : e[c];
+            for (int r = 0; r < R; ++r) {
+                x[r][c0] = (T)dx[0][r], x[r][c0 + 1] = (T)dx[1][r];
+                g[r][c0] = (T)dg[0][r], g[r][c0 + 1] = (T)dg[1][r];
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        store_strip<T, MODE>(dx, a.dx, tile, p, there, a.width);
-        store_strip<T, MODE>(dg, a.dgate, tile, p, there, a.width);
+        if (valid < there) zero_behind<T>(x, p, valid), zero_behind<T>(g, p, valid);
+        store_strip<T, MODE>(x, a.dx, tile, p, there, a.width);
+        store_strip<T, MODE>(g, a.dgate, tile, p, there, a.width);
     }
     if (speaks && a.dstate && first == 0) store_state<MODE>(a.dstate + p.b * a.width, carry, p.col, a.width);
 }
@@ -429,9 +473,10 @@ int size_of(int32_t dtype) { return dtype == DEAR_BF16 ? 2 : 4; }
 // Channels of a workgroup.
 int64_t groups_of(const dear_recurrence_t &r) { return ceil_div(r.width, CG); }
 
-// Whether the tiles of a sequence go to workgroups of their own, which takes a launch more and reads the inputs twice (backward two of
-// three): where there are several tiles and the sequences' channels alone do not fill the chip.
+// Whether the tiles of a sequence go to workgroups of their own, which takes a launch more: where there are several tiles and the sequences'
+// channels alone do not fill the chip.
 bool shares(const dear_recurrence_t &r) { return r.steps > KEPT && r.batch * groups_of(r) < 512; }
+constexpr int64_t TICKET_BYTES = 256;
 
 int check(const dear_recurrence_t *r) {
     if (!r || (r->dtype != DEAR_F32 && r->dtype != DEAR_BF16) || r->batch < 0 || r->steps < 0 || r->steps > MAX_STEPS) return DEAR_EINVAL;
@@ -460,7 +505,7 @@ int check_tensor(const dear_recurrence_t &r, const dear_steps_t &t, bool written
 }
 
 int64_t workspace_of(const dear_recurrence_t &r) {
-    return r.batch && shares(r) ? (int64_t)r.batch * (ceil_div(r.steps, KEPT) + 1) * 2 * r.width * 4 : 0;
+    return r.batch && shares(r) ? TICKET_BYTES + (int64_t)r.batch * (ceil_div(r.steps, KEPT) + 1) * r.width * 8 : 0;
 }
 
 bool vectors(const dear_recurrence_t &r, const dear_steps_t &t) {
@@ -500,18 +545,22 @@ __global__ __launch_bounds__(256) void copy_state_kernel(const float *from, floa
     if (i < n) to[i] = from ? from[i] : 0.f;
 }
 
-template <typename T, int MODE, bool BACKWARD> void launch(const params &a, int64_t groups, bool shared, hipStream_t stream) {
+template <typename T, int MODE, bool BACKWARD> void launch(params a, int64_t batch, bool shared, void *workspace, hipStream_t stream) {
+    const int64_t groups = batch * a.groups;
     auto by_waves = [&](auto waves) {
         constexpr int W = decltype(waves)::value;
         if (BACKWARD) recurrence_backward_kernel<T, W, MODE, false><<<(unsigned)groups, 64 * W, 0, stream>>>(a);
         else recurrence_kernel<T, W, MODE, false><<<(unsigned)groups, 64 * W, 0, stream>>>(a);
     };
     if (shared) {
-        constexpr int W = WAVES;
-        const unsigned n = (unsigned)(groups * a.tiles);
-        maps_kernel<T, W, MODE, BACKWARD><<<n, 64 * W, 0, stream>>>(a);
-        if (BACKWARD) recurrence_backward_kernel<T, W, MODE, true><<<n, 64 * W, 0, stream>>>(a);
-        else recurrence_kernel<T, W, MODE, true><<<n, 64 * W, 0, stream>>>(a);
+        const int64_t states = batch * a.width, n = states * a.tiles;
+        a.ticket = (uint32_t *)workspace, a.maps = (uint64_t *)((char *)workspace + TICKET_BYTES);
+        float *copy = (float *)(a.maps + n);
+        untold_kernel<<<(unsigned)ceil_div(n, 256), 256, 0, stream>>>(a.maps, n, a.ticket, BACKWARD ? a.dlast : a.state, copy, states);
+        a.state = a.dlast = copy;
+        const unsigned all = (unsigned)(groups * a.tiles);
+        if (BACKWARD) recurrence_backward_kernel<T, WAVES, MODE, true><<<all, 64 * WAVES, 0, stream>>>(a);
+        else recurrence_kernel<T, WAVES, MODE, true><<<all, 64 * WAVES, 0, stream>>>(a);
     } else if (a.steps <= WAVE_STEPS) {
         by_waves(std::integral_constant<int, 1>());
     } else if (a.steps <= 3 * WAVE_STEPS) {
@@ -537,16 +586,15 @@ int call(const dear_recurrence_t *r, bool backward, hipStream_t stream) {
     params a = {};
     a.x = rows(r->x), a.gate = rows(r->gate), a.h = rows(r->h), a.dh = rows(r->dh), a.dx = rows(r->dx), a.dgate = rows(r->dgate);
     a.state = r->state, a.dlast = r->dlast, a.last = r->last, a.dstate = r->dstate, a.kept = r->kept, a.lens = r->lens;
-    a.maps = (float *)r->workspace, a.steps = r->steps, a.width = r->width;
-    const int64_t groups = groups_of(*r) * r->batch;
+    a.steps = r->steps, a.width = r->width;
     a.groups = (int32_t)groups_of(*r), a.tiles = (int32_t)ceil_div(r->steps, KEPT);
     bool vec = r->width % N == 0 && vectors(*r, r->x) && vectors(*r, r->gate);
     vec = vec && (backward ? vectors(*r, r->dh) && vectors(*r, r->dx) && vectors(*r, r->dgate) : vectors(*r, r->h));
     vec = vec && aligned(r->state, 16) && aligned(r->last, 16) && aligned(r->kept, 16) && aligned(r->dlast, 16) && aligned(r->dstate, 16);
     auto by_mode = [&](auto t, auto mode) {
         typedef decltype(t) T;
-        if (backward) launch<T, decltype(mode)::value, true>(a, groups, shares(*r), stream);
-        else launch<T, decltype(mode)::value, false>(a, groups, shares(*r), stream);
+        if (backward) launch<T, decltype(mode)::value, true>(a, r->batch, shares(*r), r->workspace, stream);
+        else launch<T, decltype(mode)::value, false>(a, r->batch, shares(*r), r->workspace, stream);
     };
     auto by_type = [&](auto t) {
         if (vec) by_mode(t, std::integral_constant<int, ALIGNED>());
