@@ -212,8 +212,7 @@ typedef struct {
 
 /* Tensors are aligned to their element types (16 bytes, with strides and widths to match, are faster).
  * Errors: DEAR_EINVAL, DEAR_EALIGN, DEAR_EHIP; DEAR_ETOOBIG where workspace_bytes is less than the call needs, or where a
- * launch would have 2^32 threads or more: 512 for every 64 channels (fp32: 32) of a sequence or, where there are less than
- * 512 such groups, of every 256 steps. */
+ * launch would have 2^32 threads or more: 512 for every 64 channels of every 256 steps of a sequence. */
 int dear_recurrence(const dear_recurrence_t *args, void *hip_stream);
 int dear_recurrence_backward(const dear_recurrence_t *args, void *hip_stream);
 /* Bytes of workspace that either call with these sizes needs (pointers and strides are not looked at). */

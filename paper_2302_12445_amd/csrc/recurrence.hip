@@ -5,7 +5,7 @@
 //
 // A stretch of steps is a map s -> A s + H with A the product of its a; two stretches in a row are again one:
 // (A2 A1, A2 H1 + H2).  Backward the map is e -> A e + E with the same A, from the last step to the first.  So a tile of
-// 256 steps is cut into strips of eight: a lane joins its own steps, lanes and waves join theirs, and a second
+// 256 steps is cut into strips of sixteen: a lane joins its own steps, lanes and waves join theirs, and a second
 // walk over the strip, from the state before it, gives the outputs; every tensor is read once.  Where sequences and channels
 // alone do not fill the chip, each tile has a workgroup of its own, which tells the others its map and joins those of the tiles before
 // it.  The backward pass needs the states before each step as well: it computes them again, in fp32, from the states that the
@@ -23,9 +23,9 @@ namespace {
 using namespace dear_ops;
 
 constexpr int KEPT = DEAR_RECURRENCE_KEPT;  // steps from one kept state to the next: a whole tile
-constexpr int R = 8;                        // steps of a lane's strip
-constexpr int N = 4;                        // channels of a lane
-constexpr int ROW_LANES = 16;               // lanes across the channels; the wave's other axis is time, four strips
+constexpr int R = 16;                       // steps of a lane's strip
+constexpr int N = 2;                        // channels of a lane
+constexpr int ROW_LANES = 32;               // lanes across the channels; the halves of a wave are two strips
 constexpr int STRIPS = 64 / ROW_LANES;
 constexpr int WAVE_STEPS = STRIPS * R;
 constexpr int CG = N * ROW_LANES;           // channels of a workgroup: in bf16 128 bytes of a row, a line of the cache
@@ -42,7 +42,7 @@ struct params {
     const float *state, *dlast;
     float *last, *dstate, *kept;
     const int32_t *lens;
-    uint32_t *ticket;   // workgroups that have begun, where they share a sequence's steps
+    uint32_t *tickets;  // workgroups that have begun of those that share a sequence's channels, one count a line of the cache
     uint64_t *maps;     // of their tiles, [batch, tiles, width]: A and H, or E, of the tiles in their order; at first all ones
     int64_t steps;
     int32_t width, groups, tiles;
@@ -56,32 +56,32 @@ __device__ __forceinline__ void gates(float g, float &a, float &b) {
     b = t * a;
 }
 
-// Of a lane and the one at distance 16 or 32: the value of the earlier and of the later.
-template <int D> __device__ __forceinline__ void neighbours(float x, float &earlier, float &later) {
+// The halves' values of x: the earlier strip's and the later one's.
+__device__ __forceinline__ void halves(float x, float &earlier, float &later) {
     const uint32_t u = __float_as_uint(x);
-    auto w = D == 16 ? __builtin_amdgcn_permlane16_swap(u, u, false, false) : __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    auto w = __builtin_amdgcn_permlane32_swap(u, u, false, false);
     earlier = __uint_as_float(w[0]), later = __uint_as_float(w[1]);
 }
 
-// One level of joining the strips of a wave.  A, H, E: the map of the lane's block of strips, which becomes that of the block twice
-// as long.  before: the map from the block's first step to the lane's, behind: backward from the block's last step to the lane's.
-template <int D, bool FORWARD, bool BACKWARD>
+// Joins the strips of a wave.  A, H, E: the map of the lane's strip, which becomes the wave's.  before: the map from the wave's first step to
+// the strip's, behind: backward from the wave's last step to the strip's.
+template <bool FORWARD, bool BACKWARD>
 __device__ __forceinline__ void join(float &A, float &H, float &E, float &before_A, float &before_H, float &behind_A, float &behind_E, int lane) {
     float A0, A1;
-    neighbours<D>(A, A0, A1);
-    const bool later = lane & D;
+    halves(A, A0, A1);
+    const bool later = lane & 32;
     if (FORWARD) {
         float H0, H1;
-        neighbours<D>(H, H0, H1);
-        before_H = later ? before_A * H0 + before_H : before_H;
-        before_A = later ? before_A * A0 : before_A;
+        halves(H, H0, H1);
+        before_A = later ? A0 : 1.f;
+        before_H = later ? H0 : 0.f;
         H = A1 * H0 + H1;
     }
     if (BACKWARD) {
         float E0, E1;
-        neighbours<D>(E, E0, E1);
-        behind_E = later ? behind_E : behind_A * E1 + behind_E;
-        behind_A = later ? behind_A : behind_A * A1;
+        halves(E, E0, E1);
+        behind_A = later ? 1.f : A1;
+        behind_E = later ? 0.f : E1;
         E = A0 * E1 + E0;
     }
     A = A0 * A1;
@@ -108,24 +108,36 @@ __device__ __forceinline__ int64_t length(const params &a, int64_t b) {
     return a.lens ? min(max((int64_t)a.lens[b], (int64_t)0), a.steps) : a.steps;
 }
 
-template <typename T> struct four { typedef T type __attribute__((ext_vector_type(N))); };
-template <typename T> using values = typename four<T>::type;
-template <typename T> struct four_anywhere { typedef values<T> type __attribute__((aligned(sizeof(T)))); };  // global memory takes it
+// A lane's channels of a step as they are in memory, in whole registers: two values of bf16 are one.
+typedef uint32_t u32;
+template <typename T> struct raw_of { typedef u32 type; };
+template <> struct raw_of<float> { typedef f32x2 type; };
+template <typename T> using raw = typename raw_of<T>::type;
+template <typename R> struct anywhere_of { typedef R type __attribute__((aligned(2))); };  // global memory takes it
+template <> struct anywhere_of<f32x2> { typedef f32x2 type __attribute__((aligned(4))); };
 
-template <typename T, int MODE> __device__ __forceinline__ values<T> load(const T *row, int col, int cols) {
-    if (MODE == ALIGNED) return *(const values<T> *)(row + col);
-    if (MODE == ANYWHERE) return *(const typename four_anywhere<T>::type *)(row + col);
-    values<T> v;
-#pragma unroll
-    for (int c = 0; c < N; ++c) v[c] = row[min(col + c, cols - 1)];
-    return v;
+__device__ __forceinline__ float get(u32 x, int c) { return __uint_as_float(c ? x & 0xffff0000u : x << 16); }
+__device__ __forceinline__ float get(f32x2 x, int c) { return x[c]; }
+// To bf16 rounded to nearest, halves to even.
+template <typename T> __device__ __forceinline__ raw<T> both(float x, float y) {
+    if constexpr (sizeof(T) == 2) return __builtin_bit_cast(u32, bf16x2{(bf16)x, (bf16)y});
+    else return f32x2{x, y};
 }
-template <typename T, int MODE> __device__ __forceinline__ void store(T *row, values<T> v, int col, int cols) {
-    if (MODE == ALIGNED) *(values<T> *)(row + col) = v;
-    else if (MODE == ANYWHERE) *(typename four_anywhere<T>::type *)(row + col) = v;
+
+// at: the row, or bytes before it that are the same for the whole workgroup, and off the others.
+template <typename T, int MODE> __device__ __forceinline__ raw<T> load(const char *at, uint32_t off, int col, int cols) {
+    if (MODE == ALIGNED) return *(const raw<T> *)(at + (off + (uint32_t)(col * (int)sizeof(T))));
+    if (MODE == ANYWHERE) return *(const typename anywhere_of<raw<T>>::type *)(at + (off + (uint32_t)(col * (int)sizeof(T))));
+    const T x = *(const T *)(at + (off + (uint32_t)(min(col, cols - 1) * (int)sizeof(T))));
+    const T y = *(const T *)(at + (off + (uint32_t)(min(col + 1, cols - 1) * (int)sizeof(T))));
+    return both<T>((float)x, (float)y);
+}
+template <typename T, int MODE> __device__ __forceinline__ void store(char *at, uint32_t off, raw<T> v, int col, int cols) {
+    if (MODE == ALIGNED) *(raw<T> *)(at + (off + (uint32_t)(col * (int)sizeof(T)))) = v;
+    else if (MODE == ANYWHERE) *(typename anywhere_of<raw<T>>::type *)(at + (off + (uint32_t)(col * (int)sizeof(T)))) = v;
     else
 #pragma unroll
-        for (int c = 0; c < N; ++c) row[min(col + c, cols - 1)] = v[c];
+        for (int c = 0; c < N; ++c) *(T *)(at + (off + (uint32_t)(min(col + c, cols - 1) * (int)sizeof(T)))) = (T)get(v, c);
 }
 
 // Of a tensor the R rows of a lane's strip in a tile that starts at `at` (the same for the whole workgroup, so that a lane's address is
@@ -134,19 +146,29 @@ template <typename T> __device__ __forceinline__ char *tile_at(const rows_t &t, 
     return (char *)t.data + (b * t.batch_stride + (int64_t)tile * KEPT * t.step_stride) * (int64_t)sizeof(T);
 }
 template <typename T, int MODE>
-__device__ __forceinline__ void load_strip(values<T> (&v)[R], const rows_t &from, int tile, const place &p, int valid, int cols) {
+__device__ __forceinline__ void load_strip(raw<T> (&v)[R], const rows_t &from, int tile, const place &p, int valid, int cols) {
     const char *at = tile_at<T>(from, p.b, tile);
-    const uint32_t stride = (uint32_t)from.step_stride * (uint32_t)sizeof(T);
+    const uint32_t stride = (uint32_t)from.step_stride * (uint32_t)sizeof(T), last = (uint32_t)(valid - 1) * stride, off = (uint32_t)p.step * stride;
+    if (valid == KEPT) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) v[r] = load<T, MODE>((const T *)(at + (uint32_t)min(p.step + r, valid - 1) * stride), p.col, cols);
+        for (int r = 0; r < R; ++r) v[r] = load<T, MODE>(at + (int64_t)r * stride, off, p.col, cols);
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r) v[r] = load<T, MODE>(at, min(off + (uint32_t)r * stride, last), p.col, cols);
+    }
 }
 template <typename T, int MODE>
-__device__ __forceinline__ void store_strip(const values<T> (&v)[R], const rows_t &to, int tile, const place &p, int there, int cols) {
+__device__ __forceinline__ void store_strip(const raw<T> (&v)[R], const rows_t &to, int tile, const place &p, int there, int cols) {
     char *at = tile_at<T>(to, p.b, tile);
-    const uint32_t stride = (uint32_t)to.step_stride * (uint32_t)sizeof(T);
+    const uint32_t stride = (uint32_t)to.step_stride * (uint32_t)sizeof(T), off = (uint32_t)p.step * stride;
+    if (there == KEPT) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-        if (p.step + r < there) store<T, MODE>((T *)(at + (uint32_t)(p.step + r) * stride), v[r], p.col, cols);
+        for (int r = 0; r < R; ++r) store<T, MODE>(at + (int64_t)r * stride, off, v[r], p.col, cols);
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            if (p.step + r < there) store<T, MODE>(at + (int64_t)r * stride, off, v[r], p.col, cols);
+    }
 }
 // Of the steps left from a tile's first on, those within it.
 __device__ __forceinline__ int within(int64_t steps, int tile) {
@@ -155,12 +177,12 @@ __device__ __forceinline__ int within(int64_t steps, int tile) {
 
 // A row of states.
 template <int MODE> __device__ __forceinline__ void load_state(float *s, const float *row, int col, int cols) {
-    const values<float> v = load<float, MODE>(row, col, cols);
+    const f32x2 v = load<float, MODE>((const char *)row, 0, col, cols);
 #pragma unroll
     for (int c = 0; c < N; ++c) s[c] = v[c];
 }
 template <int MODE> __device__ __forceinline__ void store_state(float *row, const float *s, int col, int cols) {
-    store<float, MODE>(row, values<float>{s[0], s[1], s[2], s[3]}, col, cols);
+    store<float, MODE>((char *)row, 0, f32x2{s[0], s[1]}, col, cols);
 }
 
 // The map of a tile's steps before the last wave has been joined: each wave's in LDS, [wave][A, H or E][channel].
@@ -169,29 +191,39 @@ template <int W> using wave_maps = typename wave_maps_of<W>::type;
 
 // s through a wave's map, of A and H (1) or E (2); one wave's after another, as all of them at once take registers.
 template <int WHICH, int W> __device__ __forceinline__ void pass(float *s, const wave_maps<W> &maps, int w, const place &p) {
-    const values<float> A = *(const values<float> *)&maps[w][0][p.lane % ROW_LANES * N], H = *(const values<float> *)&maps[w][WHICH][p.lane % ROW_LANES * N];
+    const f32x2 A = *(const f32x2 *)&maps[w][0][p.lane % ROW_LANES * N], H = *(const f32x2 *)&maps[w][WHICH][p.lane % ROW_LANES * N];
 #pragma unroll
     for (int c = 0; c < N; ++c) s[c] = A[c] * s[c] + H[c];
     __builtin_amdgcn_sched_barrier(0);
 }
 
 constexpr uint64_t UNTOLD = ~(uint64_t)0;
+constexpr int TICKET = 32;  // counts of workgroups lie 128 bytes apart
 
 // What workgroups share, before they begin: maps, and a copy of the state that they start from, as its place may be the last one's too.
-__global__ __launch_bounds__(256) void untold_kernel(uint64_t *maps, int64_t n, uint32_t *ticket, const float *from, float *state, int64_t states) {
+__global__ __launch_bounds__(256) void untold_kernel(uint64_t *maps, int64_t n, uint32_t *tickets, const float *from, float *state, int64_t states,
+                                                     int64_t counts) {
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i < n) maps[i] = UNTOLD;
     if (i < states) state[i] = from ? from[i] : 0.f;
-    if (i == 0) *ticket = 0;
+    if (i < counts) tickets[i * TICKET] = 0;
 }
 
-// The workgroup's place among those that have begun: whoever has a smaller number has begun before, and tells its map without waiting for
-// anyone, so that every wait for a smaller number ends, in whatever order workgroups are started.
-__device__ __forceinline__ uint32_t take_ticket(uint32_t *ticket) {
+// The workgroup's place among those that have begun on the same channels, which is its tile: whoever has a smaller number has begun before,
+// and tells its map without waiting for anyone, so that every wait for a smaller number ends, in whatever order workgroups are started.
+__device__ __forceinline__ int take_ticket(uint32_t *ticket) {
     __shared__ uint32_t mine;
     if (threadIdx.x == 0) mine = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    return __builtin_amdgcn_readfirstlane(mine);
+    return (int)__builtin_amdgcn_readfirstlane(mine);
+}
+
+// The sequence and channels of a workgroup that shares them: neighbours take neighbouring channels, and the next row of workgroups is turned
+// by one, so that an XCD (every eighth workgroup) does not keep to some channels of all rows, which a part of its cache would have to serve (1 x
+// 32768 x 512 45 us, so 34).
+__device__ __forceinline__ uint32_t turned_group(const params &a) {
+    const uint32_t all = gridDim.x / a.tiles;
+    return (blockIdx.x + blockIdx.x / all) % all;
 }
 
 // A map as one word, so that who reads it reads all of it, and needs no fence.
@@ -235,8 +267,7 @@ template <int W> __device__ __forceinline__ void through_earlier(float *s, const
     float none = 0.f;
 #pragma unroll
     for (int c = 0; c < N; ++c) {
-        join<16, true, false>(A[c], H[c], none, none, none, none, none, p.lane);
-        join<32, true, false>(A[c], H[c], none, none, none, none, none, p.lane);
+        join<true, false>(A[c], H[c], none, none, none, none, none, p.lane);
         if (p.lane < ROW_LANES) maps[p.wave][0][p.lane * N + c] = A[c], maps[p.wave][1][p.lane * N + c] = H[c];
     }
     __syncthreads();
@@ -244,223 +275,205 @@ template <int W> __device__ __forceinline__ void through_earlier(float *s, const
 }
 
 // Steps behind the last one: a = 1 and nothing added, by gates of infinity and values of 0.
-template <typename T> __device__ __forceinline__ void still(values<T> (&g)[R], values<T> (&x)[R], const place &p, int valid) {
-    const T open = (T)__builtin_inff();
+template <typename T> __device__ __forceinline__ void still(raw<T> (&g)[R], raw<T> (&x)[R], const place &p, int valid) {
+    asm volatile("");  // in a branch of its own: whole tiles are to pass it by
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const bool in = p.step + r < valid;
-        g[r] = in ? g[r] : values<T>{open, open, open, open};
-        x[r] = in ? x[r] : values<T>{};
+        g[r] = in ? g[r] : both<T>(__builtin_inff(), __builtin_inff());
+        x[r] = in ? x[r] : raw<T>{};
     }
 }
-template <typename T> __device__ __forceinline__ void zero_behind(values<T> (&x)[R], const place &p, int valid) {
+template <typename T> __device__ __forceinline__ void zero_behind(raw<T> (&x)[R], const place &p, int valid) {
+    asm volatile("");
 #pragma unroll
-    for (int r = 0; r < R; ++r) x[r] = p.step + r < valid ? x[r] : values<T>{};
+    for (int r = 0; r < R; ++r) x[r] = p.step + r < valid ? x[r] : raw<T>{};
 }
 
-// Workgroups that take a sequence's tiles one after another have two sets of maps: a wave that writes the next tile's has read those of the
-// tile before.  Those that share a sequence (SHARED) take one tile, and have the earlier tiles' maps in the second set.
-template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W, SHARED && sizeof(T) == 2 ? 4 : 2) void recurrence_kernel(params a) {
-    __shared__ wave_maps<W> lds[2];
-    const uint32_t id = SHARED ? take_ticket(a.ticket) : blockIdx.x, all = SHARED ? gridDim.x / a.tiles : 1;
-    const place p(a, SHARED ? id % all : id, MODE);
-    const int first = SHARED ? (int)(id / all) : 0, behind = SHARED ? first + 1 : a.tiles;
+// A workgroup of W waves takes one tile, all of a sequence's steps or (SHARED) those that its ticket says; the second set of maps is for the
+// tiles before.
+template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W, 4) void recurrence_kernel(params a) {
+    __shared__ wave_maps<W> lds[SHARED ? 2 : 1];
+    const uint32_t id = SHARED ? turned_group(a) : blockIdx.x;
+    const place p(a, id, MODE);
+    const int tile = SHARED ? take_ticket(a.tickets + id * TICKET) : 0;
     const int64_t end = length(a, p.b);
     const bool speaks = threadIdx.x < ROW_LANES;  // stores states
     float carry[N] = {};
     if (a.state) load_state<MODE>(carry, a.state + p.b * a.width, p.col, a.width);
-#pragma clang loop unroll(disable)
-    for (int tile = first; tile < behind; ++tile) {
-        const int valid = within(end, tile), there = within(a.steps, tile);
-        values<T> g[R], x[R];
-        if (valid > 0) {
-            load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
-            load_strip<T, MODE>(x, a.x, tile, p, valid, a.width);
-        } else {
+    const int valid = within(end, tile), there = within(a.steps, tile);
+    raw<T> g[R], x[R];
+    if (valid > 0) {
+        load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
+        load_strip<T, MODE>(x, a.x, tile, p, valid, a.width);
+    } else {
 #pragma unroll
-            for (int r = 0; r < R; ++r) g[r] = x[r] = values<T>{};
+        for (int r = 0; r < R; ++r) g[r] = x[r] = raw<T>{};
+    }
+    if (valid < WAVE_STEPS * W) still<T>(g, x, p, valid);
+    auto &maps = lds[0];
+    float ga[R][N], gx[R][N], before_A[N], before_H[N];
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        float A = 1.f, H = 0.f, none = 0.f;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float gb;
+            gates(get(g[r], c), ga[r][c], gb);
+            gx[r][c] = gb * get(x[r], c);
+            A *= ga[r][c];
+            H = ga[r][c] * H + gx[r][c];
         }
-        if (valid < WAVE_STEPS * W) still<T>(g, x, p, valid);
-        auto &maps = lds[SHARED ? 0 : tile & 1];
-        float ga[R][N], gx[R][N], before_A[N], before_H[N];
-#pragma unroll
-        for (int c = 0; c < N; ++c) {
-            float A = 1.f, H = 0.f, none = 0.f;
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float gb;
-                gates((float)g[r][c], ga[r][c], gb);
-                gx[r][c] = gb * (float)x[r][c];
-                A *= ga[r][c];
-                H = ga[r][c] * H + gx[r][c];
-            }
-            before_A[c] = 1.f, before_H[c] = 0.f;
-            join<16, true, false>(A, H, none, before_A[c], before_H[c], none, none, p.lane);
-            join<32, true, false>(A, H, none, before_A[c], before_H[c], none, none, p.lane);
-            if (p.lane < ROW_LANES) maps[p.wave][0][p.lane * N + c] = A, maps[p.wave][1][p.lane * N + c] = H;
-            __builtin_amdgcn_sched_barrier(0);  // one channel after another: together they take registers that waves could have
-        }
-        __syncthreads();
-        if (SHARED) {
-            if (speaks && first + 1 < a.tiles) {
-                float A[N], H[N];
-#pragma unroll
-                for (int c = 0; c < N; ++c) {
-                    A[c] = 1.f, H[c] = 0.f;
-#pragma unroll
-                    for (int w = 0; w < W; ++w) {
-                        const float m = maps[w][0][p.lane * N + c];
-                        H[c] = m * H[c] + maps[w][1][p.lane * N + c];
-                        A[c] *= m;
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                tell(a, p, tile, A, H);
-            }
-            if (tile > 0) through_earlier<W>(carry, a, p, tile, lds[1]);
-        }
-        if (speaks && a.kept) store_state<MODE>(a.kept + (p.b * a.tiles + tile) * a.width, carry, p.col, a.width);
-        float s[N];
-#pragma unroll
-        for (int w = 0; w < W; ++w) {
-            if (w == p.wave)
-#pragma unroll
-                for (int c = 0; c < N; ++c) s[c] = carry[c];
-            if (!SHARED || w < p.wave || (p.wave == 0 && tile == a.tiles - 1)) pass<1, W>(carry, maps, w, p);
-        }
-#pragma unroll
-        for (int c = 0; c < N; ++c) s[c] = before_A[c] * s[c] + before_H[c];
-#pragma unroll
-        for (int r = 0; r < R; ++r)
+        join<true, false>(A, H, none, before_A[c], before_H[c], none, none, p.lane);
+        if (p.lane < ROW_LANES) maps[p.wave][0][p.lane * N + c] = A, maps[p.wave][1][p.lane * N + c] = H;
+        __builtin_amdgcn_sched_barrier(0);  // one channel after another: together they take registers that waves could have
+    }
+    __syncthreads();
+    if (SHARED) {
+        if (speaks && tile + 1 < a.tiles) {
+            float A[N], H[N];
 #pragma unroll
             for (int c = 0; c < N; ++c) {
-                s[c] = ga[r][c] * s[c] + gx[r][c];
-                x[r][c] = (T)s[c];
+                A[c] = 1.f, H[c] = 0.f;
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    const float m = maps[w][0][p.lane * N + c];
+                    H[c] = m * H[c] + maps[w][1][p.lane * N + c];
+                    A[c] *= m;
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-        if (valid < there) zero_behind<T>(x, p, valid);
-        store_strip<T, MODE>(x, a.h, tile, p, there, a.width);
+            tell(a, p, tile, A, H);
+        }
+        if (tile > 0) through_earlier<W>(carry, a, p, tile, lds[SHARED ? 1 : 0]);
     }
-    if (speaks && a.last && behind == a.tiles) store_state<MODE>(a.last + p.b * a.width, carry, p.col, a.width);
+    if (speaks && a.kept) store_state<MODE>(a.kept + (p.b * a.tiles + tile) * a.width, carry, p.col, a.width);
+    float s[N];
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        if (w == p.wave)
+#pragma unroll
+            for (int c = 0; c < N; ++c) s[c] = carry[c];
+        if (w < p.wave || (p.wave == 0 && tile == a.tiles - 1)) pass<1, W>(carry, maps, w, p);
+    }
+#pragma unroll
+    for (int c = 0; c < N; ++c) s[c] = before_A[c] * s[c] + before_H[c];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+#pragma unroll
+        for (int c = 0; c < N; ++c) s[c] = ga[r][c] * s[c] + gx[r][c];
+        x[r] = both<T>(s[0], s[1]);
+    }
+    if (valid < there) zero_behind<T>(x, p, valid);
+    store_strip<T, MODE>(x, a.h, tile, p, there, a.width);
+    if (speaks && a.last && tile == a.tiles - 1) store_state<MODE>(a.last + p.b * a.width, carry, p.col, a.width);
 }
 
 // As above, from the last tile to the first; the states before the tile's steps come from the kept one.
-template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W, SHARED && sizeof(T) == 2 ? 4 : 2) void recurrence_backward_kernel(params a) {
-    __shared__ wave_maps<W> lds[2];
-    const uint32_t id = SHARED ? take_ticket(a.ticket) : blockIdx.x, all = SHARED ? gridDim.x / a.tiles : 1;
-    const place p(a, SHARED ? id % all : id, MODE);
-    const int order = SHARED ? (int)(id / all) : 0, last = a.tiles - 1 - order, first = SHARED ? last : 0;
+template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W, sizeof(T) == 2 ? 4 : 2) void recurrence_backward_kernel(params a) {
+    __shared__ wave_maps<W> lds[SHARED ? 2 : 1];
+    const uint32_t id = SHARED ? turned_group(a) : blockIdx.x;
+    const place p(a, id, MODE);
+    const int order = SHARED ? take_ticket(a.tickets + id * TICKET) : 0, tile = a.tiles - 1 - order;
     const int64_t end = length(a, p.b);
     const bool speaks = threadIdx.x < ROW_LANES;
     float carry[N] = {};
     if (a.dlast) load_state<MODE>(carry, a.dlast + p.b * a.width, p.col, a.width);
-#pragma clang loop unroll(disable)
-    for (int tile = last; tile >= first; --tile) {
-        const int valid = within(end, tile), there = within(a.steps, tile);
-        values<T> g[R], x[R], dh[R];
-        if (valid > 0) {
-            load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
-            load_strip<T, MODE>(x, a.x, tile, p, valid, a.width);
-            load_strip<T, MODE>(dh, a.dh, tile, p, valid, a.width);
-        } else {
+    const int valid = within(end, tile), there = within(a.steps, tile);
+    raw<T> g[R], x[R], dh[R];
+    if (valid > 0) {
+        load_strip<T, MODE>(g, a.gate, tile, p, valid, a.width);
+        load_strip<T, MODE>(x, a.x, tile, p, valid, a.width);
+        load_strip<T, MODE>(dh, a.dh, tile, p, valid, a.width);
+    } else {
 #pragma unroll
-            for (int r = 0; r < R; ++r) g[r] = x[r] = dh[r] = values<T>{};
-        }
-        if (valid < WAVE_STEPS * W) still<T>(g, x, p, valid), zero_behind<T>(dh, p, valid);
-        float s[N];
-        load_state<MODE>(s, a.kept + (p.b * a.tiles + tile) * a.width, p.col, a.width);
-        auto &maps = lds[SHARED ? 0 : tile & 1];
-        float before_A[N], before_H[N], behind_A[N], behind_E[N];
+        for (int r = 0; r < R; ++r) g[r] = x[r] = dh[r] = raw<T>{};
+    }
+    if (valid < WAVE_STEPS * W) still<T>(g, x, p, valid), zero_behind<T>(dh, p, valid);
+    float s[N];
+    load_state<MODE>(s, a.kept + (p.b * a.tiles + tile) * a.width, p.col, a.width);
+    auto &maps = lds[0];
+    float before_A[N], before_H[N], behind_A[N], behind_E[N];
 #pragma unroll
-        for (int c = 0; c < N; ++c) {
-            float A = 1.f, H = 0.f, E = 0.f, ga[R];
+    for (int c = 0; c < N; ++c) {
+        float A = 1.f, H = 0.f, E = 0.f, ga[R];
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float gb;
-                gates((float)g[r][c], ga[r], gb);
-                A *= ga[r];
-                H = ga[r] * H + gb * (float)x[r][c];
-            }
-#pragma unroll
-            for (int r = R - 1; r >= 0; --r) E = ga[r] * E + ga[r] * (float)dh[r][c];
-            before_A[c] = behind_A[c] = 1.f, before_H[c] = behind_E[c] = 0.f;
-            join<16, true, true>(A, H, E, before_A[c], before_H[c], behind_A[c], behind_E[c], p.lane);
-            join<32, true, true>(A, H, E, before_A[c], before_H[c], behind_A[c], behind_E[c], p.lane);
-            if (p.lane < ROW_LANES) {
-                maps[p.wave][0][p.lane * N + c] = A;
-                maps[p.wave][1][p.lane * N + c] = H;
-                maps[p.wave][2][p.lane * N + c] = E;
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        __syncthreads();
-        if (SHARED) {
-            if (speaks && first > 0) {
-                float A[N], E[N];
-#pragma unroll
-                for (int c = 0; c < N; ++c) {
-                    A[c] = 1.f, E[c] = 0.f;
-#pragma unroll
-                    for (int w = W - 1; w >= 0; --w) {
-                        const float m = maps[w][0][p.lane * N + c];
-                        E[c] = m * E[c] + maps[w][2][p.lane * N + c];
-                        A[c] *= m;
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                tell(a, p, order, A, E);
-            }
-            if (order > 0) through_earlier<W>(carry, a, p, order, lds[1]);
-        }
-        float e[N];
-#pragma unroll
-        for (int w = W - 1; w >= 0; --w) {
-            if (w == p.wave)
-#pragma unroll
-                for (int c = 0; c < N; ++c) e[c] = carry[c];
-            if (!SHARED || w > p.wave || (p.wave == 0 && tile == 0)) pass<2, W>(carry, maps, w, p);
+        for (int r = 0; r < R; ++r) {
+            float gb;
+            gates(get(g[r], c), ga[r], gb);
+            A *= ga[r];
+            H = ga[r] * H + gb * get(x[r], c);
         }
 #pragma unroll
-        for (int w = 0; w < W - 1; ++w)
-            if (w < p.wave) pass<1, W>(s, maps, w, p);
-        // the gates are computed again, channel by channel, and the gradients take the inputs' places: kept from above they would take 64 registers
+        for (int r = R - 1; r >= 0; --r) E = ga[r] * E + ga[r] * get(dh[r], c);
+        join<true, true>(A, H, E, before_A[c], before_H[c], behind_A[c], behind_E[c], p.lane);
+        if (p.lane < ROW_LANES) {
+            maps[p.wave][0][p.lane * N + c] = A;
+            maps[p.wave][1][p.lane * N + c] = H;
+            maps[p.wave][2][p.lane * N + c] = E;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    __syncthreads();
+    if (SHARED) {
+        if (speaks && tile > 0) {
+            float A[N], E[N];
 #pragma unroll
-        for (int r = 0; r < R; ++r) asm("" : "+v"(g[r]), "+v"(x[r]), "+v"(dh[r]));
+            for (int c = 0; c < N; ++c) {
+                A[c] = 1.f, E[c] = 0.f;
 #pragma unroll
-        for (int c0 = 0; c0 < N; c0 += 2) {
-            float dx[2][R], dg[2][R];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int c = c0 + k;
-                s[c] = before_A[c] * s[c] + before_H[c];
-                e[c] = behind_A[c] * e[c] + behind_E[c];
-                float ga[R], gb[R], q[R];
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    gates((float)g[r][c], ga[r], gb[r]);
-                    q[r] = (s[c] - (float)x[r][c]) * ga[r];
-                    s[c] = ga[r] * s[c] + gb[r] * (float)x[r][c];
-                }
-#pragma unroll
-                for (int r = R - 1; r >= 0; --r) {
-                    const float G = (float)dh[r][c] + e[c];
-                    dx[k][r] = gb[r] * G;
-                    dg[k][r] = q[r] * dx[k][r];
-                    e[c] = ga[r] * G;
+                for (int w = W - 1; w >= 0; --w) {
+                    const float m = maps[w][0][p.lane * N + c];
+                    E[c] = m * E[c] + maps[w][2][p.lane * N + c];
+                    A[c] *= m;
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                x[r][c0] = (T)dx[0][r], x[r][c0 + 1] = (T)dx[1][r];
-                g[r][c0] = (T)dg[0][r], g[r][c0 + 1] = (T)dg[1][r];
-            }
-            __builtin_amdgcn_sched_barrier(0);
+            tell(a, p, order, A, E);
         }
-        if (valid < there) zero_behind<T>(x, p, valid), zero_behind<T>(g, p, valid);
-        store_strip<T, MODE>(x, a.dx, tile, p, there, a.width);
-        store_strip<T, MODE>(g, a.dgate, tile, p, there, a.width);
+        if (order > 0) through_earlier<W>(carry, a, p, order, lds[SHARED ? 1 : 0]);
     }
-    if (speaks && a.dstate && first == 0) store_state<MODE>(a.dstate + p.b * a.width, carry, p.col, a.width);
+    float e[N];
+#pragma unroll
+    for (int w = W - 1; w >= 0; --w) {
+        if (w == p.wave)
+#pragma unroll
+            for (int c = 0; c < N; ++c) e[c] = carry[c];
+        if (w > p.wave || (p.wave == 0 && tile == 0)) pass<2, W>(carry, maps, w, p);
+    }
+#pragma unroll
+    for (int w = 0; w < W - 1; ++w)
+        if (w < p.wave) pass<1, W>(s, maps, w, p);
+    // the gates are computed again, channel by channel, and the gradients take the inputs' places: kept from above they would take 64 registers
+#pragma unroll
+    for (int r = 0; r < R; ++r) asm("" : "+v"(g[r]), "+v"(x[r]), "+v"(dh[r]));
+    float dx[N][R], dg[N][R];
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        s[c] = before_A[c] * s[c] + before_H[c];
+        e[c] = behind_A[c] * e[c] + behind_E[c];
+        float ga[R], gb[R], q[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            gates(get(g[r], c), ga[r], gb[r]);
+            q[r] = (s[c] - get(x[r], c)) * ga[r];
+            s[c] = ga[r] * s[c] + gb[r] * get(x[r], c);
+        }
+#pragma unroll
+        for (int r = R - 1; r >= 0; --r) {
+            const float G = get(dh[r], c) + e[c];
+            dx[c][r] = gb[r] * G;
+            dg[c][r] = q[r] * dx[c][r];
+            e[c] = ga[r] * G;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) x[r] = both<T>(dx[0][r], dx[1][r]), g[r] = both<T>(dg[0][r], dg[1][r]);
+    if (valid < there) zero_behind<T>(x, p, valid), zero_behind<T>(g, p, valid);
+    store_strip<T, MODE>(x, a.dx, tile, p, there, a.width);
+    store_strip<T, MODE>(g, a.dgate, tile, p, there, a.width);
+    if (speaks && a.dstate && tile == 0) store_state<MODE>(a.dstate + p.b * a.width, carry, p.col, a.width);
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -473,10 +486,8 @@ int size_of(int32_t dtype) { return dtype == DEAR_BF16 ? 2 : 4; }
 // Channels of a workgroup.
 int64_t groups_of(const dear_recurrence_t &r) { return ceil_div(r.width, CG); }
 
-// Whether the tiles of a sequence go to workgroups of their own, which takes a launch more: where there are several tiles and the sequences'
-// channels alone do not fill the chip.
-bool shares(const dear_recurrence_t &r) { return r.steps > KEPT && r.batch * groups_of(r) < 512; }
-constexpr int64_t TICKET_BYTES = 256;
+// Whether workgroups share a sequence's channels, a tile each, which takes a launch more.
+bool shares(const dear_recurrence_t &r) { return r.steps > KEPT; }
 
 int check(const dear_recurrence_t *r) {
     if (!r || (r->dtype != DEAR_F32 && r->dtype != DEAR_BF16) || r->batch < 0 || r->steps < 0 || r->steps > MAX_STEPS) return DEAR_EINVAL;
@@ -505,7 +516,7 @@ int check_tensor(const dear_recurrence_t &r, const dear_steps_t &t, bool written
 }
 
 int64_t workspace_of(const dear_recurrence_t &r) {
-    return r.batch && shares(r) ? TICKET_BYTES + (int64_t)r.batch * (ceil_div(r.steps, KEPT) + 1) * r.width * 8 : 0;
+    return r.batch && shares(r) ? r.batch * (groups_of(r) * TICKET * 4 + (ceil_div(r.steps, KEPT) + 1) * r.width * 8) : 0;
 }
 
 bool vectors(const dear_recurrence_t &r, const dear_steps_t &t) {
@@ -534,7 +545,7 @@ int check_call(const dear_recurrence_t *r, bool backward) {
         if (need && !r->workspace) return DEAR_EINVAL;
         if (need && !aligned(r->workspace, 256)) return DEAR_EALIGN;
         if (need > r->workspace_bytes) return DEAR_ETOOBIG;
-        if (r->batch * groups_of(*r) * (shares(*r) ? ceil_div(r->steps, KEPT) : 1) * 64 * WAVES > MAX_THREADS) return DEAR_ETOOBIG;
+        if (r->batch * groups_of(*r) * ceil_div(r->steps, KEPT) * 64 * WAVES > MAX_THREADS) return DEAR_ETOOBIG;
     }
     return DEAR_OK;
 }
@@ -554,9 +565,9 @@ template <typename T, int MODE, bool BACKWARD> void launch(params a, int64_t bat
     };
     if (shared) {
         const int64_t states = batch * a.width, n = states * a.tiles;
-        a.ticket = (uint32_t *)workspace, a.maps = (uint64_t *)((char *)workspace + TICKET_BYTES);
+        a.tickets = (uint32_t *)workspace, a.maps = (uint64_t *)(a.tickets + groups * TICKET);
         float *copy = (float *)(a.maps + n);
-        untold_kernel<<<(unsigned)ceil_div(n, 256), 256, 0, stream>>>(a.maps, n, a.ticket, BACKWARD ? a.dlast : a.state, copy, states);
+        untold_kernel<<<(unsigned)ceil_div(n, 256), 256, 0, stream>>>(a.maps, n, a.tickets, BACKWARD ? a.dlast : a.state, copy, states, groups);
         a.state = a.dlast = copy;
         const unsigned all = (unsigned)(groups * a.tiles);
         if (BACKWARD) recurrence_backward_kernel<T, WAVES, MODE, true><<<all, 64 * WAVES, 0, stream>>>(a);
@@ -590,7 +601,7 @@ int call(const dear_recurrence_t *r, bool backward, hipStream_t stream) {
     a.groups = (int32_t)groups_of(*r), a.tiles = (int32_t)ceil_div(r->steps, KEPT);
     bool vec = r->width % N == 0 && vectors(*r, r->x) && vectors(*r, r->gate);
     vec = vec && (backward ? vectors(*r, r->dh) && vectors(*r, r->dx) && vectors(*r, r->dgate) : vectors(*r, r->h));
-    vec = vec && aligned(r->state, 16) && aligned(r->last, 16) && aligned(r->kept, 16) && aligned(r->dlast, 16) && aligned(r->dstate, 16);
+    vec = vec && aligned(r->state, 8) && aligned(r->last, 8) && aligned(r->kept, 8) && aligned(r->dlast, 8) && aligned(r->dstate, 8);
     auto by_mode = [&](auto t, auto mode) {
         typedef decltype(t) T;
         if (backward) launch<T, decltype(mode)::value, true>(a, r->batch, shares(*r), r->workspace, stream);
