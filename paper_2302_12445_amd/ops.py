@@ -21,6 +21,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import itertools
 import math
 import os
 import struct
@@ -620,31 +621,37 @@ def _grad_norm(tensors: Sequence[torch.Tensor], out: Optional[Sequence[torch.Ten
     outs = tensors if out is None else list(out)
     if len(outs) != len(tensors):
         raise ValueError("%d tensors and %d outputs" % (len(tensors), len(outs)))
-    device, members, held = tensors[0].device, [], []
-    if tensors[0].is_cuda and tensors[0].get_device() != _current_device():
-        with torch.cuda.device(device):
+    first = tensors[0]
+    if _elsewhere(first):
+        with torch.cuda.device(first.device):
             return _grad_norm(tensors, out, max_norm)
-    for g, o in zip(tensors, outs):
-        d, od = _dtype(g, "a gradient"), _dtype(o, "an output")
-        if g.device != device or o.device != device:
-            raise ValueError("tensors are on %s, %s and %s" % (device, g.device, o.device))
-        if o.shape != g.shape:
-            raise ValueError("an output has shape %s, its gradient %s" % (tuple(o.shape), tuple(g.shape)))
-        if clip and not _dense(o):
-            raise ValueError("an output of shape %s and strides %s has gaps" % (tuple(o.shape), o.stride()))
-        if (o.stride() != g.stride() and not (o.is_contiguous() and g.is_contiguous())) or not _dense(g):
-            g = torch.empty_strided(o.shape, o.stride(), dtype=g.dtype, device=device).copy_(g) if clip else g.contiguous()
-            held.append(g)
-        members += (g.data_ptr(), o.data_ptr(), g.numel(), d, od)
+    # a list at a time: a model has some hundred tensors, and each question to one takes the host 50 ns
+    index, types = first.get_device(), [_DTYPE.get(t.dtype) for t in tensors]
+    out_types = types if outs is tensors else [_DTYPE.get(t.dtype) for t in outs]
+    for group, kinds, what in ((tensors, types, "a gradient"), (outs, out_types, "an output")):
+        if None in kinds or any(t.get_device() != index for t in group) or index < 0:
+            for t in group:
+                _dtype(t, what)
+            raise ValueError("tensors are on several devices")
+    if outs is not tensors and any(o.shape != g.shape for o, g in zip(outs, tensors)):
+        raise ValueError("an output has another shape than its gradient")
+    if not all(t.is_contiguous() for t in tensors) or (outs is not tensors and not all(t.is_contiguous() for t in outs)):
+        if clip and not all(_dense(o) for o in outs):
+            raise ValueError("an output has gaps between its elements")
+        # elements in the outputs' order
+        tensors = [g if _dense(g) and (g.stride() == o.stride() or not clip) else
+                   torch.empty_strided(o.shape, o.stride(), dtype=g.dtype, device=g.device).copy_(g) if clip else g.contiguous()
+                   for g, o in zip(tensors, outs)]
     lib, count = load_library(), len(tensors)
-    norm = torch.empty((), dtype=torch.float32, device=device)
+    norm = torch.empty((), dtype=torch.float32, device=first.device)
     need = _workspace("dear_grad_norm_workspace", count)
-    space = torch.empty(need, dtype=torch.uint8, device=device)
-    packed, stream = _grad_layout(count).pack(*members), _raw_stream(norm.get_device())
+    space = torch.empty(need, dtype=torch.uint8, device=first.device)
+    at = [t.data_ptr() for t in tensors]
+    members = zip(at, at if outs is tensors else [t.data_ptr() for t in outs], [t.numel() for t in tensors], types, out_types)
+    packed, stream = _grad_layout(count).pack(*itertools.chain.from_iterable(members)), _raw_stream(index)
     if clip:
         _check(lib.dear_clip_grads(packed, count, max_norm, norm.data_ptr(), space.data_ptr(), need, stream), "dear_clip_grads")
-        for o in outs:
-            torch.autograd.graph.increment_version(o)
+        torch.autograd.graph.increment_version(outs)
     else:
         _check(lib.dear_grad_norm(packed, count, norm.data_ptr(), space.data_ptr(), need, stream), "dear_grad_norm")
     return norm
