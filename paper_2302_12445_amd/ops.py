@@ -625,17 +625,19 @@ def _grad_norm(tensors: Sequence[torch.Tensor], out: Optional[Sequence[torch.Ten
     if _elsewhere(first):
         with torch.cuda.device(first.device):
             return _grad_norm(tensors, out, max_norm)
-    # a list at a time: a model has some hundred tensors, and each question to one takes the host 50 ns
+    # a list at a time: a model has some hundred tensors, and each question to one takes the host some 50 ns
     index, types = first.get_device(), [_DTYPE.get(t.dtype) for t in tensors]
     out_types = types if outs is tensors else [_DTYPE.get(t.dtype) for t in outs]
-    for group, kinds, what in ((tensors, types, "a gradient"), (outs, out_types, "an output")):
-        if None in kinds or any(t.get_device() != index for t in group) or index < 0:
-            for t in group:
-                _dtype(t, what)
-            raise ValueError("tensors are on several devices")
+    where = set(map(torch.Tensor.get_device, tensors)) | set(map(torch.Tensor.get_device, outs))
+    if None in types or None in out_types or len(where) > 1 or index < 0:
+        for t in tensors:
+            _dtype(t, "a gradient")
+        for t in outs:
+            _dtype(t, "an output")
+        raise ValueError("tensors are on several devices")
     if outs is not tensors and any(o.shape != g.shape for o, g in zip(outs, tensors)):
         raise ValueError("an output has another shape than its gradient")
-    if not all(t.is_contiguous() for t in tensors) or (outs is not tensors and not all(t.is_contiguous() for t in outs)):
+    if not all(map(torch.Tensor.is_contiguous, tensors)) or not all(map(torch.Tensor.is_contiguous, outs)):
         if clip and not all(_dense(o) for o in outs):
             raise ValueError("an output has gaps between its elements")
         # elements in the outputs' order
@@ -646,8 +648,7 @@ def _grad_norm(tensors: Sequence[torch.Tensor], out: Optional[Sequence[torch.Ten
     norm = torch.empty((), dtype=torch.float32, device=first.device)
     need = _workspace("dear_grad_norm_workspace", count)
     space = torch.empty(need, dtype=torch.uint8, device=first.device)
-    at = [t.data_ptr() for t in tensors]
-    members = zip(at, at if outs is tensors else [t.data_ptr() for t in outs], [t.numel() for t in tensors], types, out_types)
+    members = zip(map(torch.Tensor.data_ptr, tensors), map(torch.Tensor.data_ptr, outs), map(torch.Tensor.numel, tensors), types, out_types)
     packed, stream = _grad_layout(count).pack(*itertools.chain.from_iterable(members)), _raw_stream(index)
     if clip:
         _check(lib.dear_clip_grads(packed, count, max_norm, norm.data_ptr(), space.data_ptr(), need, stream), "dear_clip_grads")
