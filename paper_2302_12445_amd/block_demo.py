@@ -4,6 +4,7 @@ DistOptim inside the backward passes.  The task: predict the token before (a cau
 Prints one JSON line: losses and step time.
 
     python -m paper_2302_12445_amd.block_demo --replicas 4 --width 256 --layers 2 --steps 150
+    python -m paper_2302_12445_amd.block_demo --mixer recurrence --experts 8 --clip 1.0     # recurrent blocks with expert layers
 """
 from __future__ import annotations
 
@@ -12,20 +13,28 @@ import copy
 import json
 import sys
 import time
+from typing import Optional
 
 import torch
 
-from .layers import AddRMSNorm, TransformerBlock
+from .layers import AddRMSNorm, RecurrentBlock, TransformerBlock
 
 
 class TinyTransformer(torch.nn.Module):
-    """Embedding, blocks, norm and a projection to the vocabulary; activations in `dtype`, parameters fp32."""
+    """Embedding, blocks, norm and a projection to the vocabulary; activations in `dtype`, parameters fp32.  Blocks mix tokens by
+    attention or, with mixer "recurrence", by a gated linear recurrence, and then may have several experts."""
 
-    def __init__(self, vocab: int, width: int, heads: int, kv_heads: int, layers: int, tokens: int, dtype: torch.dtype):
+    def __init__(self, vocab: int, width: int, heads: int, kv_heads: int, layers: int, tokens: int, dtype: torch.dtype,
+                 mixer: str = "attention", experts: int = 0, top: int = 2):
         super().__init__()
         self.embed = torch.nn.Embedding(vocab, width)
         self.position = torch.nn.Embedding(tokens, width)
-        self.blocks = torch.nn.ModuleList(TransformerBlock(width, heads, kv_heads) for _ in range(layers))
+        if mixer == "recurrence":
+            self.blocks = torch.nn.ModuleList(RecurrentBlock(width, experts=experts, top=top) for _ in range(layers))
+        elif mixer == "attention" and not experts:
+            self.blocks = torch.nn.ModuleList(TransformerBlock(width, heads, kv_heads) for _ in range(layers))
+        else:
+            raise ValueError("mixer %s with %d experts: experts are for recurrent blocks" % (mixer, experts))
         self.norm = AddRMSNorm(width)
         self.head = torch.nn.Linear(width, vocab)
         self.dtype = dtype
@@ -34,7 +43,7 @@ class TinyTransformer(torch.nn.Module):
         at = torch.arange(tokens.shape[1], device=tokens.device)
         x, residual = (self.embed(tokens) + self.position(at)).to(self.dtype), None
         for block in self.blocks:
-            x, residual = block(x, residual, lens)
+            x, residual = block(x, residual, lens=lens)
         _, y, _ = self.norm(x, residual, keep=False)
         return self.head(y.float())
 
@@ -49,14 +58,15 @@ def batch_of(vocab: int, batch: int, tokens: int, gen: torch.Generator, device: 
 
 
 def train(replicas: int, width: int, heads: int, kv_heads: int, layers: int, tokens: int, batch: int, steps: int, lr: float,
-          dtype: torch.dtype, seed: int = 0, device: str = "cuda:0"):
+          dtype: torch.dtype, seed: int = 0, device: str = "cuda:0", mixer: str = "attention", experts: int = 0,
+          max_grad_norm: Optional[float] = None):
     """Losses of the steps, seconds a step behind the first five, and the replicas."""
     from .dist_optim import DistOptim
     vocab = 64
     torch.manual_seed(seed)
-    model = TinyTransformer(vocab, width, heads, kv_heads, layers, tokens, dtype).to(device)
+    model = TinyTransformer(vocab, width, heads, kv_heads, layers, tokens, dtype, mixer, experts, min(2, experts)).to(device)
     models = [copy.deepcopy(model) for _ in range(replicas)]
-    optim = DistOptim(models, lr=lr, momentum=0.9, fusion_threshold_bytes=4 << 20)
+    optim = DistOptim(models, lr=lr, momentum=0.9, fusion_threshold_bytes=4 << 20, max_grad_norm=max_grad_norm)
     gen = torch.Generator().manual_seed(seed + 1)
     losses, began = [], 0.0
     for step in range(steps):
@@ -90,14 +100,18 @@ def main() -> None:
     ap.add_argument("--steps", type=int, default=150)
     ap.add_argument("--lr", type=float, default=0.2)
     ap.add_argument("--dtype", default="bf16", choices=["bf16", "f32"], help="type of the activations")
+    ap.add_argument("--mixer", default="attention", choices=["attention", "recurrence"], help="what mixes the tokens of a block")
+    ap.add_argument("--experts", type=int, default=0, help="experts of a recurrent block's feed-forward layer, 0 for one network")
+    ap.add_argument("--clip", type=float, default=None, help="largest norm of the gradients")
     args = ap.parse_args()
     if not torch.cuda.is_available():
         print("block_demo needs a GPU", file=sys.stderr)
         sys.exit(2)
     dtype = torch.bfloat16 if args.dtype == "bf16" else torch.float32
     losses, seconds, _ = train(args.replicas, args.width, args.heads, args.kv_heads, args.layers, args.tokens, args.batch, args.steps,
-                               args.lr, dtype)
-    print(json.dumps({"demo": "transformer blocks under DistOptim", "replicas": args.replicas, "width": args.width,
+                               args.lr, dtype, mixer=args.mixer, experts=args.experts, max_grad_norm=args.clip)
+    name = "transformer" if args.mixer == "attention" else "recurrent"
+    print(json.dumps({"demo": name + " blocks under DistOptim", "replicas": args.replicas, "width": args.width,
                       "layers": args.layers, "tokens": args.tokens, "batch": args.batch, "dtype": args.dtype,
                       "first_loss": losses[0], "last_loss": losses[-1], "ms_per_step": seconds * 1e3}))
 

@@ -8,6 +8,10 @@ all-gathers are issued in forward order and a layer's forward computation waits 
 all-gather of its group (FeedPipe).  Users call synchronize() before reading parameters
 (Section V-B).
 
+With max_grad_norm the norm over the averaged gradients of all groups is needed before any group can be updated: the
+reduce-scatters run inside the backward pass as always, and step() queues the norm, the clipping and the update
+behind them, on the owned shards, where each averaged gradient lies once.
+
 Here the P "workers" are P copies of a torch module in one process.  Their .grad and
 .data tensors are handed to libdear as they are (no staging copy): hooks only count
 arrivals, record events and launch the library's kernels on a communication stream.
@@ -22,21 +26,26 @@ arrivals, record events and launch the library's kernels on a communication stre
 """
 from __future__ import annotations
 
-from typing import Dict, List, Sequence
+from typing import Dict, List, Optional, Sequence
 
 import torch
 
 from . import binding as B
+from . import ops
 
 
 class DistOptim:
     def __init__(self, models: Sequence[torch.nn.Module], lr: float, momentum: float,
-                 fusion_threshold_bytes: int = 25 << 20, fused_update: bool = True):
+                 fusion_threshold_bytes: int = 25 << 20, fused_update: bool = True, max_grad_norm: Optional[float] = None):
         if not models:
             raise ValueError("need at least one replica")
+        if max_grad_norm is not None and not max_grad_norm > 0:
+            raise ValueError("max_grad_norm %g: expected a number above 0" % max_grad_norm)
         self.models = list(models)
         self.P = len(self.models)
         self.lr, self.momentum, self.fused_update = lr, momentum, fused_update
+        self.max_grad_norm = max_grad_norm
+        self.grad_norm: Optional[torch.Tensor] = None  # of the last step, where gradients are clipped; on the GPU
         per_model = [[p for p in m.parameters() if p.requires_grad] for m in self.models]
         self.params = per_model
         sizes = [p.numel() for p in per_model[0]]
@@ -108,7 +117,9 @@ class DistOptim:
         self._grad_ready[b].record(torch.cuda.current_stream())
         self.comm.wait_event(self._grad_ready[b])
         h = self.comm.cuda_stream
-        if self.fused_update:
+        if self.max_grad_norm is not None:
+            B.dear_reduce_scatter(self.ctx, b, self.shard_grad.data_ptr(), h)
+        elif self.fused_update:
             B.dear_reduce_scatter_update(self.ctx, b, self.shard_param.data_ptr(), self.shard_mom.data_ptr(),
                                          self.lr, self.momentum, h)
         else:
@@ -129,6 +140,13 @@ class DistOptim:
         if got != self._grad_ptrs:
             raise RuntimeError("a .grad tensor was replaced; keep gradients in place (set_to_none=False)")
         h = self.comm.cuda_stream
+        if self.max_grad_norm is not None:
+            # slots that belong to no gradient are 0
+            with torch.cuda.stream(self.comm):
+                self.grad_norm = ops.clip_grads([self.shard_grad], self.max_grad_norm)
+            self.grad_norm.record_stream(torch.cuda.current_stream())
+            B.dear_shard_update(self.ctx, -1, self.shard_grad.data_ptr(), self.shard_param.data_ptr(),
+                                self.shard_mom.data_ptr(), self.lr, self.momentum, h)
         rs_done = torch.cuda.Event()       # all reduce-scatters are queued: they precede every all-gather
         rs_done.record(self.comm)
         for b in reversed(range(nb)):

@@ -5,6 +5,8 @@ operator allows it.
     h, y, kept = AddRMSNorm(width)(x, residual)   # kept: y in 8 bits, from the norm's own kernel
     z = CheckpointLinear(width, outs)(y, kept)    # weight gradient from the checkpoint; makes one itself where none is given
     out = attend(q, k, v, causal=True)            # keeps q, k, v, out and the log-sum-exp; recomputes the probabilities
+    h, last = recur(x, gate, state)               # keeps x, the gates and every 256th state; recomputes the others
+    y = ExpertLinear(experts, ins, outs)(x, ends) # keeps x; rows sorted by expert
 
 The operators' gradients cannot be differentiated again: second derivatives that need it raise RuntimeError.
 """
@@ -41,7 +43,8 @@ class _FirstOrder(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, *_):
-        raise RuntimeError("attention, RMS norm and the weight gradient from a checkpoint have no second derivatives")
+        raise RuntimeError("attention, RMS norm, the recurrence, products by expert and the weight gradient from a checkpoint have no second "
+                           "derivatives")
 
 
 def _first_order(gradients, *tensors):
@@ -70,6 +73,64 @@ def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, causal: bool = Fal
            q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None) -> torch.Tensor:
     """ops.attention's out, with gradients of q, k and v."""
     return _apply(_Attention, q, k, v, causal, scale, q_lens, kv_lens)
+
+
+class _Recurrence(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gate, state, lens, keep):
+        h, last, kept = ops.recurrence(x, gate, state, lens, keep=keep)
+        ctx.save_for_backward(x, gate, kept, lens, state)
+        ctx.set_materialize_grads(False)
+        return h, last
+
+    @staticmethod
+    def backward(ctx, dh, dlast):
+        x, gate, kept, lens, state = ctx.saved_tensors
+        if dh is None and dlast is None:
+            return None, None, None, None, None
+        given = dh, dlast
+        if dh is None:
+            dh = torch.zeros_like(x)
+        grads = ops.recurrence_backward(dh, x, gate, kept, lens, None if dlast is None else dlast.contiguous())
+        dx, dgate, dstate = _first_order(grads, *given, x, gate, state)
+        return dx, dgate, dstate if state is not None else None, None, None
+
+
+def recur(x: torch.Tensor, gate: torch.Tensor, state: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None
+          ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """ops.recurrence's h and last, with gradients of x, the gates and the state."""
+    keep = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, gate, state))
+    return _apply(_Recurrence, x, gate, state, lens, keep)
+
+
+class _ExpertLinear(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, ends):
+        ctx.save_for_backward(x, weight, ends)
+        return ops.expert_linear(x, weight.to(x.dtype), ends)
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, ends = ctx.saved_tensors
+        dx = dw = None
+        if ctx.needs_input_grad[0]:
+            dx, = _first_order((ops.expert_input_grad(dy, weight.to(dy.dtype), ends),), dy, weight)
+        if ctx.needs_input_grad[1]:
+            dw, = _first_order((ops.expert_weight_grad(dy, x, ends).to(weight.dtype),), dy, x)
+        return dx, dw, None
+
+
+class ExpertLinear(torch.nn.Module):
+    """A linear layer for each of several experts, without biases: rows [M, ins] sorted by expert, expert e's up to row ends[e]; rows
+    behind the last one's give 0.  Parameters and their gradients are fp32, products in the rows' type."""
+
+    def __init__(self, experts: int, ins: int, outs: int):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.empty(experts, outs, ins))
+        torch.nn.init.uniform_(self.weight, -1 / math.sqrt(ins), 1 / math.sqrt(ins))
+
+    def forward(self, x: torch.Tensor, ends: torch.Tensor) -> torch.Tensor:
+        return _apply(_ExpertLinear, x, self.weight, ends)
 
 
 class _AddRMSNorm(torch.autograd.Function):
@@ -210,6 +271,69 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         super().__init__(pack, unpack)
 
 
+class _Spread(torch.autograd.Function):
+    """Rows [M, width], each to `top` places: out[place[m, i]] = rows[m].  Gradients are added over the places in their order."""
+
+    @staticmethod
+    def forward(ctx, rows, place, source):
+        ctx.save_for_backward(place, source)
+        return rows[source]
+
+    @staticmethod
+    def backward(ctx, dout):
+        place, source = ctx.saved_tensors
+        return _Gather.apply(dout, place, source).sum(1), None, None
+
+
+class _Gather(torch.autograd.Function):
+    """out[m, i] = rows[place[m, i]], with every row in one place."""
+
+    @staticmethod
+    def forward(ctx, rows, place, source):
+        ctx.save_for_backward(place, source)
+        return rows[place]
+
+    @staticmethod
+    def backward(ctx, dout):
+        place, source = ctx.saved_tensors
+        flat = dout.flatten(0, 1)
+        order = torch.empty_like(source).scatter_(0, place.flatten(), torch.arange(source.numel(), device=source.device))
+        return flat[order], None, None
+
+
+class Experts(torch.nn.Module):
+    """Feed-forward layer of several experts: a router sends each token to `top` of them, whose results are added with the router's
+    weights (a softmax over the chosen ones).  Tokens behind the sequences' lengths go to none, and give 0."""
+
+    def __init__(self, width: int, ffn: int, experts: int, top: int = 2):
+        super().__init__()
+        if not 1 <= top <= experts:
+            raise ValueError("top %d of %d experts" % (top, experts))
+        self.experts, self.top = experts, top
+        self.router = torch.nn.Parameter(torch.empty(experts, width))
+        torch.nn.init.uniform_(self.router, -1 / math.sqrt(width), 1 / math.sqrt(width))
+        self.up = ExpertLinear(experts, width, ffn)
+        self.down = ExpertLinear(experts, ffn, width)
+
+    def forward(self, y: torch.Tensor, lens: Optional[torch.Tensor] = None) -> torch.Tensor:
+        batch, tokens, width = y.shape
+        rows = y.reshape(-1, width)
+        # chosen in fp32, whatever the activations' type: a rounding must not send a token elsewhere
+        scores, chosen = (rows.float() @ self.router.t()).topk(self.top, -1)
+        share = torch.softmax(scores, -1)
+        if lens is not None:
+            valid = (torch.arange(tokens, device=y.device) < lens.view(-1, 1)).view(-1, 1)
+            chosen = torch.where(valid, chosen, self.experts)
+        sorted_, order = chosen.flatten().sort(stable=True)
+        ends = torch.searchsorted(sorted_, torch.arange(self.experts, device=y.device), right=True).to(torch.int32)
+        place = torch.empty_like(order).scatter_(0, order, torch.arange(order.numel(), device=y.device)).view(-1, self.top)
+        u = self.up(_Spread.apply(rows, place, order // self.top), ends)
+        with saved_in_8_bits():
+            z = torch.nn.functional.gelu(u)
+        z = _Gather.apply(self.down(z, ends), place, order // self.top)
+        return (z * share.unsqueeze(2).to(z.dtype)).sum(1).view(y.shape)
+
+
 class TransformerBlock(torch.nn.Module):
     """Pre-norm transformer block over (x, residual), as one layer of a stack: attention and a feed-forward network, each
     behind a norm that adds the residual on the way.  Gives the block's (output, residual) for the next one's norm."""
@@ -237,3 +361,40 @@ class TransformerBlock(torch.nn.Module):
         with saved_in_8_bits():
             z = torch.nn.functional.gelu(u)
         return self.down(z), h
+
+
+class RecurrentBlock(torch.nn.Module):
+    """Pre-norm block over (x, residual) as TransformerBlock, with a gated linear recurrence in the place of attention, whose result is
+    gated by the token, and a feed-forward network or, with `experts`, several of them.  Gives the block's (output, residual)."""
+
+    def __init__(self, width: int, ffn: Optional[int] = None, experts: int = 0, top: int = 2):
+        super().__init__()
+        self.norm1 = AddRMSNorm(width)
+        self.into = CheckpointLinear(width, 3 * width)
+        self.proj = CheckpointLinear(width, width)
+        self.norm2 = AddRMSNorm(width)
+        self.experts = Experts(width, ffn or 4 * width, experts, top) if experts else None
+        if not experts:
+            self.up = CheckpointLinear(width, ffn or 4 * width)
+            self.down = CheckpointLinear(ffn or 4 * width, width)
+        with torch.no_grad():  # memories of some steps to some hundred
+            self.into.bias[width:2 * width] = torch.linspace(1, 6, width)
+
+    def forward(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None,
+                state: Optional[torch.Tensor] = None):
+        """With a state (fp32 [batch, width], zeros at a sequence's start) also the state behind these tokens, for a call on the next."""
+        width = x.shape[-1]
+        trained = torch.is_grad_enabled()
+        h, y, kept = self.norm1(x, residual, trained and self.into.weight.requires_grad)
+        v, gate, open_ = self.into(y, kept).split(width, 2)
+        s, last = recur(v, gate, state, lens)
+        h, y, kept = self.norm2(self.proj(s * torch.nn.functional.silu(open_)), h,
+                                trained and self.experts is None and self.up.weight.requires_grad)
+        if self.experts is not None:
+            out = self.experts(y, lens)
+        else:
+            u = self.up(y, kept)
+            with saved_in_8_bits():
+                z = torch.nn.functional.gelu(u)
+            out = self.down(z)
+        return (out, h) if state is None else (out, h, last)
