@@ -28,6 +28,8 @@ struct params {
     int32_t sum;         // summed index (of a weight gradient, the expert's rows)
     int32_t n_a, n_b;    // outputs' rows (of a weight gradient; otherwise the tile's expert has them) and columns
     int32_t a_tiles, b_tiles;
+    int32_t splits, chunk;  // of the summed index: sums of their own, and how much of it each has
+    float *parts;           // [splits, rows, columns], where there are several
 };
 
 // ------------------------------------------------------------------------------------ a tile's expert
@@ -107,13 +109,14 @@ __device__ __forceinline__ part rows_of(const params &p, int32_t expert) {
 
 // ------------------------------------------------------------------------------------ any type, any size
 constexpr int THREADS = 256;
-constexpr int BA = 128, BB = 128, BS = 32;  // outputs' rows and columns of a workgroup, summed index of a step
+constexpr int BB = 128;  // outputs' columns of a workgroup
 
-// An operand's part of a step on its way from memory to LDS, in pieces of 16 bytes: BA rows of BS values along the summed index or, ACROSS
-// it, BS rows of BA values.  Values beyond the sum are zeros in both operands, so that nothing that stands there counts; rows and columns
+// An operand's part of a step on its way from memory to LDS, in pieces of 16 bytes: OUT rows of BS values along the summed index or, ACROSS
+// it, BS rows of OUT values.  Values beyond the sum are zeros in both operands, so that nothing that stands there counts; rows and columns
 // beyond the outputs are whatever is there, and not stored.
-template <typename T, bool VEC, bool ACROSS> struct stage {
-    static constexpr int E = 16 / sizeof(T), N = BA * BS / E / THREADS, W = ACROSS ? BA : BS;
+template <typename T, bool VEC, bool ACROSS, int OUT, int BS> struct stage {
+    static constexpr int E = 16 / sizeof(T), N = OUT * BS / E / THREADS, W = ACROSS ? OUT : BS;
+    static_assert(N * E * THREADS == OUT * BS, "whole pieces for every thread");
     typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
     typedef vec vec_anywhere __attribute__((aligned(sizeof(T))));  // global memory takes 16-byte loads from any element on
     vec v[N];
@@ -161,26 +164,29 @@ template <int W> __device__ __forceinline__ f32x8 along(const DEAR_LDS float *s,
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// 128 x 128 outputs a workgroup, 64 x 64 a wave; a step's operands go through registers to LDS, the next one's loads beside its products.
-template <typename T, bool VEC, int KIND> __global__ __launch_bounds__(THREADS, 2) void experts_kernel(params p) {
+// BA x 128 outputs a workgroup: four waves of 64 x 64, of 32 x 64 or, of 32 rows, of 32 x 32.  A step's operands go through registers to LDS,
+// the next one's loads beside its products.
+template <typename T, bool VEC, int KIND, int BA> __global__ __launch_bounds__(THREADS, 2) void experts_kernel(params p) {
     constexpr bool A_ACROSS = KIND == WEIGHT_GRAD, B_ACROSS = KIND != LINEAR;
-    typedef stage<T, VEC, A_ACROSS> stage_a;
-    typedef stage<T, VEC, B_ACROSS> stage_b;
+    constexpr int BS = BA == 32 ? 64 : 32;  // of the summed index a step
+    constexpr int WAVES_A = BA == 32 ? 1 : 2, WAVES_B = 4 / WAVES_A, F = BA / WAVES_A / 32, G = BB / WAVES_B / 32;
+    typedef stage<T, VEC, A_ACROSS, BA, BS> stage_a;
+    typedef stage<T, VEC, B_ACROSS, BB, BS> stage_b;
     constexpr int BYTES_A = tile<T, stage_a::W>::bytes(A_ACROSS ? BS : BA), BYTES_B = tile<T, stage_b::W>::bytes(B_ACROSS ? BS : BB);
     __shared__ __attribute__((aligned(16))) char lds[BYTES_A + BYTES_B];
     DEAR_LDS T *as = (DEAR_LDS T *)lds, *bs = (DEAR_LDS T *)(lds + BYTES_A);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const unsigned per = (unsigned)p.a_tiles * p.b_tiles;
-    const unsigned id = KIND == WEIGHT_GRAD ? blockIdx.x % per : blockIdx.x;
-    const part t = KIND == WEIGHT_GRAD ? rows_of(p, (int)(blockIdx.x / per)) : find<BA>(p, (int)(id / p.b_tiles));
+    const unsigned per = (unsigned)p.a_tiles * p.b_tiles, id = blockIdx.x % per, which = blockIdx.x / per;  // expert, or split
+    const part t = KIND == WEIGHT_GRAD ? rows_of(p, (int)which) : find<BA>(p, (int)(id / p.b_tiles));
     if (t.none) return;
     const int b0 = (int)(id % p.b_tiles) * BB, a0 = KIND == WEIGHT_GRAD ? (int)(id / p.b_tiles) * BA : 0;
     const bool behind = KIND != WEIGHT_GRAD && t.expert == p.experts;  // rows of no expert
-    const int64_t begin = KIND == WEIGHT_GRAD ? t.begin : 0, end = behind ? 0 : KIND == WEIGHT_GRAD ? t.end : p.sum;
+    const int64_t begin = KIND == WEIGHT_GRAD ? t.begin : (int64_t)which * p.chunk;
+    const int64_t end = behind ? 0 : KIND == WEIGHT_GRAD ? t.end : min(begin + p.chunk, (int64_t)p.sum);
     const T *a = (const T *)p.a, *b = (const T *)p.b;
     if (KIND == LINEAR) b += (int64_t)t.expert * p.n_b * p.sum;
     if (KIND == INPUT_GRAD) b += (int64_t)t.expert * p.sum * p.n_b;
-    f32x16 acc[2][2] = {};
+    f32x16 acc[F][G] = {};
     stage_a sa;
     stage_b sb;
     auto load = [&](int64_t s0) {
@@ -198,33 +204,58 @@ template <typename T, bool VEC, int KIND> __global__ __launch_bounds__(THREADS, 
         if (s0 + BS < end) load(s0 + BS);
 #pragma unroll
         for (int s = 0; s < BS / 16; ++s) {
-            frag<T> f[2], g[2];
+            frag<T> f[F], g[G];
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int row = (wave / 2) * 64 + 32 * u, col = (wave % 2) * 64 + 32 * u;
+            for (int u = 0; u < F; ++u) {
+                const int row = (wave / WAVES_B) * F * 32 + 32 * u;
                 f[u] = A_ACROSS ? transposed<stage_a::W>(as, 16 * s, row, lane) : along<stage_a::W>(as, row, s, lane);
+            }
+#pragma unroll
+            for (int u = 0; u < G; ++u) {
+                const int col = (wave % WAVES_B) * G * 32 + 32 * u;
                 g[u] = B_ACROSS ? transposed<stage_b::W>(bs, 16 * s, col, lane) : along<stage_b::W>(bs, col, s, lane);
             }
 #pragma unroll
-            for (int u = 0; u < 2; ++u)
+            for (int u = 0; u < F; ++u)
 #pragma unroll
-                for (int w = 0; w < 2; ++w) acc[u][w] = mma(f[u], g[w], acc[u][w]);
+                for (int w = 0; w < G; ++w) acc[u][w] = mma(f[u], g[w], acc[u][w]);
         }
     }
     typedef typename std::conditional<KIND == WEIGHT_GRAD, float, T>::type O;
     const int64_t row0 = KIND == WEIGHT_GRAD ? a0 : t.first, row_end = KIND == WEIGHT_GRAD ? p.n_a : t.end;
-    O *out = (O *)p.out + (KIND == WEIGHT_GRAD ? (int64_t)t.expert * p.n_a * p.n_b : 0);
+    auto store = [&](auto *out) {
+        typedef typename std::remove_reference<decltype(*out)>::type to;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < F; ++u)
 #pragma unroll
-        for (int w = 0; w < 2; ++w) {
-            const int col = b0 + (wave % 2) * 64 + 32 * w + (lane & 31);
+            for (int w = 0; w < G; ++w) {
+                const int col = b0 + (wave % WAVES_B) * G * 32 + 32 * w + (lane & 31);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int64_t row = row0 + (wave / 2) * 64 + 32 * u + row_of(r, lane >> 5);
-                if (row < row_end && col < p.n_b) out[row * p.n_b + col] = (O)acc[u][w][r];
+                for (int r = 0; r < 16; ++r) {
+                    const int64_t row = row0 + (wave / WAVES_B) * F * 32 + 32 * u + row_of(r, lane >> 5);
+                    if (row < row_end && col < p.n_b) out[row * p.n_b + col] = (to)acc[u][w][r];
+                }
             }
-        }
+    };
+    if (KIND != WEIGHT_GRAD && p.splits > 1) store(p.parts + (int64_t)which * p.rows * p.n_b);
+    else store((O *)p.out + (KIND == WEIGHT_GRAD ? (int64_t)t.expert * p.n_a * p.n_b : 0));
+}
+
+// Sum of the splits, in their order, eight loads in flight, rounded once.
+template <typename T> __global__ __launch_bounds__(256) void parts_sum_kernel(const float *parts, int splits, int64_t n, T *out) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    float s = 0.f;
+    int k = 0;
+    for (; k + 8 <= splits; k += 8) {
+        float x[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) x[u] = parts[(k + u) * n + i];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += x[u];
+    }
+    for (; k < splits; ++k) s += parts[k * n + i];
+    out[i] = (T)s;
 }
 
 // ------------------------------------------------------------------------------------ bf16, whole vectors
@@ -701,7 +732,38 @@ template <int KIND> bool wide(const dear_experts_t &x, bool vec, const params &p
     return x.rows / x.experts >= 128;
 }
 
-template <int KIND> int64_t workspace_of(const dear_experts_t &) { return 0; }
+// Rows of a tile of the other kernel: as many as an expert has, in the mean of those that may have some.
+int tile_rows(const dear_experts_t &x) {
+    const int64_t rows = x.rows / (x.experts < x.rows ? x.experts : x.rows);
+    return rows <= 32 ? 32 : rows <= 96 ? 64 : 128;
+}
+
+// Splits of the summed index, of the least time by this estimate in microseconds.  A CU takes three workgroups (of 32 rows six) at a time; for
+// 32 of the summed index each takes A0 as long as loads are what it waits for, and a share S of the CU when there are more.  Several splits' sums are
+// written, read and added, 5 TB/s, in another launch.
+int choose_splits(const dear_experts_t &x, int64_t sum, int64_t columns) {
+    const int ba = tile_rows(x);
+    const int64_t tiles = (x.rows / ba + (x.experts < x.rows ? x.experts : x.rows) / 2 + 1) * ceil_div(columns, BB);
+    const double resident = ba == 32 ? 6 : 3, alone = x.dtype == DEAR_F32 ? 1.0 + 1.3 * ba / 128 : 0.7, share = (x.dtype == DEAR_F32 ? 1.8 : 0.25) * (ba + 16) / 144;
+    const int64_t upper = (x.rows / ba + x.experts + 1) * ceil_div(columns, BB);
+    int best = 1;
+    double least = 0;
+    for (int64_t s = 1; s <= 32 && (s == 1 || (s * 128 <= sum && upper * s * THREADS <= MAX_THREADS && x.rows * columns <= MAX_THREADS)); ++s) {
+        const double steps = (double)ceil_div(ceil_div(sum, s), 64) * 2, a_cu = (double)ceil_div(tiles * s, CUS);
+        const double wait = (double)(int64_t)((a_cu + resident - 1) / resident) * (3 + steps * alone), work = a_cu * steps * share;
+        const double us = 2 + (wait > work ? wait : work) + (s == 1 ? 0 : 3 + (double)(s + 1) * (double)x.rows * (double)columns * 4 / 5e6);
+        if (s == 1 || us < least) best = (int)s, least = us;
+    }
+    return best;
+}
+
+template <int KIND> int64_t workspace_of(const dear_experts_t &x) {
+    if (KIND == WEIGHT_GRAD || x.rows == 0) return 0;
+    // (a call of the wide kernel needs none, but what it takes depends on pointers)
+    const int64_t sum = KIND == LINEAR ? x.ins : x.outs, columns = KIND == LINEAR ? x.outs : x.ins;
+    const int splits = choose_splits(x, sum, columns);
+    return splits > 1 ? splits * x.rows * columns * 4 : 0;
+}
 
 template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
     if (int rc = check(x)) return rc;
@@ -738,19 +800,39 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
         return launch_status();
     }
     // tiles of rows: each expert, and the rows behind the last, may have one that is not whole
-    p.a_tiles = (int32_t)(KIND == WEIGHT_GRAD ? ceil_div(x->outs, BA) : x->rows / BA + x->experts + 1);
+    const int ba = KIND == WEIGHT_GRAD ? 128 : tile_rows(*x);
+    p.splits = KIND == WEIGHT_GRAD ? 1 : choose_splits(*x, p.sum, p.n_b);
+    p.chunk = (int32_t)(ceil_div(ceil_div(p.sum, p.splits), 64) * 64), p.parts = (float *)x->workspace;
+    p.a_tiles = (int32_t)(KIND == WEIGHT_GRAD ? ceil_div(x->outs, ba) : x->rows / ba + x->experts + 1);
     p.b_tiles = (int32_t)ceil_div(p.n_b, BB);
-    const int64_t groups = (int64_t)p.a_tiles * p.b_tiles * (KIND == WEIGHT_GRAD ? x->experts : 1);
+    const int64_t groups = (int64_t)p.a_tiles * p.b_tiles * (KIND == WEIGHT_GRAD ? x->experts : p.splits);
     if (groups * THREADS > MAX_THREADS) return DEAR_ETOOBIG;
     const unsigned n = (unsigned)groups;
+    auto by_rows = [&](auto t, auto v) {
+        typedef decltype(t) T;
+        constexpr bool VEC = decltype(v)::value;
+        if constexpr (KIND != WEIGHT_GRAD) {
+            if (ba == 32) return experts_kernel<T, VEC, KIND, 32><<<n, THREADS, 0, stream>>>(p);
+            if (ba == 64) return experts_kernel<T, VEC, KIND, 64><<<n, THREADS, 0, stream>>>(p);
+        }
+        experts_kernel<T, VEC, KIND, 128><<<n, THREADS, 0, stream>>>(p);
+    };
     if (x->dtype == DEAR_BF16) {
-        if (vec) experts_kernel<bf16, true, KIND><<<n, THREADS, 0, stream>>>(p);
-        else experts_kernel<bf16, false, KIND><<<n, THREADS, 0, stream>>>(p);
+        if (vec) by_rows(bf16(), std::true_type());
+        else by_rows(bf16(), std::false_type());
     } else {
-        if (vec) experts_kernel<float, true, KIND><<<n, THREADS, 0, stream>>>(p);
-        else experts_kernel<float, false, KIND><<<n, THREADS, 0, stream>>>(p);
+        if (vec) by_rows(float(), std::true_type());
+        else by_rows(float(), std::false_type());
     }
-    return launch_status();
+    if (int rc = launch_status()) return rc;
+    if (p.splits > 1) {
+        const int64_t all = p.rows * p.n_b;
+        const unsigned blocks = (unsigned)ceil_div(all, 256);
+        if (x->dtype == DEAR_BF16) parts_sum_kernel<<<blocks, 256, 0, stream>>>(p.parts, p.splits, all, (bf16 *)p.out);
+        else parts_sum_kernel<<<blocks, 256, 0, stream>>>(p.parts, p.splits, all, (float *)p.out);
+        return launch_status();
+    }
+    return DEAR_OK;
 }
 
 template <int KIND> int workspace(const dear_experts_t *x, int64_t *bytes) {
