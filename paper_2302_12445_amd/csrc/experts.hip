@@ -6,6 +6,7 @@
 // All three are sums of products of two operands that lie in memory either along the summed index (x and w for y, dy for dx) or across
 // it (w for dx, both for dw); the former are read from LDS in rows, the latter with the transposing reads.  Rows of an expert start
 // anywhere: a workgroup finds the expert of its tile from the ends, on the device, so that nothing waits for the host to know them.
+#include <cmath>
 #include <type_traits>
 
 #include "ops_common.h"
@@ -268,11 +269,14 @@ constexpr int WS = 64;          // summed index of a step
 constexpr int CUS = 256;
 constexpr int TABLE = 1024;     // experts that the table in LDS has places for
 
-// An operand's step in LDS.  Along the summed index: SIZE rows of 64 values, read in rows.  Across it: 64 rows of 128 columns, twice in tiles
-// of 256, read with transposing reads so that slots 0 .. 7 of half h are rows 8 h .. 8 h + 7 of sixteen, as in rows.  Pieces of 16 bytes are
-// turned within their row, as memory fills it, so that reads of several rows lie in different banks.
-template <bool ACROSS, int SIZE> struct side {
-    static constexpr int F = SIZE / 64, LOADS = SIZE / 32;  // fragments of a wave; its loads for a step, 1 KB each
+// An operand's step in LDS, for SIZE outputs that WAYS groups of waves have a part of each.  Along the summed index: SIZE rows of 64 values,
+// read in rows.  Across it: 64 rows of 128 columns, twice in tiles of 256, read with transposing reads so that slots 0 .. 7 of half h are
+// rows 8 h .. 8 h + 7 of sixteen, as in rows.  Pieces of 16 bytes are turned within their row, as memory fills it, so that reads of several
+// rows lie in different banks.
+template <bool ACROSS, int SIZE, int WAYS> struct side {
+    static constexpr int F = SIZE / WAYS / 32, LOADS = SIZE / 32;  // fragments of a wave; its loads for a step, 1 KB each
+    static constexpr int BYTES = SIZE * WS * 2;
+    static_assert(!ACROSS || SIZE >= 128, "rows of 128 columns");
     __device__ static __forceinline__ int turn(int row) {
         return ACROSS ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
     }
@@ -280,10 +284,10 @@ template <bool ACROSS, int SIZE> struct side {
     uint32_t load_at[LOADS];               // bytes from the step's place in memory, of this lane's pieces
     int lane, wave;
 
-    // which: the wave's half of the tile's outputs
+    // which: the wave's part of the tile's outputs
     __device__ __forceinline__ side(int which, int lane_, int wave_) : lane(lane_), wave(wave_) {
         if (ACROSS) {
-            const int row = 8 * (lane >> 5) + (lane & 15) / 4, c = 2 * (lane >> 4 & 1) + (lane & 3) / 2 + (SIZE == 128 ? 8 * which : 0);
+            const int row = 8 * (lane >> 5) + (lane & 15) / 4, c = 2 * (lane >> 4 & 1) + (lane & 3) / 2 + (SIZE == 128 ? 4 * F * which : 0);
 #pragma unroll
             for (int u = 0; u < F; ++u)
 #pragma unroll
@@ -292,7 +296,7 @@ template <bool ACROSS, int SIZE> struct side {
         } else {
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
-                read_at[kk] = which * (SIZE / 2 * 128) + (lane & 31) * 128 + ((2 * kk + (lane >> 5)) ^ turn(lane & 31)) * 16;
+                read_at[kk] = which * (SIZE / WAYS * 128) + (lane & 31) * 128 + ((2 * kk + (lane >> 5)) ^ turn(lane & 31)) * 16;
         }
     }
     // Fragment u (32 outputs) of quarter step kk.
@@ -324,7 +328,11 @@ template <bool ACROSS, int SIZE> struct side {
             load_at[i] = (uint32_t)r * stride + (v < (ACROSS ? outputs : left) ? v : 0) * 2;
         }
     }
-    __device__ __forceinline__ void load(const char *from, DEAR_LDS char *to, int i) const { load_to_lds(from + load_at[i], place(to, i)); }
+    // Eighths from .. to of the loads.
+    __device__ __forceinline__ void load(const char *at, DEAR_LDS char *s, int from, int to) const {
+#pragma unroll
+        for (int i = LOADS * from / 8; i < LOADS * to / 8; ++i) load_to_lds(at + load_at[i], place(s, i));
+    }
     // Zeros behind the first `left` of the summed index, in the pieces that this lane has loaded.
     __device__ __forceinline__ void clear(DEAR_LDS char *to, int left) const {
 #pragma unroll
@@ -342,16 +350,20 @@ struct wide_tile {
     bool none;
 };
 
-// The tiles that next() gives, one after another.  xa, ya and xb, yb: the operands' places for steps in turn, arrays of their own, so that a
-// read from one need not wait for what memory brings to another; lines: 4 KB a wave.
-template <int KIND, int SIZE, typename NEXT>
-__device__ __forceinline__ void run(const params &p, DEAR_LDS char *xa, DEAR_LDS char *ya, DEAR_LDS char *xb, DEAR_LDS char *yb,
+// The tiles of SA x SB outputs that next() gives, one after another.  xa, ya and xb, yb: the operands' places for steps in turn, arrays of
+// their own, so that a read from one need not wait for what memory brings to another; lines: 4 KB a wave, or null where the second step's
+// place is to serve for it as well.  PARTS: outputs are fp32 sums.
+template <int KIND, int SA, int SB, bool PARTS, typename NEXT>
+__device__ __forceinline__ void run(const params &p, void *outputs, DEAR_LDS char *xa, DEAR_LDS char *ya, DEAR_LDS char *xb, DEAR_LDS char *yb,
                                     DEAR_LDS char *lines, NEXT next) {
     constexpr bool A_ACROSS = KIND == WEIGHT_GRAD, B_ACROSS = KIND != LINEAR;
-    constexpr int F = SIZE / 64, LOADS = SIZE / 32, WAVE = SIZE / 2;
+    constexpr int WAYS_A = SA == 32 ? 1 : 2, WAYS_B = 4 / WAYS_A, WAVE_A = SA / WAYS_A, WAVE_B = SB / WAYS_B;
+    typedef side<A_ACROSS, SA, WAYS_A> side_a;
+    typedef side<B_ACROSS, SB, WAYS_B> side_b;
+    constexpr int F = side_a::F, G = side_b::F;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    side<A_ACROSS, SIZE> a(wave / 2, lane, wave);
-    side<B_ACROSS, SIZE> b(wave % 2, lane, wave);
+    side_a a(wave / WAYS_B, lane, wave);
+    side_b b(wave % WAYS_B, lane, wave);
     const uint32_t a_stride = (uint32_t)p.a_stride * 2, b_stride = (uint32_t)p.b_stride * 2;
     const char *from_a = nullptr, *from_b = nullptr;
     int64_t left = 0;  // of the summed index, from the step that is loaded next on
@@ -370,47 +382,50 @@ __device__ __forceinline__ void run(const params &p, DEAR_LDS char *xa, DEAR_LDS
         from_b += B_ACROSS ? (int64_t)WS * b_stride : WS * 2;
         left -= WS;
     };
-    auto load = [&](DEAR_LDS char *to_a, DEAR_LDS char *to_b, int from, int to) {
-#pragma unroll
-        for (int i = from; i < to; ++i) a.load(from_a, to_a, i), b.load(from_b, to_b, i);
-    };
+    auto load = [&](DEAR_LDS char *to_a, DEAR_LDS char *to_b, int from, int to) { a.load(from_a, to_a, from, to), b.load(from_b, to_b, from, to); };
 
-    f32x16 acc[F][F];
+    f32x16 acc[F][G];
     struct {
-        bf16x8 a[F], b[F];
+        bf16x8 a[F], b[G];
     } f, g;
     constexpr std::true_type yes;
     constexpr std::false_type no;
     auto read = [&](auto &x, const DEAR_LDS char *from_a, const DEAR_LDS char *from_b, int kk) {
 #pragma unroll
-        for (int u = 0; u < F; ++u) x.a[u] = a.read(from_a, u, kk), x.b[u] = b.read(from_b, u, kk);
+        for (int u = 0; u < F; ++u) x.a[u] = a.read(from_a, u, kk);
+#pragma unroll
+        for (int u = 0; u < G; ++u) x.b[u] = b.read(from_b, u, kk);
     };
     auto multiply = [&](auto &x, auto first) {  // first: of a tile's sums
 #pragma unroll
         for (int u = 0; u < F; ++u)
 #pragma unroll
-            for (int v = 0; v < F; ++v)  // a lane has one row of the outputs
+            for (int v = 0; v < G; ++v)  // a lane has one row of the outputs
                 acc[u][v] = mma(x.b[v], x.a[u], decltype(first)::value ? f32x16{} : acc[u][v]);
     };
-    // A lane has, of a row, columns apart: through 4 KB of LDS a wave, 32 rows of 128 bytes at a time, eight lanes get a whole line each.  Stored
+    // A lane has, of a row, columns apart: through 4 KB of LDS a wave, 32 rows of a line at a time, neighbouring lanes get a whole one.  Stored
     // from the lanes they come as quarters of lines (16384 x 4096 x 1024 145 us, so 132); and past the caches, which the operands want (8192
     // x 8192 x 8192 weight gradient 830 us, so 798).
     auto store = [&](const wide_tile &t) {
-        typedef typename std::conditional<KIND == WEIGHT_GRAD, float, bf16>::type O;
-        constexpr int BLOCKS = KIND == WEIGHT_GRAD ? 1 : 2;  // of 32 columns in a line
-        DEAR_LDS char *s = lines + wave * 4096;
-        const int l = lane & 31, line_at = lane / 8 * 128 + (lane % 8 ^ lane / 8) * 16;
-        const int rows = (int)min(t.row_end - t.out, (int64_t)SIZE), cols = min(p.n_b - t.col, SIZE), pitch = p.n_b * (int)sizeof(O);
-        const int row0 = (wave / 2) * WAVE + lane / 8, col0 = (wave % 2) * WAVE + lane % 8 * (int)(16 / sizeof(O));
+        constexpr bool F32 = KIND == WEIGHT_GRAD || PARTS;
+        typedef typename std::conditional<F32, float, bf16>::type O;
+        constexpr int BLOCKS = F32 || G == 1 ? 1 : 2;                  // of 32 columns in a line
+        constexpr int PIECES = BLOCKS * 32 * (int)sizeof(O) / 16;      // of 16 bytes
+        constexpr int ROWS = 64 / PIECES;                              // of a store
+        auto turned = [](int row, int piece) { return row * PIECES * 16 + (piece ^ (PIECES == 8 ? row & 7 : row >> 1 & 3)) * 16; };
+        DEAR_LDS char *s = (lines ? lines : yb) + wave * 4096;
+        const int l = lane & 31, r = lane / PIECES, line_at = turned(r, lane % PIECES);
+        const int rows = (int)min(t.row_end - t.out, (int64_t)SA), cols = min(p.n_b - t.col, SB), pitch = p.n_b * (int)sizeof(O);
+        const int row0 = (wave / WAYS_B) * WAVE_A + r, col0 = (wave % WAYS_B) * WAVE_B + lane % PIECES * (int)(16 / sizeof(O));
         const uint32_t off = (uint32_t)row0 * (uint32_t)pitch + col0 * (uint32_t)sizeof(O);
-        char *const at = (char *)((O *)p.out + t.out * p.n_b + t.col);
-        const bool whole = rows == SIZE && cols == SIZE;
+        char *const at = (char *)((O *)outputs + t.out * p.n_b + t.col);
+        const bool whole = rows == SA && cols == SB;
 #pragma unroll
         for (int u = 0; u < F; ++u)
 #pragma unroll
-            for (int v = 0; v < F; v += BLOCKS) {
-                auto put = [&](int piece, u32x4 x) { *(DEAR_LDS u32x4 *)(s + l * 128 + (piece ^ (l & 7)) * 16) = x; };
-                if (KIND == WEIGHT_GRAD) {
+            for (int v = 0; v < G; v += BLOCKS) {
+                auto put = [&](int piece, u32x4 x) { *(DEAR_LDS u32x4 *)(s + turned(l, piece)) = x; };
+                if constexpr (F32) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         f32x4 x;
@@ -421,7 +436,7 @@ __device__ __forceinline__ void run(const params &p, DEAR_LDS char *xa, DEAR_LDS
                 } else {
                     // the halves of the wave exchange fours of columns, and have eight in a row each
 #pragma unroll
-                    for (int w = 0; w < 2; ++w)
+                    for (int w = 0; w < BLOCKS; ++w)
 #pragma unroll
                         for (int q = 0; q < 2; ++q) {
                             uint32_t x[2][2];
@@ -440,17 +455,17 @@ __device__ __forceinline__ void run(const params &p, DEAR_LDS char *xa, DEAR_LDS
                 }
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < 32 / ROWS; ++i) {
                     const u32x4 x = *(DEAR_LDS u32x4 *)(s + i * 1024 + line_at);
-                    if (whole || (row0 + 32 * u + 8 * i < rows && col0 + 32 * v < cols))
-                        __builtin_nontemporal_store(x, (u32x4 *)(at + (int64_t)(32 * u + 8 * i) * pitch + 32 * v * (int)sizeof(O) + off));
+                    if (whole || (row0 + 32 * u + ROWS * i < rows && col0 + 32 * v < cols))
+                        __builtin_nontemporal_store(x, (u32x4 *)(at + (int64_t)(32 * u + ROWS * i) * pitch + 32 * v * (int)sizeof(O) + off));
                 }
                 __builtin_amdgcn_wave_barrier();
             }
     };
     // Beside the matrix instructions of a quarter step its reads, and `loads` loads.
     auto beside = [](auto loads) {
-        constexpr int N = F * F, READS = F * ((A_ACROSS ? 2 : 1) + (B_ACROSS ? 2 : 1)), LOADS = decltype(loads)::value;
+        constexpr int N = F * G, READS = F * (A_ACROSS ? 2 : 1) + G * (B_ACROSS ? 2 : 1), LOADS = decltype(loads)::value;
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -479,21 +494,23 @@ __device__ __forceinline__ void run(const params &p, DEAR_LDS char *xa, DEAR_LDS
     auto step = [&](DEAR_LDS char *x, DEAR_LDS char *y, DEAR_LDS char *to_a, DEAR_LDS char *to_b) {
         // half of the loads in the first quarter, and none in the last: all in the first one wait for one another's way (8192 x 8192 x 8192
         // 1013 us, so 947), and spread over all they come too late (988)
-        typedef std::integral_constant<int, LOADS> half;
-        typedef std::integral_constant<int, LOADS / 2> fourth;
+        constexpr int A = side_a::LOADS, B = side_b::LOADS;
+        typedef std::integral_constant<int, A * 4 / 8 + B * 4 / 8> half;
+        typedef std::integral_constant<int, A * 6 / 8 + B * 6 / 8 - half::value> fourth;
+        typedef std::integral_constant<int, A + B - half::value - fourth::value> last;
         typedef std::integral_constant<int, 0> none;
         read(f, x, y, 0);
-        load(to_a, to_b, 0, LOADS / 2);
+        load(to_a, to_b, 0, 4);
         multiply(g, no);
         beside(half());
         read(g, x, y, 1);
-        load(to_a, to_b, LOADS / 2, LOADS * 3 / 4);
+        load(to_a, to_b, 4, 6);
         multiply(f, no);
         beside(fourth());
         read(f, x, y, 2);
-        load(to_a, to_b, LOADS * 3 / 4, LOADS);
+        load(to_a, to_b, 6, 8);
         multiply(g, no);
-        beside(fourth());
+        beside(last());
         read(g, x, y, 3);
         multiply(f, no);
         beside(none());
@@ -501,21 +518,23 @@ __device__ __forceinline__ void run(const params &p, DEAR_LDS char *xa, DEAR_LDS
     };
 
     begin(now);
-    load(xa, ya, 0, LOADS);
+    load(xa, ya, 0, 8);
     loaded();
     bool any = false;  // sums of a tile to store
     for (;;) {
         if (!now.none) rest(now);
         ready(xa, ya, left + WS);
-        if (!now.none) {
-            load(xb, yb, 0, LOADS);
-            loaded();
-        }
+        if (lines && !now.none) load(xb, yb, 0, 8);
         if (any) {
             multiply(g, no);
             store(done);
         }
         if (now.none) break;
+        if (!lines) {
+            if (any) __syncthreads();  // all waves' lines are out of the second step's place
+            load(xb, yb, 0, 8);
+        }
+        loaded();
         read(f, xa, ya, 0);
         read(g, xa, ya, 1);
         multiply(f, yes);
@@ -589,25 +608,25 @@ template <int KIND, int SIZE> __device__ __forceinline__ void fill(experts_table
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // Rows of no expert: zeros.
-template <typename O> __device__ __forceinline__ void zero_rows(const params &p, int64_t first, int64_t behind) {
+template <typename O> __device__ __forceinline__ void zero_rows(const params &p, O *outputs, int64_t first, int64_t behind) {
     constexpr int E = 16 / sizeof(O);
     const int64_t n = (behind - first) * (p.n_b / E);
-    u32x4 *out = (u32x4 *)((O *)p.out + first * p.n_b);
+    u32x4 *out = (u32x4 *)(outputs + first * p.n_b);
     for (int64_t i = (int64_t)blockIdx.x * THREADS + threadIdx.x; i < n; i += (int64_t)gridDim.x * THREADS) out[i] = u32x4{0, 0, 0, 0};
 }
 
-// Tile (a_tile, b_tile) of the experts' tiles of SIZE, or a part of it: rows and columns from `down` and `across` on.  Its sum is 0 where
+// Tile (a_tile, b_tile) of the experts' tiles of SA x SB, or a part of it: rows and columns from `down` and `across` on.  Its sum is 0 where
 // there are no outputs.
-template <int KIND, int SIZE>
+template <int KIND, int SA, int SB>
 __device__ __forceinline__ wide_tile tile_of(const experts_table &x, const params &p, int rank, int a_tile, int b_tile, int down, int across) {
     wide_tile t;
     t.none = false;
-    t.col = b_tile * SIZE + across;
+    t.col = b_tile * SB + across;
     t.b_rows = p.n_b - t.col;
     int expert = 0;
     if (KIND == WEIGHT_GRAD) {
         expert = uniform(x.upto[rank]);
-        const int begin = expert ? uniform(x.ends[expert - 1]) : 0, row = a_tile * SIZE + down;
+        const int begin = expert ? uniform(x.ends[expert - 1]) : 0, row = a_tile * SA + down;
         t.sum = uniform(x.ends[expert]) - begin;
         t.a_rows = p.n_a - row;
         t.a = (const char *)p.a + ((int64_t)begin * p.a_stride + row) * 2;
@@ -623,7 +642,7 @@ __device__ __forceinline__ wide_tile tile_of(const experts_table &x, const param
             }
         }
         const int begin = expert ? uniform(x.ends[expert - 1]) : 0, end = uniform(x.ends[expert]);
-        const int64_t first = begin + (int64_t)(a_tile - (expert ? uniform(x.upto[expert - 1]) : 0)) * SIZE + down;
+        const int64_t first = begin + (int64_t)(a_tile - (expert ? uniform(x.upto[expert - 1]) : 0)) * SA + down;
         t.sum = p.sum;
         t.a_rows = (int)(end - first);
         t.a = (const char *)p.a + first * p.a_stride * 2;
@@ -663,10 +682,10 @@ template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_k
     const unsigned b_tiles = (unsigned)p.b_tiles, a_tiles = KIND == WEIGHT_GRAD ? (unsigned)p.a_tiles : (unsigned)uniform(table.upto[p.experts - 1]);
     const unsigned per = a_tiles * b_tiles, items = KIND == WEIGHT_GRAD ? per * p.experts : per, over = items % CUS;
     const unsigned whole = over <= CUS / 2 ? items - over : items;
-    if (KIND != WEIGHT_GRAD) zero_rows<bf16>(p, uniform(table.ends[p.experts - 1]), p.rows);
+    if (KIND != WEIGHT_GRAD) zero_rows(p, (bf16 *)p.out, uniform(table.ends[p.experts - 1]), p.rows);
     auto xa = (DEAR_LDS char *)a0, ya = (DEAR_LDS char *)b0, xb = (DEAR_LDS char *)a1, yb = (DEAR_LDS char *)b1;
     unsigned round = 0;
-    run<KIND, 256>(p, xa, ya, xb, yb, (DEAR_LDS char *)lines, [&] {
+    run<KIND, 256, 256, false>(p, p.out, xa, ya, xb, yb, (DEAR_LDS char *)lines, [&] {
         wide_tile t;
         for (;;) {
             const unsigned in_round = blockIdx.x % 8 * 32 + blockIdx.x / 8;
@@ -676,7 +695,7 @@ template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_k
             ++round;
             if (item >= whole) continue;
             const in_strips at(item % per, a_tiles, b_tiles);
-            t = tile_of<KIND, 256>(table, p, (int)(item / per), at.a, at.b, 0, 0);
+            t = tile_of<KIND, 256, 256>(table, p, (int)(item / per), at.a, at.b, 0, 0);
             if (t.sum > 0) return t;
             zero_tile<256>(p, t);
         }
@@ -684,7 +703,7 @@ template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_k
     if (whole == items) return;
     __syncthreads();
     round = 0;
-    run<KIND, 128>(p, xa, ya, xb, yb, (DEAR_LDS char *)lines, [&] {
+    run<KIND, 128, 128, false>(p, p.out, xa, ya, xb, yb, (DEAR_LDS char *)lines, [&] {
         wide_tile t;
         for (;;) {
             const unsigned item = round * CUS + blockIdx.x;
@@ -693,10 +712,43 @@ template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_k
             ++round;
             if (item >= 4 * over) continue;
             const in_strips at((whole + item / 4) % per, a_tiles, b_tiles);
-            t = tile_of<KIND, 256>(table, p, (int)((whole + item / 4) / per), at.a, at.b, (int)(item / 2 % 2) * 128, (int)(item % 2) * 128);
+            t = tile_of<KIND, 256, 256>(table, p, (int)((whole + item / 4) / per), at.a, at.b, (int)(item / 2 % 2) * 128, (int)(item % 2) * 128);
             if (t.sum > 0) return t;
             if (KIND == WEIGHT_GRAD && t.a_rows > 0 && t.b_rows > 0) zero_tile<128>(p, t);
         }
+    });
+}
+
+// Tiles of SA x 128, of 32 rows or of 128, for fewer rows: two workgroups a CU (of 32 rows three), and sums in several splits (PARTS) where there are
+// few tiles.  Weights are read once if an expert's rows are one tile, and bound it.
+template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, 2) void experts_few_kernel(params p) {
+    __shared__ __attribute__((aligned(16))) char a0[SA * WS * 2], a1[SA * WS * 2], b0[128 * WS * 2], b1[128 * WS * 2];
+    __shared__ experts_table table;
+    fill<KIND, SA>(table, p);
+    const unsigned b_tiles = (unsigned)p.b_tiles, a_tiles = (unsigned)uniform(table.upto[p.experts - 1]), per = a_tiles * b_tiles;
+    const unsigned items = per * (PARTS ? p.splits : 1);
+    typedef typename std::conditional<PARTS, float, bf16>::type O;
+    for (int s = 0; s < (PARTS ? p.splits : 1); ++s)
+        zero_rows(p, PARTS ? (O *)p.parts + (int64_t)s * p.rows * p.n_b : (O *)p.out, uniform(table.ends[p.experts - 1]), p.rows);
+    unsigned item = blockIdx.x;
+    run<KIND, SA, 128, PARTS>(p, PARTS ? (void *)p.parts : p.out, (DEAR_LDS char *)a0, (DEAR_LDS char *)b0, (DEAR_LDS char *)a1, (DEAR_LDS char *)b1,
+                              nullptr, [&] {
+        wide_tile t;
+        t.none = item >= items;
+        if (t.none) return t;
+        const unsigned split = PARTS ? item / per : 0;
+        const in_strips at(item - split * per, a_tiles, b_tiles);
+        t = tile_of<KIND, SA, 128>(table, p, 0, at.a, at.b, 0, 0);
+        if (PARTS) {
+            const int64_t begin = (int64_t)split * p.chunk;  // below the sum's end, as the host has it
+            t.a += begin * 2;
+            t.b += (KIND == LINEAR ? begin : begin * p.b_stride) * 2;
+            t.sum = min((int64_t)p.chunk, t.sum - begin);
+            const int64_t rows = (int64_t)split * p.rows;  // the split's outputs are as many rows further on
+            t.out += rows, t.row_end += rows;
+        }
+        item += gridDim.x;
+        return t;
     });
 }
 
@@ -723,46 +775,74 @@ bool vectors(const dear_experts_t &x, const void *p, int64_t stride, int64_t wid
     return aligned(p, 16) && stride * n % 16 == 0 && width * n % 16 == 0;
 }
 
-// Whether the wide kernel takes a call: bf16 in whole vectors, with rows that 32-bit offsets reach, and enough of it.
-template <int KIND> bool wide(const dear_experts_t &x, bool vec, const params &p) {
+// How a call's outputs are cut: tiles of 256 (WIDE), tiles of 32 or 128 rows that memory fills directly (FEW32, FEW128), or tiles whose operands
+// go through registers (ANY32, ANY64, ANY128); and the splits of the summed index.
+enum cut { WIDE, FEW32, FEW128, ANY32, ANY64, ANY128 };
+struct choice {
+    cut how;
+    int splits;
+    double us;
+};
+
+// Whether memory can fill tiles directly: bf16 in whole vectors, with rows that 32-bit offsets reach.
+template <int KIND> bool direct(const dear_experts_t &x, bool vec, const params &p) {
     const int64_t most = 1 << 22;
     if (x.dtype != DEAR_BF16 || !vec || !aligned(p.out, 16) || x.experts > TABLE || p.n_b % 8 || p.a_stride >= most || p.b_stride >= most) return false;
-    const int64_t a_tiles = KIND == WEIGHT_GRAD ? ceil_div(x.outs, 256) * x.experts : x.rows / 256 + x.experts;
-    if (a_tiles * ceil_div(p.n_b, 256) > INT32_MAX / 8) return false;
-    return x.rows / x.experts >= 128;
+    const int64_t a_tiles = KIND == WEIGHT_GRAD ? ceil_div(x.outs, 256) * x.experts : x.rows / 32 + x.experts;
+    return a_tiles * ceil_div(p.n_b, 128) <= INT32_MAX / 64;
 }
 
-// Rows of a tile of the other kernel: as many as an expert has, in the mean of those that may have some.
-int tile_rows(const dear_experts_t &x) {
-    const int64_t rows = x.rows / (x.experts < x.rows ? x.experts : x.rows);
-    return rows <= 32 ? 32 : rows <= 96 ? 64 : 128;
+// Tiles of n rows that the experts are expected to have: half of each one's last is empty.
+double row_tiles(const dear_experts_t &x, int n) {
+    const double used = (double)(x.experts < x.rows ? x.experts : x.rows), tiles = (double)x.rows / n + used / 2;
+    return tiles < used ? used : tiles;
 }
 
-// Splits of the summed index, of the least time by this estimate in microseconds.  A CU takes three workgroups (of 32 rows six) at a time; for
-// 32 of the summed index each takes A0 as long as loads are what it waits for, and a share S of the CU when there are more.  Several splits' sums are
-// written, read and added, 5 TB/s, in another launch.
-int choose_splits(const dear_experts_t &x, int64_t sum, int64_t columns) {
-    const int ba = tile_rows(x);
-    const int64_t tiles = (x.rows / ba + (x.experts < x.rows ? x.experts : x.rows) / 2 + 1) * ceil_div(columns, BB);
-    const double resident = ba == 32 ? 6 : 3, alone = x.dtype == DEAR_F32 ? 1.0 + 1.3 * ba / 128 : 0.7, share = (x.dtype == DEAR_F32 ? 1.8 : 0.25) * (ba + 16) / 144;
-    const int64_t upper = (x.rows / ba + x.experts + 1) * ceil_div(columns, BB);
-    int best = 1;
-    double least = 0;
-    for (int64_t s = 1; s <= 32 && (s == 1 || (s * 128 <= sum && upper * s * THREADS <= MAX_THREADS && x.rows * columns <= MAX_THREADS)); ++s) {
-        const double steps = (double)ceil_div(ceil_div(sum, s), 64) * 2, a_cu = (double)ceil_div(tiles * s, CUS);
-        const double wait = (double)(int64_t)((a_cu + resident - 1) / resident) * (3 + steps * alone), work = a_cu * steps * share;
-        const double us = 2 + (wait > work ? wait : work) + (s == 1 ? 0 : 3 + (double)(s + 1) * (double)x.rows * (double)columns * 4 / 5e6);
-        if (s == 1 || us < least) best = (int)s, least = us;
+// The cut and splits of the least time by this estimate, in microseconds.  A CU takes `resident` workgroups at a time; a step of 64 of the summed
+// index takes each `alone` as long as loads are what it waits for, and a `share` of the CU when there are more; all weights take their way
+// from memory.  Several splits' sums are written, read and added, 4 TB/s, in another launch.  Tiles of 256 fill the chip once each and are not
+// split; their last round goes in quarters where it is no more than half full.  Measured, over 8 experts, 4096 x 1024, tiles of 256, of 32 rows
+// and of 128: 32 rows 34, 18 and 20 us, 1024 rows 37, 36 and 25, 4096 rows 36, 95 and 50; the input gradient's, in splits of 8 of 32 rows 55,
+// 19 and 20, of 4 of 1024 rows 60, 52 and 32, and one of 4096 rows 64, 113 and 65.
+choice choose(const dear_experts_t &x, bool is_direct, int64_t sum, int64_t columns) {
+    const double steps = (double)ceil_div(sum, WS), size = x.dtype == DEAR_F32 ? 4 : 2;
+    const double weights = (double)(x.experts < x.rows ? x.experts : x.rows) * (double)sum * (double)columns * size / 5.5e6;
+    choice best = {ANY128, 1, 0};
+    auto take = [&](cut how, int n, double us) {
+        us = us > weights ? us : weights;
+        us += 4 + (n == 1 ? 0 : 3 + (double)(n + 1) * (double)x.rows * (double)columns * 4 / 4e6);
+        if (best.us == 0 || us < best.us) best = {how, n, us};
+    };
+    auto splits = [&](cut how, int ba, double resident, double alone, double share) {
+        const double tiles = row_tiles(x, ba) * (double)ceil_div(columns, BB);
+        const int64_t upper = (x.rows / ba + x.experts + 1) * ceil_div(columns, BB);
+        for (int64_t n = 1; n <= 32 && (n == 1 || (n * 2 * WS <= sum && upper * n * THREADS <= MAX_THREADS && x.rows * columns <= MAX_THREADS)); ++n) {
+            const double a_cu = std::ceil(tiles * n / CUS), each = std::ceil(steps / n);
+            const double wait = std::ceil(a_cu / resident) * (3 + each * alone), work = a_cu * each * share;
+            take(how, (int)n, wait > work ? wait : work);
+        }
+    };
+    const bool f32 = x.dtype == DEAR_F32;
+    if (is_direct) {
+        const double tiles = std::ceil(row_tiles(x, 256)) * (double)ceil_div(columns, 256), rounds = std::floor(tiles / CUS), over = tiles - rounds * CUS;
+        take(WIDE, 1, 3 + steps * 1.5 * (rounds + (over > CUS / 2 ? 1 : 0.5 * std::ceil(4 * over / CUS))));
+        splits(FEW32, 32, 3, 0.75, 0.35);
+        splits(FEW128, 128, 2, 0.85, 0.6);
+    } else {
+        splits(ANY32, 32, f32 ? 3 : 6, f32 ? 2.6 : 1.4, f32 ? 1.2 : 0.7);
+        splits(ANY64, 64, f32 ? 4 : 5, f32 ? 3.2 : 1.4, f32 ? 2.0 : 0.7);
+        splits(ANY128, 128, 3, f32 ? 4.6 : 1.4, f32 ? 3.6 : 0.7);
     }
     return best;
 }
 
 template <int KIND> int64_t workspace_of(const dear_experts_t &x) {
     if (KIND == WEIGHT_GRAD || x.rows == 0) return 0;
-    // (a call of the wide kernel needs none, but what it takes depends on pointers)
+    // what a call takes depends on its pointers
     const int64_t sum = KIND == LINEAR ? x.ins : x.outs, columns = KIND == LINEAR ? x.outs : x.ins;
-    const int splits = choose_splits(x, sum, columns);
-    return splits > 1 ? splits * x.rows * columns * 4 : 0;
+    const int any = choose(x, false, sum, columns).splits, direct = x.dtype == DEAR_BF16 ? choose(x, true, sum, columns).splits : 1;
+    const int most = any > direct ? any : direct;
+    return most > 1 ? most * x.rows * columns * 4 : 0;
 }
 
 template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
@@ -794,19 +874,31 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
         p.a = x->dy, p.a_stride = x->dy_stride, p.b = x->x, p.b_stride = x->x_stride, p.n_a = x->outs, p.n_b = x->ins;
         vec = vectors(*x, p.a, p.a_stride, x->outs) && vectors(*x, p.b, p.b_stride, x->ins);
     }
-    if (wide<KIND>(*x, vec, p)) {
+    const bool is_direct = direct<KIND>(*x, vec, p);
+    const choice c = KIND != WEIGHT_GRAD ? choose(*x, is_direct, p.sum, p.n_b) : choice{is_direct && x->rows / x->experts >= 128 ? WIDE : ANY128, 1, 0};
+    p.chunk = (int32_t)(ceil_div(ceil_div(p.sum, c.splits), WS) * WS);
+    p.splits = KIND == WEIGHT_GRAD ? 1 : (int32_t)ceil_div(p.sum, p.chunk), p.parts = (float *)x->workspace;
+    if (c.how == WIDE) {
         p.a_tiles = (int32_t)ceil_div(p.n_a, 256), p.b_tiles = (int32_t)ceil_div(p.n_b, 256);
         experts_wide_kernel<KIND><<<CUS, THREADS, 0, stream>>>(p);
         return launch_status();
     }
-    // tiles of rows: each expert, and the rows behind the last, may have one that is not whole
-    const int ba = KIND == WEIGHT_GRAD ? 128 : tile_rows(*x);
-    p.splits = KIND == WEIGHT_GRAD ? 1 : choose_splits(*x, p.sum, p.n_b);
-    p.chunk = (int32_t)(ceil_div(ceil_div(p.sum, p.splits), 64) * 64), p.parts = (float *)x->workspace;
-    p.a_tiles = (int32_t)(KIND == WEIGHT_GRAD ? ceil_div(x->outs, ba) : x->rows / ba + x->experts + 1);
     p.b_tiles = (int32_t)ceil_div(p.n_b, BB);
+    // tiles of rows: each expert, and the rows behind the last, may have one that is not whole
+    const int ba = c.how == FEW32 || c.how == ANY32 ? 32 : c.how == ANY64 ? 64 : 128;
+    p.a_tiles = (int32_t)(KIND == WEIGHT_GRAD ? ceil_div(x->outs, ba) : x->rows / ba + x->experts + 1);
     const int64_t groups = (int64_t)p.a_tiles * p.b_tiles * (KIND == WEIGHT_GRAD ? x->experts : p.splits);
     if (groups * THREADS > MAX_THREADS) return DEAR_ETOOBIG;
+    if constexpr (KIND != WEIGHT_GRAD) {
+        if (is_direct) {
+            const int64_t most = CUS * (c.how == FEW32 ? 3 : 2);
+            const unsigned n = (unsigned)(groups < most ? groups : most);
+            if (c.how == FEW32 && p.splits > 1) experts_few_kernel<KIND, 32, true><<<n, THREADS, 0, stream>>>(p);
+            else if (c.how == FEW32) experts_few_kernel<KIND, 32, false><<<n, THREADS, 0, stream>>>(p);
+            else if (p.splits > 1) experts_few_kernel<KIND, 128, true><<<n, THREADS, 0, stream>>>(p);
+            else experts_few_kernel<KIND, 128, false><<<n, THREADS, 0, stream>>>(p);
+        }
+    }
     const unsigned n = (unsigned)groups;
     auto by_rows = [&](auto t, auto v) {
         typedef decltype(t) T;
@@ -817,12 +909,14 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
         }
         experts_kernel<T, VEC, KIND, 128><<<n, THREADS, 0, stream>>>(p);
     };
-    if (x->dtype == DEAR_BF16) {
-        if (vec) by_rows(bf16(), std::true_type());
-        else by_rows(bf16(), std::false_type());
-    } else {
-        if (vec) by_rows(float(), std::true_type());
-        else by_rows(float(), std::false_type());
+    if (c.how >= ANY32) {
+        if (x->dtype == DEAR_BF16) {
+            if (vec) by_rows(bf16(), std::true_type());
+            else by_rows(bf16(), std::false_type());
+        } else {
+            if (vec) by_rows(float(), std::true_type());
+            else by_rows(float(), std::false_type());
+        }
     }
     if (int rc = launch_status()) return rc;
     if (p.splits > 1) {
