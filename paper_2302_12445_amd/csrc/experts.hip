@@ -247,15 +247,13 @@ template <typename T> __global__ __launch_bounds__(256) void parts_sum_kernel(co
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= n) return;
     float s = 0.f;
-    int k = 0;
-    for (; k + 8 <= splits; k += 8) {
+    for (int k = 0; k < splits; k += 8) {
         float x[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) x[u] = parts[(k + u) * n + i];
+        for (int u = 0; u < 8; ++u) x[u] = parts[min(k + u, splits - 1) * n + i];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) s += x[u];
+        for (int u = 0; u < 8; ++u) s += k + u < splits ? x[u] : 0.f;
     }
-    for (; k < splits; ++k) s += parts[k * n + i];
     out[i] = (T)s;
 }
 
@@ -350,14 +348,76 @@ struct wide_tile {
     bool none;
 };
 
+// A tile's sums to its outputs.  A lane has, of a row, columns apart: through 4 KB of LDS a wave, 32 rows of a line at a time, neighbouring lanes
+// get a whole one.  Stored from the lanes they come as quarters of lines (16384 x 4096 x 1024 145 us, so 132); and past the caches, which the
+// operands want (8192 x 8192 x 8192 weight gradient 830 us, so 798).  PARTS: outputs are fp32 sums.
+template <int KIND, int SA, int SB, bool PARTS, int F, int G>
+__device__ __forceinline__ void store_tile(const params &p, void *outputs, const wide_tile &t, const f32x16 (&acc)[F][G], DEAR_LDS char *lines, int lane, int wave) {
+    constexpr int WAYS_A = SA == 32 ? 1 : 2, WAYS_B = 4 / WAYS_A, WAVE_A = SA / WAYS_A, WAVE_B = SB / WAYS_B;
+    constexpr bool F32 = KIND == WEIGHT_GRAD || PARTS;
+    typedef typename std::conditional<F32, float, bf16>::type O;
+    constexpr int BLOCKS = F32 || G == 1 ? 1 : 2;                  // of 32 columns in a line
+    constexpr int PIECES = BLOCKS * 32 * (int)sizeof(O) / 16;      // of 16 bytes
+    constexpr int ROWS = 64 / PIECES;                              // of a store
+    auto turned = [](int row, int piece) { return row * PIECES * 16 + (piece ^ (PIECES == 8 ? row & 7 : row >> 1 & 3)) * 16; };
+    DEAR_LDS char *s = lines + wave * 4096;
+    const int l = lane & 31, r = lane / PIECES, line_at = turned(r, lane % PIECES);
+    const int rows = (int)min(t.row_end - t.out, (int64_t)SA), cols = min(p.n_b - t.col, SB), pitch = p.n_b * (int)sizeof(O);
+    const int row0 = (wave / WAYS_B) * WAVE_A + r, col0 = (wave % WAYS_B) * WAVE_B + lane % PIECES * (int)(16 / sizeof(O));
+    const uint32_t off = (uint32_t)row0 * (uint32_t)pitch + col0 * (uint32_t)sizeof(O);
+    char *const at = (char *)((O *)outputs + t.out * p.n_b + t.col);
+    const bool whole = rows == SA && cols == SB;
+#pragma unroll
+    for (int u = 0; u < F; ++u)
+#pragma unroll
+        for (int v = 0; v < G; v += BLOCKS) {
+            auto put = [&](int piece, u32x4 x) { *(DEAR_LDS u32x4 *)(s + turned(l, piece)) = x; };
+            if constexpr (F32) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    f32x4 x;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[k] = acc[u][v][4 * q + k];
+                    put(2 * q + (lane >> 5), __builtin_bit_cast(u32x4, x));
+                }
+            } else {
+                // the halves of the wave exchange fours of columns, and have eight in a row each
+#pragma unroll
+                for (int w = 0; w < BLOCKS; ++w)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t x[2][2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const f32x16 &c = acc[u][v + w];
+                                const bf16x2 y = {(bf16)c[8 * q + 4 * h + 2 * k], (bf16)c[8 * q + 4 * h + 2 * k + 1]};
+                                x[h][k] = __builtin_bit_cast(uint32_t, y);
+                            }
+                        const auto w0 = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
+                        const auto w1 = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
+                        put(4 * w + 2 * q + (lane >> 5), u32x4{(uint32_t)w0[0], (uint32_t)w1[0], (uint32_t)w0[1], (uint32_t)w1[1]});
+                    }
+            }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < 32 / ROWS; ++i) {
+                const u32x4 x = *(DEAR_LDS u32x4 *)(s + i * 1024 + line_at);
+                if (whole || (row0 + 32 * u + ROWS * i < rows && col0 + 32 * v < cols))
+                    __builtin_nontemporal_store(x, (u32x4 *)(at + (int64_t)(32 * u + ROWS * i) * pitch + 32 * v * (int)sizeof(O) + off));
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+}
+
 // The tiles of SA x SB outputs that next() gives, one after another.  xa, ya and xb, yb: the operands' places for steps in turn, arrays of
-// their own, so that a read from one need not wait for what memory brings to another; lines: 4 KB a wave, or null where the second step's
-// place is to serve for it as well.  PARTS: outputs are fp32 sums.
+// their own, so that a read from one need not wait for what memory brings to another; lines: 4 KB a wave.
 template <int KIND, int SA, int SB, bool PARTS, typename NEXT>
 __device__ __forceinline__ void run(const params &p, void *outputs, DEAR_LDS char *xa, DEAR_LDS char *ya, DEAR_LDS char *xb, DEAR_LDS char *yb,
                                     DEAR_LDS char *lines, NEXT next) {
     constexpr bool A_ACROSS = KIND == WEIGHT_GRAD, B_ACROSS = KIND != LINEAR;
-    constexpr int WAYS_A = SA == 32 ? 1 : 2, WAYS_B = 4 / WAYS_A, WAVE_A = SA / WAYS_A, WAVE_B = SB / WAYS_B;
+    constexpr int WAYS_A = SA == 32 ? 1 : 2, WAYS_B = 4 / WAYS_A;
     typedef side<A_ACROSS, SA, WAYS_A> side_a;
     typedef side<B_ACROSS, SB, WAYS_B> side_b;
     constexpr int F = side_a::F, G = side_b::F;
@@ -402,66 +462,6 @@ __device__ __forceinline__ void run(const params &p, void *outputs, DEAR_LDS cha
 #pragma unroll
             for (int v = 0; v < G; ++v)  // a lane has one row of the outputs
                 acc[u][v] = mma(x.b[v], x.a[u], decltype(first)::value ? f32x16{} : acc[u][v]);
-    };
-    // A lane has, of a row, columns apart: through 4 KB of LDS a wave, 32 rows of a line at a time, neighbouring lanes get a whole one.  Stored
-    // from the lanes they come as quarters of lines (16384 x 4096 x 1024 145 us, so 132); and past the caches, which the operands want (8192
-    // x 8192 x 8192 weight gradient 830 us, so 798).
-    auto store = [&](const wide_tile &t) {
-        constexpr bool F32 = KIND == WEIGHT_GRAD || PARTS;
-        typedef typename std::conditional<F32, float, bf16>::type O;
-        constexpr int BLOCKS = F32 || G == 1 ? 1 : 2;                  // of 32 columns in a line
-        constexpr int PIECES = BLOCKS * 32 * (int)sizeof(O) / 16;      // of 16 bytes
-        constexpr int ROWS = 64 / PIECES;                              // of a store
-        auto turned = [](int row, int piece) { return row * PIECES * 16 + (piece ^ (PIECES == 8 ? row & 7 : row >> 1 & 3)) * 16; };
-        DEAR_LDS char *s = (lines ? lines : yb) + wave * 4096;
-        const int l = lane & 31, r = lane / PIECES, line_at = turned(r, lane % PIECES);
-        const int rows = (int)min(t.row_end - t.out, (int64_t)SA), cols = min(p.n_b - t.col, SB), pitch = p.n_b * (int)sizeof(O);
-        const int row0 = (wave / WAYS_B) * WAVE_A + r, col0 = (wave % WAYS_B) * WAVE_B + lane % PIECES * (int)(16 / sizeof(O));
-        const uint32_t off = (uint32_t)row0 * (uint32_t)pitch + col0 * (uint32_t)sizeof(O);
-        char *const at = (char *)((O *)outputs + t.out * p.n_b + t.col);
-        const bool whole = rows == SA && cols == SB;
-#pragma unroll
-        for (int u = 0; u < F; ++u)
-#pragma unroll
-            for (int v = 0; v < G; v += BLOCKS) {
-                auto put = [&](int piece, u32x4 x) { *(DEAR_LDS u32x4 *)(s + turned(l, piece)) = x; };
-                if constexpr (F32) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        f32x4 x;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) x[k] = acc[u][v][4 * q + k];
-                        put(2 * q + (lane >> 5), __builtin_bit_cast(u32x4, x));
-                    }
-                } else {
-                    // the halves of the wave exchange fours of columns, and have eight in a row each
-#pragma unroll
-                    for (int w = 0; w < BLOCKS; ++w)
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            uint32_t x[2][2];
-#pragma unroll
-                            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                                for (int k = 0; k < 2; ++k) {
-                                    const f32x16 &c = acc[u][v + w];
-                                    const bf16x2 y = {(bf16)c[8 * q + 4 * h + 2 * k], (bf16)c[8 * q + 4 * h + 2 * k + 1]};
-                                    x[h][k] = __builtin_bit_cast(uint32_t, y);
-                                }
-                            const auto w0 = __builtin_amdgcn_permlane32_swap(x[0][0], x[1][0], false, false);
-                            const auto w1 = __builtin_amdgcn_permlane32_swap(x[0][1], x[1][1], false, false);
-                            put(4 * w + 2 * q + (lane >> 5), u32x4{(uint32_t)w0[0], (uint32_t)w1[0], (uint32_t)w0[1], (uint32_t)w1[1]});
-                        }
-                }
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                for (int i = 0; i < 32 / ROWS; ++i) {
-                    const u32x4 x = *(DEAR_LDS u32x4 *)(s + i * 1024 + line_at);
-                    if (whole || (row0 + 32 * u + ROWS * i < rows && col0 + 32 * v < cols))
-                        __builtin_nontemporal_store(x, (u32x4 *)(at + (int64_t)(32 * u + ROWS * i) * pitch + 32 * v * (int)sizeof(O) + off));
-                }
-                __builtin_amdgcn_wave_barrier();
-            }
     };
     // Beside the matrix instructions of a quarter step its reads, and `loads` loads.
     auto beside = [](auto loads) {
@@ -527,7 +527,7 @@ __device__ __forceinline__ void run(const params &p, void *outputs, DEAR_LDS cha
         if (lines && !now.none) load(xb, yb, 0, 8);
         if (any) {
             multiply(g, no);
-            store(done);
+            store_tile<KIND, SA, SB, PARTS>(p, outputs, done, acc, lines ? lines : yb, lane, wave);
         }
         if (now.none) break;
         if (!lines) {
@@ -752,6 +752,112 @@ template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, 2)
     });
 }
 
+// The same tiles where there is no more than one a CU: what it waits for is the weights' way from memory, and D - 1 steps are under way at a
+// time, 100 KB of a CU (32 rows, 4096 x 1024 over 8 15.6 us, 4.3 TB/s; with one step and three workgroups a CU 18.2).  A wave waits for its own
+// loads by the count of those behind them, and the barrier is bare: __syncthreads() waits for all loads, and makes it 18.1.
+template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, 1) void experts_deep_kernel(params p) {
+    constexpr bool B_ACROSS = KIND == INPUT_GRAD;
+    constexpr int D = SA == 32 ? 6 : 4, SB = 128, WAYS_A = SA == 32 ? 1 : 2, WAYS_B = 4 / WAYS_A;
+    typedef side<false, SA, WAYS_A> side_a;
+    typedef side<B_ACROSS, SB, WAYS_B> side_b;
+    constexpr int F = side_a::F, G = side_b::F;
+    // in arrays of their own: a read from one need not wait for what memory brings to another
+    __shared__ __attribute__((aligned(16))) char a0[side_a::BYTES], a1[side_a::BYTES], a2[side_a::BYTES], a3[side_a::BYTES], a4[D > 4 ? side_a::BYTES : 16],
+        a5[D > 4 ? side_a::BYTES : 16];
+    __shared__ __attribute__((aligned(16))) char b0[side_b::BYTES], b1[side_b::BYTES], b2[side_b::BYTES], b3[side_b::BYTES], b4[D > 4 ? side_b::BYTES : 16],
+        b5[D > 4 ? side_b::BYTES : 16];
+    __shared__ experts_table table;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    fill<KIND, SA>(table, p);
+    const unsigned b_tiles = (unsigned)p.b_tiles, a_tiles = (unsigned)uniform(table.upto[p.experts - 1]), per = a_tiles * b_tiles;
+    const unsigned items = per * (PARTS ? p.splits : 1);
+    typedef typename std::conditional<PARTS, float, bf16>::type O;
+    for (int s = 0; s < (PARTS ? p.splits : 1); ++s)
+        zero_rows(p, PARTS ? (O *)p.parts + (int64_t)s * p.rows * p.n_b : (O *)p.out, uniform(table.ends[p.experts - 1]), p.rows);
+    side_a a(wave / WAYS_B, lane, wave);
+    side_b b(wave % WAYS_B, lane, wave);
+    const uint32_t a_stride = (uint32_t)p.a_stride * 2, b_stride = (uint32_t)p.b_stride * 2;
+
+    for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
+        const unsigned split = PARTS ? item / per : 0;
+        const in_strips at(item - split * per, a_tiles, b_tiles);
+        wide_tile t = tile_of<KIND, SA, SB>(table, p, 0, at.a, at.b, 0, 0);
+        if (PARTS) {
+            const int64_t begin = (int64_t)split * p.chunk;  // below the sum's end, as the host has it
+            t.a += begin * 2;
+            t.b += (KIND == LINEAR ? begin : begin * p.b_stride) * 2;
+            t.sum = min((int64_t)p.chunk, t.sum - begin);
+            const int64_t rows = (int64_t)split * p.rows;  // the split's outputs are as many rows further on
+            t.out += rows, t.row_end += rows;
+        }
+        const int steps = (int)((t.sum + WS - 1) / WS), last = (int)(t.sum - (int64_t)(steps - 1) * WS);  // of the sum in the last step
+        a.aim(a_stride, t.a_rows, WS), b.aim(b_stride, t.b_rows, WS);
+        const char *from_a = t.a, *from_b = t.b;
+        auto load = [&](int step, DEAR_LDS char *to_a, DEAR_LDS char *to_b) {
+            if (step == steps - 1 && last < WS) a.aim(a_stride, t.a_rows, last), b.aim(b_stride, t.b_rows, last);
+            a.load(from_a, to_a, 0, 8), b.load(from_b, to_b, 0, 8);
+            from_a += WS * 2, from_b += B_ACROSS ? (int64_t)WS * b_stride : WS * 2;
+        };
+        DEAR_LDS char *const x[6] = {(DEAR_LDS char *)a0, (DEAR_LDS char *)a1, (DEAR_LDS char *)a2, (DEAR_LDS char *)a3, (DEAR_LDS char *)a4, (DEAR_LDS char *)a5};
+        DEAR_LDS char *const y[6] = {(DEAR_LDS char *)b0, (DEAR_LDS char *)b1, (DEAR_LDS char *)b2, (DEAR_LDS char *)b3, (DEAR_LDS char *)b4, (DEAR_LDS char *)b5};
+        __syncthreads();  // what is loaded over has been read
+#pragma unroll
+        for (int k = 0; k < D - 1; ++k)
+            if (k < steps) load(k, x[k], y[k]);
+        f32x16 acc[F][G] = {};
+        struct {
+            bf16x8 a[F], b[G];
+        } f, g;
+#pragma unroll
+        for (int u = 0; u < F; ++u) g.a[u] = bf16x8{};
+#pragma unroll
+        for (int u = 0; u < G; ++u) g.b[u] = bf16x8{};
+        auto read = [&](auto &q, const DEAR_LDS char *s, const DEAR_LDS char *r, int kk) {
+#pragma unroll
+            for (int u = 0; u < F; ++u) q.a[u] = a.read(s, u, kk);
+#pragma unroll
+            for (int u = 0; u < G; ++u) q.b[u] = b.read(r, u, kk);
+        };
+        auto multiply = [&](auto &q) {
+#pragma unroll
+            for (int u = 0; u < F; ++u)
+#pragma unroll
+                for (int v = 0; v < G; ++v) acc[u][v] = mma(q.b[v], q.a[u], acc[u][v]);
+        };
+        for (int base = 0; base < steps; base += D) {
+#pragma unroll
+            for (int k = 0; k < D; ++k) {
+                const int step = base + k;
+                if (step < steps) {
+                    // this step is there, of all waves, and all have read the one that is loaded over: its own loads by the count of those behind them
+                    constexpr int behind = (D - 2) * (side_a::LOADS + side_b::LOADS);
+                    if (step + D - 2 < steps) __builtin_amdgcn_s_waitcnt(0x0070 | (behind & 15) | (behind >> 4) << 14);
+                    else __builtin_amdgcn_s_waitcnt(0x0070);
+                    if (step == steps - 1 && last < WS) {
+                        a.clear(x[k], last), b.clear(y[k], last);
+                        __builtin_amdgcn_s_waitcnt(0xc07f);
+                    }
+                    asm volatile("" ::: "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    if (step + D - 1 < steps) load(step + D - 1, x[(k + D - 1) % D], y[(k + D - 1) % D]);
+                    read(f, x[k], y[k], 0);
+                    multiply(g);
+                    read(g, x[k], y[k], 1);
+                    multiply(f);
+                    read(f, x[k], y[k], 2);
+                    multiply(g);
+                    read(g, x[k], y[k], 3);
+                    multiply(f);
+                }
+            }
+        }
+        multiply(g);
+        __syncthreads();
+        store_tile<KIND, SA, SB, PARTS>(p, PARTS ? (void *)p.parts : p.out, t, acc, y[0], lane, wave);
+    }
+}
+
 // ------------------------------------------------------------------------------------ host
 constexpr int64_t MAX_ROWS = INT32_MAX;
 constexpr int32_t MAX_EXPERTS = 1 << 16, MAX_WIDTH = 1 << 20;
@@ -775,9 +881,9 @@ bool vectors(const dear_experts_t &x, const void *p, int64_t stride, int64_t wid
     return aligned(p, 16) && stride * n % 16 == 0 && width * n % 16 == 0;
 }
 
-// How a call's outputs are cut: tiles of 256 (WIDE), tiles of 32 or 128 rows that memory fills directly (FEW32, FEW128), or tiles whose operands
-// go through registers (ANY32, ANY64, ANY128); and the splits of the summed index.
-enum cut { WIDE, FEW32, FEW128, ANY32, ANY64, ANY128 };
+// How a call's outputs are cut: tiles of 256 (WIDE), tiles of 32 or 128 rows that memory fills directly (FEW32, FEW128, or one a CU with more steps
+// under way, DEEP32, DEEP128), or tiles whose operands go through registers (ANY32, ANY64, ANY128); and the splits of the summed index.
+enum cut { WIDE, FEW32, FEW128, DEEP32, DEEP128, ANY32, ANY64, ANY128 };
 struct choice {
     cut how;
     int splits;
@@ -800,16 +906,19 @@ double row_tiles(const dear_experts_t &x, int n) {
 
 // The cut and splits of the least time by this estimate, in microseconds.  A CU takes `resident` workgroups at a time; a step of 64 of the summed
 // index takes each `alone` as long as loads are what it waits for, and a `share` of the CU when there are more; all weights take their way
-// from memory.  Several splits' sums are written, read and added, 4 TB/s, in another launch.  Tiles of 256 fill the chip once each and are not
-// split; their last round goes in quarters where it is no more than half full.  Measured, over 8 experts, 4096 x 1024, tiles of 256, of 32 rows
-// and of 128: 32 rows 34, 18 and 20 us, 1024 rows 37, 36 and 25, 4096 rows 36, 95 and 50; the input gradient's, in splits of 8 of 32 rows 55,
-// 19 and 20, of 4 of 1024 rows 60, 52 and 32, and one of 4096 rows 64, 113 and 65.
+// from memory, a part of which tiles of 256 and those that begin and end at other times leave unused.  Several splits' sums are written, read
+// and added, 4 TB/s, in another launch.  Tiles of 256 fill the chip once each and are not split; their last round goes in quarters where it is
+// no more than half full.  Measured, microseconds, over 8 experts, 4096 x 1024, tiles of 256, and of 32 rows and of 128 several a CU and one a CU:
+// 32 rows 34, 18, 20, 16 and 16, 1024 rows 37, 36, 25, 38 and 21, 4096 rows 36, 95, 50, 117 and 55; over 64, 1024 x 1024, 512 rows 39, 31, -, 32
+// and 34.  The input gradient's in their best splits: 32 rows 55, 19, 20, 20 and 21, 1024 rows 60, 52, 32, 40 and 30, 4096 rows 64, 113, 65, 108
+// and 54.
 choice choose(const dear_experts_t &x, bool is_direct, int64_t sum, int64_t columns) {
     const double steps = (double)ceil_div(sum, WS), size = x.dtype == DEAR_F32 ? 4 : 2;
-    const double weights = (double)(x.experts < x.rows ? x.experts : x.rows) * (double)sum * (double)columns * size / 5.5e6;
+    const double weights = (double)(x.experts < x.rows ? x.experts : x.rows) * (double)sum * (double)columns * size / 5.8e6;
     choice best = {ANY128, 1, 0};
-    auto take = [&](cut how, int n, double us) {
-        us = us > weights ? us : weights;
+    auto take = [&](cut how, int n, double us, bool deep = false) {
+        const double least = weights * (deep ? 1 : how == WIDE ? 1.5 : 1.2);
+        us = us > least ? us : least;
         us += 4 + (n == 1 ? 0 : 3 + (double)(n + 1) * (double)x.rows * (double)columns * 4 / 4e6);
         if (best.us == 0 || us < best.us) best = {how, n, us};
     };
@@ -819,7 +928,7 @@ choice choose(const dear_experts_t &x, bool is_direct, int64_t sum, int64_t colu
         for (int64_t n = 1; n <= 32 && (n == 1 || (n * 2 * WS <= sum && upper * n * THREADS <= MAX_THREADS && x.rows * columns <= MAX_THREADS)); ++n) {
             const double a_cu = std::ceil(tiles * n / CUS), each = std::ceil(steps / n);
             const double wait = std::ceil(a_cu / resident) * (3 + each * alone), work = a_cu * each * share;
-            take(how, (int)n, wait > work ? wait : work);
+            take(how, (int)n, wait > work ? wait : work, (how == DEEP32 || how == DEEP128) && a_cu <= 1);
         }
     };
     const bool f32 = x.dtype == DEAR_F32;
@@ -828,6 +937,8 @@ choice choose(const dear_experts_t &x, bool is_direct, int64_t sum, int64_t colu
         take(WIDE, 1, 3 + steps * 1.5 * (rounds + (over > CUS / 2 ? 1 : 0.5 * std::ceil(4 * over / CUS))));
         splits(FEW32, 32, 3, 0.75, 0.35);
         splits(FEW128, 128, 2, 0.85, 0.6);
+        splits(DEEP32, 32, 1, 0.35, 0.35);
+        splits(DEEP128, 128, 1, 0.55, 0.55);
     } else {
         splits(ANY32, 32, f32 ? 3 : 6, f32 ? 2.6 : 1.4, f32 ? 1.2 : 0.7);
         splits(ANY64, 64, f32 ? 4 : 5, f32 ? 3.2 : 1.4, f32 ? 2.0 : 0.7);
@@ -885,18 +996,26 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
     }
     p.b_tiles = (int32_t)ceil_div(p.n_b, BB);
     // tiles of rows: each expert, and the rows behind the last, may have one that is not whole
-    const int ba = c.how == FEW32 || c.how == ANY32 ? 32 : c.how == ANY64 ? 64 : 128;
+    const int ba = c.how == FEW32 || c.how == DEEP32 || c.how == ANY32 ? 32 : c.how == ANY64 ? 64 : 128;
     p.a_tiles = (int32_t)(KIND == WEIGHT_GRAD ? ceil_div(x->outs, ba) : x->rows / ba + x->experts + 1);
     const int64_t groups = (int64_t)p.a_tiles * p.b_tiles * (KIND == WEIGHT_GRAD ? x->experts : p.splits);
     if (groups * THREADS > MAX_THREADS) return DEAR_ETOOBIG;
     if constexpr (KIND != WEIGHT_GRAD) {
         if (is_direct) {
-            const int64_t most = CUS * (c.how == FEW32 ? 3 : 2);
-            const unsigned n = (unsigned)(groups < most ? groups : most);
-            if (c.how == FEW32 && p.splits > 1) experts_few_kernel<KIND, 32, true><<<n, THREADS, 0, stream>>>(p);
-            else if (c.how == FEW32) experts_few_kernel<KIND, 32, false><<<n, THREADS, 0, stream>>>(p);
-            else if (p.splits > 1) experts_few_kernel<KIND, 128, true><<<n, THREADS, 0, stream>>>(p);
-            else experts_few_kernel<KIND, 128, false><<<n, THREADS, 0, stream>>>(p);
+            auto of = [&](auto rows, auto parts) {
+                constexpr int SA = decltype(rows)::value;
+                constexpr bool PARTS = decltype(parts)::value;
+                const int64_t most = c.how == DEEP32 || c.how == DEEP128 ? CUS : SA == 32 ? 3 * CUS : 2 * CUS;
+                const unsigned n = (unsigned)(groups < most ? groups : most);
+                if (c.how == DEEP32 || c.how == DEEP128) experts_deep_kernel<KIND, SA, PARTS><<<n, THREADS, 0, stream>>>(p);
+                else experts_few_kernel<KIND, SA, PARTS><<<n, THREADS, 0, stream>>>(p);
+            };
+            auto by_parts = [&](auto rows) {
+                if (p.splits > 1) of(rows, std::true_type());
+                else of(rows, std::false_type());
+            };
+            if (ba == 32) by_parts(std::integral_constant<int, 32>());
+            else by_parts(std::integral_constant<int, 128>());
         }
     }
     const unsigned n = (unsigned)groups;
