@@ -671,125 +671,51 @@ struct in_strips {
     }
 };
 
-// Tiles of 256.  Items go to the eight XCDs in runs of 32, one for each of its CUs; of a weight gradient, whose tiles differ, every other round
-// backwards.  What fills a last round by half at most goes in quarters, tiles of 128: 256 of them take 0.38 of a round of tiles (sums of 4096:
-// 40 of 106 us), so that one or two rounds of quarters are ahead of a round, and three are not (12288 x 1024 x 4096 126 against 106 us).
-template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_kernel(params p) {
-    constexpr int BYTES = 256 * WS * 2;
-    __shared__ __attribute__((aligned(16))) char a0[BYTES], a1[BYTES], b0[BYTES], b1[BYTES], lines[THREADS / 64 * 4096];
-    __shared__ experts_table table;
-    fill<KIND, 256>(table, p);
-    const unsigned b_tiles = (unsigned)p.b_tiles, a_tiles = KIND == WEIGHT_GRAD ? (unsigned)p.a_tiles : (unsigned)uniform(table.upto[p.experts - 1]);
-    const unsigned per = a_tiles * b_tiles, items = KIND == WEIGHT_GRAD ? per * p.experts : per, over = items % CUS;
-    const unsigned whole = over <= CUS / 2 ? items - over : items;
-    if (KIND != WEIGHT_GRAD) zero_rows(p, (bf16 *)p.out, uniform(table.ends[p.experts - 1]), p.rows);
-    auto xa = (DEAR_LDS char *)a0, ya = (DEAR_LDS char *)b0, xb = (DEAR_LDS char *)a1, yb = (DEAR_LDS char *)b1;
-    unsigned round = 0;
-    run<KIND, 256, 256, false>(p, p.out, xa, ya, xb, yb, (DEAR_LDS char *)lines, [&] {
-        wide_tile t;
-        for (;;) {
-            const unsigned in_round = blockIdx.x % 8 * 32 + blockIdx.x / 8;
-            const unsigned item = round * CUS + (KIND == WEIGHT_GRAD && round % 2 ? CUS - 1 - in_round : in_round);
-            t.none = round * CUS >= whole;
-            if (t.none) return t;
-            ++round;
-            if (item >= whole) continue;
-            const in_strips at(item % per, a_tiles, b_tiles);
-            t = tile_of<KIND, 256, 256>(table, p, (int)(item / per), at.a, at.b, 0, 0);
-            if (t.sum > 0) return t;
-            zero_tile<256>(p, t);
-        }
-    });
-    if (whole == items) return;
-    __syncthreads();
-    round = 0;
-    run<KIND, 128, 128, false>(p, p.out, xa, ya, xb, yb, (DEAR_LDS char *)lines, [&] {
-        wide_tile t;
-        for (;;) {
-            const unsigned item = round * CUS + blockIdx.x;
-            t.none = round * CUS >= 4 * over;
-            if (t.none) return t;
-            ++round;
-            if (item >= 4 * over) continue;
-            const in_strips at((whole + item / 4) % per, a_tiles, b_tiles);
-            t = tile_of<KIND, 256, 256>(table, p, (int)((whole + item / 4) / per), at.a, at.b, (int)(item / 2 % 2) * 128, (int)(item % 2) * 128);
-            if (t.sum > 0) return t;
-            if (KIND == WEIGHT_GRAD && t.a_rows > 0 && t.b_rows > 0) zero_tile<128>(p, t);
-        }
-    });
+// Tiles of SA x 128 outputs of splits of the sum, one after another.
+template <int KIND, int SA, bool PARTS> __device__ __forceinline__ wide_tile few_tile(const experts_table &table, const params &p, unsigned &item) {
+    const unsigned b_tiles = (unsigned)p.b_tiles, a_tiles = (unsigned)uniform(table.upto[p.experts - 1]), per = a_tiles * b_tiles;
+    wide_tile t;
+    t.none = item >= per * (PARTS ? p.splits : 1);
+    if (t.none) return t;
+    const unsigned split = PARTS ? item / per : 0;
+    const in_strips at(item - split * per, a_tiles, b_tiles);
+    t = tile_of<KIND, SA, 128>(table, p, 0, at.a, at.b, 0, 0);
+    if (PARTS) {
+        const int64_t begin = (int64_t)split * p.chunk;  // below the sum's end, as the host has it
+        t.a += begin * 2;
+        t.b += (KIND == LINEAR ? begin : begin * p.b_stride) * 2;
+        t.sum = min((int64_t)p.chunk, t.sum - begin);
+        const int64_t rows = (int64_t)split * p.rows;  // the split's outputs are as many rows further on
+        t.out += rows, t.row_end += rows;
+    }
+    item += gridDim.x;
+    return t;
 }
 
-// Tiles of SA x 128, of 32 rows or of 128, for fewer rows: two workgroups a CU (of 32 rows three), and sums in several splits (PARTS) where there are
-// few tiles.  Weights are read once if an expert's rows are one tile, and bound it.
-template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, 2) void experts_few_kernel(params p) {
-    __shared__ __attribute__((aligned(16))) char a0[SA * WS * 2], a1[SA * WS * 2], b0[128 * WS * 2], b1[128 * WS * 2];
-    __shared__ experts_table table;
-    fill<KIND, SA>(table, p);
-    const unsigned b_tiles = (unsigned)p.b_tiles, a_tiles = (unsigned)uniform(table.upto[p.experts - 1]), per = a_tiles * b_tiles;
-    const unsigned items = per * (PARTS ? p.splits : 1);
+// Zeros in the rows of no expert, in all splits' sums.
+template <bool PARTS> __device__ __forceinline__ void few_rest(const experts_table &table, const params &p) {
     typedef typename std::conditional<PARTS, float, bf16>::type O;
     for (int s = 0; s < (PARTS ? p.splits : 1); ++s)
         zero_rows(p, PARTS ? (O *)p.parts + (int64_t)s * p.rows * p.n_b : (O *)p.out, uniform(table.ends[p.experts - 1]), p.rows);
-    unsigned item = blockIdx.x;
-    run<KIND, SA, 128, PARTS>(p, PARTS ? (void *)p.parts : p.out, (DEAR_LDS char *)a0, (DEAR_LDS char *)b0, (DEAR_LDS char *)a1, (DEAR_LDS char *)b1,
-                              nullptr, [&] {
-        wide_tile t;
-        t.none = item >= items;
-        if (t.none) return t;
-        const unsigned split = PARTS ? item / per : 0;
-        const in_strips at(item - split * per, a_tiles, b_tiles);
-        t = tile_of<KIND, SA, 128>(table, p, 0, at.a, at.b, 0, 0);
-        if (PARTS) {
-            const int64_t begin = (int64_t)split * p.chunk;  // below the sum's end, as the host has it
-            t.a += begin * 2;
-            t.b += (KIND == LINEAR ? begin : begin * p.b_stride) * 2;
-            t.sum = min((int64_t)p.chunk, t.sum - begin);
-            const int64_t rows = (int64_t)split * p.rows;  // the split's outputs are as many rows further on
-            t.out += rows, t.row_end += rows;
-        }
-        item += gridDim.x;
-        return t;
-    });
 }
 
-// The same tiles where there is no more than one a CU: what it waits for is the weights' way from memory, and D - 1 steps are under way at a
-// time, 100 KB of a CU (32 rows, 4096 x 1024 over 8 15.6 us, 4.3 TB/s; with one step and three workgroups a CU 18.2).  A wave waits for its own
-// loads by the count of those behind them, and the barrier is bare: __syncthreads() waits for all loads, and makes it 18.1.
-template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, 1) void experts_deep_kernel(params p) {
+// The tiles of SA x 128 outputs that next() gives, with D - 1 steps under way.  x, y: the operands' places for D steps in turn; the first of y
+// holds 16 KB.
+template <int KIND, int SA, bool PARTS, int D, typename NEXT>
+__device__ __forceinline__ void run_deep(const params &p, void *outputs, DEAR_LDS char *const (&x)[D], DEAR_LDS char *const (&y)[D], NEXT next) {
     constexpr bool B_ACROSS = KIND == INPUT_GRAD;
-    constexpr int D = SA == 32 ? 6 : 4, SB = 128, WAYS_A = SA == 32 ? 1 : 2, WAYS_B = 4 / WAYS_A;
+    constexpr int SB = 128, WAYS_A = SA == 32 ? 1 : 2, WAYS_B = 4 / WAYS_A;
     typedef side<false, SA, WAYS_A> side_a;
     typedef side<B_ACROSS, SB, WAYS_B> side_b;
     constexpr int F = side_a::F, G = side_b::F;
-    // in arrays of their own: a read from one need not wait for what memory brings to another
-    __shared__ __attribute__((aligned(16))) char a0[side_a::BYTES], a1[side_a::BYTES], a2[side_a::BYTES], a3[side_a::BYTES], a4[D > 4 ? side_a::BYTES : 16],
-        a5[D > 4 ? side_a::BYTES : 16];
-    __shared__ __attribute__((aligned(16))) char b0[side_b::BYTES], b1[side_b::BYTES], b2[side_b::BYTES], b3[side_b::BYTES], b4[D > 4 ? side_b::BYTES : 16],
-        b5[D > 4 ? side_b::BYTES : 16];
-    __shared__ experts_table table;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    fill<KIND, SA>(table, p);
-    const unsigned b_tiles = (unsigned)p.b_tiles, a_tiles = (unsigned)uniform(table.upto[p.experts - 1]), per = a_tiles * b_tiles;
-    const unsigned items = per * (PARTS ? p.splits : 1);
-    typedef typename std::conditional<PARTS, float, bf16>::type O;
-    for (int s = 0; s < (PARTS ? p.splits : 1); ++s)
-        zero_rows(p, PARTS ? (O *)p.parts + (int64_t)s * p.rows * p.n_b : (O *)p.out, uniform(table.ends[p.experts - 1]), p.rows);
     side_a a(wave / WAYS_B, lane, wave);
     side_b b(wave % WAYS_B, lane, wave);
     const uint32_t a_stride = (uint32_t)p.a_stride * 2, b_stride = (uint32_t)p.b_stride * 2;
 
-    for (unsigned item = blockIdx.x; item < items; item += gridDim.x) {
-        const unsigned split = PARTS ? item / per : 0;
-        const in_strips at(item - split * per, a_tiles, b_tiles);
-        wide_tile t = tile_of<KIND, SA, SB>(table, p, 0, at.a, at.b, 0, 0);
-        if (PARTS) {
-            const int64_t begin = (int64_t)split * p.chunk;  // below the sum's end, as the host has it
-            t.a += begin * 2;
-            t.b += (KIND == LINEAR ? begin : begin * p.b_stride) * 2;
-            t.sum = min((int64_t)p.chunk, t.sum - begin);
-            const int64_t rows = (int64_t)split * p.rows;  // the split's outputs are as many rows further on
-            t.out += rows, t.row_end += rows;
-        }
+    for (;;) {
+        const wide_tile t = next();
+        if (t.none) return;
         const int steps = (int)((t.sum + WS - 1) / WS), last = (int)(t.sum - (int64_t)(steps - 1) * WS);  // of the sum in the last step
         a.aim(a_stride, t.a_rows, WS), b.aim(b_stride, t.b_rows, WS);
         const char *from_a = t.a, *from_b = t.b;
@@ -798,8 +724,6 @@ template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, 1)
             a.load(from_a, to_a, 0, 8), b.load(from_b, to_b, 0, 8);
             from_a += WS * 2, from_b += B_ACROSS ? (int64_t)WS * b_stride : WS * 2;
         };
-        DEAR_LDS char *const x[6] = {(DEAR_LDS char *)a0, (DEAR_LDS char *)a1, (DEAR_LDS char *)a2, (DEAR_LDS char *)a3, (DEAR_LDS char *)a4, (DEAR_LDS char *)a5};
-        DEAR_LDS char *const y[6] = {(DEAR_LDS char *)b0, (DEAR_LDS char *)b1, (DEAR_LDS char *)b2, (DEAR_LDS char *)b3, (DEAR_LDS char *)b4, (DEAR_LDS char *)b5};
         __syncthreads();  // what is loaded over has been read
 #pragma unroll
         for (int k = 0; k < D - 1; ++k)
@@ -854,7 +778,112 @@ template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, 1)
         }
         multiply(g);
         __syncthreads();
-        store_tile<KIND, SA, SB, PARTS>(p, PARTS ? (void *)p.parts : p.out, t, acc, y[0], lane, wave);
+        store_tile<KIND, SA, SB, PARTS>(p, outputs, t, acc, y[0], lane, wave);
+    }
+}
+
+// Tiles of 256.  Items go to the eight XCDs in runs of 32, one for each of its CUs; of a weight gradient, whose tiles differ, every other round
+// backwards.  What fills a last round by half at most goes in quarters, tiles of 128: 256 of them take 0.38 of a round of tiles (sums of 4096:
+// 40 of 106 us), so that one or two rounds of quarters are ahead of a round, and three are not (12288 x 1024 x 4096 126 against 106 us).  Where
+// it fills no more than a sixteenth, 32 x 128 outputs a CU take 25 us in place of 40 (16385 x 4096 x 1024, input gradient, 148 to 132 us).
+template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_kernel(params p) {
+    constexpr int BYTES = 256 * WS * 2;
+    __shared__ __attribute__((aligned(16))) char a0[BYTES], a1[BYTES], b0[BYTES], b1[BYTES], lines[THREADS / 64 * 4096];
+    __shared__ experts_table table;
+    fill<KIND, 256>(table, p);
+    const unsigned b_tiles = (unsigned)p.b_tiles, a_tiles = KIND == WEIGHT_GRAD ? (unsigned)p.a_tiles : (unsigned)uniform(table.upto[p.experts - 1]);
+    const unsigned per = a_tiles * b_tiles, items = KIND == WEIGHT_GRAD ? per * p.experts : per, over = items % CUS;
+    const unsigned whole = over <= CUS / 2 ? items - over : items;
+    if (KIND != WEIGHT_GRAD) zero_rows(p, (bf16 *)p.out, uniform(table.ends[p.experts - 1]), p.rows);
+    auto xa = (DEAR_LDS char *)a0, ya = (DEAR_LDS char *)b0, xb = (DEAR_LDS char *)a1, yb = (DEAR_LDS char *)b1;
+    unsigned round = 0;
+    run<KIND, 256, 256, false>(p, p.out, xa, ya, xb, yb, (DEAR_LDS char *)lines, [&] {
+        wide_tile t;
+        for (;;) {
+            const unsigned in_round = blockIdx.x % 8 * 32 + blockIdx.x / 8;
+            const unsigned item = round * CUS + (KIND == WEIGHT_GRAD && round % 2 ? CUS - 1 - in_round : in_round);
+            t.none = round * CUS >= whole;
+            if (t.none) return t;
+            ++round;
+            if (item >= whole) continue;
+            const in_strips at(item % per, a_tiles, b_tiles);
+            t = tile_of<KIND, 256, 256>(table, p, (int)(item / per), at.a, at.b, 0, 0);
+            if (t.sum > 0) return t;
+            zero_tile<256>(p, t);
+        }
+    });
+    if (whole == items) return;
+    __syncthreads();
+    if constexpr (KIND != WEIGHT_GRAD) {
+        if (over <= CUS / 16) {
+            constexpr int A = 32 * WS * 2;
+            DEAR_LDS char *const x[4] = {xa, xb, ya, yb}, *const y[4] = {xa + A, xb + A, ya + A, yb + A};
+            unsigned item = blockIdx.x;
+            run_deep<KIND, 32, false, 4>(p, p.out, x, y, [&] {
+                wide_tile t;
+                for (;;) {
+                    t.none = item >= 16 * over;
+                    if (t.none) return t;
+                    const in_strips at((whole + item / 16) % per, a_tiles, b_tiles);
+                    t = tile_of<KIND, 256, 256>(table, p, 0, at.a, at.b, (int)(item / 2 % 8) * 32, (int)(item % 2) * 128);
+                    item += CUS;
+                    if (t.sum > 0) return t;
+                }
+            });
+            return;
+        }
+    }
+    round = 0;
+    run<KIND, 128, 128, false>(p, p.out, xa, ya, xb, yb, (DEAR_LDS char *)lines, [&] {
+        wide_tile t;
+        for (;;) {
+            const unsigned item = round * CUS + blockIdx.x;
+            t.none = round * CUS >= 4 * over;
+            if (t.none) return t;
+            ++round;
+            if (item >= 4 * over) continue;
+            const in_strips at((whole + item / 4) % per, a_tiles, b_tiles);
+            t = tile_of<KIND, 256, 256>(table, p, (int)((whole + item / 4) / per), at.a, at.b, (int)(item / 2 % 2) * 128, (int)(item % 2) * 128);
+            if (t.sum > 0) return t;
+            if (KIND == WEIGHT_GRAD && t.a_rows > 0 && t.b_rows > 0) zero_tile<128>(p, t);
+        }
+    });
+}
+
+// Tiles of SA x 128, of 32 rows or of 128, for fewer rows: two workgroups a CU (of 32 rows three), and sums in several splits (PARTS) where there are
+// few tiles.  Weights are read once if an expert's rows are one tile, and bound it.
+template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, 2) void experts_few_kernel(params p) {
+    __shared__ __attribute__((aligned(16))) char a0[SA * WS * 2], a1[SA * WS * 2], b0[128 * WS * 2], b1[128 * WS * 2];
+    __shared__ experts_table table;
+    fill<KIND, SA>(table, p);
+    few_rest<PARTS>(table, p);
+    unsigned item = blockIdx.x;
+    run<KIND, SA, 128, PARTS>(p, PARTS ? (void *)p.parts : p.out, (DEAR_LDS char *)a0, (DEAR_LDS char *)b0, (DEAR_LDS char *)a1, (DEAR_LDS char *)b1,
+                              nullptr, [&] { return few_tile<KIND, SA, PARTS>(table, p, item); });
+}
+
+// The same tiles where there is no more than one a CU: what it waits for is the weights' way from memory, and D - 1 steps are under way at a
+// time, 100 KB of a CU (32 rows, 4096 x 1024 over 8 15.6 us, 4.3 TB/s; with one step and three workgroups a CU 18.2).  A wave waits for its own
+// loads by the count of those behind them, and the barrier is bare: __syncthreads() waits for all loads, and makes it 18.1.
+template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, 1) void experts_deep_kernel(params p) {
+    constexpr int D = SA == 32 ? 6 : 4, A = SA * WS * 2, B = 128 * WS * 2;
+    // in arrays of their own: a read from one need not wait for what memory brings to another
+    __shared__ __attribute__((aligned(16))) char a0[A], a1[A], a2[A], a3[A], a4[D > 4 ? A : 16], a5[D > 4 ? A : 16];
+    __shared__ __attribute__((aligned(16))) char b0[B], b1[B], b2[B], b3[B], b4[D > 4 ? B : 16], b5[D > 4 ? B : 16];
+    __shared__ experts_table table;
+    fill<KIND, SA>(table, p);
+    unsigned item = blockIdx.x;
+    auto next = [&] { return few_tile<KIND, SA, PARTS>(table, p, item); };
+    few_rest<PARTS>(table, p);
+    void *const outputs = PARTS ? (void *)p.parts : p.out;
+    if constexpr (D == 6) {
+        DEAR_LDS char *const x[D] = {(DEAR_LDS char *)a0, (DEAR_LDS char *)a1, (DEAR_LDS char *)a2, (DEAR_LDS char *)a3, (DEAR_LDS char *)a4, (DEAR_LDS char *)a5};
+        DEAR_LDS char *const y[D] = {(DEAR_LDS char *)b0, (DEAR_LDS char *)b1, (DEAR_LDS char *)b2, (DEAR_LDS char *)b3, (DEAR_LDS char *)b4, (DEAR_LDS char *)b5};
+        run_deep<KIND, SA, PARTS, D>(p, outputs, x, y, next);
+    } else {
+        DEAR_LDS char *const x[D] = {(DEAR_LDS char *)a0, (DEAR_LDS char *)a1, (DEAR_LDS char *)a2, (DEAR_LDS char *)a3};
+        DEAR_LDS char *const y[D] = {(DEAR_LDS char *)b0, (DEAR_LDS char *)b1, (DEAR_LDS char *)b2, (DEAR_LDS char *)b3};
+        run_deep<KIND, SA, PARTS, D>(p, outputs, x, y, next);
     }
 }
 
@@ -934,7 +963,7 @@ choice choose(const dear_experts_t &x, bool is_direct, int64_t sum, int64_t colu
     const bool f32 = x.dtype == DEAR_F32;
     if (is_direct) {
         const double tiles = std::ceil(row_tiles(x, 256)) * (double)ceil_div(columns, 256), rounds = std::floor(tiles / CUS), over = tiles - rounds * CUS;
-        take(WIDE, 1, 3 + steps * 1.5 * (rounds + (over > CUS / 2 ? 1 : 0.5 * std::ceil(4 * over / CUS))));
+        take(WIDE, 1, 3 + steps * 1.5 * (rounds + (over > CUS / 2 ? 1 : over > CUS / 16 ? 0.5 * std::ceil(4 * over / CUS) : over > 0 ? 0.3 : 0)));
         splits(FEW32, 32, 3, 0.75, 0.35);
         splits(FEW128, 128, 2, 0.85, 0.6);
         splits(DEEP32, 32, 1, 0.35, 0.35);

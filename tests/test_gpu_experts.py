@@ -117,6 +117,12 @@ def test_long_sums_and_many_tiles(ops, sizes):
     check(ops, *make(counts, 0, outs, ins, BF16, 13))
 
 
+@pytest.mark.parametrize("outs, ins", [(136, 1000), (1000, 136)])
+def test_few_tiles_behind_a_round(ops, outs, ins):
+    """66 x 4 tiles of 256: one for each of 256 units, and eight."""
+    check(ops, *make([8001, 20, 8200], 5, outs, ins, BF16, 40))
+
+
 def test_far_weights(ops):
     """Weights of more elements than 31 bits count: the last expert's, and far rows."""
     E, N, K = 9, 16384, 16384
