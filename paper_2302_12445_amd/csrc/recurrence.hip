@@ -607,9 +607,13 @@ int call(const dear_recurrence_t *r, bool backward, hipStream_t stream) {
         if (backward) launch<T, decltype(mode)::value, true>(a, r->batch, shares(*r), r->workspace, stream);
         else launch<T, decltype(mode)::value, false>(a, r->batch, shares(*r), r->workspace, stream);
     };
+    // Of an odd width two workgroups take the last channel but one, with the same results.  Where the state before is overwritten with the one
+    // behind, the second could find the latter: there each channel has one workgroup.
+    const bool over_itself = backward ? r->dstate && r->dstate == r->dlast : r->last && r->last == r->state;
+    const bool apart = over_itself && r->width % N && r->width > CG && !shares(*r);
     auto by_type = [&](auto t) {
         if (vec) by_mode(t, std::integral_constant<int, ALIGNED>());
-        else if (r->width >= N) by_mode(t, std::integral_constant<int, ANYWHERE>());
+        else if (r->width >= N && !apart) by_mode(t, std::integral_constant<int, ANYWHERE>());
         else by_mode(t, std::integral_constant<int, SINGLE>());
     };
     if (r->dtype == DEAR_BF16) by_type(bf16());

@@ -250,6 +250,28 @@ def test_state_in_place(ops):
         assert all(torch.equal(a, b) for a, b in zip((dx, dg, dlast), grads))
 
 
+@pytest.mark.parametrize("shape", [(4000, 1, 65), (900, 100, 129), (3, 200, 1001), (1, 20, 1)])
+def test_state_in_place_of_odd_widths(ops, shape):
+    """The last channels of an odd width are not read by a workgroup that does not write them."""
+    x, gate, state = inputs(shape, F32, 51)
+    want = ops.recurrence(x, gate, state)
+    s, h = state.clone(), torch.empty_like(x)
+    lib, (B, T, C) = ops.load_library(), shape
+    held, places, head = ops._recurrence_sizes(x, gate, None)
+    space, at, need = ops._recurrence_space(head, x.device)
+    none = (0, 0, 0)
+    packed = ops._RECURRENCE.pack(*head, *places, s.data_ptr(), 0, h.data_ptr(), T * C, C, s.data_ptr(), *none, 0, *none, *none, 0, at, need)
+    assert lib.dear_recurrence(packed, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(h, want[0]) and torch.equal(s, want[1])
+    dlast = normal(torch.Generator().manual_seed(52), state.shape)
+    grads = ops.recurrence_backward(h, x, gate, want[2], dlast=dlast)
+    dx, dg = torch.empty_like(x), torch.empty_like(x)
+    packed = ops._RECURRENCE.pack(*head, *places, 0, want[2].data_ptr(), *none, 0, h.data_ptr(), T * C, C, dlast.data_ptr(), dx.data_ptr(),
+                                  T * C, C, dg.data_ptr(), T * C, C, dlast.data_ptr(), at, need)
+    assert lib.dear_recurrence_backward(packed, torch.cuda.current_stream().cuda_stream) == 0
+    assert all(torch.equal(a, b) for a, b in zip((dx, dg, dlast), grads))
+
+
 def test_far_elements(ops):
     """Sequences whose elements lie further apart than 32 bits count."""
     B, T, C = 3, 300, 64
