@@ -318,11 +318,13 @@ class Experts(torch.nn.Module):
     def forward(self, y: torch.Tensor, lens: Optional[torch.Tensor] = None) -> torch.Tensor:
         batch, tokens, width = y.shape
         rows = y.reshape(-1, width)
+        if lens is not None:
+            valid = (torch.arange(tokens, device=y.device) < lens.view(-1, 1)).view(-1, 1)
+            rows = torch.where(valid, rows, 0)  # what stands behind the lengths may be anything: the router is not to see it
         # chosen in fp32, whatever the activations' type: a rounding must not send a token elsewhere
         scores, chosen = (rows.float() @ self.router.t()).topk(self.top, -1)
         share = torch.softmax(scores, -1)
         if lens is not None:
-            valid = (torch.arange(tokens, device=y.device) < lens.view(-1, 1)).view(-1, 1)
             chosen = torch.where(valid, chosen, self.experts)
         sorted_, order = chosen.flatten().sort(stable=True)
         ends = torch.searchsorted(sorted_, torch.arange(self.experts, device=y.device), right=True).to(torch.int32)

@@ -106,6 +106,27 @@ def test_tokens_one_by_one():
     assert share(torch.cat(parts, 1), want.double().cpu()) < 1e-5
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_experts_take_nothing_from_behind_the_sequences(dtype):
+    """What stands behind the lengths, NaN here, reaches neither results nor gradients."""
+    from paper_2302_12445_amd.layers import Experts
+    torch.manual_seed(6)
+    layer = Experts(32, 48, 5, 2).to(DEV)
+    y = torch.randn(3, 7, 32, device=DEV).to(dtype)
+    lens = torch.tensor([7, 0, 3], dtype=torch.int32, device=DEV)
+    results = []
+    for fill in (0.0, math.nan):
+        a = y.clone()
+        a[1], a[2, 3:] = fill, fill
+        a.requires_grad_()
+        layer.zero_grad()
+        out = layer(a, lens)
+        out.float().square().sum().backward()
+        results.append([out, a.grad] + [p.grad.clone() for p in layer.parameters()])
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    assert not results[1][0][1].any() and not results[1][1][2, 3:].any()
+
+
 def test_experts_spread_and_gather():
     """Each token goes to its experts and back, none to others; gradients of tokens that go to several are added."""
     from paper_2302_12445_amd.layers import Experts
