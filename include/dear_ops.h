@@ -247,7 +247,7 @@ typedef struct {
 /* A call looks only at the members that its product has.  Strides are at least the rows' widths, where there are several rows.
  * Tensors are aligned to their element types (16 bytes, with strides and widths to match, are faster).
  * Errors: DEAR_EINVAL, DEAR_EALIGN, DEAR_EHIP; DEAR_ETOOBIG where workspace_bytes is less than the call needs, or where a launch
- * would have 2^32 threads or more: 256 for every 128 x 128 outputs of an expert. */
+ * would have 2^32 threads or more: 256 for every 32 x 128 outputs of an expert, of a weight gradient for every 128 x 128. */
 int dear_expert_linear(const dear_experts_t *args, void *hip_stream);
 int dear_expert_input_grad(const dear_experts_t *args, void *hip_stream);
 int dear_expert_weight_grad(const dear_experts_t *args, void *hip_stream);
@@ -260,7 +260,7 @@ int dear_expert_weight_grad_workspace(const dear_experts_t *args, int64_t *bytes
  * The norm over the gradients of all tensors of a list, and the gradients scaled down to a largest norm:
  *     norm = sqrt(sum of g^2 over all elements of all tensors)
  *     out = g * min(1, max_norm / norm), rounded to out_dtype
- * Squares are added in 64 bits, norm is rounded to fp32 once.  A NaN or an infinity among the gradients makes the norm one;
+ * Squares are added in 64 bits (those of bf16 first by eights in fp32, where it holds them), norm is rounded to fp32 once.  A NaN or an infinity among the gradients makes the norm one;
  * with a norm of NaN every out is NaN, with an infinite one finite gradients become 0 and infinite ones NaN.
  */
 typedef struct {

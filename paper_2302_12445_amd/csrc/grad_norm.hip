@@ -84,7 +84,8 @@ __device__ __forceinline__ void add_squares(double &s, vec<float, 4> v) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) s = __builtin_fma((double)v[k], (double)v[k], s);
 }
-// Of eight bf16 values: their squares are exact in fp32, and are added there, as 64 bits would take longer than memory, unless fp32 does not hold what there is, or does not hold all of it.
+// Of eight bf16 values: their squares are exact in fp32, and are added there, as 64 bits would take longer than memory (seven roundings, less
+// than 2^-21 of the group's sum), unless fp32 does not hold what there is, or does not hold all of it.
 __device__ __forceinline__ void add_squares(double &s, vec<bf16, 8> v) {
     float t = 0.f;
 #pragma unroll
