@@ -177,3 +177,22 @@ def test_graph(ops, counts):
         want = ops.expert_linear(*fresh[:2], fresh[3]), ops.expert_input_grad(fresh[2], fresh[1], fresh[3]), ops.expert_weight_grad(fresh[2], fresh[0], fresh[3])
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+def test_refusals(ops):
+    """Wrong arguments raise before anything is enqueued."""
+    from paper_2302_12445_amd import DearError
+    x, w, dy, ends = make([3, 4], 1, 16, 24, F32, 81)
+    for call in (lambda: ops.expert_linear(x[:, :16], w, ends), lambda: ops.expert_linear(x, w[0], ends), lambda: ops.expert_linear(x, w, ends[:1]),
+                 lambda: ops.expert_linear(x, w, ends.long()), lambda: ops.expert_linear(x, w, ends.cpu()), lambda: ops.expert_linear(x, w.cpu(), ends),
+                 lambda: ops.expert_linear(x[None], w, ends), lambda: ops.expert_input_grad(dy[:, :8], w, ends),
+                 lambda: ops.expert_input_grad(dy, w, ends.view(1, 2)), lambda: ops.expert_weight_grad(dy[:4], x, ends),
+                 lambda: ops.expert_weight_grad(dy, x, ends.repeat(2)[::2])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: ops.expert_linear(x.half(), w.half(), ends), lambda: ops.expert_linear(x, w.bfloat16(), ends),
+                 lambda: ops.expert_weight_grad(dy, x.bfloat16(), ends)):
+        with pytest.raises((TypeError, ValueError)):
+            call()
+    with pytest.raises((DearError, ValueError)):
+        ops.expert_linear(x, w[:0], ends[:0])

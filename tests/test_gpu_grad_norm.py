@@ -169,3 +169,17 @@ def test_far_elements(ops):
     g[-1], g[n // 2], g[0] = 3.0, 4.0, 12.0
     assert ops.clip_grads([g], 6.5) == 13.0
     assert g[-1] == 1.5 and g[n // 2] == 2.0 and g[0] == 6.0 and g.count_nonzero() == 3
+
+
+def test_refusals(ops):
+    """Wrong arguments raise before anything is enqueued."""
+    t = normal(torch.Generator().manual_seed(9), (6, 4))
+    before = t.clone()
+    for call in (lambda: ops.clip_grads([t, t.cpu()], 1.0), lambda: ops.clip_grads([t], 1.0, [t.cpu()]), lambda: ops.clip_grads([t], 1.0, [t[:3]]),
+                 lambda: ops.clip_grads([t[:, ::2]], 1.0), lambda: ops.clip_grads([t[:1].expand(6, 4)], 1.0), lambda: ops.grad_norm([t, t.cpu()])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: ops.clip_grads([t.half()], 1.0), lambda: ops.clip_grads([t], 1.0, [t.double()]), lambda: ops.grad_norm([t, t.int()])):
+        with pytest.raises((TypeError, ValueError)):
+            call()
+    assert torch.equal(t, before)

@@ -286,3 +286,26 @@ def test_far_elements(ops):
     wide.copy_(x[:1])
     got = ops.recurrence(wide, gate[:1], state[:1])
     assert all(torch.equal(a, b[:1]) for a, b in zip(got, want))
+
+
+def test_refusals(ops):
+    """Wrong arguments raise before anything is enqueued."""
+    from paper_2302_12445_amd import DearError
+    x, gate, state = inputs((2, 5, 8), F32, 71)
+    _, _, kept = ops.recurrence(x, gate, state)
+    lens = torch.tensor([5, 2], dtype=torch.int32, device=DEV)
+    for call in (lambda: ops.recurrence(x, gate[:, :4]), lambda: ops.recurrence(x[0], gate[0]), lambda: ops.recurrence(x, gate.cpu()),
+                 lambda: ops.recurrence(x, gate, state.cpu()), lambda: ops.recurrence(x, gate, state[:1]), lambda: ops.recurrence(x, gate, state.bfloat16()),
+                 lambda: ops.recurrence(x, gate, state, lens.cpu()), lambda: ops.recurrence(x, gate, state, lens.long()),
+                 lambda: ops.recurrence(x, gate, state, lens[:1]), lambda: ops.recurrence(x[..., :0], gate[..., :0]),
+                 lambda: ops.recurrence_backward(x[:, :4], x, gate, kept), lambda: ops.recurrence_backward(x, x, gate, kept[:, :0]),
+                 lambda: ops.recurrence_backward(x, x, gate, kept, dlast=state[:, ::2])):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: ops.recurrence(x.half(), gate.half()), lambda: ops.recurrence(x, gate.bfloat16()),
+                 lambda: ops.recurrence_backward(x.bfloat16(), x, gate, kept)):
+        with pytest.raises((TypeError, ValueError)):
+            call()
+    wide = torch.zeros(1, 1, device=DEV).expand(2, 1 << 22)
+    with pytest.raises(DearError):
+        ops.recurrence(wide[None], wide[None])
