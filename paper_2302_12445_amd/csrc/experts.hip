@@ -114,42 +114,71 @@ constexpr int BB = 128;  // outputs' columns of a workgroup
 
 // An operand's part of a step on its way from memory to LDS, in pieces of 16 bytes: OUT rows of BS values along the summed index or, ACROSS
 // it, BS rows of OUT values.  Values beyond the sum are zeros in both operands, so that nothing that stands there counts; rows and columns
-// beyond the outputs are whatever is there, and not stored.
+// beyond the outputs are whatever is there, and not stored.  No load has a branch of its own, which would wait for the one before: pieces
+// beyond an end are read from before it, and pieces that begin before a row's end and end behind it are read as they are, up to the end of the
+// matrix; only steps that would pass that go value by value (bf16 333 rows, 1001 x 999 over 5, input gradient, 28 us with branches).
 template <typename T, bool VEC, bool ACROSS, int OUT, int BS> struct stage {
-    static constexpr int E = 16 / sizeof(T), N = OUT * BS / E / THREADS, W = ACROSS ? OUT : BS;
-    static_assert(N * E * THREADS == OUT * BS, "whole pieces for every thread");
+    static constexpr int E = 16 / sizeof(T), N = OUT * BS / E / THREADS, W = ACROSS ? OUT : BS, ROWS = THREADS * E / W;
+    static_assert(N * E * THREADS == OUT * BS && THREADS * E % W == 0, "whole pieces for every thread, in one column");
     typedef T vec __attribute__((ext_vector_type(16 / sizeof(T))));
     typedef vec vec_anywhere __attribute__((aligned(sizeof(T))));  // global memory takes 16-byte loads from any element on
     vec v[N];
+    const T *data;
+    int64_t at[N];      // this lane's pieces of the next step
+    int64_t furthest;   // the last piece of the tile's rows and columns, with the step's first of the summed index
+    int64_t stop;       // the matrix's end
+    int64_t stride;
+    int row, col;       // of the lane's first piece; the others are ROWS rows further on each
 
-    // rows: of the operand in memory; row0, col0: the step's first; row_end, col_end: behind the last that may be read
-    __device__ __forceinline__ void load(const T *data, int64_t stride, int64_t row0, int64_t row_end, int col0, int col_end) {
+    // Where the last of `n` values' piece begins; all pieces of a whole tile lie before its end.
+    static __device__ __forceinline__ int begin_of_last(int n, int whole) { return n >= whole ? whole - E : VEC ? (n - 1) / E * E : n - 1; }
+    // out0, outs: the tile's first output, and how many there are from it on, one at least; s0: the first of the summed index
+    __device__ __forceinline__ void aim(const T *data_, int64_t stride_, int64_t rows, int64_t width, int64_t out0, int64_t outs_left, int64_t s0) {
+        data = data_, stride = stride_, row = (int)threadIdx.x / (W / E), col = (int)threadIdx.x % (W / E) * E;
+        const int outs = (int)min(outs_left, (int64_t)OUT);
+        const int64_t first = ACROSS ? s0 * stride + out0 : out0 * stride + s0;
+        stop = (rows - 1) * stride + width;
+        furthest = ACROSS ? first + begin_of_last(outs, OUT) : first + (outs - 1) * stride;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = threadIdx.x + i * THREADS, col = col0 + c % (W / E) * E;
-            const int64_t row = row0 + c / (W / E);
-            const T *p = data + row * stride + col;
-#pragma unroll
-            for (int u = 0; u < E; ++u) v[i][u] = (T)0.f;
-            if (row < row_end) {
-                if (VEC) {
-                    if (col < col_end) v[i] = *(const vec *)p;
-                } else if (col + E <= col_end) {
-                    v[i] = *(const vec_anywhere *)p;
-                } else {
-#pragma unroll
-                    for (int u = 0; u < E - 1; ++u)
-                        if (col + u < col_end) v[i][u] = p[u];
-                }
-            }
-        }
+        for (int i = 0; i < N; ++i)
+            at[i] = ACROSS ? first + (row + i * ROWS) * stride + min(col, begin_of_last(outs, OUT)) : first + min(row + i * ROWS, outs - 1) * stride + col;
     }
-    __device__ __forceinline__ void store(DEAR_LDS T *s) const {
+    // left: of the summed index from the step's first on, one at least
+    __device__ __forceinline__ void load(int left) {
+        int64_t p[N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int c = threadIdx.x + i * THREADS;
-            *(DEAR_LDS vec *)(s + c / (W / E) * tile<T, W>::stride + c % (W / E) * E) = v[i];
+        for (int i = 0; i < N; ++i) p[i] = at[i];
+        if (left < BS) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                p[i] += ACROSS ? (min(row + i * ROWS, left - 1) - (row + i * ROWS)) * stride : (int64_t)(min(col, begin_of_last(left, BS)) - col);
         }
+        const int64_t end = furthest + (ACROSS ? (min(left, BS) - 1) * stride : (int64_t)begin_of_last(left, BS)) + E;
+        if (VEC) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = *(const vec *)(data + p[i]);
+        } else if (end <= stop) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = *(const vec_anywhere *)(data + p[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int u = 0; u < E; ++u) v[i][u] = data[min(p[i] + u, stop - 1)];
+        }
+        furthest += ACROSS ? BS * stride : BS;
+#pragma unroll
+        for (int i = 0; i < N; ++i) at[i] += ACROSS ? BS * stride : BS;
+    }
+    __device__ __forceinline__ void store(DEAR_LDS T *s, int left) {
+        if (left < BS)
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int u = 0; u < E; ++u)
+                    if ((ACROSS ? row + i * ROWS : col + u) >= left) v[i][u] = (T)0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) *(DEAR_LDS vec *)(s + (row + i * ROWS) * tile<T, W>::stride + col) = v[i];
     }
 };
 
@@ -190,19 +219,19 @@ template <typename T, bool VEC, int KIND, int BA> __global__ __launch_bounds__(T
     f32x16 acc[F][G] = {};
     stage_a sa;
     stage_b sb;
-    auto load = [&](int64_t s0) {
-        if (KIND == WEIGHT_GRAD) sa.load(a, p.a_stride, s0, end, a0, p.n_a);
-        else sa.load(a, p.a_stride, t.first, t.end, (int)s0, (int)end);
-        if (B_ACROSS) sb.load(b, p.b_stride, s0, end, b0, p.n_b);
-        else sb.load(b, p.b_stride, b0, p.n_b, (int)s0, (int)end);
-    };
-    if (begin < end) load(begin);
+    const int64_t out0 = KIND == WEIGHT_GRAD ? a0 : t.first, outs = (KIND == WEIGHT_GRAD ? p.n_a : t.end) - out0;
+    auto left = [&](int64_t s0) { return (int)min(end - s0, (int64_t)BS); };
+    if (begin < end) {
+        sa.aim(a, p.a_stride, p.rows, KIND == WEIGHT_GRAD ? p.n_a : p.sum, out0, outs, begin);
+        sb.aim(b, p.b_stride, KIND == LINEAR ? p.n_b : KIND == INPUT_GRAD ? p.sum : p.rows, KIND == LINEAR ? p.sum : p.n_b, b0, p.n_b - b0, begin);
+        sa.load(left(begin)), sb.load(left(begin));
+    }
     for (int64_t s0 = begin; s0 < end; s0 += BS) {
         __syncthreads();
-        sa.store(as);
-        sb.store(bs);
+        sa.store(as, left(s0));
+        sb.store(bs, left(s0));
         __syncthreads();
-        if (s0 + BS < end) load(s0 + BS);
+        if (s0 + BS < end) sa.load(left(s0 + BS)), sb.load(left(s0 + BS));
 #pragma unroll
         for (int s = 0; s < BS / 16; ++s) {
             frag<T> f[F], g[G];
