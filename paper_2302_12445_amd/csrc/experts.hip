@@ -30,7 +30,7 @@ struct params {
     int32_t n_a, n_b;    // outputs' rows (of a weight gradient; otherwise the tile's expert has them) and columns
     int32_t a_tiles, b_tiles;
     int32_t splits, chunk;  // of the summed index: sums of their own, and how much of it each has
-    float *parts;           // [splits, rows, columns], where there are several
+    float *parts;           // [splits, outputs], where there are several
 };
 
 // ------------------------------------------------------------------------------------ a tile's expert
@@ -206,13 +206,15 @@ template <typename T, bool VEC, int KIND, int BA> __global__ __launch_bounds__(T
     __shared__ __attribute__((aligned(16))) char lds[BYTES_A + BYTES_B];
     DEAR_LDS T *as = (DEAR_LDS T *)lds, *bs = (DEAR_LDS T *)(lds + BYTES_A);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const unsigned per = (unsigned)p.a_tiles * p.b_tiles, id = blockIdx.x % per, which = blockIdx.x / per;  // expert, or split
-    const part t = KIND == WEIGHT_GRAD ? rows_of(p, (int)which) : find<BA>(p, (int)(id / p.b_tiles));
+    const unsigned per = (unsigned)p.a_tiles * p.b_tiles, id = blockIdx.x % per, block = blockIdx.x / per;
+    const unsigned which = KIND == WEIGHT_GRAD ? block / (unsigned)p.experts : block;  // split
+    const part t = KIND == WEIGHT_GRAD ? rows_of(p, (int)(block - which * (unsigned)p.experts)) : find<BA>(p, (int)(id / p.b_tiles));
     if (t.none) return;
     const int b0 = (int)(id % p.b_tiles) * BB, a0 = KIND == WEIGHT_GRAD ? (int)(id / p.b_tiles) * BA : 0;
     const bool behind = KIND != WEIGHT_GRAD && t.expert == p.experts;  // rows of no expert
-    const int64_t begin = KIND == WEIGHT_GRAD ? t.begin : (int64_t)which * p.chunk;
-    const int64_t end = behind ? 0 : KIND == WEIGHT_GRAD ? t.end : min(begin + p.chunk, (int64_t)p.sum);
+    const int64_t chunk = KIND == WEIGHT_GRAD ? ((t.end - t.begin + p.splits - 1) / p.splits + BS - 1) / BS * BS : p.chunk;
+    const int64_t begin = (KIND == WEIGHT_GRAD ? t.begin : 0) + which * chunk;
+    const int64_t end = behind ? 0 : min(begin + chunk, KIND == WEIGHT_GRAD ? t.end : (int64_t)p.sum);
     const T *a = (const T *)p.a, *b = (const T *)p.b;
     if (KIND == LINEAR) b += (int64_t)t.expert * p.n_b * p.sum;
     if (KIND == INPUT_GRAD) b += (int64_t)t.expert * p.sum * p.n_b;
@@ -267,8 +269,9 @@ template <typename T, bool VEC, int KIND, int BA> __global__ __launch_bounds__(T
                 }
             }
     };
-    if (KIND != WEIGHT_GRAD && p.splits > 1) store(p.parts + (int64_t)which * p.rows * p.n_b);
-    else store((O *)p.out + (KIND == WEIGHT_GRAD ? (int64_t)t.expert * p.n_a * p.n_b : 0));
+    const int64_t first = KIND == WEIGHT_GRAD ? (int64_t)t.expert * p.n_a * p.n_b : 0;
+    if (p.splits > 1) store(p.parts + which * (KIND == WEIGHT_GRAD ? p.experts * (int64_t)p.n_a : p.rows) * p.n_b + first);
+    else store((O *)p.out + first);
 }
 
 // Sum of the splits, in their order, eight loads in flight, rounded once.
@@ -1005,13 +1008,43 @@ choice choose(const dear_experts_t &x, bool is_direct, int64_t sum, int64_t colu
     return best;
 }
 
+// Of a weight gradient, by a like estimate, with the rows shared out evenly: tiles of 256 where an expert has more than a few steps, or of 128
+// in splits of each expert's rows.  Measured, microseconds, tiles of 256, and of 128 in one, four and sixteen splits: 16384 rows, 4096 x 1024 over
+// 8 123, 208, 405 and 1074, 1024 x 1024 over 8 50, 53, 99 and 275; 30000 rows, 1024 x 1024 over 2 146, 255, 102 and 132; 16000 rows, 512 x 512
+// of one 140, 269, 73 and 30, 100 x 100 over 4 -, 81, 26 and 13; 500 rows, 4096 x 1024 over 8 33 and 28; fp32 16384 rows, 128 x 64 over 8 -, 157,
+// 45 and 18.
+choice choose_weight_grad(const dear_experts_t &x, bool is_direct) {
+    const bool f32 = x.dtype == DEAR_F32;
+    const int64_t rows = ceil_div(x.rows, x.experts);
+    const double steps = (double)ceil_div(rows, WS), outputs = (double)x.experts * x.outs * x.ins, written = outputs * 4 / 4e6;
+    auto tiles = [&](int n) { return (double)x.experts * (double)(ceil_div(x.outs, n) * ceil_div(x.ins, n)); };
+    choice best = {ANY128, 1, 0};
+    for (int64_t n = 1; n <= 32 && (n == 1 || (n * 2 * WS <= rows && tiles(128) * n * THREADS <= MAX_THREADS && outputs <= MAX_THREADS)); ++n) {
+        const double a_cu = std::ceil(tiles(128) * n / CUS), each = std::ceil(steps / n), resident = f32 ? 2 : 3;
+        const double wait = std::ceil(a_cu / resident) * (3 + each * (f32 ? 4.6 : 1.3)), work = a_cu * each * (f32 ? 3.6 : 0.7);
+        const double us = (wait > work ? wait : work) + (n == 1 ? written : 3 + (2 * n + 1) * written);
+        if (n == 1 || us < best.us) best = {ANY128, (int)n, us};
+    }
+    if (is_direct && rows >= 2 * WS) {
+        const double rounds = std::floor(tiles(256) / CUS), over = tiles(256) - rounds * CUS;
+        const double us = 3 + steps * 1.5 * (rounds + (over > CUS / 2 ? 1 : 0.45 * std::ceil(4 * over / CUS))) + written / 2;
+        if (us <= best.us) best = {WIDE, 1, us};
+    }
+    return best;
+}
+
+template <int KIND> choice choose_cut(const dear_experts_t &x, bool is_direct) {
+    if (KIND == WEIGHT_GRAD) return choose_weight_grad(x, is_direct);
+    return KIND == LINEAR ? choose(x, is_direct, x.ins, x.outs) : choose(x, is_direct, x.outs, x.ins);
+}
+
 template <int KIND> int64_t workspace_of(const dear_experts_t &x) {
-    if (KIND == WEIGHT_GRAD || x.rows == 0) return 0;
+    if (x.rows == 0) return 0;
     // what a call takes depends on its pointers
-    const int64_t sum = KIND == LINEAR ? x.ins : x.outs, columns = KIND == LINEAR ? x.outs : x.ins;
-    const int any = choose(x, false, sum, columns).splits, direct = x.dtype == DEAR_BF16 ? choose(x, true, sum, columns).splits : 1;
-    const int most = any > direct ? any : direct;
-    return most > 1 ? most * x.rows * columns * 4 : 0;
+    const int any = choose_cut<KIND>(x, false).splits, direct = x.dtype == DEAR_BF16 ? choose_cut<KIND>(x, true).splits : 1;
+    const int64_t most = any > direct ? any : direct;
+    const int64_t outputs = KIND == WEIGHT_GRAD ? (int64_t)x.experts * x.outs * x.ins : x.rows * (KIND == LINEAR ? x.outs : x.ins);
+    return most > 1 ? most * outputs * 4 : 0;
 }
 
 template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
@@ -1044,9 +1077,9 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
         vec = vectors(*x, p.a, p.a_stride, x->outs) && vectors(*x, p.b, p.b_stride, x->ins);
     }
     const bool is_direct = direct<KIND>(*x, vec, p);
-    const choice c = KIND != WEIGHT_GRAD ? choose(*x, is_direct, p.sum, p.n_b) : choice{is_direct && x->rows / x->experts >= 128 ? WIDE : ANY128, 1, 0};
+    const choice c = choose_cut<KIND>(*x, is_direct);
     p.chunk = (int32_t)(ceil_div(ceil_div(p.sum, c.splits), WS) * WS);
-    p.splits = KIND == WEIGHT_GRAD ? 1 : (int32_t)ceil_div(p.sum, p.chunk), p.parts = (float *)x->workspace;
+    p.splits = KIND == WEIGHT_GRAD ? c.splits : (int32_t)ceil_div(p.sum, p.chunk), p.parts = (float *)x->workspace;
     if (c.how == WIDE) {
         p.a_tiles = (int32_t)ceil_div(p.n_a, 256), p.b_tiles = (int32_t)ceil_div(p.n_b, 256);
         experts_wide_kernel<KIND><<<CUS, THREADS, 0, stream>>>(p);
@@ -1056,7 +1089,7 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
     // tiles of rows: each expert, and the rows behind the last, may have one that is not whole
     const int ba = c.how == FEW32 || c.how == DEEP32 || c.how == ANY32 ? 32 : c.how == ANY64 ? 64 : 128;
     p.a_tiles = (int32_t)(KIND == WEIGHT_GRAD ? ceil_div(x->outs, ba) : x->rows / ba + x->experts + 1);
-    const int64_t groups = (int64_t)p.a_tiles * p.b_tiles * (KIND == WEIGHT_GRAD ? x->experts : p.splits);
+    const int64_t groups = (int64_t)p.a_tiles * p.b_tiles * p.splits * (KIND == WEIGHT_GRAD ? x->experts : 1);
     if (groups * THREADS > MAX_THREADS) return DEAR_ETOOBIG;
     if constexpr (KIND != WEIGHT_GRAD) {
         if (is_direct) {
@@ -1097,9 +1130,9 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
     }
     if (int rc = launch_status()) return rc;
     if (p.splits > 1) {
-        const int64_t all = p.rows * p.n_b;
+        const int64_t all = (KIND == WEIGHT_GRAD ? (int64_t)p.experts * p.n_a : p.rows) * p.n_b;
         const unsigned blocks = (unsigned)ceil_div(all, 256);
-        if (x->dtype == DEAR_BF16) parts_sum_kernel<<<blocks, 256, 0, stream>>>(p.parts, p.splits, all, (bf16 *)p.out);
+        if (x->dtype == DEAR_BF16 && KIND != WEIGHT_GRAD) parts_sum_kernel<<<blocks, 256, 0, stream>>>(p.parts, p.splits, all, (bf16 *)p.out);
         else parts_sum_kernel<<<blocks, 256, 0, stream>>>(p.parts, p.splits, all, (float *)p.out);
         return launch_status();
     }

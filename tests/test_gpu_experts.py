@@ -117,6 +117,13 @@ def test_long_sums_and_many_tiles(ops, sizes):
     check(ops, *make(counts, 0, outs, ins, BF16, 13))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("outs, ins", [(40, 24), (37, 51), (128, 264)])
+def test_many_rows_of_few_outputs(ops, outs, ins, dtype):
+    """Weight gradients whose rows go to several workgroups; of one expert fewer rows than there are of them."""
+    check(ops, *make([3000, 0, 905, 2, 64], 7, outs, ins, dtype, 44))
+
+
 @pytest.mark.parametrize("outs, ins", [(136, 1000), (1000, 136)])
 def test_few_tiles_behind_a_round(ops, outs, ins):
     """66 x 4 tiles of 256: one for each of 256 units, and eight."""
