@@ -449,13 +449,12 @@ template <int KIND, int SA, int SB, bool PARTS, typename NEXT>
 __device__ __forceinline__ void run(const params &p, void *outputs, DEAR_LDS char *xa, DEAR_LDS char *ya, DEAR_LDS char *xb, DEAR_LDS char *yb,
                                     DEAR_LDS char *lines, NEXT next) {
     constexpr bool A_ACROSS = KIND == WEIGHT_GRAD, B_ACROSS = KIND != LINEAR;
-    constexpr int WAYS_A = SA == 32 ? 1 : 2, WAYS_B = 4 / WAYS_A;
-    typedef side<A_ACROSS, SA, WAYS_A> side_a;
-    typedef side<B_ACROSS, SB, WAYS_B> side_b;
+    typedef side<A_ACROSS, SA, 2> side_a;
+    typedef side<B_ACROSS, SB, 2> side_b;
     constexpr int F = side_a::F, G = side_b::F;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    side_a a(wave / WAYS_B, lane, wave);
-    side_b b(wave % WAYS_B, lane, wave);
+    side_a a(wave / 2, lane, wave);
+    side_b b(wave % 2, lane, wave);
     const uint32_t a_stride = (uint32_t)p.a_stride * 2, b_stride = (uint32_t)p.b_stride * 2;
     const char *from_a = nullptr, *from_b = nullptr;
     int64_t left = 0;  // of the summed index, from the step that is loaded next on
@@ -731,10 +730,18 @@ template <bool PARTS> __device__ __forceinline__ void few_rest(const experts_tab
         zero_rows(p, PARTS ? (O *)p.parts + (int64_t)s * p.rows * p.n_b : (O *)p.out, uniform(table.ends[p.experts - 1]), p.rows);
 }
 
-// The tiles of SA x 128 outputs that next() gives, with D - 1 steps under way.  x, y: the operands' places for D steps in turn; the first of y
-// holds 16 KB.
+// Waits for what is read or loaded, but for the last n times EACH loads, n <= MOST.
+template <int MOST, int EACH> __device__ __forceinline__ void wait_for_all_but(int n) {
+    if constexpr (MOST > 0)
+        if (n < MOST) return wait_for_all_but<MOST - 1, EACH>(n);
+    __builtin_amdgcn_s_waitcnt(0x0070 | (MOST * EACH & 15) | (MOST * EACH >> 4) << 14);
+}
+
+// The tiles of SA x 128 outputs that next() gives, with D - 1 steps under way.  A wave waits for its own loads by the count of those behind
+// them, and the barrier is bare: __syncthreads() waits for all loads.  x, y: the operands' places for D steps in turn; the first of y holds
+// 16 KB.
 template <int KIND, int SA, bool PARTS, int D, typename NEXT>
-__device__ __forceinline__ void run_deep(const params &p, void *outputs, DEAR_LDS char *const (&x)[D], DEAR_LDS char *const (&y)[D], NEXT next) {
+__device__ __forceinline__ void run_ring(const params &p, void *outputs, DEAR_LDS char *const (&x)[D], DEAR_LDS char *const (&y)[D], NEXT next) {
     constexpr bool B_ACROSS = KIND == INPUT_GRAD;
     constexpr int SB = 128, WAYS_A = SA == 32 ? 1 : 2, WAYS_B = 4 / WAYS_A;
     typedef side<false, SA, WAYS_A> side_a;
@@ -763,11 +770,7 @@ __device__ __forceinline__ void run_deep(const params &p, void *outputs, DEAR_LD
         f32x16 acc[F][G] = {};
         struct {
             bf16x8 a[F], b[G];
-        } f, g;
-#pragma unroll
-        for (int u = 0; u < F; ++u) g.a[u] = bf16x8{};
-#pragma unroll
-        for (int u = 0; u < G; ++u) g.b[u] = bf16x8{};
+        } q[4];
         auto read = [&](auto &q, const DEAR_LDS char *s, const DEAR_LDS char *r, int kk) {
 #pragma unroll
             for (int u = 0; u < F; ++u) q.a[u] = a.read(s, u, kk);
@@ -786,9 +789,7 @@ __device__ __forceinline__ void run_deep(const params &p, void *outputs, DEAR_LD
                 const int step = base + k;
                 if (step < steps) {
                     // this step is there, of all waves, and all have read the one that is loaded over: its own loads by the count of those behind them
-                    constexpr int behind = (D - 2) * (side_a::LOADS + side_b::LOADS);
-                    if (step + D - 2 < steps) __builtin_amdgcn_s_waitcnt(0x0070 | (behind & 15) | (behind >> 4) << 14);
-                    else __builtin_amdgcn_s_waitcnt(0x0070);
+                    wait_for_all_but<D - 2, side_a::LOADS + side_b::LOADS>(steps - 1 - step);
                     if (step == steps - 1 && last < WS) {
                         a.clear(x[k], last), b.clear(y[k], last);
                         __builtin_amdgcn_s_waitcnt(0xc07f);
@@ -796,19 +797,16 @@ __device__ __forceinline__ void run_deep(const params &p, void *outputs, DEAR_LD
                     asm volatile("" ::: "memory");
                     __builtin_amdgcn_s_barrier();
                     asm volatile("" ::: "memory");
+                    // all of the step's reads before its products
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) read(q[kk], x[k], y[k], kk);
+                    __builtin_amdgcn_sched_barrier(0);
                     if (step + D - 1 < steps) load(step + D - 1, x[(k + D - 1) % D], y[(k + D - 1) % D]);
-                    read(f, x[k], y[k], 0);
-                    multiply(g);
-                    read(g, x[k], y[k], 1);
-                    multiply(f);
-                    read(f, x[k], y[k], 2);
-                    multiply(g);
-                    read(g, x[k], y[k], 3);
-                    multiply(f);
+#pragma unroll
+                    for (int kk = 0; kk < 4; ++kk) multiply(q[kk]);
                 }
             }
         }
-        multiply(g);
         __syncthreads();
         store_tile<KIND, SA, SB, PARTS>(p, outputs, t, acc, y[0], lane, wave);
     }
@@ -851,7 +849,7 @@ template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_k
             constexpr int A = 32 * WS * 2;
             DEAR_LDS char *const x[4] = {xa, xb, ya, yb}, *const y[4] = {xa + A, xb + A, ya + A, yb + A};
             unsigned item = blockIdx.x;
-            run_deep<KIND, 32, false, 4>(p, p.out, x, y, [&] {
+            run_ring<KIND, 32, false, 4>(p, p.out, x, y, [&] {
                 wide_tile t;
                 for (;;) {
                     t.none = item >= 16 * over;
@@ -882,41 +880,31 @@ template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_k
     });
 }
 
-// Tiles of SA x 128, of 32 rows or of 128, for fewer rows: two workgroups a CU (of 32 rows three), and sums in several splits (PARTS) where there are
-// few tiles.  Weights are read once if an expert's rows are one tile, and bound it.
-template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, 2) void experts_few_kernel(params p) {
-    __shared__ __attribute__((aligned(16))) char a0[SA * WS * 2], a1[SA * WS * 2], b0[128 * WS * 2], b1[128 * WS * 2];
+// Tiles of 128 x 128 for fewer rows, two workgroups a CU, and sums in several splits (PARTS) where there are few tiles.
+template <int KIND, bool PARTS> __global__ __launch_bounds__(THREADS, 2) void experts_few_kernel(params p) {
+    __shared__ __attribute__((aligned(16))) char a0[128 * WS * 2], a1[128 * WS * 2], b0[128 * WS * 2], b1[128 * WS * 2];
     __shared__ experts_table table;
-    fill<KIND, SA>(table, p);
+    fill<KIND, 128>(table, p);
     few_rest<PARTS>(table, p);
     unsigned item = blockIdx.x;
-    run<KIND, SA, 128, PARTS>(p, PARTS ? (void *)p.parts : p.out, (DEAR_LDS char *)a0, (DEAR_LDS char *)b0, (DEAR_LDS char *)a1, (DEAR_LDS char *)b1,
-                              nullptr, [&] { return few_tile<KIND, SA, PARTS>(table, p, item); });
+    run<KIND, 128, 128, PARTS>(p, PARTS ? (void *)p.parts : p.out, (DEAR_LDS char *)a0, (DEAR_LDS char *)b0, (DEAR_LDS char *)a1, (DEAR_LDS char *)b1,
+                               nullptr, [&] { return few_tile<KIND, 128, PARTS>(table, p, item); });
 }
 
-// The same tiles where there is no more than one a CU: what it waits for is the weights' way from memory, and D - 1 steps are under way at a
-// time, 100 KB of a CU (32 rows, 4096 x 1024 over 8 15.6 us, 4.3 TB/s; with one step and three workgroups a CU 18.2).  A wave waits for its own
-// loads by the count of those behind them, and the barrier is bare: __syncthreads() waits for all loads, and makes it 18.1.
-template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, 1) void experts_deep_kernel(params p) {
-    constexpr int D = SA == 32 ? 6 : 4, A = SA * WS * 2, B = 128 * WS * 2;
+// The same tiles, of 32 rows two a CU or of 128 one, with two steps under way where the third is multiplied: what they wait for is the weights'
+// way from memory (32 rows, 4096 x 1024 over 8 14.8 us, 4.5 TB/s from HBM; 12.6 where the last cache holds them).  With one step under way
+// 18.2 and 13.4 us, with five 15.3 and 14.4, with two pairs of steps 15.1 and 14.1.
+template <int KIND, int SA, bool PARTS> __global__ __launch_bounds__(THREADS, SA == 32 ? 2 : 1) void experts_ring_kernel(params p) {
+    constexpr int A = SA * WS * 2, B = 128 * WS * 2;
     // in arrays of their own: a read from one need not wait for what memory brings to another
-    __shared__ __attribute__((aligned(16))) char a0[A], a1[A], a2[A], a3[A], a4[D > 4 ? A : 16], a5[D > 4 ? A : 16];
-    __shared__ __attribute__((aligned(16))) char b0[B], b1[B], b2[B], b3[B], b4[D > 4 ? B : 16], b5[D > 4 ? B : 16];
+    __shared__ __attribute__((aligned(16))) char a0[A], a1[A], a2[A], b0[B], b1[B], b2[B];
     __shared__ experts_table table;
     fill<KIND, SA>(table, p);
-    unsigned item = blockIdx.x;
-    auto next = [&] { return few_tile<KIND, SA, PARTS>(table, p, item); };
     few_rest<PARTS>(table, p);
-    void *const outputs = PARTS ? (void *)p.parts : p.out;
-    if constexpr (D == 6) {
-        DEAR_LDS char *const x[D] = {(DEAR_LDS char *)a0, (DEAR_LDS char *)a1, (DEAR_LDS char *)a2, (DEAR_LDS char *)a3, (DEAR_LDS char *)a4, (DEAR_LDS char *)a5};
-        DEAR_LDS char *const y[D] = {(DEAR_LDS char *)b0, (DEAR_LDS char *)b1, (DEAR_LDS char *)b2, (DEAR_LDS char *)b3, (DEAR_LDS char *)b4, (DEAR_LDS char *)b5};
-        run_deep<KIND, SA, PARTS, D>(p, outputs, x, y, next);
-    } else {
-        DEAR_LDS char *const x[D] = {(DEAR_LDS char *)a0, (DEAR_LDS char *)a1, (DEAR_LDS char *)a2, (DEAR_LDS char *)a3};
-        DEAR_LDS char *const y[D] = {(DEAR_LDS char *)b0, (DEAR_LDS char *)b1, (DEAR_LDS char *)b2, (DEAR_LDS char *)b3};
-        run_deep<KIND, SA, PARTS, D>(p, outputs, x, y, next);
-    }
+    unsigned item = blockIdx.x;
+    DEAR_LDS char *const x[3] = {(DEAR_LDS char *)a0, (DEAR_LDS char *)a1, (DEAR_LDS char *)a2};
+    DEAR_LDS char *const y[3] = {(DEAR_LDS char *)b0, (DEAR_LDS char *)b1, (DEAR_LDS char *)b2};
+    run_ring<KIND, SA, PARTS, 3>(p, PARTS ? (void *)p.parts : p.out, x, y, [&] { return few_tile<KIND, SA, PARTS>(table, p, item); });
 }
 
 // ------------------------------------------------------------------------------------ host
@@ -942,9 +930,10 @@ bool vectors(const dear_experts_t &x, const void *p, int64_t stride, int64_t wid
     return aligned(p, 16) && stride * n % 16 == 0 && width * n % 16 == 0;
 }
 
-// How a call's outputs are cut: tiles of 256 (WIDE), tiles of 32 or 128 rows that memory fills directly (FEW32, FEW128, or one a CU with more steps
-// under way, DEEP32, DEEP128), or tiles whose operands go through registers (ANY32, ANY64, ANY128); and the splits of the summed index.
-enum cut { WIDE, FEW32, FEW128, DEEP32, DEEP128, ANY32, ANY64, ANY128 };
+// How a call's outputs are cut: tiles of 256 (WIDE), tiles of 32 or 128 rows that memory fills directly, with two steps under way (RING32, RING128) or
+// with one and two workgroups a CU (FEW128), or tiles whose operands go through registers (ANY32, ANY64, ANY128); and the splits of the
+// summed index.
+enum cut { WIDE, RING32, RING128, FEW128, ANY32, ANY64, ANY128 };
 struct choice {
     cut how;
     int splits;
@@ -966,44 +955,43 @@ double row_tiles(const dear_experts_t &x, int n) {
 }
 
 // The cut and splits of the least time by this estimate, in microseconds.  A CU takes `resident` workgroups at a time; a step of 64 of the summed
-// index takes each `alone` as long as loads are what it waits for, and a `share` of the CU when there are more; all weights take their way
-// from memory, a part of which tiles of 256 and those that begin and end at other times leave unused.  Several splits' sums are written, read
-// and added, 4 TB/s, in another launch.  Tiles of 256 fill the chip once each and are not split; their last round goes in quarters where it is
-// no more than half full.  Measured, microseconds, over 8 experts, 4096 x 1024, tiles of 256, and of 32 rows and of 128 several a CU and one a CU:
-// 32 rows 34, 18, 20, 16 and 16, 1024 rows 37, 36, 25, 38 and 21, 4096 rows 36, 95, 50, 117 and 55; over 64, 1024 x 1024, 512 rows 39, 31, -, 32
-// and 34.  The input gradient's in their best splits: 32 rows 55, 19, 20, 20 and 21, 1024 rows 60, 52, 32, 40 and 30, 4096 rows 64, 113, 65, 108
-// and 54.
+// index takes each `alone` as long as loads are what it waits for, and a `share` of the CU, or of what the caches give it, when there are more;
+// all weights take their way from memory, a part of which tiles of 256 and those that begin and end at other times leave unused.  Several
+// splits' sums are written, read, eight at a time, and added, 4 TB/s, in another launch.  Tiles of 256 fill the chip once each and are not
+// split; their last round goes in smaller ones where it is no more than half full.  Measured, microseconds, over 8 experts, 4096 x 1024, tiles
+// of 256, and RING32, RING128 and FEW128: 32 rows 34, 15, 16 and 20, 1024 rows 37, 32, 21 and 25, 2048 rows -, 53, 32 and 39, 4096 rows 36,
+// 95, 55 and 50; over 64, 1024 x 1024, 4096 rows 41, 53, 37 and 33.  The input gradient's in one split and four: 32 rows RING32 33 and 19,
+// RING128 41 and 20, 1024 rows 40 and 47, 45 and 29, 4096 rows in one, tiles of 256 64 and RING128 54.
 choice choose(const dear_experts_t &x, bool is_direct, int64_t sum, int64_t columns) {
     const double steps = (double)ceil_div(sum, WS), size = x.dtype == DEAR_F32 ? 4 : 2;
     const double weights = (double)(x.experts < x.rows ? x.experts : x.rows) * (double)sum * (double)columns * size / 5.8e6;
     choice best = {ANY128, 1, 0};
-    auto take = [&](cut how, int n, double us, bool deep = false) {
-        const double least = weights * (deep ? 1 : how == WIDE ? 1.5 : 1.2);
+    auto take = [&](cut how, int n, double us, bool at_once) {
+        const double least = weights * (how == WIDE ? 1.5 : at_once && how <= RING128 ? 1 : 1.2);
         us = us > least ? us : least;
-        us += 4 + (n == 1 ? 0 : 3 + (double)(n + 1) * (double)x.rows * (double)columns * 4 / 4e6);
+        us += 4 + (n == 1 ? 0 : 1.5 + 1.5 * (double)ceil_div(n, 8) + (double)(n + 1) * (double)x.rows * (double)columns * 4 / 4e6);
         if (best.us == 0 || us < best.us) best = {how, n, us};
     };
-    auto splits = [&](cut how, int ba, double resident, double alone, double share) {
+    auto splits = [&](cut how, int ba, double resident, double begin, double alone, double share) {
         const double tiles = row_tiles(x, ba) * (double)ceil_div(columns, BB);
         const int64_t upper = (x.rows / ba + x.experts + 1) * ceil_div(columns, BB);
         for (int64_t n = 1; n <= 32 && (n == 1 || (n * 2 * WS <= sum && upper * n * THREADS <= MAX_THREADS && x.rows * columns <= MAX_THREADS)); ++n) {
             const double a_cu = std::ceil(tiles * n / CUS), each = std::ceil(steps / n);
-            const double wait = std::ceil(a_cu / resident) * (3 + each * alone), work = a_cu * each * share;
-            take(how, (int)n, wait > work ? wait : work, (how == DEEP32 || how == DEEP128) && a_cu <= 1);
+            const double wait = std::ceil(a_cu / resident) * (begin + each * alone), work = a_cu * each * share;
+            take(how, (int)n, wait > work ? wait : work, a_cu <= 1);
         }
     };
     const bool f32 = x.dtype == DEAR_F32;
     if (is_direct) {
+        splits(RING32, 32, 2, 1, 0.45, 0.42);
+        splits(FEW128, 128, 2, 3, 0.85, 0.6);
+        splits(RING128, 128, 1, 1, 0.7, 0.7);
         const double tiles = std::ceil(row_tiles(x, 256)) * (double)ceil_div(columns, 256), rounds = std::floor(tiles / CUS), over = tiles - rounds * CUS;
-        take(WIDE, 1, 3 + steps * 1.5 * (rounds + (over > CUS / 2 ? 1 : over > CUS / 16 ? 0.5 * std::ceil(4 * over / CUS) : over > 0 ? 0.3 : 0)));
-        splits(FEW32, 32, 3, 0.75, 0.35);
-        splits(FEW128, 128, 2, 0.85, 0.6);
-        splits(DEEP32, 32, 1, 0.35, 0.35);
-        splits(DEEP128, 128, 1, 0.55, 0.55);
+        take(WIDE, 1, 3 + steps * 1.5 * (rounds + (over > CUS / 2 ? 1 : over > CUS / 16 ? 0.5 * std::ceil(4 * over / CUS) : over > 0 ? 0.3 : 0)), false);
     } else {
-        splits(ANY32, 32, f32 ? 3 : 6, f32 ? 2.6 : 1.4, f32 ? 1.2 : 0.7);
-        splits(ANY64, 64, f32 ? 4 : 5, f32 ? 3.2 : 1.4, f32 ? 2.0 : 0.7);
-        splits(ANY128, 128, 3, f32 ? 4.6 : 1.4, f32 ? 3.6 : 0.7);
+        splits(ANY32, 32, f32 ? 3 : 6, 3, f32 ? 2.6 : 1.4, f32 ? 1.2 : 0.7);
+        splits(ANY64, 64, f32 ? 4 : 5, 3, f32 ? 3.2 : 1.4, f32 ? 2.0 : 0.7);
+        splits(ANY128, 128, 3, 3, f32 ? 4.6 : 1.4, f32 ? 3.6 : 0.7);
     }
     return best;
 }
@@ -1087,26 +1075,22 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
     }
     p.b_tiles = (int32_t)ceil_div(p.n_b, BB);
     // tiles of rows: each expert, and the rows behind the last, may have one that is not whole
-    const int ba = c.how == FEW32 || c.how == DEEP32 || c.how == ANY32 ? 32 : c.how == ANY64 ? 64 : 128;
+    const int ba = c.how == RING32 || c.how == ANY32 ? 32 : c.how == ANY64 ? 64 : 128;
     p.a_tiles = (int32_t)(KIND == WEIGHT_GRAD ? ceil_div(x->outs, ba) : x->rows / ba + x->experts + 1);
     const int64_t groups = (int64_t)p.a_tiles * p.b_tiles * p.splits * (KIND == WEIGHT_GRAD ? x->experts : 1);
     if (groups * THREADS > MAX_THREADS) return DEAR_ETOOBIG;
     if constexpr (KIND != WEIGHT_GRAD) {
         if (is_direct) {
-            auto of = [&](auto rows, auto parts) {
-                constexpr int SA = decltype(rows)::value;
+            const int64_t most = c.how == RING128 ? CUS : 2 * CUS;
+            const unsigned n = (unsigned)(groups < most ? groups : most);
+            auto by_parts = [&](auto parts) {
                 constexpr bool PARTS = decltype(parts)::value;
-                const int64_t most = c.how == DEEP32 || c.how == DEEP128 ? CUS : SA == 32 ? 3 * CUS : 2 * CUS;
-                const unsigned n = (unsigned)(groups < most ? groups : most);
-                if (c.how == DEEP32 || c.how == DEEP128) experts_deep_kernel<KIND, SA, PARTS><<<n, THREADS, 0, stream>>>(p);
-                else experts_few_kernel<KIND, SA, PARTS><<<n, THREADS, 0, stream>>>(p);
+                if (c.how == RING32) experts_ring_kernel<KIND, 32, PARTS><<<n, THREADS, 0, stream>>>(p);
+                else if (c.how == RING128) experts_ring_kernel<KIND, 128, PARTS><<<n, THREADS, 0, stream>>>(p);
+                else experts_few_kernel<KIND, PARTS><<<n, THREADS, 0, stream>>>(p);
             };
-            auto by_parts = [&](auto rows) {
-                if (p.splits > 1) of(rows, std::true_type());
-                else of(rows, std::false_type());
-            };
-            if (ba == 32) by_parts(std::integral_constant<int, 32>());
-            else by_parts(std::integral_constant<int, 128>());
+            if (p.splits > 1) by_parts(std::true_type());
+            else by_parts(std::false_type());
         }
     }
     const unsigned n = (unsigned)groups;
