@@ -5,7 +5,8 @@ is its thin ctypes binding.  Importing the package does not load the library; th
 call does, and raises if the library has not been built.
 
 ops.py and layers.py are the training operators of libdear_ops.so (include/dear_ops.h): attention, RMS
-norm and 8-bit checkpoints for the transformer blocks whose gradients are aggregated.
+norm and 8-bit checkpoints for the transformer blocks whose gradients are aggregated, a gated linear
+recurrence and products by expert for recurrent ones, and the clipping of what is aggregated.
 """
 from .binding import (  # noqa: F401
     DEAR_BF16, DEAR_F32, DEAR_NO_LIMIT, DEAR_SHARD_ALIGN, Context, DearError, Plan,
