@@ -194,11 +194,10 @@ template <int W> __device__ __forceinline__ f32x8 along(const DEAR_LDS float *s,
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// BA x 128 outputs a workgroup: four waves of 64 x 64, of 32 x 64 or, of 32 rows, of 32 x 32.  A step's operands go through registers to LDS,
-// the next one's loads beside its products.
-template <typename T, bool VEC, int KIND, int BA> __global__ __launch_bounds__(THREADS, 2) void experts_kernel(params p) {
+// BA x 128 outputs a workgroup: four waves of 64 x 64, of 32 x 64 or, of 32 rows, of 32 x 32.  A step's operands, BS of the summed index, go
+// through registers to LDS, the next one's loads beside its products.
+template <typename T, bool VEC, int KIND, int BA, int BS> __global__ __launch_bounds__(THREADS, 2) void experts_kernel(params p) {
     constexpr bool A_ACROSS = KIND == WEIGHT_GRAD, B_ACROSS = KIND != LINEAR;
-    constexpr int BS = BA == 32 ? 64 : 32;  // of the summed index a step
     constexpr int WAVES_A = BA == 32 ? 1 : 2, WAVES_B = 4 / WAVES_A, F = BA / WAVES_A / 32, G = BB / WAVES_B / 32;
     typedef stage<T, VEC, A_ACROSS, BA, BS> stage_a;
     typedef stage<T, VEC, B_ACROSS, BB, BS> stage_b;
@@ -1098,10 +1097,14 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
         typedef decltype(t) T;
         constexpr bool VEC = decltype(v)::value;
         if constexpr (KIND != WEIGHT_GRAD) {
-            if (ba == 32) return experts_kernel<T, VEC, KIND, 32><<<n, THREADS, 0, stream>>>(p);
-            if (ba == 64) return experts_kernel<T, VEC, KIND, 64><<<n, THREADS, 0, stream>>>(p);
+            if (ba == 32) return experts_kernel<T, VEC, KIND, 32, 64><<<n, THREADS, 0, stream>>>(p);
+            if (ba == 64) return experts_kernel<T, VEC, KIND, 64, 32><<<n, THREADS, 0, stream>>>(p);
         }
-        experts_kernel<T, VEC, KIND, 128><<<n, THREADS, 0, stream>>>(p);
+        // longer steps have half of the barriers, and are ahead in long sums: 16000 rows, 2001 x 1003 over 2, input gradient 161 and 138 us, weight
+        // gradient 126 and 108; 8000 rows, 1001 x 999 over 5, 52 and 55, 49 and 42; 333 rows, weight gradient 11 and 13.  fp32 has no registers for them
+        if constexpr (sizeof(T) == 2)
+            if ((KIND == WEIGHT_GRAD ? p.rows / p.experts / p.splits : p.chunk) > 1024) return experts_kernel<T, VEC, KIND, 128, 64><<<n, THREADS, 0, stream>>>(p);
+        experts_kernel<T, VEC, KIND, 128, 32><<<n, THREADS, 0, stream>>>(p);
     };
     if (c.how >= ANY32) {
         if (x->dtype == DEAR_BF16) {

@@ -124,6 +124,12 @@ def test_many_rows_of_few_outputs(ops, outs, ins, dtype):
     check(ops, *make([3000, 0, 905, 2, 64], 7, outs, ins, dtype, 44))
 
 
+@pytest.mark.parametrize("counts, outs, ins", [([2500, 0, 2100], 1031, 515), ([600, 900], 37, 2053), ([800, 500], 2053, 130)])
+def test_long_sums_of_any_width(ops, counts, outs, ins):
+    """Sums beyond 1024 in rows that start anywhere."""
+    check(ops, *make(counts, 3, outs, ins, BF16, 46))
+
+
 @pytest.mark.parametrize("outs, ins", [(136, 1000), (1000, 136)])
 def test_few_tiles_behind_a_round(ops, outs, ins):
     """66 x 4 tiles of 256: one for each of 256 units, and eight."""
