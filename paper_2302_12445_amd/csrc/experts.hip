@@ -6,6 +6,9 @@
 // All three are sums of products of two operands that lie in memory either along the summed index (x and w for y, dy for dx) or across
 // it (w for dx, both for dw); the former are read from LDS in rows, the latter with the transposing reads.  Rows of an expert start
 // anywhere: a workgroup finds the expert of its tile from the ends, on the device, so that nothing waits for the host to know them.
+//
+// Matrix instructions bound large calls, at the clock that the card's power leaves them (16384 rows, 4096 x 1024 over 8, bf16: 1000 to 1200
+// TFLOP/s, a library's product of 8192 x 8192 x 8192 1394); the weights' way from memory bounds few rows (32: 4.5 TB/s).
 #include <cmath>
 #include <type_traits>
 
@@ -443,7 +446,8 @@ __device__ __forceinline__ void store_tile(const params &p, void *outputs, const
 }
 
 // The tiles of SA x SB outputs that next() gives, one after another.  xa, ya and xb, yb: the operands' places for steps in turn, arrays of
-// their own, so that a read from one need not wait for what memory brings to another; lines: 4 KB a wave.
+// their own, so that a read from one need not wait for what memory brings to another; lines: 4 KB a wave, or null where the second step's
+// place is to serve for it as well.
 template <int KIND, int SA, int SB, bool PARTS, typename NEXT>
 __device__ __forceinline__ void run(const params &p, void *outputs, DEAR_LDS char *xa, DEAR_LDS char *ya, DEAR_LDS char *xb, DEAR_LDS char *yb,
                                     DEAR_LDS char *lines, NEXT next) {
@@ -1101,9 +1105,9 @@ template <int KIND> int call(const dear_experts_t *x, hipStream_t stream) {
             if (ba == 64) return experts_kernel<T, VEC, KIND, 64, 32><<<n, THREADS, 0, stream>>>(p);
         }
         // longer steps have half of the barriers, and are ahead in long sums: 16000 rows, 2001 x 1003 over 2, input gradient 161 and 138 us, weight
-        // gradient 126 and 108; 8000 rows, 1001 x 999 over 5, 52 and 55, 49 and 42; 333 rows, weight gradient 11 and 13.  fp32 has no registers for them
-        if constexpr (sizeof(T) == 2)
-            if ((KIND == WEIGHT_GRAD ? p.rows / p.experts / p.splits : p.chunk) > 1024) return experts_kernel<T, VEC, KIND, 128, 64><<<n, THREADS, 0, stream>>>(p);
+        // gradient 126 and 108, in fp32 636 and 571, 556 and 544; 8000 rows, 1001 x 999 over 5, 52 and 55, 49 and 42; 333 rows, weight gradient 11 and 13
+        if ((KIND == WEIGHT_GRAD ? p.rows / p.experts / p.splits : p.chunk) > 1024)
+            return experts_kernel<T, VEC, KIND, 128, 64><<<n, THREADS, 0, stream>>>(p);
         experts_kernel<T, VEC, KIND, 128, 32><<<n, THREADS, 0, stream>>>(p);
     };
     if (c.how >= ANY32) {

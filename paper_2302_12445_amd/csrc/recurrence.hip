@@ -11,7 +11,8 @@
 // it.  The backward pass needs the states before each step as well: it computes them again, in fp32, from the states that the
 // forward pass kept at each tile's first step, which takes less traffic than to read h, and no rounding.
 //
-// HBM bounds it, 6 bytes of bf16 an element forward and 10 backward, and the vector instructions come close to that.
+// HBM bounds it, 6 bytes of bf16 an element forward and 10 backward, and the vector instructions come close to that: single tiles, 64 x 256 x
+// 1024 bf16, 18.4 us = 5.5 TB/s and 37.5 = 4.5; tiles that are joined, 2 x 8192 x 1024, with the launch that clears their maps 26 and 45.
 #include <type_traits>
 
 #include "ops_common.h"
@@ -369,7 +370,30 @@ template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__
     if (speaks && a.last && tile == a.tiles - 1) store_state<MODE>(a.last + p.b * a.width, carry, p.col, a.width);
 }
 
-// As above, from the last tile to the first; the states before the tile's steps come from the kept one.
+// One step, as of sequences that are continued token by token: a lane has two channels of a sequence, and nothing to join (16 x 1 x 1024 bf16 2.2
+// us, 256 x 1 x 1024 2.5; by the kernel above, whose lanes have sixteen steps, 3.7 and 7.0).
+template <typename T, int MODE> __global__ __launch_bounds__(256) void recurrence_step_kernel(params a, uint32_t pairs, uint32_t all) {
+    const uint32_t i = blockIdx.x * 256 + threadIdx.x;
+    if (i >= all) return;
+    const int64_t b = i / pairs;
+    int col = (int)(i % pairs) * N;
+    if (MODE != SINGLE) col = min(col, a.width - N);
+    const raw<T> g = load<T, MODE>(tile_at<T>(a.gate, b, 0), 0, col, a.width), x = load<T, MODE>(tile_at<T>(a.x, b, 0), 0, col, a.width);
+    float s[N] = {}, h[N] = {};
+    if (a.state) load_state<MODE>(s, a.state + b * a.width, col, a.width);
+    if (a.kept) store_state<MODE>(a.kept + b * a.width, s, col, a.width);
+    if (length(a, b) > 0)
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            float ga, gb;
+            gates(get(g, c), ga, gb);
+            h[c] = s[c] = ga * s[c] + gb * get(x, c);
+        }
+    store<T, MODE>(tile_at<T>(a.h, b, 0), 0, both<T>(h[0], h[1]), col, a.width);
+    if (a.last) store_state<MODE>(a.last + b * a.width, s, col, a.width);
+}
+
+// As recurrence_kernel, from the last tile to the first; the states before the tile's steps come from the kept one.
 template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W, sizeof(T) == 2 ? 4 : 2) void recurrence_backward_kernel(params a) {
     __shared__ wave_maps<W> lds[SHARED ? 2 : 1];
     const uint32_t id = SHARED ? turned_group(a) : blockIdx.x;
@@ -572,12 +596,18 @@ template <typename T, int MODE, bool BACKWARD> void launch(params a, int64_t bat
         const unsigned all = (unsigned)(groups * a.tiles);
         if (BACKWARD) recurrence_backward_kernel<T, WAVES, MODE, true><<<all, 64 * WAVES, 0, stream>>>(a);
         else recurrence_kernel<T, WAVES, MODE, true><<<all, 64 * WAVES, 0, stream>>>(a);
-    } else if (a.steps <= WAVE_STEPS) {
-        by_waves(std::integral_constant<int, 1>());
-    } else if (a.steps <= 3 * WAVE_STEPS) {
-        by_waves(std::integral_constant<int, 3>());
+    } else if (a.steps == 1 && !BACKWARD) {
+        const int64_t pairs = ceil_div(a.width, N), all = batch * pairs;
+        recurrence_step_kernel<T, MODE><<<(unsigned)ceil_div(all, 256), 256, 0, stream>>>(a, (uint32_t)pairs, (uint32_t)all);
     } else {
-        by_waves(std::integral_constant<int, WAVES>());
+        // waves that no step would fill take time all the same: 256 x 32 x 1024 bf16 10.7 us with one, 18 with three, 40 with eight; 128 x 128 x 1024
+        // 18.7 with four, 25.6 with eight; 64 x 192 x 1024 18.2 with six, 17.5 with eight
+        const int64_t waves = ceil_div(a.steps, WAVE_STEPS);
+        if (waves <= 1) by_waves(std::integral_constant<int, 1>());
+        else if (waves <= 2) by_waves(std::integral_constant<int, 2>());
+        else if (waves <= 3) by_waves(std::integral_constant<int, 3>());
+        else if (waves <= 4) by_waves(std::integral_constant<int, 4>());
+        else by_waves(std::integral_constant<int, WAVES>());
     }
 }
 
@@ -607,10 +637,10 @@ int call(const dear_recurrence_t *r, bool backward, hipStream_t stream) {
         if (backward) launch<T, decltype(mode)::value, true>(a, r->batch, shares(*r), r->workspace, stream);
         else launch<T, decltype(mode)::value, false>(a, r->batch, shares(*r), r->workspace, stream);
     };
-    // Of an odd width two workgroups take the last channel but one, with the same results.  Where the state before is overwritten with the one
-    // behind, the second could find the latter: there each channel has one workgroup.
+    // Of an odd width the last channel but one is taken twice, by two workgroups or, of one step, perhaps two waves, with the same results.  Where
+    // the state before is overwritten with the one behind, the second could find the latter: there each channel is taken by one lane.
     const bool over_itself = backward ? r->dstate && r->dstate == r->dlast : r->last && r->last == r->state;
-    const bool apart = over_itself && r->width % N && r->width > CG && !shares(*r);
+    const bool apart = over_itself && r->width % N && (r->width > CG || r->steps == 1) && !shares(*r);
     auto by_type = [&](auto t) {
         if (vec) by_mode(t, std::integral_constant<int, ALIGNED>());
         else if (r->width >= N && !apart) by_mode(t, std::integral_constant<int, ANYWHERE>());

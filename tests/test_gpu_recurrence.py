@@ -250,7 +250,7 @@ def test_state_in_place(ops):
         assert all(torch.equal(a, b) for a, b in zip((dx, dg, dlast), grads))
 
 
-@pytest.mark.parametrize("shape", [(4000, 1, 65), (900, 100, 129), (3, 200, 1001), (1, 20, 1)])
+@pytest.mark.parametrize("shape", [(4000, 1, 65), (4000, 1, 33), (900, 100, 129), (3, 200, 1001), (1, 20, 1)])
 def test_state_in_place_of_odd_widths(ops, shape):
     """The last channels of an odd width are not read by a workgroup that does not write them."""
     x, gate, state = inputs(shape, F32, 51)
@@ -309,3 +309,18 @@ def test_refusals(ops):
     wide = torch.zeros(1, 1, device=DEV).expand(2, 1 << 22)
     with pytest.raises(DearError):
         ops.recurrence(wide[None], wide[None])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("width", [1, 2, 63, 64, 1001])
+def test_one_step(ops, width, dtype):
+    """One step, of which some sequences have none, with a state and without, apart and of larger tensors."""
+    x, gate, state = inputs((70, 1, width), dtype, 81)
+    lens = [int(b % 3 > 0) for b in range(70)]
+    check(ops, x, gate, state)
+    check(ops, x, gate, state, lens)
+    check(ops, x, gate, None, lens)
+    wide = torch.empty(70, 3, 2 * width + 1, dtype=dtype, device=DEV).fill_(NAN)
+    part = wide[:, 1:2, 1:width + 1]
+    part.copy_(x)
+    assert all(torch.equal(a, b) for a, b in zip(ops.recurrence(part, gate, state), ops.recurrence(x, gate, state)))
