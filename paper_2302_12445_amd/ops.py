@@ -21,7 +21,6 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
-import itertools
 import math
 import os
 import struct
@@ -593,7 +592,8 @@ def expert_weight_grad(dy: torch.Tensor, x: torch.Tensor, ends: torch.Tensor) ->
 
 
 # ------------------------------------------------------------------------------------ gradients
-_GRAD_MEMBERS = "2Qq2i"  # dear_grad_t
+_GRAD_MEMBERS = "2Q2q"  # dear_grad_t, its two types as one number
+_dtype_of = torch.Tensor.dtype.__get__
 
 
 @functools.lru_cache(maxsize=256)
@@ -624,32 +624,44 @@ def _grad_norm(tensors: Sequence[torch.Tensor], out: Optional[Sequence[torch.Ten
     first = tensors[0]
     if _elsewhere(first):
         with torch.cuda.device(first.device):
-            return _grad_norm(tensors, out, max_norm)
+            return _grad_norm(tensors, None if out is None else outs, max_norm)
     # a list at a time: a model has some hundred tensors, and each question to one takes the host some 50 ns
-    index, types = first.get_device(), [_DTYPE.get(t.dtype) for t in tensors]
-    out_types = types if outs is tensors else [_DTYPE.get(t.dtype) for t in outs]
-    where = set(map(torch.Tensor.get_device, tensors)) | set(map(torch.Tensor.get_device, outs))
-    if None in types or None in out_types or len(where) > 1 or index < 0:
+    index, count = first.get_device(), len(tensors)
+    here, kinds = set(map(torch.Tensor.get_device, tensors)), set(map(_dtype_of, tensors))
+    out_kinds = kinds if outs is tensors else set(map(_dtype_of, outs))
+    if outs is not tensors:
+        here.update(map(torch.Tensor.get_device, outs))
+    if len(here) > 1 or index < 0 or not all(k in _DTYPE for k in kinds | out_kinds):
         for t in tensors:
             _dtype(t, "a gradient")
         for t in outs:
             _dtype(t, "an output")
         raise ValueError("tensors are on several devices")
-    if outs is not tensors and any(o.shape != g.shape for o, g in zip(outs, tensors)):
-        raise ValueError("an output has another shape than its gradient")
-    if not all(map(torch.Tensor.is_contiguous, tensors)) or not all(map(torch.Tensor.is_contiguous, outs)):
+    sizes = list(map(torch.Tensor.numel, tensors))
+    if outs is not tensors and sizes != list(map(torch.Tensor.numel, outs)):
+        raise ValueError("an output has more or fewer elements than its gradient")
+    if not all(map(torch.Tensor.is_contiguous, tensors)) or not (outs is tensors or all(map(torch.Tensor.is_contiguous, outs))):
+        if any(o.shape != g.shape for o, g in zip(outs, tensors)):
+            raise ValueError("tensors that are not contiguous: an output has another shape than its gradient")
         if clip and not all(_dense(o) for o in outs):
             raise ValueError("an output has gaps between its elements")
         # elements in the outputs' order
         tensors = [g if _dense(g) and (g.stride() == o.stride() or not clip) else
                    torch.empty_strided(o.shape, o.stride(), dtype=g.dtype, device=g.device).copy_(g) if clip else g.contiguous()
                    for g, o in zip(tensors, outs)]
-    lib, count = load_library(), len(tensors)
+    lib = load_library()
     norm = torch.empty((), dtype=torch.float32, device=first.device)
     need = _workspace("dear_grad_norm_workspace", count)
     space = torch.empty(need, dtype=torch.uint8, device=first.device)
-    members = zip(map(torch.Tensor.data_ptr, tensors), map(torch.Tensor.data_ptr, outs), map(torch.Tensor.numel, tensors), types, out_types)
-    packed, stream = _grad_layout(count).pack(*itertools.chain.from_iterable(members)), _raw_stream(index)
+    members = [0] * (4 * count)
+    members[::4] = places = list(map(torch.Tensor.data_ptr, tensors))
+    members[1::4] = places if outs is tensors else map(torch.Tensor.data_ptr, outs)
+    members[2::4] = sizes
+    if len(kinds) == 1 and len(out_kinds) == 1:
+        members[3::4] = [_DTYPE[first.dtype] | _DTYPE[outs[0].dtype] << 32] * count
+    else:
+        members[3::4] = [_DTYPE[g.dtype] | _DTYPE[o.dtype] << 32 for g, o in zip(tensors, outs)]
+    packed, stream = _grad_layout(count).pack(*members), _raw_stream(index)
     if clip:
         _check(lib.dear_clip_grads(packed, count, max_norm, norm.data_ptr(), space.data_ptr(), need, stream), "dear_clip_grads")
         torch.autograd.graph.increment_version(outs)
@@ -666,8 +678,8 @@ def grad_norm(tensors: Sequence[torch.Tensor]) -> torch.Tensor:
 def clip_grads(tensors: Sequence[torch.Tensor], max_norm: float, out: Optional[Sequence[torch.Tensor]] = None) -> torch.Tensor:
     """Scales the tensors by min(1, max_norm / norm), with norm that over all of them, and gives norm.
 
-    In place, or into `out`: tensors of the same shapes, bf16 or fp32 each, so that fp32 gradients can be had of bf16 ones.  Nothing is
-    written that need not change.  The norm stays on the GPU: nothing waits for it.
+    In place, or into `out`: tensors of the same shapes or, contiguous ones, of as many elements (slices of a flat buffer), bf16 or fp32 each,
+    so that fp32 gradients can be had of bf16 ones.  Nothing is written that need not change.  The norm stays on the GPU: nothing waits for it.
     """
     max_norm = float(max_norm)
     if not max_norm > 0:

@@ -85,6 +85,21 @@ def test_shapes_and_orders(ops):
         ops.clip_grads([gaps], 0.5)
 
 
+def test_into_slices_of_a_flat_buffer(ops):
+    """Contiguous outputs need as many elements only; others the same shape.  Both lists may be had once."""
+    gen = torch.Generator().manual_seed(17)
+    grads = [normal(gen, (5, 7), BF16), normal(gen, (33,), BF16), normal(gen, (2, 3, 4), BF16)]
+    flat = torch.zeros(35 + 33 + 24, device=DEV)
+    slices = flat.split([35, 33, 24])
+    norm = ops.clip_grads(iter(grads), 0.5, out=iter(slices))
+    want = [torch.empty(g.shape, device=DEV) for g in grads]
+    assert torch.equal(norm, ops.clip_grads(grads, 0.5, out=want))
+    assert torch.equal(flat, torch.cat([w.flatten() for w in want]))
+    for bad in ([grads[0].t()], [slices[0].as_strided((7, 5), (1, 7))]):  # (5, 7) is asked for
+        with pytest.raises(ValueError):
+            ops.clip_grads([grads[0]], 0.5, out=bad)
+
+
 def test_places_that_are_shared_are_refused(ops):
     from paper_2302_12445_amd import DearError
     t = normal(torch.Generator().manual_seed(5), (100,))
