@@ -326,6 +326,7 @@ class Experts(torch.nn.Module):
         share = torch.softmax(scores, -1)
         if lens is not None:
             chosen = torch.where(valid, chosen, self.experts)
+            share = torch.where(valid, share, 0)  # nor what the incoming gradient holds there: it would reach the router through the softmax
         sorted_, order = chosen.flatten().sort(stable=True)
         ends = torch.searchsorted(sorted_, torch.arange(self.experts, device=y.device), right=True).to(torch.int32)
         place = torch.empty_like(order).scatter_(0, order, torch.arange(order.numel(), device=y.device)).view(-1, self.top)

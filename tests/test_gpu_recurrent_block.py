@@ -127,6 +127,25 @@ def test_experts_take_nothing_from_behind_the_sequences(dtype):
     assert not results[1][0][1].any() and not results[1][1][2, 3:].any()
 
 
+@pytest.mark.parametrize("fill", [math.nan, math.inf])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_behind_the_sequences_reach_nothing(dtype, fill):
+    """What the incoming gradient holds behind the lengths changes no gradient."""
+    from paper_2302_12445_amd.layers import Experts
+    torch.manual_seed(8)
+    layer = Experts(32, 48, 5, 2).to(DEV)
+    y, dout = (torch.randn(3, 7, 32, device=DEV).to(dtype) for _ in range(2))
+    lens = torch.tensor([7, 0, 3], dtype=torch.int32, device=DEV)
+    results = []
+    for behind in (0.0, fill):
+        a, d = y.clone().requires_grad_(), dout.clone()
+        d[1], d[2, 3:] = behind, behind
+        layer.zero_grad()
+        layer(a, lens).backward(d)
+        results.append([a.grad] + [p.grad.clone() for p in layer.parameters()])
+    assert all(torch.equal(p, q) for p, q in zip(*results)) and results[1][1].any()
+
+
 def test_experts_spread_and_gather():
     """Each token goes to its experts and back, none to others; gradients of tokens that go to several are added."""
     from paper_2302_12445_amd.layers import Experts

@@ -144,3 +144,19 @@ def test_experts_refuse_more_than_there_are():
     for top in (0, 3):
         with pytest.raises(ValueError, match="top"):
             layers.Experts(4, 4, 2, top)
+
+
+@pytest.mark.parametrize("fill", [float("nan"), float("inf")])
+def test_gradients_behind_the_lengths_reach_nothing(plain, fill):
+    """What the incoming gradient holds behind the lengths changes no gradient, the router's among them."""
+    torch.manual_seed(1)
+    layer = layers.Experts(4, 6, 5, 2)
+    y, dout, lens = torch.randn(3, 6, 4), torch.randn(3, 6, 4), torch.tensor([6, 0, 3])
+    results = []
+    for behind in (0.0, fill):
+        a, d = y.clone().requires_grad_(), dout.clone()
+        d[1], d[2, 3:] = behind, behind
+        layer.zero_grad()
+        layer(a, lens).backward(d)
+        results.append([a.grad] + [p.grad.clone() for p in layer.parameters()])
+    assert all(torch.equal(p, q) for p, q in zip(*results)) and results[1][1].any()
