@@ -13,6 +13,7 @@
 //
 // HBM bounds it, 6 bytes of bf16 an element forward and 10 backward, and the vector instructions come close to that: single tiles, 64 x 256 x
 // 1024 bf16, 18.4 us = 5.5 TB/s and 37.5 = 4.5; tiles that are joined, 2 x 8192 x 1024, with the launch that clears their maps 26 and 45.
+#include <cfloat>
 #include <type_traits>
 
 #include "ops_common.h"
@@ -44,7 +45,7 @@ struct params {
     float *last, *dstate, *kept;
     const int32_t *lens;
     uint32_t *tickets;  // workgroups that have begun of those that share a sequence's channels, one count a line of the cache
-    uint64_t *maps;     // of their tiles, [batch, tiles, width]: A and H, or E, of the tiles in their order; at first all ones
+    uint64_t *maps;     // of their tiles, [batch, tiles, width]: C and H, or E, of the tiles in their order; at first all ones
     int64_t steps;
     int32_t width, groups, tiles;
 };
@@ -64,12 +65,36 @@ __device__ __forceinline__ void halves(float x, float &earlier, float &later) {
     earlier = __uint_as_float(w[0]), later = __uint_as_float(w[1]);
 }
 
-// Joins the strips of a wave.  A, H, E: the map of the lane's strip, which becomes the wave's.  before: the map from the wave's first step to
-// the strip's, behind: backward from the wave's last step to the strip's.
+// What a map keeps of the state, A, is told on as one number C: A itself below a half, from there on -(1 - A), with the sign, by which the state
+// goes on as s + (H - (1 - A) s).  An A near 1 that is rounded by itself is wrong by the same 2^-25 each time that a gate stays, which adds up over
+// all that a channel remembers, to 2^-25 / (1 - a) (of fp32 steps with a gate of 9, 4e-4); by C the state goes to where H and 1 - A say, however
+// long the sequence is.  So go states from tile to tile and from call to call (2 x 8192 x 1024 bf16 forward 27.9 us, so 29.4); within a tile, from a
+// state that is at hand, they go by A.  -0 leaves a state as it is.
+__device__ __forceinline__ float coefficient(float A, float B) { return B <= 0.5f ? -B : A; }
+__device__ __forceinline__ bool by_complement(float C) { return (int32_t)__float_as_uint(C) < 0; }
+__device__ __forceinline__ float whole(float C) { return by_complement(C) ? 1.f + C : C; }
+// (An infinite state stays one: only what is subtracted is kept finite.)
+__device__ __forceinline__ float through(float C, float H, float s) {
+    const bool less = by_complement(C);
+    const float t = less ? __builtin_amdgcn_fmed3f(s, -FLT_MAX, FLT_MAX) : s;
+    return __builtin_fmaf(C, t, H) + (less ? s : 0.f);
+}
+// A and B = 1 - A of several stretches in a row, in either order.
+struct stretches {
+    float A = 1.f, B = 0.f;
+    __device__ __forceinline__ void add(float C) {
+        B += A * (by_complement(C) ? -C : 1.f - C);
+        A *= whole(C);
+    }
+};
+
+// Joins the strips of a wave.  C, H, E: the map of the lane's strip, which becomes the wave's.  before: the map from the wave's first step to
+// the strip's, behind: backward from the wave's last step to the strip's, by A.
 template <bool FORWARD, bool BACKWARD>
-__device__ __forceinline__ void join(float &A, float &H, float &E, float &before_A, float &before_H, float &behind_A, float &behind_E, int lane) {
-    float A0, A1;
-    halves(A, A0, A1);
+__device__ __forceinline__ void join(float &C, float &H, float &E, float &before_A, float &before_H, float &behind_A, float &behind_E, int lane) {
+    float C0, C1;
+    halves(C, C0, C1);
+    const float A0 = whole(C0), A1 = whole(C1);
     const bool later = lane & 32;
     if (FORWARD) {
         float H0, H1;
@@ -85,22 +110,28 @@ __device__ __forceinline__ void join(float &A, float &H, float &E, float &before
         behind_E = later ? 0.f : E1;
         E = A0 * E1 + E0;
     }
-    A = A0 * A1;
+    const float B = -C0 - C1 * A0;  // 1 - A0 A1, where both are held by 1 - A
+    C = by_complement(C0) && by_complement(C1) && B <= 0.5f ? -B : A0 * A1;
 }
 
 // How a lane's N channels lie in memory.
 enum { SINGLE, ANYWHERE, ALIGNED };
 
-// Where a lane stands: its channels, its strip and, of a tile, its first step.  Lanes behind the last channel take the last ones over
-// again, with the same results, so that no lane needs a branch.
+// First of a workgroup's N channels number `pair`.  Lanes behind the last channel take the last ones over again, with the same results, so that no
+// lane needs a branch.
+template <int MODE> __device__ __forceinline__ int first_of(const params &a, int group, int pair) {
+    const int col = group * CG + pair * N;
+    return MODE != SINGLE ? min(col, a.width - N) : col;
+}
+// Where a lane stands: its channels, its strip and, of a tile, its first step.
 struct place {
     int64_t b;
-    int lane, wave, col, step;
-    __device__ __forceinline__ place(const params &a, uint32_t sequence_group, int mode) {
+    int lane, wave, group, col, step;
+    template <int MODE> __device__ __forceinline__ place(const params &a, uint32_t sequence_group, std::integral_constant<int, MODE>) {
         lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         b = sequence_group / a.groups;
-        col = (int)(sequence_group % a.groups) * CG + lane % ROW_LANES * N;
-        if (mode != SINGLE) col = min(col, a.width - N);
+        group = (int)(sequence_group % a.groups);
+        col = first_of<MODE>(a, group, lane % ROW_LANES);
         step = wave * WAVE_STEPS + lane / ROW_LANES * R;
     }
 };
@@ -186,15 +217,16 @@ template <int MODE> __device__ __forceinline__ void store_state(float *row, cons
     store<float, MODE>((char *)row, 0, f32x2{s[0], s[1]}, col, cols);
 }
 
-// The map of a tile's steps before the last wave has been joined: each wave's in LDS, [wave][A, H or E][channel].
-template <int W> struct wave_maps_of { typedef float type[W][3][CG] __attribute__((aligned(16))); };
+// The map of a tile's steps before the last wave has been joined: each wave's in LDS, [wave][A, C, H or E][channel].
+enum { MAP_A, MAP_C, MAP_H, MAP_E };
+template <int W> struct wave_maps_of { typedef float type[W][4][CG] __attribute__((aligned(16))); };
 template <int W> using wave_maps = typename wave_maps_of<W>::type;
 
-// s through a wave's map, of A and H (1) or E (2); one wave's after another, as all of them at once take registers.
-template <int WHICH, int W> __device__ __forceinline__ void pass(float *s, const wave_maps<W> &maps, int w, const place &p) {
-    const f32x2 A = *(const f32x2 *)&maps[w][0][p.lane % ROW_LANES * N], H = *(const f32x2 *)&maps[w][WHICH][p.lane % ROW_LANES * N];
+// s through a wave's map, of H or E: by C, or within a tile by A alone, as in a strip.  One wave's after another, as all of them at once take registers.
+template <int BY, int WHICH, int W> __device__ __forceinline__ void pass(float *s, const wave_maps<W> &maps, int w, const place &p) {
+    const f32x2 M = *(const f32x2 *)&maps[w][BY][p.lane % ROW_LANES * N], H = *(const f32x2 *)&maps[w][WHICH][p.lane % ROW_LANES * N];
 #pragma unroll
-    for (int c = 0; c < N; ++c) s[c] = A[c] * s[c] + H[c];
+    for (int c = 0; c < N; ++c) s[c] = BY == MAP_C ? through(M[c], H[c], s[c]) : M[c] * s[c] + H[c];
     __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -231,21 +263,30 @@ __device__ __forceinline__ uint32_t turned_group(const params &a) {
 __device__ __forceinline__ uint64_t *map_at(const params &a, int64_t b, int order, int col, int c) {
     return a.maps + (b * a.tiles + order) * a.width + min(col + c, a.width - 1);
 }
-__device__ __forceinline__ void tell(const params &a, const place &p, int order, const float *A, const float *H) {
+// A tile's map from its waves', of H or E: a lane of the first wave takes one channel.
+template <int WHICH, int MODE, int W> __device__ __forceinline__ void tell(const params &a, const place &p, int order, const wave_maps<W> &maps) {
+    static_assert(CG == 64, "a channel a lane");
+    stretches all;
+    float H = 0.f;
 #pragma unroll
-    for (int c = 0; c < N; ++c) {
-        const uint32_t x = A[c] != A[c] ? 0x7fc00000u : __float_as_uint(A[c]);  // (some NaN is all ones)
-        __hip_atomic_store(map_at(a, p.b, order, p.col, c), (uint64_t)__float_as_uint(H[c]) << 32 | x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int i = 0; i < W; ++i) {
+        const int w = WHICH == MAP_H ? i : W - 1 - i;
+        const float C = maps[w][MAP_C][p.lane];
+        H = maps[w][MAP_A][p.lane] * H + maps[w][WHICH][p.lane];
+        all.add(C);
     }
+    const float C = coefficient(all.A, all.B);
+    const uint32_t x = C != C ? 0x7fc00000u : __float_as_uint(C);  // (some NaN is all ones)
+    __hip_atomic_store(map_at(a, p.b, order, first_of<MODE>(a, p.group, p.lane / N), p.lane % N), (uint64_t)__float_as_uint(H) << 32 | x, __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // s through the maps of the tiles before `order`: strips take a run of tiles each, and are joined as a tile's are.  The order in which maps
 // are joined does not depend on when they are told.
 template <int W> __device__ __forceinline__ void through_earlier(float *s, const params &a, const place &p, int order, wave_maps<W> &maps) {
     const int each = (order + W * STRIPS - 1) / (W * STRIPS), first = (p.wave * STRIPS + p.lane / ROW_LANES) * each;
-    float A[N], H[N];
-#pragma unroll
-    for (int c = 0; c < N; ++c) A[c] = 1.f, H[c] = 0.f;
+    stretches before[N];
+    float H[N] = {};
     for (int i = first; i < min(first + each, order); ++i) {
         uint64_t x[N];
         for (;;) {
@@ -261,18 +302,19 @@ template <int W> __device__ __forceinline__ void through_earlier(float *s, const
 #pragma unroll
         for (int c = 0; c < N; ++c) {
             const float mine = __uint_as_float((uint32_t)x[c]);
-            H[c] = mine * H[c] + __uint_as_float((uint32_t)(x[c] >> 32));
-            A[c] *= mine;
+            H[c] = through(mine, __uint_as_float((uint32_t)(x[c] >> 32)), H[c]);
+            before[c].add(mine);
         }
     }
     float none = 0.f;
 #pragma unroll
     for (int c = 0; c < N; ++c) {
-        join<true, false>(A[c], H[c], none, none, none, none, none, p.lane);
-        if (p.lane < ROW_LANES) maps[p.wave][0][p.lane * N + c] = A[c], maps[p.wave][1][p.lane * N + c] = H[c];
+        float C = coefficient(before[c].A, before[c].B);
+        join<true, false>(C, H[c], none, none, none, none, none, p.lane);
+        if (p.lane < ROW_LANES) maps[p.wave][MAP_C][p.lane * N + c] = C, maps[p.wave][MAP_H][p.lane * N + c] = H[c];
     }
     __syncthreads();
-    for (int w = 0; w < W; ++w) pass<1, W>(s, maps, w, p);
+    for (int w = 0; w < W; ++w) pass<MAP_C, MAP_H, W>(s, maps, w, p);
 }
 
 // Steps behind the last one: a = 1 and nothing added, by gates of infinity and values of 0.
@@ -296,7 +338,7 @@ template <typename T> __device__ __forceinline__ void zero_behind(raw<T> (&x)[R]
 template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W, 4) void recurrence_kernel(params a) {
     __shared__ wave_maps<W> lds[SHARED ? 2 : 1];
     const uint32_t id = SHARED ? turned_group(a) : blockIdx.x;
-    const place p(a, id, MODE);
+    const place p(a, id, std::integral_constant<int, MODE>());
     const int tile = SHARED ? take_ticket(a.tickets + id * TICKET) : 0;
     const int64_t end = length(a, p.b);
     const bool speaks = threadIdx.x < ROW_LANES;  // stores states
@@ -316,46 +358,41 @@ template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__
     float ga[R][N], gx[R][N], before_A[N], before_H[N];
 #pragma unroll
     for (int c = 0; c < N; ++c) {
-        float A = 1.f, H = 0.f, none = 0.f;
+        float A = 1.f, B = 0.f, H = 0.f, none = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float gb;
             gates(get(g[r], c), ga[r][c], gb);
             gx[r][c] = gb * get(x[r], c);
             A *= ga[r][c];
+            B = ga[r][c] * B + gb;  // 1 - A
             H = ga[r][c] * H + gx[r][c];
         }
-        join<true, false>(A, H, none, before_A[c], before_H[c], none, none, p.lane);
-        if (p.lane < ROW_LANES) maps[p.wave][0][p.lane * N + c] = A, maps[p.wave][1][p.lane * N + c] = H;
+        float C = coefficient(A, B);
+        join<true, false>(C, H, none, before_A[c], before_H[c], none, none, p.lane);
+        if (p.lane < ROW_LANES) {
+            maps[p.wave][MAP_A][p.lane * N + c] = whole(C);
+            maps[p.wave][MAP_C][p.lane * N + c] = C;
+            maps[p.wave][MAP_H][p.lane * N + c] = H;
+        }
         __builtin_amdgcn_sched_barrier(0);  // one channel after another: together they take registers that waves could have
     }
     __syncthreads();
     if (SHARED) {
-        if (speaks && tile + 1 < a.tiles) {
-            float A[N], H[N];
-#pragma unroll
-            for (int c = 0; c < N; ++c) {
-                A[c] = 1.f, H[c] = 0.f;
-#pragma unroll
-                for (int w = 0; w < W; ++w) {
-                    const float m = maps[w][0][p.lane * N + c];
-                    H[c] = m * H[c] + maps[w][1][p.lane * N + c];
-                    A[c] *= m;
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            tell(a, p, tile, A, H);
-        }
+        if (p.wave == 0 && tile + 1 < a.tiles) tell<MAP_H, MODE, W>(a, p, tile, maps);
         if (tile > 0) through_earlier<W>(carry, a, p, tile, lds[SHARED ? 1 : 0]);
     }
     if (speaks && a.kept) store_state<MODE>(a.kept + (p.b * a.tiles + tile) * a.width, carry, p.col, a.width);
     float s[N];
 #pragma unroll
-    for (int w = 0; w < W; ++w) {
-        if (w == p.wave)
+    for (int c = 0; c < N; ++c) s[c] = carry[c];
+    if (p.wave == 0 && tile == a.tiles - 1) {
 #pragma unroll
-            for (int c = 0; c < N; ++c) s[c] = carry[c];
-        if (w < p.wave || (p.wave == 0 && tile == a.tiles - 1)) pass<1, W>(carry, maps, w, p);
+        for (int w = 0; w < W; ++w) pass<MAP_C, MAP_H, W>(carry, maps, w, p);
+    } else {
+#pragma unroll
+        for (int w = 0; w < W - 1; ++w)
+            if (w < p.wave) pass<MAP_A, MAP_H, W>(s, maps, w, p);
     }
 #pragma unroll
     for (int c = 0; c < N; ++c) s[c] = before_A[c] * s[c] + before_H[c];
@@ -387,7 +424,8 @@ template <typename T, int MODE> __global__ __launch_bounds__(256) void recurrenc
         for (int c = 0; c < N; ++c) {
             float ga, gb;
             gates(get(g, c), ga, gb);
-            h[c] = s[c] = ga * s[c] + gb * get(x, c);
+            const float y = through(coefficient(ga, gb), gb * get(x, c), s[c]);
+            h[c] = s[c] = y;
         }
     store<T, MODE>(tile_at<T>(a.h, b, 0), 0, both<T>(h[0], h[1]), col, a.width);
     if (a.last) store_state<MODE>(a.last + b * a.width, s, col, a.width);
@@ -397,7 +435,7 @@ template <typename T, int MODE> __global__ __launch_bounds__(256) void recurrenc
 template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W, sizeof(T) == 2 ? 4 : 2) void recurrence_backward_kernel(params a) {
     __shared__ wave_maps<W> lds[SHARED ? 2 : 1];
     const uint32_t id = SHARED ? turned_group(a) : blockIdx.x;
-    const place p(a, id, MODE);
+    const place p(a, id, std::integral_constant<int, MODE>());
     const int order = SHARED ? take_ticket(a.tickets + id * TICKET) : 0, tile = a.tiles - 1 - order;
     const int64_t end = length(a, p.b);
     const bool speaks = threadIdx.x < ROW_LANES;
@@ -420,54 +458,51 @@ template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__
     float before_A[N], before_H[N], behind_A[N], behind_E[N];
 #pragma unroll
     for (int c = 0; c < N; ++c) {
-        float A = 1.f, H = 0.f, E = 0.f, ga[R];
+        float A = 1.f, B = 0.f, H = 0.f, E = 0.f, ga[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             float gb;
             gates(get(g[r], c), ga[r], gb);
             A *= ga[r];
+            B = ga[r] * B + gb;
             H = ga[r] * H + gb * get(x[r], c);
         }
 #pragma unroll
         for (int r = R - 1; r >= 0; --r) E = ga[r] * E + ga[r] * get(dh[r], c);
-        join<true, true>(A, H, E, before_A[c], before_H[c], behind_A[c], behind_E[c], p.lane);
+        float C = coefficient(A, B);
+        join<true, true>(C, H, E, before_A[c], before_H[c], behind_A[c], behind_E[c], p.lane);
         if (p.lane < ROW_LANES) {
-            maps[p.wave][0][p.lane * N + c] = A;
-            maps[p.wave][1][p.lane * N + c] = H;
-            maps[p.wave][2][p.lane * N + c] = E;
+            maps[p.wave][MAP_A][p.lane * N + c] = whole(C);
+            maps[p.wave][MAP_C][p.lane * N + c] = C;
+            maps[p.wave][MAP_H][p.lane * N + c] = H;
+            maps[p.wave][MAP_E][p.lane * N + c] = E;
         }
         __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
     if (SHARED) {
-        if (speaks && tile > 0) {
-            float A[N], E[N];
-#pragma unroll
-            for (int c = 0; c < N; ++c) {
-                A[c] = 1.f, E[c] = 0.f;
-#pragma unroll
-                for (int w = W - 1; w >= 0; --w) {
-                    const float m = maps[w][0][p.lane * N + c];
-                    E[c] = m * E[c] + maps[w][2][p.lane * N + c];
-                    A[c] *= m;
-                }
-                __builtin_amdgcn_sched_barrier(0);
-            }
-            tell(a, p, order, A, E);
-        }
+        if (p.wave == 0 && tile > 0) tell<MAP_E, MODE, W>(a, p, order, maps);
         if (order > 0) through_earlier<W>(carry, a, p, order, lds[SHARED ? 1 : 0]);
     }
     float e[N];
+    if (p.wave == 0 && tile == 0) {
 #pragma unroll
-    for (int w = W - 1; w >= 0; --w) {
-        if (w == p.wave)
+        for (int w = W - 1; w >= 0; --w) {
+            if (w == 0)
 #pragma unroll
-            for (int c = 0; c < N; ++c) e[c] = carry[c];
-        if (w > p.wave || (p.wave == 0 && tile == 0)) pass<2, W>(carry, maps, w, p);
+                for (int c = 0; c < N; ++c) e[c] = carry[c];
+            pass<MAP_C, MAP_E, W>(carry, maps, w, p);
+        }
+    } else {
+#pragma unroll
+        for (int c = 0; c < N; ++c) e[c] = carry[c];
+#pragma unroll
+        for (int w = W - 1; w > 0; --w)
+            if (w > p.wave) pass<MAP_A, MAP_E, W>(e, maps, w, p);
     }
 #pragma unroll
     for (int w = 0; w < W - 1; ++w)
-        if (w < p.wave) pass<1, W>(s, maps, w, p);
+        if (w < p.wave) pass<MAP_A, MAP_H, W>(s, maps, w, p);
     // the gates are computed again, channel by channel, and the gradients take the inputs' places: kept from above they would take 64 registers
 #pragma unroll
     for (int r = 0; r < R; ++r) asm("" : "+v"(g[r]), "+v"(x[r]), "+v"(dh[r]));

@@ -324,3 +324,66 @@ def test_one_step(ops, width, dtype):
     part = wide[:, 1:2, 1:width + 1]
     part.copy_(x)
     assert all(torch.equal(a, b) for a, b in zip(ops.recurrence(part, gate, state), ops.recurrence(x, gate, state)))
+
+
+STEADY = [-1.0, 0.0, 2.0, 5.0, 8.0, 9.1, 10.2, 11.5, 12.0, 13.3, 14.1]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("steps", [513, 8192, 32845])
+def test_steady_gates_add_nothing_up(ops, steps, dtype):
+    """A state of 1, inputs of 1 and gates that stay: all states are 1, and with gradients of 1 - a each step's is 1, however long the
+    sequence is.  In half units of fp32: a and b are off by less than 5 from their sum of 1 in each of a strip's sixteen steps, which go by a
+    alone; H and 1 - A differ by four at each of the 17 levels that join 129 tiles, and by 95 in a strip that forgets half (5 over 1 - a of
+    at least 1 / 20), of which as much again is left by the maps before; nine levels within a tile go by A alone, two each: 424 in all, below
+    2^-15.  The gates' own error, below
+    2^-18 for these, moves the gradients with it."""
+    print("case steady", steps, dtype, flush=True)
+    gate = torch.tensor(STEADY, device=DEV).to(dtype).expand(2, steps, len(STEADY))
+    x, state = torch.ones_like(gate), torch.ones(2, len(STEADY), device=DEV)
+    h, last, kept = ops.recurrence(x, gate, state)
+    for got, r in ((h, ref.R[dtype]), (last, 0.0), (kept, 0.0)):
+        off = (got.double() - 1).abs().amax(tuple(range(got.dim() - 1)))
+        assert (off <= 2.0 ** -15 + r).all(), off
+    b = 1 / (1 + torch.exp(ref.f64(gate[:, 0])))
+    dh = b.to(dtype).to(DEV)  # what its rounding makes of the gradients is known
+    unit = (ref.f64(dh) / b)[0].to(DEV)
+    dlast = (unit * (1 - b[0].to(DEV))).float().expand(2, -1).contiguous()
+    dx, _, dstate = ops.recurrence_backward(dh.unsqueeze(1).expand_as(x), x, gate, kept, dlast=dlast)
+    for got, want, r in ((dx, unit * b[0].to(DEV), ref.R[dtype]), (dstate, unit * (1 - b[0].to(DEV)), 0.0)):
+        off = (got.double() / want - 1).abs().amax(tuple(range(got.dim() - 1)))
+        assert (off <= 2.0 ** -15 + 2.0 ** -18 + r).all(), off
+
+
+@pytest.mark.parametrize("piece", [1, 7, 256])
+def test_steady_gates_add_nothing_up_over_calls(ops, piece):
+    """The same, token by token and in pieces, each from the state that the one before leaves; a piece is one level or three."""
+    gate = torch.tensor(STEADY, device=DEV).expand(2, piece, len(STEADY)).contiguous()
+    x, state = torch.ones_like(gate), torch.ones(2, len(STEADY), device=DEV)
+    for _ in range(2500):
+        h, state, _ = ops.recurrence(x, gate, state, keep=False)
+    assert ((h.double() - 1).abs() <= 2.0 ** -15).all() and ((state.double() - 1).abs() <= 2.0 ** -15).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("gate", [4.0, 12.0])
+def test_infinity_stays(ops, gate, dtype):
+    """An infinite state of a channel that remembers it stays one, and becomes a NaN only where the other infinity meets it; backward likewise."""
+    x = normal(torch.Generator().manual_seed(91), (2, 1300, 6), dtype)
+    g = torch.full_like(x, gate)
+    state = torch.zeros(2, 6, device=DEV)
+    state[0, 1], x[0, 300, 2], x[1, 40, 3], x[0, 20, 4], x[0, 900, 4] = -math.inf, math.inf, -math.inf, math.inf, -math.inf
+    want, _, kept = ops.recurrence(x, g, state)
+    bad = torch.zeros(2, 1300, 6, device=DEV)
+    bad[0, :, 1], bad[0, 300:, 2], bad[1, 40:, 3], bad[0, 20:900, 4] = -math.inf, math.inf, -math.inf, math.inf
+    bad[0, 900:, 4] = NAN
+    h = want.float()
+    assert torch.equal(torch.isnan(h), torch.isnan(bad))
+    assert torch.equal(torch.where(torch.isfinite(h), 0.0, h.nan_to_num(7.0, math.inf, -math.inf)), bad.nan_to_num(7.0, math.inf, -math.inf))
+    dh = normal(torch.Generator().manual_seed(92), x.shape, dtype)
+    dh[1, 700, 0], dh[0, 1299, 5] = math.inf, -math.inf
+    dx, _, dstate = ops.recurrence_backward(dh, torch.zeros_like(x), g, torch.zeros_like(kept))
+    assert (dx[1, :701, 0] == math.inf).all() and torch.isfinite(dx[1, 701:, 0].float()).all() and (dx[0, :, 5] == -math.inf).all()
+    assert dstate[1, 0] == math.inf and dstate[0, 5] == -math.inf and torch.isfinite(dstate).sum() == 10
+    token = ops.recurrence(x[:, :1], g[:, :1], state)[1]
+    assert token[0, 1] == -math.inf and torch.isfinite(token).sum() == 11
