@@ -387,3 +387,18 @@ def test_infinity_stays(ops, gate, dtype):
     assert dstate[1, 0] == math.inf and dstate[0, 5] == -math.inf and torch.isfinite(dstate).sum() == 10
     token = ops.recurrence(x[:, :1], g[:, :1], state)[1]
     assert token[0, 1] == -math.inf and torch.isfinite(token).sum() == 11
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shape", [(2, 40, 131), (2, 700, 66), (3, 1000, 1003), (1, 5000, 67)])
+def test_a_channel_s_place_changes_no_bit(ops, shape, dtype):
+    """Of a lane's two channels both are computed alike: shifted by one, and with an odd width, whose last but one is taken twice, a channel has the
+    same bits, in each run."""
+    x, gate, state = inputs(shape, dtype, 95)
+    dh = normal(torch.Generator().manual_seed(96), shape, dtype)
+    first = ops.recurrence(x, gate, state)
+    grads = ops.recurrence_backward(dh, x, gate, first[2])
+    for _ in range(5):
+        again = ops.recurrence(x[..., 1:], gate[..., 1:], state[:, 1:].contiguous())
+        more = ops.recurrence_backward(dh[..., 1:], x[..., 1:], gate[..., 1:], again[2])
+        assert all(torch.equal(a, b[..., 1:]) for a, b in zip((*again, *more), (*first, *grads)))
