@@ -402,3 +402,29 @@ def test_a_channel_s_place_changes_no_bit(ops, shape, dtype):
         again = ops.recurrence(x[..., 1:], gate[..., 1:], state[:, 1:].contiguous())
         more = ops.recurrence_backward(dh[..., 1:], x[..., 1:], gate[..., 1:], again[2])
         assert all(torch.equal(a, b[..., 1:]) for a, b in zip((*again, *more), (*first, *grads)))
+
+
+@pytest.mark.parametrize("steps", [1, 2, 300])
+def test_gates_to_all_bits(ops, steps):
+    """a and 1 - a of fp32 gates of all sizes, as they come out where the state, the input or the gradient is 1 and the others 0, are each off by
+    8 units of 2^-24 and a rounding at most, whatever the gate is; where fp32 does not hold them in full, by exp(-87.3365), 2^-125.99995: 1 / a stops there,
+    so that it is in range, and a b below 2^-126 may be 0."""
+    least = math.exp(-87.3365) * (1 + 9 * 2.0 ** -24)
+    gen = torch.Generator().manual_seed(101)
+    gate = torch.cat([torch.linspace(-100, 100, 4001), 20 * torch.randn(4000, generator=gen), torch.randn(4000, generator=gen)]).to(DEV)
+    C = gate.numel()
+    gates = gate.view(1, 1, C).expand(1, steps, C)
+    a, b = 1 / (1 + torch.exp(-ref.f64(gate))), 1 / (1 + torch.exp(ref.f64(gate)))
+    x = torch.zeros(1, steps, C, device=DEV)
+    x[:, 0] = 1
+    none, one = torch.zeros(1, C, device=DEV), torch.ones(1, C, device=DEV)
+    got_b = ops.recurrence(x, gates, none)[0][0, 0]
+    got_a = ops.recurrence(torch.zeros_like(x), gates, one)[0][0, 0]
+    dh = torch.zeros_like(x)
+    dh[:, 0] = 1  # (of a step in the middle the sum behind it is 0 likewise)
+    dx, _, dstate = ops.recurrence_backward(dh, torch.zeros_like(x), gates, torch.zeros(1, -(-steps // 256), C, device=DEV))
+    for got, want, name in ((got_b, b, "b"), (got_a, a, "a"), (dx[0, 0], b, "dx"), (dstate[0], a, "dstate")):
+        off = (ref.f64(got) - want).abs()
+        worst = ((off - least).clamp(min=0) / want).max().item() * 2 ** 24
+        print("steps %d %s: %.2f units" % (steps, name, worst), flush=True)
+        assert (off <= 9 * 2.0 ** -24 * want + least).all(), name
