@@ -215,7 +215,7 @@ typedef struct {
  * launch would have 2^32 threads or more: 512 for every 64 channels of every 256 steps of a sequence. */
 int dear_recurrence(const dear_recurrence_t *args, void *hip_stream);
 int dear_recurrence_backward(const dear_recurrence_t *args, void *hip_stream);
-/* Bytes of workspace that either call with these sizes needs (pointers and strides are not looked at). */
+/* Bytes of workspace that either call with these sizes needs (pointers and strides are not looked at); DEAR_ETOOBIG as above. */
 int dear_recurrence_workspace(const dear_recurrence_t *args, int64_t *bytes);
 
 /* ---------------------------------------------------------------------------------

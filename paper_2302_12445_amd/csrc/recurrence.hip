@@ -565,10 +565,19 @@ int check(const dear_recurrence_t *r) {
     return DEAR_OK;
 }
 
+// Whether a launch would have more threads than it takes.  Asked by division, as products of the sizes may pass 64 bits; what is below the limit,
+// workspaces among it, stays far from that.
+bool too_many(const dear_recurrence_t &r) {
+    if (r.batch == 0 || r.steps == 0) return false;
+    return groups_of(r) * ceil_div(r.steps, KEPT) > MAX_THREADS / (64 * WAVES) / r.batch;
+}
+
 // A tensor of the structure, which is read or, where it is written, has a place of its own for each element.
 int check_tensor(const dear_recurrence_t &r, const dear_steps_t &t, bool written) {
     if (!t.data || t.batch_stride < 0 || t.step_stride < 0) return DEAR_EINVAL;
     if (r.steps > 1 && t.step_stride >= MAX_STEP_STRIDE) return DEAR_ETOOBIG;
+    const int64_t sequence = r.width + (r.steps > 1 ? (r.steps - 1) * t.step_stride : 0);
+    if (r.batch > 1 && t.batch_stride > (INT64_MAX / 4 - sequence) / (r.batch - 1)) return DEAR_EINVAL;  // (4 bytes an element)
     if (written) {
         const int64_t batch = r.batch, steps = r.steps;
         const bool by_batch = t.batch_stride >= t.step_stride;  // which of the axes lies further apart
@@ -597,6 +606,7 @@ bool vectors(const dear_recurrence_t &r, const dear_steps_t &t) {
 int check_call(const dear_recurrence_t *r, bool backward) {
     if (int rc = check(r)) return rc;
     if (r->batch == 0) return DEAR_OK;
+    if (too_many(*r)) return DEAR_ETOOBIG;
     if (!aligned(r->lens, 4) || !aligned(r->state, 4) || !aligned(r->last, 4) || !aligned(r->kept, 4) || !aligned(r->dlast, 4) ||
         !aligned(r->dstate, 4))
         return DEAR_EALIGN;
@@ -615,7 +625,6 @@ int check_call(const dear_recurrence_t *r, bool backward) {
         if (need && !r->workspace) return DEAR_EINVAL;
         if (need && !aligned(r->workspace, 256)) return DEAR_EALIGN;
         if (need > r->workspace_bytes) return DEAR_ETOOBIG;
-        if (r->batch * groups_of(*r) * ceil_div(r->steps, KEPT) * 64 * WAVES > MAX_THREADS) return DEAR_ETOOBIG;
     }
     return DEAR_OK;
 }
@@ -708,6 +717,7 @@ int dear_recurrence_backward(const dear_recurrence_t *args, void *hip_stream) { 
 int dear_recurrence_workspace(const dear_recurrence_t *args, int64_t *bytes) {
     if (!bytes) return DEAR_EINVAL;
     if (int rc = check(args)) return rc;
+    if (too_many(*args)) return DEAR_ETOOBIG;
     *bytes = workspace_of(*args);
     return DEAR_OK;
 }

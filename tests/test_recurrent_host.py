@@ -116,6 +116,30 @@ def test_recurrence_workspace():
     assert f(recurrence(), None) == EINVAL and f(None, C.byref(n)) == EINVAL and f(recurrence(width=0), C.byref(n)) == EINVAL
 
 
+@pytest.mark.parametrize("batch,width,steps", [
+    (1 << 30, 1 << 20, 1 << 27), ((1 << 31) - 1, 1 << 24, 1 << 30), (1 << 24, 1 << 22, 1 << 30), (1 << 28, 1 << 22, 1 << 30), (1, 1 << 24, 1 << 23),
+    ((1 << 31) - 1, 64, 1), (1 << 17, 1 << 12, 256), (1 << 30, (1 << 21) + 64, 1 << 27)])
+def test_recurrence_refuses_sizes_whose_products_pass_64_bits(batch, width, steps):
+    """Workgroups, and bytes of workspace, of more than a launch has threads, also where their number, or its bits below 2^64, would fit."""
+    lib, n, step = ops.load_library(), C.c_int64(-1), min(width, (1 << 22) - 1)
+    change = dict(batch=batch, width=width, steps=steps, workspace_bytes=(1 << 63) - 1)
+    assert lib.dear_recurrence_workspace(recurrence(**change), C.byref(n)) == ETOOBIG and n.value == -1
+    if width < 1 << 22:  # (outputs that are wider than steps lie apart have no places of their own)
+        tensors = {name: (SPACE, steps * step, step) for name in ("x", "gate", "h", "dh", "dx", "dgate")}
+        assert lib.dear_recurrence(recurrence(**change, **tensors), None) == ETOOBIG
+        assert lib.dear_recurrence_backward(recurrence(**change, **tensors), None) == ETOOBIG
+
+
+def test_recurrence_refuses_tensors_that_pass_64_bits():
+    lib = ops.load_library()
+    for batch, stride in ((3, 1 << 62), (2, (1 << 63) - 1), (5, 1 << 61), (1 << 20, 1 << 45)):
+        far = (SPACE, stride, 64)
+        for name in ("x", "gate", "h"):
+            assert lib.dear_recurrence(recurrence(batch=batch, **{name: far}), None) == EINVAL, (name, batch, stride)
+        for name in ("x", "gate", "dh", "dx", "dgate"):
+            assert lib.dear_recurrence_backward(recurrence(batch=batch, **{name: far}), None) == EINVAL, (name, batch, stride)
+
+
 BAD_EXPERTS = [
     (dict(rows=-1), EINVAL), (dict(rows=1 << 31), EINVAL), (dict(experts=0), EINVAL), (dict(experts=(1 << 16) + 1), EINVAL),
     (dict(outs=0), EINVAL), (dict(ins=0), EINVAL), (dict(outs=(1 << 20) + 1), EINVAL), (dict(ins=(1 << 20) + 1), EINVAL),
