@@ -79,7 +79,8 @@ class _Recurrence(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, gate, state, lens, keep):
         h, last, kept = ops.recurrence(x, gate, state, lens, keep=keep)
-        ctx.save_for_backward(x, gate, kept, lens, state)
+        # nothing is computed from the state: where it has a gradient, that is tied to it
+        ctx.save_for_backward(x, gate, kept, lens, state if ctx.needs_input_grad[2] else None)
         ctx.set_materialize_grads(False)
         return h, last
 
@@ -93,7 +94,7 @@ class _Recurrence(torch.autograd.Function):
             dh = torch.zeros_like(x)
         grads = ops.recurrence_backward(dh, x, gate, kept, lens, None if dlast is None else dlast.contiguous())
         dx, dgate, dstate = _first_order(grads, *given, x, gate, state)
-        return dx, dgate, dstate if state is not None else None, None, None
+        return dx, dgate, dstate if ctx.needs_input_grad[2] else None, None, None
 
 
 def recur(x: torch.Tensor, gate: torch.Tensor, state: Optional[torch.Tensor] = None, lens: Optional[torch.Tensor] = None

@@ -131,6 +131,25 @@ def test_what_is_not_asked_for_is_not_made(plain):
     assert plain == ["recurrence_backward"]
 
 
+def test_a_state_carried_in_place(plain):
+    """A buffer of states that takes no gradient may be written over before the backward pass, which does not read it, and is not kept alive
+    by it; a state that has a gradient has to stay, as an input of it."""
+    x, gate, buffer = leaf(2, 5, 3), leaf(2, 5, 3, seed=1), leaf(2, 3, seed=2).detach()
+    want = torch.autograd.grad(layers.recur(x, gate, buffer.clone())[0].sum(), (x, gate))
+    h, last = layers.recur(x, gate, buffer)
+    buffer.copy_(last.detach())
+    assert all(torch.equal(p, q) for p, q in zip(torch.autograd.grad(h.sum(), (x, gate)), want))
+    state = leaf(2, 3, seed=3).detach()
+    h, _ = layers.recur(x, gate, state)
+    seen = weakref.ref(state)
+    del state
+    gc.collect()
+    assert seen() is None
+    start = leaf(2, 3, seed=4)
+    h, _ = layers.recur(x, gate, start)
+    assert torch.autograd.grad(h.sum(), start)[0].shape == start.shape
+
+
 def test_graphs_are_freed(plain):
     x, gate = leaf(2, 5, 3), leaf(2, 5, 3, seed=1)
     h, last = layers.recur(x * 1, gate * 1)
