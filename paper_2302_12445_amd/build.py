@@ -20,7 +20,8 @@ OPS_SOURCES = [os.path.join(CSRC, f) for f in ("attention.hip", "norm.hip", "wei
 # accumulators of 16 values stay whole where control flow meets: taken apart into single values, as the compiler would
 # by its own measure, they are copied one by one in every step (attention's dk and dv: 48 spilled registers, and none so)
 OPS_FLAGS = ["-mllvm", "-amdgpu-codegenprepare-break-large-phis=false"]
-OPS_HEADERS = [os.path.join(CSRC, "ops_common.h"), os.path.join(ROOT, "include", "dear_ops.h"), os.path.join(ROOT, "include", "dear.h")]
+OPS_HEADERS = [os.path.join(CSRC, "ops_common.h"), os.path.join(CSRC, "ops_sizes.h"), os.path.join(CSRC, "experts_cut.h"),
+               os.path.join(ROOT, "include", "dear_ops.h"), os.path.join(ROOT, "include", "dear.h")]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-shared",

@@ -9,9 +9,9 @@
 //
 // Matrix instructions bound large calls, at the clock that the card's power leaves them (16384 rows, 4096 x 1024 over 8, bf16: 1000 to 1200
 // TFLOP/s, a library's product of 8192 x 8192 x 8192 1394); the weights' way from memory bounds few rows (32: 4.5 TB/s).
-#include <cmath>
 #include <type_traits>
 
+#include "experts_cut.h"
 #include "ops_common.h"
 
 #pragma clang fp contract(fast)
@@ -19,8 +19,6 @@
 namespace {
 
 using namespace dear_ops;
-
-enum product { LINEAR, INPUT_GRAD, WEIGHT_GRAD };
 
 struct params {
     const void *a, *b;  // operands of the outputs' rows and columns
@@ -112,9 +110,6 @@ __device__ __forceinline__ part rows_of(const params &p, int32_t expert) {
 }
 
 // ------------------------------------------------------------------------------------ any type, any size
-constexpr int THREADS = 256;
-constexpr int BB = 128;  // outputs' columns of a workgroup
-
 // An operand's part of a step on its way from memory to LDS, in pieces of 16 bytes: OUT rows of BS values along the summed index or, ACROSS
 // it, BS rows of OUT values.  Values beyond the sum are zeros in both operands, so that nothing that stands there counts; rows and columns
 // beyond the outputs are whatever is there, and not stored.  No load has a branch of its own, which would wait for the one before: pieces
@@ -297,8 +292,6 @@ template <typename T> __global__ __launch_bounds__(256) void parts_sum_kernel(co
 // instruction has to be issued beside them: fragments of a quarter step are read while those of the one before are multiplied, across the
 // barrier of a step too, and memory fills one half of LDS by itself while the other is read.  Workgroups stay for several tiles: the first
 // step of the next tile is loaded beside the last one of this, and sums are stored beside the loads of the second.
-constexpr int WS = 64;          // summed index of a step
-constexpr int CUS = 256;
 constexpr int TABLE = 1024;     // experts that the table in LDS has places for
 
 // An operand's step in LDS, for SIZE outputs that WAYS groups of waves have a part of each.  Along the summed index: SIZE rows of 64 values,
@@ -826,7 +819,7 @@ template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_k
     fill<KIND, 256>(table, p);
     const unsigned b_tiles = (unsigned)p.b_tiles, a_tiles = KIND == WEIGHT_GRAD ? (unsigned)p.a_tiles : (unsigned)uniform(table.upto[p.experts - 1]);
     const unsigned per = a_tiles * b_tiles, items = KIND == WEIGHT_GRAD ? per * p.experts : per, over = items % CUS;
-    const unsigned whole = over <= CUS / 2 ? items - over : items;
+    const unsigned whole = over <= MOST_IN_QUARTERS ? items - over : items;
     if (KIND != WEIGHT_GRAD) zero_rows(p, (bf16 *)p.out, uniform(table.ends[p.experts - 1]), p.rows);
     auto xa = (DEAR_LDS char *)a0, ya = (DEAR_LDS char *)b0, xb = (DEAR_LDS char *)a1, yb = (DEAR_LDS char *)b1;
     unsigned round = 0;
@@ -848,7 +841,7 @@ template <int KIND> __global__ __launch_bounds__(THREADS, 1) void experts_wide_k
     if (whole == items) return;
     __syncthreads();
     if constexpr (KIND != WEIGHT_GRAD) {
-        if (over <= CUS / 16) {
+        if (over <= MOST_SMALL) {
             constexpr int A = 32 * WS * 2;
             DEAR_LDS char *const x[4] = {xa, xb, ya, yb}, *const y[4] = {xa + A, xb + A, ya + A, yb + A};
             unsigned item = blockIdx.x;
@@ -933,100 +926,12 @@ bool vectors(const dear_experts_t &x, const void *p, int64_t stride, int64_t wid
     return aligned(p, 16) && stride * n % 16 == 0 && width * n % 16 == 0;
 }
 
-// How a call's outputs are cut: tiles of 256 (WIDE), tiles of 32 or 128 rows that memory fills directly, with two steps under way (RING32, RING128) or
-// with one and two workgroups a CU (FEW128), or tiles whose operands go through registers (ANY32, ANY64, ANY128); and the splits of the
-// summed index.
-enum cut { WIDE, RING32, RING128, FEW128, ANY32, ANY64, ANY128 };
-struct choice {
-    cut how;
-    int splits;
-    double us;
-};
-
 // Whether memory can fill tiles directly: bf16 in whole vectors, with rows that 32-bit offsets reach.
 template <int KIND> bool direct(const dear_experts_t &x, bool vec, const params &p) {
     const int64_t most = 1 << 22;
     if (x.dtype != DEAR_BF16 || !vec || !aligned(p.out, 16) || x.experts > TABLE || p.n_b % 8 || p.a_stride >= most || p.b_stride >= most) return false;
     const int64_t a_tiles = KIND == WEIGHT_GRAD ? ceil_div(x.outs, 256) * x.experts : x.rows / 32 + x.experts;
     return a_tiles * ceil_div(p.n_b, 128) <= INT32_MAX / 64;
-}
-
-// Tiles of n rows that the experts are expected to have: half of each one's last is empty.
-double row_tiles(const dear_experts_t &x, int n) {
-    const double used = (double)(x.experts < x.rows ? x.experts : x.rows), tiles = (double)x.rows / n + used / 2;
-    return tiles < used ? used : tiles;
-}
-
-// The cut and splits of the least time by this estimate, in microseconds.  A CU takes `resident` workgroups at a time; a step of 64 of the summed
-// index takes each `alone` as long as loads are what it waits for, and a `share` of the CU, or of what the caches give it, when there are more;
-// all weights take their way from memory, a part of which tiles of 256 and those that begin and end at other times leave unused.  Several
-// splits' sums are written, read, eight at a time, and added, 4 TB/s, in another launch.  Tiles of 256 fill the chip once each and are not
-// split; their last round goes in smaller ones where it is no more than half full.  Measured, microseconds, over 8 experts, 4096 x 1024, tiles
-// of 256, and RING32, RING128 and FEW128: 32 rows 34, 15, 16 and 20, 1024 rows 37, 32, 21 and 25, 2048 rows -, 53, 32 and 39, 4096 rows 36,
-// 95, 55 and 50; over 64, 1024 x 1024, 4096 rows 41, 53, 37 and 33.  The input gradient's in one split and four: 32 rows RING32 33 and 19,
-// RING128 41 and 20, 1024 rows 40 and 47, 45 and 29, 4096 rows in one, tiles of 256 64 and RING128 54.
-choice choose(const dear_experts_t &x, bool is_direct, int64_t sum, int64_t columns) {
-    const double steps = (double)ceil_div(sum, WS), size = x.dtype == DEAR_F32 ? 4 : 2;
-    const double weights = (double)(x.experts < x.rows ? x.experts : x.rows) * (double)sum * (double)columns * size / 5.8e6;
-    choice best = {ANY128, 1, 0};
-    auto take = [&](cut how, int n, double us, bool at_once) {
-        const double least = weights * (how == WIDE ? 1.5 : at_once && how <= RING128 ? 1 : 1.2);
-        us = us > least ? us : least;
-        us += 4 + (n == 1 ? 0 : 1.5 + 1.5 * (double)ceil_div(n, 8) + (double)(n + 1) * (double)x.rows * (double)columns * 4 / 4e6);
-        if (best.us == 0 || us < best.us) best = {how, n, us};
-    };
-    auto splits = [&](cut how, int ba, double resident, double begin, double alone, double share) {
-        const double tiles = row_tiles(x, ba) * (double)ceil_div(columns, BB);
-        const int64_t upper = (x.rows / ba + x.experts + 1) * ceil_div(columns, BB);
-        for (int64_t n = 1; n <= 32 && (n == 1 || (n * 2 * WS <= sum && upper * n * THREADS <= MAX_THREADS && x.rows * columns <= MAX_THREADS)); ++n) {
-            const double a_cu = std::ceil(tiles * n / CUS), each = std::ceil(steps / n);
-            const double wait = std::ceil(a_cu / resident) * (begin + each * alone), work = a_cu * each * share;
-            take(how, (int)n, wait > work ? wait : work, a_cu <= 1);
-        }
-    };
-    const bool f32 = x.dtype == DEAR_F32;
-    if (is_direct) {
-        splits(RING32, 32, 2, 1, 0.45, 0.42);
-        splits(FEW128, 128, 2, 3, 0.85, 0.6);
-        splits(RING128, 128, 1, 1, 0.7, 0.7);
-        const double tiles = std::ceil(row_tiles(x, 256)) * (double)ceil_div(columns, 256), rounds = std::floor(tiles / CUS), over = tiles - rounds * CUS;
-        take(WIDE, 1, 3 + steps * 1.5 * (rounds + (over > CUS / 2 ? 1 : over > CUS / 16 ? 0.5 * std::ceil(4 * over / CUS) : over > 0 ? 0.3 : 0)), false);
-    } else {
-        splits(ANY32, 32, f32 ? 3 : 6, 3, f32 ? 2.6 : 1.4, f32 ? 1.2 : 0.7);
-        splits(ANY64, 64, f32 ? 4 : 5, 3, f32 ? 3.2 : 1.4, f32 ? 2.0 : 0.7);
-        splits(ANY128, 128, 3, 3, f32 ? 4.6 : 1.4, f32 ? 3.6 : 0.7);
-    }
-    return best;
-}
-
-// Of a weight gradient, by a like estimate, with the rows shared out evenly: tiles of 256 where an expert has more than a few steps, or of 128
-// in splits of each expert's rows.  Measured, microseconds, tiles of 256, and of 128 in one, four and sixteen splits: 16384 rows, 4096 x 1024 over
-// 8 123, 208, 405 and 1074, 1024 x 1024 over 8 50, 53, 99 and 275; 30000 rows, 1024 x 1024 over 2 146, 255, 102 and 132; 16000 rows, 512 x 512
-// of one 140, 269, 73 and 30, 100 x 100 over 4 -, 81, 26 and 13; 500 rows, 4096 x 1024 over 8 33 and 28; fp32 16384 rows, 128 x 64 over 8 -, 157,
-// 45 and 18.
-choice choose_weight_grad(const dear_experts_t &x, bool is_direct) {
-    const bool f32 = x.dtype == DEAR_F32;
-    const int64_t rows = ceil_div(x.rows, x.experts);
-    const double steps = (double)ceil_div(rows, WS), outputs = (double)x.experts * x.outs * x.ins, written = outputs * 4 / 4e6;
-    auto tiles = [&](int n) { return (double)x.experts * (double)(ceil_div(x.outs, n) * ceil_div(x.ins, n)); };
-    choice best = {ANY128, 1, 0};
-    for (int64_t n = 1; n <= 32 && (n == 1 || (n * 2 * WS <= rows && tiles(128) * n * THREADS <= MAX_THREADS && outputs <= MAX_THREADS)); ++n) {
-        const double a_cu = std::ceil(tiles(128) * n / CUS), each = std::ceil(steps / n), resident = f32 ? 2 : 3;
-        const double wait = std::ceil(a_cu / resident) * (3 + each * (f32 ? 4.6 : 1.3)), work = a_cu * each * (f32 ? 3.6 : 0.7);
-        const double us = (wait > work ? wait : work) + (n == 1 ? written : 3 + (2 * n + 1) * written);
-        if (n == 1 || us < best.us) best = {ANY128, (int)n, us};
-    }
-    if (is_direct && rows >= 2 * WS) {
-        const double rounds = std::floor(tiles(256) / CUS), over = tiles(256) - rounds * CUS;
-        const double us = 3 + steps * 1.5 * (rounds + (over > CUS / 2 ? 1 : 0.45 * std::ceil(4 * over / CUS))) + written / 2;
-        if (us <= best.us) best = {WIDE, 1, us};
-    }
-    return best;
-}
-
-template <int KIND> choice choose_cut(const dear_experts_t &x, bool is_direct) {
-    if (KIND == WEIGHT_GRAD) return choose_weight_grad(x, is_direct);
-    return KIND == LINEAR ? choose(x, is_direct, x.ins, x.outs) : choose(x, is_direct, x.outs, x.ins);
 }
 
 template <int KIND> int64_t workspace_of(const dear_experts_t &x) {

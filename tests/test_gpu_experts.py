@@ -10,6 +10,7 @@ import pytest
 import torch
 
 sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import experts_cases  # noqa: E402
 import ops_reference as ref  # noqa: E402
 import recurrent_reference as rec  # noqa: E402
 
@@ -128,6 +129,14 @@ def test_many_rows_of_few_outputs(ops, outs, ins, dtype):
 def test_long_sums_of_any_width(ops, counts, outs, ins):
     """Sums beyond 1024 in rows that start anywhere."""
     check(ops, *make(counts, 3, outs, ins, BF16, 46))
+
+
+@pytest.mark.parametrize("case", range(len(experts_cases.CASES)))
+def test_each_way(ops, case):
+    """At sizes that take each way that there is (the host's choice is checked on the CPU)."""
+    counts, spare, outs, ins, dtype, *ways = experts_cases.CASES[case]
+    print("case", len(counts), sum(counts), spare, outs, ins, dtype, ways, flush=True)
+    check(ops, *make(counts, spare, outs, ins, {"bf16": BF16, "f32": F32}[dtype], 60 + case))
 
 
 @pytest.mark.parametrize("outs, ins", [(136, 1000), (1000, 136)])
