@@ -260,8 +260,9 @@ int dear_expert_weight_grad_workspace(const dear_experts_t *args, int64_t *bytes
  * The norm over the gradients of all tensors of a list, and the gradients scaled down to a largest norm:
  *     norm = sqrt(sum of g^2 over all elements of all tensors)
  *     out = g * min(1, max_norm / norm), rounded to out_dtype
- * Squares are added in 64 bits (those of bf16 first by eights in fp32, where it holds them), norm is rounded to fp32 once.  A NaN or an infinity among the gradients makes the norm one;
- * with a norm of NaN every out is NaN, with an infinite one finite gradients become 0 and infinite ones NaN.
+ * Squares are added in 64 bits (those of bf16 first by eights in fp32, where it holds them), norm is rounded to fp32 once, and the factor is that of
+ * the norm before it is rounded: one that fp32 does not hold is said to be infinite, and clips by what it is.  A NaN or an infinity among the gradients
+ * makes the norm one; with a norm of NaN every out is NaN, with an infinity finite gradients become 0 and infinite ones NaN.
  */
 typedef struct {
     const void *data;        /* elements in a row, without gaps; aligned to their type           */

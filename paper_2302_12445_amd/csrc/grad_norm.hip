@@ -173,20 +173,29 @@ template <typename T, typename O> __device__ __forceinline__ void scale(const T 
     if (i < n)
         for (int k = 0; k < V - 1 && i + k < n; ++k) o[i + k] = (O)((float)p[i + k] * by);
 }
+// By a factor that fp32 does not hold in full: gradients near the largest number, scaled to a norm of 1, which is too rare to be fast.
+template <typename T, typename O> __device__ __forceinline__ void scale(const T *p, O *o, int64_t n, double by) {
+#pragma unroll 1
+    for (int64_t i = threadIdx.x; i < n; i += THREADS) o[i] = (O)(float)((double)(float)p[i] * by);
+}
 
 template <bool HERE>
 __global__ __launch_bounds__(THREADS) void scale_kernel(const table t, const entry *far, const double *parts, int n, float max_norm, float *norm) {
     const double whole = norm_of(parts, n);
     if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)whole;
     const bool clip = !(whole <= (double)max_norm);  // (a NaN clips, so that it shows in every gradient)
-    const float by = clip ? (float)((double)max_norm / whole) : 1.f;
-    each<HERE>(t, far, [&](const entry &e, int64_t first, int64_t count) {
-        if (!clip && e.in == e.out) return;  // is what it is to be
-        if (e.bf16s == 0) scale((const float *)e.in + first, (float *)e.out + first, count, by);
-        else if (e.bf16s == 1) scale((const bf16 *)e.in + first, (float *)e.out + first, count, by);
-        else if (e.bf16s == 2) scale((const float *)e.in + first, (bf16 *)e.out + first, count, by);
-        else scale((const bf16 *)e.in + first, (bf16 *)e.out + first, count, by);
-    });
+    const double by = clip ? (double)max_norm / whole : 1.;
+    auto scale_all = [&](auto by) {
+        each<HERE>(t, far, [&](const entry &e, int64_t first, int64_t count) {
+            if (!clip && e.in == e.out) return;  // is what it is to be
+            if (e.bf16s == 0) scale((const float *)e.in + first, (float *)e.out + first, count, by);
+            else if (e.bf16s == 1) scale((const bf16 *)e.in + first, (float *)e.out + first, count, by);
+            else if (e.bf16s == 2) scale((const float *)e.in + first, (bf16 *)e.out + first, count, by);
+            else scale((const bf16 *)e.in + first, (bf16 *)e.out + first, count, by);
+        });
+    };
+    if (by < 0x1p-126) scale_all(by);
+    else scale_all((float)by);
 }
 
 // ------------------------------------------------------------------------------------ host

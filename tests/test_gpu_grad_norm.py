@@ -119,6 +119,18 @@ def test_magnitudes(ops, scale):
     check(ops, [g], scale / 8)
 
 
+@pytest.mark.parametrize("max_norm", [1e-30, 1e-3, 1.0, 1e4])
+@pytest.mark.parametrize("scale", [1e33, 2e36, 6e37])
+def test_factors_that_fp32_does_not_hold(ops, scale, max_norm):
+    """Norms so far above the largest one that their ratio has few bits in fp32, or none: what is scaled has all of its own."""
+    gen = torch.Generator().manual_seed(9)
+    for kinds in ((F32, F32), (BF16, F32), (F32, BF16), (BF16, BF16)):
+        print("case", scale, max_norm, kinds, flush=True)
+        grads = [normal(gen, (n,), kinds[0], scale) for n in (4097, 3, 20000)]
+        assert all(torch.isfinite(g).all() for g in grads)
+        check(ops, grads, max_norm, [torch.empty(g.numel(), dtype=kinds[1], device=DEV) for g in grads])
+
+
 def test_not_finite(ops):
     gen = torch.Generator().manual_seed(6)
     a, b = normal(gen, (5000,)), normal(gen, (300,), BF16)
