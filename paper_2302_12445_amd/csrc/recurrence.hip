@@ -55,8 +55,7 @@ struct params {
 // four roundings); where gates are bf16 that would cost 5 % of the time (2 x 8192 x 1024 forward 29.2 us, so 30.6, of fp32 56.5 and 57.4), and results of
 // bf16 are rounded by 2^15 units.  Where fp32 has no more: below gates of -87.3, where t stops so that 1 + t has a reciprocal, a is some 2^-126, and above
 // 87.3 b may be 0.  A NaN stays one.
-template <typename T> __device__ __forceinline__ void gates(float g, float &a, float &b) {
-    float t;
+template <typename T> __device__ __forceinline__ void gates(float g, float &a, float &b, float &t) {
     if (sizeof(T) == 4) {
         const float f = __builtin_elementwise_maximum(__builtin_elementwise_minimum(g, 128.f), -87.3365f), y = f * -0x1.715476p+0f;
         const float r = __builtin_fmaf(y, 0x1.05c61p-29f, __builtin_fmaf(y, -0x1.62e43p-1f, -f));
@@ -67,6 +66,10 @@ template <typename T> __device__ __forceinline__ void gates(float g, float &a, f
     }
     a = __builtin_amdgcn_rcpf(1.f + t);
     b = t * a;
+}
+template <typename T> __device__ __forceinline__ void gates(float g, float &a, float &b) {
+    float t;
+    gates<T>(g, a, b, t);
 }
 
 // The halves' values of x: the earlier strip's and the later one's.
@@ -79,33 +82,39 @@ __device__ __forceinline__ void halves(float x, float &earlier, float &later) {
 // What a map keeps of the state, A, is told on as one number C: A itself below a half, from there on -(1 - A), with the sign, by which the state
 // goes on as s + (H - (1 - A) s).  An A near 1 that is rounded by itself is wrong by the same 2^-25 each time that a gate stays, which adds up over
 // all that a channel remembers, to 2^-25 / (1 - a) (of fp32 steps with a gate of 9, 4e-4); by C the state goes to where H and 1 - A say, however
-// long the sequence is.  So go states from tile to tile and from call to call (2 x 8192 x 1024 bf16 forward 27.9 us, so 29.4); within a tile, from a
+// long the sequence is.  So go states from tile to tile and from call to call (2 x 8192 x 1024 bf16 forward 27.5 us, so 28.4); within a tile, from a
 // state that is at hand, they go by A.  -0 leaves a state as it is.
 __device__ __forceinline__ float coefficient(float A, float B) { return B <= 0.5f ? -B : A; }
 __device__ __forceinline__ bool by_complement(float C) { return (int32_t)__float_as_uint(C) < 0; }
 __device__ __forceinline__ float whole(float C) { return by_complement(C) ? 1.f + C : C; }
+__device__ __forceinline__ float complement(float C) { return by_complement(C) ? -C : 1.f - C; }
 // (An infinite state stays one: only what is subtracted is kept finite.)
 __device__ __forceinline__ float through(float C, float H, float s) {
     const bool less = by_complement(C);
     const float t = less ? __builtin_amdgcn_fmed3f(s, -FLT_MAX, FLT_MAX) : s;
     return __builtin_fmaf(C, t, H) + (less ? s : 0.f);
 }
-// A and B = 1 - A of several stretches in a row, in either order.
+// A, B = 1 - A and H of several stretches in a row (or A, B and E from the last to the first).  H, which starts from 0, goes by A: it is off by a
+// rounding a stretch, whatever the state is.
 struct stretches {
-    float A = 1.f, B = 0.f;
-    __device__ __forceinline__ void add(float C) {
-        B += A * (by_complement(C) ? -C : 1.f - C);
-        A *= whole(C);
+    float A = 1.f, B = 0.f, H = 0.f;
+    __device__ __forceinline__ void add(float A1, float B1, float H1) {
+        H = A1 * H + H1;
+        B += A * B1;
+        A *= A1;
     }
 };
 
-// Joins the strips of a wave.  C, H, E: the map of the lane's strip, which becomes the wave's.  before: the map from the wave's first step to
-// the strip's, behind: backward from the wave's last step to the strip's, by A.
+// Joins the strips of a wave.  q: of a strip 1 / A is the product of its 1 + t, and q what that is above 1, q = (1 + t) q + t from step to step: a sum
+// of nothing below 0, out of which A and, where it is near 1, B = 1 - A come as exactly as it is.  (A large q has no inverse that fp32 holds, or is
+// infinite, or 0 of that and so a NaN: A is 0 there.)  H and E become the wave's.  before: the map from the wave's first step to the strip's, behind:
+// backward from the wave's last step to the strip's, by A.
 template <bool FORWARD, bool BACKWARD>
-__device__ __forceinline__ void join(float &C, float &H, float &E, float &before_A, float &before_H, float &behind_A, float &behind_E, int lane) {
-    float C0, C1;
-    halves(C, C0, C1);
-    const float A0 = whole(C0), A1 = whole(C1);
+__device__ __forceinline__ void join(float q, float &A, float &B, float &H, float &E, float &before_A, float &before_H, float &behind_A, float &behind_E,
+                                     int lane) {
+    float q0, q1;
+    halves(q, q0, q1);
+    const float A0 = __builtin_amdgcn_rcpf(1.f + q0), A1 = __builtin_amdgcn_rcpf(1.f + q1);
     const bool later = lane & 32;
     if (FORWARD) {
         float H0, H1;
@@ -121,8 +130,9 @@ __device__ __forceinline__ void join(float &C, float &H, float &E, float &before
         behind_E = later ? 0.f : E1;
         E = A0 * E1 + E0;
     }
-    const float B = -C0 - C1 * A0;  // 1 - A0 A1, where both are held by 1 - A
-    C = by_complement(C0) && by_complement(C1) && B <= 0.5f ? -B : A0 * A1;
+    A = A0 * A1;
+    const float all = q1 * (1.f + q0) + q0;
+    B = all <= 1.f ? all * A : 1.f - A;
 }
 
 // How a lane's N channels lie in memory.
@@ -228,17 +238,31 @@ template <int MODE> __device__ __forceinline__ void store_state(float *row, cons
     store<float, MODE>((char *)row, 0, f32x2{s[0], s[1]}, col, cols);
 }
 
-// The map of a tile's steps before the last wave has been joined: each wave's in LDS, [wave][A, C, H or E][channel].
-enum { MAP_A, MAP_C, MAP_H, MAP_E };
+// The map of a tile's steps before the last wave has been joined: each wave's in LDS, [wave][A, 1 - A, H or E][channel].
+enum { MAP_A, MAP_B, MAP_H, MAP_E };
 template <int W> struct wave_maps_of { typedef float type[W][4][CG] __attribute__((aligned(16))); };
 template <int W> using wave_maps = typename wave_maps_of<W>::type;
 
-// s through a wave's map, of H or E: by C, or within a tile by A alone, as in a strip.  One wave's after another, as all of them at once take registers.
-template <int BY, int WHICH, int W> __device__ __forceinline__ void pass(float *s, const wave_maps<W> &maps, int w, const place &p) {
-    const f32x2 M = *(const f32x2 *)&maps[w][BY][p.lane % ROW_LANES * N], H = *(const f32x2 *)&maps[w][WHICH][p.lane % ROW_LANES * N];
+// s through a wave's map, of H or E, within a tile: by A alone, as in a strip.  One wave's after another, as all of them at once take registers.
+template <int WHICH, int W> __device__ __forceinline__ void pass(float *s, const wave_maps<W> &maps, int w, const place &p) {
+    const f32x2 A = *(const f32x2 *)&maps[w][MAP_A][p.lane % ROW_LANES * N], H = *(const f32x2 *)&maps[w][WHICH][p.lane % ROW_LANES * N];
 #pragma unroll
-    for (int c = 0; c < N; ++c) s[c] = BY == MAP_C ? through(M[c], H[c], s[c]) : M[c] * s[c] + H[c];
+    for (int c = 0; c < N; ++c) s[c] = A[c] * s[c] + H[c];
     __builtin_amdgcn_sched_barrier(0);
+}
+// s through all waves' maps, joined before.
+template <int WHICH, int W> __device__ __forceinline__ void pass_all(float *s, const wave_maps<W> &maps, const place &p) {
+    stretches all[N];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const int w = WHICH == MAP_H ? i : W - 1 - i, at = p.lane % ROW_LANES * N;
+        const f32x2 A = *(const f32x2 *)&maps[w][MAP_A][at], B = *(const f32x2 *)&maps[w][MAP_B][at], H = *(const f32x2 *)&maps[w][WHICH][at];
+#pragma unroll
+        for (int c = 0; c < N; ++c) all[c].add(A[c], B[c], H[c]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int c = 0; c < N; ++c) s[c] = through(coefficient(all[c].A, all[c].B), all[c].H, s[c]);
 }
 
 constexpr uint64_t UNTOLD = ~(uint64_t)0;
@@ -278,17 +302,14 @@ __device__ __forceinline__ uint64_t *map_at(const params &a, int64_t b, int orde
 template <int WHICH, int MODE, int W> __device__ __forceinline__ void tell(const params &a, const place &p, int order, const wave_maps<W> &maps) {
     static_assert(CG == 64, "a channel a lane");
     stretches all;
-    float H = 0.f;
 #pragma unroll
     for (int i = 0; i < W; ++i) {
         const int w = WHICH == MAP_H ? i : W - 1 - i;
-        const float C = maps[w][MAP_C][p.lane];
-        H = maps[w][MAP_A][p.lane] * H + maps[w][WHICH][p.lane];
-        all.add(C);
+        all.add(maps[w][MAP_A][p.lane], maps[w][MAP_B][p.lane], maps[w][WHICH][p.lane]);
     }
     const float C = coefficient(all.A, all.B);
     const uint32_t x = C != C ? 0x7fc00000u : __float_as_uint(C);  // (some NaN is all ones)
-    __hip_atomic_store(map_at(a, p.b, order, first_of<MODE>(a, p.group, p.lane / N), p.lane % N), (uint64_t)__float_as_uint(H) << 32 | x, __ATOMIC_RELAXED,
+    __hip_atomic_store(map_at(a, p.b, order, first_of<MODE>(a, p.group, p.lane / N), p.lane % N), (uint64_t)__float_as_uint(all.H) << 32 | x, __ATOMIC_RELAXED,
                        __HIP_MEMORY_SCOPE_AGENT);
 }
 
@@ -297,7 +318,6 @@ template <int WHICH, int MODE, int W> __device__ __forceinline__ void tell(const
 template <int W> __device__ __forceinline__ void through_earlier(float *s, const params &a, const place &p, int order, wave_maps<W> &maps) {
     const int each = (order + W * STRIPS - 1) / (W * STRIPS), first = (p.wave * STRIPS + p.lane / ROW_LANES) * each;
     stretches before[N];
-    float H[N] = {};
     for (int i = first; i < min(first + each, order); ++i) {
         uint64_t x[N];
         for (;;) {
@@ -313,19 +333,24 @@ template <int W> __device__ __forceinline__ void through_earlier(float *s, const
 #pragma unroll
         for (int c = 0; c < N; ++c) {
             const float mine = __uint_as_float((uint32_t)x[c]);
-            H[c] = through(mine, __uint_as_float((uint32_t)(x[c] >> 32)), H[c]);
-            before[c].add(mine);
+            const float H = through(mine, __uint_as_float((uint32_t)(x[c] >> 32)), before[c].H);  // (of any number of stretches)
+            before[c].add(whole(mine), complement(mine), 0.f);
+            before[c].H = H;
         }
     }
-    float none = 0.f;
 #pragma unroll
     for (int c = 0; c < N; ++c) {
-        float C = coefficient(before[c].A, before[c].B);
-        join<true, false>(C, H[c], none, none, none, none, none, p.lane);
-        if (p.lane < ROW_LANES) maps[p.wave][MAP_C][p.lane * N + c] = C, maps[p.wave][MAP_H][p.lane * N + c] = H[c];
+        stretches both, later;
+        halves(before[c].A, both.A, later.A), halves(before[c].B, both.B, later.B), halves(before[c].H, both.H, later.H);
+        both.add(later.A, later.B, later.H);
+        if (p.lane < ROW_LANES) {
+            maps[p.wave][MAP_A][p.lane * N + c] = both.A;
+            maps[p.wave][MAP_B][p.lane * N + c] = both.B;
+            maps[p.wave][MAP_H][p.lane * N + c] = both.H;
+        }
     }
     __syncthreads();
-    for (int w = 0; w < W; ++w) pass<MAP_C, MAP_H, W>(s, maps, w, p);
+    pass_all<MAP_H, W>(s, maps, p);
 }
 
 // Steps behind the last one: a = 1 and nothing added, by gates of infinity and values of 0.
@@ -369,21 +394,19 @@ template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__
     float ga[R][N], gx[R][N], before_A[N], before_H[N];
 #pragma unroll
     for (int c = 0; c < N; ++c) {
-        float A = 1.f, B = 0.f, H = 0.f, none = 0.f;
+        float q = 0.f, A, B, H = 0.f, none = 0.f;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float gb;
-            gates<T>(get(g[r], c), ga[r][c], gb);
+            float gb, t;
+            gates<T>(get(g[r], c), ga[r][c], gb, t);
             gx[r][c] = gb * get(x[r], c);
-            A *= ga[r][c];
-            B = ga[r][c] * B + gb;  // 1 - A
+            q = (1.f + t) * q + t;
             H = ga[r][c] * H + gx[r][c];
         }
-        float C = coefficient(A, B);
-        join<true, false>(C, H, none, before_A[c], before_H[c], none, none, p.lane);
+        join<true, false>(q, A, B, H, none, before_A[c], before_H[c], none, none, p.lane);
         if (p.lane < ROW_LANES) {
-            maps[p.wave][MAP_A][p.lane * N + c] = whole(C);
-            maps[p.wave][MAP_C][p.lane * N + c] = C;
+            maps[p.wave][MAP_A][p.lane * N + c] = A;
+            maps[p.wave][MAP_B][p.lane * N + c] = B;
             maps[p.wave][MAP_H][p.lane * N + c] = H;
         }
         __builtin_amdgcn_sched_barrier(0);  // one channel after another: together they take registers that waves could have
@@ -398,12 +421,11 @@ template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__
 #pragma unroll
     for (int c = 0; c < N; ++c) s[c] = carry[c];
     if (p.wave == 0 && tile == a.tiles - 1) {
-#pragma unroll
-        for (int w = 0; w < W; ++w) pass<MAP_C, MAP_H, W>(carry, maps, w, p);
+        pass_all<MAP_H, W>(carry, maps, p);
     } else {
 #pragma unroll
         for (int w = 0; w < W - 1; ++w)
-            if (w < p.wave) pass<MAP_A, MAP_H, W>(s, maps, w, p);
+            if (w < p.wave) pass<MAP_H, W>(s, maps, w, p);
     }
 #pragma unroll
     for (int c = 0; c < N; ++c) s[c] = before_A[c] * s[c] + before_H[c];
@@ -469,22 +491,20 @@ template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__
     float before_A[N], before_H[N], behind_A[N], behind_E[N];
 #pragma unroll
     for (int c = 0; c < N; ++c) {
-        float A = 1.f, B = 0.f, H = 0.f, E = 0.f, ga[R];
+        float q = 0.f, A, B, H = 0.f, E = 0.f, ga[R];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float gb;
-            gates<T>(get(g[r], c), ga[r], gb);
-            A *= ga[r];
-            B = ga[r] * B + gb;
+            float gb, t;
+            gates<T>(get(g[r], c), ga[r], gb, t);
+            q = (1.f + t) * q + t;
             H = ga[r] * H + gb * get(x[r], c);
         }
 #pragma unroll
         for (int r = R - 1; r >= 0; --r) E = ga[r] * E + ga[r] * get(dh[r], c);
-        float C = coefficient(A, B);
-        join<true, true>(C, H, E, before_A[c], before_H[c], behind_A[c], behind_E[c], p.lane);
+        join<true, true>(q, A, B, H, E, before_A[c], before_H[c], behind_A[c], behind_E[c], p.lane);
         if (p.lane < ROW_LANES) {
-            maps[p.wave][MAP_A][p.lane * N + c] = whole(C);
-            maps[p.wave][MAP_C][p.lane * N + c] = C;
+            maps[p.wave][MAP_A][p.lane * N + c] = A;
+            maps[p.wave][MAP_B][p.lane * N + c] = B;
             maps[p.wave][MAP_H][p.lane * N + c] = H;
             maps[p.wave][MAP_E][p.lane * N + c] = E;
         }
@@ -496,24 +516,15 @@ template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__
         if (order > 0) through_earlier<W>(carry, a, p, order, lds[SHARED ? 1 : 0]);
     }
     float e[N];
-    if (p.wave == 0 && tile == 0) {
 #pragma unroll
-        for (int w = W - 1; w >= 0; --w) {
-            if (w == 0)
+    for (int c = 0; c < N; ++c) e[c] = carry[c];
 #pragma unroll
-                for (int c = 0; c < N; ++c) e[c] = carry[c];
-            pass<MAP_C, MAP_E, W>(carry, maps, w, p);
-        }
-    } else {
-#pragma unroll
-        for (int c = 0; c < N; ++c) e[c] = carry[c];
-#pragma unroll
-        for (int w = W - 1; w > 0; --w)
-            if (w > p.wave) pass<MAP_A, MAP_E, W>(e, maps, w, p);
-    }
+    for (int w = W - 1; w > 0; --w)
+        if (w > p.wave) pass<MAP_E, W>(e, maps, w, p);
 #pragma unroll
     for (int w = 0; w < W - 1; ++w)
-        if (w < p.wave) pass<MAP_A, MAP_H, W>(s, maps, w, p);
+        if (w < p.wave) pass<MAP_H, W>(s, maps, w, p);
+    if (p.wave == 0 && tile == 0) pass_all<MAP_E, W>(carry, maps, p);
     // the gates are computed again, channel by channel, and the gradients take the inputs' places: kept from above they would take 64 registers
 #pragma unroll
     for (int r = 0; r < R; ++r) asm("" : "+v"(g[r]), "+v"(x[r]), "+v"(dh[r]));

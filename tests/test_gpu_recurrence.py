@@ -334,10 +334,10 @@ STEADY = [-1.0, 0.0, 2.0, 5.0, 8.0, 9.1, 10.2, 11.5, 12.0, 13.3, 14.1]
 def test_steady_gates_add_nothing_up(ops, steps, dtype):
     """A state of 1, inputs of 1 and gates that stay: all states are 1, and with gradients of 1 - a each step's is 1, however long the
     sequence is.  In half units of fp32: a and b are off by less than 5 from their sum of 1 in each of a strip's sixteen steps, which go by a
-    alone; H and 1 - A differ by four at each of the 17 levels that join 129 tiles, and by 95 in a strip that forgets half (5 over 1 - a of
-    at least 1 / 20), of which as much again is left by the maps before; nine levels within a tile go by A alone, two each: 424 in all, below
-    2^-15.  The gates' own error, below
-    2^-18 for these, moves the gradients with it."""
+    alone; H and 1 - A differ by four at each of the 17 levels that join 129 tiles, by 70 in a strip (of sixteen steps, which a's error and
+    a rounding each move) and by 95 in a strip that forgets half (5 over 1 - a of at least 1 / 20), of which as much again is left by the
+    maps before; nine levels within a tile go by A alone, two each: 494 in all, below 2^-15.  The gates' own error, below 2^-18 for these,
+    moves the gradients with it."""
     print("case steady", steps, dtype, flush=True)
     gate = torch.tensor(STEADY, device=DEV).to(dtype).expand(2, steps, len(STEADY))
     x, state = torch.ones_like(gate), torch.ones(2, len(STEADY), device=DEV)
@@ -363,6 +363,20 @@ def test_steady_gates_add_nothing_up_over_calls(ops, piece):
     for _ in range(2500):
         h, state, _ = ops.recurrence(x, gate, state, keep=False)
     assert ((h.double() - 1).abs() <= 2.0 ** -15).all() and ((state.double() - 1).abs() <= 2.0 ** -15).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("steps", [2, 16, 40, 257, 700])
+def test_what_is_forgotten_stays_so(ops, steps, dtype):
+    """Gates whose products pass the smallest number that fp32 holds, and the largest of their inverses, after any number of steps: nothing is left of
+    a state, or of a gradient behind, of 10^6."""
+    print("case forgotten", steps, dtype, flush=True)
+    gate = torch.cat([-torch.logspace(0, 2, 400), torch.linspace(-5.7, -5.3, 101), torch.linspace(-45, -42, 101)]).to(DEV)
+    C = gate.numel()
+    gen = torch.Generator().manual_seed(111)
+    state, dlast = (1e6 * (1 + torch.rand(2, C, generator=gen)).to(DEV) for _ in range(2))
+    check(ops, normal(gen, (2, steps, C), dtype), gate.to(dtype).expand(2, steps, C), state, dlast=dlast)
+    check(ops, normal(gen, (2, steps, C), dtype), gate.to(dtype).expand(2, steps, C), state, [steps, steps // 2 + 1], dlast)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
