@@ -286,14 +286,6 @@ __device__ __forceinline__ int take_ticket(uint32_t *ticket) {
     return (int)__builtin_amdgcn_readfirstlane(mine);
 }
 
-// The sequence and channels of a workgroup that shares them: neighbours take neighbouring channels, and the next row of workgroups is turned
-// by one, so that an XCD (every eighth workgroup) does not keep to some channels of all rows, which a part of its cache would have to serve (1 x
-// 32768 x 512 45 us, so 34).
-__device__ __forceinline__ uint32_t turned_group(const params &a) {
-    const uint32_t all = gridDim.x / a.tiles;
-    return (blockIdx.x + blockIdx.x / all) % all;
-}
-
 // A map as one word, so that who reads it reads all of it, and needs no fence.
 __device__ __forceinline__ uint64_t *map_at(const params &a, int64_t b, int order, int col, int c) {
     return a.maps + (b * a.tiles + order) * a.width + min(col + c, a.width - 1);
@@ -373,7 +365,7 @@ template <typename T> __device__ __forceinline__ void zero_behind(raw<T> (&x)[R]
 // tiles before.
 template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W, 4) void recurrence_kernel(params a) {
     __shared__ wave_maps<W> lds[SHARED ? 2 : 1];
-    const uint32_t id = SHARED ? turned_group(a) : blockIdx.x;
+    const uint32_t id = SHARED ? blockIdx.x % (gridDim.x / a.tiles) : blockIdx.x;  // a sequence and its channels: neighbours take neighbouring ones
     const place p(a, id, std::integral_constant<int, MODE>());
     const int tile = SHARED ? take_ticket(a.tickets + id * TICKET) : 0;
     const int64_t end = length(a, p.b);
@@ -467,7 +459,7 @@ template <typename T, int MODE> __global__ __launch_bounds__(256) void recurrenc
 // As recurrence_kernel, from the last tile to the first; the states before the tile's steps come from the kept one.
 template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__(64 * W, sizeof(T) == 2 ? 4 : 2) void recurrence_backward_kernel(params a) {
     __shared__ wave_maps<W> lds[SHARED ? 2 : 1];
-    const uint32_t id = SHARED ? turned_group(a) : blockIdx.x;
+    const uint32_t id = SHARED ? blockIdx.x % (gridDim.x / a.tiles) : blockIdx.x;  // a sequence and its channels: neighbours take neighbouring ones
     const place p(a, id, std::integral_constant<int, MODE>());
     const int order = SHARED ? take_ticket(a.tickets + id * TICKET) : 0, tile = a.tiles - 1 - order;
     const int64_t end = length(a, p.b);
