@@ -176,7 +176,8 @@ int dear_add_rms_norm_backward_workspace(int32_t dtype, int64_t rows, int64_t co
  *     G[t] = dh[t] + a[t+1] * G[t+1]  (G = dlast behind the last step, as if through a = 1)
  *     dx[t] = (1 - a[t]) * G[t];  dgate[t] = G[t] * (s[t-1] - x[t]) * a[t] * (1 - a[t]);  dstate = a[0] * G[0]
  * and 0 behind the last step.  States and sums are fp32 throughout: the backward pass computes the
- * states again from those that the forward pass kept.  A NaN or an infinity stays within its sequence and channel.
+ * states again from those that the forward pass kept.  Roundings of gates near 1 do not add up along a sequence, nor over calls that
+ * continue one another.  A NaN or an infinity stays within its sequence and channel.
  */
 #define DEAR_RECURRENCE_KEPT 256 /* steps from one kept state to the next */
 
@@ -210,7 +211,7 @@ typedef struct {
     int64_t workspace_bytes;
 } dear_recurrence_t;
 
-/* Tensors are aligned to their element types (16 bytes, with strides and widths to match, are faster).
+/* Tensors are aligned to their element types (to two elements, with even strides and widths, they are faster).
  * Errors: DEAR_EINVAL, DEAR_EALIGN, DEAR_EHIP; DEAR_ETOOBIG where workspace_bytes is less than the call needs, or where a
  * launch would have 2^32 threads or more: 512 for every 64 channels of every 256 steps of a sequence. */
 int dear_recurrence(const dear_recurrence_t *args, void *hip_stream);

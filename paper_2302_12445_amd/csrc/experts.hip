@@ -7,8 +7,8 @@
 // it (w for dx, both for dw); the former are read from LDS in rows, the latter with the transposing reads.  Rows of an expert start
 // anywhere: a workgroup finds the expert of its tile from the ends, on the device, so that nothing waits for the host to know them.
 //
-// Matrix instructions bound large calls, at the clock that the card's power leaves them (16384 rows, 4096 x 1024 over 8, bf16: 1000 to 1200
-// TFLOP/s, a library's product of 8192 x 8192 x 8192 1394); the weights' way from memory bounds few rows (32: 4.5 TB/s).
+// Matrix instructions bound large calls, at the clock that the card's power leaves them (16384 uneven rows, 4096 x 1024 over 8, bf16: 980, 985 and 855
+// TFLOP/s for the three products, a library's of 8192 x 8192 x 8192 1394); the weights' way from memory bounds few rows (32: 4.5 TB/s).
 #include <type_traits>
 
 #include "experts_cut.h"

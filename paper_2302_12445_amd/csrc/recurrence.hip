@@ -6,13 +6,14 @@
 // A stretch of steps is a map s -> A s + H with A the product of its a; two stretches in a row are again one:
 // (A2 A1, A2 H1 + H2).  Backward the map is e -> A e + E with the same A, from the last step to the first.  So a tile of
 // 256 steps is cut into strips of sixteen: a lane joins its own steps, lanes and waves join theirs, and a second
-// walk over the strip, from the state before it, gives the outputs; every tensor is read once.  Where sequences and channels
-// alone do not fill the chip, each tile has a workgroup of its own, which tells the others its map and joins those of the tiles before
+// walk over the strip, from the state before it, gives the outputs; every tensor is read once.  Of sequences of several
+// tiles each tile has a workgroup of its own, which tells the others its map and joins those of the tiles before
 // it.  The backward pass needs the states before each step as well: it computes them again, in fp32, from the states that the
 // forward pass kept at each tile's first step, which takes less traffic than to read h, and no rounding.
 //
-// HBM bounds it, 6 bytes of bf16 an element forward and 10 backward, and the vector instructions come close to that: single tiles, 64 x 256 x
-// 1024 bf16, 18.4 us = 5.5 TB/s and 37.5 = 4.5; tiles that are joined, 2 x 8192 x 1024, with the launch that clears their maps 26 and 45.
+// What it reads and writes, 6 bytes of bf16 an element forward and 10 backward, and the vector instructions, which issue 64 and 72 % of the time, bound it
+// together: single tiles, 64 x 256 x 1024 bf16, 18.6 and 32.7 us, where 15 and 25 are what a large copy would take (calls in a row find about half
+// of it in the last cache); tiles that are joined, 2 x 8192 x 1024, with the launch that clears their maps 25.5 and 40.1.
 #include <cfloat>
 #include <type_traits>
 
@@ -52,8 +53,8 @@ struct params {
 
 // a = sigmoid(g) and b = 1 - a: with t = exp(-g) they are 1 / (1 + t) and t / (1 + t).  exp2's argument y is rounded, by |g| 2^-24 and more, which
 // is an error of t's.  Of fp32 gates, t is mended by what y leaves of -g, so that a and b are right to 8 units of 2^-24 (exp2 and the reciprocal 2 each,
-// four roundings); where gates are bf16 that would cost 5 % of the time (2 x 8192 x 1024 forward 29.2 us, so 30.6, of fp32 56.5 and 57.4), and results of
-// bf16 are rounded by 2^15 units.  Where fp32 has no more: below gates of -87.3, where t stops so that 1 + t has a reciprocal, a is some 2^-126, and above
+// four roundings); where gates are bf16 that would cost 4 to 5 % of the time (64 x 256 x 1024 18.6 us, so 19.4, backward 32.7 and 34.4; of fp32 gates less than 1), and
+// results of bf16 are rounded by 2^15 units.  Where fp32 has no more: below gates of -87.3, where t stops so that 1 + t has a reciprocal, a is some 2^-126, and above
 // 87.3 b may be 0.  A NaN stays one.
 template <typename T> __device__ __forceinline__ void gates(float g, float &a, float &b, float &t) {
     if (sizeof(T) == 4) {
@@ -82,7 +83,7 @@ __device__ __forceinline__ void halves(float x, float &earlier, float &later) {
 // What a map keeps of the state, A, is told on as one number C: A itself below a half, from there on -(1 - A), with the sign, by which the state
 // goes on as s + (H - (1 - A) s).  An A near 1 that is rounded by itself is wrong by the same 2^-25 each time that a gate stays, which adds up over
 // all that a channel remembers, to 2^-25 / (1 - a) (of fp32 steps with a gate of 9, 4e-4); by C the state goes to where H and 1 - A say, however
-// long the sequence is.  So go states from tile to tile and from call to call (2 x 8192 x 1024 bf16 forward 27.5 us, so 28.4); within a tile, from a
+// long the sequence is.  So go states from tile to tile and from call to call (2 x 8192 x 1024 bf16 forward 27.1 us, so 27.9); within a tile, from a
 // state that is at hand, they go by A.  -0 leaves a state as it is.
 __device__ __forceinline__ float coefficient(float A, float B) { return B <= 0.5f ? -B : A; }
 __device__ __forceinline__ bool by_complement(float C) { return (int32_t)__float_as_uint(C) < 0; }
@@ -432,8 +433,8 @@ template <typename T, int W, int MODE, bool SHARED> __global__ __launch_bounds__
     if (speaks && a.last && tile == a.tiles - 1) store_state<MODE>(a.last + p.b * a.width, carry, p.col, a.width);
 }
 
-// One step, as of sequences that are continued token by token: a lane has two channels of a sequence, and nothing to join (16 x 1 x 1024 bf16 2.2
-// us, 256 x 1 x 1024 2.5; by the kernel above, whose lanes have sixteen steps, 3.7 and 7.0).
+// One step, as of sequences that are continued token by token: a lane has two channels of a sequence, and nothing to join (of launches in a row 16 x 1
+// x 1024 bf16 2.3 us, 256 x 1 x 1024 2.6; by the kernel above, whose lanes have sixteen steps, 3.9 and 7.4).
 template <typename T, int MODE> __global__ __launch_bounds__(256) void recurrence_step_kernel(params a, uint32_t pairs, uint32_t all) {
     const uint32_t i = blockIdx.x * 256 + threadIdx.x;
     if (i >= all) return;
@@ -658,8 +659,8 @@ template <typename T, int MODE, bool BACKWARD> void launch(params a, int64_t bat
         const int64_t pairs = ceil_div(a.width, N), all = batch * pairs;
         recurrence_step_kernel<T, MODE><<<(unsigned)ceil_div(all, 256), 256, 0, stream>>>(a, (uint32_t)pairs, (uint32_t)all);
     } else {
-        // waves that no step would fill take time all the same: 256 x 32 x 1024 bf16 10.7 us with one, 18 with three, 40 with eight; 128 x 128 x 1024
-        // 18.7 with four, 25.6 with eight; 64 x 192 x 1024 18.2 with six, 17.5 with eight
+        // waves that no step would fill take time all the same: 256 x 32 x 1024 bf16 11.3 us with one, 18 with three, 40 with eight; 128 x 128 x 1024
+        // 19.1 with four, 26.1 with eight; 64 x 192 x 1024 18.2 with six, 17.8 with eight
         const int64_t waves = ceil_div(a.steps, WAVE_STEPS);
         if (waves <= 1) by_waves(std::integral_constant<int, 1>());
         else if (waves <= 2) by_waves(std::integral_constant<int, 2>());

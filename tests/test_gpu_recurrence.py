@@ -80,7 +80,7 @@ def test_recurrence(ops, shape, dtype):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("shape", [(513, 300, 6), (65, 600, 520), (600, 40, 64), (530, 80, 33)])
 def test_sequences_that_fill_the_chip(ops, shape, dtype):
-    """Workgroups that take a sequence's tiles one after another."""
+    """More workgroups than the chip takes at a time, of one tile and of several."""
     print("case", shape, dtype, flush=True)
     x, gate, state = inputs(shape, dtype, sum(shape))
     lens = torch.randint(0, shape[1] + 1, (shape[0],), generator=torch.Generator().manual_seed(1)).tolist()
