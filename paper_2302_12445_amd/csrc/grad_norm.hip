@@ -194,7 +194,7 @@ __global__ __launch_bounds__(THREADS) void scale_kernel(const table t, const ent
             else scale((const bf16 *)e.in + first, (bf16 *)e.out + first, count, by);
         });
     };
-    if (by < 0x1p-126) scale_all(by);
+    if (by > 0. && by < 0x1p-126) scale_all(by);  // (0 is that of an infinite norm, as steps that overflow have)
     else scale_all((float)by);
 }
 
